@@ -336,6 +336,121 @@ pf_status proxy_segments_bwd(const pf_layer_desc *desc, int32_t n_seg, const pf_
                              const pf_layer_grads *grads, const pf_segment_grads *seg_grads,
                              void *ws, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Attention of the local stream (the local Transformer that Sec. 3.5 leaves to
+ * the user after the injection, and the self-attention of the generation side
+ * of Sec. 3.7 for many requests): norm and rotation of queries and keys, a
+ * paged cache of keys and values and the attention of a new token over it.
+ * Buffers as everywhere; rows of a matrix may lie further apart than their
+ * width (leading dimensions ld_* in elements, multiples of 16 bytes), heads of
+ * a row one after the other, head h at column h*dh.                           */
+
+/* Rows of queries [., n_heads*dh], keys and values [., n_kv*dh].             */
+typedef struct {
+  void *q, *k, *v;
+  int64_t ld_q, ld_k, ld_v;
+} pf_qkv;
+
+/* Norm and rotation of queries and keys.
+ *   n_heads, n_kv : query heads and key (and value) heads
+ *   dh            : head width, 64 or 128
+ *   dtype         : PF_BF16 or PF_F32 (the paged cache: PF_BF16)
+ *   n_axes, pairs : position axes (0 to 3; 0: no rotation) and the pairs
+ *                   (2j, 2j+1) of a head that each turns, one axis after the
+ *                   other; at most dh/2 in total, the rest is not turned
+ *   theta, eps    : base of the rotation's frequencies, and the norm's epsilon
+ *                   (both > 0)                                               */
+typedef struct {
+  int32_t n_heads, n_kv, dh, dtype;
+  int32_t n_axes, pairs[3];
+  double theta, eps;
+} pf_qk_desc;
+
+/* Every query and key head x of `rows` rows (dh values):
+ *   y = w x / sqrt(mean(x^2) + eps)          (w_q, w_k [dh] fp32; NULL: y = x)
+ *   pair i of axis a's pairs[a] turned by the angle pos_a * theta^(-i/pairs[a])
+ * pos [rows, n_axes] int32, or NULL with at most one axis: the row's place in
+ * its sequence, row mod seq_len.  out->q, out->k are written (v is not used)
+ * and may be x->q, x->k themselves (same leading dimension) but not overlap
+ * them otherwise.  The angle is exact for every int32 position: frequencies
+ * are kept as 64-bit fractions of a turn.                                    */
+pf_status pf_qk_rope_fwd(const pf_qk_desc *desc, int64_t rows, int64_t seq_len, const pf_qkv *x,
+                         const float *w_q, const float *w_k, const int32_t *pos,
+                         const pf_qkv *out, void *stream);
+
+size_t pf_qk_rope_workspace_size(const pf_qk_desc *desc);
+
+/* Its backward: dx from the gradients dout of out, and the norms' gradients
+ * dw_q, dw_k [dh] fp32 (overwritten; NULL where w_q, w_k is NULL, or where not
+ * wanted).  x: the forward's input (of a head without norm it is not read).
+ * dx->q, dx->k may be dout->q, dout->k.  ws: pf_qk_rope_workspace_size bytes,
+ * may be NULL without dw_q and dw_k.                                         */
+pf_status pf_qk_rope_bwd(const pf_qk_desc *desc, int64_t rows, int64_t seq_len, const pf_qkv *x,
+                         const float *w_q, const float *w_k, const int32_t *pos,
+                         const pf_qkv *dout, const pf_qkv *dx, float *dw_q, float *dw_k, void *ws,
+                         size_t ws_bytes, void *stream);
+
+/* Paged cache of one layer's keys and values (bf16).
+ *   batch     : sequences, at most 2048
+ *   n_heads, n_kv, dh : as above; at most 16 query heads to a key head
+ *   page      : rows of a page, a multiple of 16
+ *   max_pages : entries of a sequence's page table
+ *   n_pages   : pages of the pool
+ *   window, n_sink : what a token sees: every row (window 0), or the last
+ *               `window` rows, itself among them, and the first n_sink       */
+typedef struct {
+  int32_t batch, n_heads, n_kv, dh;
+  int32_t page, max_pages;
+  int64_t n_pages;
+  int32_t window, n_sink;
+} pf_paged_desc;
+
+/* Device memory of the caller; table and len serve the caches of all layers.
+ *   K, V  [n_pages, n_kv, page, dh] bf16
+ *   table [batch, max_pages] int32: row r of sequence b lies on page
+ *         table[b, r / page].  Entries of pages that no call reaches (past the
+ *         end, or before the window and past the sinks) are not read
+ *   len   [batch] int32: rows of every sequence, those of the current step
+ *         included (pf_paged_advance)                                        */
+typedef struct {
+  void *K, *V;
+  const int32_t *table;
+  int32_t *len;
+} pf_paged_cache;
+
+/* Start of a step: len[b] += start[b+1] - start[b], or 1 where start is NULL.
+ * A sequence whose table would not hold its rows stays as it is and is flagged
+ * (PF_ERR_CAPACITY via pf_sync_check).                                       */
+pf_status pf_paged_advance(const pf_paged_desc *desc, const int32_t *start, pf_paged_cache *cache,
+                           void *stream);
+
+/* Keys and values of `rows` new tokens into the cache, whose len already counts
+ * them.  Tokens start[b] .. start[b+1] of x (start [batch+1] int32, device,
+ * start[0] = 0, start[batch] = rows) are the last of sequence b; start NULL:
+ * one token for each sequence, rows = batch.  Keys are normed and rotated on
+ * the way as in pf_qk_rope_fwd, at the token's row in the sequence or, given,
+ * at pos [rows, n_axes]; values are copied.  q_out [rows, n_heads*dh]: the
+ * queries, normed and rotated (x->q and q_out may be NULL; q_out may be x->q).
+ * qk: norm and rotation; its heads must be desc's.  A token whose row or page
+ * is out of range is left out and flagged (PF_ERR_CAPACITY via pf_sync_check).
+ */
+pf_status pf_paged_append(const pf_paged_desc *desc, const pf_qk_desc *qk, int64_t rows,
+                          const pf_qkv *x, const float *w_q, const float *w_k,
+                          const int32_t *start, const int32_t *pos, pf_paged_cache *cache,
+                          void *q_out, int64_t ld_q_out, void *stream);
+
+size_t pf_paged_attn_workspace_size(const pf_paged_desc *desc);
+
+/* Attention of every sequence's newest token, with queries q [batch,
+ * n_heads*dh] (leading dimension ld_q), over the rows that it sees:
+ *   out_h = softmax(q_h K^T / sqrt(dh)) V,   key head h / (n_heads/n_kv).
+ * A sequence without rows gives zeros.  A length or page out of range is
+ * flagged (PF_ERR_CAPACITY via pf_sync_check); such rows are not read.  The
+ * lengths stay on the device, so that a captured graph serves every step.    */
+pf_status pf_paged_attn(const pf_paged_desc *desc, const void *q, int64_t ld_q,
+                        const pf_paged_cache *cache, void *out, int64_t ld_out, void *ws,
+                        size_t ws_bytes, void *stream);
+
 /* Thread-local message describing the last non-OK status of this thread. */
 const char *pf_last_error(void);
 

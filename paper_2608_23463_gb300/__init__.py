@@ -81,12 +81,31 @@ class AppendParams(ctypes.Structure):
     _fields_ = [(n, _vp) for n in ("W_c1", "b_c1", "W_c2", "b_c2", "W_kvh")]
 
 
+class QKV(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in "qkv"] + [(f"ld_{n}", ctypes.c_int64) for n in "qkv"]
+
+
+class QKDesc(ctypes.Structure):
+    _fields_ = ([(n, _c_i32) for n in ("n_heads", "n_kv", "dh", "dtype", "n_axes")]
+                + [("pairs", _c_i32 * 3), ("theta", ctypes.c_double), ("eps", ctypes.c_double)])
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = ([(n, _c_i32) for n in ("batch", "n_heads", "n_kv", "dh", "page", "max_pages")]
+                + [("n_pages", ctypes.c_int64), ("window", _c_i32), ("n_sink", _c_i32)])
+
+
+class PagedCache(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("K", "V", "table", "len")]
+
+
 EXPORTED = ("proxy_layer_check", "proxy_layer_saved_size", "proxy_layer_workspace_size",
             "proxy_layer_fwd", "proxy_layer_bwd", "proxy_decode_workspace_size",
             "proxy_decode_step", "proxy_append_workspace_size", "proxy_kv_append",
             "proxy_prefill_workspace_size", "proxy_kv_prefill", "proxy_layer_prefill",
             "proxy_segments_saved_size", "proxy_segments_workspace_size", "proxy_segments_fwd",
-            "proxy_segments_bwd",
+            "proxy_segments_bwd", "pf_qk_rope_fwd", "pf_qk_rope_workspace_size", "pf_qk_rope_bwd",
+            "pf_paged_advance", "pf_paged_append", "pf_paged_attn_workspace_size", "pf_paged_attn",
             "pf_last_error", "pf_sync_check", "pf_gemm_bf16", "pf_timing_enable",
             "pf_timing_collect", "pf_timing_label", "pf_timing_ms", "pf_timing_launches",
             "pf_timing_flops", "pf_timing_bytes", "proxy_layer_bwd_noalloc",
@@ -148,6 +167,23 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                        P(SegmentParams), _vp, _vp, _vp, _vp, P(LayerGrads),
                                        P(SegmentParams), _vp, sz, _vp]
     lib.proxy_segments_bwd.restype = ctypes.c_int
+    i64 = ctypes.c_int64
+    lib.pf_qk_rope_fwd.argtypes = [P(QKDesc), i64, i64, P(QKV), _vp, _vp, _vp, P(QKV), _vp]
+    lib.pf_qk_rope_fwd.restype = ctypes.c_int
+    lib.pf_qk_rope_workspace_size.argtypes = [P(QKDesc)]
+    lib.pf_qk_rope_workspace_size.restype = sz
+    lib.pf_qk_rope_bwd.argtypes = [P(QKDesc), i64, i64, P(QKV), _vp, _vp, _vp, P(QKV), P(QKV), _vp,
+                                   _vp, _vp, sz, _vp]
+    lib.pf_qk_rope_bwd.restype = ctypes.c_int
+    lib.pf_paged_advance.argtypes = [P(PagedDesc), _vp, P(PagedCache), _vp]
+    lib.pf_paged_advance.restype = ctypes.c_int
+    lib.pf_paged_append.argtypes = [P(PagedDesc), P(QKDesc), i64, P(QKV), _vp, _vp, _vp, _vp,
+                                    P(PagedCache), _vp, i64, _vp]
+    lib.pf_paged_append.restype = ctypes.c_int
+    lib.pf_paged_attn_workspace_size.argtypes = [P(PagedDesc)]
+    lib.pf_paged_attn_workspace_size.restype = sz
+    lib.pf_paged_attn.argtypes = [P(PagedDesc), _vp, i64, P(PagedCache), _vp, i64, _vp, sz, _vp]
+    lib.pf_paged_attn.restype = ctypes.c_int
     lib.pf_last_error.argtypes = []
     lib.pf_last_error.restype = ctypes.c_char_p
     lib.pf_sync_check.argtypes = [_vp]
@@ -319,6 +355,48 @@ def proxy_segments_bwd(desc, segs, shared, seg_params, X, saved, dX_out, dX, gra
                                      seg_params, _ptr(X), _ptr(saved), _ptr(dX_out), _ptr(dX),
                                      ctypes.byref(grads), seg_grads, _ptr(ws), int(ws_bytes),
                                      stream))
+
+
+def qkv(q=None, k=None, v=None) -> QKV:
+    """pf_qkv of 2D tensors (their row strides are the leading dimensions)."""
+    ld = lambda t: 0 if t is None else int(t.stride(0))
+    return QKV(_ptr(q), _ptr(k), _ptr(v), ld(q), ld(k), ld(v))
+
+
+def pf_qk_rope_fwd(desc, rows, seq_len, x, w_q, w_k, pos, out, stream=None):
+    _check(load().pf_qk_rope_fwd(ctypes.byref(desc), int(rows), int(seq_len), ctypes.byref(x),
+                                 _ptr(w_q), _ptr(w_k), _ptr(pos), ctypes.byref(out), stream))
+
+
+def pf_qk_rope_workspace_size(desc) -> int:
+    return load().pf_qk_rope_workspace_size(ctypes.byref(desc))
+
+
+def pf_qk_rope_bwd(desc, rows, seq_len, x, w_q, w_k, pos, dout, dx, dw_q, dw_k, ws, ws_bytes,
+                   stream=None):
+    _check(load().pf_qk_rope_bwd(ctypes.byref(desc), int(rows), int(seq_len), ctypes.byref(x),
+                                 _ptr(w_q), _ptr(w_k), _ptr(pos), ctypes.byref(dout),
+                                 ctypes.byref(dx), _ptr(dw_q), _ptr(dw_k), _ptr(ws), int(ws_bytes),
+                                 stream))
+
+
+def pf_paged_advance(desc, start, cache, stream=None):
+    _check(load().pf_paged_advance(ctypes.byref(desc), _ptr(start), ctypes.byref(cache), stream))
+
+
+def pf_paged_append(desc, qk, rows, x, w_q, w_k, start, pos, cache, q_out, ld_q_out, stream=None):
+    _check(load().pf_paged_append(ctypes.byref(desc), ctypes.byref(qk), int(rows), ctypes.byref(x),
+                                  _ptr(w_q), _ptr(w_k), _ptr(start), _ptr(pos),
+                                  ctypes.byref(cache), _ptr(q_out), int(ld_q_out), stream))
+
+
+def pf_paged_attn_workspace_size(desc) -> int:
+    return load().pf_paged_attn_workspace_size(ctypes.byref(desc))
+
+
+def pf_paged_attn(desc, q, ld_q, cache, out, ld_out, ws, ws_bytes, stream=None):
+    _check(load().pf_paged_attn(ctypes.byref(desc), _ptr(q), int(ld_q), ctypes.byref(cache),
+                                _ptr(out), int(ld_out), _ptr(ws), int(ws_bytes), stream))
 
 
 def pf_sync_check(stream=None) -> None:

@@ -1,0 +1,53 @@
+// Internal launch interface of the local stream's attention operators
+// (local_api.cu checks the arguments, the kernels are in local_rope.cu,
+// paged_attn.cu, window_attn.cu and window_attn_bwd.cu).
+#pragma once
+
+#include "kernels.h"
+
+namespace pf {
+
+// Rows of three matrices, leading dimensions in elements (of bf16 or fp32).
+struct QkvPtr {
+  void *q, *k, *v;
+  long ldq, ldk, ldv;
+};
+
+struct QkRope {
+  int H, KV, dh, f32, n_axes, pairs[3];
+  double theta, eps;
+};
+
+struct Paged {
+  int B, H, KV, dh, page, max_pages;
+  long n_pages;
+  int window, sinks;
+  bf16 *K, *V;  // [n_pages, KV, page, dh]
+  const int *table, *len;
+};
+
+cudaError_t qk_rope_fwd(const QkRope& s, const QkvPtr& x, const QkvPtr& o, const float* w_q,
+                        const float* w_k, const int* pos, long rows, long seq_len,
+                        cudaStream_t st);
+// part: qk_rope_part_bytes(dh), read and written only with dw_q or dw_k.
+size_t qk_rope_part_bytes(int dh);
+cudaError_t qk_rope_bwd(const QkRope& s, const QkvPtr& x, const QkvPtr& dout, const QkvPtr& dx,
+                        const float* w_q, const float* w_k, const int* pos, float* dw_q,
+                        float* dw_k, float* part, long rows, long seq_len, cudaStream_t st);
+cudaError_t paged_append(const QkRope& s, const Paged& c, const QkvPtr& x, bf16* q_out, long ldqo,
+                         const float* w_q, const float* w_k, const int* start, const int* pos,
+                         long rows, cudaStream_t st);
+cudaError_t paged_advance(const Paged& c, const int* start, int* len, cudaStream_t st);
+
+#define PF_PAGED_MAX_BATCH 2048  // sequences of a call
+#define PF_PAGED_ROWS 16         // a page holds a multiple of so many rows
+size_t paged_attn_ws_bytes(const Paged& c);
+cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long ldo, float* ws,
+                       cudaStream_t st);
+
+int take_dev_error_local_rope();
+int take_dev_error_paged_attn();
+int set_wait_limit_local_rope(unsigned long long ns);
+int set_wait_limit_paged_attn(unsigned long long ns);
+
+}  // namespace pf

@@ -1,0 +1,238 @@
+// C ABI of the local stream's attention operators (include/proxyformer.h):
+// argument validation and the launches.
+#include <stdarg.h>
+#include <stdio.h>
+
+#include "local.h"
+#include "proxyformer.h"
+
+using namespace pf;
+
+pf_status pf_set_error(pf_status s, const char* msg);
+
+namespace {
+
+pf_status fail(pf_status s, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  return pf_set_error(s, buf);
+}
+
+#define PF_CUDA(call)                                                                 \
+  do {                                                                                \
+    cudaError_t e_ = (call);                                                          \
+    if (e_ != cudaSuccess) return fail(PF_ERR_CUDA, "%s: %s", #call, cudaGetErrorString(e_)); \
+  } while (0)
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Rows of a matrix: present, aligned, wide enough.
+pf_status check_rows(const char* name, const void* p, int64_t ld, int64_t width, int size) {
+  if (!p || !aligned16(p)) return fail(PF_ERR_INVALID_ARG, "%s is required, 16-byte aligned", name);
+  if (ld < width || ld * size % 16 != 0 || ld > (int64_t(1) << 31))
+    return fail(PF_ERR_INVALID_ARG, "%s: leading dimension %lld, needs at least %lld and whole 16 bytes",
+                name, (long long)ld, (long long)width);
+  return PF_OK;
+}
+
+#define PF_TRY(call)                     \
+  do {                                   \
+    pf_status s_ = (call);               \
+    if (s_ != PF_OK) return s_;          \
+  } while (0)
+
+pf_status check_heads(int32_t H, int32_t KV, int32_t dh) {
+  if (H < 1 || KV < 1 || H % KV != 0 || H > 65535)
+    return fail(PF_ERR_INVALID_ARG, "n_heads must be a positive multiple of n_kv");
+  if (dh != 64 && dh != 128) return fail(PF_ERR_UNSUPPORTED, "head width must be 64 or 128");
+  return PF_OK;
+}
+
+pf_status check_qk(const pf_qk_desc* s) {
+  if (!s) return fail(PF_ERR_INVALID_ARG, "qk descriptor is NULL");
+  PF_TRY(check_heads(s->n_heads, s->n_kv, s->dh));
+  if (s->dtype != PF_BF16 && s->dtype != PF_F32)
+    return fail(PF_ERR_INVALID_ARG, "dtype must be PF_BF16 or PF_F32");
+  if (s->n_axes < 0 || s->n_axes > 3) return fail(PF_ERR_INVALID_ARG, "n_axes must be in [0, 3]");
+  int64_t p = 0;
+  for (int i = 0; i < s->n_axes; ++i) {
+    if (s->pairs[i] < 0) return fail(PF_ERR_INVALID_ARG, "pairs must not be negative");
+    p += s->pairs[i];
+  }
+  if (p > s->dh / 2) return fail(PF_ERR_INVALID_ARG, "more pairs than the head holds");
+  if (!(s->theta > 0) || !(s->eps > 0) || s->theta > 1e300)
+    return fail(PF_ERR_INVALID_ARG, "theta and eps must be positive");
+  return PF_OK;
+}
+
+QkRope rope_of(const pf_qk_desc& s) {
+  QkRope r{s.n_heads, s.n_kv, s.dh, s.dtype == PF_F32, s.n_axes, {0, 0, 0}, s.theta, s.eps};
+  for (int i = 0; i < s.n_axes; ++i) r.pairs[i] = s.pairs[i];
+  return r;
+}
+
+QkvPtr ptr_of(const pf_qkv& x) {
+  return {x.q, x.k, x.v, (long)x.ld_q, (long)x.ld_k, (long)x.ld_v};
+}
+
+pf_status check_qk_rows(const char* what, const pf_qkv* x, const pf_qk_desc& s) {
+  if (!x) return fail(PF_ERR_INVALID_ARG, "%s is NULL", what);
+  const int size = s.dtype == PF_F32 ? 4 : 2;
+  PF_TRY(check_rows("q", x->q, x->ld_q, (int64_t)s.n_heads * s.dh, size));
+  return check_rows("k", x->k, x->ld_k, (int64_t)s.n_kv * s.dh, size);
+}
+
+pf_status check_count(int64_t rows, int64_t seq_len, const int32_t* pos, int n_axes) {
+  if (rows < 0 || rows > 0x7fffffff) return fail(PF_ERR_INVALID_ARG, "rows must be in [0, 2^31)");
+  if (!pos && n_axes > 1) return fail(PF_ERR_INVALID_ARG, "several axes need positions");
+  if (!pos && (seq_len < 1 || seq_len > 0x7fffffff))
+    return fail(PF_ERR_INVALID_ARG, "seq_len must be in [1, 2^31)");
+  return PF_OK;
+}
+
+pf_status check_paged(const pf_paged_desc* s) {
+  if (!s) return fail(PF_ERR_INVALID_ARG, "paged descriptor is NULL");
+  if (s->batch < 1) return fail(PF_ERR_INVALID_ARG, "batch must be >= 1");
+  if (s->batch > PF_PAGED_MAX_BATCH)
+    return fail(PF_ERR_UNSUPPORTED, "at most %d sequences", PF_PAGED_MAX_BATCH);
+  PF_TRY(check_heads(s->n_heads, s->n_kv, s->dh));
+  if (s->n_heads / s->n_kv > 16)
+    return fail(PF_ERR_UNSUPPORTED, "at most 16 query heads to a key head");
+  if (s->page < PF_PAGED_ROWS || s->page % PF_PAGED_ROWS != 0)
+    return fail(PF_ERR_INVALID_ARG, "page must be a multiple of %d", PF_PAGED_ROWS);
+  if (s->max_pages < 1 || s->n_pages < 1 || s->n_pages > 0x7fffffff)
+    return fail(PF_ERR_INVALID_ARG, "max_pages and n_pages must be positive");
+  if (s->window < 0 || s->n_sink < 0)
+    return fail(PF_ERR_INVALID_ARG, "window and n_sink must not be negative");
+  return PF_OK;
+}
+
+pf_status check_cache(const pf_paged_cache* c) {
+  if (!c || !c->K || !c->V || !c->table || !c->len || !aligned16(c->K) || !aligned16(c->V))
+    return fail(PF_ERR_INVALID_ARG, "K, V (16-byte aligned), table and len are required");
+  return PF_OK;
+}
+
+Paged paged_of(const pf_paged_desc& s, const pf_paged_cache* c) {
+  Paged p{s.batch, s.n_heads, s.n_kv, s.dh, s.page, s.max_pages, (long)s.n_pages, s.window, s.n_sink,
+          nullptr, nullptr, nullptr, nullptr};
+  if (c) {
+    p.K = static_cast<bf16*>(c->K);
+    p.V = static_cast<bf16*>(c->V);
+    p.table = c->table;
+    p.len = c->len;
+  }
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+pf_status pf_qk_rope_fwd(const pf_qk_desc* desc, int64_t rows, int64_t seq_len, const pf_qkv* x,
+                         const float* w_q, const float* w_k, const int32_t* pos,
+                         const pf_qkv* out, void* stream) {
+  PF_TRY(check_qk(desc));
+  PF_TRY(check_count(rows, seq_len, pos, desc->n_axes));
+  if (rows == 0) return PF_OK;
+  PF_TRY(check_qk_rows("x", x, *desc));
+  PF_TRY(check_qk_rows("out", out, *desc));
+  PF_CUDA(qk_rope_fwd(rope_of(*desc), ptr_of(*x), ptr_of(*out), w_q, w_k, pos, rows, seq_len,
+                      static_cast<cudaStream_t>(stream)));
+  return PF_OK;
+}
+
+size_t pf_qk_rope_workspace_size(const pf_qk_desc* desc) {
+  return check_qk(desc) == PF_OK ? qk_rope_part_bytes(desc->dh) : 0;
+}
+
+pf_status pf_qk_rope_bwd(const pf_qk_desc* desc, int64_t rows, int64_t seq_len, const pf_qkv* x,
+                         const float* w_q, const float* w_k, const int32_t* pos,
+                         const pf_qkv* dout, const pf_qkv* dx, float* dw_q, float* dw_k, void* ws,
+                         size_t ws_bytes, void* stream) {
+  PF_TRY(check_qk(desc));
+  PF_TRY(check_count(rows, seq_len, pos, desc->n_axes));
+  if ((dw_q && !w_q) || (dw_k && !w_k))
+    return fail(PF_ERR_INVALID_ARG, "a weight that is NULL has no gradient");
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    for (float* g : {dw_q, dw_k})
+      if (g) PF_CUDA(cudaMemsetAsync(g, 0, desc->dh * sizeof(float), cs));
+    return PF_OK;
+  }
+  PF_TRY(check_qk_rows("x", x, *desc));
+  PF_TRY(check_qk_rows("dout", dout, *desc));
+  PF_TRY(check_qk_rows("dx", dx, *desc));
+  const bool dw = dw_q || dw_k;
+  if (dw && (!ws || !aligned16(ws) || ws_bytes < qk_rope_part_bytes(desc->dh)))
+    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu",
+                qk_rope_part_bytes(desc->dh), ws ? ws_bytes : 0);
+  PF_CUDA(qk_rope_bwd(rope_of(*desc), ptr_of(*x), ptr_of(*dout), ptr_of(*dx), w_q, w_k, pos, dw_q,
+                      dw_k, static_cast<float*>(ws), rows, seq_len, cs));
+  return PF_OK;
+}
+
+pf_status pf_paged_advance(const pf_paged_desc* desc, const int32_t* start, pf_paged_cache* cache,
+                           void* stream) {
+  PF_TRY(check_paged(desc));
+  if (!cache || !cache->len) return fail(PF_ERR_INVALID_ARG, "len is required");
+  PF_CUDA(paged_advance(paged_of(*desc, cache), start, cache->len,
+                        static_cast<cudaStream_t>(stream)));
+  return PF_OK;
+}
+
+pf_status pf_paged_append(const pf_paged_desc* desc, const pf_qk_desc* qk, int64_t rows,
+                          const pf_qkv* x, const float* w_q, const float* w_k,
+                          const int32_t* start, const int32_t* pos, pf_paged_cache* cache,
+                          void* q_out, int64_t ld_q_out, void* stream) {
+  PF_TRY(check_paged(desc));
+  PF_TRY(check_qk(qk));
+  if (qk->n_heads != desc->n_heads || qk->n_kv != desc->n_kv || qk->dh != desc->dh)
+    return fail(PF_ERR_INVALID_ARG, "the two descriptors' heads differ");
+  if (qk->dtype != PF_BF16) return fail(PF_ERR_UNSUPPORTED, "the paged cache is bf16");
+  PF_TRY(check_count(rows, 1, pos, qk->n_axes));
+  if (!start && rows != desc->batch)
+    return fail(PF_ERR_INVALID_ARG, "without start every sequence has one token: rows must be batch");
+  PF_TRY(check_cache(cache));
+  if (rows == 0) return PF_OK;
+  if (!x) return fail(PF_ERR_INVALID_ARG, "x is NULL");
+  if ((x->q == nullptr) != (q_out == nullptr))
+    return fail(PF_ERR_INVALID_ARG, "x->q and q_out go together");
+  if (q_out) {
+    PF_TRY(check_rows("q", x->q, x->ld_q, (int64_t)desc->n_heads * desc->dh, 2));
+    PF_TRY(check_rows("q_out", q_out, ld_q_out, (int64_t)desc->n_heads * desc->dh, 2));
+  }
+  PF_TRY(check_rows("k", x->k, x->ld_k, (int64_t)desc->n_kv * desc->dh, 2));
+  PF_TRY(check_rows("v", x->v, x->ld_v, (int64_t)desc->n_kv * desc->dh, 2));
+  QkRope r = rope_of(*qk);
+  if (!q_out) r.H = 0;
+  PF_CUDA(paged_append(r, paged_of(*desc, cache), ptr_of(*x), static_cast<bf16*>(q_out), (long)ld_q_out,
+                       w_q, w_k, start, pos, rows, static_cast<cudaStream_t>(stream)));
+  return PF_OK;
+}
+
+size_t pf_paged_attn_workspace_size(const pf_paged_desc* desc) {
+  return check_paged(desc) == PF_OK ? paged_attn_ws_bytes(paged_of(*desc, nullptr)) : 0;
+}
+
+pf_status pf_paged_attn(const pf_paged_desc* desc, const void* q, int64_t ld_q,
+                        const pf_paged_cache* cache, void* out, int64_t ld_out, void* ws,
+                        size_t ws_bytes, void* stream) {
+  PF_TRY(check_paged(desc));
+  PF_TRY(check_rows("q", q, ld_q, (int64_t)desc->n_heads * desc->dh, 2));
+  PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
+  PF_TRY(check_cache(cache));
+  const Paged p = paged_of(*desc, cache);
+  const size_t need = paged_attn_ws_bytes(p);
+  if (!ws || !aligned16(ws) || ws_bytes < need)
+    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need,
+                ws ? ws_bytes : 0);
+  PF_CUDA(paged_attn(p, static_cast<const bf16*>(q), (long)ld_q, static_cast<bf16*>(out), (long)ld_out,
+                     static_cast<float*>(ws), static_cast<cudaStream_t>(stream)));
+  return PF_OK;
+}
+
+}  // extern "C"

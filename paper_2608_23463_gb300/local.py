@@ -1,0 +1,191 @@
+"""Attention of the local stream (PyTorch holds memory).
+
+``QKRope`` norms and rotates queries and keys (``pf_qk_rope_*``) and
+``PagedKVCache`` keeps the keys and values of many sequences in pages
+(``pf_paged_*``): ``append`` writes new tokens' rows, ``attend`` is the attention
+of every sequence's newest token.  All calls run on the current CUDA stream;
+none does arithmetic of its own.  Matrices are 2D tensors whose rows may lie
+apart (a slice of a projection's output serves as it is).
+"""
+from __future__ import annotations
+
+from typing import Optional, Sequence, Tuple
+
+import torch
+
+from . import (PF_BF16, PF_ERR_CAPACITY, PF_ERR_INVALID_ARG, PF_F32, PagedCache, PagedDesc,
+               ProxyFormerError, QKDesc, _ptr, pf_paged_advance, pf_paged_append, pf_paged_attn,
+               pf_paged_attn_workspace_size, pf_qk_rope_bwd, pf_qk_rope_fwd,
+               pf_qk_rope_workspace_size, qkv)
+
+
+def _stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _rows(name: str, t: torch.Tensor, rows: int, width: int, dtype: torch.dtype) -> torch.Tensor:
+    """t as the library takes it: a 2D CUDA matrix with its values side by side in a row."""
+    if (t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or t.dtype != dtype
+            or not t.is_cuda or (width > 1 and t.stride(1) != 1)):
+        raise ProxyFormerError(PF_ERR_INVALID_ARG, f"{name} must be a [{rows}, {width}] {dtype} "
+                               "CUDA matrix with contiguous rows")
+    if rows == 1 and t.stride(0) != width:  # the stride of a single row says nothing
+        t = t.as_strided((1, width), (width, 1))
+    return t
+
+
+def _ints(name: str, t: Optional[torch.Tensor], *shape: int) -> Optional[torch.Tensor]:
+    if t is not None and (tuple(t.shape) != shape or t.dtype != torch.int32 or not t.is_cuda
+                          or not t.is_contiguous()):
+        raise ProxyFormerError(PF_ERR_INVALID_ARG, f"{name} must be a contiguous int32 CUDA tensor "
+                               f"of shape {list(shape)}")
+    return t
+
+
+class QKRope:
+    """RMSNorm of every query and key head (with weights w_q, w_k [dh]; None: no
+    norm) and its position rotation: ``pairs`` pairs of a head for every position
+    axis (default: one axis, all of them; (): no rotation)."""
+
+    def __init__(self, n_heads: int, n_kv: int, dh: int, w_q: Optional[torch.Tensor] = None,
+                 w_k: Optional[torch.Tensor] = None, pairs: Optional[Sequence[int]] = None,
+                 theta: float = 10000.0, eps: float = 1e-6, dtype: torch.dtype = torch.bfloat16):
+        pairs = (dh // 2,) if pairs is None else tuple(pairs)
+        if len(pairs) > 3 or dtype not in (torch.bfloat16, torch.float32):
+            raise ProxyFormerError(PF_ERR_INVALID_ARG, "at most 3 axes; bf16 or fp32")
+        for n, w in (("w_q", w_q), ("w_k", w_k)):
+            if w is not None and (w.shape != (dh,) or w.dtype != torch.float32
+                                  or not w.is_contiguous() or not w.is_cuda):
+                raise ProxyFormerError(PF_ERR_INVALID_ARG, f"{n} must be {dh} fp32 values on the GPU")
+        self.n_heads, self.n_kv, self.dh, self.dtype, self.n_axes = n_heads, n_kv, dh, dtype, len(pairs)
+        self.w_q, self.w_k = w_q, w_k
+        self.desc = QKDesc(n_heads, n_kv, dh, PF_F32 if dtype == torch.float32 else PF_BF16,
+                           len(pairs), (pairs + (0, 0, 0))[:3], theta, eps)
+        self.ws: Optional[torch.Tensor] = None
+
+    def _qk(self, rows: int, q: torch.Tensor, k: torch.Tensor):
+        return (_rows("q", q, rows, self.n_heads * self.dh, self.dtype),
+                _rows("k", k, rows, self.n_kv * self.dh, self.dtype))
+
+    def forward(self, q: torch.Tensor, k: torch.Tensor, L: Optional[int] = None,
+                pos: Optional[torch.Tensor] = None, out=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """q [rows, n_heads*dh], k [rows, n_kv*dh] -> the same normed and turned (into
+        ``out``, a pair, which may be (q, k) itself).  Positions: pos [rows, axes]
+        int32, or the row's place in its sequence of L rows (default: one sequence)."""
+        rows = int(q.shape[0])
+        q, k = self._qk(rows, q, k)
+        qo, ko = (torch.empty((rows, t.shape[1]), dtype=t.dtype, device=t.device) for t in (q, k)) \
+            if out is None else self._qk(rows, *out)
+        pf_qk_rope_fwd(self.desc, rows, L or max(rows, 1), qkv(q, k), self.w_q, self.w_k,
+                       _ints("pos", pos, rows, self.n_axes), qkv(qo, ko), _stream())
+        return qo, ko
+
+    def backward(self, q: torch.Tensor, k: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
+                 L: Optional[int] = None, pos: Optional[torch.Tensor] = None, out=None):
+        """From the forward's inputs and the gradients of its results: the gradients
+        of q and k (into ``out``, which may be (dq, dk) itself) and of w_q and w_k
+        (None without them)."""
+        rows = int(q.shape[0])
+        q, k = self._qk(rows, q, k)
+        dq, dk = self._qk(rows, dq, dk)
+        xq, xk = (torch.empty((rows, t.shape[1]), dtype=t.dtype, device=t.device) for t in (q, k)) \
+            if out is None else self._qk(rows, *out)
+        dw_q, dw_k = (None if w is None else torch.empty_like(w) for w in (self.w_q, self.w_k))
+        if self.ws is None and (dw_q is not None or dw_k is not None):
+            self.ws = torch.empty(pf_qk_rope_workspace_size(self.desc), dtype=torch.uint8,
+                                  device=q.device)
+        pf_qk_rope_bwd(self.desc, rows, L or max(rows, 1), qkv(q, k), self.w_q, self.w_k,
+                       _ints("pos", pos, rows, self.n_axes), qkv(dq, dk), qkv(xq, xk), dw_q, dw_k,
+                       self.ws, 0 if self.ws is None else self.ws.numel(), _stream())
+        return xq, xk, dw_q, dw_k
+
+
+class PagedKVCache:
+    """Keys and values of ``batch`` sequences of one layer in a pool of pages.
+
+    ``table`` and ``len`` (device tensors) may be shared by the caches of all
+    layers: pass those of the first.  A step: ``reserve`` pages for the new rows
+    (host), ``advance`` the lengths once, then ``append`` and ``attend`` layer by
+    layer.  ``rope`` (a QKRope) is applied to keys, and queries, on the way in;
+    without it they are taken as they are."""
+
+    def __init__(self, batch: int, n_heads: int, n_kv: int, dh: int, page: int, n_pages: int,
+                 max_pages: int, rope: Optional[QKRope] = None, window: int = 0, n_sink: int = 0,
+                 K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None,
+                 table: Optional[torch.Tensor] = None, len: Optional[torch.Tensor] = None,
+                 device="cuda"):
+        self.batch, self.n_heads, self.n_kv, self.dh, self.page = batch, n_heads, n_kv, dh, page
+        self.n_pages, self.max_pages = n_pages, max_pages
+        self.rope = rope or QKRope(n_heads, n_kv, dh, pairs=())
+        shape = (n_pages, n_kv, page, dh)
+        self.K, self.V = (torch.zeros(shape, dtype=torch.bfloat16, device=device) if t is None else t
+                          for t in (K, V))
+        for t in (self.K, self.V):
+            if tuple(t.shape) != shape or t.dtype != torch.bfloat16 or not t.is_contiguous():
+                raise ProxyFormerError(PF_ERR_INVALID_ARG, f"K and V must be contiguous bf16 {shape}")
+        self.table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device) \
+            if table is None else _ints("table", table, batch, max_pages)
+        self.len = torch.zeros(batch, dtype=torch.int32, device=device) \
+            if len is None else _ints("len", len, batch)
+        self.desc = PagedDesc(batch, n_heads, n_kv, dh, page, max_pages, n_pages, window, n_sink)
+        self.cache = PagedCache(_ptr(self.K), _ptr(self.V), _ptr(self.table), _ptr(self.len))
+        self.ws = torch.empty(max(16, pf_paged_attn_workspace_size(self.desc)), dtype=torch.uint8,
+                              device=device)
+        self.free = list(range(n_pages - 1, -1, -1))  # pages that reserve() hands out
+        self.held = [[] for _ in range(batch)]        # and has handed out, by sequence
+
+    def reserve(self, rows: Sequence[int]) -> None:
+        """Pages for rows[b] rows in all of every sequence b (host bookkeeping; a
+        cache that was given its table keeps its own)."""
+        need = [max(0, -(-int(r) // self.page) - len(p)) for r, p in zip(rows, self.held)]
+        if sum(need) > len(self.free) or any(
+                n + len(p) > self.max_pages for n, p in zip(need, self.held)):
+            raise ProxyFormerError(PF_ERR_CAPACITY, "no pages left for these rows")
+        for b, n in enumerate(need):
+            if n:
+                new = [self.free.pop() for _ in range(n)]
+                at = len(self.held[b])
+                self.held[b] += new
+                self.table[b, at:at + n] = torch.tensor(new, dtype=torch.int32,
+                                                        device=self.table.device)
+
+    def release(self, b: int) -> None:
+        """Sequence b gives its pages back and is empty."""
+        self.free += self.held[b][::-1]
+        self.held[b] = []
+        self.len[b] = 0
+
+    def advance(self, start: Optional[torch.Tensor] = None) -> None:
+        """The lengths at the start of a step: start[b+1] - start[b] more rows of
+        every sequence b, or one."""
+        pf_paged_advance(self.desc, _ints("start", start, self.batch + 1), self.cache, _stream())
+
+    def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+               start: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """The step's tokens, k, v [rows, n_kv*dh], into the cache; returns their
+        queries q [rows, n_heads*dh] normed and turned (None without them).  start
+        [batch+1] int32: first token of every sequence; None: one each."""
+        rows, bf = int(k.shape[0]), torch.bfloat16
+        k, v = (_rows(n, t, rows, self.n_kv * self.dh, bf) for n, t in (("k", k), ("v", v)))
+        if q is not None:
+            q = _rows("q", q, rows, self.n_heads * self.dh, bf)
+            out = torch.empty((rows, q.shape[1]), dtype=bf, device=q.device) if out is None else \
+                _rows("out", out, rows, q.shape[1], bf)
+        else:
+            out = None
+        pf_paged_append(self.desc, self.rope.desc, rows, qkv(q, k, v), self.rope.w_q, self.rope.w_k,
+                        _ints("start", start, self.batch + 1),
+                        _ints("pos", pos, rows, self.rope.n_axes), self.cache, out,
+                        0 if out is None else out.stride(0), _stream())
+        return out
+
+    def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of every sequence's newest token, q [batch, n_heads*dh]."""
+        width = self.n_heads * self.dh
+        q = _rows("q", q, self.batch, width, torch.bfloat16)
+        out = torch.empty((self.batch, width), dtype=q.dtype, device=q.device) if out is None else \
+            _rows("out", out, self.batch, width, q.dtype)
+        pf_paged_attn(self.desc, q, q.stride(0), self.cache, out, out.stride(0), self.ws,
+                      self.ws.numel(), _stream())
+        return out

@@ -1,0 +1,110 @@
+"""Argument checks of the local stream's operators (no GPU): every refusal comes
+before anything is launched."""
+import pytest
+
+import paper_2608_23463_gb300 as pf
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    from paper_2608_23463_gb300.buildlib import build
+    build()
+    return pf.load()
+
+
+A = 1 << 12  # an aligned address that nothing reads
+
+
+def refused(status, f, *a):
+    with pytest.raises(pf.ProxyFormerError) as e:
+        f(*a)
+    assert e.value.status == status, e.value
+
+
+def qk(n_heads=4, n_kv=2, dh=64, dtype=pf.PF_BF16, n_axes=1, pairs=(32, 0, 0), theta=1e4, eps=1e-6):
+    return pf.QKDesc(n_heads, n_kv, dh, dtype, n_axes, pairs, theta, eps)
+
+
+def rows(q=A, k=A, v=A, ld_q=256, ld_k=128, ld_v=128):
+    return pf.QKV(q, k, v, ld_q, ld_k, ld_v)
+
+
+def test_rope_refusals():
+    f = lambda d=qk(), n=8, L=8, x=rows(), pos=None, out=rows(): pf.pf_qk_rope_fwd(d, n, L, x, A, A, pos, out)
+    bad, no = pf.PF_ERR_INVALID_ARG, pf.PF_ERR_UNSUPPORTED
+    for kw in (dict(n_heads=5), dict(n_kv=0), dict(n_heads=-4), dict(dtype=7), dict(n_axes=4), dict(n_axes=-1),
+               dict(pairs=(33, 0, 0)), dict(n_axes=2, pairs=(30, 3, 0)), dict(pairs=(-1, 0, 0)), dict(theta=0.0),
+               dict(theta=float("nan")), dict(eps=0.0)):
+        refused(bad, f, qk(**kw))
+        assert pf.pf_qk_rope_workspace_size(qk(**kw)) == 0
+    refused(no, f, qk(dh=96))
+    refused(bad, lambda: f(n=-1))
+    refused(bad, lambda: f(n=1 << 31))
+    refused(bad, lambda: f(L=0))
+    refused(bad, lambda: f(qk(n_axes=2, pairs=(16, 16, 0))))  # several axes need positions
+    for kw in (dict(q=None), dict(k=A + 8), dict(ld_q=248), dict(ld_k=132), dict(ld_q=1 << 40)):
+        refused(bad, lambda: f(x=rows(**kw)))
+        refused(bad, lambda: f(out=rows(**kw)))
+    refused(bad, lambda: f(qk(dtype=pf.PF_F32), x=rows(ld_q=258)))
+
+
+def test_rope_backward_refusals():
+    def f(d=qk(), n=8, dout=rows(), dx=rows(), w_q=A, dw_q=A, ws=A, size=1 << 30):
+        pf.pf_qk_rope_bwd(d, n, 8, rows(), w_q, A, None, dout, dx, dw_q, A, ws, size)
+    refused(pf.PF_ERR_INVALID_ARG, lambda: f(dout=rows(q=None)))
+    refused(pf.PF_ERR_INVALID_ARG, lambda: f(dx=rows(ld_k=64)))
+    refused(pf.PF_ERR_INVALID_ARG, lambda: f(w_q=None))
+    need = pf.pf_qk_rope_workspace_size(qk())
+    refused(pf.PF_ERR_WORKSPACE, lambda: f(size=need - 1))
+    refused(pf.PF_ERR_WORKSPACE, lambda: f(ws=None))
+    refused(pf.PF_ERR_WORKSPACE, lambda: f(ws=A + 4))
+
+
+def paged(batch=3, n_heads=4, n_kv=2, dh=64, page=16, max_pages=4, n_pages=9, window=0, n_sink=0):
+    return pf.PagedDesc(batch, n_heads, n_kv, dh, page, max_pages, n_pages, window, n_sink)
+
+
+def cache(K=A, V=A, table=A, length=A):
+    return pf.PagedCache(K, V, table, length)
+
+
+def test_paged_refusals():
+    bad, no = pf.PF_ERR_INVALID_ARG, pf.PF_ERR_UNSUPPORTED
+    attn = lambda d=paged(), q=A, ld=256, c=cache(), out=A, ld_o=256, ws=A, size=1 << 30: pf.pf_paged_attn(
+        d, q, ld, c, out, ld_o, ws, size)
+    app = lambda d=paged(), k=qk(), n=3, x=rows(), start=None, c=cache(), qo=A, ld=256: pf.pf_paged_append(
+        d, k, n, x, A, A, start, None, c, qo, ld)
+    for s, kws in ((bad, (dict(batch=0), dict(n_kv=3), dict(page=0), dict(page=24), dict(max_pages=0), dict(n_pages=0),
+                          dict(window=-1), dict(n_sink=-1))),
+                   (no, (dict(batch=2049), dict(dh=80), dict(n_heads=34)))):
+        for kw in kws:
+            refused(s, attn, paged(**kw))
+            refused(s, app, paged(**kw))
+            refused(s, pf.pf_paged_advance, paged(**kw), None, cache())
+            assert pf.pf_paged_attn_workspace_size(paged(**kw)) == 0
+    for kw in (dict(K=None), dict(V=A + 2), dict(table=None), dict(length=None)):
+        refused(bad, lambda: attn(c=cache(**kw)))
+        refused(bad, lambda: app(c=cache(**kw)))
+    refused(bad, lambda: pf.pf_paged_advance(paged(), None, cache(length=None)))
+    for kw in (dict(q=None), dict(q=A + 8), dict(ld=252), dict(ld=248), dict(out=None), dict(ld_o=128)):
+        refused(bad, lambda: attn(**kw))
+    need = pf.pf_paged_attn_workspace_size(paged())
+    refused(pf.PF_ERR_WORKSPACE, lambda: attn(size=need - 1))
+    refused(pf.PF_ERR_WORKSPACE, lambda: attn(ws=None))
+    refused(bad, lambda: app(k=qk(n_heads=8)))
+    refused(bad, lambda: app(k=qk(dh=128)))
+    refused(no, lambda: app(k=qk(dtype=pf.PF_F32)))
+    refused(bad, lambda: app(k=qk(n_axes=2, pairs=(16, 16, 0))))
+    refused(bad, lambda: app(n=4))  # one token a sequence without start
+    refused(bad, lambda: app(qo=None))
+    refused(bad, lambda: app(x=rows(q=None)))
+    for kw in (dict(k=None), dict(v=A + 8), dict(ld_v=120)):
+        refused(bad, lambda: app(x=rows(**kw)))
+    assert app(n=0, start=A, x=rows(q=0, k=0, v=0)) is None  # no token: nothing to do
+
+
+def test_workspace_follows_the_split():
+    """Two places for each CTA: at most 304, or one for each 64 rows of a key head."""
+    size = pf.pf_paged_attn_workspace_size
+    assert size(paged(batch=1, max_pages=4)) == 2 * 2 * 2 * 66 * 4
+    assert size(paged(batch=64, max_pages=1000)) == size(paged(batch=2048, max_pages=1 << 30)) == 2 * 304 * 2 * 66 * 4
