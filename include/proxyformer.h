@@ -339,8 +339,9 @@ pf_status proxy_segments_bwd(const pf_layer_desc *desc, int32_t n_seg, const pf_
 /* ---------------------------------------------------------------------------
  * Attention of the local stream (the local Transformer that Sec. 3.5 leaves to
  * the user after the injection, and the self-attention of the generation side
- * of Sec. 3.7 for many requests): norm and rotation of queries and keys, a
- * paged cache of keys and values and the attention of a new token over it.
+ * of Sec. 3.7 for many requests): norm and rotation of queries and keys,
+ * attention in a sliding window with its backward, a paged cache of keys and
+ * values and the attention of a new token over it.
  * Buffers as everywhere; rows of a matrix may lie further apart than their
  * width (leading dimensions ld_* in elements, multiples of 16 bytes), heads of
  * a row one after the other, head h at column h*dh.                           */
@@ -389,6 +390,33 @@ pf_status pf_qk_rope_bwd(const pf_qk_desc *desc, int64_t rows, int64_t seq_len, 
                          const float *w_q, const float *w_k, const int32_t *pos,
                          const pf_qkv *dout, const pf_qkv *dx, float *dw_q, float *dw_k, void *ws,
                          size_t ws_bytes, void *stream);
+
+/* Causal attention in a sliding window with sinks over `batch` sequences of L
+ * rows, bf16: query i sees the keys j <= i with i - j < window (0: all) or
+ * j < n_sink.
+ *   n_heads, n_kv, dh : as above, head width 64
+ * L below 2^30, batch * L below 2^31.                                        */
+typedef struct {
+  int32_t batch, L, n_heads, n_kv, dh;
+  int32_t window, n_sink;
+} pf_window_desc;
+
+/* out_h = softmax(q_h K^T / sqrt(dh)) V over the keys that a row sees, key head
+ * h / (n_heads/n_kv); rows b*L + i of x and out [batch*L, n_heads*dh] (leading
+ * dimension ld_out).  lse [batch, n_heads, L] fp32 for the backward, or NULL.
+ * Keys and values must be finite: those that a row does not see are multiplied
+ * by zero.                                                                   */
+pf_status pf_window_attn_fwd(const pf_window_desc *desc, const pf_qkv *x, void *out,
+                             int64_t ld_out, float *lse, void *stream);
+
+size_t pf_window_attn_workspace_size(const pf_window_desc *desc);
+
+/* Its backward: dx->q, dx->k, dx->v (overwritten; those of a key head sum over
+ * its query heads) from the forward's x, out and lse and the gradient dout of
+ * out.  dx may not overlap x, out or dout.                                   */
+pf_status pf_window_attn_bwd(const pf_window_desc *desc, const pf_qkv *x, const void *out,
+                             int64_t ld_out, const float *lse, const void *dout, int64_t ld_dout,
+                             const pf_qkv *dx, void *ws, size_t ws_bytes, void *stream);
 
 /* Paged cache of one layer's keys and values (bf16).
  *   batch     : sequences, at most 2048

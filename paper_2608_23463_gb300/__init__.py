@@ -90,6 +90,10 @@ class QKDesc(ctypes.Structure):
                 + [("pairs", _c_i32 * 3), ("theta", ctypes.c_double), ("eps", ctypes.c_double)])
 
 
+class WindowDesc(ctypes.Structure):
+    _fields_ = [(n, _c_i32) for n in ("batch", "L", "n_heads", "n_kv", "dh", "window", "n_sink")]
+
+
 class PagedDesc(ctypes.Structure):
     _fields_ = ([(n, _c_i32) for n in ("batch", "n_heads", "n_kv", "dh", "page", "max_pages")]
                 + [("n_pages", ctypes.c_int64), ("window", _c_i32), ("n_sink", _c_i32)])
@@ -105,6 +109,7 @@ EXPORTED = ("proxy_layer_check", "proxy_layer_saved_size", "proxy_layer_workspac
             "proxy_prefill_workspace_size", "proxy_kv_prefill", "proxy_layer_prefill",
             "proxy_segments_saved_size", "proxy_segments_workspace_size", "proxy_segments_fwd",
             "proxy_segments_bwd", "pf_qk_rope_fwd", "pf_qk_rope_workspace_size", "pf_qk_rope_bwd",
+            "pf_window_attn_fwd", "pf_window_attn_workspace_size", "pf_window_attn_bwd",
             "pf_paged_advance", "pf_paged_append", "pf_paged_attn_workspace_size", "pf_paged_attn",
             "pf_last_error", "pf_sync_check", "pf_gemm_bf16", "pf_timing_enable",
             "pf_timing_collect", "pf_timing_label", "pf_timing_ms", "pf_timing_launches",
@@ -175,6 +180,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pf_qk_rope_bwd.argtypes = [P(QKDesc), i64, i64, P(QKV), _vp, _vp, _vp, P(QKV), P(QKV), _vp,
                                    _vp, _vp, sz, _vp]
     lib.pf_qk_rope_bwd.restype = ctypes.c_int
+    lib.pf_window_attn_fwd.argtypes = [P(WindowDesc), P(QKV), _vp, i64, _vp, _vp]
+    lib.pf_window_attn_fwd.restype = ctypes.c_int
+    lib.pf_window_attn_workspace_size.argtypes = [P(WindowDesc)]
+    lib.pf_window_attn_workspace_size.restype = sz
+    lib.pf_window_attn_bwd.argtypes = [P(WindowDesc), P(QKV), _vp, i64, _vp, _vp, i64, P(QKV), _vp,
+                                       sz, _vp]
+    lib.pf_window_attn_bwd.restype = ctypes.c_int
     lib.pf_paged_advance.argtypes = [P(PagedDesc), _vp, P(PagedCache), _vp]
     lib.pf_paged_advance.restype = ctypes.c_int
     lib.pf_paged_append.argtypes = [P(PagedDesc), P(QKDesc), i64, P(QKV), _vp, _vp, _vp, _vp,
@@ -378,6 +390,21 @@ def pf_qk_rope_bwd(desc, rows, seq_len, x, w_q, w_k, pos, dout, dx, dw_q, dw_k, 
                                  _ptr(w_q), _ptr(w_k), _ptr(pos), ctypes.byref(dout),
                                  ctypes.byref(dx), _ptr(dw_q), _ptr(dw_k), _ptr(ws), int(ws_bytes),
                                  stream))
+
+
+def pf_window_attn_fwd(desc, x, out, ld_out, lse, stream=None):
+    _check(load().pf_window_attn_fwd(ctypes.byref(desc), ctypes.byref(x), _ptr(out), int(ld_out),
+                                     _ptr(lse), stream))
+
+
+def pf_window_attn_workspace_size(desc) -> int:
+    return load().pf_window_attn_workspace_size(ctypes.byref(desc))
+
+
+def pf_window_attn_bwd(desc, x, out, ld_out, lse, dout, ld_dout, dx, ws, ws_bytes, stream=None):
+    _check(load().pf_window_attn_bwd(ctypes.byref(desc), ctypes.byref(x), _ptr(out), int(ld_out),
+                                     _ptr(lse), _ptr(dout), int(ld_dout), ctypes.byref(dx),
+                                     _ptr(ws), int(ws_bytes), stream))
 
 
 def pf_paged_advance(desc, start, cache, stream=None):

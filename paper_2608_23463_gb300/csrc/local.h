@@ -26,6 +26,19 @@ struct Paged {
   const int *table, *len;
 };
 
+// Windowed attention of B sequences of L rows: H query and KV key heads of 64.
+struct Window {
+  int B, L, H, KV, window, sinks;  // window 0: no limit
+};
+double window_pairs(const Window& c);  // visible (query, key) pairs of a head and sequence
+// lse [B, H, L] in log2 units for the backward, or null.
+cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, float* lse,
+                       cudaStream_t st);
+size_t window_bwd_ws_bytes(const Window& c);
+cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long ldo,
+                       const float* lse, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
+                       cudaStream_t st);
+
 cudaError_t qk_rope_fwd(const QkRope& s, const QkvPtr& x, const QkvPtr& o, const float* w_q,
                         const float* w_k, const int* pos, long rows, long seq_len,
                         cudaStream_t st);
@@ -47,7 +60,11 @@ cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long 
 
 int take_dev_error_local_rope();
 int take_dev_error_paged_attn();
+int take_dev_error_window_attn();
+int take_dev_error_window_attn_bwd();
 int set_wait_limit_local_rope(unsigned long long ns);
 int set_wait_limit_paged_attn(unsigned long long ns);
+int set_wait_limit_window_attn(unsigned long long ns);
+int set_wait_limit_window_attn_bwd(unsigned long long ns);
 
 }  // namespace pf

@@ -93,6 +93,32 @@ pf_status check_count(int64_t rows, int64_t seq_len, const int32_t* pos, int n_a
   return PF_OK;
 }
 
+pf_status check_window(const pf_window_desc* s) {
+  if (!s) return fail(PF_ERR_INVALID_ARG, "window descriptor is NULL");
+  if (s->batch < 1 || s->L < 1) return fail(PF_ERR_INVALID_ARG, "batch and L must be >= 1");
+  if (s->L >= 1 << 30 || (int64_t)s->batch * s->L >= int64_t(1) << 31)
+    return fail(PF_ERR_UNSUPPORTED, "L must be below 2^30 and batch * L below 2^31");
+  PF_TRY(check_heads(s->n_heads, s->n_kv, s->dh));
+  if (s->dh != 64) return fail(PF_ERR_UNSUPPORTED, "windowed attention: head width must be 64");
+  if ((int64_t)s->batch * s->n_heads * ((s->L + 127) / 128) >= 1 << 28)
+    return fail(PF_ERR_UNSUPPORTED, "too many query tiles");
+  if (s->window < 0 || s->n_sink < 0)
+    return fail(PF_ERR_INVALID_ARG, "window and n_sink must not be negative");
+  return PF_OK;
+}
+
+Window window_of(const pf_window_desc& s) {
+  return {s.batch, s.L, s.n_heads, s.n_kv, s.window, s.n_sink};
+}
+
+pf_status check_window_rows(const char* what, const pf_qkv* x, const pf_window_desc& s) {
+  if (!x) return fail(PF_ERR_INVALID_ARG, "%s is NULL", what);
+  const int64_t nq = (int64_t)s.n_heads * s.dh, nk = (int64_t)s.n_kv * s.dh;
+  PF_TRY(check_rows("q", x->q, x->ld_q, nq, 2));
+  PF_TRY(check_rows("k", x->k, x->ld_k, nk, 2));
+  return check_rows("v", x->v, x->ld_v, nk, 2);
+}
+
 pf_status check_paged(const pf_paged_desc* s) {
   if (!s) return fail(PF_ERR_INVALID_ARG, "paged descriptor is NULL");
   if (s->batch < 1) return fail(PF_ERR_INVALID_ARG, "batch must be >= 1");
@@ -172,6 +198,44 @@ pf_status pf_qk_rope_bwd(const pf_qk_desc* desc, int64_t rows, int64_t seq_len, 
                 qk_rope_part_bytes(desc->dh), ws ? ws_bytes : 0);
   PF_CUDA(qk_rope_bwd(rope_of(*desc), ptr_of(*x), ptr_of(*dout), ptr_of(*dx), w_q, w_k, pos, dw_q,
                       dw_k, static_cast<float*>(ws), rows, seq_len, cs));
+  return PF_OK;
+}
+
+pf_status pf_window_attn_fwd(const pf_window_desc* desc, const pf_qkv* x, void* out,
+                             int64_t ld_out, float* lse, void* stream) {
+  PF_TRY(check_window(desc));
+  PF_TRY(check_window_rows("x", x, *desc));
+  PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
+  PF_CUDA(window_fwd(window_of(*desc), ptr_of(*x), static_cast<bf16*>(out), (long)ld_out, lse,
+                     static_cast<cudaStream_t>(stream)));
+  return PF_OK;
+}
+
+size_t pf_window_attn_workspace_size(const pf_window_desc* desc) {
+  return check_window(desc) == PF_OK ? window_bwd_ws_bytes(window_of(*desc)) : 0;
+}
+
+pf_status pf_window_attn_bwd(const pf_window_desc* desc, const pf_qkv* x, const void* out,
+                             int64_t ld_out, const float* lse, const void* dout, int64_t ld_dout,
+                             const pf_qkv* dx, void* ws, size_t ws_bytes, void* stream) {
+  PF_TRY(check_window(desc));
+  PF_TRY(check_window_rows("x", x, *desc));
+  PF_TRY(check_window_rows("dx", dx, *desc));
+  PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
+  PF_TRY(check_rows("dout", dout, ld_dout, (int64_t)desc->n_heads * desc->dh, 2));
+  if (!lse) return fail(PF_ERR_INVALID_ARG, "lse is required");
+  for (const void* d : {dx->q, dx->k, dx->v})
+    for (const void* i : {static_cast<const void*>(x->q), static_cast<const void*>(x->k),
+                          static_cast<const void*>(x->v), out, dout})
+      if (d == i) return fail(PF_ERR_INVALID_ARG, "dx may not overlap an input");
+  const Window c = window_of(*desc);
+  const size_t need = window_bwd_ws_bytes(c);
+  if (!ws || !aligned16(ws) || ws_bytes < need)
+    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need,
+                ws ? ws_bytes : 0);
+  PF_CUDA(window_bwd(c, ptr_of(*x), static_cast<const bf16*>(out), (long)ld_out, lse,
+                     static_cast<const bf16*>(dout), (long)ld_dout, ptr_of(*dx), ws,
+                     static_cast<cudaStream_t>(stream)));
   return PF_OK;
 }
 

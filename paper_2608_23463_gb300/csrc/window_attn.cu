@@ -1,0 +1,501 @@
+// Causal attention in a sliding window with sinks, forward, on the
+// 5th-generation tensor cores: tcgen05.mma with TMEM accumulators, TMA tiles,
+// head width 64, grouped heads.
+//
+//   o_i = sum_j softmax_j(q_i . k_j / 8) v_j  over the keys
+//   j <= i with i - j < W or j < S   (W: window, S: sinks)
+//
+// Work item = (two consecutive 128-query tiles A and B, query head, sequence);
+// one persistent CTA per SM walks the items.  An item's key tiles are the
+// sinks' [0, ns) and the window's [lo, hi], without those in between: its work
+// is that of the window, whatever the length.  A tile takes no part in key
+// tiles of its neighbour's that it does not see.
+//   warp 0    TMA producer: the item's two Q tiles (double-buffered across
+//             items) and a WA_STAGES-deep ring of (K, V) 128-key tiles, shared
+//             by both query tiles; rows past the end of a sequence read as zero
+//   warp 1    MMA issuer: S_w = Q_w K_j^T (M=128, N=128, K=64) into tile w's
+//             TMEM score buffer, O_w += P_w V_j (M=128, N=64, K=128) with P_w
+//             from TMEM
+//   warps 4-7 softmax group A, warps 8-11 group B: one query row per thread
+//             (TMEM lane), its 128 scores in registers; P goes back to TMEM
+// A row's probabilities are taken against a reference m, the maximum of the
+// first tile in which the row sees a key, raised only when a later tile's
+// maximum exceeds it by more than WA_RESCALE (log2 units); then O and the sum
+// are scaled.  P <= 2^WA_RESCALE is rounded to bf16 for its product (relative
+// 2^-8, as any value), the sums take it unrounded.  A tile may hide all of its
+// keys from a row (the window's first tile, seen by the tile's first rows
+// only): such a row keeps no reference and adds zeros.
+// Masked scores are set to -inf after the product, so a masked K may hold
+// anything; P = 0 meets its V in the MMA, so values must be finite up to the
+// end of the tile that a row sees.
+#include <algorithm>
+#include <atomic>
+
+#include "local.h"
+#include "window_tiles.cuh"
+
+namespace pf {
+
+int take_dev_error_window_attn() { return take_dev_error_tu(); }
+int set_wait_limit_window_attn(unsigned long long ns) { return set_wait_limit_tu(ns); }
+
+namespace {
+
+constexpr int WA_D = 64;  // head width
+constexpr int WA_STAGES = 4;
+constexpr int WA_THREADS = 384;  // producer, MMA, two idle warps, two softmax groups of four
+// A softmax thread holds a row's 128 scores: the control warps give registers up, of the
+// 168 that each thread has at launch.
+constexpr int WA_REGS_CTRL = 88, WA_REGS_ROWS = 208;
+static_assert(WA_REGS_CTRL * 128 + WA_REGS_ROWS * 256 == 168 * WA_THREADS, "register split");
+constexpr float WA_RESCALE = 8.f;
+constexpr uint32_t WA_T_BYTES = WT * WA_D * 2;  // 16 KB: a Q, K or V tile
+constexpr uint32_t WA_OFF_KV = 4 * WA_T_BYTES;  // Q: [2 items][tiles A, B]
+constexpr uint32_t WA_OFF_BAR = WA_OFF_KV + WA_STAGES * 2 * WA_T_BYTES;
+constexpr uint32_t WA_OFF_STG = WA_OFF_BAR + 256;  // 32 output rows of each softmax warp
+constexpr uint32_t WA_SMEM = WA_OFF_STG + 8 * 32 * WA_D * 2 + 1024;
+// TMEM columns of group w: scores S at 128 w (fp32), O at 256 + 64 w (fp32),
+// P at 384 + 64 w (bf16 pairs: key 2c in the low half of column c)
+constexpr uint32_t WA_TMEM_COLS = 512;
+
+struct WaArgs {
+  bf16* out;   // [B*L, ldo], head h at column h*64
+  float* lse;  // [B, H, L] in log2 units, or null
+  long ldo;
+  int B, H, g;  // g: query heads to a key head
+  WinTiles w;
+  int n_st, n_items;  // tile pairs
+  float sl2;          // log2(e) / sqrt(64)
+};
+
+// Items are ranked from the last tile pair on (the first ones see the fewest
+// keys); CTA c takes rank c of round 0, rank G-1-c of round 1, and so on.
+__device__ __forceinline__ int wa_rank(int c, int round) {
+  return round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - c : c);
+}
+
+// Item k: tile pair, head, sequence and the key tiles of both query tiles
+// together: step j's is j < ns ? j : lo + j - ns; n of them.
+struct WaItem {
+  int u, h, b, ns, lo, n;
+  __device__ __forceinline__ WaItem(const WaArgs& a, int k) {
+    const int per = a.H * a.B;
+    u = a.n_st - 1 - k / per;
+    const int r = k % per;
+    h = r % a.H;
+    b = r / a.H;
+    lo = a.w.lo(2 * u);
+    ns = min(a.w.sT, lo);
+    n = ns + min(2 * u + 1, a.w.n_t - 1) - lo + 1;
+  }
+  __device__ __forceinline__ int tile(int j) const { return j < ns ? j : lo + j - ns; }
+};
+
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__global__ void __launch_bounds__(WA_THREADS, 1)
+    window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                      const __grid_constant__ CUtensorMap tmV, WaArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + WA_OFF_BAR);
+  // q_full[2] q_empty[2] kv_full[S] kv_empty[S], per group w: s_full s_free
+  // p_full p_free o_full o_free, done
+  const uint32_t b0 = smem_u32(bars);
+  const uint32_t q_full = b0, q_empty = b0 + 16, kv_full = b0 + 32,
+                 kv_empty = kv_full + 8 * WA_STAGES, grp0 = kv_empty + 8 * WA_STAGES,
+                 done = grp0 + 2 * 48;
+  auto s_full = [&](int w) { return grp0 + 48 * w; };
+  auto s_free = [&](int w) { return grp0 + 48 * w + 8; };
+  auto p_full = [&](int w) { return grp0 + 48 * w + 16; };
+  auto p_free = [&](int w) { return grp0 + 48 * w + 24; };
+  auto o_full = [&](int w) { return grp0 + 48 * w + 32; };
+  auto o_free = [&](int w) { return grp0 + 48 * w + 40; };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + WA_OFF_BAR + 240);
+  const uint32_t sbase = smem_u32(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(q_full + 8 * i, 1);
+      mbar_init(q_empty + 8 * i, 1);
+      mbar_init(s_full(i), 1);
+      mbar_init(s_free(i), 4);  // one arrival per softmax warp of the group
+      mbar_init(p_full(i), 4);
+      mbar_init(p_free(i), 1);
+      mbar_init(o_full(i), 1);
+      mbar_init(o_free(i), 4);
+    }
+    for (int i = 0; i < WA_STAGES; ++i) {
+      mbar_init(kv_full + 8 * i, 1);
+      mbar_init(kv_empty + 8 * i, 1);
+    }
+    mbar_init(done, 1);
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), WA_TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_enter();  // the setup above overlaps the kernel before this one
+  uint32_t kv_issued = 0, q_issued = 0;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(WA_REGS_CTRL));
+    if (warp == 0 && lane == 0) {
+      // ------------------------------------------------------------ producer
+      prefetch_tmap(&tmQ);
+      prefetch_tmap(&tmK);
+      prefetch_tmap(&tmV);
+      bool ok = true;
+      uint32_t it = 0;
+      for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items && ok;
+           k = wa_rank(blockIdx.x, ++rd), ++it) {
+        const WaItem m(a, k);
+        const int kc = m.h / a.g * WA_D;
+        const uint32_t qb = it & 1;
+        const bool two = 2 * m.u + 1 < a.w.n_t;
+        if (!mbar_wait(q_empty + 8 * qb, ((it >> 1) & 1) ^ 1)) break;
+        mbar_arrive_expect_tx(q_full + 8 * qb, two ? 2 * WA_T_BYTES : WA_T_BYTES);
+        for (int w = 0; w < (two ? 2 : 1); ++w)
+          tma_load_3d(sbase + (2 * qb + w) * WA_T_BYTES, &tmQ, q_full + 8 * qb, m.h * WA_D,
+                      (2 * m.u + w) * WT, m.b);
+        q_issued = it + 1;
+        for (int j = 0; j < m.n; ++j) {
+          const uint32_t g = kv_issued, st = g % WA_STAGES;
+          if (!mbar_wait(kv_empty + 8 * st, ((g / WA_STAGES) & 1) ^ 1)) {
+            ok = false;
+            break;
+          }
+          const uint32_t kdst = sbase + WA_OFF_KV + st * 2 * WA_T_BYTES;
+          const int row = m.tile(j) * WT;
+          mbar_arrive_expect_tx(kv_full + 8 * st, 2 * WA_T_BYTES);
+          tma_load_3d(kdst, &tmK, kv_full + 8 * st, kc, row, m.b);
+          tma_load_3d(kdst + WA_T_BYTES, &tmV, kv_full + 8 * st, kc, row, m.b);
+          kv_issued = g + 1;
+        }
+      }
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ MMA issuer
+      // The whole warp runs the loop; one elected lane issues and commits.
+      constexpr uint32_t idesc_s = idesc_bf16_f32(WT, WT, 0, 0);
+      constexpr uint32_t idesc_o = idesc_bf16_f32(WT, WA_D, 0, 1);
+      bool ok = true;
+      uint32_t G = 0, it = 0;
+      uint32_t gs[2] = {0, 0}, gp[2] = {0, 0};  // score and P V products of each group so far
+      uint32_t io[2] = {0, 0};                  // items of each group so far
+      int pv[2];                                // P V products of the item so far
+      // O_w (+)= P_w V for step jj of item m (G: its first stage)
+      auto issue_pv = [&](const WaItem& m, int jj) -> bool {
+        const uint32_t st = (G + jj) % WA_STAGES;
+        const uint32_t vb = sbase + WA_OFF_KV + st * 2 * WA_T_BYTES + WA_T_BYTES;
+        const int kt = m.tile(jj);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const int t = 2 * m.u + w;
+          if (!a.w.sees(t, kt)) continue;
+          if (!mbar_wait_warp(p_full(w), gp[w] & 1)) return false;
+          if (pv[w] == 0 && io[w] > 0 && !mbar_wait_warp(o_free(w), (io[w] - 1) & 1)) return false;
+          tc_fence_after();
+          const uint32_t pt = tmem + 384 + 64 * w, ot = tmem + 256 + 64 * w;
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < WT / 16; ++kk)
+              tc_mma_f16_ts(ot, pt + kk * 8, smem_desc_sw128(vb + kk * 2048, 8192, 1024), idesc_o,
+                            (pv[w] > 0 || kk > 0) ? 1u : 0u);
+            tc_commit(p_free(w));
+            if (kt == t) tc_commit(o_full(w));  // the diagonal tile is a row's last
+          }
+          __syncwarp();
+          ++gp[w];
+          ++pv[w];
+        }
+        if (elect_one()) tc_commit(kv_empty + 8 * st);
+        __syncwarp();
+        return true;
+      };
+      for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items && ok;
+           k = wa_rank(blockIdx.x, ++rd), ++it) {
+        const WaItem m(a, k);
+        const uint32_t qb = it & 1;
+        pv[0] = pv[1] = 0;
+        if (!mbar_wait_warp(q_full + 8 * qb, (it >> 1) & 1)) break;
+        tc_fence_after();
+        for (int j = 0; j < m.n && ok; ++j) {
+          const uint32_t st = (G + j) % WA_STAGES;
+          if (!mbar_wait_warp(kv_full + 8 * st, ((G + j) / WA_STAGES) & 1)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t ks = sbase + WA_OFF_KV + st * 2 * WA_T_BYTES;
+          const int kt = m.tile(j);
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            if (!a.w.sees(2 * m.u + w, kt)) continue;
+            if (gs[w] > 0 && !mbar_wait_warp(s_free(w), (gs[w] - 1) & 1)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t qs = sbase + (2 * qb + w) * WA_T_BYTES;
+            if (elect_one()) {
+#pragma unroll
+              for (int kk = 0; kk < WA_D / 16; ++kk)
+                tc_mma_f16(tmem + 128 * w, smem_desc_sw128(qs + kk * 32, 16, 1024),
+                           smem_desc_sw128(ks + kk * 32, 16, 1024), idesc_s, kk ? 1u : 0u);
+              tc_commit(s_full(w));
+            }
+            __syncwarp();
+            ++gs[w];
+          }
+          if (!ok) break;
+          if (j == m.n - 1) {
+            if (elect_one()) tc_commit(q_empty + 8 * qb);
+            __syncwarp();
+          }
+          if (j > 0 && !issue_pv(m, j - 1)) ok = false;
+        }
+        if (!ok || !issue_pv(m, m.n - 1)) break;
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+          if (pv[w] > 0) ++io[w];
+        G += m.n;
+      }
+      if (elect_one()) tc_commit(done);
+      __syncwarp();
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(WA_REGS_ROWS));
+    // ------------------------------------------------------------ softmax
+    const int w = (warp - 4) >> 2;  // group: query tile A (0) or B (1)
+    const int q4 = warp & 3;         // TMEM lane quarter
+    const int r = q4 * 32 + lane;    // query row in the tile = TMEM lane
+    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
+    const uint32_t ts = tl + 128 * w, to = tl + 256 + 64 * w, tp = tl + 384 + 64 * w;
+    bool ok = true;
+    uint32_t g = 0, io = 0;
+    for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items && ok;
+         k = wa_rank(blockIdx.x, ++rd)) {
+      const WaItem m(a, k);
+      const int t = 2 * m.u + w;
+      if (t >= a.w.n_t) continue;
+      const int q = t * WT + r;  // query index in the sequence
+      float mref = -INFINITY, l = 0.f;
+      bool first = true;
+      for (int j = 0; j < m.n; ++j) {
+        const int kt = m.tile(j);
+        if (!a.w.sees(t, kt)) continue;
+        if (!mbar_wait_warp(s_full(w), g & 1)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        // the row's scores into registers; then the next scores may replace them
+        uint32_t sc[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) tmem_ld32_async(ts + c, sc + c);
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) tmem_wait_ld(sc + c);
+        tc_fence_before();
+        mbar_arrive_warp(s_free(w));
+        if (kt == t) {  // the diagonal
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c > r) sc[c] = 0xff800000u;  // -inf
+        }
+        if (!a.w.inside(t, kt)) {  // keys that the window has passed
+          const int low = q - a.w.W + 1 - kt * WT, sk = a.w.S - kt * WT;
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c < low && c >= sk) sc[c] = 0xff800000u;
+        }
+        // the row maximum (log2 units), three-input maxima
+        float mt;
+        {
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < 128; c += 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              mx[i] = max3f(mx[i], __uint_as_float(sc[c + 2 * i]),
+                            __uint_as_float(sc[c + 2 * i + 1]));
+          mt = fmaxf(max3f(mx[0], mx[1], mx[2]), mx[3]) * a.sl2;
+        }
+        // the first keys set the reference; later ones raise it only by more than
+        // WA_RESCALE, scaling O and the running sum
+        float corr = 1.f, mnew = mref;
+        if (mt > mref + WA_RESCALE) {
+          mnew = mt;
+          if (mref != -INFINITY) corr = ex2_approx(mref - mnew);
+        }
+        // P_w of the previous tile has been consumed (and O_w updated) by
+        // the time this wait returns; a new item waited on o_full instead
+        if (!first && !mbar_wait_warp(p_free(w), (g - 1) & 1)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        // P = 2^(s * sl2 - m) into TMEM as bf16 pairs (key 2c, 2c + 1 in
+        // column c) and the row sum, with packed fp32x2 arithmetic
+        float2 ps = make_float2(0.f, 0.f);
+        {
+          const float ref = mnew == -INFINITY ? 0.f : mnew;
+          const float2 sl = make_float2(a.sl2, a.sl2), nm = make_float2(-ref, -ref);
+#pragma unroll
+          for (int hh = 0; hh < 4; ++hh) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) {
+              const float2 z = __ffma2_rn(make_float2(__uint_as_float(sc[32 * hh + c]),
+                                                      __uint_as_float(sc[32 * hh + c + 1])),
+                                          sl, nm);
+              const float2 pp = make_float2(ex2_approx(z.x), ex2_approx(z.y));
+              ps = __fadd2_rn(ps, pp);
+              pk[c >> 1] = pack_bf16(pp.x, pp.y);
+            }
+            tmem_st16(tp + 16 * hh, pk);
+          }
+        }
+        const float psum = ps.x + ps.y;
+        if (__any_sync(0xffffffffu, corr != 1.f)) {  // rescale this warp's rows of O
+#pragma unroll 1
+          for (int c = 0; c < 64; c += 16) {
+            uint32_t ov[16];
+            tmem_ld16(to + c, ov);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr);
+            tmem_st16(to + c, ov);
+          }
+        }
+        l = fmaf(l, corr, psum);
+        mref = mnew;
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive_warp(p_full(w));
+        ++g;
+        first = false;
+      }
+      if (!ok) break;
+      // the item's O: after its last P.V
+      if (!mbar_wait_warp(o_full(w), io & 1)) break;
+      ++io;
+      tc_fence_after();
+      uint32_t ov[64];
+      tmem_ld32_async(to, ov);
+      tmem_ld32_async(to + 32, ov + 32);
+      tmem_wait_ld(ov);
+      tmem_wait_ld(ov + 32);
+      tc_fence_before();
+      mbar_arrive_warp(o_free(w));
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      // the warp's 32 rows through its own stage (16-byte piece p of row i at piece
+      // p ^ (i & 7)), so that 8 lanes store a row's 128 bytes
+      uint8_t* const stg = smem + WA_OFF_STG + (warp - 4) * 4096;
+      const int q0 = t * WT + q4 * 32;
+#pragma unroll
+      for (int i = 0; i < WA_D; i += 8) {
+        const float* o = reinterpret_cast<const float*>(ov + i);
+        *reinterpret_cast<uint4*>(stg + lane * 128 + (((i >> 3) ^ (lane & 7)) << 4)) =
+            make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
+                       pack_bf16(o[4] * inv, o[5] * inv), pack_bf16(o[6] * inv, o[7] * inv));
+      }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        const int rr = i + (lane >> 3), p = lane & 7;
+        const uint4 v = *reinterpret_cast<const uint4*>(stg + rr * 128 + ((p ^ (rr & 7)) << 4));
+        if (q0 + rr < a.w.L)
+          *reinterpret_cast<uint4*>(a.out + ((long)m.b * a.w.L + q0 + rr) * a.ldo + m.h * WA_D +
+                                    p * 8) = v;
+      }
+      __syncwarp();
+      if (a.lse && q < a.w.L)
+        a.lse[((long)m.b * a.H + m.h) * a.w.L + q] = mref + log2f(l);  // log2 units
+    }
+  }
+  tc_fence_before();
+  if (__syncthreads_or(*(volatile int*)&g_dev_error != 0)) {
+    // error path: let this CTA's copies and MMAs land before smem / TMEM go
+    if (warp == 0 && lane == 0) {
+      for (uint32_t G = kv_issued > WA_STAGES ? kv_issued - WA_STAGES : 0; G < kv_issued; ++G)
+        mbar_wait_drain(kv_full + 8 * (G % WA_STAGES), (G / WA_STAGES) & 1);
+      for (uint32_t t = q_issued > 2 ? q_issued - 2 : 0; t < q_issued; ++t)
+        mbar_wait_drain(q_full + 8 * (t & 1), (t >> 1) & 1);
+    }
+    if (warp == 1 && lane == 0) mbar_wait_drain(done, 0);
+  } else if (warp == 1 && lane == 0) {
+    mbar_wait(done, 0);
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, WA_TMEM_COLS);
+  }
+}
+
+// The registers that the softmax warps ask for (setmaxnreg) must be in the block's
+// pool, which holds what it was launched with: else they would wait for ever.
+cudaError_t wa_registers_ok() {
+  static std::atomic<int> regs{0};  // a constant of the binary
+  int n = regs.load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaFuncAttributes at;
+    const cudaError_t e = cudaFuncGetAttributes(&at, window_fwd_kernel);
+    if (e != cudaSuccess) return e;
+    regs.store(n = at.numRegs, std::memory_order_relaxed);
+  }
+  return n * WA_THREADS >= WA_REGS_CTRL * 128 + WA_REGS_ROWS * 256 ? cudaSuccess
+                                                                    : cudaErrorInvalidConfiguration;
+}
+
+}  // namespace
+
+double window_pairs(const Window& c) {
+  const double L = c.L, W = c.window > 0 ? std::min(c.window, c.L) : c.L;
+  const double S = std::min<double>(c.sinks, L - W);
+  // the window's triangle and band, and the sinks that lie below it, coming into sight one by one
+  return W * (W + 1) / 2 + (L - W) * W + S * (S + 1) / 2 + (L - W - S) * S;
+}
+
+cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, float* lse,
+                       cudaStream_t st) {
+  CUtensorMap tq, tk, tv;
+  if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WA_D, c.L, c.B, x.ldq, WA_D, WT) ||
+      !tmap_bf16_seq(&tk, x.k, (uint64_t)c.KV * WA_D, c.L, c.B, x.ldk, WA_D, WT) ||
+      !tmap_bf16_seq(&tv, x.v, (uint64_t)c.KV * WA_D, c.L, c.B, x.ldv, WA_D, WT))
+    return cudaErrorInvalidValue;
+  WaArgs a{};
+  a.out = out;
+  a.lse = lse;
+  a.ldo = ldo;
+  a.B = c.B;
+  a.H = c.H;
+  a.g = c.H / c.KV;
+  a.w = WinTiles(c);
+  a.n_st = (a.w.n_t + 1) / 2;
+  const long items = (long)a.n_st * c.H * c.B;
+  if (items > 0x3fffffff) return cudaErrorInvalidValue;
+  a.n_items = (int)items;
+  a.sl2 = 1.4426950408889634f / sqrtf((float)WA_D);
+  cudaError_t e = wa_registers_ok();
+  if (e != cudaSuccess) return e;
+  e = cudaFuncSetAttribute(window_fwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WA_SMEM);
+  if (e != cudaSuccess) return e;
+  const double pairs = (double)c.B * c.H * window_pairs(c);
+  LaunchTimer lt("window_fwd", st, 4.0 * WA_D * pairs,
+                 2.0 * c.B * c.L * WA_D * (2.0 * c.H + 2.0 * c.KV) + 4.0 * c.B * c.H * c.L);
+  const int grid = std::min(a.n_items, num_sms());
+  return launch_kernel(window_fwd_kernel, grid, WA_THREADS, WA_SMEM, st, tq, tk, tv, a);
+}
+
+}  // namespace pf

@@ -1,0 +1,666 @@
+// Backward of the windowed attention with sinks on the tcgen05 tensor cores,
+// head width 64, grouped heads.  With P = softmax(q k / 8) recomputed from the
+// saved LSE and Di = rowsum(dO * O):
+//   dP = dO V^T,   dS = P * (dP - Di),   dV = P^T dO,   dK = dS^T Q / 8,
+//   dQ = dS K / 8,   dK and dV summed over the query heads of a key head.
+// Two kernels share one skeleton (no atomics, deterministic):
+//   DKDV: stationary X1 = K, X2 = V of a 128-key tile; streamed Y1 = Q_j, Y2 =
+//         dO_j of the query tiles that see it, one query head of the group
+//         after the other, into the same accumulators
+//           T1 = X1 Y1^T = S^T,  T2 = X2 Y2^T = dP^T     (TMEM, M=128 N=128)
+//           E1 = P^T, E2 = dS^T  (bf16, written to TMEM by the row warps)
+//           dV += E1 Y2,  dK += E2 Y1    (A from TMEM; TMEM accumulators)
+//   DQ:   stationary X1 = Q, X2 = dO of a 128-query tile and head; streamed
+//         Y1 = K_j, Y2 = V_j of the sinks' and the window's tiles
+//           T1 = S,  T2 = dP,  E2 = dS,  dQ += E2 Y1
+// Roles: warp 0 TMA producer (DKDV: it also stages each step's (LSE, Di)
+// pairs of the streamed queries in shared memory), warp 1 MMA issuer, warps
+// 2-17 the row warps: four per TMEM lane quarter, each thread one row (TMEM
+// lane) and one quarter of the 128 streamed columns.
+// The sinks are seen by every later query: a key tile's steps are cut into
+// pieces of at most `C` steps, so that a sink tile of a long sequence (and, in
+// a short one, any tile) is shared by several CTAs.  Pieces of a cut tile
+// leave fp32 sums; window_join_kernel adds them in order.
+// Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the
+// end of a sequence read as zero.
+#include <algorithm>
+#include <type_traits>
+
+#include "local.h"
+#include "window_tiles.cuh"
+
+namespace pf {
+
+int take_dev_error_window_attn_bwd() { return take_dev_error_tu(); }
+int set_wait_limit_window_attn_bwd(unsigned long long ns) { return set_wait_limit_tu(ns); }
+
+namespace {
+
+constexpr int WB_D = 64;   // head width
+constexpr int WB_STAGES = 4;
+constexpr int WB_ROW_THREADS = 512;  // warps 2-17
+constexpr int WB_THREADS = 64 + WB_ROW_THREADS;
+constexpr uint32_t WB_T_BYTES = WT * WB_D * 2;  // 16 KB per tile
+constexpr uint32_t WB_OFF_Y = 2 * 2 * WB_T_BYTES;                     // X: [2 bufs][X1, X2]
+constexpr uint32_t WB_OFF_LD = WB_OFF_Y + WB_STAGES * 2 * WB_T_BYTES;  // Y: [stage][Y1, Y2]
+constexpr uint32_t WB_OFF_BAR = WB_OFF_LD + WB_STAGES * WT * 8;        // (lse, Di) [stage][128]
+constexpr uint32_t WB_SMEM = WB_OFF_BAR + 256 + 1024;
+// TMEM columns: T1 at 0, T2 at 128 (fp32), accumulators at 256 (dV or dQ) and 320
+// (dK), E1 at 384, E2 at 448 (bf16 pairs: streamed column c in 32-bit column c / 2)
+constexpr uint32_t WB_TMEM_COLS = 512;
+constexpr uint32_t WB_TM_E = 384;
+constexpr int WB_ACC = 2 * WB_D;  // dV | dK of a key
+
+struct WbArgs {
+  bf16 *out_u, *out_w;  // DKDV: dV, dK; DQ: dQ.  Head h at column 64 h
+  long ld_u, ld_w;
+  const float* lse;  // [B, H, L], log2 units
+  const float* Di;   // [B, H, L]
+  int B, H, KV, g;
+  WinTiles w;
+  // DKDV: steps of a piece, pieces of a sink tile and of another tile, and the
+  // pieces' sums [piece][128][dV | dK], fp32
+  int C, np_s, np_w;
+  float* part;
+  int n_items;
+  float sl2, scale;
+};
+
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Snake order over the CTAs of items ranked heaviest first.
+__device__ __forceinline__ int wb_rank(int c, int round) {
+  return round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - c : c);
+}
+
+// Query tiles that see key tile t: [t, t + wb_queries(t)).
+__host__ __device__ __forceinline__ int wb_queries(const WinTiles& w, int t) {
+  return (t < w.sT ? w.n_t - 1 : w.last_q(t)) - t + 1;
+}
+
+// Item k: stationary tile t of sequence b, its n steps, and head h (DKDV: the key
+// head; DQ: the query head).  Step j streams
+//   DKDV: query tile t + (s0 + j) % nq of the group's head (s0 + j) / nq
+//   DQ:   key tile j < ns ? j : lo + j - ns
+template <bool DKDV>
+struct WbItem {
+  int t, h, b, n;
+  int s0, nq, piece;  // DKDV; piece < 0: the tile is not cut
+  int ns, lo;         // DQ
+  __device__ __forceinline__ WbItem(const WbArgs& a, int k) {
+    if (DKDV) {
+      const int per = a.KV * a.B, sinks = a.w.sT * a.np_s * per;
+      int p;
+      piece = k;
+      if (k < sinks) {
+        p = k / per % a.np_s;
+        t = k / per / a.np_s;
+      } else {
+        p = (k - sinks) / per % a.np_w;
+        t = a.w.sT + (k - sinks) / per / a.np_w;
+      }
+      if ((t < a.w.sT ? a.np_s : a.np_w) == 1) piece = -1;
+      h = k % per % a.KV;  // `sinks` is a multiple of per
+      b = k % per / a.KV;
+      nq = wb_queries(a.w, t);
+      s0 = p * a.C;
+      n = max(0, min(nq * a.g - s0, a.C));
+      ns = lo = 0;
+    } else {
+      const int per = a.H * a.B;
+      t = a.w.n_t - 1 - k / per;
+      h = k % per % a.H;
+      b = k % per / a.H;
+      lo = a.w.lo(t);
+      ns = min(a.w.sT, lo);
+      n = ns + t - lo + 1;
+      s0 = nq = 0;
+      piece = -1;
+    }
+  }
+  __device__ __forceinline__ int tile(int j) const {
+    return DKDV ? t + (s0 + j) % nq : j < ns ? j : lo + j - ns;
+  }
+  __device__ __forceinline__ int head(const WbArgs& a, int j) const {  // of the streamed tile
+    return DKDV ? h * a.g + (s0 + j) / nq : h / a.g;
+  }
+};
+
+template <bool DKDV>
+__global__ void __launch_bounds__(WB_THREADS, 1)
+    window_bwd_kernel(const __grid_constant__ CUtensorMap tmX1, const __grid_constant__ CUtensorMap tmX2,
+                      const __grid_constant__ CUtensorMap tmY1, const __grid_constant__ CUtensorMap tmY2,
+                      WbArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~uintptr_t(1023));
+  const uint32_t b0 = smem_u32(smem + WB_OFF_BAR);
+  // x_full[2] x_empty[2] y_full[S] y_empty[S] t_full t_free e_full e_free acc_full
+  // acc_free done
+  const uint32_t x_full = b0, x_empty = b0 + 16, y_full = b0 + 32,
+                 y_empty = y_full + 8 * WB_STAGES, t_full = y_empty + 8 * WB_STAGES,
+                 t_free = t_full + 8, e_full = t_free + 8, e_free = e_full + 8,
+                 acc_full = e_free + 8, acc_free = acc_full + 8, done = acc_free + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + WB_OFF_BAR + 240);
+  const uint32_t sbase = smem_u32(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(x_full + 8 * i, 1);
+      mbar_init(x_empty + 8 * i, 1);
+    }
+    mbar_init(t_full, 1);
+    mbar_init(t_free, WB_ROW_THREADS / 32);  // one arrival per row warp
+    mbar_init(e_full, WB_ROW_THREADS / 32);
+    mbar_init(e_free, 1);
+    for (int i = 0; i < WB_STAGES; ++i) {
+      mbar_init(y_full + 8 * i, 1);
+      mbar_init(y_empty + 8 * i, 1);
+    }
+    mbar_init(acc_full, 1);
+    mbar_init(acc_free, WB_ROW_THREADS / 32);
+    mbar_init(done, 1);
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), WB_TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_enter();  // the setup above overlaps the kernel before this one
+  uint32_t y_issued = 0, x_issued = 0;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ producer
+    // Lane 0 issues the copies.  DKDV: the whole warp also stages the (lse,
+    // Di) pairs of each step's 128 streamed queries in the stage's slot before
+    // lane 0 arms the stage's full barrier, so that the row warps read them
+    // after that barrier (the next step's are loaded one step ahead, four
+    // queries per lane).
+    if (lane == 0) {
+      prefetch_tmap(&tmX1);
+      prefetch_tmap(&tmX2);
+      prefetch_tmap(&tmY1);
+      prefetch_tmap(&tmY2);
+    }
+    float2* ld_ring = reinterpret_cast<float2*>(smem + WB_OFF_LD);
+    float2 ldp[WT / 32];  // next step's pairs of queries lane + 32 i
+    auto fetch_step = [&](const WbItem<DKDV>& m, int j) {
+      const int q0 = m.tile(j) * WT;
+      const long o = ((long)m.b * a.H + m.head(a, j)) * a.w.L + q0;
+#pragma unroll
+      for (int i = 0; i < WT / 32; ++i) {
+        const int c = lane + 32 * i;
+        ldp[i] = q0 + c < a.w.L ? make_float2(a.lse[o + c], a.Di[o + c]) : make_float2(0.f, 0.f);
+      }
+    };
+    int k = wb_rank(blockIdx.x, 0);
+    if (DKDV && k < a.n_items) {
+      const WbItem<DKDV> m(a, k);
+      if (m.n) fetch_step(m, 0);
+    }
+    bool ok = true;
+    uint32_t it = 0;
+    for (int rd = 0; k < a.n_items && ok; k = wb_rank(blockIdx.x, ++rd)) {
+      const WbItem<DKDV> m(a, k);
+      const int k2 = wb_rank(blockIdx.x, rd + 1);
+      if (m.n == 0) {
+        if (DKDV && k2 < a.n_items) {
+          const WbItem<DKDV> m2(a, k2);
+          if (m2.n) fetch_step(m2, 0);
+        }
+        continue;
+      }
+      const uint32_t xb = it & 1;
+      if (!mbar_wait_warp(x_empty + 8 * xb, ((it >> 1) & 1) ^ 1)) break;
+      if (lane == 0) {
+        const uint32_t xdst = sbase + xb * 2 * WB_T_BYTES;
+        mbar_arrive_expect_tx(x_full + 8 * xb, 2 * WB_T_BYTES);
+        tma_load_3d(xdst, &tmX1, x_full + 8 * xb, m.h * WB_D, m.t * WT, m.b);
+        tma_load_3d(xdst + WB_T_BYTES, &tmX2, x_full + 8 * xb, m.h * WB_D, m.t * WT, m.b);
+      }
+      x_issued = ++it;
+      for (int j = 0; j < m.n; ++j) {
+        const uint32_t G = y_issued, st = G % WB_STAGES;
+        if (!mbar_wait_warp(y_empty + 8 * st, ((G / WB_STAGES) & 1) ^ 1)) {
+          ok = false;
+          break;
+        }
+        if (DKDV) {
+#pragma unroll
+          for (int i = 0; i < WT / 32; ++i) ld_ring[st * WT + 32 * i + lane] = ldp[i];
+          __syncwarp();
+        }
+        if (lane == 0) {
+          const uint32_t ydst = sbase + WB_OFF_Y + st * 2 * WB_T_BYTES;
+          const int yrow = m.tile(j) * WT, ycol = m.head(a, j) * WB_D;
+          mbar_arrive_expect_tx(y_full + 8 * st, 2 * WB_T_BYTES);
+          tma_load_3d(ydst, &tmY1, y_full + 8 * st, ycol, yrow, m.b);
+          tma_load_3d(ydst + WB_T_BYTES, &tmY2, y_full + 8 * st, ycol, yrow, m.b);
+        }
+        y_issued = G + 1;
+        if (DKDV) {  // the pairs of the next step (this item's or the next item's first)
+          if (j + 1 < m.n) {
+            fetch_step(m, j + 1);
+          } else if (k2 < a.n_items) {
+            const WbItem<DKDV> m2(a, k2);
+            if (m2.n) fetch_step(m2, 0);
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    // The whole warp runs the loop; one elected lane issues and commits.
+    constexpr uint32_t idesc_t = idesc_bf16_f32(WT, WT, 0, 0);
+    constexpr uint32_t idesc_a = idesc_bf16_f32(WT, WB_D, 0, 1);
+    bool ok = true;
+    uint32_t it = 0, G = 0;
+    // accumulate step G (local step j of its item): E_G times the step's Y tiles
+    auto acc_step = [&](uint32_t G_, int j, uint32_t it_) -> bool {
+      const uint32_t st = G_ % WB_STAGES;
+      if (!mbar_wait_warp(e_full, G_ & 1)) return false;
+      if (j == 0 && !mbar_wait_warp(acc_free, (it_ & 1) ^ 1)) return false;
+      tc_fence_after();
+      const uint32_t e1 = tmem + WB_TM_E, e2 = e1 + WT / 2;
+      const uint32_t y1 = sbase + WB_OFF_Y + st * 2 * WB_T_BYTES, y2 = y1 + WB_T_BYTES;
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < WT / 16; ++kk) {
+          const uint32_t acc = (j > 0 || kk > 0) ? 1u : 0u;
+          const uint64_t bd1 = smem_desc_sw128(y1 + kk * 2048, 8192, 1024);
+          if (DKDV) {
+            const uint64_t bd2 = smem_desc_sw128(y2 + kk * 2048, 8192, 1024);
+            tc_mma_f16_ts(tmem + 256, e1 + kk * 8, bd2, idesc_a, acc);  // dV += P^T dO
+            tc_mma_f16_ts(tmem + 320, e2 + kk * 8, bd1, idesc_a, acc);  // dK += dS^T Q
+          } else {
+            tc_mma_f16_ts(tmem + 256, e2 + kk * 8, bd1, idesc_a, acc);  // dQ += dS K
+          }
+        }
+        tc_commit(e_free);
+        tc_commit(y_empty + 8 * st);
+      }
+      __syncwarp();
+      return true;
+    };
+    for (int rd = 0, k = wb_rank(blockIdx.x, 0); k < a.n_items && ok;
+         k = wb_rank(blockIdx.x, ++rd)) {
+      const WbItem<DKDV> m(a, k);
+      if (m.n == 0) continue;
+      const uint32_t xb = it & 1;
+      if (!mbar_wait_warp(x_full + 8 * xb, (it >> 1) & 1)) break;
+      tc_fence_after();
+      const uint32_t x1 = sbase + xb * 2 * WB_T_BYTES, x2 = x1 + WB_T_BYTES;
+      for (int j = 0; j < m.n; ++j) {
+        const uint32_t Gj = G + j, st = Gj % WB_STAGES;
+        if (!mbar_wait_warp(y_full + 8 * st, (Gj / WB_STAGES) & 1) ||
+            !mbar_wait_warp(t_free, (Gj & 1) ^ 1)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t y1 = sbase + WB_OFF_Y + st * 2 * WB_T_BYTES, y2 = y1 + WB_T_BYTES;
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < WB_D / 16; ++kk) {
+            tc_mma_f16(tmem, smem_desc_sw128(x1 + kk * 32, 16, 1024),
+                       smem_desc_sw128(y1 + kk * 32, 16, 1024), idesc_t, kk ? 1u : 0u);
+            tc_mma_f16(tmem + WT, smem_desc_sw128(x2 + kk * 32, 16, 1024),
+                       smem_desc_sw128(y2 + kk * 32, 16, 1024), idesc_t, kk ? 1u : 0u);
+          }
+          tc_commit(t_full);
+          if (j == m.n - 1) tc_commit(x_empty + 8 * xb);
+        }
+        __syncwarp();
+        if (j > 0 && !acc_step(Gj - 1, j - 1, it)) {
+          ok = false;
+          break;
+        }
+      }
+      if (!ok || !acc_step(G + m.n - 1, m.n - 1, it)) break;
+      if (elect_one()) tc_commit(acc_full);
+      __syncwarp();
+      G += m.n;
+      ++it;
+    }
+    if (elect_one()) tc_commit(done);
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ row warps
+    const int q4 = warp & 3;
+    const int r = q4 * 32 + lane;  // stationary row in the tile = TMEM lane
+    const int ch = (warp - 2) >> 2;   // quarter of the streamed columns: [32 ch, 32 ch + 32)
+    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
+    const float2* ld_ring = reinterpret_cast<const float2*>(smem + WB_OFF_LD);  // [stage][128]
+    bool ok = true;
+    uint32_t G = 0, it = 0;
+    for (int rd = 0, k = wb_rank(blockIdx.x, 0); k < a.n_items && ok;
+         k = wb_rank(blockIdx.x, ++rd)) {
+      const WbItem<DKDV> m(a, k);
+      if (m.n == 0) continue;
+      const int row = m.t * WT + r;  // key (DKDV) or query (DQ) index in the sequence
+      float lse_r = 0.f, di_r = 0.f;
+      if (!DKDV && row < a.w.L) {
+        const long o = ((long)m.b * a.H + m.h) * a.w.L + row;
+        lse_r = a.lse[o];
+        di_r = a.Di[o];
+      }
+      for (int j = 0; j < m.n; ++j) {
+        const uint32_t Gj = G + j;
+        const int yt = m.tile(j), c0 = yt * WT;  // first streamed index of this step
+        // DKDV: the step's (lse, Di) pairs, staged by the producer before the
+        // stage's full barrier (already complete: the step's scores used it;
+        // the slot is refilled only after this step's E has been consumed)
+        if (DKDV && !mbar_wait(y_full + 8 * (Gj % WB_STAGES), (Gj / WB_STAGES) & 1)) {
+          ok = false;
+          break;
+        }
+        if (!mbar_wait(t_full, Gj & 1)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        uint32_t sa[32], pa[32];  // this thread's 32 columns of T1 and T2
+        tmem_ld32_async(tl + 32 * ch, sa);
+        tmem_ld32_async(tl + WT + 32 * ch, pa);
+        tmem_wait_ld(sa);
+        tmem_wait_ld(pa);
+        tc_fence_before();
+        mbar_arrive_warp(t_free);
+        // visible streamed columns: [lo, hi), and (DQ) the sinks below sk
+        int lo, hi, sk = 0;
+        if (DKDV) {  // the queries that see this key
+          lo = row - c0;
+          hi = min(row < a.w.S ? a.w.L : min(a.w.L, row + a.w.W), c0 + WT) - c0;
+        } else {  // the keys this query sees
+          lo = row - a.w.W + 1 - c0;
+          hi = row + 1 - c0;
+          sk = a.w.S - c0;
+        }
+        const float2* lds = ld_ring + (Gj % WB_STAGES) * WT;
+        // P and dS of the thread's 32 columns from kb on, as bf16 pairs
+        auto emit = [&](auto masked, int kb, uint32_t* pk, uint32_t* dk) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const uint32_t* sv = sa + g * 8;
+            const uint32_t* dv = pa + g * 8;
+            // (lse, Di) of two columns per 128-bit shared load (DKDV); packed fp32x2
+            // arithmetic on column pairs (each lane an IEEE fp32 operation)
+            const float4* l4 = reinterpret_cast<const float4*>(lds + kb) + g * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int c = kb + g * 8 + 2 * e;
+              float2 nl = make_float2(-lse_r, -lse_r), nd = make_float2(-di_r, -di_r);
+              if (DKDV) {
+                const float4 v = l4[e];
+                nl = make_float2(-v.x, -v.z);
+                nd = make_float2(-v.y, -v.w);
+              }
+              const float2 z = __ffma2_rn(
+                  make_float2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1])),
+                  make_float2(a.sl2, a.sl2), nl);
+              float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
+              float2 ds = __fmul2_rn(
+                  p, __fadd2_rn(make_float2(__uint_as_float(dv[2 * e]), __uint_as_float(dv[2 * e + 1])),
+                                nd));
+              if (decltype(masked)::value) {
+                if ((c < lo && c >= sk) || c >= hi) p.x = ds.x = 0.f;
+                if ((c + 1 < lo && c + 1 >= sk) || c + 1 >= hi) p.y = ds.y = 0.f;
+              }
+              pk[4 * g + e] = pack_bf16(p.x, p.y);
+              dk[4 * g + e] = pack_bf16(ds.x, ds.y);
+            }
+          }
+        };
+        uint32_t pk[16], dk[16];  // this thread's 32 columns of E1 and E2
+        const int kb = 32 * ch;
+        if ((lo <= kb || sk >= kb + 32) && hi >= kb + 32)
+          emit(std::false_type{}, kb, pk, dk);
+        else
+          emit(std::true_type{}, kb, pk, dk);
+        if (!mbar_wait(e_free, (Gj & 1) ^ 1)) {  // the previous step's E has been read
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t te = tl + WB_TM_E + 16 * ch;
+        if (DKDV) tmem_st16(te, pk);
+        tmem_st16(te + WT / 2, dk);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive_warp(e_full);
+      }
+      if (!ok) break;
+      G += m.n;
+      // accumulators -> dK, dV (DKDV) or dQ (DQ) rows
+      if (!mbar_wait(acc_full, it & 1)) break;
+      ++it;
+      tc_fence_after();
+      uint32_t u0[16], w0[16];  // this thread's 16 columns of dV / dQ and of dK
+      tmem_ld16(tl + 256 + 16 * ch, u0);
+      if (DKDV) tmem_ld16(tl + 320 + 16 * ch, w0);
+      tc_fence_before();
+      mbar_arrive_warp(acc_free);
+      if (row < a.w.L) {
+        const long srow = (long)m.b * a.w.L + row;
+        auto store = [&](bf16* o, const uint32_t* v, float sc) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 8)
+            *reinterpret_cast<uint4*>(o + i) = make_uint4(
+                pack_bf16(__uint_as_float(v[i]) * sc, __uint_as_float(v[i + 1]) * sc),
+                pack_bf16(__uint_as_float(v[i + 2]) * sc, __uint_as_float(v[i + 3]) * sc),
+                pack_bf16(__uint_as_float(v[i + 4]) * sc, __uint_as_float(v[i + 5]) * sc),
+                pack_bf16(__uint_as_float(v[i + 6]) * sc, __uint_as_float(v[i + 7]) * sc));
+        };
+        if (DKDV && m.piece >= 0) {  // a cut tile's sums
+          float* o = a.part + ((long)m.piece * WT + r) * WB_ACC + 16 * ch;
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            *reinterpret_cast<uint4*>(o + i) = make_uint4(u0[i], u0[i + 1], u0[i + 2], u0[i + 3]);
+            *reinterpret_cast<uint4*>(o + WB_D + i) = make_uint4(w0[i], w0[i + 1], w0[i + 2], w0[i + 3]);
+          }
+        } else {
+          store(a.out_u + srow * a.ld_u + m.h * WB_D + 16 * ch, u0, DKDV ? 1.f : a.scale);
+          if (DKDV) store(a.out_w + srow * a.ld_w + m.h * WB_D + 16 * ch, w0, a.scale);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  if (__syncthreads_or(*(volatile int*)&g_dev_error != 0)) {
+    // error path: let this CTA's copies and MMAs land before smem / TMEM go
+    if (warp == 0 && lane == 0) {
+      for (uint32_t Gd = y_issued > WB_STAGES ? y_issued - WB_STAGES : 0; Gd < y_issued; ++Gd)
+        mbar_wait_drain(y_full + 8 * (Gd % WB_STAGES), (Gd / WB_STAGES) & 1);
+      for (uint32_t t = x_issued > 2 ? x_issued - 2 : 0; t < x_issued; ++t)
+        mbar_wait_drain(x_full + 8 * (t & 1), (t >> 1) & 1);
+    }
+    if (warp == 1 && lane == 0) mbar_wait_drain(done, 0);
+  } else if (warp == 1 && lane == 0) {
+    mbar_wait(done, 0);
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, WB_TMEM_COLS);
+  }
+}
+
+// Sums of a cut key tile's pieces, in order.  CTA (16 rows, key head and
+// sequence, tile): 8 threads to a row, 16 columns of dV | dK each.
+__global__ void __launch_bounds__(128) window_join_kernel(WbArgs a) {
+  pdl_enter();
+  const int per = a.KV * a.B, hb = blockIdx.y, h = hb % a.KV, b = hb / a.KV;
+  const int cut_s = a.np_s > 1 ? a.w.sT : 0;  // cut tiles: the sinks', or all
+  const int t = (a.np_s > 1 ? 0 : a.w.sT) + blockIdx.z;
+  const bool sink = (int)blockIdx.z < cut_s;
+  const int first = sink ? t * a.np_s * per + hb
+                         : a.w.sT * a.np_s * per + (t - a.w.sT) * a.np_w * per + hb;
+  const int n = (wb_queries(a.w, t) * a.g + a.C - 1) / a.C;  // the pieces that have steps
+  const int r = blockIdx.x * 16 + threadIdx.x / 8, c = threadIdx.x % 8 * 16, row = t * WT + r;
+  if (row >= a.w.L) return;
+  float v[16] = {};
+  for (int i = 0; i < n; ++i) {
+    const float4* p = reinterpret_cast<const float4*>(
+        a.part + ((long)(first + i * per) * WT + r) * WB_ACC + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float4 x = p[e];
+      v[4 * e] += x.x; v[4 * e + 1] += x.y; v[4 * e + 2] += x.z; v[4 * e + 3] += x.w;
+    }
+  }
+  const long srow = (long)b * a.w.L + row;
+  bf16* o = c < WB_D ? a.out_u + srow * a.ld_u + h * WB_D + c
+                     : a.out_w + srow * a.ld_w + h * WB_D + c - WB_D;
+  if (c >= WB_D)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= a.scale;
+  store8_bf16(o, v);
+  store8_bf16(o + 8, v + 8);
+}
+
+// Di = rowsum(dO * O) per (sequence, head, query): eight lanes per (row, head),
+// each eight of the head's 64 columns with 16-byte loads.
+__global__ void __launch_bounds__(256) window_dot_kernel(const bf16* __restrict__ dO, long lddo,
+                                                         const bf16* __restrict__ O, long ldo,
+                                                         float* __restrict__ Di, long rows, int L,
+                                                         int H) {
+  const int pz = pdl_enter();
+  const long gid = ((long)blockIdx.x * blockDim.x + threadIdx.x + pz) >> 3, items = rows * H;
+  const int sub = threadIdx.x & 7;
+  const bool live = gid < items;
+  const long it = live ? gid : items - 1, row = it / H;
+  const int h = (int)(it % H);
+  float x[8], y[8], v = 0.f;
+  load8_bf16(dO + row * lddo + h * WB_D + sub * 8, x);
+  load8_bf16(O + row * ldo + h * WB_D + sub * 8, y);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v = fmaf(x[k], y[k], v);
+#pragma unroll
+  for (int s = 4; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
+  if (live && sub == 0) Di[(row / L * H + h) * L + row % L] = v;
+}
+
+// How the key tiles' steps are cut.  A key tile of the window takes g * (W / 128
+// + 1) steps, one of the sinks g * n_t.  With fewer uncut tiles than SMs, every
+// tile is cut to half an SM's share of all steps; else only what is longer than
+// that and than a tile of the window.
+struct Cut {
+  int C, np_s, np_w;
+  long items;
+};
+Cut wb_cut(const Window& c) {
+  constexpr long SMS = 152;  // whatever the device has: the sums keep their order
+  const WinTiles w(c);
+  const int g = c.H / c.KV;
+  long steps = 0;
+  for (int t = 0; t < w.n_t; ++t) steps += wb_queries(w, t);
+  const long heads = (long)c.KV * c.B, share = std::max(1L, steps * g * heads / (2 * SMS));
+  long longest = 0;  // of the tiles that are not sinks
+  for (int t = w.sT; t < w.n_t; ++t) longest = std::max<long>(longest, (long)wb_queries(w, t) * g);
+  const bool few = w.n_t * heads < SMS;
+  Cut r;
+  r.C = (int)(few ? share : std::max(longest, share));
+  const long sink = w.sT > 0 ? (long)wb_queries(w, 0) * g : 1;
+  r.np_s = (int)((sink + r.C - 1) / r.C);
+  r.np_w = (int)std::max(1L, (longest + r.C - 1) / r.C);
+  r.items = heads * ((long)w.sT * r.np_s + (long)(w.n_t - w.sT) * r.np_w);
+  return r;
+}
+
+struct WbWs {
+  float *Di, *part;
+  size_t bytes;
+};
+WbWs wb_carve(void* ws, const Window& c) {
+  const Cut k = wb_cut(c);
+  auto up = [](size_t n) { return (n + 255) & ~size_t(255); };
+  WbWs r;
+  const size_t di = up((size_t)c.B * c.H * c.L * sizeof(float));
+  r.Di = static_cast<float*>(ws);
+  r.part = reinterpret_cast<float*>(static_cast<char*>(ws) + di);
+  // pieces are numbered as the items: those of tiles that are not cut hold nothing
+  const WinTiles w(c);
+  const long sinks = (long)c.KV * c.B * w.sT * k.np_s;
+  const long pieces = k.np_w > 1 ? k.items : k.np_s > 1 ? sinks : 0;
+  r.bytes = di + (size_t)pieces * WT * WB_ACC * sizeof(float) + 256;
+  return r;
+}
+
+template <bool DKDV>
+cudaError_t wb_launch(const CUtensorMap& x1, const CUtensorMap& x2, const CUtensorMap& y1,
+                      const CUtensorMap& y2, const WbArgs& a, const char* label, double flops,
+                      double bytes, cudaStream_t st) {
+  auto kern = window_bwd_kernel<DKDV>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, WB_SMEM);
+  if (e != cudaSuccess) return e;
+  LaunchTimer lt(label, st, flops, bytes);
+  return launch_kernel(kern, std::min(a.n_items, num_sms()), WB_THREADS, WB_SMEM, st, x1, x2, y1, y2,
+                       a);
+}
+
+}  // namespace
+
+size_t window_bwd_ws_bytes(const Window& c) { return wb_carve(nullptr, c).bytes; }
+
+cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long ldo,
+                       const float* lse, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
+                       cudaStream_t st) {
+  CUtensorMap tq, tk, tv, td;
+  if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WB_D, c.L, c.B, x.ldq, WB_D, WT) ||
+      !tmap_bf16_seq(&tk, x.k, (uint64_t)c.KV * WB_D, c.L, c.B, x.ldk, WB_D, WT) ||
+      !tmap_bf16_seq(&tv, x.v, (uint64_t)c.KV * WB_D, c.L, c.B, x.ldv, WB_D, WT) ||
+      !tmap_bf16_seq(&td, dout, (uint64_t)c.H * WB_D, c.L, c.B, lddo, WB_D, WT))
+    return cudaErrorInvalidValue;
+  const WbWs v = wb_carve(ws, c);
+  const Cut k = wb_cut(c);
+  WbArgs a{};
+  a.lse = lse;
+  a.Di = v.Di;
+  a.part = v.part;
+  a.B = c.B; a.H = c.H; a.KV = c.KV; a.g = c.H / c.KV;
+  a.w = WinTiles(c);
+  a.C = k.C; a.np_s = k.np_s; a.np_w = k.np_w;
+  a.scale = 1.0f / sqrtf((float)WB_D);
+  a.sl2 = a.scale * 1.4426950408889634f;
+  const long q_items = (long)a.w.n_t * c.H * c.B;
+  if (k.items > 0x3fffffff || q_items > 0x3fffffff) return cudaErrorInvalidValue;
+  const double rows = (double)c.B * c.L, pairs = (double)c.B * c.H * window_pairs(c);
+  cudaError_t e;
+  {
+    LaunchTimer lt("window_bwd_dot", st, 2.0 * rows * c.H * WB_D, rows * c.H * (4.0 * WB_D + 4.0));
+    const long n = (long)c.B * c.L;
+    e = launch_kernel(window_dot_kernel, (unsigned)((n * c.H * 8 + 255) / 256), 256, 0, st, dout, lddo,
+                      out, ldo, v.Di, n, c.L, c.H);
+    if (e != cudaSuccess) return e;
+  }
+  a.out_u = static_cast<bf16*>(dx.v);
+  a.ld_u = dx.ldv;
+  a.out_w = static_cast<bf16*>(dx.k);
+  a.ld_w = dx.ldk;
+  a.n_items = (int)k.items;
+  e = wb_launch<true>(tk, tv, tq, td, a, "window_bwd_dkdv", 8.0 * WB_D * pairs,
+                      2.0 * rows * WB_D * (2.0 * c.H + 4.0 * c.KV), st);
+  if (e != cudaSuccess) return e;
+  const int cut = (k.np_s > 1 ? a.w.sT : 0) + (k.np_w > 1 ? a.w.n_t - a.w.sT : 0);
+  if (cut > 0) {
+    LaunchTimer lt("window_bwd_join", st, 0.0, 0.0);
+    e = launch_kernel(window_join_kernel, dim3(WT / 16, c.KV * c.B, cut), 128, 0, st, a);
+    if (e != cudaSuccess) return e;
+  }
+  a.out_u = static_cast<bf16*>(dx.q);
+  a.ld_u = dx.ldq;
+  a.n_items = (int)q_items;
+  return wb_launch<false>(tq, td, tk, tv, a, "window_bwd_dq", 6.0 * WB_D * pairs,
+                          2.0 * rows * WB_D * (3.0 * c.H + 2.0 * c.KV), st);
+}
+
+}  // namespace pf

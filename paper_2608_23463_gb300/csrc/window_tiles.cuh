@@ -1,0 +1,43 @@
+// Which 128-row tiles of keys the 128-row tiles of queries see, for causal
+// attention in a sliding window with sinks (window_attn.cu, window_attn_bwd.cu).
+#pragma once
+
+#include "local.h"
+
+namespace pf {
+
+constexpr int WT = 128;  // rows of a tile
+
+struct WinTiles {
+  int L, W, S;  // length; window (L: no limit); sinks below the window
+  int n_t, sT;  // tiles of the sequence, and those that hold sinks
+  WinTiles() = default;
+  explicit WinTiles(const Window& c) {
+    L = c.L;
+    W = c.window > 0 && c.window < c.L ? c.window : c.L;
+    S = W < L ? (c.sinks < L ? c.sinks : L) : 0;  // a window of everything holds the sinks
+    n_t = (L + WT - 1) / WT;
+    sT = (S + WT - 1) / WT;
+  }
+  // first tile of the window of query tile t
+  __host__ __device__ __forceinline__ int lo(int t) const {
+    const int k = t * WT - W + 1;
+    return k > 0 ? k / WT : 0;
+  }
+  // last query tile with key tile t in its window
+  __host__ __device__ __forceinline__ int last_q(int t) const {
+    const long q = ((long)t * WT + WT - 1 + W - 1) / WT;
+    return q < n_t - 1 ? (int)q : n_t - 1;
+  }
+  // some query of tile t sees some key of tile kt
+  __host__ __device__ __forceinline__ bool sees(int t, int kt) const {
+    return t < n_t && kt <= t && (kt >= lo(t) || kt < sT);
+  }
+  // every query of tile t that is not before the keys of tile kt has them in its
+  // window or among the sinks
+  __host__ __device__ __forceinline__ bool inside(int t, int kt) const {
+    return kt * WT > t * WT + WT - 1 - W || kt * WT + WT <= S;
+  }
+};
+
+}  // namespace pf

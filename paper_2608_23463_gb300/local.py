@@ -1,6 +1,7 @@
 """Attention of the local stream (PyTorch holds memory).
 
-``QKRope`` norms and rotates queries and keys (``pf_qk_rope_*``) and
+``QKRope`` norms and rotates queries and keys (``pf_qk_rope_*``), ``WindowAttention``
+is causal attention in a sliding window with sinks (``pf_window_attn_*``) and
 ``PagedKVCache`` keeps the keys and values of many sequences in pages
 (``pf_paged_*``): ``append`` writes new tokens' rows, ``attend`` is the attention
 of every sequence's newest token.  All calls run on the current CUDA stream;
@@ -14,9 +15,10 @@ from typing import Optional, Sequence, Tuple
 import torch
 
 from . import (PF_BF16, PF_ERR_CAPACITY, PF_ERR_INVALID_ARG, PF_F32, PagedCache, PagedDesc,
-               ProxyFormerError, QKDesc, _ptr, pf_paged_advance, pf_paged_append, pf_paged_attn,
-               pf_paged_attn_workspace_size, pf_qk_rope_bwd, pf_qk_rope_fwd,
-               pf_qk_rope_workspace_size, qkv)
+               ProxyFormerError, QKDesc, WindowDesc, _ptr, pf_paged_advance, pf_paged_append,
+               pf_paged_attn, pf_paged_attn_workspace_size, pf_qk_rope_bwd, pf_qk_rope_fwd,
+               pf_qk_rope_workspace_size, pf_window_attn_bwd, pf_window_attn_fwd,
+               pf_window_attn_workspace_size, qkv)
 
 
 def _stream() -> int:
@@ -98,6 +100,56 @@ class QKRope:
                        _ints("pos", pos, rows, self.n_axes), qkv(dq, dk), qkv(xq, xk), dw_q, dw_k,
                        self.ws, 0 if self.ws is None else self.ws.numel(), _stream())
         return xq, xk, dw_q, dw_k
+
+
+class WindowAttention:
+    """Causal attention of ``batch`` sequences of L rows: row i sees the last ``window``
+    rows up to itself (0: all) and the first ``n_sink``.  bf16, head width 64."""
+
+    def __init__(self, batch: int, L: int, n_heads: int, n_kv: int, dh: int = 64, window: int = 0,
+                 n_sink: int = 0):
+        self.rows, self.nq, self.nk = batch * L, n_heads * dh, n_kv * dh
+        self.desc = WindowDesc(batch, L, n_heads, n_kv, dh, window, n_sink)
+        self.lse_shape = (batch, n_heads, L)
+        self.lse: Optional[torch.Tensor] = None  # of the last forward for training
+        self.ws: Optional[torch.Tensor] = None
+
+    def _qkv(self, q, k, v):
+        w, bf = self.rows, torch.bfloat16
+        return tuple(_rows(n, t, w, c, bf) for n, t, c in (("q", q, self.nq), ("k", k, self.nk),
+                                                           ("v", v, self.nk)))
+
+    def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, train: bool = True,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """q [batch*L, n_heads*dh], k, v [batch*L, n_kv*dh] -> [batch*L, n_heads*dh];
+        ``train`` keeps the rows' log-sums for the backward."""
+        q, k, v = self._qkv(q, k, v)
+        out = torch.empty((self.rows, self.nq), dtype=q.dtype, device=q.device) if out is None else \
+            _rows("out", out, self.rows, self.nq, q.dtype)
+        if train:  # a new buffer: the last forward's may still be read on another stream
+            self.lse = torch.empty(self.lse_shape, dtype=torch.float32, device=q.device)
+        pf_window_attn_fwd(self.desc, qkv(q, k, v), out, out.stride(0), self.lse if train else None,
+                           _stream())
+        return out
+
+    def backward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                 dout: torch.Tensor, lse: Optional[torch.Tensor] = None, into=None):
+        """From the forward's inputs and result and the gradient of the result: the
+        gradients of q, k and v (into ``into``, three matrices, if given).  lse: the
+        forward's ``self.lse``, if another forward has run since."""
+        q, k, v = self._qkv(q, k, v)
+        out, dout = (_rows(n, t, self.rows, self.nq, q.dtype) for n, t in (("out", out), ("dout", dout)))
+        lse = self.lse if lse is None else lse
+        if lse is None:
+            raise ProxyFormerError(PF_ERR_INVALID_ARG, "backward needs a forward with train=True")
+        dx = tuple(torch.empty((self.rows, t.shape[1]), dtype=t.dtype, device=t.device)
+                   for t in (q, k, v)) if into is None else self._qkv(*into)
+        if self.ws is None:
+            self.ws = torch.empty(pf_window_attn_workspace_size(self.desc), dtype=torch.uint8,
+                                  device=q.device)
+        pf_window_attn_bwd(self.desc, qkv(q, k, v), out, out.stride(0), lse, dout, dout.stride(0),
+                           qkv(*dx), self.ws, self.ws.numel(), _stream())
+        return dx
 
 
 class PagedKVCache:

@@ -60,6 +60,50 @@ def test_rope_backward_refusals():
     refused(pf.PF_ERR_WORKSPACE, lambda: f(ws=A + 4))
 
 
+def win(batch=2, L=300, n_heads=4, n_kv=2, dh=64, window=100, n_sink=4):
+    return pf.WindowDesc(batch, L, n_heads, n_kv, dh, window, n_sink)
+
+
+def test_window_refusals():
+    bad, no = pf.PF_ERR_INVALID_ARG, pf.PF_ERR_UNSUPPORTED
+    B = A * 2  # addresses of the gradients
+    grads = lambda **kw: rows(**{**dict(q=B, k=B, v=B), **kw})
+    fwd = lambda d=win(), x=rows(), out=A, ld=256, lse=A: pf.pf_window_attn_fwd(d, x, out, ld, lse)
+
+    def bwd(d=win(), x=rows(), out=A, ld=256, lse=A, dout=A, ld_d=256, dx=None, ws=A, size=1 << 40):
+        pf.pf_window_attn_bwd(d, x, out, ld, lse, dout, ld_d, dx or grads(), ws, size)
+    for s, kws in ((bad, (dict(batch=0), dict(L=0), dict(n_kv=3), dict(window=-1), dict(n_sink=-2))),
+                   (no, (dict(dh=128), dict(dh=32), dict(L=1 << 30), dict(batch=1 << 16, L=1 << 15),
+                         dict(batch=1 << 20, L=1024, n_heads=64)))):
+        for kw in kws:
+            refused(s, fwd, win(**kw))
+            refused(s, bwd, win(**kw))
+            assert pf.pf_window_attn_workspace_size(win(**kw)) == 0
+    for kw in (dict(q=None), dict(k=A + 8), dict(v=None), dict(ld_q=248), dict(ld_k=132), dict(ld_v=64)):
+        refused(bad, lambda: fwd(x=rows(**kw)))
+        refused(bad, lambda: bwd(x=rows(**kw)))
+        refused(bad, lambda: bwd(dx=grads(**{n: (v + A if v and v > A else v) for n, v in kw.items()})))
+    for kw in (dict(out=None), dict(out=A + 2), dict(ld=128), dict(ld=260)):
+        refused(bad, lambda: fwd(**kw))
+        refused(bad, lambda: bwd(**kw))
+    refused(bad, lambda: bwd(lse=None))
+    refused(bad, lambda: bwd(dout=None))
+    refused(bad, lambda: bwd(dx=grads(k=A)))  # a gradient over an input
+    need = pf.pf_window_attn_workspace_size(win())
+    refused(pf.PF_ERR_WORKSPACE, lambda: bwd(size=need - 1))
+    refused(pf.PF_ERR_WORKSPACE, lambda: bwd(ws=None))
+
+
+def test_window_workspace_stays_small():
+    """The sums of cut tiles: some hundreds of 64 KB, whatever the length."""
+    for d in (win(1, 262144, 16, 16, window=1024, n_sink=4), win(1, 262144, 16, 1, window=0),
+              win(4, 65536, 32, 2, window=4096, n_sink=300), win(1, 1, 1, 1), win(3, 999, 64, 1, window=1, n_sink=998)):
+        rest = 4 * d.batch * d.n_heads * d.L + 512
+        tiles = d.batch * d.n_kv * -(-d.L // 128)
+        pieces = (pf.pf_window_attn_workspace_size(d) - rest) / 65536
+        assert pieces <= 2 * 304 + 4 * d.batch * d.n_kv * 3 + (2 * tiles if tiles < 152 else 0)
+
+
 def paged(batch=3, n_heads=4, n_kv=2, dh=64, page=16, max_pages=4, n_pages=9, window=0, n_sink=0):
     return pf.PagedDesc(batch, n_heads, n_kv, dh, page, max_pages, n_pages, window, n_sink)
 
