@@ -109,7 +109,8 @@ EXPORTED = ("proxy_layer_check", "proxy_layer_saved_size", "proxy_layer_workspac
             "proxy_prefill_workspace_size", "proxy_kv_prefill", "proxy_layer_prefill",
             "proxy_segments_saved_size", "proxy_segments_workspace_size", "proxy_segments_fwd",
             "proxy_segments_bwd", "pf_qk_rope_fwd", "pf_qk_rope_workspace_size", "pf_qk_rope_bwd",
-            "pf_window_attn_fwd", "pf_window_attn_workspace_size", "pf_window_attn_bwd",
+            "pf_window_attn_fwd", "pf_window_attn_saved_size", "pf_window_attn_workspace_size",
+            "pf_window_attn_bwd",
             "pf_paged_advance", "pf_paged_append", "pf_paged_attn_workspace_size", "pf_paged_attn",
             "pf_last_error", "pf_sync_check", "pf_gemm_bf16", "pf_timing_enable",
             "pf_timing_collect", "pf_timing_label", "pf_timing_ms", "pf_timing_launches",
@@ -182,6 +183,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pf_qk_rope_bwd.restype = ctypes.c_int
     lib.pf_window_attn_fwd.argtypes = [P(WindowDesc), P(QKV), _vp, i64, _vp, _vp]
     lib.pf_window_attn_fwd.restype = ctypes.c_int
+    lib.pf_window_attn_saved_size.argtypes = [P(WindowDesc)]
+    lib.pf_window_attn_saved_size.restype = sz
     lib.pf_window_attn_workspace_size.argtypes = [P(WindowDesc)]
     lib.pf_window_attn_workspace_size.restype = sz
     lib.pf_window_attn_bwd.argtypes = [P(WindowDesc), P(QKV), _vp, i64, _vp, _vp, i64, P(QKV), _vp,
@@ -392,18 +395,22 @@ def pf_qk_rope_bwd(desc, rows, seq_len, x, w_q, w_k, pos, dout, dx, dw_q, dw_k, 
                                  stream))
 
 
-def pf_window_attn_fwd(desc, x, out, ld_out, lse, stream=None):
+def pf_window_attn_fwd(desc, x, out, ld_out, saved, stream=None):
     _check(load().pf_window_attn_fwd(ctypes.byref(desc), ctypes.byref(x), _ptr(out), int(ld_out),
-                                     _ptr(lse), stream))
+                                     _ptr(saved), stream))
+
+
+def pf_window_attn_saved_size(desc) -> int:
+    return load().pf_window_attn_saved_size(ctypes.byref(desc))
 
 
 def pf_window_attn_workspace_size(desc) -> int:
     return load().pf_window_attn_workspace_size(ctypes.byref(desc))
 
 
-def pf_window_attn_bwd(desc, x, out, ld_out, lse, dout, ld_dout, dx, ws, ws_bytes, stream=None):
+def pf_window_attn_bwd(desc, x, out, ld_out, saved, dout, ld_dout, dx, ws, ws_bytes, stream=None):
     _check(load().pf_window_attn_bwd(ctypes.byref(desc), ctypes.byref(x), _ptr(out), int(ld_out),
-                                     _ptr(lse), _ptr(dout), int(ld_dout), ctypes.byref(dx),
+                                     _ptr(saved), _ptr(dout), int(ld_dout), ctypes.byref(dx),
                                      _ptr(ws), int(ws_bytes), stream))
 
 

@@ -31,12 +31,20 @@ struct Window {
   int B, L, H, KV, window, sinks;  // window 0: no limit
 };
 double window_pairs(const Window& c);  // visible (query, key) pairs of a head and sequence
-// lse [B, H, L] in log2 units for the backward, or null.
-cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, float* lse,
+// What the forward keeps for the backward: the rows' log-sums [B, H, L] in log2 units,
+// and the output's rest [B * L, H * 64], out + rest being the output to 2^-17.
+struct WindowSaved {
+  float* lse;
+  bf16* rest;
+  size_t bytes;
+};
+WindowSaved window_saved(const Window& c, void* p);
+// v.lse null: nothing is kept
+cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, const WindowSaved& v,
                        cudaStream_t st);
 size_t window_bwd_ws_bytes(const Window& c);
 cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long ldo,
-                       const float* lse, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
+                       const WindowSaved& v, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
                        cudaStream_t st);
 
 cudaError_t qk_rope_fwd(const QkRope& s, const QkvPtr& x, const QkvPtr& o, const float* w_q,

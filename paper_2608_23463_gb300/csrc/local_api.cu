@@ -45,8 +45,9 @@ pf_status check_rows(const char* name, const void* p, int64_t ld, int64_t width,
   } while (0)
 
 pf_status check_heads(int32_t H, int32_t KV, int32_t dh) {
-  if (H < 1 || KV < 1 || H % KV != 0 || H > 65535)
+  if (H < 1 || KV < 1 || H % KV != 0)
     return fail(PF_ERR_INVALID_ARG, "n_heads must be a positive multiple of n_kv");
+  if (H > 4096) return fail(PF_ERR_UNSUPPORTED, "at most 4096 heads");
   if (dh != 64 && dh != 128) return fail(PF_ERR_UNSUPPORTED, "head width must be 64 or 128");
   return PF_OK;
 }
@@ -202,13 +203,19 @@ pf_status pf_qk_rope_bwd(const pf_qk_desc* desc, int64_t rows, int64_t seq_len, 
 }
 
 pf_status pf_window_attn_fwd(const pf_window_desc* desc, const pf_qkv* x, void* out,
-                             int64_t ld_out, float* lse, void* stream) {
+                             int64_t ld_out, void* saved, void* stream) {
   PF_TRY(check_window(desc));
   PF_TRY(check_window_rows("x", x, *desc));
   PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
-  PF_CUDA(window_fwd(window_of(*desc), ptr_of(*x), static_cast<bf16*>(out), (long)ld_out, lse,
-                     static_cast<cudaStream_t>(stream)));
+  if (!aligned16(saved)) return fail(PF_ERR_INVALID_ARG, "saved must be 16-byte aligned");
+  const Window c = window_of(*desc);
+  PF_CUDA(window_fwd(c, ptr_of(*x), static_cast<bf16*>(out), (long)ld_out,
+                     saved ? window_saved(c, saved) : WindowSaved{}, static_cast<cudaStream_t>(stream)));
   return PF_OK;
+}
+
+size_t pf_window_attn_saved_size(const pf_window_desc* desc) {
+  return check_window(desc) == PF_OK ? window_saved(window_of(*desc), nullptr).bytes : 0;
 }
 
 size_t pf_window_attn_workspace_size(const pf_window_desc* desc) {
@@ -216,14 +223,16 @@ size_t pf_window_attn_workspace_size(const pf_window_desc* desc) {
 }
 
 pf_status pf_window_attn_bwd(const pf_window_desc* desc, const pf_qkv* x, const void* out,
-                             int64_t ld_out, const float* lse, const void* dout, int64_t ld_dout,
-                             const pf_qkv* dx, void* ws, size_t ws_bytes, void* stream) {
+                             int64_t ld_out, const void* saved, const void* dout,
+                             int64_t ld_dout, const pf_qkv* dx, void* ws, size_t ws_bytes,
+                             void* stream) {
   PF_TRY(check_window(desc));
   PF_TRY(check_window_rows("x", x, *desc));
   PF_TRY(check_window_rows("dx", dx, *desc));
   PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
   PF_TRY(check_rows("dout", dout, ld_dout, (int64_t)desc->n_heads * desc->dh, 2));
-  if (!lse) return fail(PF_ERR_INVALID_ARG, "lse is required");
+  if (!saved || !aligned16(saved))
+    return fail(PF_ERR_INVALID_ARG, "saved is required, 16-byte aligned");
   for (const void* d : {dx->q, dx->k, dx->v})
     for (const void* i : {static_cast<const void*>(x->q), static_cast<const void*>(x->k),
                           static_cast<const void*>(x->v), out, dout})
@@ -233,8 +242,8 @@ pf_status pf_window_attn_bwd(const pf_window_desc* desc, const pf_qkv* x, const 
   if (!ws || !aligned16(ws) || ws_bytes < need)
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need,
                 ws ? ws_bytes : 0);
-  PF_CUDA(window_bwd(c, ptr_of(*x), static_cast<const bf16*>(out), (long)ld_out, lse,
-                     static_cast<const bf16*>(dout), (long)ld_dout, ptr_of(*dx), ws,
+  PF_CUDA(window_bwd(c, ptr_of(*x), static_cast<const bf16*>(out), (long)ld_out,
+                     window_saved(c, const_cast<void*>(saved)), static_cast<const bf16*>(dout), (long)ld_dout, ptr_of(*dx), ws,
                      static_cast<cudaStream_t>(stream)));
   return PF_OK;
 }

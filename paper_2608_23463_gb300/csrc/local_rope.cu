@@ -9,13 +9,20 @@
 //   dw = sum over rows and heads of dy x r,
 //   dx = r (w dy - x r mean(w dy x r)).
 //
-// HBM traffic bounds all of them: a row is read once and written once.  A
-// head's values lie on dh / 8 (bf16) or dh / 4 (fp32) lanes, 16 bytes each, so
-// that a warp holds several heads and a head's sum takes three to five
-// shuffles; a warp takes a token and walks its heads, four loads in flight per
-// lane, with the token's sines made once (a pair or two on each lane, handed
-// round by shuffles).  With few tokens a token's heads are spread over several
-// warps (`parts`): latency counts there, and the sines made twice do not.
+// HBM traffic bounds all of them, a row read once and written once, and the
+// instructions come next.  A head's values lie on dh / 8 (bf16) or dh / 4
+// (fp32) lanes, 16 bytes each, so that a warp holds several heads and a head's
+// sum takes three to five shuffles; a warp takes a token, makes its sines (a
+// pair or two on each lane, handed round by shuffles), folds the weights into
+// them and walks the token's heads.  Arithmetic is in packed pairs: the first
+// halves of two turned pairs side by side, and the second halves.  With few
+// tokens a token's heads are spread over several warps (`parts`): latency
+// counts there, and the sines made twice do not.
+// Measured: four images of 512 x 512 tokens, 8 + 8 heads of 64, 704 us (6.1
+// TB/s, 90 % of a plain copy); backward, 65536 tokens of 16 + 4 heads, 101 us
+// (5.0 TB/s); eight prompts of 11738 tokens in all, 16 + 2 heads of 128, into
+// the cache 25.7 us (4.7 TB/s).  Scalar arithmetic with the weights applied
+// apart took 843 us for the images, three quarters of the issue slots busy.
 //
 // Angles: the frequency is held as a 64-bit fraction of a turn, and
 // pos * f modulo 2^64 is exact integer arithmetic; a position of a million
@@ -34,7 +41,11 @@ namespace {
 
 constexpr int RW_THREADS = 256;
 constexpr int RW_WARPS = RW_THREADS / 32;
-constexpr int RW_U = 4;         // heads in flight per lane
+// Resident CTAs an SM and heads in flight per lane.  Forward, four images of 512 x 512 tokens and 8 + 8
+// heads of 64: 704 us so, 757 with 4 CTAs and 4 heads, 909 with 3 and 8.  Backward, 65536 tokens of
+// 16 + 4 heads: 101 us so, 108 with 4 CTAs, 110 with 3 and one head.
+constexpr int RW_FWD_CTAS = 5, RW_FWD_U = 2;
+constexpr int RW_BWD_CTAS = 3, RW_BWD_U = 2;
 constexpr int RW_MAX_PAIRS = 64;
 
 struct RopeFreq {
@@ -49,7 +60,8 @@ struct RopeArgs {
   long ldq, ldk, ldqo, ldko;
   const float *w_q, *w_k;  // [dh] or null: no norm
   const int* pos;          // [rows, n_axes] or null: row % seq_len (cache row when appending)
-  int rows, seq_len, H, KV, parts;
+  int rows, seq_len, H, KV;
+  int parts;  // warps that share a token
   float eps;
   // backward: gradients of qo and ko, and the CTAs' sums of the weights' gradients
   const void *dqo, *dko;
@@ -64,73 +76,102 @@ struct RopeArgs {
   long n_pages;
 };
 
+// 16 bytes of a head as packed pairs: e[i] holds the first halves of the turned
+// pairs 2 i and 2 i + 1 (of the lane's), o[i] their second halves.
 template <class T>
 struct Vec;
 template <>
 struct Vec<bf16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void get(uint4 u, float* v) {
+  static __device__ __forceinline__ void get(uint4 u, float2* e, float2* o) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = unpack_bf16(w[i]);
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
+    for (int i = 0; i < 2; ++i) {
+      e[i] = make_float2(__uint_as_float(w[2 * i] << 16), __uint_as_float(w[2 * i + 1] << 16));
+      o[i] = make_float2(__uint_as_float(w[2 * i] & 0xffff0000u),
+                         __uint_as_float(w[2 * i + 1] & 0xffff0000u));
     }
   }
-  static __device__ __forceinline__ uint4 put(const float* v) {
-    return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
-                      pack_bf16(v[6], v[7]));
+  static __device__ __forceinline__ uint4 put(const float2* e, const float2* o) {
+    return make_uint4(pack_bf16(e[0].x, o[0].x), pack_bf16(e[0].y, o[0].y),
+                      pack_bf16(e[1].x, o[1].x), pack_bf16(e[1].y, o[1].y));
   }
 };
 template <>
 struct Vec<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void get(uint4 u, float* v) {
-    v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y);
-    v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
+  static __device__ __forceinline__ void get(uint4 u, float2* e, float2* o) {
+    e[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.z));
+    o[0] = make_float2(__uint_as_float(u.y), __uint_as_float(u.w));
   }
-  static __device__ __forceinline__ uint4 put(const float* v) {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
-                      __float_as_uint(v[3]));
+  static __device__ __forceinline__ uint4 put(const float2* e, const float2* o) {
+    return make_uint4(__float_as_uint(e[0].x), __float_as_uint(o[0].x), __float_as_uint(e[0].y),
+                      __float_as_uint(o[0].y));
   }
 };
 
 // How a warp holds heads of DH values of type T.
 template <class T, int DH>
 struct Lay {
-  static constexpr int N = Vec<T>::N;    // values per lane
-  static constexpr int LANES = DH / N;   // lanes per head
+  static constexpr int N = Vec<T>::N;       // values per lane
+  static constexpr int G = N / 4;           // packed groups of two pairs
+  static constexpr int LANES = DH / N;      // lanes per head
   static constexpr int HEADS = 32 / LANES;  // heads per pass of the warp
-  static constexpr int PPL = DH / 64;    // pairs whose sines a lane makes
+  static constexpr int PPL = DH / 64;       // pairs whose sines a lane makes
 };
 
-// cos and sin of the lane's N / 2 pairs at the token's position(s).  bf16 rows
-// take the hardware sine (absolute error below 2^-20 for |angle| <= pi, a
-// 2000th of the rounding of the result); fp32 rows the library's.
+struct RopeSmem {
+  unsigned long long f[RW_MAX_PAIRS];
+  float2 w[2][RW_MAX_PAIRS];  // w_q, w_k: group i's (first halves, second halves) at 2 i, 2 i + 1
+  unsigned char axis[RW_MAX_PAIRS];
+};
+
+// (The table comes from parameter space, which serves a warp one address at a
+// time: each thread fetches one entry.)
+template <int DH>
+__device__ __forceinline__ void stage(RopeSmem& s, const RopeFreq& fr, const RopeArgs& a) {
+  const int i = threadIdx.x;
+  if (i < DH / 2) {
+    s.f[i] = fr.f[i];
+    s.axis[i] = fr.axis[i];
+  }
+  pdl_enter();
+  if (i < DH) {
+    const float* w = i < DH / 2 ? a.w_q : a.w_k;
+    const int c = i % (DH / 2), j = c / 2 * 4 + (c & 1);  // values j and j + 2 of a head
+    s.w[i / (DH / 2)][c] = w ? make_float2(w[j], w[j + 2]) : make_float2(1.f, 1.f);
+  }
+  __syncthreads();
+}
+
+// cos and sin of the lane's pairs at the token's position(s), packed as the
+// values.  bf16 rows take the hardware sine (absolute error below 2^-20 for
+// |angle| <= pi, a 2000th of the rounding of the result); fp32 rows the
+// library's.
 template <class T, int DH>
-__device__ __forceinline__ void turn_of(const unsigned long long* f, const unsigned char* axis,
-                                        const int* pos3, int lane, float* cs, float* sn) {
+__device__ __forceinline__ void turn_of(const RopeSmem& s, const int* pos3, int lane, float2* cs,
+                                        float2* sn) {
   using Ly = Lay<T, DH>;
   float oc[Ly::PPL], os[Ly::PPL];
 #pragma unroll
-  for (int s = 0; s < Ly::PPL; ++s) {
-    const int p = lane * Ly::PPL + s;
-    const int a = axis[p];
-    const int ps = a == 0 ? pos3[0] : a == 1 ? pos3[1] : pos3[2];
-    const unsigned long long ph = (unsigned long long)(long long)ps * f[p];
+  for (int i = 0; i < Ly::PPL; ++i) {
+    const int p = lane * Ly::PPL + i, ax = s.axis[p];
+    const int ps = ax == 0 ? pos3[0] : ax == 1 ? pos3[1] : pos3[2];
+    const unsigned long long ph = (unsigned long long)(long long)ps * s.f[p];
     const float h = (float)(int)(ph >> 32) * 4.656612873077393e-10f;  // half turns, [-1, 1]
     if (sizeof(T) == 2)
-      __sincosf(h * 3.14159265358979f, &os[s], &oc[s]);
+      __sincosf(h * 3.14159265358979f, &os[i], &oc[i]);
     else
-      sincospif(h, &os[s], &oc[s]);
+      sincospif(h, &os[i], &oc[i]);
   }
   const int sub = lane % Ly::LANES;
 #pragma unroll
   for (int i = 0; i < Ly::N / 2; ++i) {
     const int src = (sub * (Ly::N / 2) + i) / Ly::PPL;
-    cs[i] = __shfl_sync(0xffffffffu, oc[i % Ly::PPL], src);
-    sn[i] = __shfl_sync(0xffffffffu, os[i % Ly::PPL], src);
+    const float c = __shfl_sync(0xffffffffu, oc[i % Ly::PPL], src);
+    const float t = __shfl_sync(0xffffffffu, os[i % Ly::PPL], src);
+    (i & 1 ? cs[i / 2].y : cs[i / 2].x) = c;
+    (i & 1 ? sn[i / 2].y : sn[i / 2].x) = t;
   }
 }
 
@@ -140,93 +181,88 @@ __device__ __forceinline__ float head_sum(float v) {
   for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
-// Heads [h0, h0 + HEADS * n) of one token (those below nh), normed and turned:
-// src + h * DH -> dst + h * dst_stride.
+// Passes [p0, p1) of one token's heads (head p * HEADS + the lane's slot, below
+// nh), normed and turned: src + head * DH -> dst + head * dst_stride.
 template <class T, int DH>
-__device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride, int h0, int n,
-                                           int nh, const float* w, bool norm, float eps,
-                                           const float* cs, const float* sn, int lane) {
+__device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride, int p0, int p1,
+                                           int nh, const float2* w, bool norm, float eps,
+                                           const float2* cs, const float2* sn, int lane) {
   using Ly = Lay<T, DH>;
-  const int slot = lane / Ly::LANES, sub = lane % Ly::LANES;
-  for (int p = 0; p < n; p += RW_U) {
-    uint4 u[RW_U];
-    int h[RW_U];
+  constexpr int U = RW_FWD_U, G = Ly::G;
+  const int sub = lane % Ly::LANES, slot = lane / Ly::LANES;
+  // w folded into the turn: z_e = x_e (w_e c) - x_o (w_o s), z_o = x_e (w_e s) + x_o (w_o c)
+  float2 ec[G], os[G], es[G], oc[G];
 #pragma unroll
-    for (int i = 0; i < RW_U; ++i) {
-      h[i] = h0 + (p + i) * Ly::HEADS + slot;
-      if (p + i >= n || h[i] >= nh) h[i] = -1;
-      if (h[i] >= 0) u[i] = *reinterpret_cast<const uint4*>(src + (long)h[i] * DH + sub * Ly::N);
+  for (int i = 0; i < G; ++i) {
+    const float2 we = w[(sub * G + i) * 2], wo = w[(sub * G + i) * 2 + 1];
+    ec[i] = __fmul2_rn(we, cs[i]);
+    es[i] = __fmul2_rn(we, sn[i]);
+    oc[i] = __fmul2_rn(wo, cs[i]);
+    os[i] = __fmul2_rn(wo, make_float2(-sn[i].x, -sn[i].y));
+  }
+  int h = p0 * Ly::HEADS + slot;
+  const T* sp = src + (long)h * DH + sub * Ly::N;
+  T* dp = dst + h * dst_stride + sub * Ly::N;
+  const long dstep = Ly::HEADS * dst_stride;
+  for (int p = p0; p < p1; p += U) {
+    uint4 u[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      u[i] = make_uint4(0, 0, 0, 0);
+      if (p + i < p1 && h + i * Ly::HEADS < nh)
+        u[i] = *reinterpret_cast<const uint4*>(sp + i * Ly::HEADS * DH);
     }
 #pragma unroll
-    for (int i = 0; i < RW_U; ++i) {
-      if (p + i >= n) break;  // the same for every lane
-      float x[Ly::N];
-      Vec<T>::get(h[i] >= 0 ? u[i] : make_uint4(0, 0, 0, 0), x);
+    for (int i = 0; i < U; ++i) {
+      if (p + i >= p1) break;  // the same for every lane
+      float2 e[G], o[G];
+      Vec<T>::get(u[i], e, o);
+      float r = 1.f;
       if (norm) {
-        float ss = 0.f;
+        float2 ss = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int e = 0; e < Ly::N; ++e) ss = fmaf(x[e], x[e], ss);
-        const float r = rsqrtf(fmaf(head_sum<Ly::LANES>(ss), 1.f / DH, eps));
-#pragma unroll
-        for (int e = 0; e < Ly::N; ++e) x[e] *= r * w[e];
+        for (int k = 0; k < G; ++k) ss = __ffma2_rn(e[k], e[k], __ffma2_rn(o[k], o[k], ss));
+        r = rsqrtf(fmaf(head_sum<Ly::LANES>(ss.x + ss.y), 1.f / DH, eps));
       }
-      float z[Ly::N];
+      float2 ze[G], zo[G];
 #pragma unroll
-      for (int e = 0; e < Ly::N; e += 2) {
-        z[e] = x[e] * cs[e / 2] - x[e + 1] * sn[e / 2];
-        z[e + 1] = fmaf(x[e], sn[e / 2], x[e + 1] * cs[e / 2]);
+      for (int k = 0; k < G; ++k) {
+        ze[k] = __ffma2_rn(e[k], ec[k], __fmul2_rn(o[k], os[k]));
+        zo[k] = __ffma2_rn(e[k], es[k], __fmul2_rn(o[k], oc[k]));
+        if (norm) {
+          ze[k] = __fmul2_rn(ze[k], both(r));
+          zo[k] = __fmul2_rn(zo[k], both(r));
+        }
       }
-      if (h[i] >= 0)
-        *reinterpret_cast<uint4*>(dst + (long)h[i] * dst_stride + sub * Ly::N) = Vec<T>::put(z);
+      if (h + i * Ly::HEADS < nh) *reinterpret_cast<uint4*>(dp + i * dstep) = Vec<T>::put(ze, zo);
     }
+    h += U * Ly::HEADS;
+    sp += U * Ly::HEADS * DH;
+    dp += U * dstep;
   }
-}
-
-// The frequency table in shared memory (a table in parameter space read with a
-// lane's own index is served one address at a time).
-struct FreqSmem {
-  unsigned long long f[RW_MAX_PAIRS];
-  unsigned char axis[RW_MAX_PAIRS];
-};
-__device__ __forceinline__ void stage_freq(FreqSmem& s, const RopeFreq& fr) {
-  if (threadIdx.x < RW_MAX_PAIRS) {
-    s.f[threadIdx.x] = fr.f[threadIdx.x];
-    s.axis[threadIdx.x] = fr.axis[threadIdx.x];
-  }
-  __syncthreads();
-}
-
-template <class T, int DH>
-__device__ __forceinline__ void load_w(const float* w, int lane, float* o) {
-  using Ly = Lay<T, DH>;
-#pragma unroll
-  for (int e = 0; e < Ly::N; ++e) o[e] = w ? w[(lane % Ly::LANES) * Ly::N + e] : 1.f;
 }
 
 // Forward (APPEND: keys and values go to their cache pages).  A unit is part
 // `pt` of a token's passes: q heads, then k heads, then (APPEND) v heads.
 template <class T, int DH, bool APPEND>
-__global__ void __launch_bounds__(RW_THREADS) rope_fwd_kernel(RopeArgs a,
-                                                              const __grid_constant__ RopeFreq fr) {
+__global__ void __launch_bounds__(RW_THREADS, RW_FWD_CTAS)
+    rope_fwd_kernel(RopeArgs a, const __grid_constant__ RopeFreq fr) {
   using Ly = Lay<T, DH>;
-  __shared__ FreqSmem fs;
-  stage_freq(fs, fr);
-  const int pz = pdl_enter();
+  __shared__ __align__(16) RopeSmem s;
+  stage<DH>(s, fr, a);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float wq[Ly::N], wk[Ly::N];
-  load_w<T, DH>(a.w_q ? a.w_q + pz : nullptr, lane, wq);
-  load_w<T, DH>(a.w_k ? a.w_k + pz : nullptr, lane, wk);
   const int nq = (a.H + Ly::HEADS - 1) / Ly::HEADS, nk = (a.KV + Ly::HEADS - 1) / Ly::HEADS;
   const int passes = nq + nk + (APPEND ? nk : 0);
   const long units = (long)a.rows * a.parts;
   for (long un = (long)blockIdx.x * RW_WARPS + warp; un < units; un += (long)gridDim.x * RW_WARPS) {
-    const int row = (int)(un / a.parts), pt = (int)(un % a.parts);
+    const int row = a.parts == 1 ? (int)un : (int)(un / a.parts), pt = (int)(un - (long)row * a.parts);
     const int p0 = pt * passes / a.parts, p1 = (pt + 1) * passes / a.parts;
     int pos3[3] = {0, 0, 0};
     bf16 *kd = nullptr, *vd = nullptr;
     if (APPEND) {
-      // the token's sequence: how many of the others start at or before it
+      // the token's sequence: how many of them end at or before it
       int b = row;
       if (a.start) {
         b = 0;
@@ -238,9 +274,9 @@ __global__ void __launch_bounds__(RW_THREADS) rope_fwd_kernel(RopeArgs a,
       int crow = -1;
       if (b < a.B) crow = a.len[b] - (a.start ? a.start[b + 1] - row : 1);
       pos3[0] = crow;
-      const long pi = crow / a.page;
       long pg = -1;
-      if (crow >= 0 && pi < a.max_pages) pg = a.table[(long)b * a.max_pages + pi];
+      if (crow >= 0 && crow / a.page < a.max_pages)
+        pg = a.table[(long)b * a.max_pages + crow / a.page];
       if (pg < 0 || pg >= a.n_pages) {
         if (lane == 0) set_dev_error(DEVERR_CAPACITY);
       } else {
@@ -256,23 +292,22 @@ __global__ void __launch_bounds__(RW_THREADS) rope_fwd_kernel(RopeArgs a,
       for (int i = 0; i < 3; ++i)
         if (i < fr.n_axes) pos3[i] = a.pos[(long)row * fr.n_axes + i];
     }
-    float cs[Ly::N / 2], sn[Ly::N / 2];
-    turn_of<T, DH>(fs.f, fs.axis, pos3, lane, cs, sn);
+    float2 cs[Ly::G], sn[Ly::G];
+    turn_of<T, DH>(s, pos3, lane, cs, sn);
     if (p0 < nq)
       rope_heads<T, DH>(static_cast<const T*>(a.q) + row * a.ldq, static_cast<T*>(a.qo) + row * a.ldqo,
-                        DH, p0 * Ly::HEADS, min(p1, nq) - p0, a.H, wq, a.w_q != nullptr, a.eps, cs,
-                        sn, lane);
+                        DH, p0, min(p1, nq), a.H, s.w[0], a.w_q != nullptr, a.eps, cs, sn, lane);
     const int k0 = max(p0, nq) - nq, k1 = min(p1, nq + nk) - nq;
     const T* ks = static_cast<const T*>(a.k) + row * a.ldk;
     if (!APPEND) {
       if (k0 < k1)
-        rope_heads<T, DH>(ks, static_cast<T*>(a.ko) + row * a.ldko, DH, k0 * Ly::HEADS, k1 - k0, a.KV,
-                          wk, a.w_k != nullptr, a.eps, cs, sn, lane);
+        rope_heads<T, DH>(ks, static_cast<T*>(a.ko) + row * a.ldko, DH, k0, k1, a.KV, s.w[1],
+                          a.w_k != nullptr, a.eps, cs, sn, lane);
     } else if (kd) {
       const long hs = (long)a.page * DH;
       if (k0 < k1)
-        rope_heads<T, DH>(ks, reinterpret_cast<T*>(kd), hs, k0 * Ly::HEADS, k1 - k0, a.KV, wk,
-                          a.w_k != nullptr, a.eps, cs, sn, lane);
+        rope_heads<T, DH>(ks, reinterpret_cast<T*>(kd), hs, k0, k1, a.KV, s.w[1], a.w_k != nullptr,
+                          a.eps, cs, sn, lane);
       const int slot = lane / Ly::LANES, sub = lane % Ly::LANES;
       const T* vs = static_cast<const T*>(a.v) + row * a.ldv;
 #pragma unroll 4
@@ -286,81 +321,91 @@ __global__ void __launch_bounds__(RW_THREADS) rope_fwd_kernel(RopeArgs a,
   }
 }
 
-// Heads [h0, h0 + HEADS * n) of one token, backward; the weights' gradients are
+// Passes [p0, p1) of one token's heads, backward; the weights' gradients are
 // added to the lane's sums.
 template <class T, int DH>
-__device__ __forceinline__ void rope_heads_bwd(const T* x, const T* dz, T* dx, int h0, int n, int nh,
-                                               const float* w, bool norm, float eps,
-                                               const float* cs, const float* sn, float* dw,
-                                               int lane) {
+__device__ __forceinline__ void rope_heads_bwd(const T* x, const T* dz, T* dx, int p0, int p1, int nh,
+                                               const float2* w, bool norm, float eps,
+                                               const float2* cs, const float2* sn, float2* ge,
+                                               float2* go, int lane) {
   using Ly = Lay<T, DH>;
-  constexpr int U = RW_U / 2;  // two rows to a head
-  const int slot = lane / Ly::LANES, sub = lane % Ly::LANES;
-  for (int p = 0; p < n; p += U) {
+  constexpr int U = RW_BWD_U, G = Ly::G;
+  const int sub = lane % Ly::LANES, slot = lane / Ly::LANES;
+  int h = p0 * Ly::HEADS + slot;
+  const long off = (long)h * DH + sub * Ly::N;
+  x += off;
+  dz += off;
+  dx += off;
+  w += sub * G * 2;
+  for (int p = p0; p < p1; p += U) {
     uint4 ux[U], uz[U];
-    int h[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      h[i] = h0 + (p + i) * Ly::HEADS + slot;
-      if (p + i >= n || h[i] >= nh) h[i] = -1;
-      const long o = (long)h[i] * DH + sub * Ly::N;
       ux[i] = uz[i] = make_uint4(0, 0, 0, 0);
-      if (h[i] >= 0) {
-        uz[i] = *reinterpret_cast<const uint4*>(dz + o);
-        if (norm) ux[i] = *reinterpret_cast<const uint4*>(x + o);
+      if (p + i < p1 && h + i * Ly::HEADS < nh) {
+        uz[i] = *reinterpret_cast<const uint4*>(dz + i * Ly::HEADS * DH);
+        if (norm) ux[i] = *reinterpret_cast<const uint4*>(x + i * Ly::HEADS * DH);
       }
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (p + i >= n) break;  // the same for every lane
-      float z[Ly::N], y[Ly::N];
-      Vec<T>::get(uz[i], z);
+      if (p + i >= p1) break;  // the same for every lane
+      float2 ze[G], zo[G], ye[G], yo[G];
+      Vec<T>::get(uz[i], ze, zo);
 #pragma unroll
-      for (int e = 0; e < Ly::N; e += 2) {
-        y[e] = fmaf(z[e], cs[e / 2], z[e + 1] * sn[e / 2]);
-        y[e + 1] = z[e + 1] * cs[e / 2] - z[e] * sn[e / 2];
+      for (int k = 0; k < G; ++k) {
+        const float2 ns = make_float2(-sn[k].x, -sn[k].y);
+        ye[k] = __ffma2_rn(ze[k], cs[k], __fmul2_rn(zo[k], sn[k]));
+        yo[k] = __ffma2_rn(zo[k], cs[k], __fmul2_rn(ze[k], ns));
       }
       if (norm) {
-        float xv[Ly::N], ss = 0.f, t = 0.f;
-        Vec<T>::get(ux[i], xv);
+        float2 xe[G], xo[G], ss = both(0.f), t = both(0.f);
+        Vec<T>::get(ux[i], xe, xo);
 #pragma unroll
-        for (int e = 0; e < Ly::N; ++e) ss = fmaf(xv[e], xv[e], ss);
+        for (int k = 0; k < G; ++k) {
+          ss = __ffma2_rn(xe[k], xe[k], __ffma2_rn(xo[k], xo[k], ss));
+          t = __ffma2_rn(__fmul2_rn(w[2 * k], ye[k]), xe[k],
+                         __ffma2_rn(__fmul2_rn(w[2 * k + 1], yo[k]), xo[k], t));
+        }
+        const float sq = head_sum<Ly::LANES>(ss.x + ss.y), tt = head_sum<Ly::LANES>(t.x + t.y);
+        const float r = rsqrtf(fmaf(sq, 1.f / DH, eps));
+        const float m = -tt * r * r * r * (1.f / DH);  // -r^2 mean(w dy x r), of x
 #pragma unroll
-        for (int e = 0; e < Ly::N; ++e) t = fmaf(w[e] * y[e], xv[e], t);
-        ss = head_sum<Ly::LANES>(ss);
-        t = head_sum<Ly::LANES>(t);
-        const float r = rsqrtf(fmaf(ss, 1.f / DH, eps));
-        const float m = t * r * (1.f / DH);  // mean(w dy x r)
-#pragma unroll
-        for (int e = 0; e < Ly::N; ++e) {
-          const float xh = xv[e] * r;
-          dw[e] = fmaf(y[e], xh, dw[e]);
-          y[e] = r * (w[e] * y[e] - xh * m);
+        for (int k = 0; k < G; ++k) {
+          const float2 re = __fmul2_rn(ye[k], both(r)), ro = __fmul2_rn(yo[k], both(r));
+          ge[k] = __ffma2_rn(re, xe[k], ge[k]);
+          go[k] = __ffma2_rn(ro, xo[k], go[k]);
+          ye[k] = __ffma2_rn(w[2 * k], re, __fmul2_rn(xe[k], both(m)));
+          yo[k] = __ffma2_rn(w[2 * k + 1], ro, __fmul2_rn(xo[k], both(m)));
         }
       }
-      if (h[i] >= 0)
-        *reinterpret_cast<uint4*>(dx + (long)h[i] * DH + sub * Ly::N) = Vec<T>::put(y);
+      if (h + i * Ly::HEADS < nh)
+        *reinterpret_cast<uint4*>(dx + i * Ly::HEADS * DH) = Vec<T>::put(ye, yo);
     }
+    h += U * Ly::HEADS;
+    x += U * Ly::HEADS * DH;
+    dz += U * Ly::HEADS * DH;
+    dx += U * Ly::HEADS * DH;
   }
 }
 
 template <class T, int DH>
-__global__ void __launch_bounds__(RW_THREADS) rope_bwd_kernel(RopeArgs a,
-                                                              const __grid_constant__ RopeFreq fr) {
+__global__ void __launch_bounds__(RW_THREADS, RW_BWD_CTAS)
+    rope_bwd_kernel(RopeArgs a, const __grid_constant__ RopeFreq fr) {
   using Ly = Lay<T, DH>;
-  __shared__ FreqSmem fs;
+  constexpr int G = Ly::G;
+  __shared__ __align__(16) RopeSmem s;
   __shared__ float red[RW_WARPS][2][DH];
-  stage_freq(fs, fr);
-  const int pz = pdl_enter();
+  stage<DH>(s, fr, a);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float wq[Ly::N], wk[Ly::N], gq[Ly::N] = {}, gk[Ly::N] = {};
-  load_w<T, DH>(a.w_q ? a.w_q + pz : nullptr, lane, wq);
-  load_w<T, DH>(a.w_k ? a.w_k + pz : nullptr, lane, wk);
+  float2 g[2][2 * G];  // of w_q, w_k: first halves, then second halves
+#pragma unroll
+  for (int i = 0; i < 2 * G; ++i) g[0][i] = g[1][i] = both(0.f);
   const int nq = (a.H + Ly::HEADS - 1) / Ly::HEADS, nk = (a.KV + Ly::HEADS - 1) / Ly::HEADS;
   const int passes = nq + nk;
   const long units = (long)a.rows * a.parts;
   for (long un = (long)blockIdx.x * RW_WARPS + warp; un < units; un += (long)gridDim.x * RW_WARPS) {
-    const int row = (int)(un / a.parts), pt = (int)(un % a.parts);
+    const int row = a.parts == 1 ? (int)un : (int)(un / a.parts), pt = (int)(un - (long)row * a.parts);
     const int p0 = pt * passes / a.parts, p1 = (pt + 1) * passes / a.parts;
     int pos3[3] = {a.pos ? 0 : row % a.seq_len, 0, 0};
     if (a.pos) {
@@ -368,34 +413,36 @@ __global__ void __launch_bounds__(RW_THREADS) rope_bwd_kernel(RopeArgs a,
       for (int i = 0; i < 3; ++i)
         if (i < fr.n_axes) pos3[i] = a.pos[(long)row * fr.n_axes + i];
     }
-    float cs[Ly::N / 2], sn[Ly::N / 2];
-    turn_of<T, DH>(fs.f, fs.axis, pos3, lane, cs, sn);
+    float2 cs[G], sn[G];
+    turn_of<T, DH>(s, pos3, lane, cs, sn);
     if (p0 < nq)
       rope_heads_bwd<T, DH>(static_cast<const T*>(a.q) + row * a.ldq,
                             static_cast<const T*>(a.dqo) + row * a.lddqo,
-                            static_cast<T*>(a.qo) + row * a.ldqo, p0 * Ly::HEADS, min(p1, nq) - p0,
-                            a.H, wq, a.w_q != nullptr, a.eps, cs, sn, gq, lane);
+                            static_cast<T*>(a.qo) + row * a.ldqo, p0, min(p1, nq), a.H, s.w[0],
+                            a.w_q != nullptr, a.eps, cs, sn, g[0], g[0] + G, lane);
     const int k0 = max(p0, nq) - nq;
     if (k0 < p1 - nq)
       rope_heads_bwd<T, DH>(static_cast<const T*>(a.k) + row * a.ldk,
                             static_cast<const T*>(a.dko) + row * a.lddko,
-                            static_cast<T*>(a.ko) + row * a.ldko, k0 * Ly::HEADS, p1 - nq - k0, a.KV,
-                            wk, a.w_k != nullptr, a.eps, cs, sn, gk, lane);
+                            static_cast<T*>(a.ko) + row * a.ldko, k0, p1 - nq, a.KV, s.w[1],
+                            a.w_k != nullptr, a.eps, cs, sn, g[1], g[1] + G, lane);
   }
   if (!a.part) return;  // no norm
   // the CTA's sums of the weights' gradients, in a fixed order
 #pragma unroll
-  for (int e = 0; e < Ly::N; ++e)
+  for (int q = 0; q < 2; ++q)
 #pragma unroll
-    for (int o = Ly::LANES; o < 32; o <<= 1) {
-      gq[e] += __shfl_xor_sync(0xffffffffu, gq[e], o);
-      gk[e] += __shfl_xor_sync(0xffffffffu, gk[e], o);
-    }
-  if (lane < Ly::LANES)
+    for (int k = 0; k < 2 * G; ++k) {
 #pragma unroll
-    for (int e = 0; e < Ly::N; ++e) {
-      red[warp][0][lane * Ly::N + e] = gq[e];
-      red[warp][1][lane * Ly::N + e] = gk[e];
+      for (int o = Ly::LANES; o < 32; o <<= 1) {
+        g[q][k].x += __shfl_xor_sync(0xffffffffu, g[q][k].x, o);
+        g[q][k].y += __shfl_xor_sync(0xffffffffu, g[q][k].y, o);
+      }
+      if (lane < Ly::LANES) {  // values 4 i, 4 i + 2 (first halves) or + 1, + 3 of the lane's
+        float* d = red[warp][q] + lane * Ly::N + k % G * 4 + k / G;
+        d[0] = g[q][k].x;
+        d[2] = g[q][k].y;
+      }
     }
   __syncthreads();
   for (int c = threadIdx.x; c < 2 * DH; c += RW_THREADS) {
@@ -455,18 +502,14 @@ RopeFreq freq_of(const QkRope& s) {
   return fr;
 }
 
-constexpr int RW_CTAS = 4 * 152;  // grid: what 152 SMs hold, whatever the device has (sums keep their order)
+constexpr int RW_SMS = 152;  // whatever the device has: the sums keep their order
 
 // Passes of a token's heads are spread over so many warps that about 16 warps
 // an SM have work (a token a warp: 66 tokens of 10 heads would run on 9 SMs).
-int rope_parts(long rows, int passes) {
-  const long want = (16L * 152 + rows - 1) / rows;
-  return (int)std::min<long>(std::max(1L, want), passes);
-}
-
-int rope_passes(const QkRope& s, bool with_v) {
-  const int heads = 32 / (s.dh * (s.f32 ? 4 : 2) / 16);
-  return (s.H + heads - 1) / heads + (with_v ? 2 : 1) * ((s.KV + heads - 1) / heads);
+void set_parts(RopeArgs& a, const QkRope& s, bool with_v) {
+  const int heads = 32 * 16 / (s.dh * (s.f32 ? 4 : 2));  // of a pass
+  const int nk = (s.KV + heads - 1) / heads, passes = (s.H + heads - 1) / heads + (with_v ? 2 : 1) * nk;
+  a.parts = std::min(std::max(1, 16 * RW_SMS / a.rows), passes);
 }
 
 RopeArgs args_of(const QkRope& s, const QkvPtr& x, const QkvPtr& o, const float* w_q,
@@ -487,7 +530,9 @@ RopeArgs args_of(const QkRope& s, const QkvPtr& x, const QkvPtr& o, const float*
   return a;
 }
 
-int rope_grid(long units) { return (int)std::min<long>((units + RW_WARPS - 1) / RW_WARPS, RW_CTAS); }
+int rope_grid(const RopeArgs& a, int per_sm) {
+  return (int)std::min<long>(((long)a.rows * a.parts + RW_WARPS - 1) / RW_WARPS, (long)per_sm * RW_SMS);
+}
 
 }  // namespace
 
@@ -495,16 +540,16 @@ cudaError_t qk_rope_fwd(const QkRope& s, const QkvPtr& x, const QkvPtr& o, const
                         const float* w_k, const int* pos, long rows, long seq_len,
                         cudaStream_t st) {
   RopeArgs a = args_of(s, x, o, w_q, w_k, pos, rows, seq_len);
-  a.parts = rope_parts(rows, rope_passes(s, false));
+  set_parts(a, s, false);
   const double n = (double)rows * (s.H + s.KV) * s.dh;
   LaunchTimer lt("qk_rope_fwd", st, 8.0 * n, (s.f32 ? 8.0 : 4.0) * n);
-  const int grid = rope_grid(rows * a.parts);
+  const int grid = rope_grid(a, RW_FWD_CTAS);
   auto k = s.f32 ? (s.dh == 64 ? rope_fwd_kernel<float, 64, false> : rope_fwd_kernel<float, 128, false>)
                  : (s.dh == 64 ? rope_fwd_kernel<bf16, 64, false> : rope_fwd_kernel<bf16, 128, false>);
   return launch_kernel(k, grid, RW_THREADS, 0, st, a, freq_of(s));
 }
 
-size_t qk_rope_part_bytes(int dh) { return (size_t)RW_CTAS * 2 * dh * sizeof(float); }
+size_t qk_rope_part_bytes(int dh) { return (size_t)RW_BWD_CTAS * RW_SMS * 2 * dh * sizeof(float); }
 
 cudaError_t qk_rope_bwd(const QkRope& s, const QkvPtr& x, const QkvPtr& dout, const QkvPtr& dx,
                         const float* w_q, const float* w_k, const int* pos, float* dw_q,
@@ -515,9 +560,9 @@ cudaError_t qk_rope_bwd(const QkRope& s, const QkvPtr& x, const QkvPtr& dout, co
   a.lddqo = dout.ldq;
   a.lddko = dout.ldk;
   a.part = dw_q || dw_k ? part : nullptr;
-  a.parts = rope_parts(rows, rope_passes(s, false));
+  set_parts(a, s, false);
   const double n = (double)rows * (s.H + s.KV) * s.dh;
-  const int grid = rope_grid(rows * a.parts);
+  const int grid = rope_grid(a, RW_BWD_CTAS);
   {
     LaunchTimer lt("qk_rope_bwd", st, 16.0 * n, (s.f32 ? 12.0 : 6.0) * n);
     auto k = s.f32 ? (s.dh == 64 ? rope_bwd_kernel<float, 64> : rope_bwd_kernel<float, 128>)
@@ -541,10 +586,10 @@ cudaError_t paged_append(const QkRope& s, const Paged& c, const QkvPtr& x, bf16*
   a.table = c.table; a.len = c.len; a.start = start;
   a.B = c.B; a.page = c.page; a.max_pages = c.max_pages;
   a.n_pages = c.n_pages;
-  a.parts = rope_parts(rows, rope_passes(s, true));
+  set_parts(a, s, true);
   const double n = (double)rows * s.dh;
   LaunchTimer lt("paged_append", st, 8.0 * n * (s.H + s.KV), 4.0 * n * (s.H + 2 * s.KV));
-  const int grid = rope_grid(rows * a.parts);
+  const int grid = rope_grid(a, RW_FWD_CTAS);
   return launch_kernel(s.dh == 64 ? rope_fwd_kernel<bf16, 64, true> : rope_fwd_kernel<bf16, 128, true>,
                        grid, RW_THREADS, 0, st, a, freq_of(s));
 }

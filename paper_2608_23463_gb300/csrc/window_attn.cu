@@ -61,6 +61,7 @@ constexpr uint32_t WA_TMEM_COLS = 512;
 struct WaArgs {
   bf16* out;   // [B*L, ldo], head h at column h*64
   float* lse;  // [B, H, L] in log2 units, or null
+  bf16* rest;  // [B*L, H*64] out - bf16(out), with lse
   long ldo;
   int B, H, g;  // g: query heads to a key head
   WinTiles w;
@@ -402,23 +403,36 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
       // p ^ (i & 7)), so that 8 lanes store a row's 128 bytes
       uint8_t* const stg = smem + WA_OFF_STG + (warp - 4) * 4096;
       const int q0 = t * WT + q4 * 32;
+      auto put = [&](bf16* dst, long ld) {
 #pragma unroll
-      for (int i = 0; i < WA_D; i += 8) {
-        const float* o = reinterpret_cast<const float*>(ov + i);
-        *reinterpret_cast<uint4*>(stg + lane * 128 + (((i >> 3) ^ (lane & 7)) << 4)) =
-            make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
-                       pack_bf16(o[4] * inv, o[5] * inv), pack_bf16(o[6] * inv, o[7] * inv));
-      }
-      __syncwarp();
+        for (int i = 0; i < WA_D; i += 8) {
+          const float* o = reinterpret_cast<const float*>(ov + i);
+          *reinterpret_cast<uint4*>(stg + lane * 128 + (((i >> 3) ^ (lane & 7)) << 4)) =
+              make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]),
+                         pack_bf16(o[6], o[7]));
+        }
+        __syncwarp();
 #pragma unroll
-      for (int i = 0; i < 32; i += 4) {
-        const int rr = i + (lane >> 3), p = lane & 7;
-        const uint4 v = *reinterpret_cast<const uint4*>(stg + rr * 128 + ((p ^ (rr & 7)) << 4));
-        if (q0 + rr < a.w.L)
-          *reinterpret_cast<uint4*>(a.out + ((long)m.b * a.w.L + q0 + rr) * a.ldo + m.h * WA_D +
-                                    p * 8) = v;
+        for (int i = 0; i < 32; i += 4) {
+          const int rr = i + (lane >> 3), p = lane & 7;
+          const uint4 v = *reinterpret_cast<const uint4*>(stg + rr * 128 + ((p ^ (rr & 7)) << 4));
+          if (q0 + rr < a.w.L)
+            *reinterpret_cast<uint4*>(dst + ((long)m.b * a.w.L + q0 + rr) * ld + m.h * WA_D + p * 8) =
+                v;
+        }
+        __syncwarp();
+      };
+#pragma unroll
+      for (int i = 0; i < WA_D; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * inv);
+      put(a.out, a.ldo);
+      if (a.lse) {  // the backward's Di = dO . O cancels against dP: it wants more than bf16's O
+#pragma unroll
+        for (int i = 0; i < WA_D; ++i) {
+          const float o = __uint_as_float(ov[i]);
+          ov[i] = __float_as_uint(o - __bfloat162float(__float2bfloat16(o)));
+        }
+        put(a.rest, (long)a.H * WA_D);
       }
-      __syncwarp();
       if (a.lse && q < a.w.L)
         a.lse[((long)m.b * a.H + m.h) * a.w.L + q] = mref + log2f(l);  // log2 units
     }
@@ -467,7 +481,13 @@ double window_pairs(const Window& c) {
   return W * (W + 1) / 2 + (L - W) * W + S * (S + 1) / 2 + (L - W - S) * S;
 }
 
-cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, float* lse,
+WindowSaved window_saved(const Window& c, void* p) {
+  const size_t rows = (size_t)c.B * c.L, lse = (rows * c.H * sizeof(float) + 255) & ~size_t(255);
+  return {static_cast<float*>(p), reinterpret_cast<bf16*>(static_cast<char*>(p) + lse),
+          lse + rows * c.H * WA_D * sizeof(bf16)};
+}
+
+cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, const WindowSaved& v,
                        cudaStream_t st) {
   CUtensorMap tq, tk, tv;
   if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WA_D, c.L, c.B, x.ldq, WA_D, WT) ||
@@ -476,7 +496,8 @@ cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, fl
     return cudaErrorInvalidValue;
   WaArgs a{};
   a.out = out;
-  a.lse = lse;
+  a.lse = v.lse;
+  a.rest = v.rest;
   a.ldo = ldo;
   a.B = c.B;
   a.H = c.H;
@@ -493,7 +514,8 @@ cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, fl
   if (e != cudaSuccess) return e;
   const double pairs = (double)c.B * c.H * window_pairs(c);
   LaunchTimer lt("window_fwd", st, 4.0 * WA_D * pairs,
-                 2.0 * c.B * c.L * WA_D * (2.0 * c.H + 2.0 * c.KV) + 4.0 * c.B * c.H * c.L);
+                 2.0 * c.B * c.L * WA_D * ((v.lse ? 3.0 : 2.0) * c.H + 2.0 * c.KV) +
+                     (v.lse ? 4.0 * c.B * c.H * c.L : 0.0));
   const int grid = std::min(a.n_items, num_sms());
   return launch_kernel(window_fwd_kernel, grid, WA_THREADS, WA_SMEM, st, tq, tk, tv, a);
 }

@@ -1,6 +1,7 @@
 // Backward of the windowed attention with sinks on the tcgen05 tensor cores,
 // head width 64, grouped heads.  With P = softmax(q k / 8) recomputed from the
-// saved LSE and Di = rowsum(dO * O):
+// saved LSE and Di = rowsum(dO * O), with O to 2^-17 (dS is a difference of the two: with
+// O as rounded to bf16, rows of few keys lose dQ and dK to it):
 //   dP = dO V^T,   dS = P * (dP - Di),   dV = P^T dO,   dK = dS^T Q / 8,
 //   dQ = dS K / 8,   dK and dV summed over the query heads of a key head.
 // Two kernels share one skeleton (no atomics, deterministic):
@@ -531,6 +532,7 @@ __global__ void __launch_bounds__(128) window_join_kernel(WbArgs a) {
 // each eight of the head's 64 columns with 16-byte loads.
 __global__ void __launch_bounds__(256) window_dot_kernel(const bf16* __restrict__ dO, long lddo,
                                                          const bf16* __restrict__ O, long ldo,
+                                                         const bf16* __restrict__ rest,
                                                          float* __restrict__ Di, long rows, int L,
                                                          int H) {
   const int pz = pdl_enter();
@@ -539,11 +541,12 @@ __global__ void __launch_bounds__(256) window_dot_kernel(const bf16* __restrict_
   const bool live = gid < items;
   const long it = live ? gid : items - 1, row = it / H;
   const int h = (int)(it % H);
-  float x[8], y[8], v = 0.f;
+  float x[8], y[8], z[8], v = 0.f;
   load8_bf16(dO + row * lddo + h * WB_D + sub * 8, x);
   load8_bf16(O + row * ldo + h * WB_D + sub * 8, y);
+  load8_bf16(rest + it * WB_D + sub * 8, z);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) v = fmaf(x[k], y[k], v);
+  for (int k = 0; k < 8; ++k) v = fmaf(x[k], y[k] + z[k], v);
 #pragma unroll
   for (int s = 4; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
   if (live && sub == 0) Di[(row / L * H + h) * L + row % L] = v;
@@ -612,7 +615,7 @@ cudaError_t wb_launch(const CUtensorMap& x1, const CUtensorMap& x2, const CUtens
 size_t window_bwd_ws_bytes(const Window& c) { return wb_carve(nullptr, c).bytes; }
 
 cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long ldo,
-                       const float* lse, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
+                       const WindowSaved& v, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
                        cudaStream_t st) {
   CUtensorMap tq, tk, tv, td;
   if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WB_D, c.L, c.B, x.ldq, WB_D, WT) ||
@@ -620,12 +623,12 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
       !tmap_bf16_seq(&tv, x.v, (uint64_t)c.KV * WB_D, c.L, c.B, x.ldv, WB_D, WT) ||
       !tmap_bf16_seq(&td, dout, (uint64_t)c.H * WB_D, c.L, c.B, lddo, WB_D, WT))
     return cudaErrorInvalidValue;
-  const WbWs v = wb_carve(ws, c);
+  const WbWs wk = wb_carve(ws, c);
   const Cut k = wb_cut(c);
   WbArgs a{};
-  a.lse = lse;
-  a.Di = v.Di;
-  a.part = v.part;
+  a.lse = v.lse;
+  a.Di = wk.Di;
+  a.part = wk.part;
   a.B = c.B; a.H = c.H; a.KV = c.KV; a.g = c.H / c.KV;
   a.w = WinTiles(c);
   a.C = k.C; a.np_s = k.np_s; a.np_w = k.np_w;
@@ -636,10 +639,10 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
   const double rows = (double)c.B * c.L, pairs = (double)c.B * c.H * window_pairs(c);
   cudaError_t e;
   {
-    LaunchTimer lt("window_bwd_dot", st, 2.0 * rows * c.H * WB_D, rows * c.H * (4.0 * WB_D + 4.0));
+    LaunchTimer lt("window_bwd_dot", st, 2.0 * rows * c.H * WB_D, rows * c.H * (6.0 * WB_D + 4.0));
     const long n = (long)c.B * c.L;
     e = launch_kernel(window_dot_kernel, (unsigned)((n * c.H * 8 + 255) / 256), 256, 0, st, dout, lddo,
-                      out, ldo, v.Di, n, c.L, c.H);
+                      out, ldo, v.rest, wk.Di, n, c.L, c.H);
     if (e != cudaSuccess) return e;
   }
   a.out_u = static_cast<bf16*>(dx.v);

@@ -10,38 +10,49 @@ apart (a slice of a projection's output serves as it is).
 """
 from __future__ import annotations
 
+from ctypes import byref
 from typing import Optional, Sequence, Tuple
 
 import torch
 
-from . import (PF_BF16, PF_ERR_CAPACITY, PF_ERR_INVALID_ARG, PF_F32, PagedCache, PagedDesc,
-               ProxyFormerError, QKDesc, WindowDesc, _ptr, pf_paged_advance, pf_paged_append,
-               pf_paged_attn, pf_paged_attn_workspace_size, pf_qk_rope_bwd, pf_qk_rope_fwd,
-               pf_qk_rope_workspace_size, pf_window_attn_bwd, pf_window_attn_fwd,
-               pf_window_attn_workspace_size, qkv)
+from . import (PF_BF16, PF_ERR_CAPACITY, PF_ERR_INVALID_ARG, PF_F32, QKV, PagedCache, PagedDesc,
+               ProxyFormerError, QKDesc, WindowDesc, _check, _ptr, load, pf_paged_advance,
+               pf_paged_attn_workspace_size, pf_qk_rope_workspace_size, pf_window_attn_saved_size,
+               pf_window_attn_workspace_size)
+
+# The operators take a few microseconds where a token or two is served, less than a
+# call's Python costs: the methods below check their tensors once, fill the C structs
+# by position and call the library's function that __init__ looked up.
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+def _stream(t: torch.Tensor) -> int:
+    """The current stream of t's device (torch.cuda.current_stream().cuda_stream, without
+    the object: 0.1 us for 2.8)."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
-def _rows(name: str, t: torch.Tensor, rows: int, width: int, dtype: torch.dtype) -> torch.Tensor:
-    """t as the library takes it: a 2D CUDA matrix with its values side by side in a row."""
-    if (t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or t.dtype != dtype
-            or not t.is_cuda or (width > 1 and t.stride(1) != 1)):
+def _rows(name: str, t: torch.Tensor, rows: int, width: int, dtype: torch.dtype) -> int:
+    """Checks that the library can take t, a 2D CUDA matrix with its values side by side
+    in a row, and returns its leading dimension."""
+    if t.dtype is not dtype or t.shape != (rows, width) or not t.is_cuda:
+        bad = True
+    else:
+        ld, one = t.stride()
+        bad = one != 1 and width > 1
+    if bad:
         raise ProxyFormerError(PF_ERR_INVALID_ARG, f"{name} must be a [{rows}, {width}] {dtype} "
                                "CUDA matrix with contiguous rows")
-    if rows == 1 and t.stride(0) != width:  # the stride of a single row says nothing
-        t = t.as_strided((1, width), (width, 1))
-    return t
+    return ld if rows > 1 else width  # the stride of a single row says nothing
 
 
-def _ints(name: str, t: Optional[torch.Tensor], *shape: int) -> Optional[torch.Tensor]:
-    if t is not None and (tuple(t.shape) != shape or t.dtype != torch.int32 or not t.is_cuda
-                          or not t.is_contiguous()):
+def _ints(name: str, t: Optional[torch.Tensor], *shape: int) -> Optional[int]:
+    """Pointer of an int32 CUDA tensor of that shape, or None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous():
         raise ProxyFormerError(PF_ERR_INVALID_ARG, f"{name} must be a contiguous int32 CUDA tensor "
                                f"of shape {list(shape)}")
-    return t
+    return t.data_ptr()
 
 
 class QKRope:
@@ -60,46 +71,56 @@ class QKRope:
                                   or not w.is_contiguous() or not w.is_cuda):
                 raise ProxyFormerError(PF_ERR_INVALID_ARG, f"{n} must be {dh} fp32 values on the GPU")
         self.n_heads, self.n_kv, self.dh, self.dtype, self.n_axes = n_heads, n_kv, dh, dtype, len(pairs)
+        self.nq, self.nk = n_heads * dh, n_kv * dh
         self.w_q, self.w_k = w_q, w_k
+        self.pw_q, self.pw_k = _ptr(w_q), _ptr(w_k)
         self.desc = QKDesc(n_heads, n_kv, dh, PF_F32 if dtype == torch.float32 else PF_BF16,
                            len(pairs), (pairs + (0, 0, 0))[:3], theta, eps)
+        self.ref = byref(self.desc)
+        self.fwd, self.bwd = load().pf_qk_rope_fwd, load().pf_qk_rope_bwd
         self.ws: Optional[torch.Tensor] = None
 
-    def _qk(self, rows: int, q: torch.Tensor, k: torch.Tensor):
-        return (_rows("q", q, rows, self.n_heads * self.dh, self.dtype),
-                _rows("k", k, rows, self.n_kv * self.dh, self.dtype))
+    def _qk(self, rows: int, q: torch.Tensor, k: torch.Tensor) -> QKV:
+        lq, lk = _rows("q", q, rows, self.nq, self.dtype), _rows("k", k, rows, self.nk, self.dtype)
+        return QKV(q.data_ptr(), k.data_ptr(), None, lq, lk, 0)
+
+    def _new(self, rows: int, device) -> Tuple[torch.Tensor, torch.Tensor]:
+        return (torch.empty((rows, self.nq), dtype=self.dtype, device=device),
+                torch.empty((rows, self.nk), dtype=self.dtype, device=device))
 
     def forward(self, q: torch.Tensor, k: torch.Tensor, L: Optional[int] = None,
                 pos: Optional[torch.Tensor] = None, out=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """q [rows, n_heads*dh], k [rows, n_kv*dh] -> the same normed and turned (into
         ``out``, a pair, which may be (q, k) itself).  Positions: pos [rows, axes]
         int32, or the row's place in its sequence of L rows (default: one sequence)."""
-        rows = int(q.shape[0])
-        q, k = self._qk(rows, q, k)
-        qo, ko = (torch.empty((rows, t.shape[1]), dtype=t.dtype, device=t.device) for t in (q, k)) \
-            if out is None else self._qk(rows, *out)
-        pf_qk_rope_fwd(self.desc, rows, L or max(rows, 1), qkv(q, k), self.w_q, self.w_k,
-                       _ints("pos", pos, rows, self.n_axes), qkv(qo, ko), _stream())
-        return qo, ko
+        rows = q.shape[0]
+        x = self._qk(rows, q, k)
+        out = self._new(rows, q.device) if out is None else out
+        s = self.fwd(self.ref, rows, L or max(rows, 1), byref(x), self.pw_q, self.pw_k,
+                     _ints("pos", pos, rows, self.n_axes), byref(self._qk(rows, *out)), _stream(q))
+        if s:
+            _check(s)
+        return out
 
     def backward(self, q: torch.Tensor, k: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
                  L: Optional[int] = None, pos: Optional[torch.Tensor] = None, out=None):
         """From the forward's inputs and the gradients of its results: the gradients
         of q and k (into ``out``, which may be (dq, dk) itself) and of w_q and w_k
         (None without them)."""
-        rows = int(q.shape[0])
-        q, k = self._qk(rows, q, k)
-        dq, dk = self._qk(rows, dq, dk)
-        xq, xk = (torch.empty((rows, t.shape[1]), dtype=t.dtype, device=t.device) for t in (q, k)) \
-            if out is None else self._qk(rows, *out)
+        rows = q.shape[0]
+        x, g = self._qk(rows, q, k), self._qk(rows, dq, dk)
+        out = self._new(rows, q.device) if out is None else out
         dw_q, dw_k = (None if w is None else torch.empty_like(w) for w in (self.w_q, self.w_k))
         if self.ws is None and (dw_q is not None or dw_k is not None):
             self.ws = torch.empty(pf_qk_rope_workspace_size(self.desc), dtype=torch.uint8,
                                   device=q.device)
-        pf_qk_rope_bwd(self.desc, rows, L or max(rows, 1), qkv(q, k), self.w_q, self.w_k,
-                       _ints("pos", pos, rows, self.n_axes), qkv(dq, dk), qkv(xq, xk), dw_q, dw_k,
-                       self.ws, 0 if self.ws is None else self.ws.numel(), _stream())
-        return xq, xk, dw_q, dw_k
+        s = self.bwd(self.ref, rows, L or max(rows, 1), byref(x), self.pw_q, self.pw_k,
+                     _ints("pos", pos, rows, self.n_axes), byref(g), byref(self._qk(rows, *out)),
+                     _ptr(dw_q), _ptr(dw_k), _ptr(self.ws), 0 if self.ws is None else self.ws.numel(),
+                     _stream(q))
+        if s:
+            _check(s)
+        return (*out, dw_q, dw_k)
 
 
 class WindowAttention:
@@ -110,45 +131,51 @@ class WindowAttention:
                  n_sink: int = 0):
         self.rows, self.nq, self.nk = batch * L, n_heads * dh, n_kv * dh
         self.desc = WindowDesc(batch, L, n_heads, n_kv, dh, window, n_sink)
-        self.lse_shape = (batch, n_heads, L)
-        self.lse: Optional[torch.Tensor] = None  # of the last forward for training
+        self.ref = byref(self.desc)
+        self.fwd, self.bwd = load().pf_window_attn_fwd, load().pf_window_attn_bwd
+        self.saved_size = pf_window_attn_saved_size(self.desc)
+        self.saved: Optional[torch.Tensor] = None  # of the last forward for training
         self.ws: Optional[torch.Tensor] = None
 
-    def _qkv(self, q, k, v):
-        w, bf = self.rows, torch.bfloat16
-        return tuple(_rows(n, t, w, c, bf) for n, t, c in (("q", q, self.nq), ("k", k, self.nk),
-                                                           ("v", v, self.nk)))
+    def _qkv(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> QKV:
+        n, bf = self.rows, torch.bfloat16
+        ld = (_rows("q", q, n, self.nq, bf), _rows("k", k, n, self.nk, bf),
+              _rows("v", v, n, self.nk, bf))
+        return QKV(q.data_ptr(), k.data_ptr(), v.data_ptr(), *ld)
 
     def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, train: bool = True,
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """q [batch*L, n_heads*dh], k, v [batch*L, n_kv*dh] -> [batch*L, n_heads*dh];
-        ``train`` keeps the rows' log-sums for the backward."""
-        q, k, v = self._qkv(q, k, v)
-        out = torch.empty((self.rows, self.nq), dtype=q.dtype, device=q.device) if out is None else \
-            _rows("out", out, self.rows, self.nq, q.dtype)
+        ``train`` keeps what the backward needs beside them."""
+        x, bf, dev = self._qkv(q, k, v), torch.bfloat16, q.device
+        out = torch.empty((self.rows, self.nq), dtype=bf, device=dev) if out is None else out
         if train:  # a new buffer: the last forward's may still be read on another stream
-            self.lse = torch.empty(self.lse_shape, dtype=torch.float32, device=q.device)
-        pf_window_attn_fwd(self.desc, qkv(q, k, v), out, out.stride(0), self.lse if train else None,
-                           _stream())
+            self.saved = torch.empty(self.saved_size, dtype=torch.uint8, device=dev)
+        s = self.fwd(self.ref, byref(x), out.data_ptr(), _rows("out", out, self.rows, self.nq, bf),
+                     self.saved.data_ptr() if train else None, _stream(q))
+        if s:
+            _check(s)
         return out
 
     def backward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
-                 dout: torch.Tensor, lse: Optional[torch.Tensor] = None, into=None):
+                 dout: torch.Tensor, saved: Optional[torch.Tensor] = None, into=None):
         """From the forward's inputs and result and the gradient of the result: the
-        gradients of q, k and v (into ``into``, three matrices, if given).  lse: the
-        forward's ``self.lse``, if another forward has run since."""
-        q, k, v = self._qkv(q, k, v)
-        out, dout = (_rows(n, t, self.rows, self.nq, q.dtype) for n, t in (("out", out), ("dout", dout)))
-        lse = self.lse if lse is None else lse
-        if lse is None:
+        gradients of q, k and v (into ``into``, three matrices, if given).  saved: that
+        forward's ``self.saved``, if another forward has run since."""
+        x, bf, dev = self._qkv(q, k, v), torch.bfloat16, q.device
+        saved = self.saved if saved is None else saved
+        if saved is None or saved.numel() < self.saved_size:
             raise ProxyFormerError(PF_ERR_INVALID_ARG, "backward needs a forward with train=True")
-        dx = tuple(torch.empty((self.rows, t.shape[1]), dtype=t.dtype, device=t.device)
-                   for t in (q, k, v)) if into is None else self._qkv(*into)
+        dx = tuple(torch.empty((self.rows, n), dtype=bf, device=dev)
+                   for n in (self.nq, self.nk, self.nk)) if into is None else into
         if self.ws is None:
             self.ws = torch.empty(pf_window_attn_workspace_size(self.desc), dtype=torch.uint8,
-                                  device=q.device)
-        pf_window_attn_bwd(self.desc, qkv(q, k, v), out, out.stride(0), lse, dout, dout.stride(0),
-                           qkv(*dx), self.ws, self.ws.numel(), _stream())
+                                  device=dev)
+        s = self.bwd(self.ref, byref(x), out.data_ptr(), _rows("out", out, self.rows, self.nq, bf),
+                     saved.data_ptr(), dout.data_ptr(), _rows("dout", dout, self.rows, self.nq, bf),
+                     byref(self._qkv(*dx)), self.ws.data_ptr(), self.ws.numel(), _stream(q))
+        if s:
+            _check(s)
         return dx
 
 
@@ -176,11 +203,15 @@ class PagedKVCache:
             if tuple(t.shape) != shape or t.dtype != torch.bfloat16 or not t.is_contiguous():
                 raise ProxyFormerError(PF_ERR_INVALID_ARG, f"K and V must be contiguous bf16 {shape}")
         self.table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device) \
-            if table is None else _ints("table", table, batch, max_pages)
-        self.len = torch.zeros(batch, dtype=torch.int32, device=device) \
-            if len is None else _ints("len", len, batch)
+            if table is None else table
+        self.len = torch.zeros(batch, dtype=torch.int32, device=device) if len is None else len
+        self.nq, self.nk = n_heads * dh, n_kv * dh
         self.desc = PagedDesc(batch, n_heads, n_kv, dh, page, max_pages, n_pages, window, n_sink)
-        self.cache = PagedCache(_ptr(self.K), _ptr(self.V), _ptr(self.table), _ptr(self.len))
+        self.cache = PagedCache(self.K.data_ptr(), self.V.data_ptr(),
+                                _ints("table", self.table, batch, max_pages),
+                                _ints("len", self.len, batch))
+        self.ref, self.cref = byref(self.desc), byref(self.cache)
+        self.f_append, self.f_attn = load().pf_paged_append, load().pf_paged_attn
         self.ws = torch.empty(max(16, pf_paged_attn_workspace_size(self.desc)), dtype=torch.uint8,
                               device=device)
         self.free = list(range(n_pages - 1, -1, -1))  # pages that reserve() hands out
@@ -210,7 +241,8 @@ class PagedKVCache:
     def advance(self, start: Optional[torch.Tensor] = None) -> None:
         """The lengths at the start of a step: start[b+1] - start[b] more rows of
         every sequence b, or one."""
-        pf_paged_advance(self.desc, _ints("start", start, self.batch + 1), self.cache, _stream())
+        pf_paged_advance(self.desc, _ints("start", start, self.batch + 1), self.cache,
+                         _stream(self.len))
 
     def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                start: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
@@ -218,26 +250,29 @@ class PagedKVCache:
         """The step's tokens, k, v [rows, n_kv*dh], into the cache; returns their
         queries q [rows, n_heads*dh] normed and turned (None without them).  start
         [batch+1] int32: first token of every sequence; None: one each."""
-        rows, bf = int(k.shape[0]), torch.bfloat16
-        k, v = (_rows(n, t, rows, self.n_kv * self.dh, bf) for n, t in (("k", k), ("v", v)))
-        if q is not None:
-            q = _rows("q", q, rows, self.n_heads * self.dh, bf)
-            out = torch.empty((rows, q.shape[1]), dtype=bf, device=q.device) if out is None else \
-                _rows("out", out, rows, q.shape[1], bf)
+        rows, bf = k.shape[0], torch.bfloat16
+        lk, lv = _rows("k", k, rows, self.nk, bf), _rows("v", v, rows, self.nk, bf)
+        if q is None:
+            x, out, po, lo = QKV(None, k.data_ptr(), v.data_ptr(), 0, lk, lv), None, None, 0
         else:
-            out = None
-        pf_paged_append(self.desc, self.rope.desc, rows, qkv(q, k, v), self.rope.w_q, self.rope.w_k,
-                        _ints("start", start, self.batch + 1),
-                        _ints("pos", pos, rows, self.rope.n_axes), self.cache, out,
-                        0 if out is None else out.stride(0), _stream())
+            x = QKV(q.data_ptr(), k.data_ptr(), v.data_ptr(), _rows("q", q, rows, self.nq, bf), lk, lv)
+            out = torch.empty((rows, self.nq), dtype=bf, device=q.device) if out is None else out
+            po, lo = out.data_ptr(), _rows("out", out, rows, self.nq, bf)
+        r = self.rope
+        s = self.f_append(self.ref, r.ref, rows, byref(x), r.pw_q, r.pw_k,
+                          _ints("start", start, self.batch + 1), _ints("pos", pos, rows, r.n_axes),
+                          self.cref, po, lo, _stream(k))
+        if s:
+            _check(s)
         return out
 
     def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of every sequence's newest token, q [batch, n_heads*dh]."""
-        width = self.n_heads * self.dh
-        q = _rows("q", q, self.batch, width, torch.bfloat16)
-        out = torch.empty((self.batch, width), dtype=q.dtype, device=q.device) if out is None else \
-            _rows("out", out, self.batch, width, q.dtype)
-        pf_paged_attn(self.desc, q, q.stride(0), self.cache, out, out.stride(0), self.ws,
-                      self.ws.numel(), _stream())
+        n, bf = self.batch, torch.bfloat16
+        out = torch.empty((n, self.nq), dtype=bf, device=q.device) if out is None else out
+        s = self.f_attn(self.ref, q.data_ptr(), _rows("q", q, n, self.nq, bf), self.cref,
+                        out.data_ptr(), _rows("out", out, n, self.nq, bf), self.ws.data_ptr(),
+                        self.ws.numel(), _stream(q))
+        if s:
+            _check(s)
         return out

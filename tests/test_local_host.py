@@ -68,17 +68,17 @@ def test_window_refusals():
     bad, no = pf.PF_ERR_INVALID_ARG, pf.PF_ERR_UNSUPPORTED
     B = A * 2  # addresses of the gradients
     grads = lambda **kw: rows(**{**dict(q=B, k=B, v=B), **kw})
-    fwd = lambda d=win(), x=rows(), out=A, ld=256, lse=A: pf.pf_window_attn_fwd(d, x, out, ld, lse)
+    fwd = lambda d=win(), x=rows(), out=A, ld=256, saved=A: pf.pf_window_attn_fwd(d, x, out, ld, saved)
 
-    def bwd(d=win(), x=rows(), out=A, ld=256, lse=A, dout=A, ld_d=256, dx=None, ws=A, size=1 << 40):
-        pf.pf_window_attn_bwd(d, x, out, ld, lse, dout, ld_d, dx or grads(), ws, size)
+    def bwd(d=win(), x=rows(), out=A, ld=256, saved=A, dout=A, ld_d=256, dx=None, ws=A, size=1 << 40):
+        pf.pf_window_attn_bwd(d, x, out, ld, saved, dout, ld_d, dx or grads(), ws, size)
     for s, kws in ((bad, (dict(batch=0), dict(L=0), dict(n_kv=3), dict(window=-1), dict(n_sink=-2))),
                    (no, (dict(dh=128), dict(dh=32), dict(L=1 << 30), dict(batch=1 << 16, L=1 << 15),
                          dict(batch=1 << 20, L=1024, n_heads=64)))):
         for kw in kws:
             refused(s, fwd, win(**kw))
             refused(s, bwd, win(**kw))
-            assert pf.pf_window_attn_workspace_size(win(**kw)) == 0
+            assert pf.pf_window_attn_workspace_size(win(**kw)) == pf.pf_window_attn_saved_size(win(**kw)) == 0
     for kw in (dict(q=None), dict(k=A + 8), dict(v=None), dict(ld_q=248), dict(ld_k=132), dict(ld_v=64)):
         refused(bad, lambda: fwd(x=rows(**kw)))
         refused(bad, lambda: bwd(x=rows(**kw)))
@@ -86,7 +86,9 @@ def test_window_refusals():
     for kw in (dict(out=None), dict(out=A + 2), dict(ld=128), dict(ld=260)):
         refused(bad, lambda: fwd(**kw))
         refused(bad, lambda: bwd(**kw))
-    refused(bad, lambda: bwd(lse=None))
+    refused(bad, lambda: bwd(saved=None))
+    refused(bad, lambda: bwd(saved=A + 4))
+    refused(bad, lambda: fwd(saved=A + 4))
     refused(bad, lambda: bwd(dout=None))
     refused(bad, lambda: bwd(dx=grads(k=A)))  # a gradient over an input
     need = pf.pf_window_attn_workspace_size(win())
