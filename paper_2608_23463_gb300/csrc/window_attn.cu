@@ -13,10 +13,10 @@
 //   warp 0    TMA producer: the item's two Q tiles (double-buffered across
 //             items) and a WA_STAGES-deep ring of (K, V) 128-key tiles, shared
 //             by both query tiles; rows past the end of a sequence read as zero
-//   warp 1    MMA issuer: S_w = Q_w K_j^T (M=128, N=128, K=64) into tile w's
-//             TMEM score buffer, O_w += P_w V_j (M=128, N=64, K=128) with P_w
-//             from TMEM
-//   warps 4-7 softmax group A, warps 8-11 group B: one query row per thread
+//   warps 1-2 MMA issuers of tile A and tile B: S = Q K_j^T (M=128, N=128, K=64)
+//             into the tile's TMEM score buffer as soon as its last scores are
+//             in registers, O += P V_j (M=128, N=64, K=128) with P from TMEM
+//   warps 4-7 softmax of tile A, warps 8-11 of tile B: one query row per thread
 //             (TMEM lane), its 128 scores in registers; P goes back to TMEM
 // A row's probabilities are taken against a reference m, the maximum of the
 // first tile in which the row sees a key, raised only when a later tile's
@@ -43,7 +43,7 @@ namespace {
 
 constexpr int WA_D = 64;  // head width
 constexpr int WA_STAGES = 4;
-constexpr int WA_THREADS = 384;  // producer, MMA, two idle warps, two softmax groups of four
+constexpr int WA_THREADS = 384;  // producer, two MMA issuers, an idle warp, two groups of four
 // A softmax thread holds a row's 128 scores: the control warps give registers up, of the
 // 168 that each thread has at launch.
 constexpr int WA_REGS_CTRL = 88, WA_REGS_ROWS = 208;
@@ -51,12 +51,14 @@ static_assert(WA_REGS_CTRL * 128 + WA_REGS_ROWS * 256 == 168 * WA_THREADS, "regi
 constexpr float WA_RESCALE = 8.f;
 constexpr uint32_t WA_T_BYTES = WT * WA_D * 2;  // 16 KB: a Q, K or V tile
 constexpr uint32_t WA_OFF_KV = 4 * WA_T_BYTES;  // Q: [2 items][tiles A, B]
-constexpr uint32_t WA_OFF_BAR = WA_OFF_KV + WA_STAGES * 2 * WA_T_BYTES;
-constexpr uint32_t WA_OFF_STG = WA_OFF_BAR + 256;  // 32 output rows of each softmax warp
-constexpr uint32_t WA_SMEM = WA_OFF_STG + 8 * 32 * WA_D * 2 + 1024;
-// TMEM columns of group w: scores S at 128 w (fp32), O at 256 + 64 w (fp32),
-// P at 384 + 64 w (bf16 pairs: key 2c in the low half of column c)
+constexpr uint32_t WA_OFF_STG = WA_OFF_KV + WA_STAGES * 2 * WA_T_BYTES;  // a softmax warp's 32 output rows
+constexpr uint32_t WA_OFF_BAR = WA_OFF_STG + 8 * 32 * WA_D * 2;
+constexpr uint32_t WA_SMEM = WA_OFF_BAR + 512 + 1024;
+static_assert(WA_SMEM <= 227 * 1024, "shared memory");
+// TMEM columns of tile w: scores S at 128 w (fp32), O at 256 + 64 w (fp32), P at
+// 384 + 64 w (bf16 pairs: key 2c in the low half of column c)
 constexpr uint32_t WA_TMEM_COLS = 512;
+constexpr uint32_t WA_TM_O = 256, WA_TM_P = 384;
 
 struct WaArgs {
   bf16* out;   // [B*L, ldo], head h at column h*64
@@ -92,10 +94,30 @@ struct WaItem {
   __device__ __forceinline__ int tile(int j) const { return j < ns ? j : lo + j - ns; }
 };
 
+// The steps of an item that query tile t takes part in: [0, a0) and [a1, a2).  Tile B
+// may have left key tiles behind that A's window still holds, and A does not reach
+// B's diagonal.
+struct WaSteps {
+  int a0, a1, a2;
+  __device__ __forceinline__ WaSteps(const WaArgs& a, const WaItem& m, int t) {
+    const int gap = max(m.lo, a.w.sT);  // first tile that only the window can show
+    a1 = m.ns + max(a.w.lo(t) - m.lo, 0);
+    a0 = min(m.ns + gap - m.lo, a1);
+    a2 = t < a.w.n_t ? m.ns + t - m.lo + 1 : 0;
+    if (t >= a.w.n_t) a0 = a1 = 0;
+  }
+};
+
 __device__ __forceinline__ float ex2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// mbar_wait_warp with the common case, a phase that has completed, up front.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
+  if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
+  return mbar_wait_warp(bar, parity);
 }
 
 __global__ void __launch_bounds__(WA_THREADS, 1)
@@ -104,10 +126,9 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + WA_OFF_BAR);
-  // q_full[2] q_empty[2] kv_full[S] kv_empty[S], per group w: s_full s_free
-  // p_full p_free o_full o_free, done
-  const uint32_t b0 = smem_u32(bars);
+  // q_full[2] q_empty[2] kv_full[S] kv_empty[S], per tile w: s_full s_free p_full
+  // p_free o_full o_free, done
+  const uint32_t b0 = smem_u32(smem + WA_OFF_BAR);
   const uint32_t q_full = b0, q_empty = b0 + 16, kv_full = b0 + 32,
                  kv_empty = kv_full + 8 * WA_STAGES, grp0 = kv_empty + 8 * WA_STAGES,
                  done = grp0 + 2 * 48;
@@ -117,16 +138,16 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
   auto p_free = [&](int w) { return grp0 + 48 * w + 24; };
   auto o_full = [&](int w) { return grp0 + 48 * w + 32; };
   auto o_free = [&](int w) { return grp0 + 48 * w + 40; };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + WA_OFF_BAR + 240);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + WA_OFF_BAR + 448);
   const uint32_t sbase = smem_u32(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full + 8 * i, 1);
-      mbar_init(q_empty + 8 * i, 1);
+      mbar_init(q_empty + 8 * i, 2);  // one arrival per MMA issuer
       mbar_init(s_full(i), 1);
-      mbar_init(s_free(i), 4);  // one arrival per softmax warp of the group
+      mbar_init(s_free(i), 4);  // one arrival per softmax warp of the tile
       mbar_init(p_full(i), 4);
       mbar_init(p_free(i), 1);
       mbar_init(o_full(i), 1);
@@ -134,9 +155,9 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
     }
     for (int i = 0; i < WA_STAGES; ++i) {
       mbar_init(kv_full + 8 * i, 1);
-      mbar_init(kv_empty + 8 * i, 1);
+      mbar_init(kv_empty + 8 * i, 2);  // one arrival per MMA issuer
     }
-    mbar_init(done, 1);
+    mbar_init(done, 2);
     fence_barrier_init();
   }
   if (warp == 1) {
@@ -185,91 +206,77 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
           kv_issued = g + 1;
         }
       }
-    } else if (warp == 1) {
-      // ------------------------------------------------------------ MMA issuer
+    } else if (warp == 1 || warp == 2) {
+      // ------------------------------------------------------------ MMA issuers
       // The whole warp runs the loop; one elected lane issues and commits.
+      const int w = warp - 1;
       constexpr uint32_t idesc_s = idesc_bf16_f32(WT, WT, 0, 0);
       constexpr uint32_t idesc_o = idesc_bf16_f32(WT, WA_D, 0, 1);
-      bool ok = true;
-      uint32_t G = 0, it = 0;
-      uint32_t gs[2] = {0, 0}, gp[2] = {0, 0};  // score and P V products of each group so far
-      uint32_t io[2] = {0, 0};                  // items of each group so far
-      int pv[2];                                // P V products of the item so far
-      // O_w (+)= P_w V for step jj of item m (G: its first stage)
-      auto issue_pv = [&](const WaItem& m, int jj) -> bool {
-        const uint32_t st = (G + jj) % WA_STAGES;
-        const uint32_t vb = sbase + WA_OFF_KV + st * 2 * WA_T_BYTES + WA_T_BYTES;
-        const int kt = m.tile(jj);
+      const uint32_t tS = tmem + 128 * w, tO = tmem + WA_TM_O + 64 * w, tP = tmem + WA_TM_P + 64 * w;
+      const uint64_t dq0 = smem_desc_sw128(sbase + w * WA_T_BYTES, 16, 1024);
+      const uint64_t dk0 = smem_desc_sw128(sbase + WA_OFF_KV, 16, 1024);
+      const uint64_t dv0 = smem_desc_sw128(sbase + WA_OFF_KV + WA_T_BYTES, 8192, 1024);
+      constexpr uint64_t STEP = 2 * WA_T_BYTES >> 4;  // a stage, in a descriptor's units
+      uint32_t G = 0;   // stages so far
+      uint32_t gs = 0;  // score products so far; those of P V are one behind
+      uint32_t io = 0;  // items so far
+      // O (+)= P V of the tile in stage st, the group's product gp
+      auto issue_pv = [&](uint32_t st, uint32_t gp, bool first, bool last) -> bool {
+        if (!wait_warp(p_full(w), gp & 1)) return false;
+        if (first && io > 0 && !wait_warp(o_free(w), (io - 1) & 1)) return false;
+        tc_fence_after();
+        const uint64_t dv = dv0 + st * STEP;
+        if (elect_one()) {
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const int t = 2 * m.u + w;
-          if (!a.w.sees(t, kt)) continue;
-          if (!mbar_wait_warp(p_full(w), gp[w] & 1)) return false;
-          if (pv[w] == 0 && io[w] > 0 && !mbar_wait_warp(o_free(w), (io[w] - 1) & 1)) return false;
-          tc_fence_after();
-          const uint32_t pt = tmem + 384 + 64 * w, ot = tmem + 256 + 64 * w;
-          if (elect_one()) {
-#pragma unroll
-            for (int kk = 0; kk < WT / 16; ++kk)
-              tc_mma_f16_ts(ot, pt + kk * 8, smem_desc_sw128(vb + kk * 2048, 8192, 1024), idesc_o,
-                            (pv[w] > 0 || kk > 0) ? 1u : 0u);
-            tc_commit(p_free(w));
-            if (kt == t) tc_commit(o_full(w));  // the diagonal tile is a row's last
-          }
-          __syncwarp();
-          ++gp[w];
-          ++pv[w];
+          for (int kk = 0; kk < WT / 16; ++kk)
+            tc_mma_f16_ts(tO, tP + kk * 8, dv + kk * (2048 >> 4), idesc_o, (!first || kk > 0) ? 1u : 0u);
+          tc_commit(p_free(w));
+          tc_commit(kv_empty + 8 * st);
+          if (last) tc_commit(o_full(w));
         }
-        if (elect_one()) tc_commit(kv_empty + 8 * st);
         __syncwarp();
         return true;
       };
-      for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items && ok;
-           k = wa_rank(blockIdx.x, ++rd), ++it) {
+      uint32_t it = 0;
+      for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items; k = wa_rank(blockIdx.x, ++rd), ++it) {
         const WaItem m(a, k);
+        const WaSteps sp(a, m, 2 * m.u + w);
         const uint32_t qb = it & 1;
-        pv[0] = pv[1] = 0;
-        if (!mbar_wait_warp(q_full + 8 * qb, (it >> 1) & 1)) break;
-        tc_fence_after();
-        for (int j = 0; j < m.n && ok; ++j) {
+        if (!wait_warp(q_full + 8 * qb, (it >> 1) & 1)) break;
+        const uint64_t dq = dq0 + qb * (2 * WA_T_BYTES >> 4);
+        uint32_t before = 0, seen = 0;  // stage of the tile before, tiles so far
+        int j = 0;
+        for (; j < m.n; ++j) {
           const uint32_t st = (G + j) % WA_STAGES;
-          if (!mbar_wait_warp(kv_full + 8 * st, ((G + j) / WA_STAGES) & 1)) {
-            ok = false;
-            break;
+          if (!wait_warp(kv_full + 8 * st, ((G + j) / WA_STAGES) & 1)) break;
+          if (j >= sp.a2 || (j >= sp.a0 && j < sp.a1)) {
+            // not this tile's (after the wait: else it could pass the ring's round)
+            if (elect_one()) mbar_arrive(kv_empty + 8 * st);
+            __syncwarp();
+            continue;
           }
+          if (gs > 0 && !wait_warp(s_free(w), (gs - 1) & 1)) break;
           tc_fence_after();
-          const uint32_t ks = sbase + WA_OFF_KV + st * 2 * WA_T_BYTES;
-          const int kt = m.tile(j);
+          const uint64_t dk = dk0 + st * STEP;
+          if (elect_one()) {
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            if (!a.w.sees(2 * m.u + w, kt)) continue;
-            if (gs[w] > 0 && !mbar_wait_warp(s_free(w), (gs[w] - 1) & 1)) {
-              ok = false;
-              break;
-            }
-            tc_fence_after();
-            const uint32_t qs = sbase + (2 * qb + w) * WA_T_BYTES;
-            if (elect_one()) {
-#pragma unroll
-              for (int kk = 0; kk < WA_D / 16; ++kk)
-                tc_mma_f16(tmem + 128 * w, smem_desc_sw128(qs + kk * 32, 16, 1024),
-                           smem_desc_sw128(ks + kk * 32, 16, 1024), idesc_s, kk ? 1u : 0u);
-              tc_commit(s_full(w));
-            }
-            __syncwarp();
-            ++gs[w];
+            for (int kk = 0; kk < WA_D / 16; ++kk)
+              tc_mma_f16(tS, dq + kk * 2, dk + kk * 2, idesc_s, kk ? 1u : 0u);
+            tc_commit(s_full(w));
           }
-          if (!ok) break;
-          if (j == m.n - 1) {
-            if (elect_one()) tc_commit(q_empty + 8 * qb);
-            __syncwarp();
-          }
-          if (j > 0 && !issue_pv(m, j - 1)) ok = false;
+          __syncwarp();
+          if (seen > 0 && !issue_pv(before, gs - 1, seen == 1, false)) break;
+          before = st;
+          ++seen;
+          ++gs;
         }
-        if (!ok || !issue_pv(m, m.n - 1)) break;
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-          if (pv[w] > 0) ++io[w];
+        if (j < m.n) break;  // a wait ran out
+        if (elect_one()) tc_commit(q_empty + 8 * qb);
+        __syncwarp();
+        if (seen > 0) {
+          if (!issue_pv(before, gs - 1, seen == 1, true)) break;
+          ++io;
+        }
         G += m.n;
       }
       if (elect_one()) tc_commit(done);
@@ -278,30 +285,31 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(WA_REGS_ROWS));
     // ------------------------------------------------------------ softmax
-    const int w = (warp - 4) >> 2;  // group: query tile A (0) or B (1)
+    const int w = (warp - 4) >> 2;  // query tile A (0) or B (1)
     const int q4 = warp & 3;         // TMEM lane quarter
     const int r = q4 * 32 + lane;    // query row in the tile = TMEM lane
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
-    const uint32_t ts = tl + 128 * w, to = tl + 256 + 64 * w, tp = tl + 384 + 64 * w;
+    const uint32_t ts = tl + 128 * w, to = tl + WA_TM_O + 64 * w, tp = tl + WA_TM_P + 64 * w;
+    const float2 sl = make_float2(a.sl2, a.sl2);
     bool ok = true;
     uint32_t g = 0, io = 0;
-    for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items && ok;
-         k = wa_rank(blockIdx.x, ++rd)) {
+    for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items && ok; k = wa_rank(blockIdx.x, ++rd)) {
       const WaItem m(a, k);
       const int t = 2 * m.u + w;
       if (t >= a.w.n_t) continue;
       const int q = t * WT + r;  // query index in the sequence
+      // its key tiles: the sinks' [0, ns) and the window's [lo, t]; those of [whole, clear)
+      // lie partly before some row's window and are not all sinks
+      const int lo = a.w.lo(t), ns = min(a.w.sT, lo), whole = a.w.S / WT;
+      const int past = t * WT + WT - 1 - a.w.W, clear = past >= 0 ? past / WT + 1 : 0;
       float mref = -INFINITY, l = 0.f;
-      bool first = true;
-      for (int j = 0; j < m.n; ++j) {
-        const int kt = m.tile(j);
-        if (!a.w.sees(t, kt)) continue;
-        if (!mbar_wait_warp(s_full(w), g & 1)) {
+      for (int kt = ns > 0 ? 0 : lo; kt <= t; kt = kt + 1 == ns ? lo : kt + 1, ++g) {
+        if (!wait_warp(s_full(w), g & 1)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        // the row's scores into registers; then the next scores may replace them
+        // the scores into registers; then the next may replace them
         uint32_t sc[128];
 #pragma unroll
         for (int c = 0; c < 128; c += 32) tmem_ld32_async(ts + c, sc + c);
@@ -309,86 +317,91 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
         for (int c = 0; c < 128; c += 32) tmem_wait_ld(sc + c);
         tc_fence_before();
         mbar_arrive_warp(s_free(w));
-        if (kt == t) {  // the diagonal
+        if (kt < clear || kt == t) {
+          if (kt == t) {  // the diagonal
 #pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if (c > r) sc[c] = 0xff800000u;  // -inf
-        }
-        if (!a.w.inside(t, kt)) {  // keys that the window has passed
-          const int low = q - a.w.W + 1 - kt * WT, sk = a.w.S - kt * WT;
+            for (int c = 0; c < 128; ++c)
+              if (c > r) sc[c] = 0xff800000u;  // -inf
+          }
+          if (kt < clear && kt >= whole) {  // keys that the window has passed
+            const int low = q - a.w.W + 1 - kt * WT, sk = a.w.S - kt * WT;
 #pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if (c < low && c >= sk) sc[c] = 0xff800000u;
+            for (int c = 0; c < 128; ++c)
+              if (c < low && c >= sk) sc[c] = 0xff800000u;
+          }
         }
-        // the row maximum (log2 units), three-input maxima
+        // the maximum (log2 units), three-input maxima
         float mt;
         {
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float mx[8];
 #pragma unroll
-          for (int c = 0; c < 128; c += 8)
+          for (int c = 0; c < 8; ++c)
+            mx[c] = fmaxf(__uint_as_float(sc[2 * c]), __uint_as_float(sc[2 * c + 1]));
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              mx[i] = max3f(mx[i], __uint_as_float(sc[c + 2 * i]),
-                            __uint_as_float(sc[c + 2 * i + 1]));
-          mt = fmaxf(max3f(mx[0], mx[1], mx[2]), mx[3]) * a.sl2;
+          for (int c = 16; c < 128; c += 16)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              mx[e] = max3f(mx[e], __uint_as_float(sc[c + 2 * e]), __uint_as_float(sc[c + 2 * e + 1]));
+          mt = max3f(max3f(mx[0], mx[1], mx[2]), max3f(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * a.sl2;
         }
         // the first keys set the reference; later ones raise it only by more than
         // WA_RESCALE, scaling O and the running sum
-        float corr = 1.f, mnew = mref;
-        if (mt > mref + WA_RESCALE) {
-          mnew = mt;
-          if (mref != -INFINITY) corr = ex2_approx(mref - mnew);
+        if (__any_sync(0xffffffffu, mt > mref + WA_RESCALE)) {
+          float corr = 1.f;
+          if (mt > mref + WA_RESCALE) {
+            if (mref != -INFINITY) corr = ex2_approx(mref - mt);
+            mref = mt;
+          }
+          if (__any_sync(0xffffffffu, corr != 1.f)) {  // this warp's rows of O
+            if (!wait_warp(p_free(w), (g - 1) & 1)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < 64; c += 16) {
+              uint32_t ov[16];
+              tmem_ld16(to + c, ov);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+              tmem_st16(to + c, ov);
+            }
+            l *= corr;
+          }
         }
-        // P_w of the previous tile has been consumed (and O_w updated) by
-        // the time this wait returns; a new item waited on o_full instead
-        if (!first && !mbar_wait_warp(p_free(w), (g - 1) & 1)) {
+        // P = 2^(s * sl2 - m) as bf16 pairs (key 2c, 2c + 1 in column c) and the row
+        // sum, with packed fp32x2 arithmetic
+        const float ref = mref == -INFINITY ? 0.f : mref;
+        const float2 nm = make_float2(-ref, -ref);
+        float2 ps[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        // the last tile's P has been consumed
+        if (g > 0 && !wait_warp(p_free(w), (g - 1) & 1)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        // P = 2^(s * sl2 - m) into TMEM as bf16 pairs (key 2c, 2c + 1 in
-        // column c) and the row sum, with packed fp32x2 arithmetic
-        float2 ps = make_float2(0.f, 0.f);
-        {
-          const float ref = mnew == -INFINITY ? 0.f : mnew;
-          const float2 sl = make_float2(a.sl2, a.sl2), nm = make_float2(-ref, -ref);
 #pragma unroll
-          for (int hh = 0; hh < 4; ++hh) {
-            uint32_t pk[16];
+        for (int hh = 0; hh < 4; ++hh) {
+          uint32_t pk[16];
 #pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-              const float2 z = __ffma2_rn(make_float2(__uint_as_float(sc[32 * hh + c]),
-                                                      __uint_as_float(sc[32 * hh + c + 1])),
-                                          sl, nm);
-              const float2 pp = make_float2(ex2_approx(z.x), ex2_approx(z.y));
-              ps = __fadd2_rn(ps, pp);
-              pk[c >> 1] = pack_bf16(pp.x, pp.y);
-            }
-            tmem_st16(tp + 16 * hh, pk);
+          for (int c = 0; c < 16; ++c) {
+            const float2 z = __ffma2_rn(make_float2(__uint_as_float(sc[32 * hh + 2 * c]),
+                                                    __uint_as_float(sc[32 * hh + 2 * c + 1])),
+                                        sl, nm);
+            const float2 pp = make_float2(ex2_approx(z.x), ex2_approx(z.y));
+            ps[c & 1] = __fadd2_rn(ps[c & 1], pp);
+            pk[c] = pack_bf16(pp.x, pp.y);
           }
+          tmem_st16(tp + 16 * hh, pk);
         }
-        const float psum = ps.x + ps.y;
-        if (__any_sync(0xffffffffu, corr != 1.f)) {  // rescale this warp's rows of O
-#pragma unroll 1
-          for (int c = 0; c < 64; c += 16) {
-            uint32_t ov[16];
-            tmem_ld16(to + c, ov);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr);
-            tmem_st16(to + c, ov);
-          }
-        }
-        l = fmaf(l, corr, psum);
-        mref = mnew;
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive_warp(p_full(w));
-        ++g;
-        first = false;
+        l += (ps[0].x + ps[0].y) + (ps[1].x + ps[1].y);
       }
       if (!ok) break;
       // the item's O: after its last P.V
-      if (!mbar_wait_warp(o_full(w), io & 1)) break;
+      if (!wait_warp(o_full(w), io & 1)) break;
       ++io;
       tc_fence_after();
       uint32_t ov[64];
@@ -432,9 +445,9 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
           ov[i] = __float_as_uint(o - __bfloat162float(__float2bfloat16(o)));
         }
         put(a.rest, (long)a.H * WA_D);
+        if (q < a.w.L)
+          a.lse[((long)m.b * a.H + m.h) * a.w.L + q] = mref + log2f(l);  // log2 units
       }
-      if (a.lse && q < a.w.L)
-        a.lse[((long)m.b * a.H + m.h) * a.w.L + q] = mref + log2f(l);  // log2 units
     }
   }
   tc_fence_before();
