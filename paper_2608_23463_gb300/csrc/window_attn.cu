@@ -374,15 +374,9 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
         const float ref = mref == -INFINITY ? 0.f : mref;
         const float2 nm = make_float2(-ref, -ref);
         float2 ps[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        // the last tile's P has been consumed
-        if (g > 0 && !wait_warp(p_free(w), (g - 1) & 1)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
+        uint32_t pk[64];
 #pragma unroll
         for (int hh = 0; hh < 4; ++hh) {
-          uint32_t pk[16];
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
             const float2 z = __ffma2_rn(make_float2(__uint_as_float(sc[32 * hh + 2 * c]),
@@ -390,10 +384,17 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
                                         sl, nm);
             const float2 pp = make_float2(ex2_approx(z.x), ex2_approx(z.y));
             ps[c & 1] = __fadd2_rn(ps[c & 1], pp);
-            pk[c] = pack_bf16(pp.x, pp.y);
+            pk[16 * hh + c] = pack_bf16(pp.x, pp.y);
           }
-          tmem_st16(tp + 16 * hh, pk);
         }
+        // the last tile's P has been consumed
+        if (g > 0 && !wait_warp(p_free(w), (g - 1) & 1)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < 64; c += 16) tmem_st16(tp + c, pk + c);
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive_warp(p_full(w));

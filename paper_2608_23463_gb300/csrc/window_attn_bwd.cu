@@ -22,6 +22,9 @@
 // pieces of at most `C` steps, so that a sink tile of a long sequence (and, in
 // a short one, any tile) is shared by several CTAs.  Pieces of a cut tile
 // leave fp32 sums; window_join_kernel adds them in order.
+// The producer alone works out the items; the others read them from shared memory and
+// count their steps up: what each step costs a warp beside its products and its 32
+// columns is on the chain of every step.
 // Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the
 // end of a sequence read as zero.
 #include <algorithm>
@@ -45,7 +48,8 @@ constexpr uint32_t WB_T_BYTES = WT * WB_D * 2;  // 16 KB per tile
 constexpr uint32_t WB_OFF_Y = 2 * 2 * WB_T_BYTES;                     // X: [2 bufs][X1, X2]
 constexpr uint32_t WB_OFF_LD = WB_OFF_Y + WB_STAGES * 2 * WB_T_BYTES;  // Y: [stage][Y1, Y2]
 constexpr uint32_t WB_OFF_BAR = WB_OFF_LD + WB_STAGES * WT * 8;        // (lse, Di) [stage][128]
-constexpr uint32_t WB_SMEM = WB_OFF_BAR + 256 + 1024;
+constexpr uint32_t WB_OFF_ITEM = WB_OFF_BAR + 256;  // four items
+constexpr uint32_t WB_SMEM = WB_OFF_ITEM + 4 * 32 + 1024;
 // TMEM columns: T1 at 0, T2 at 128 (fp32), accumulators at 256 (dV or dQ) and 320
 // (dK), E1 at 384, E2 at 448 (bf16 pairs: streamed column c in 32-bit column c / 2)
 constexpr uint32_t WB_TMEM_COLS = 512;
@@ -83,53 +87,69 @@ __host__ __device__ __forceinline__ int wb_queries(const WinTiles& w, int t) {
   return (t < w.sT ? w.n_t - 1 : w.last_q(t)) - t + 1;
 }
 
-// Item k: stationary tile t of sequence b, its n steps, and head h (DKDV: the key
-// head; DQ: the query head).  Step j streams
-//   DKDV: query tile t + (s0 + j) % nq of the group's head (s0 + j) / nq
-//   DQ:   key tile j < ns ? j : lo + j - ns
-template <bool DKDV>
-struct WbItem {
+// A work item: stationary tile t of sequence b, head h (DKDV: the key head; DQ: the query
+// head) and its n steps.  They stream
+//   DKDV: query tiles t .. t + m - 1 of the group's heads in turn, from query tile
+//         `tile` of head `head` on
+//   DQ:   the sinks' key tiles [0, m) and the window's [lo, t], lo in `head`
+struct __align__(16) WbItem {
   int t, h, b, n;
-  int s0, nq, piece;  // DKDV; piece < 0: the tile is not cut
-  int ns, lo;         // DQ
-  __device__ __forceinline__ WbItem(const WbArgs& a, int k) {
+  int tile, head, m, piece;  // piece < 0: the key tile is not cut
+};
+
+template <bool DKDV>
+__device__ __forceinline__ WbItem wb_item(const WbArgs& a, int k) {
+  WbItem i;
+  if (DKDV) {
+    const int per = a.KV * a.B, sinks = a.w.sT * a.np_s * per;
+    const bool sink = k < sinks;
+    const int kk = (sink ? k : k - sinks) / per, np = sink ? a.np_s : a.np_w, p = kk % np;
+    i.t = (sink ? 0 : a.w.sT) + kk / np;
+    i.piece = np == 1 ? -1 : k;
+    i.h = k % per % a.KV;  // `sinks` is a multiple of per
+    i.b = k % per / a.KV;
+    i.m = wb_queries(a.w, i.t);
+    const int s0 = p * a.C;
+    i.n = max(0, min(i.m * a.g - s0, a.C));
+    i.tile = i.t + s0 % i.m;
+    i.head = i.h * a.g + s0 / i.m;
+  } else {
+    const int per = a.H * a.B;
+    i.t = a.w.n_t - 1 - k / per;
+    i.h = k % per % a.H;
+    i.b = k % per / a.H;
+    i.head = a.w.lo(i.t);
+    i.m = min(a.w.sT, i.head);
+    i.n = i.m + i.t - i.head + 1;
+    i.tile = i.m > 0 ? 0 : i.head;
+    i.piece = -1;
+  }
+  return i;
+}
+
+// The streamed tile of an item's steps, one after the other.
+template <bool DKDV>
+struct WbStep {
+  int tile, head;  // head (DKDV): of the streamed queries
+  __device__ __forceinline__ explicit WbStep(const WbItem& i) : tile(i.tile), head(i.head) {}
+  __device__ __forceinline__ void next(const WbItem& i) {
+    ++tile;
     if (DKDV) {
-      const int per = a.KV * a.B, sinks = a.w.sT * a.np_s * per;
-      int p;
-      piece = k;
-      if (k < sinks) {
-        p = k / per % a.np_s;
-        t = k / per / a.np_s;
-      } else {
-        p = (k - sinks) / per % a.np_w;
-        t = a.w.sT + (k - sinks) / per / a.np_w;
+      if (tile == i.t + i.m) {
+        tile = i.t;
+        ++head;
       }
-      if ((t < a.w.sT ? a.np_s : a.np_w) == 1) piece = -1;
-      h = k % per % a.KV;  // `sinks` is a multiple of per
-      b = k % per / a.KV;
-      nq = wb_queries(a.w, t);
-      s0 = p * a.C;
-      n = max(0, min(nq * a.g - s0, a.C));
-      ns = lo = 0;
-    } else {
-      const int per = a.H * a.B;
-      t = a.w.n_t - 1 - k / per;
-      h = k % per % a.H;
-      b = k % per / a.H;
-      lo = a.w.lo(t);
-      ns = min(a.w.sT, lo);
-      n = ns + t - lo + 1;
-      s0 = nq = 0;
-      piece = -1;
+    } else if (tile == i.m) {
+      tile = i.head;
     }
   }
-  __device__ __forceinline__ int tile(int j) const {
-    return DKDV ? t + (s0 + j) % nq : j < ns ? j : lo + j - ns;
-  }
-  __device__ __forceinline__ int head(const WbArgs& a, int j) const {  // of the streamed tile
-    return DKDV ? h * a.g + (s0 + j) / nq : h / a.g;
-  }
 };
+
+// A wait of a converged warp, the common case of a completed phase up front.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
+  if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
+  return mbar_wait_warp(bar, parity);
+}
 
 template <bool DKDV>
 __global__ void __launch_bounds__(WB_THREADS, 1)
@@ -193,45 +213,59 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       prefetch_tmap(&tmY2);
     }
     float2* ld_ring = reinterpret_cast<float2*>(smem + WB_OFF_LD);
+    WbItem* const ring = reinterpret_cast<WbItem*>(smem + WB_OFF_ITEM);
     float2 ldp[WT / 32];  // next step's pairs of queries lane + 32 i
-    auto fetch_step = [&](const WbItem<DKDV>& m, int j) {
-      const int q0 = m.tile(j) * WT;
-      const long o = ((long)m.b * a.H + m.head(a, j)) * a.w.L + q0;
+    auto fetch_step = [&](const WbItem& m, const WbStep<DKDV>& sp) {
+      const int q0 = sp.tile * WT + lane;
+      const long o = ((long)m.b * a.H + sp.head) * a.w.L + q0;
 #pragma unroll
-      for (int i = 0; i < WT / 32; ++i) {
-        const int c = lane + 32 * i;
-        ldp[i] = q0 + c < a.w.L ? make_float2(a.lse[o + c], a.Di[o + c]) : make_float2(0.f, 0.f);
+      for (int i = 0; i < WT / 32; ++i)
+        ldp[i] = q0 + 32 * i < a.w.L ? make_float2(a.lse[o + 32 * i], a.Di[o + 32 * i])
+                                     : make_float2(0.f, 0.f);
+    };
+    int rd = 0;
+    // the next item that has steps; n < 0 at the end
+    auto next_item = [&]() -> WbItem {
+      for (;; ++rd) {
+        const int k = wb_rank(blockIdx.x, rd);
+        if (k >= a.n_items) {
+          WbItem e{};
+          e.n = -1;
+          return e;
+        }
+        const WbItem i = wb_item<DKDV>(a, k);
+        if (i.n > 0) {
+          ++rd;
+          return i;
+        }
       }
     };
-    int k = wb_rank(blockIdx.x, 0);
-    if (DKDV && k < a.n_items) {
-      const WbItem<DKDV> m(a, k);
-      if (m.n) fetch_step(m, 0);
-    }
+    WbItem m = next_item();
+    if (DKDV && m.n > 0) fetch_step(m, WbStep<DKDV>(m));
     bool ok = true;
-    uint32_t it = 0;
-    for (int rd = 0; k < a.n_items && ok; k = wb_rank(blockIdx.x, ++rd)) {
-      const WbItem<DKDV> m(a, k);
-      const int k2 = wb_rank(blockIdx.x, rd + 1);
-      if (m.n == 0) {
-        if (DKDV && k2 < a.n_items) {
-          const WbItem<DKDV> m2(a, k2);
-          if (m2.n) fetch_step(m2, 0);
-        }
-        continue;
-      }
+    for (uint32_t it = 0; ok; ++it) {
       const uint32_t xb = it & 1;
-      if (!mbar_wait_warp(x_empty + 8 * xb, ((it >> 1) & 1) ^ 1)) break;
+      // (four slots: the row warps may be an item behind the products that freed X)
+      if (!wait_warp(x_empty + 8 * xb, ((it >> 1) & 1) ^ 1)) break;
       if (lane == 0) {
-        const uint32_t xdst = sbase + xb * 2 * WB_T_BYTES;
-        mbar_arrive_expect_tx(x_full + 8 * xb, 2 * WB_T_BYTES);
-        tma_load_3d(xdst, &tmX1, x_full + 8 * xb, m.h * WB_D, m.t * WT, m.b);
-        tma_load_3d(xdst + WB_T_BYTES, &tmX2, x_full + 8 * xb, m.h * WB_D, m.t * WT, m.b);
+        ring[it & 3] = m;
+        if (m.n > 0) {
+          const uint32_t xdst = sbase + xb * 2 * WB_T_BYTES;
+          mbar_arrive_expect_tx(x_full + 8 * xb, 2 * WB_T_BYTES);
+          tma_load_3d(xdst, &tmX1, x_full + 8 * xb, m.h * WB_D, m.t * WT, m.b);
+          tma_load_3d(xdst + WB_T_BYTES, &tmX2, x_full + 8 * xb, m.h * WB_D, m.t * WT, m.b);
+        } else {
+          mbar_arrive(x_full + 8 * xb);
+        }
       }
-      x_issued = ++it;
+      if (m.n < 0) break;
+      x_issued = it + 1;
+      const WbItem m2 = next_item();
+      WbStep<DKDV> sp(m);
+      const int kv = m.h / a.g;  // DQ: the key head
       for (int j = 0; j < m.n; ++j) {
         const uint32_t G = y_issued, st = G % WB_STAGES;
-        if (!mbar_wait_warp(y_empty + 8 * st, ((G / WB_STAGES) & 1) ^ 1)) {
+        if (!wait_warp(y_empty + 8 * st, ((G / WB_STAGES) & 1) ^ 1)) {
           ok = false;
           break;
         }
@@ -242,48 +276,51 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         }
         if (lane == 0) {
           const uint32_t ydst = sbase + WB_OFF_Y + st * 2 * WB_T_BYTES;
-          const int yrow = m.tile(j) * WT, ycol = m.head(a, j) * WB_D;
+          const int yrow = sp.tile * WT, ycol = (DKDV ? sp.head : kv) * WB_D;
           mbar_arrive_expect_tx(y_full + 8 * st, 2 * WB_T_BYTES);
           tma_load_3d(ydst, &tmY1, y_full + 8 * st, ycol, yrow, m.b);
           tma_load_3d(ydst + WB_T_BYTES, &tmY2, y_full + 8 * st, ycol, yrow, m.b);
         }
         y_issued = G + 1;
+        sp.next(m);
         if (DKDV) {  // the pairs of the next step (this item's or the next item's first)
-          if (j + 1 < m.n) {
-            fetch_step(m, j + 1);
-          } else if (k2 < a.n_items) {
-            const WbItem<DKDV> m2(a, k2);
-            if (m2.n) fetch_step(m2, 0);
-          }
+          if (j + 1 < m.n)
+            fetch_step(m, sp);
+          else if (m2.n > 0)
+            fetch_step(m2, WbStep<DKDV>(m2));
         }
       }
+      m = m2;
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
     // The whole warp runs the loop; one elected lane issues and commits.
     constexpr uint32_t idesc_t = idesc_bf16_f32(WT, WT, 0, 0);
     constexpr uint32_t idesc_a = idesc_bf16_f32(WT, WB_D, 0, 1);
+    const WbItem* const ring = reinterpret_cast<const WbItem*>(smem + WB_OFF_ITEM);
+    const uint64_t dx0 = smem_desc_sw128(sbase, 16, 1024);
+    const uint64_t dy0 = smem_desc_sw128(sbase + WB_OFF_Y, 16, 1024);
+    const uint64_t da0 = smem_desc_sw128(sbase + WB_OFF_Y, 8192, 1024);
+    constexpr uint64_t TILE = WB_T_BYTES >> 4;  // in a descriptor's units
     bool ok = true;
     uint32_t it = 0, G = 0;
     // accumulate step G (local step j of its item): E_G times the step's Y tiles
-    auto acc_step = [&](uint32_t G_, int j, uint32_t it_) -> bool {
+    auto acc_step = [&](uint32_t G_, bool first) -> bool {
       const uint32_t st = G_ % WB_STAGES;
-      if (!mbar_wait_warp(e_full, G_ & 1)) return false;
-      if (j == 0 && !mbar_wait_warp(acc_free, (it_ & 1) ^ 1)) return false;
+      if (!wait_warp(e_full, G_ & 1)) return false;
+      if (first && !wait_warp(acc_free, (it & 1) ^ 1)) return false;
       tc_fence_after();
       const uint32_t e1 = tmem + WB_TM_E, e2 = e1 + WT / 2;
-      const uint32_t y1 = sbase + WB_OFF_Y + st * 2 * WB_T_BYTES, y2 = y1 + WB_T_BYTES;
+      const uint64_t d1 = da0 + st * 2 * TILE, d2 = d1 + TILE;
       if (elect_one()) {
 #pragma unroll
         for (int kk = 0; kk < WT / 16; ++kk) {
-          const uint32_t acc = (j > 0 || kk > 0) ? 1u : 0u;
-          const uint64_t bd1 = smem_desc_sw128(y1 + kk * 2048, 8192, 1024);
+          const uint32_t acc = (!first || kk > 0) ? 1u : 0u;
           if (DKDV) {
-            const uint64_t bd2 = smem_desc_sw128(y2 + kk * 2048, 8192, 1024);
-            tc_mma_f16_ts(tmem + 256, e1 + kk * 8, bd2, idesc_a, acc);  // dV += P^T dO
-            tc_mma_f16_ts(tmem + 320, e2 + kk * 8, bd1, idesc_a, acc);  // dK += dS^T Q
+            tc_mma_f16_ts(tmem + 256, e1 + kk * 8, d2 + kk * (2048 >> 4), idesc_a, acc);  // dV += P^T dO
+            tc_mma_f16_ts(tmem + 320, e2 + kk * 8, d1 + kk * (2048 >> 4), idesc_a, acc);  // dK += dS^T Q
           } else {
-            tc_mma_f16_ts(tmem + 256, e2 + kk * 8, bd1, idesc_a, acc);  // dQ += dS K
+            tc_mma_f16_ts(tmem + 256, e2 + kk * 8, d1 + kk * (2048 >> 4), idesc_a, acc);  // dQ += dS K
           }
         }
         tc_commit(e_free);
@@ -292,45 +329,39 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       __syncwarp();
       return true;
     };
-    for (int rd = 0, k = wb_rank(blockIdx.x, 0); k < a.n_items && ok;
-         k = wb_rank(blockIdx.x, ++rd)) {
-      const WbItem<DKDV> m(a, k);
-      if (m.n == 0) continue;
+    for (;; ++it) {
       const uint32_t xb = it & 1;
-      if (!mbar_wait_warp(x_full + 8 * xb, (it >> 1) & 1)) break;
+      if (!wait_warp(x_full + 8 * xb, (it >> 1) & 1)) break;
+      const int n = ring[it & 3].n;
+      if (n < 0) break;
       tc_fence_after();
-      const uint32_t x1 = sbase + xb * 2 * WB_T_BYTES, x2 = x1 + WB_T_BYTES;
-      for (int j = 0; j < m.n; ++j) {
-        const uint32_t Gj = G + j, st = Gj % WB_STAGES;
-        if (!mbar_wait_warp(y_full + 8 * st, (Gj / WB_STAGES) & 1) ||
-            !mbar_wait_warp(t_free, (Gj & 1) ^ 1)) {
+      const uint64_t d1 = dx0 + xb * 2 * TILE, d2 = d1 + TILE;
+      for (int j = 0; j < n; ++j, ++G) {
+        const uint32_t st = G % WB_STAGES;
+        if (!wait_warp(y_full + 8 * st, (G / WB_STAGES) & 1) || !wait_warp(t_free, (G & 1) ^ 1)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        const uint32_t y1 = sbase + WB_OFF_Y + st * 2 * WB_T_BYTES, y2 = y1 + WB_T_BYTES;
+        const uint64_t y1 = dy0 + st * 2 * TILE, y2 = y1 + TILE;
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < WB_D / 16; ++kk) {
-            tc_mma_f16(tmem, smem_desc_sw128(x1 + kk * 32, 16, 1024),
-                       smem_desc_sw128(y1 + kk * 32, 16, 1024), idesc_t, kk ? 1u : 0u);
-            tc_mma_f16(tmem + WT, smem_desc_sw128(x2 + kk * 32, 16, 1024),
-                       smem_desc_sw128(y2 + kk * 32, 16, 1024), idesc_t, kk ? 1u : 0u);
+            tc_mma_f16(tmem, d1 + kk * 2, y1 + kk * 2, idesc_t, kk ? 1u : 0u);
+            tc_mma_f16(tmem + WT, d2 + kk * 2, y2 + kk * 2, idesc_t, kk ? 1u : 0u);
           }
           tc_commit(t_full);
-          if (j == m.n - 1) tc_commit(x_empty + 8 * xb);
+          if (j == n - 1) tc_commit(x_empty + 8 * xb);
         }
         __syncwarp();
-        if (j > 0 && !acc_step(Gj - 1, j - 1, it)) {
+        if (j > 0 && !acc_step(G - 1, j == 1)) {
           ok = false;
           break;
         }
       }
-      if (!ok || !acc_step(G + m.n - 1, m.n - 1, it)) break;
+      if (!ok || !acc_step(G - 1, n == 1)) break;
       if (elect_one()) tc_commit(acc_full);
       __syncwarp();
-      G += m.n;
-      ++it;
     }
     if (elect_one()) tc_commit(done);
     __syncwarp();
@@ -341,12 +372,13 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     const int ch = (warp - 2) >> 2;   // quarter of the streamed columns: [32 ch, 32 ch + 32)
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
     const float2* ld_ring = reinterpret_cast<const float2*>(smem + WB_OFF_LD);  // [stage][128]
+    const WbItem* const ring = reinterpret_cast<const WbItem*>(smem + WB_OFF_ITEM);
     bool ok = true;
-    uint32_t G = 0, it = 0;
-    for (int rd = 0, k = wb_rank(blockIdx.x, 0); k < a.n_items && ok;
-         k = wb_rank(blockIdx.x, ++rd)) {
-      const WbItem<DKDV> m(a, k);
-      if (m.n == 0) continue;
+    uint32_t G = 0;
+    for (uint32_t it = 0; ok; ++it) {
+      if (!wait_warp(x_full + 8 * (it & 1), (it >> 1) & 1)) break;
+      const WbItem m = ring[it & 3];
+      if (m.n < 0) break;
       const int row = m.t * WT + r;  // key (DKDV) or query (DQ) index in the sequence
       float lse_r = 0.f, di_r = 0.f;
       if (!DKDV && row < a.w.L) {
@@ -354,17 +386,27 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         lse_r = a.lse[o];
         di_r = a.Di[o];
       }
-      for (int j = 0; j < m.n; ++j) {
-        const uint32_t Gj = G + j;
-        const int yt = m.tile(j), c0 = yt * WT;  // first streamed index of this step
+      // streamed tiles in which some pair of a row is hidden: the diagonal's, the sequence's
+      // last, and DKDV those from `edge` on, past some key's window, DQ those before it
+      const int past = DKDV ? 0 : m.t * WT + WT - 1 - a.w.W;
+      const int edge = DKDV ? (m.t * WT + WT <= a.w.S ? a.w.n_t : m.t + a.w.W / WT)
+                            : past >= 0 ? past / WT + 1 : 0;
+      const int last = a.w.L % WT && DKDV ? a.w.n_t - 1 : -1, whole = a.w.S / WT;
+      WbStep<DKDV> sp(m);
+      for (int j = 0; j < m.n; ++j, ++G) {
+        const uint32_t Gj = G;
+        const int yt = sp.tile, c0 = yt * WT;  // first streamed index of this step
+        sp.next(m);
+        const bool hidden = yt == m.t || yt == last ||
+                            (DKDV ? yt >= edge : yt < edge && yt >= whole);
         // DKDV: the step's (lse, Di) pairs, staged by the producer before the
         // stage's full barrier (already complete: the step's scores used it;
         // the slot is refilled only after this step's E has been consumed)
-        if (DKDV && !mbar_wait(y_full + 8 * (Gj % WB_STAGES), (Gj / WB_STAGES) & 1)) {
+        if (DKDV && !wait_warp(y_full + 8 * (Gj % WB_STAGES), (Gj / WB_STAGES) & 1)) {
           ok = false;
           break;
         }
-        if (!mbar_wait(t_full, Gj & 1)) {
+        if (!wait_warp(t_full, Gj & 1)) {
           ok = false;
           break;
         }
@@ -376,19 +418,21 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         tmem_wait_ld(pa);
         tc_fence_before();
         mbar_arrive_warp(t_free);
-        // visible streamed columns: [lo, hi), and (DQ) the sinks below sk
-        int lo, hi, sk = 0;
-        if (DKDV) {  // the queries that see this key
-          lo = row - c0;
-          hi = min(row < a.w.S ? a.w.L : min(a.w.L, row + a.w.W), c0 + WT) - c0;
-        } else {  // the keys this query sees
-          lo = row - a.w.W + 1 - c0;
-          hi = row + 1 - c0;
-          sk = a.w.S - c0;
-        }
         const float2* lds = ld_ring + (Gj % WB_STAGES) * WT;
         // P and dS of the thread's 32 columns from kb on, as bf16 pairs
         auto emit = [&](auto masked, int kb, uint32_t* pk, uint32_t* dk) {
+          // visible streamed columns: [lo, hi), and (DQ) the sinks below sk
+          int lo = 0, hi = WT, sk = 0;
+          if (decltype(masked)::value) {
+            if (DKDV) {  // the queries that see this key
+              lo = row - c0;
+              hi = min(row < a.w.S ? a.w.L : min(a.w.L, row + a.w.W), c0 + WT) - c0;
+            } else {  // the keys this query sees
+              lo = row - a.w.W + 1 - c0;
+              hi = row + 1 - c0;
+              sk = a.w.S - c0;
+            }
+          }
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const uint32_t* sv = sa + g * 8;
@@ -423,11 +467,11 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         };
         uint32_t pk[16], dk[16];  // this thread's 32 columns of E1 and E2
         const int kb = 32 * ch;
-        if ((lo <= kb || sk >= kb + 32) && hi >= kb + 32)
-          emit(std::false_type{}, kb, pk, dk);
-        else
+        if (hidden)
           emit(std::true_type{}, kb, pk, dk);
-        if (!mbar_wait(e_free, (Gj & 1) ^ 1)) {  // the previous step's E has been read
+        else
+          emit(std::false_type{}, kb, pk, dk);
+        if (!wait_warp(e_free, (Gj & 1) ^ 1)) {  // the previous step's E has been read
           ok = false;
           break;
         }
@@ -440,10 +484,8 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         mbar_arrive_warp(e_full);
       }
       if (!ok) break;
-      G += m.n;
       // accumulators -> dK, dV (DKDV) or dQ (DQ) rows
-      if (!mbar_wait(acc_full, it & 1)) break;
-      ++it;
+      if (!wait_warp(acc_full, it & 1)) break;
       tc_fence_after();
       uint32_t u0[16], w0[16];  // this thread's 16 columns of dV / dQ and of dK
       tmem_ld16(tl + 256 + 16 * ch, u0);
