@@ -16,18 +16,24 @@
 //           T1 = S,  T2 = dP,  E2 = dS,  dQ += E2 Y1
 // Roles: warp 0 TMA producer (DKDV: it also stages each step's (LSE, Di)
 // pairs of the streamed queries in shared memory), warp 1 MMA issuer, warps
-// 2-17 the row warps: four per TMEM lane quarter, each thread one row (TMEM
+// 4-19 the row warps: four per TMEM lane quarter, each thread one row (TMEM
 // lane) and one quarter of the 128 streamed columns.
-// The sinks are seen by every later query: a key tile's steps are cut into
-// pieces of at most `C` steps, so that a sink tile of a long sequence (and, in
-// a short one, any tile) is shared by several CTAs.  Pieces of a cut tile
-// leave fp32 sums; window_join_kernel adds them in order.
+// The sinks are seen by every later query: their key tiles' steps are cut into
+// pieces (wb_cut), as are all tiles' where there are few.  The pieces of a cut
+// tile leave fp32 sums, those past its window of the sinks' rows alone;
+// window_join_kernel adds them in order.  Items go round the CTAs, so that those
+// at work at one time share their streamed tiles in L2.  (The steps of all tiles
+// dealt to the CTAs in equal ranges instead: 65536 tokens of 16 heads on 4 key
+// heads, window 1024: 800 us, 664 so; a range's tiles are too far apart.)
+// An item's sums are read out in the next item's first step, when that step's E waits
+// for them anyway: no warp waits for the end of an item's products.
 // The producer alone works out the items; the others read them from shared memory and
 // count their steps up: what each step costs a warp beside its products and its 32
 // columns is on the chain of every step.
 // Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the
 // end of a sequence read as zero.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "local.h"
@@ -42,14 +48,18 @@ namespace {
 
 constexpr int WB_D = 64;   // head width
 constexpr int WB_STAGES = 4;
-constexpr int WB_ROW_THREADS = 512;  // warps 2-17
-constexpr int WB_THREADS = 64 + WB_ROW_THREADS;
+constexpr int WB_ROW_THREADS = 512;  // warps 4-19
+constexpr int WB_THREADS = 128 + WB_ROW_THREADS;
+// A row thread holds 64 values of a step: the control warps (two of them idle) give
+// registers up, of the 96 that each thread has at launch.
+constexpr int WB_REGS_CTRL = 64, WB_REGS_ROWS = 104;
+static_assert(WB_REGS_CTRL * 128 + WB_REGS_ROWS * 512 <= 96 * WB_THREADS, "register split");
 constexpr uint32_t WB_T_BYTES = WT * WB_D * 2;  // 16 KB per tile
 constexpr uint32_t WB_OFF_Y = 2 * 2 * WB_T_BYTES;                     // X: [2 bufs][X1, X2]
 constexpr uint32_t WB_OFF_LD = WB_OFF_Y + WB_STAGES * 2 * WB_T_BYTES;  // Y: [stage][Y1, Y2]
 constexpr uint32_t WB_OFF_BAR = WB_OFF_LD + WB_STAGES * WT * 8;        // (lse, Di) [stage][128]
 constexpr uint32_t WB_OFF_ITEM = WB_OFF_BAR + 256;  // four items
-constexpr uint32_t WB_SMEM = WB_OFF_ITEM + 4 * 32 + 1024;
+constexpr uint32_t WB_SMEM = WB_OFF_ITEM + 4 * 48 + 1024;
 // TMEM columns: T1 at 0, T2 at 128 (fp32), accumulators at 256 (dV or dQ) and 320
 // (dK), E1 at 384, E2 at 448 (bf16 pairs: streamed column c in 32-bit column c / 2)
 constexpr uint32_t WB_TMEM_COLS = 512;
@@ -86,6 +96,12 @@ __device__ __forceinline__ int wb_rank(int c, int round) {
 __host__ __device__ __forceinline__ int wb_queries(const WinTiles& w, int t) {
   return (t < w.sT ? w.n_t - 1 : w.last_q(t)) - t + 1;
 }
+// Rows of key tile t that the steps [s0, s0 + n) of its list add to: all, or the sinks
+// alone where every query tile is past its window.
+__device__ __forceinline__ int wb_rows(const WinTiles& w, int t, int m, int s0, int n) {
+  const int i = s0 % m;
+  return t < w.sT && i + n <= m && t + i > w.last_q(t) ? min(WT, w.S - t * WT) : WT;
+}
 
 // A work item: stationary tile t of sequence b, head h (DKDV: the key head; DQ: the query
 // head) and its n steps.  They stream
@@ -94,36 +110,41 @@ __host__ __device__ __forceinline__ int wb_queries(const WinTiles& w, int t) {
 //   DQ:   the sinks' key tiles [0, m) and the window's [lo, t], lo in `head`
 struct __align__(16) WbItem {
   int t, h, b, n;
-  int tile, head, m, piece;  // piece < 0: the key tile is not cut
+  int tile, head, m, piece;  // piece < 0: all of the tile's steps
+  int rows, pad[3];          // DKDV: rows that a piece adds to
 };
 
-template <bool DKDV>
-__device__ __forceinline__ WbItem wb_item(const WbArgs& a, int k) {
+// DKDV: item k: the pieces of the sinks' tiles, then those of the others; n may be 0.
+__device__ __forceinline__ WbItem wb_key_item(const WbArgs& a, int k) {
   WbItem i;
-  if (DKDV) {
-    const int per = a.KV * a.B, sinks = a.w.sT * a.np_s * per;
-    const bool sink = k < sinks;
-    const int kk = (sink ? k : k - sinks) / per, np = sink ? a.np_s : a.np_w, p = kk % np;
-    i.t = (sink ? 0 : a.w.sT) + kk / np;
-    i.piece = np == 1 ? -1 : k;
-    i.h = k % per % a.KV;  // `sinks` is a multiple of per
-    i.b = k % per / a.KV;
-    i.m = wb_queries(a.w, i.t);
-    const int s0 = p * a.C;
-    i.n = max(0, min(i.m * a.g - s0, a.C));
-    i.tile = i.t + s0 % i.m;
-    i.head = i.h * a.g + s0 / i.m;
-  } else {
-    const int per = a.H * a.B;
-    i.t = a.w.n_t - 1 - k / per;
-    i.h = k % per % a.H;
-    i.b = k % per / a.H;
-    i.head = a.w.lo(i.t);
-    i.m = min(a.w.sT, i.head);
-    i.n = i.m + i.t - i.head + 1;
-    i.tile = i.m > 0 ? 0 : i.head;
-    i.piece = -1;
-  }
+  const int per = a.KV * a.B, sinks = a.w.sT * a.np_s * per;
+  const bool sink = k < sinks;
+  const int kk = (sink ? k : k - sinks) / per, np = sink ? a.np_s : a.np_w, p = kk % np;
+  const int hb = (sink ? k : k - sinks) - kk * per;
+  i.t = (sink ? 0 : a.w.sT) + kk / np;
+  i.b = hb / a.KV;
+  i.h = hb - i.b * a.KV;
+  i.m = wb_queries(a.w, i.t);
+  const int s0 = p * a.C;
+  i.n = max(0, min(i.m * a.g - s0, a.C));
+  i.tile = i.t + s0 % i.m;
+  i.head = i.h * a.g + s0 / i.m;
+  i.piece = np == 1 ? -1 : k;
+  i.rows = wb_rows(a.w, i.t, i.m, s0, i.n);
+  return i;
+}
+// DQ: item k, from the last query tile on.
+__device__ __forceinline__ WbItem wb_query_item(const WbArgs& a, int k) {
+  WbItem i;
+  const int per = a.H * a.B;
+  i.t = a.w.n_t - 1 - k / per;
+  i.h = k % per % a.H;
+  i.b = k % per / a.H;
+  i.head = a.w.lo(i.t);
+  i.m = min(a.w.sT, i.head);
+  i.n = i.m + i.t - i.head + 1;
+  i.tile = i.m > 0 ? 0 : i.head;
+  i.piece = -1;
   return i;
 }
 
@@ -160,12 +181,10 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   const uint32_t b0 = smem_u32(smem + WB_OFF_BAR);
-  // x_full[2] x_empty[2] y_full[S] y_empty[S] t_full t_free e_full e_free acc_full
-  // acc_free done
+  // x_full[2] x_empty[2] y_full[S] y_empty[S] t_full t_free e_full e_free done
   const uint32_t x_full = b0, x_empty = b0 + 16, y_full = b0 + 32,
                  y_empty = y_full + 8 * WB_STAGES, t_full = y_empty + 8 * WB_STAGES,
-                 t_free = t_full + 8, e_full = t_free + 8, e_free = e_full + 8,
-                 acc_full = e_free + 8, acc_free = acc_full + 8, done = acc_free + 8;
+                 t_free = t_full + 8, e_full = t_free + 8, e_free = e_full + 8, done = e_free + 8;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + WB_OFF_BAR + 240);
   const uint32_t sbase = smem_u32(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -183,8 +202,6 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       mbar_init(y_full + 8 * i, 1);
       mbar_init(y_empty + 8 * i, 1);
     }
-    mbar_init(acc_full, 1);
-    mbar_init(acc_free, WB_ROW_THREADS / 32);
     mbar_init(done, 1);
     fence_barrier_init();
   }
@@ -199,6 +216,8 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
   pdl_enter();  // the setup above overlaps the kernel before this one
   uint32_t y_issued = 0, x_issued = 0;
 
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(WB_REGS_CTRL));
   if (warp == 0) {
     // ------------------------------------------------------------ producer
     // Lane 0 issues the copies.  DKDV: the whole warp also stages the (lse,
@@ -212,7 +231,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       prefetch_tmap(&tmY1);
       prefetch_tmap(&tmY2);
     }
-    float2* ld_ring = reinterpret_cast<float2*>(smem + WB_OFF_LD);
+    float* const ld_ring = reinterpret_cast<float*>(smem + WB_OFF_LD);
     WbItem* const ring = reinterpret_cast<WbItem*>(smem + WB_OFF_ITEM);
     float2 ldp[WT / 32];  // next step's pairs of queries lane + 32 i
     auto fetch_step = [&](const WbItem& m, const WbStep<DKDV>& sp) {
@@ -220,25 +239,21 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       const long o = ((long)m.b * a.H + sp.head) * a.w.L + q0;
 #pragma unroll
       for (int i = 0; i < WT / 32; ++i)
-        ldp[i] = q0 + 32 * i < a.w.L ? make_float2(a.lse[o + 32 * i], a.Di[o + 32 * i])
+        ldp[i] = q0 + 32 * i < a.w.L ? make_float2(-a.lse[o + 32 * i], -a.Di[o + 32 * i])
                                      : make_float2(0.f, 0.f);
     };
     int rd = 0;
-    // the next item that has steps; n < 0 at the end
-    auto next_item = [&]() -> WbItem {
-      for (;; ++rd) {
-        const int k = wb_rank(blockIdx.x, rd);
-        if (k >= a.n_items) {
-          WbItem e{};
-          e.n = -1;
-          return e;
-        }
-        const WbItem i = wb_item<DKDV>(a, k);
+    auto next_item = [&]() -> WbItem {  // the next one with steps; n < 0 at the end
+      for (int k; (k = wb_rank(blockIdx.x, rd)) < a.n_items; ++rd) {
+        const WbItem i = DKDV ? wb_key_item(a, k) : wb_query_item(a, k);
         if (i.n > 0) {
           ++rd;
           return i;
         }
       }
+      WbItem i{};
+      i.n = -1;
+      return i;
     };
     WbItem m = next_item();
     if (DKDV && m.n > 0) fetch_step(m, WbStep<DKDV>(m));
@@ -271,7 +286,11 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         }
         if (DKDV) {
 #pragma unroll
-          for (int i = 0; i < WT / 32; ++i) ld_ring[st * WT + 32 * i + lane] = ldp[i];
+          for (int i = 0; i < WT / 32; ++i) {  // queries c, c + 1 (even c): -lse -lse -Di -Di
+            float* d = ld_ring + st * 2 * WT + (32 * i + lane) / 2 * 4 + (lane & 1);
+            d[0] = ldp[i].x;
+            d[2] = ldp[i].y;
+          }
           __syncwarp();
         }
         if (lane == 0) {
@@ -308,7 +327,6 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     auto acc_step = [&](uint32_t G_, bool first) -> bool {
       const uint32_t st = G_ % WB_STAGES;
       if (!wait_warp(e_full, G_ & 1)) return false;
-      if (first && !wait_warp(acc_free, (it & 1) ^ 1)) return false;
       tc_fence_after();
       const uint32_t e1 = tmem + WB_TM_E, e2 = e1 + WT / 2;
       const uint64_t d1 = da0 + st * 2 * TILE, d2 = d1 + TILE;
@@ -360,25 +378,68 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         }
       }
       if (!ok || !acc_step(G - 1, n == 1)) break;
-      if (elect_one()) tc_commit(acc_full);
-      __syncwarp();
     }
     if (elect_one()) tc_commit(done);
     __syncwarp();
+  }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(WB_REGS_ROWS));
     // ------------------------------------------------------------ row warps
     const int q4 = warp & 3;
     const int r = q4 * 32 + lane;  // stationary row in the tile = TMEM lane
-    const int ch = (warp - 2) >> 2;   // quarter of the streamed columns: [32 ch, 32 ch + 32)
+    const int ch = (warp - 4) >> 2;   // quarter of the streamed columns: [32 ch, 32 ch + 32)
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
-    const float2* ld_ring = reinterpret_cast<const float2*>(smem + WB_OFF_LD);  // [stage][128]
+    const float4* ld_ring = reinterpret_cast<const float4*>(smem + WB_OFF_LD);  // [stage][64]
     const WbItem* const ring = reinterpret_cast<const WbItem*>(smem + WB_OFF_ITEM);
+    struct Sums {
+      uint32_t u[16], w[16];  // 16 columns of an item's dV / dQ and of its dK
+    };
+    auto load_sums = [&](Sums& v) {
+      tmem_ld16(tl + 256 + 16 * ch, v.u);
+      if (DKDV) tmem_ld16(tl + 320 + 16 * ch, v.w);
+    };
+    auto store_sums = [&](const WbItem& m, const Sums& sum) {  // dK, dV (DKDV) or dQ (DQ) rows
+      const uint32_t *u0 = sum.u, *w0 = sum.w;
+      const int row = m.t * WT + r;
+      if (row >= a.w.L) return;
+      const long srow = (long)m.b * a.w.L + row;
+      auto store = [&](bf16* o, const uint32_t* v, float sc) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 8)
+          *reinterpret_cast<uint4*>(o + i) = make_uint4(
+              pack_bf16(__uint_as_float(v[i]) * sc, __uint_as_float(v[i + 1]) * sc),
+              pack_bf16(__uint_as_float(v[i + 2]) * sc, __uint_as_float(v[i + 3]) * sc),
+              pack_bf16(__uint_as_float(v[i + 4]) * sc, __uint_as_float(v[i + 5]) * sc),
+              pack_bf16(__uint_as_float(v[i + 6]) * sc, __uint_as_float(v[i + 7]) * sc));
+      };
+      if (DKDV && m.piece >= 0) {  // sums of a cut tile
+        if (r >= m.rows) return;
+        float* o = a.part + ((long)m.piece * WT + r) * WB_ACC + 16 * ch;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          *reinterpret_cast<uint4*>(o + i) = make_uint4(u0[i], u0[i + 1], u0[i + 2], u0[i + 3]);
+          *reinterpret_cast<uint4*>(o + WB_D + i) = make_uint4(w0[i], w0[i + 1], w0[i + 2], w0[i + 3]);
+        }
+      } else {
+        store(a.out_u + srow * a.ld_u + m.h * WB_D + 16 * ch, u0, DKDV ? 1.f : a.scale);
+        if (DKDV) store(a.out_w + srow * a.ld_w + m.h * WB_D + 16 * ch, w0, a.scale);
+      }
+    };
     bool ok = true;
     uint32_t G = 0;
     for (uint32_t it = 0; ok; ++it) {
       if (!wait_warp(x_full + 8 * (it & 1), (it >> 1) & 1)) break;
       const WbItem m = ring[it & 3];
-      if (m.n < 0) break;
+      if (m.n < 0) {  // the last item's sums
+        if (it > 0 && wait_warp(e_free, (G & 1) ^ 1)) {
+          tc_fence_after();
+          Sums v;
+          load_sums(v);
+          tc_fence_before();
+          store_sums(ring[(it - 1) & 3], v);
+        }
+        break;
+      }
       const int row = m.t * WT + r;  // key (DKDV) or query (DQ) index in the sequence
       float lse_r = 0.f, di_r = 0.f;
       if (!DKDV && row < a.w.L) {
@@ -386,19 +447,19 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         lse_r = a.lse[o];
         di_r = a.Di[o];
       }
-      // streamed tiles in which some pair of a row is hidden: the diagonal's, the sequence's
-      // last, and DKDV those from `edge` on, past some key's window, DQ those before it
+      // streamed tiles in which some pair of a row is hidden: the diagonal's, DKDV those from
+      // `edge` on, past some key's window or the sequence's end, DQ those before it that are
+      // not all sinks
       const int past = DKDV ? 0 : m.t * WT + WT - 1 - a.w.W;
-      const int edge = DKDV ? (m.t * WT + WT <= a.w.S ? a.w.n_t : m.t + a.w.W / WT)
+      const int edge = DKDV ? min(m.t * WT + WT <= a.w.S ? a.w.n_t : m.t + a.w.W / WT, a.w.L / WT)
                             : past >= 0 ? past / WT + 1 : 0;
-      const int last = a.w.L % WT && DKDV ? a.w.n_t - 1 : -1, whole = a.w.S / WT;
+      const int whole = a.w.S / WT;
       WbStep<DKDV> sp(m);
       for (int j = 0; j < m.n; ++j, ++G) {
         const uint32_t Gj = G;
         const int yt = sp.tile, c0 = yt * WT;  // first streamed index of this step
         sp.next(m);
-        const bool hidden = yt == m.t || yt == last ||
-                            (DKDV ? yt >= edge : yt < edge && yt >= whole);
+        const bool hidden = yt == m.t || (DKDV ? yt >= edge : yt < edge && yt >= whole);
         // DKDV: the step's (lse, Di) pairs, staged by the producer before the
         // stage's full barrier (already complete: the step's scores used it;
         // the slot is refilled only after this step's E has been consumed)
@@ -418,48 +479,45 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         tmem_wait_ld(pa);
         tc_fence_before();
         mbar_arrive_warp(t_free);
-        const float2* lds = ld_ring + (Gj % WB_STAGES) * WT;
+        const float4* lds = ld_ring + (Gj % WB_STAGES) * (WT / 2) + 16 * ch;
         // P and dS of the thread's 32 columns from kb on, as bf16 pairs
         auto emit = [&](auto masked, int kb, uint32_t* pk, uint32_t* dk) {
-          // visible streamed columns: [lo, hi), and (DQ) the sinks below sk
-          int lo = 0, hi = WT, sk = 0;
           if (decltype(masked)::value) {
-            if (DKDV) {  // the queries that see this key
-              lo = row - c0;
-              hi = min(row < a.w.S ? a.w.L : min(a.w.L, row + a.w.W), c0 + WT) - c0;
-            } else {  // the keys this query sees
-              lo = row - a.w.W + 1 - c0;
-              hi = row + 1 - c0;
-              sk = a.w.S - c0;
-            }
+            // visible streamed columns: [lo, hi), and (DQ) the sinks below sk; bit c of `vis`:
+            // column kb + c
+            auto low = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+            const int b0 = c0 + kb;  // the first column's index
+            const uint32_t vis =
+                DKDV ? low((row < a.w.S ? a.w.L : min(a.w.L, row + a.w.W)) - b0) & ~low(row - b0)
+                     : low(row + 1 - b0) & (~low(row - a.w.W + 1 - b0) | low(a.w.S - b0));
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              if (!(vis >> c & 1)) sa[c] = 0xff800000u;  // -inf: P = 0, and dS with it
           }
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
+            // (the shared loads of a later group wait for their turn: hoisted, they would not
+            // fit the registers)
+            if (DKDV) asm volatile("" ::: "memory");
             const uint32_t* sv = sa + g * 8;
             const uint32_t* dv = pa + g * 8;
-            // (lse, Di) of two columns per 128-bit shared load (DKDV); packed fp32x2
-            // arithmetic on column pairs (each lane an IEEE fp32 operation)
-            const float4* l4 = reinterpret_cast<const float4*>(lds + kb) + g * 4;
+            // -lse and -Di of two columns per 128-bit shared load (DKDV), as the packed
+            // fp32x2 arithmetic takes them
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int c = kb + g * 8 + 2 * e;
               float2 nl = make_float2(-lse_r, -lse_r), nd = make_float2(-di_r, -di_r);
               if (DKDV) {
-                const float4 v = l4[e];
-                nl = make_float2(-v.x, -v.z);
-                nd = make_float2(-v.y, -v.w);
+                const float4 v = lds[g * 4 + e];
+                nl = make_float2(v.x, v.y);
+                nd = make_float2(v.z, v.w);
               }
               const float2 z = __ffma2_rn(
                   make_float2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1])),
                   make_float2(a.sl2, a.sl2), nl);
-              float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
-              float2 ds = __fmul2_rn(
+              const float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
+              const float2 ds = __fmul2_rn(
                   p, __fadd2_rn(make_float2(__uint_as_float(dv[2 * e]), __uint_as_float(dv[2 * e + 1])),
                                 nd));
-              if (decltype(masked)::value) {
-                if ((c < lo && c >= sk) || c >= hi) p.x = ds.x = 0.f;
-                if ((c + 1 < lo && c + 1 >= sk) || c + 1 >= hi) p.y = ds.y = 0.f;
-              }
               pk[4 * g + e] = pack_bf16(p.x, p.y);
               dk[4 * g + e] = pack_bf16(ds.x, ds.y);
             }
@@ -476,43 +534,23 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
           break;
         }
         tc_fence_after();
-        const uint32_t te = tl + WB_TM_E + 16 * ch;
-        if (DKDV) tmem_st16(te, pk);
-        tmem_st16(te + WT / 2, dk);
-        tmem_wait_st();
-        tc_fence_before();
-        mbar_arrive_warp(e_full);
-      }
-      if (!ok) break;
-      // accumulators -> dK, dV (DKDV) or dQ (DQ) rows
-      if (!wait_warp(acc_full, it & 1)) break;
-      tc_fence_after();
-      uint32_t u0[16], w0[16];  // this thread's 16 columns of dV / dQ and of dK
-      tmem_ld16(tl + 256 + 16 * ch, u0);
-      if (DKDV) tmem_ld16(tl + 320 + 16 * ch, w0);
-      tc_fence_before();
-      mbar_arrive_warp(acc_free);
-      if (row < a.w.L) {
-        const long srow = (long)m.b * a.w.L + row;
-        auto store = [&](bf16* o, const uint32_t* v, float sc) {
-#pragma unroll
-          for (int i = 0; i < 16; i += 8)
-            *reinterpret_cast<uint4*>(o + i) = make_uint4(
-                pack_bf16(__uint_as_float(v[i]) * sc, __uint_as_float(v[i + 1]) * sc),
-                pack_bf16(__uint_as_float(v[i + 2]) * sc, __uint_as_float(v[i + 3]) * sc),
-                pack_bf16(__uint_as_float(v[i + 4]) * sc, __uint_as_float(v[i + 5]) * sc),
-                pack_bf16(__uint_as_float(v[i + 6]) * sc, __uint_as_float(v[i + 7]) * sc));
+        // the last item's sums are complete too, and nothing adds to them before this step's E
+        // is there
+        auto put_e = [&]() {
+          const uint32_t te = tl + WB_TM_E + 16 * ch;
+          if (DKDV) tmem_st16(te, pk);
+          tmem_st16(te + WT / 2, dk);
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive_warp(e_full);
         };
-        if (DKDV && m.piece >= 0) {  // a cut tile's sums
-          float* o = a.part + ((long)m.piece * WT + r) * WB_ACC + 16 * ch;
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            *reinterpret_cast<uint4*>(o + i) = make_uint4(u0[i], u0[i + 1], u0[i + 2], u0[i + 3]);
-            *reinterpret_cast<uint4*>(o + WB_D + i) = make_uint4(w0[i], w0[i + 1], w0[i + 2], w0[i + 3]);
-          }
+        if (j == 0 && it > 0) {
+          Sums v;
+          load_sums(v);
+          put_e();
+          store_sums(ring[(it - 1) & 3], v);
         } else {
-          store(a.out_u + srow * a.ld_u + m.h * WB_D + 16 * ch, u0, DKDV ? 1.f : a.scale);
-          if (DKDV) store(a.out_w + srow * a.ld_w + m.h * WB_D + 16 * ch, w0, a.scale);
+          put_e();
         }
       }
     }
@@ -542,18 +580,18 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
 __global__ void __launch_bounds__(128) window_join_kernel(WbArgs a) {
   pdl_enter();
   const int per = a.KV * a.B, hb = blockIdx.y, h = hb % a.KV, b = hb / a.KV;
-  const int cut_s = a.np_s > 1 ? a.w.sT : 0;  // cut tiles: the sinks', or all
-  const int t = (a.np_s > 1 ? 0 : a.w.sT) + blockIdx.z;
-  const bool sink = (int)blockIdx.z < cut_s;
-  const int first = sink ? t * a.np_s * per + hb
-                         : a.w.sT * a.np_s * per + (t - a.w.sT) * a.np_w * per + hb;
-  const int n = (wb_queries(a.w, t) * a.g + a.C - 1) / a.C;  // the pieces that have steps
-  const int r = blockIdx.x * 16 + threadIdx.x / 8, c = threadIdx.x % 8 * 16, row = t * WT + r;
+  const int t = (a.np_s > 1 ? 0 : a.w.sT) + blockIdx.z;  // cut tiles: the sinks', or all, or the others
+  const bool sink = t < a.w.sT;
+  const int np = sink ? a.np_s : a.np_w;
+  const int first = (sink ? t * np : a.w.sT * a.np_s + (t - a.w.sT) * np) * per + hb;
+  const int r = blockIdx.x * 16 + threadIdx.x / 8, col = threadIdx.x % 8 * 16, row = t * WT + r;
   if (row >= a.w.L) return;
+  const int m = wb_queries(a.w, t), all = m * a.g;
   float v[16] = {};
-  for (int i = 0; i < n; ++i) {
-    const float4* p = reinterpret_cast<const float4*>(
-        a.part + ((long)(first + i * per) * WT + r) * WB_ACC + c);
+  for (int s0 = 0, i = 0; s0 < all; s0 += a.C, ++i) {
+    if (r >= wb_rows(a.w, t, m, s0, min(a.C, all - s0))) continue;
+    const float4* p = reinterpret_cast<const float4*>(a.part + ((long)(first + i * per) * WT + r) * WB_ACC +
+                                                      col);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float4 x = p[e];
@@ -561,9 +599,9 @@ __global__ void __launch_bounds__(128) window_join_kernel(WbArgs a) {
     }
   }
   const long srow = (long)b * a.w.L + row;
-  bf16* o = c < WB_D ? a.out_u + srow * a.ld_u + h * WB_D + c
-                     : a.out_w + srow * a.ld_w + h * WB_D + c - WB_D;
-  if (c >= WB_D)
+  bf16* o = col < WB_D ? a.out_u + srow * a.ld_u + h * WB_D + col
+                       : a.out_w + srow * a.ld_w + h * WB_D + col - WB_D;
+  if (col >= WB_D)
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] *= a.scale;
   store8_bf16(o, v);
@@ -594,10 +632,10 @@ __global__ void __launch_bounds__(256) window_dot_kernel(const bf16* __restrict_
   if (live && sub == 0) Di[(row / L * H + h) * L + row % L] = v;
 }
 
-// How the key tiles' steps are cut.  A key tile of the window takes g * (W / 128
-// + 1) steps, one of the sinks g * n_t.  With fewer uncut tiles than SMs, every
-// tile is cut to half an SM's share of all steps; else only what is longer than
-// that and than a tile of the window.
+// How the key tiles' steps are cut.  A key tile of the window takes g (W / 128 + 1)
+// steps, one of the sinks g n_t.  With fewer tiles than SMs all are cut, into pieces of
+// half an SM's share of the steps (at least two: a piece costs 64 KB, written and read);
+// else only the sinks', into pieces of a sixteenth of it, or of a window's tile.
 struct Cut {
   int C, np_s, np_w;
   long items;
@@ -605,16 +643,17 @@ struct Cut {
 Cut wb_cut(const Window& c) {
   constexpr long SMS = 152;  // whatever the device has: the sums keep their order
   const WinTiles w(c);
-  const int g = c.H / c.KV;
-  long steps = 0;
-  for (int t = 0; t < w.n_t; ++t) steps += wb_queries(w, t);
-  const long heads = (long)c.KV * c.B, share = std::max(1L, steps * g * heads / (2 * SMS));
-  long longest = 0;  // of the tiles that are not sinks
-  for (int t = w.sT; t < w.n_t; ++t) longest = std::max<long>(longest, (long)wb_queries(w, t) * g);
-  const bool few = w.n_t * heads < SMS;
+  const long g = c.H / c.KV, heads = (long)c.KV * c.B;
+  long steps = 0, longest = 0;  // of a key head; of its longest tile that is not the sinks'
+  for (int t = 0; t < w.n_t; ++t) {
+    const long n = wb_queries(w, t) * g;
+    steps += n;
+    if (t >= w.sT) longest = std::max(longest, n);
+  }
   Cut r;
-  r.C = (int)(few ? share : std::max(longest, share));
-  const long sink = w.sT > 0 ? (long)wb_queries(w, 0) * g : 1;
+  r.C = (int)(w.n_t * heads < SMS ? std::max(2L, steps * heads / (2 * SMS))
+                                  : std::max(longest, steps * heads / (16 * SMS)));
+  const long sink = w.sT > 0 ? wb_queries(w, 0) * g : 1;
   r.np_s = (int)((sink + r.C - 1) / r.C);
   r.np_w = (int)std::max(1L, (longest + r.C - 1) / r.C);
   r.items = heads * ((long)w.sT * r.np_s + (long)(w.n_t - w.sT) * r.np_w);
@@ -626,18 +665,33 @@ struct WbWs {
   size_t bytes;
 };
 WbWs wb_carve(void* ws, const Window& c) {
-  const Cut k = wb_cut(c);
   auto up = [](size_t n) { return (n + 255) & ~size_t(255); };
+  const WinTiles w(c);
+  const Cut k = wb_cut(c);
   WbWs r;
   const size_t di = up((size_t)c.B * c.H * c.L * sizeof(float));
   r.Di = static_cast<float*>(ws);
   r.part = reinterpret_cast<float*>(static_cast<char*>(ws) + di);
-  // pieces are numbered as the items: those of tiles that are not cut hold nothing
-  const WinTiles w(c);
-  const long sinks = (long)c.KV * c.B * w.sT * k.np_s;
-  const long pieces = k.np_w > 1 ? k.items : k.np_s > 1 ? sinks : 0;
+  // pieces are numbered as the items, the sinks' first
+  const long pieces = k.np_w > 1 ? k.items : k.np_s > 1 ? (long)c.KV * c.B * w.sT * k.np_s : 0;
   r.bytes = di + (size_t)pieces * WT * WB_ACC * sizeof(float) + 256;
   return r;
+}
+
+// The registers that the row warps ask for (setmaxnreg) must be in the block's pool, which
+// holds what it was launched with: else they would wait for ever.
+template <bool DKDV>
+cudaError_t wb_registers_ok() {
+  static std::atomic<int> regs{0};  // a constant of the binary
+  int n = regs.load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaFuncAttributes at;
+    const cudaError_t e = cudaFuncGetAttributes(&at, window_bwd_kernel<DKDV>);
+    if (e != cudaSuccess) return e;
+    regs.store(n = at.numRegs, std::memory_order_relaxed);
+  }
+  return n * WB_THREADS >= WB_REGS_CTRL * 128 + WB_REGS_ROWS * 512 ? cudaSuccess
+                                                                   : cudaErrorInvalidConfiguration;
 }
 
 template <bool DKDV>
@@ -645,11 +699,13 @@ cudaError_t wb_launch(const CUtensorMap& x1, const CUtensorMap& x2, const CUtens
                       const CUtensorMap& y2, const WbArgs& a, const char* label, double flops,
                       double bytes, cudaStream_t st) {
   auto kern = window_bwd_kernel<DKDV>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, WB_SMEM);
+  cudaError_t e = wb_registers_ok<DKDV>();
+  if (e != cudaSuccess) return e;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, WB_SMEM);
   if (e != cudaSuccess) return e;
   LaunchTimer lt(label, st, flops, bytes);
-  return launch_kernel(kern, std::min(a.n_items, num_sms()), WB_THREADS, WB_SMEM, st, x1, x2, y1, y2,
-                       a);
+  const int grid = std::min(a.n_items, num_sms());
+  return launch_kernel(kern, grid, WB_THREADS, WB_SMEM, st, x1, x2, y1, y2, a);
 }
 
 }  // namespace
@@ -666,13 +722,13 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
       !tmap_bf16_seq(&td, dout, (uint64_t)c.H * WB_D, c.L, c.B, lddo, WB_D, WT))
     return cudaErrorInvalidValue;
   const WbWs wk = wb_carve(ws, c);
-  const Cut k = wb_cut(c);
   WbArgs a{};
   a.lse = v.lse;
   a.Di = wk.Di;
   a.part = wk.part;
   a.B = c.B; a.H = c.H; a.KV = c.KV; a.g = c.H / c.KV;
   a.w = WinTiles(c);
+  const Cut k = wb_cut(c);
   a.C = k.C; a.np_s = k.np_s; a.np_w = k.np_w;
   a.scale = 1.0f / sqrtf((float)WB_D);
   a.sl2 = a.scale * 1.4426950408889634f;

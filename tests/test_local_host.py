@@ -97,13 +97,13 @@ def test_window_refusals():
 
 
 def test_window_workspace_stays_small():
-    """The sums of cut tiles: some hundreds of 64 KB, whatever the length."""
+    """Di of every row and head, and the sums of cut tiles: at most some thousands of 64 KB, whatever the length."""
     for d in (win(1, 262144, 16, 16, window=1024, n_sink=4), win(1, 262144, 16, 1, window=0),
               win(4, 65536, 32, 2, window=4096, n_sink=300), win(1, 1, 1, 1), win(3, 999, 64, 1, window=1, n_sink=998)):
         rest = 4 * d.batch * d.n_heads * d.L + 512
-        tiles = d.batch * d.n_kv * -(-d.L // 128)
+        heads, tiles = d.batch * d.n_kv, -(-d.L // 128)
         pieces = (pf.pf_window_attn_workspace_size(d) - rest) / 65536
-        assert pieces <= 2 * 304 + 4 * d.batch * d.n_kv * 3 + (2 * tiles if tiles < 152 else 0)
+        assert pieces <= 16 * 152 + 3 * heads + (304 + heads * tiles if heads * tiles < 152 else 0)
 
 
 def paged(batch=3, n_heads=4, n_kv=2, dh=64, page=16, max_pages=4, n_pages=9, window=0, n_sink=0):
