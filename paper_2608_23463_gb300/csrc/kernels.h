@@ -244,6 +244,11 @@ bool tmap_bf16_2d(CUtensorMap* m, const void* base, uint64_t inner, uint64_t out
 bool tmap_bf16_seq(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint64_t n_seq,
                    uint64_t ld, uint32_t box_inner, uint32_t box_outer);
 
+// n_seq matrices of `outer` rows of 16 bf16 that follow one another, as above but with a
+// 32-byte swizzle; box 16 x box_outer.
+bool tmap_bf16_rows32(CUtensorMap* m, const void* base, uint64_t outer, uint64_t n_seq,
+                      uint32_t box_outer);
+
 // ------------------------------------------------------------- attention
 cudaError_t attn_fwd(const bf16* qkv, bf16* out, float* lse, int B, int m, int d, int nh,
                      bool causal, cudaStream_t st);

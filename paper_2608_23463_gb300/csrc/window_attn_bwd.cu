@@ -8,14 +8,18 @@
 //   DKDV: stationary X1 = K, X2 = V of a 128-key tile; streamed Y1 = Q_j, Y2 =
 //         dO_j of the query tiles that see it, one query head of the group
 //         after the other, into the same accumulators
-//           T1 = X1 Y1^T = S^T,  T2 = X2 Y2^T = dP^T     (TMEM, M=128 N=128)
+//           T1 = X1 Y1^T - 8 LSE / log2(e),  T2 = X2 Y2^T - Di  (TMEM, M=128 N=128)
 //           E1 = P^T, E2 = dS^T  (bf16, written to TMEM by the row warps)
 //           dV += E1 Y2,  dK += E2 Y1    (A from TMEM; TMEM accumulators)
 //   DQ:   stationary X1 = Q, X2 = dO of a 128-query tile and head; streamed
 //         Y1 = K_j, Y2 = V_j of the sinks' and the window's tiles
 //           T1 = S,  T2 = dP,  E2 = dS,  dQ += E2 Y1
-// Roles: warp 0 TMA producer (DKDV: it also stages each step's (LSE, Di)
-// pairs of the streamed queries in shared memory), warp 1 MMA issuer, warps
+// DKDV's rows are keys, so that LSE and Di run along the columns, the same for every
+// row: they come in as one more MMA (K=16) of ones with each query's LSE and Di, split
+// in three bf16 each (24 bits).  From shared memory every thread read both for each of
+// its columns, 128 KB a step at 128 bytes a cycle, and a producer warp staged them: 520
+// us for 16384 causal tokens of 8 heads, of which 106 for the reads alone.
+// Roles: warp 0 TMA producer, warp 1 MMA issuer, warps
 // 4-19 the row warps: four per TMEM lane quarter, each thread one row (TMEM
 // lane) and one quarter of the 128 streamed columns.
 // The sinks are seen by every later query: their key tiles' steps are cut into
@@ -47,6 +51,7 @@ int set_wait_limit_window_attn_bwd(unsigned long long ns) { return set_wait_limi
 namespace {
 
 constexpr int WB_D = 64;   // head width
+constexpr int WB_EXT = 16;  // bf16 of a query's LSE and Di: three each, the rest zero
 constexpr int WB_STAGES = 4;
 constexpr int WB_ROW_THREADS = 512;  // warps 4-19
 constexpr int WB_THREADS = 128 + WB_ROW_THREADS;
@@ -56,8 +61,10 @@ constexpr int WB_REGS_CTRL = 64, WB_REGS_ROWS = 104;
 static_assert(WB_REGS_CTRL * 128 + WB_REGS_ROWS * 512 <= 96 * WB_THREADS, "register split");
 constexpr uint32_t WB_T_BYTES = WT * WB_D * 2;  // 16 KB per tile
 constexpr uint32_t WB_OFF_Y = 2 * 2 * WB_T_BYTES;                     // X: [2 bufs][X1, X2]
-constexpr uint32_t WB_OFF_LD = WB_OFF_Y + WB_STAGES * 2 * WB_T_BYTES;  // Y: [stage][Y1, Y2]
-constexpr uint32_t WB_OFF_BAR = WB_OFF_LD + WB_STAGES * WT * 8;        // (lse, Di) [stage][128]
+constexpr uint32_t WB_OFF_E = WB_OFF_Y + WB_STAGES * 2 * WB_T_BYTES;  // Y: [stage][Y1, Y2]
+constexpr uint32_t WB_E_BYTES = WT * WB_EXT * 2;                       // LSE, Di: [stage][128][16]
+constexpr uint32_t WB_OFF_ONE = WB_OFF_E + WB_STAGES * WB_E_BYTES;     // the ones for T1, for T2
+constexpr uint32_t WB_OFF_BAR = WB_OFF_ONE + 2 * WB_E_BYTES;
 constexpr uint32_t WB_OFF_ITEM = WB_OFF_BAR + 256;  // four items
 constexpr uint32_t WB_SMEM = WB_OFF_ITEM + 4 * 48 + 1024;
 // TMEM columns: T1 at 0, T2 at 128 (fp32), accumulators at 256 (dV or dQ) and 320
@@ -166,6 +173,12 @@ struct WbStep {
   }
 };
 
+// Shared-memory matrix descriptor of a K-major tile with rows of 32 bytes, 32-byte swizzle.
+__device__ __forceinline__ uint64_t smem_desc_sw32(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | 1ull << 16 | (uint64_t)(256 >> 4) << 32 | 1ull << 46 |
+         6ull << 61;
+}
+
 // A wait of a converged warp, the common case of a completed phase up front.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
   if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
@@ -176,7 +189,7 @@ template <bool DKDV>
 __global__ void __launch_bounds__(WB_THREADS, 1)
     window_bwd_kernel(const __grid_constant__ CUtensorMap tmX1, const __grid_constant__ CUtensorMap tmX2,
                       const __grid_constant__ CUtensorMap tmY1, const __grid_constant__ CUtensorMap tmY2,
-                      WbArgs a) {
+                      const __grid_constant__ CUtensorMap tmE, WbArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -205,6 +218,16 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     mbar_init(done, 1);
     fence_barrier_init();
   }
+  if (DKDV) {
+    // rows of ones for LSE's three parts (T1) and Di's (T2), twice a row: the swizzle may put
+    // either half first, and the other half meets zeros
+    for (int i = threadIdx.x; i < 2 * WT * WB_EXT; i += WB_THREADS) {
+      const int k = i % 8;
+      reinterpret_cast<bf16*>(smem + WB_OFF_ONE)[i] =
+          __float2bfloat16((i < WT * WB_EXT ? k < 3 : k >= 3 && k < 6) ? 1.f : 0.f);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the MMAs read them
+  }
   if (warp == 1) {
     tmem_alloc(smem_u32(tmem_slot), WB_TMEM_COLS);
     tmem_relinquish();
@@ -220,28 +243,14 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(WB_REGS_CTRL));
   if (warp == 0) {
     // ------------------------------------------------------------ producer
-    // Lane 0 issues the copies.  DKDV: the whole warp also stages the (lse,
-    // Di) pairs of each step's 128 streamed queries in the stage's slot before
-    // lane 0 arms the stage's full barrier, so that the row warps read them
-    // after that barrier (the next step's are loaded one step ahead, four
-    // queries per lane).
     if (lane == 0) {
       prefetch_tmap(&tmX1);
       prefetch_tmap(&tmX2);
       prefetch_tmap(&tmY1);
       prefetch_tmap(&tmY2);
+      if (DKDV) prefetch_tmap(&tmE);
     }
-    float* const ld_ring = reinterpret_cast<float*>(smem + WB_OFF_LD);
     WbItem* const ring = reinterpret_cast<WbItem*>(smem + WB_OFF_ITEM);
-    float2 ldp[WT / 32];  // next step's pairs of queries lane + 32 i
-    auto fetch_step = [&](const WbItem& m, const WbStep<DKDV>& sp) {
-      const int q0 = sp.tile * WT + lane;
-      const long o = ((long)m.b * a.H + sp.head) * a.w.L + q0;
-#pragma unroll
-      for (int i = 0; i < WT / 32; ++i)
-        ldp[i] = q0 + 32 * i < a.w.L ? make_float2(-a.lse[o + 32 * i], -a.Di[o + 32 * i])
-                                     : make_float2(0.f, 0.f);
-    };
     int rd = 0;
     auto next_item = [&]() -> WbItem {  // the next one with steps; n < 0 at the end
       for (int k; (k = wb_rank(blockIdx.x, rd)) < a.n_items; ++rd) {
@@ -256,7 +265,6 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       return i;
     };
     WbItem m = next_item();
-    if (DKDV && m.n > 0) fetch_step(m, WbStep<DKDV>(m));
     bool ok = true;
     for (uint32_t it = 0; ok; ++it) {
       const uint32_t xb = it & 1;
@@ -284,30 +292,18 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
           ok = false;
           break;
         }
-        if (DKDV) {
-#pragma unroll
-          for (int i = 0; i < WT / 32; ++i) {  // queries c, c + 1 (even c): -lse -lse -Di -Di
-            float* d = ld_ring + st * 2 * WT + (32 * i + lane) / 2 * 4 + (lane & 1);
-            d[0] = ldp[i].x;
-            d[2] = ldp[i].y;
-          }
-          __syncwarp();
-        }
         if (lane == 0) {
           const uint32_t ydst = sbase + WB_OFF_Y + st * 2 * WB_T_BYTES;
           const int yrow = sp.tile * WT, ycol = (DKDV ? sp.head : kv) * WB_D;
-          mbar_arrive_expect_tx(y_full + 8 * st, 2 * WB_T_BYTES);
+          mbar_arrive_expect_tx(y_full + 8 * st, 2 * WB_T_BYTES + (DKDV ? WB_E_BYTES : 0u));
+          if (DKDV)
+            tma_load_3d(sbase + WB_OFF_E + st * WB_E_BYTES, &tmE, y_full + 8 * st, 0, yrow,
+                        m.b * a.H + sp.head);
           tma_load_3d(ydst, &tmY1, y_full + 8 * st, ycol, yrow, m.b);
           tma_load_3d(ydst + WB_T_BYTES, &tmY2, y_full + 8 * st, ycol, yrow, m.b);
         }
         y_issued = G + 1;
         sp.next(m);
-        if (DKDV) {  // the pairs of the next step (this item's or the next item's first)
-          if (j + 1 < m.n)
-            fetch_step(m, sp);
-          else if (m2.n > 0)
-            fetch_step(m2, WbStep<DKDV>(m2));
-        }
       }
       m = m2;
     }
@@ -320,6 +316,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     const uint64_t dx0 = smem_desc_sw128(sbase, 16, 1024);
     const uint64_t dy0 = smem_desc_sw128(sbase + WB_OFF_Y, 16, 1024);
     const uint64_t da0 = smem_desc_sw128(sbase + WB_OFF_Y, 8192, 1024);
+    const uint64_t de0 = smem_desc_sw32(sbase + WB_OFF_E), one = smem_desc_sw32(sbase + WB_OFF_ONE);
     constexpr uint64_t TILE = WB_T_BYTES >> 4;  // in a descriptor's units
     bool ok = true;
     uint32_t it = 0, G = 0;
@@ -361,12 +358,16 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
           break;
         }
         tc_fence_after();
-        const uint64_t y1 = dy0 + st * 2 * TILE, y2 = y1 + TILE;
+        const uint64_t y1 = dy0 + st * 2 * TILE, y2 = y1 + TILE, ye = de0 + st * (WB_E_BYTES >> 4);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < WB_D / 16; ++kk) {
             tc_mma_f16(tmem, d1 + kk * 2, y1 + kk * 2, idesc_t, kk ? 1u : 0u);
             tc_mma_f16(tmem + WT, d2 + kk * 2, y2 + kk * 2, idesc_t, kk ? 1u : 0u);
+          }
+          if (DKDV) {
+            tc_mma_f16(tmem, one, ye, idesc_t, 1u);
+            tc_mma_f16(tmem + WT, one + (WB_E_BYTES >> 4), ye, idesc_t, 1u);
           }
           tc_commit(t_full);
           if (j == n - 1) tc_commit(x_empty + 8 * xb);
@@ -389,7 +390,6 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     const int r = q4 * 32 + lane;  // stationary row in the tile = TMEM lane
     const int ch = (warp - 4) >> 2;   // quarter of the streamed columns: [32 ch, 32 ch + 32)
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
-    const float4* ld_ring = reinterpret_cast<const float4*>(smem + WB_OFF_LD);  // [stage][64]
     const WbItem* const ring = reinterpret_cast<const WbItem*>(smem + WB_OFF_ITEM);
     struct Sums {
       uint32_t u[16], w[16];  // 16 columns of an item's dV / dQ and of its dK
@@ -460,13 +460,6 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         const int yt = sp.tile, c0 = yt * WT;  // first streamed index of this step
         sp.next(m);
         const bool hidden = yt == m.t || (DKDV ? yt >= edge : yt < edge && yt >= whole);
-        // DKDV: the step's (lse, Di) pairs, staged by the producer before the
-        // stage's full barrier (already complete: the step's scores used it;
-        // the slot is refilled only after this step's E has been consumed)
-        if (DKDV && !wait_warp(y_full + 8 * (Gj % WB_STAGES), (Gj / WB_STAGES) & 1)) {
-          ok = false;
-          break;
-        }
         if (!wait_warp(t_full, Gj & 1)) {
           ok = false;
           break;
@@ -479,7 +472,6 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         tmem_wait_ld(pa);
         tc_fence_before();
         mbar_arrive_warp(t_free);
-        const float4* lds = ld_ring + (Gj % WB_STAGES) * (WT / 2) + 16 * ch;
         // P and dS of the thread's 32 columns from kb on, as bf16 pairs
         auto emit = [&](auto masked, int kb, uint32_t* pk, uint32_t* dk) {
           if (decltype(masked)::value) {
@@ -496,28 +488,21 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
           }
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            // (the shared loads of a later group wait for their turn: hoisted, they would not
-            // fit the registers)
-            if (DKDV) asm volatile("" ::: "memory");
             const uint32_t* sv = sa + g * 8;
             const uint32_t* dv = pa + g * 8;
-            // -lse and -Di of two columns per 128-bit shared load (DKDV), as the packed
-            // fp32x2 arithmetic takes them
+            // packed fp32x2 arithmetic (each lane an IEEE fp32 operation)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              float2 nl = make_float2(-lse_r, -lse_r), nd = make_float2(-di_r, -di_r);
-              if (DKDV) {
-                const float4 v = lds[g * 4 + e];
-                nl = make_float2(v.x, v.y);
-                nd = make_float2(v.z, v.w);
-              }
-              const float2 z = __ffma2_rn(
-                  make_float2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1])),
-                  make_float2(a.sl2, a.sl2), nl);
+              const float2 sl = make_float2(a.sl2, a.sl2);
+              const float2 sv2 =
+                  make_float2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
+              const float2 dv2 =
+                  make_float2(__uint_as_float(dv[2 * e]), __uint_as_float(dv[2 * e + 1]));
+              const float2 z = DKDV ? __fmul2_rn(sv2, sl)
+                                    : __ffma2_rn(sv2, sl, make_float2(-lse_r, -lse_r));
               const float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
-              const float2 ds = __fmul2_rn(
-                  p, __fadd2_rn(make_float2(__uint_as_float(dv[2 * e]), __uint_as_float(dv[2 * e + 1])),
-                                nd));
+              const float2 ds =
+                  __fmul2_rn(p, DKDV ? dv2 : __fadd2_rn(dv2, make_float2(-di_r, -di_r)));
               pk[4 * g + e] = pack_bf16(p.x, p.y);
               dk[4 * g + e] = pack_bf16(ds.x, ds.y);
             }
@@ -608,11 +593,13 @@ __global__ void __launch_bounds__(128) window_join_kernel(WbArgs a) {
   store8_bf16(o + 8, v + 8);
 }
 
-// Di = rowsum(dO * O) per (sequence, head, query): eight lanes per (row, head),
+// Di = rowsum(dO * O) per (sequence, head, query), alone and beside LSE: eight lanes per (row, head),
 // each eight of the head's 64 columns with 16-byte loads.
 __global__ void __launch_bounds__(256) window_dot_kernel(const bf16* __restrict__ dO, long lddo,
                                                          const bf16* __restrict__ O, long ldo,
                                                          const bf16* __restrict__ rest,
+                                                         const float* __restrict__ lse,
+                                                         bf16* __restrict__ ext,
                                                          float* __restrict__ Di, long rows, int L,
                                                          int H) {
   const int pz = pdl_enter();
@@ -629,7 +616,26 @@ __global__ void __launch_bounds__(256) window_dot_kernel(const bf16* __restrict_
   for (int k = 0; k < 8; ++k) v = fmaf(x[k], y[k] + z[k], v);
 #pragma unroll
   for (int s = 4; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
-  if (live && sub == 0) Di[(row / L * H + h) * L + row % L] = v;
+  if (live && sub < 2) {  // Di, and (LSE, Di) as the MMA of DKDV takes them
+    const long o = (row / L * H + h) * L + row % L;
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (sub == 0) {
+      Di[o] = v;
+      // three bf16 that add up to x
+      auto split = [](float x, bf16* p) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          p[i] = __float2bfloat16(x);
+          x -= __bfloat162float(p[i]);
+        }
+      };
+      __align__(16) bf16 e[8] = {};
+      split(lse[o] * (-8.f * 0.6931471805599453f), e);  // 8 / log2(e): T1 is multiplied by its inverse
+      split(-v, e + 3);
+      w = *reinterpret_cast<const uint4*>(e);
+    }
+    *reinterpret_cast<uint4*>(ext + o * WB_EXT + 8 * sub) = w;
+  }
 }
 
 // How the key tiles' steps are cut.  A key tile of the window takes g (W / 128 + 1)
@@ -662,6 +668,7 @@ Cut wb_cut(const Window& c) {
 
 struct WbWs {
   float *Di, *part;
+  bf16* ext;  // [B, H, L][16]
   size_t bytes;
 };
 WbWs wb_carve(void* ws, const Window& c) {
@@ -671,10 +678,12 @@ WbWs wb_carve(void* ws, const Window& c) {
   WbWs r;
   const size_t di = up((size_t)c.B * c.H * c.L * sizeof(float));
   r.Di = static_cast<float*>(ws);
-  r.part = reinterpret_cast<float*>(static_cast<char*>(ws) + di);
+  const size_t ext = up((size_t)c.B * c.H * c.L * WB_EXT * sizeof(bf16));
+  r.ext = reinterpret_cast<bf16*>(static_cast<char*>(ws) + di);
+  r.part = reinterpret_cast<float*>(static_cast<char*>(ws) + di + ext);
   // pieces are numbered as the items, the sinks' first
   const long pieces = k.np_w > 1 ? k.items : k.np_s > 1 ? (long)c.KV * c.B * w.sT * k.np_s : 0;
-  r.bytes = di + (size_t)pieces * WT * WB_ACC * sizeof(float) + 256;
+  r.bytes = di + ext + (size_t)pieces * WT * WB_ACC * sizeof(float) + 256;
   return r;
 }
 
@@ -696,7 +705,7 @@ cudaError_t wb_registers_ok() {
 
 template <bool DKDV>
 cudaError_t wb_launch(const CUtensorMap& x1, const CUtensorMap& x2, const CUtensorMap& y1,
-                      const CUtensorMap& y2, const WbArgs& a, const char* label, double flops,
+                      const CUtensorMap& y2, const CUtensorMap& te, const WbArgs& a, const char* label, double flops,
                       double bytes, cudaStream_t st) {
   auto kern = window_bwd_kernel<DKDV>;
   cudaError_t e = wb_registers_ok<DKDV>();
@@ -705,7 +714,7 @@ cudaError_t wb_launch(const CUtensorMap& x1, const CUtensorMap& x2, const CUtens
   if (e != cudaSuccess) return e;
   LaunchTimer lt(label, st, flops, bytes);
   const int grid = std::min(a.n_items, num_sms());
-  return launch_kernel(kern, grid, WB_THREADS, WB_SMEM, st, x1, x2, y1, y2, a);
+  return launch_kernel(kern, grid, WB_THREADS, WB_SMEM, st, x1, x2, y1, y2, te, a);
 }
 
 }  // namespace
@@ -715,13 +724,14 @@ size_t window_bwd_ws_bytes(const Window& c) { return wb_carve(nullptr, c).bytes;
 cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long ldo,
                        const WindowSaved& v, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
                        cudaStream_t st) {
-  CUtensorMap tq, tk, tv, td;
+  CUtensorMap tq, tk, tv, td, te;
   if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WB_D, c.L, c.B, x.ldq, WB_D, WT) ||
       !tmap_bf16_seq(&tk, x.k, (uint64_t)c.KV * WB_D, c.L, c.B, x.ldk, WB_D, WT) ||
       !tmap_bf16_seq(&tv, x.v, (uint64_t)c.KV * WB_D, c.L, c.B, x.ldv, WB_D, WT) ||
       !tmap_bf16_seq(&td, dout, (uint64_t)c.H * WB_D, c.L, c.B, lddo, WB_D, WT))
     return cudaErrorInvalidValue;
   const WbWs wk = wb_carve(ws, c);
+  if (!tmap_bf16_rows32(&te, wk.ext, c.L, (uint64_t)c.B * c.H, WT)) return cudaErrorInvalidValue;
   WbArgs a{};
   a.lse = v.lse;
   a.Di = wk.Di;
@@ -737,10 +747,10 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
   const double rows = (double)c.B * c.L, pairs = (double)c.B * c.H * window_pairs(c);
   cudaError_t e;
   {
-    LaunchTimer lt("window_bwd_dot", st, 2.0 * rows * c.H * WB_D, rows * c.H * (6.0 * WB_D + 4.0));
+    LaunchTimer lt("window_bwd_dot", st, 2.0 * rows * c.H * WB_D, rows * c.H * (6.0 * WB_D + 8.0 + 2.0 * WB_EXT));
     const long n = (long)c.B * c.L;
     e = launch_kernel(window_dot_kernel, (unsigned)((n * c.H * 8 + 255) / 256), 256, 0, st, dout, lddo,
-                      out, ldo, v.rest, wk.Di, n, c.L, c.H);
+                      out, ldo, v.rest, v.lse, wk.ext, wk.Di, n, c.L, c.H);
     if (e != cudaSuccess) return e;
   }
   a.out_u = static_cast<bf16*>(dx.v);
@@ -748,7 +758,7 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
   a.out_w = static_cast<bf16*>(dx.k);
   a.ld_w = dx.ldk;
   a.n_items = (int)k.items;
-  e = wb_launch<true>(tk, tv, tq, td, a, "window_bwd_dkdv", 8.0 * WB_D * pairs,
+  e = wb_launch<true>(tk, tv, tq, td, te, a, "window_bwd_dkdv", 8.0 * WB_D * pairs,
                       2.0 * rows * WB_D * (2.0 * c.H + 4.0 * c.KV), st);
   if (e != cudaSuccess) return e;
   const int cut = (k.np_s > 1 ? a.w.sT : 0) + (k.np_w > 1 ? a.w.n_t - a.w.sT : 0);
@@ -760,7 +770,7 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
   a.out_u = static_cast<bf16*>(dx.q);
   a.ld_u = dx.ldq;
   a.n_items = (int)q_items;
-  return wb_launch<false>(tq, td, tk, tv, a, "window_bwd_dq", 6.0 * WB_D * pairs,
+  return wb_launch<false>(tq, td, tk, tv, te, a, "window_bwd_dq", 6.0 * WB_D * pairs,
                           2.0 * rows * WB_D * (3.0 * c.H + 2.0 * c.KV), st);
 }
 

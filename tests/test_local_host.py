@@ -97,10 +97,10 @@ def test_window_refusals():
 
 
 def test_window_workspace_stays_small():
-    """Di of every row and head, and the sums of cut tiles: at most some thousands of 64 KB, whatever the length."""
+    """36 bytes of every row and head, and the sums of cut tiles: at most some thousands of 64 KB, whatever the length."""
     for d in (win(1, 262144, 16, 16, window=1024, n_sink=4), win(1, 262144, 16, 1, window=0),
               win(4, 65536, 32, 2, window=4096, n_sink=300), win(1, 1, 1, 1), win(3, 999, 64, 1, window=1, n_sink=998)):
-        rest = 4 * d.batch * d.n_heads * d.L + 512
+        rest = 36 * d.batch * d.n_heads * d.L + 768
         heads, tiles = d.batch * d.n_kv, -(-d.L // 128)
         pieces = (pf.pf_window_attn_workspace_size(d) - rest) / 65536
         assert pieces <= 16 * 152 + 3 * heads + (304 + heads * tiles if heads * tiles < 152 else 0)
