@@ -18,6 +18,15 @@
 //             in registers, O += P V_j (M=128, N=64, K=128) with P from TMEM
 //   warps 4-7 softmax of tile A, warps 8-11 of tile B: one query row per thread
 //             (TMEM lane), its 128 scores in registers; P goes back to TMEM
+// What bounds it: the chain of one softmax warp through a tile (about 430
+// instructions, two such warps on each scheduler), beside 1024 cycles of MMAs
+// and as many of exponentials for a pair of tiles.  262144 tokens of 16 heads on
+// 4, window 4096: 4.49 ms (0.99 PFLOP/s), timed with parts left out: 2.74 with
+// no arithmetic, 4.07 without the maxima, 3.55 without the exponentials.  One
+// MMA issuer for both tiles, which makes each wait for the other's softmax, and
+// key tiles tested one by one: 5.06; two threads to a row (sixteen softmax
+// warps): 5.27; chunks of 64 keys in two buffers a tile that P shares with the
+// scores: 5.50; O read out in the next item's first step: 5.03.
 // A row's probabilities are taken against a reference m, the maximum of the
 // first tile in which the row sees a key, raised only when a later tile's
 // maximum exceeds it by more than WA_RESCALE (log2 units); then O and the sum
