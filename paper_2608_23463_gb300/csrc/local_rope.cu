@@ -129,13 +129,16 @@ struct RopeSmem {
 // (The table comes from parameter space, which serves a warp one address at a
 // time: each thread fetches one entry.)
 template <int DH>
-__device__ __forceinline__ void stage(RopeSmem& s, const RopeFreq& fr, const RopeArgs& a) {
+__device__ __forceinline__ void stage_freq(RopeSmem& s, const RopeFreq& fr) {
   const int i = threadIdx.x;
   if (i < DH / 2) {
     s.f[i] = fr.f[i];
     s.axis[i] = fr.axis[i];
   }
-  pdl_enter();
+}
+template <int DH>
+__device__ __forceinline__ void stage_weights(RopeSmem& s, const RopeArgs& a) {
+  const int i = threadIdx.x;
   if (i < DH) {
     const float* w = i < DH / 2 ? a.w_q : a.w_k;
     const int c = i % (DH / 2), j = c / 2 * 4 + (c & 1);  // values j and j + 2 of a head
@@ -251,7 +254,9 @@ __global__ void __launch_bounds__(RW_THREADS, RW_FWD_CTAS)
     rope_fwd_kernel(RopeArgs a, const __grid_constant__ RopeFreq fr) {
   using Ly = Lay<T, DH>;
   __shared__ __align__(16) RopeSmem s;
-  stage<DH>(s, fr, a);
+  stage_freq<DH>(s, fr);
+  pdl_enter();
+  stage_weights<DH>(s, a);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int nq = (a.H + Ly::HEADS - 1) / Ly::HEADS, nk = (a.KV + Ly::HEADS - 1) / Ly::HEADS;
   const int passes = nq + nk + (APPEND ? nk : 0);
@@ -396,7 +401,9 @@ __global__ void __launch_bounds__(RW_THREADS, RW_BWD_CTAS)
   constexpr int G = Ly::G;
   __shared__ __align__(16) RopeSmem s;
   __shared__ float red[RW_WARPS][2][DH];
-  stage<DH>(s, fr, a);
+  stage_freq<DH>(s, fr);
+  pdl_enter();
+  stage_weights<DH>(s, a);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   float2 g[2][2 * G];  // of w_q, w_k: first halves, then second halves
 #pragma unroll
@@ -455,14 +462,14 @@ __global__ void __launch_bounds__(RW_THREADS, RW_BWD_CTAS)
 
 // dw[c] = sum over the CTAs of part[.][c] (c < dh: w_q, else w_k).  A CTA takes
 // 32 columns, 16 threads to a column.
-__global__ void __launch_bounds__(512) rope_dw_kernel(const float* __restrict__ part, int n, int dh,
+__global__ void __launch_bounds__(512) rope_dw_kernel(const float* part, int n, int dh,
                                                       float* dw_q, float* dw_k) {
-  const int pz = pdl_enter();
+  pdl_enter();
   __shared__ float red[16][33];
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
   float v = 0.f;
 #pragma unroll 8
-  for (int i = g + pz; i < n; i += 16) v += part[(long)i * 2 * dh + c];
+  for (int i = g; i < n; i += 16) v += part[(long)i * 2 * dh + c];
   red[g][threadIdx.x & 31] = v;
   __syncthreads();
   if (g) return;
@@ -473,9 +480,9 @@ __global__ void __launch_bounds__(512) rope_dw_kernel(const float* __restrict__ 
   if (o) o[c % dh] = v;
 }
 
-__global__ void paged_advance_kernel(const int* __restrict__ start, int* len, int B, int cap) {
-  const int pz = pdl_enter();
-  const int b = blockIdx.x * blockDim.x + threadIdx.x + pz;
+__global__ void paged_advance_kernel(const int* start, int* len, int B, int cap) {
+  pdl_enter();
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b >= B) return;
   const int n = start ? start[b + 1] - start[b] : 1;
   const int old = len[b];

@@ -595,15 +595,15 @@ __global__ void __launch_bounds__(128) window_join_kernel(WbArgs a) {
 
 // Di = rowsum(dO * O) per (sequence, head, query), alone and beside LSE: eight lanes per (row, head),
 // each eight of the head's 64 columns with 16-byte loads.
-__global__ void __launch_bounds__(256) window_dot_kernel(const bf16* __restrict__ dO, long lddo,
-                                                         const bf16* __restrict__ O, long ldo,
-                                                         const bf16* __restrict__ rest,
-                                                         const float* __restrict__ lse,
-                                                         bf16* __restrict__ ext,
-                                                         float* __restrict__ Di, long rows, int L,
+__global__ void __launch_bounds__(256) window_dot_kernel(const bf16* dO, long lddo,
+                                                         const bf16* O, long ldo,
+                                                         const bf16* rest,
+                                                         const float* lse,
+                                                         bf16* ext,
+                                                         float* Di, long rows, int L,
                                                          int H) {
-  const int pz = pdl_enter();
-  const long gid = ((long)blockIdx.x * blockDim.x + threadIdx.x + pz) >> 3, items = rows * H;
+  pdl_enter();
+  const long gid = ((long)blockIdx.x * blockDim.x + threadIdx.x) >> 3, items = rows * H;
   const int sub = threadIdx.x & 7;
   const bool live = gid < items;
   const long it = live ? gid : items - 1, row = it / H;
