@@ -3,9 +3,34 @@
 // paged_attn.cu, window_attn.cu and window_attn_bwd.cu).
 #pragma once
 
+#include <atomic>
+
 #include "kernels.h"
 
 namespace pf {
+
+// What a kernel needs of the device before its first launch there: its shared memory, and
+// (pool > 0) that its threads, `threads` of them, bring the `pool` registers that its warps
+// share out among themselves (setmaxnreg): with fewer they would wait for ever.  Asked
+// once per device and kernel: asked on every call, it took 2 of a small call's 14 us.
+struct KernelOnce {
+  std::atomic<unsigned long long> done{0};  // a bit per device
+  cudaError_t operator()(const void* kern, int smem, int threads = 0, int pool = 0) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    if (pool > 0) {
+      cudaFuncAttributes at;
+      if ((e = cudaFuncGetAttributes(&at, kern)) != cudaSuccess) return e;
+      if (at.numRegs * threads < pool) return cudaErrorInvalidConfiguration;
+    }
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+  }
+};
 
 // Rows of three matrices, leading dimensions in elements (of bf16 or fp32).
 struct QkvPtr {

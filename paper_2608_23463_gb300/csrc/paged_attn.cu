@@ -425,8 +425,8 @@ int pa_grid(const Paged& c) {
 
 template <int DH>
 cudaError_t pa_launch(const PaArgs& a, bool split, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<DH>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, PaCfg<DH>::SMEM);
+  static KernelOnce once;
+  cudaError_t e = once(reinterpret_cast<const void*>(paged_attn_kernel<DH>), PaCfg<DH>::SMEM);
   if (e != cudaSuccess) return e;
   const double rows = (double)a.B * a.KV * std::min<long>((long)a.max_pages * a.page, 0x7fffffffL);
   {

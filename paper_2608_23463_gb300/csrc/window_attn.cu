@@ -38,7 +38,6 @@
 // anything; P = 0 meets its V in the MMA, so values must be finite up to the
 // end of the tile that a row sees.
 #include <algorithm>
-#include <atomic>
 
 #include "local.h"
 #include "window_tiles.cuh"
@@ -480,21 +479,6 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
   }
 }
 
-// The registers that the softmax warps ask for (setmaxnreg) must be in the block's
-// pool, which holds what it was launched with: else they would wait for ever.
-cudaError_t wa_registers_ok() {
-  static std::atomic<int> regs{0};  // a constant of the binary
-  int n = regs.load(std::memory_order_relaxed);
-  if (n == 0) {
-    cudaFuncAttributes at;
-    const cudaError_t e = cudaFuncGetAttributes(&at, window_fwd_kernel);
-    if (e != cudaSuccess) return e;
-    regs.store(n = at.numRegs, std::memory_order_relaxed);
-  }
-  return n * WA_THREADS >= WA_REGS_CTRL * 128 + WA_REGS_ROWS * 256 ? cudaSuccess
-                                                                    : cudaErrorInvalidConfiguration;
-}
-
 }  // namespace
 
 double window_pairs(const Window& c) {
@@ -531,9 +515,9 @@ cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, co
   if (items > 0x3fffffff) return cudaErrorInvalidValue;
   a.n_items = (int)items;
   a.sl2 = 1.4426950408889634f / sqrtf((float)WA_D);
-  cudaError_t e = wa_registers_ok();
-  if (e != cudaSuccess) return e;
-  e = cudaFuncSetAttribute(window_fwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WA_SMEM);
+  static KernelOnce once;
+  const cudaError_t e = once(reinterpret_cast<const void*>(window_fwd_kernel), WA_SMEM, WA_THREADS,
+                             WA_REGS_CTRL * 128 + WA_REGS_ROWS * 256);
   if (e != cudaSuccess) return e;
   const double pairs = (double)c.B * c.H * window_pairs(c);
   LaunchTimer lt("window_fwd", st, 4.0 * WA_D * pairs,

@@ -37,7 +37,6 @@
 // Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the
 // end of a sequence read as zero.
 #include <algorithm>
-#include <atomic>
 #include <type_traits>
 
 #include "local.h"
@@ -687,30 +686,14 @@ WbWs wb_carve(void* ws, const Window& c) {
   return r;
 }
 
-// The registers that the row warps ask for (setmaxnreg) must be in the block's pool, which
-// holds what it was launched with: else they would wait for ever.
-template <bool DKDV>
-cudaError_t wb_registers_ok() {
-  static std::atomic<int> regs{0};  // a constant of the binary
-  int n = regs.load(std::memory_order_relaxed);
-  if (n == 0) {
-    cudaFuncAttributes at;
-    const cudaError_t e = cudaFuncGetAttributes(&at, window_bwd_kernel<DKDV>);
-    if (e != cudaSuccess) return e;
-    regs.store(n = at.numRegs, std::memory_order_relaxed);
-  }
-  return n * WB_THREADS >= WB_REGS_CTRL * 128 + WB_REGS_ROWS * 512 ? cudaSuccess
-                                                                   : cudaErrorInvalidConfiguration;
-}
-
 template <bool DKDV>
 cudaError_t wb_launch(const CUtensorMap& x1, const CUtensorMap& x2, const CUtensorMap& y1,
                       const CUtensorMap& y2, const CUtensorMap& te, const WbArgs& a, const char* label, double flops,
                       double bytes, cudaStream_t st) {
   auto kern = window_bwd_kernel<DKDV>;
-  cudaError_t e = wb_registers_ok<DKDV>();
-  if (e != cudaSuccess) return e;
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, WB_SMEM);
+  static KernelOnce once;
+  const cudaError_t e = once(reinterpret_cast<const void*>(kern), WB_SMEM, WB_THREADS,
+                             WB_REGS_CTRL * 128 + WB_REGS_ROWS * 512);
   if (e != cudaSuccess) return e;
   LaunchTimer lt(label, st, flops, bytes);
   const int grid = std::min(a.n_items, num_sms());
