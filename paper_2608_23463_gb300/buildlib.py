@@ -1,7 +1,8 @@
 """Build libproxyformer.so (the sm_103a CUDA library) in-tree with nvcc.
 
 Each .cu file under csrc/ compiles to an object in parallel, then one shared
-library is linked next to this file.  Usage: ``python -m
+library is linked next to this file, and the native part of local.py
+(csrc/local_binding.cpp, _local.so) against it.  Usage: ``python -m
 paper_2608_23463_gb300.buildlib`` or ``build()`` from Python.
 """
 from __future__ import annotations
@@ -17,6 +18,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libproxyformer.so")
+BINDING = os.path.join(HERE, "_local.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -31,6 +33,35 @@ def _nvcc() -> str:
 
 def _sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
+
+
+def _compile_binding(obj: str) -> None:
+    """local_binding.cpp against the headers of the installed torch."""
+    import sysconfig
+
+    import torch
+    inc = os.path.join(os.path.dirname(torch.__file__), "include")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
+    dirs = [os.path.join(ROOT, "include"), inc, os.path.join(inc, "torch", "csrc", "api", "include"),
+            sysconfig.get_paths()["include"], cuda]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *(f"-I{d}" for d in dirs), "-c", os.path.join(CSRC, "local_binding.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed on local_binding.cpp:\n{r.stdout}\n{r.stderr}")
+
+
+def _link_binding(obj: str) -> None:
+    import torch
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = [os.environ.get("CXX", "g++"), "-shared", obj, "-o", BINDING + ".tmp", f"-L{HERE}",
+           "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN", f"-L{lib}", "-lc10", "-lc10_cuda",
+           "-ltorch_cpu", "-ltorch_python"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"linking {BINDING} failed:\n{r.stdout}\n{r.stderr}")
+    os.replace(BINDING + ".tmp", BINDING)
 
 
 def build(verbose: bool = False, extra_flags=()) -> str:
@@ -56,13 +87,22 @@ def build(verbose: bool = False, extra_flags=()) -> str:
             print(r.stderr, file=sys.stderr)
         return obj
 
-    with ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
+    bind_src, bind_obj = (os.path.join(d, "local_binding" + e) for d, e in ((CSRC, ".cpp"), (OUT_DIR, ".o")))
+    bind_deps = max(os.path.getmtime(bind_src), os.path.getmtime(deps[-1]))
+
+    with ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
+        stale = not os.path.exists(bind_obj) or os.path.getmtime(bind_obj) < bind_deps
+        binding = ex.submit(_compile_binding, bind_obj) if stale else None
         objs = list(ex.map(compile_one, srcs))
-    cmd = [nvcc, *ARCH, "-shared", "-o", LIB + ".tmp", *objs]
+        if binding is not None:
+            binding.result()
+    cmd = [nvcc, *ARCH, "-shared", "-Xlinker", "-soname=" + os.path.basename(LIB), "-o", LIB + ".tmp",
+           *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(LIB + ".tmp", LIB)
+    _link_binding(bind_obj)
     return LIB
 
 

@@ -19,9 +19,9 @@
 // in three bf16 each (24 bits).  From shared memory every thread read both for each of
 // its columns, 128 KB a step at 128 bytes a cycle, and a producer warp staged them: 520
 // us for 16384 causal tokens of 8 heads, of which 106 for the reads alone.
-// Roles: warp 0 TMA producer, warp 1 MMA issuer, warps
-// 4-19 the row warps: four per TMEM lane quarter, each thread one row (TMEM
-// lane) and one quarter of the 128 streamed columns.
+// Roles: warp 0 TMA producer, warp 1 MMA issuer, warps 4-19 the row warps: four per
+// TMEM lane quarter, each thread one row (TMEM lane) and one quarter of the 128
+// streamed columns.
 // The sinks are seen by every later query: their key tiles' steps are cut into
 // pieces (wb_cut), as are all tiles' where there are few.  The pieces of a cut
 // tile leave fp32 sums, those past its window of the sinks' rows alone;
@@ -37,7 +37,6 @@
 // Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the
 // end of a sequence read as zero.
 #include <algorithm>
-#include <type_traits>
 
 #include "local.h"
 #include "window_tiles.cuh"

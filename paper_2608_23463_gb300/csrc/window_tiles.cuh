@@ -29,15 +29,6 @@ struct WinTiles {
     const long q = ((long)t * WT + WT - 1 + W - 1) / WT;
     return q < n_t - 1 ? (int)q : n_t - 1;
   }
-  // some query of tile t sees some key of tile kt
-  __host__ __device__ __forceinline__ bool sees(int t, int kt) const {
-    return t < n_t && kt <= t && (kt >= lo(t) || kt < sT);
-  }
-  // every query of tile t that is not before the keys of tile kt has them in its
-  // window or among the sinks
-  __host__ __device__ __forceinline__ bool inside(int t, int kt) const {
-    return kt * WT > t * WT + WT - 1 - W || kt * WT + WT <= S;
-  }
 };
 
 }  // namespace pf

@@ -154,3 +154,21 @@ def test_workspace_follows_the_split():
     size = pf.pf_paged_attn_workspace_size
     assert size(paged(batch=1, max_pages=4)) == 2 * 2 * 2 * 66 * 4
     assert size(paged(batch=64, max_pages=1000)) == size(paged(batch=2048, max_pages=1 << 30)) == 2 * 304 * 2 * 66 * 4
+
+
+def test_python_refusals():
+    """The classes refuse what is not on a GPU, of another type, or no tensor, before the library is called."""
+    torch = pytest.importorskip("torch")
+    from paper_2608_23463_gb300 import local
+    bf, bad = torch.bfloat16, pf.PF_ERR_INVALID_ARG
+    q, k = torch.zeros(8, 256, dtype=bf), torch.zeros(8, 128, dtype=bf)
+    rope, att = local.QKRope(4, 2, 64), local.WindowAttention(1, 8, 4, 2)
+    for x in (q, q.float(), q[:, :128], q[0], None, 7):
+        refused(bad, rope.forward, x, k)
+        refused(bad, rope.backward, x, k, q, k)
+        refused(bad, att.forward, x, k, k)
+        refused(bad, att.backward, x, k, k, q, q)
+    refused(bad, local.QKRope, 4, 2, 64, torch.zeros(64))
+    refused(bad, lambda: local.PagedKVCache(1, 4, 2, 64, 16, 4, 2, device="cpu"))
+    with pytest.raises(TypeError):
+        local._local.rope_fwd(1, 2)
