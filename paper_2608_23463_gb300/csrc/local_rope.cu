@@ -18,10 +18,10 @@
 // halves of two turned pairs side by side, and the second halves.  With few
 // tokens a token's heads are spread over several warps (`parts`): latency
 // counts there, and the sines made twice do not.
-// Measured: four images of 512 x 512 tokens, 8 + 8 heads of 64, 704 us (6.1
-// TB/s, 90 % of a plain copy); backward, 65536 tokens of 16 + 4 heads, 101 us
-// (5.0 TB/s); eight prompts of 11738 tokens in all, 16 + 2 heads of 128, into
-// the cache 25.7 us (4.7 TB/s).  Scalar arithmetic with the weights applied
+// Measured: four images of 512 x 512 tokens, 8 + 8 heads of 64, 694 us (6.2
+// TB/s, 91 % of a plain copy); backward, 65536 tokens of 16 + 4 heads, 97 us
+// (5.2 TB/s); eight prompts of 11738 tokens in all, 16 + 2 heads of 128, into
+// the cache 25.5 us (4.7 TB/s).  Scalar arithmetic with the weights applied
 // apart took 843 us for the images, three quarters of the issue slots busy.
 //
 // Angles: the frequency is held as a 64-bit fraction of a turn, and
@@ -29,6 +29,7 @@
 // loses nothing, where a product in fp32 would be off by 0.06 radians.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "local.h"
 
@@ -41,9 +42,10 @@ namespace {
 
 constexpr int RW_THREADS = 256;
 constexpr int RW_WARPS = RW_THREADS / 32;
-// Resident CTAs an SM and heads in flight per lane.  Forward, four images of 512 x 512 tokens and 8 + 8
-// heads of 64: 704 us so, 757 with 4 CTAs and 4 heads, 909 with 3 and 8.  Backward, 65536 tokens of
-// 16 + 4 heads: 101 us so, 108 with 4 CTAs, 110 with 3 and one head.
+// Resident CTAs an SM and passes in flight per lane.  Forward, four images of 512 x 512 tokens and 8 + 8
+// heads of 64: 694 us so, 723 with 4 CTAs, 802 with one pass, 877 with three and 4 CTAs.  Backward,
+// 65536 tokens of 16 + 4 heads: 97 us so, 102 with 2 CTAs and four passes, 110 with one.  Rows asked into
+// L2 a token ahead: 799 and 103.
 constexpr int RW_FWD_CTAS = 5, RW_FWD_U = 2;
 constexpr int RW_BWD_CTAS = 3, RW_BWD_U = 2;
 constexpr int RW_MAX_PAIRS = 64;
@@ -186,6 +188,15 @@ __device__ __forceinline__ float head_sum(float v) {
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
+// n passes, U at a time without a branch between them, so that their shuffles overlap, and
+// what is left of them singly.
+template <int U, class F>
+__device__ __forceinline__ void in_passes(int n, F pass) {
+  for (; n >= U; n -= U) pass(std::integral_constant<int, U>{});
+  if (U > 1)
+    for (; n > 0; --n) pass(std::integral_constant<int, 1>{});
+}
+
 // Passes [p0, p1) of one token's heads (head p * HEADS + the lane's slot, below
 // nh), normed and turned: src + head * DH -> dst + head * dst_stride.
 template <class T, int DH>
@@ -193,7 +204,7 @@ __device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride
                                            int nh, const float2* w, bool norm, float eps,
                                            const float2* cs, const float2* sn, int lane) {
   using Ly = Lay<T, DH>;
-  constexpr int U = RW_FWD_U, G = Ly::G;
+  constexpr int G = Ly::G;
   const int sub = lane % Ly::LANES, slot = lane / Ly::LANES;
   // w folded into the turn: z_e = x_e (w_e c) - x_o (w_o s), z_o = x_e (w_e s) + x_o (w_o c)
   float2 ec[G], os[G], es[G], oc[G];
@@ -209,17 +220,17 @@ __device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride
   const T* sp = src + (long)h * DH + sub * Ly::N;
   T* dp = dst + h * dst_stride + sub * Ly::N;
   const long dstep = Ly::HEADS * dst_stride;
-  for (int p = p0; p < p1; p += U) {
+  auto pass = [&](auto count) {
+    constexpr int U = decltype(count)::value;
     uint4 u[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       u[i] = make_uint4(0, 0, 0, 0);
-      if (p + i < p1 && h + i * Ly::HEADS < nh)
+      if (h + i * Ly::HEADS < nh)
         u[i] = *reinterpret_cast<const uint4*>(sp + i * Ly::HEADS * DH);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (p + i >= p1) break;  // the same for every lane
       float2 e[G], o[G];
       Vec<T>::get(u[i], e, o);
       float r = 1.f;
@@ -244,7 +255,8 @@ __device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride
     h += U * Ly::HEADS;
     sp += U * Ly::HEADS * DH;
     dp += U * dstep;
-  }
+  };
+  in_passes<RW_FWD_U>(p1 - p0, pass);
 }
 
 // Forward (APPEND: keys and values go to their cache pages).  A unit is part
@@ -334,7 +346,7 @@ __device__ __forceinline__ void rope_heads_bwd(const T* x, const T* dz, T* dx, i
                                                const float2* cs, const float2* sn, float2* ge,
                                                float2* go, int lane) {
   using Ly = Lay<T, DH>;
-  constexpr int U = RW_BWD_U, G = Ly::G;
+  constexpr int G = Ly::G;
   const int sub = lane % Ly::LANES, slot = lane / Ly::LANES;
   int h = p0 * Ly::HEADS + slot;
   const long off = (long)h * DH + sub * Ly::N;
@@ -342,19 +354,19 @@ __device__ __forceinline__ void rope_heads_bwd(const T* x, const T* dz, T* dx, i
   dz += off;
   dx += off;
   w += sub * G * 2;
-  for (int p = p0; p < p1; p += U) {
+  auto pass = [&](auto count) {
+    constexpr int U = decltype(count)::value;
     uint4 ux[U], uz[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       ux[i] = uz[i] = make_uint4(0, 0, 0, 0);
-      if (p + i < p1 && h + i * Ly::HEADS < nh) {
+      if (h + i * Ly::HEADS < nh) {
         uz[i] = *reinterpret_cast<const uint4*>(dz + i * Ly::HEADS * DH);
         if (norm) ux[i] = *reinterpret_cast<const uint4*>(x + i * Ly::HEADS * DH);
       }
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (p + i >= p1) break;  // the same for every lane
       float2 ze[G], zo[G], ye[G], yo[G];
       Vec<T>::get(uz[i], ze, zo);
 #pragma unroll
@@ -391,7 +403,8 @@ __device__ __forceinline__ void rope_heads_bwd(const T* x, const T* dz, T* dx, i
     x += U * Ly::HEADS * DH;
     dz += U * Ly::HEADS * DH;
     dx += U * Ly::HEADS * DH;
-  }
+  };
+  in_passes<RW_BWD_U>(p1 - p0, pass);
 }
 
 template <class T, int DH>
