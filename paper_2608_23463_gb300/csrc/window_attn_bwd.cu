@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(x_full + 8 * i, 1);
-      mbar_init(x_empty + 8 * i, 1);
+      mbar_init(x_empty + 8 * i, 1 + WB_ROW_THREADS / 32);
     }
     mbar_init(t_full, 1);
     mbar_init(t_free, WB_ROW_THREADS / 32);  // one arrival per row warp
@@ -266,7 +266,8 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     bool ok = true;
     for (uint32_t it = 0; ok; ++it) {
       const uint32_t xb = it & 1;
-      // (four slots: the row warps may be an item behind the products that freed X)
+      // (the row warps have begun item it - 2 too: its phase of x_full is not passed over, and
+      // the slot is not that of the item before it, whose sums they may still be storing)
       if (!wait_warp(x_empty + 8 * xb, ((it >> 1) & 1) ^ 1)) break;
       if (lane == 0) {
         ring[it & 3] = m;
@@ -428,6 +429,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     for (uint32_t it = 0; ok; ++it) {
       if (!wait_warp(x_full + 8 * (it & 1), (it >> 1) & 1)) break;
       const WbItem m = ring[it & 3];
+      mbar_arrive_warp(x_empty + 8 * (it & 1));
       if (m.n < 0) {  // the last item's sums
         if (it > 0 && wait_warp(e_free, (G & 1) ^ 1)) {
           tc_fence_after();
