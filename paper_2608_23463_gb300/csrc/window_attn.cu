@@ -21,12 +21,19 @@
 // What bounds it: the chain of one softmax warp through a tile (about 430
 // instructions, two such warps on each scheduler), beside 1024 cycles of MMAs
 // and as many of exponentials for a pair of tiles.  262144 tokens of 16 heads on
-// 4, window 4096: 4.49 ms (0.99 PFLOP/s), timed with parts left out: 2.74 with
-// no arithmetic, 4.07 without the maxima, 3.55 without the exponentials.  One
-// MMA issuer for both tiles, which makes each wait for the other's softmax, and
-// key tiles tested one by one: 5.06; two threads to a row (sixteen softmax
-// warps): 5.27; chunks of 64 keys in two buffers a tile that P shares with the
-// scores: 5.50; O read out in the next item's first step: 5.03.
+// 4, window 4096: 4.25 ms (1.04 PFLOP/s).  What shortened the chain: maxima of
+// the first half of the scores while the second comes from TMEM, P stored from
+// its half on, and a loop of its own for tiles without masked keys (4.50
+// without the three; 4.39 with the loop alone, 4.34 with it and either).
+// As it was at 4.50, with parts left out: 2.74 with no arithmetic, 4.07 without
+// the maxima, 3.55 without the exponentials.  Tried then: one MMA issuer for both
+// tiles, which makes each wait for the other's softmax, and key tiles tested one
+// by one: 5.06; two threads to a row (sixteen softmax warps): 5.27; chunks of 64
+// keys in two buffers a tile that P shares with the scores: 5.50; O read out in
+// the next item's first step: 5.03.
+// A sinks' tile before the window that holds WT_FEW sinks at most is worked off
+// as a tile of so many keys: 65536 tokens of 16 heads, window 1024, 4 sinks 448
+// us without, 422 with it (411 now).
 // A row's probabilities are taken against a reference m, the maximum of the
 // first tile in which the row sees a key, raised only when a later tile's
 // maximum exceeds it by more than WA_RESCALE (log2 units); then O and the sum
@@ -38,6 +45,7 @@
 // anything; P = 0 meets its V in the MMA, so values must be finite up to the
 // end of the tile that a row sees.
 #include <algorithm>
+#include <type_traits>
 
 #include "local.h"
 #include "window_tiles.cuh"
@@ -107,12 +115,14 @@ struct WaItem {
 // B's diagonal.
 struct WaSteps {
   int a0, a1, a2;
+  int few;  // the step of the few sinks' tile, or -1
   __device__ __forceinline__ WaSteps(const WaArgs& a, const WaItem& m, int t) {
     const int gap = max(m.lo, a.w.sT);  // first tile that only the window can show
     a1 = m.ns + max(a.w.lo(t) - m.lo, 0);
     a0 = min(m.ns + gap - m.lo, a1);
     a2 = t < a.w.n_t ? m.ns + t - m.lo + 1 : 0;
     if (t >= a.w.n_t) a0 = a1 = 0;
+    few = a.w.few >= a.w.lo(t) ? -1 : a.w.few < m.ns ? a.w.few : m.ns + a.w.few - m.lo;
   }
 };
 
@@ -218,7 +228,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
       // ------------------------------------------------------------ MMA issuers
       // The whole warp runs the loop; one elected lane issues and commits.
       const int w = warp - 1;
-      constexpr uint32_t idesc_s = idesc_bf16_f32(WT, WT, 0, 0);
+      constexpr uint32_t idesc_s = idesc_bf16_f32(WT, WT, 0, 0), idesc_few = idesc_bf16_f32(WT, WT_FEW, 0, 0);
       constexpr uint32_t idesc_o = idesc_bf16_f32(WT, WA_D, 0, 1);
       const uint32_t tS = tmem + 128 * w, tO = tmem + WA_TM_O + 64 * w, tP = tmem + WA_TM_P + 64 * w;
       const uint64_t dq0 = smem_desc_sw128(sbase + w * WA_T_BYTES, 16, 1024);
@@ -229,7 +239,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
       uint32_t gs = 0;  // score products so far; those of P V are one behind
       uint32_t io = 0;  // items so far
       // O (+)= P V of the tile in stage st, the group's product gp
-      auto issue_pv = [&](uint32_t st, uint32_t gp, bool first, bool last) -> bool {
+      auto issue_pv = [&](uint32_t st, uint32_t gp, bool few, bool first, bool last) -> bool {
         if (!wait_warp(p_full(w), gp & 1)) return false;
         if (first && io > 0 && !wait_warp(o_free(w), (io - 1) & 1)) return false;
         tc_fence_after();
@@ -237,7 +247,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < WT / 16; ++kk)
-            tc_mma_f16_ts(tO, tP + kk * 8, dv + kk * (2048 >> 4), idesc_o, (!first || kk > 0) ? 1u : 0u);
+            if (kk < WT_FEW / 16 || !few) tc_mma_f16_ts(tO, tP + kk * 8, dv + kk * (2048 >> 4), idesc_o, (!first || kk > 0) ? 1u : 0u);
           tc_commit(p_free(w));
           tc_commit(kv_empty + 8 * st);
           if (last) tc_commit(o_full(w));
@@ -253,6 +263,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
         if (!wait_warp(q_full + 8 * qb, (it >> 1) & 1)) break;
         const uint64_t dq = dq0 + qb * (2 * WA_T_BYTES >> 4);
         uint32_t before = 0, seen = 0;  // stage of the tile before, tiles so far
+        bool few_before = false;
         int j = 0;
         for (; j < m.n; ++j) {
           const uint32_t st = (G + j) % WA_STAGES;
@@ -266,15 +277,18 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
           if (gs > 0 && !wait_warp(s_free(w), (gs - 1) & 1)) break;
           tc_fence_after();
           const uint64_t dk = dk0 + st * STEP;
+          const bool few = j == sp.few;
+          const uint32_t idesc = few ? idesc_few : idesc_s;
           if (elect_one()) {
 #pragma unroll
             for (int kk = 0; kk < WA_D / 16; ++kk)
-              tc_mma_f16(tS, dq + kk * 2, dk + kk * 2, idesc_s, kk ? 1u : 0u);
+              tc_mma_f16(tS, dq + kk * 2, dk + kk * 2, idesc, kk ? 1u : 0u);
             tc_commit(s_full(w));
           }
           __syncwarp();
-          if (seen > 0 && !issue_pv(before, gs - 1, seen == 1, false)) break;
+          if (seen > 0 && !issue_pv(before, gs - 1, few_before, seen == 1, false)) break;
           before = st;
+          few_before = few;
           ++seen;
           ++gs;
         }
@@ -282,7 +296,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
         if (elect_one()) tc_commit(q_empty + 8 * qb);
         __syncwarp();
         if (seen > 0) {
-          if (!issue_pv(before, gs - 1, seen == 1, true)) break;
+          if (!issue_pv(before, gs - 1, few_before, seen == 1, true)) break;
           ++io;
         }
         G += m.n;
@@ -310,48 +324,68 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
       // lie partly before some row's window and are not all sinks
       const int lo = a.w.lo(t), ns = min(a.w.sT, lo), whole = a.w.S / WT;
       const int past = t * WT + WT - 1 - a.w.W, clear = past >= 0 ? past / WT + 1 : 0;
+      const int few = a.w.few < lo ? a.w.few : -1;  // the few sinks' tile
       float mref = -INFINITY, l = 0.f;
-      for (int kt = ns > 0 ? 0 : lo; kt <= t; kt = kt + 1 == ns ? lo : kt + 1, ++g) {
-        if (!wait_warp(s_full(w), g & 1)) {
-          ok = false;
-          break;
-        }
+      // tile kt, of which the rows see none but its first NC keys
+      auto step = [&](auto cols, auto masked, int kt) -> bool {
+        constexpr int NC = decltype(cols)::value;
+        if (!wait_warp(s_full(w), g & 1)) return false;
         tc_fence_after();
-        // the scores into registers; then the next may replace them
-        uint32_t sc[128];
+        // the scores into registers, the first half's maxima while the second comes; then the
+        // next may replace them
+        uint32_t sc[NC];
+        float mx[8];
+        auto maxima = [&](int c0) {
 #pragma unroll
-        for (int c = 0; c < 128; c += 32) tmem_ld32_async(ts + c, sc + c);
+          for (int c = c0; c < c0 + NC / 2; c += 16)
 #pragma unroll
-        for (int c = 0; c < 128; c += 32) tmem_wait_ld(sc + c);
+            for (int e = 0; e < 8; ++e)
+              mx[e] = c == 0 ? fmaxf(__uint_as_float(sc[2 * e]), __uint_as_float(sc[2 * e + 1]))
+                             : max3f(mx[e], __uint_as_float(sc[c + 2 * e]), __uint_as_float(sc[c + 2 * e + 1]));
+        };
+        constexpr bool HALVES = !decltype(masked)::value;  // (with masks too: 4.39 ms)
+        if (HALVES) {
+          tmem_ld32_async(ts, sc);
+          tmem_ld32_async(ts + 32, sc + 32);
+          tmem_wait_ld(sc);
+          tmem_wait_ld(sc + 32);
+          tmem_ld32_async(ts + 64, sc + 64);
+          tmem_ld32_async(ts + 96, sc + 96);
+          maxima(0);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) asm volatile("" : "+f"(mx[e]));
+          tmem_wait_ld(sc + 64);
+          tmem_wait_ld(sc + 96);
+        } else {
+#pragma unroll
+          for (int c = 0; c < NC; c += 32) tmem_ld32_async(ts + c, sc + c);
+#pragma unroll
+          for (int c = 0; c < NC; c += 32) tmem_wait_ld(sc + c);
+        }
         tc_fence_before();
         mbar_arrive_warp(s_free(w));
-        if (kt < clear || kt == t) {
+        if (NC < WT) {
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            if (c >= a.w.S - kt * WT) sc[c] = 0xff800000u;  // -inf
+        } else if (decltype(masked)::value) {
           if (kt == t) {  // the diagonal
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
+            for (int c = 0; c < NC; ++c)
               if (c > r) sc[c] = 0xff800000u;  // -inf
           }
           if (kt < clear && kt >= whole) {  // keys that the window has passed
             const int low = q - a.w.W + 1 - kt * WT, sk = a.w.S - kt * WT;
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
+            for (int c = 0; c < NC; ++c)
               if (c < low && c >= sk) sc[c] = 0xff800000u;
           }
         }
         // the maximum (log2 units), three-input maxima
-        float mt;
-        {
-          float mx[8];
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-            mx[c] = fmaxf(__uint_as_float(sc[2 * c]), __uint_as_float(sc[2 * c + 1]));
-#pragma unroll
-          for (int c = 16; c < 128; c += 16)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              mx[e] = max3f(mx[e], __uint_as_float(sc[c + 2 * e]), __uint_as_float(sc[c + 2 * e + 1]));
-          mt = max3f(max3f(mx[0], mx[1], mx[2]), max3f(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * a.sl2;
-        }
+        if (!HALVES) maxima(0);
+        maxima(NC / 2);
+        const float mt =
+            max3f(max3f(mx[0], mx[1], mx[2]), max3f(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * a.sl2;
         // the first keys set the reference; later ones raise it only by more than
         // WA_RESCALE, scaling O and the running sum
         if (__any_sync(0xffffffffu, mt > mref + WA_RESCALE)) {
@@ -361,10 +395,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
             mref = mt;
           }
           if (__any_sync(0xffffffffu, corr != 1.f)) {  // this warp's rows of O
-            if (!wait_warp(p_free(w), (g - 1) & 1)) {
-              ok = false;
-              break;
-            }
+            if (!wait_warp(p_free(w), (g - 1) & 1)) return false;
             tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < 64; c += 16) {
@@ -382,9 +413,10 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
         const float ref = mref == -INFINITY ? 0.f : mref;
         const float2 nm = make_float2(-ref, -ref);
         float2 ps[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        uint32_t pk[64];
+        uint32_t pk[NC / 2];
+        constexpr int OUT = NC < WT ? 0 : 2;  // P goes out from this quarter on (from 1: 4.28 ms, from 3: 4.35)
 #pragma unroll
-        for (int hh = 0; hh < 4; ++hh) {
+        for (int hh = 0; hh < NC / 32; ++hh) {
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
             const float2 z = __ffma2_rn(make_float2(__uint_as_float(sc[32 * hh + 2 * c]),
@@ -394,19 +426,34 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
             ps[c & 1] = __fadd2_rn(ps[c & 1], pp);
             pk[16 * hh + c] = pack_bf16(pp.x, pp.y);
           }
-        }
-        // the last tile's P has been consumed
-        if (g > 0 && !wait_warp(p_free(w), (g - 1) & 1)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
+          if (hh == OUT) {  // the last tile's P has been consumed
+            if (g > 0 && !wait_warp(p_free(w), (g - 1) & 1)) return false;
+            tc_fence_after();
+          }
+          if (hh >= OUT)
 #pragma unroll
-        for (int c = 0; c < 64; c += 16) tmem_st16(tp + c, pk + c);
+            for (int c = hh == OUT ? 0 : 16 * hh; c <= 16 * hh; c += 16) tmem_st16(tp + c, pk + c);
+        }
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive_warp(p_full(w));
         l += (ps[0].x + ps[0].y) + (ps[1].x + ps[1].y);
+        ++g;
+        return true;
+      };
+      // (one place each for tiles with and without masks: two of the first, and smaller cases
+      // wait for instructions, 1 us of 33 for 2 x 1000 tokens)
+      const std::integral_constant<int, WT> all{};
+      int kt = ns > 0 ? 0 : lo;
+#pragma unroll 1
+      for (;;) {
+#pragma unroll 1
+        for (; ok && (kt < clear || kt == t); kt = kt + 1 == ns ? lo : kt + 1)
+          ok = kt == few ? step(std::integral_constant<int, WT_FEW>{}, std::true_type{}, kt)
+                         : step(all, std::true_type{}, kt);
+        if (!ok || kt > t) break;
+#pragma unroll 1
+        for (; ok && kt < t; ++kt) ok = step(all, std::false_type{}, kt);
       }
       if (!ok) break;
       // the item's O: after its last P.V

@@ -7,10 +7,12 @@
 namespace pf {
 
 constexpr int WT = 128;  // rows of a tile
+constexpr int WT_FEW = 32;  // so few sinks of a tile before the window are a narrower tile
 
 struct WinTiles {
   int L, W, S;  // length; window (L: no limit); sinks below the window
   int n_t, sT;  // tiles of the sequence, and those that hold sinks
+  int few;      // the last of those if it holds WT_FEW sinks at most, else -1
   WinTiles() = default;
   explicit WinTiles(const Window& c) {
     L = c.L;
@@ -18,6 +20,7 @@ struct WinTiles {
     S = W < L ? (c.sinks < L ? c.sinks : L) : 0;  // a window of everything holds the sinks
     n_t = (L + WT - 1) / WT;
     sT = (S + WT - 1) / WT;
+    few = sT > 0 && S - (sT - 1) * WT <= WT_FEW ? sT - 1 : -1;
   }
   // first tile of the window of query tile t
   __host__ __device__ __forceinline__ int lo(int t) const {
