@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     constexpr uint64_t TILE = WB_T_BYTES >> 4;  // in a descriptor's units
     bool ok = true;
     uint32_t it = 0, G = 0;
-    // accumulate step G (local step j of its item): E_G times the step's Y tiles
+    // accumulates step G_, its item's first or not: E times the step's Y tiles
     auto acc_step = [&](uint32_t G_, bool first) -> bool {
       const uint32_t st = G_ % WB_STAGES;
       if (!wait_warp(e_full, G_ & 1)) return false;
@@ -343,11 +343,15 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       __syncwarp();
       return true;
     };
-    for (;; ++it) {
+    bool first = false;  // step G - 1 is its item's first
+    for (; ok; ++it) {
       const uint32_t xb = it & 1;
       if (!wait_warp(x_full + 8 * xb, (it >> 1) & 1)) break;
       const int n = ring[it & 3].n;
-      if (n < 0) break;
+      if (n < 0) {
+        if (G > 0) acc_step(G - 1, first);
+        break;
+      }
       tc_fence_after();
       const uint64_t d1 = dx0 + xb * 2 * TILE, d2 = d1 + TILE;
       for (int j = 0; j < n; ++j, ++G) {
@@ -372,12 +376,13 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
           if (j == n - 1) tc_commit(x_empty + 8 * xb);
         }
         __syncwarp();
-        if (j > 0 && !acc_step(G - 1, j == 1)) {
+        // (an item's last step too: its products are issued behind the next item's first T)
+        if (G > 0 && !acc_step(G - 1, first)) {
           ok = false;
           break;
         }
+        first = j == 0;
       }
-      if (!ok || !acc_step(G - 1, n == 1)) break;
     }
     if (elect_one()) tc_commit(done);
     __syncwarp();
