@@ -19,9 +19,12 @@
 // in three bf16 each (24 bits).  From shared memory every thread read both for each of
 // its columns, 128 KB a step at 128 bytes a cycle, and a producer warp staged them: 520
 // us for 16384 causal tokens of 8 heads, of which 106 for the reads alone.
-// Roles: warp 0 TMA producer, warp 1 MMA issuer, warps 4-19 the row warps: four per
-// TMEM lane quarter, each thread one row (TMEM lane) and one quarter of the 128
-// streamed columns.
+// Roles: warp 0 TMA producer, warp 1 MMA issuer of T, warp 2 MMA issuer of the sums, warps
+// 4-19 the row warps: four per TMEM lane quarter, each thread one row (TMEM lane) and
+// one quarter of the 128 streamed columns.  (One issuer for both took 700 cycles for T and
+// 900 to 1200 for the sums of a step, more than their MMAs: it shares its scheduler with
+// four row warps.  65536 tokens of 16 heads, window 1024: dK and dV 601 us with it, 493
+// so; dQ 453 and 444.)
 // The sinks are seen by every later query: their key tiles' steps are cut into
 // pieces (wb_cut), as are all tiles' where there are few.  The pieces of a cut
 // tile leave fp32 sums, those past its window of the sinks' rows alone;
@@ -203,7 +206,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(x_full + 8 * i, 1);
-      mbar_init(x_empty + 8 * i, 1 + WB_ROW_THREADS / 32);
+      mbar_init(x_empty + 8 * i, 2 + WB_ROW_THREADS / 32);
     }
     mbar_init(t_full, 1);
     mbar_init(t_free, WB_ROW_THREADS / 32);  // one arrival per row warp
@@ -213,7 +216,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       mbar_init(y_full + 8 * i, 1);
       mbar_init(y_empty + 8 * i, 1);
     }
-    mbar_init(done, 1);
+    mbar_init(done, 2);
     fence_barrier_init();
   }
   if (DKDV) {
@@ -266,8 +269,8 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     bool ok = true;
     for (uint32_t it = 0; ok; ++it) {
       const uint32_t xb = it & 1;
-      // (the row warps have begun item it - 2 too: its phase of x_full is not passed over, and
-      // the slot is not that of the item before it, whose sums they may still be storing)
+      // (the row warps and the sums' issuer have begun item it - 2 too: its phase of x_full is not
+      // passed over, and the slot is not that of the item before it, whose sums they may still store)
       if (!wait_warp(x_empty + 8 * xb, ((it >> 1) & 1) ^ 1)) break;
       if (lane == 0) {
         ring[it & 3] = m;
@@ -307,52 +310,21 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       m = m2;
     }
   } else if (warp == 1) {
-    // ------------------------------------------------------------ MMA issuer
+    // ------------------------------------------------------------ MMA issuer: T
     // The whole warp runs the loop; one elected lane issues and commits.
-    constexpr uint32_t idesc_t = idesc_bf16_f32(WT, WT, 0, 0);
-    constexpr uint32_t idesc_a = idesc_bf16_f32(WT, WB_D, 0, 1);
+    constexpr uint32_t idesc = idesc_bf16_f32(WT, WT, 0, 0);
     const WbItem* const ring = reinterpret_cast<const WbItem*>(smem + WB_OFF_ITEM);
     const uint64_t dx0 = smem_desc_sw128(sbase, 16, 1024);
     const uint64_t dy0 = smem_desc_sw128(sbase + WB_OFF_Y, 16, 1024);
-    const uint64_t da0 = smem_desc_sw128(sbase + WB_OFF_Y, 8192, 1024);
     const uint64_t de0 = smem_desc_sw32(sbase + WB_OFF_E), one = smem_desc_sw32(sbase + WB_OFF_ONE);
     constexpr uint64_t TILE = WB_T_BYTES >> 4;  // in a descriptor's units
     bool ok = true;
-    uint32_t it = 0, G = 0;
-    // accumulates step G_, its item's first or not: E times the step's Y tiles
-    auto acc_step = [&](uint32_t G_, bool first) -> bool {
-      const uint32_t st = G_ % WB_STAGES;
-      if (!wait_warp(e_full, G_ & 1)) return false;
-      tc_fence_after();
-      const uint32_t e1 = tmem + WB_TM_E, e2 = e1 + WT / 2;
-      const uint64_t d1 = da0 + st * 2 * TILE, d2 = d1 + TILE;
-      if (elect_one()) {
-#pragma unroll
-        for (int kk = 0; kk < WT / 16; ++kk) {
-          const uint32_t acc = (!first || kk > 0) ? 1u : 0u;
-          if (DKDV) {
-            tc_mma_f16_ts(tmem + 256, e1 + kk * 8, d2 + kk * (2048 >> 4), idesc_a, acc);  // dV += P^T dO
-            tc_mma_f16_ts(tmem + 320, e2 + kk * 8, d1 + kk * (2048 >> 4), idesc_a, acc);  // dK += dS^T Q
-          } else {
-            tc_mma_f16_ts(tmem + 256, e2 + kk * 8, d1 + kk * (2048 >> 4), idesc_a, acc);  // dQ += dS K
-          }
-        }
-        tc_commit(e_free);
-        tc_commit(y_empty + 8 * st);
-      }
-      __syncwarp();
-      return true;
-    };
-    bool first = false;  // step G - 1 is its item's first
-    for (; ok; ++it) {
+    uint32_t G = 0;
+    for (uint32_t it = 0; ok; ++it) {
       const uint32_t xb = it & 1;
       if (!wait_warp(x_full + 8 * xb, (it >> 1) & 1)) break;
       const int n = ring[it & 3].n;
-      if (n < 0) {
-        if (G > 0) acc_step(G - 1, first);
-        break;
-      }
-      tc_fence_after();
+      if (n < 0) break;
       const uint64_t d1 = dx0 + xb * 2 * TILE, d2 = d1 + TILE;
       for (int j = 0; j < n; ++j, ++G) {
         const uint32_t st = G % WB_STAGES;
@@ -365,23 +337,60 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < WB_D / 16; ++kk) {
-            tc_mma_f16(tmem, d1 + kk * 2, y1 + kk * 2, idesc_t, kk ? 1u : 0u);
-            tc_mma_f16(tmem + WT, d2 + kk * 2, y2 + kk * 2, idesc_t, kk ? 1u : 0u);
+            tc_mma_f16(tmem, d1 + kk * 2, y1 + kk * 2, idesc, kk ? 1u : 0u);
+            tc_mma_f16(tmem + WT, d2 + kk * 2, y2 + kk * 2, idesc, kk ? 1u : 0u);
           }
           if (DKDV) {
-            tc_mma_f16(tmem, one, ye, idesc_t, 1u);
-            tc_mma_f16(tmem + WT, one + (WB_E_BYTES >> 4), ye, idesc_t, 1u);
+            tc_mma_f16(tmem, one, ye, idesc, 1u);
+            tc_mma_f16(tmem + WT, one + (WB_E_BYTES >> 4), ye, idesc, 1u);
           }
           tc_commit(t_full);
           if (j == n - 1) tc_commit(x_empty + 8 * xb);
         }
         __syncwarp();
-        // (an item's last step too: its products are issued behind the next item's first T)
-        if (G > 0 && !acc_step(G - 1, first)) {
+      }
+    }
+    if (elect_one()) tc_commit(done);
+    __syncwarp();
+  } else if (warp == 2) {
+    // ------------------------------------------------------------ MMA issuer: sums
+    constexpr uint32_t idesc = idesc_bf16_f32(WT, WB_D, 0, 1);
+    const WbItem* const ring = reinterpret_cast<const WbItem*>(smem + WB_OFF_ITEM);
+    const uint64_t da0 = smem_desc_sw128(sbase + WB_OFF_Y, 8192, 1024);
+    constexpr uint64_t TILE = WB_T_BYTES >> 4;
+    const uint32_t e1 = tmem + WB_TM_E, e2 = e1 + WT / 2;
+    bool ok = true;
+    uint32_t G = 0;
+    for (uint32_t it = 0; ok; ++it) {
+      const uint32_t xb = it & 1;
+      if (!wait_warp(x_full + 8 * xb, (it >> 1) & 1)) break;
+      const int n = ring[it & 3].n;
+      mbar_arrive_warp(x_empty + 8 * xb);
+      if (n < 0) break;
+      for (int j = 0; j < n; ++j, ++G) {
+        const uint32_t st = G % WB_STAGES;
+        // (the row warps have E from T, and T's products Y: the wait for Y is for this warp's sake)
+        if (!wait_warp(y_full + 8 * st, (G / WB_STAGES) & 1) || !wait_warp(e_full, G & 1)) {
           ok = false;
           break;
         }
-        first = j == 0;
+        tc_fence_after();
+        const uint64_t d1 = da0 + st * 2 * TILE, d2 = d1 + TILE;
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < WT / 16; ++kk) {
+            const uint32_t acc = (j > 0 || kk > 0) ? 1u : 0u;
+            if (DKDV) {
+              tc_mma_f16_ts(tmem + 256, e1 + kk * 8, d2 + kk * (2048 >> 4), idesc, acc);  // dV += P^T dO
+              tc_mma_f16_ts(tmem + 320, e2 + kk * 8, d1 + kk * (2048 >> 4), idesc, acc);  // dK += dS^T Q
+            } else {
+              tc_mma_f16_ts(tmem + 256, e2 + kk * 8, d1 + kk * (2048 >> 4), idesc, acc);  // dQ += dS K
+            }
+          }
+          tc_commit(e_free);
+          tc_commit(y_empty + 8 * st);
+        }
+        __syncwarp();
       }
     }
     if (elect_one()) tc_commit(done);
