@@ -13,9 +13,11 @@
 //   warp 0    TMA producer: the item's two Q tiles (double-buffered across
 //             items) and a WA_STAGES-deep ring of (K, V) 128-key tiles, shared
 //             by both query tiles; rows past the end of a sequence read as zero
-//   warps 1-2 MMA issuers of tile A and tile B: S = Q K_j^T (M=128, N=128, K=64)
+//   warp 1    MMA issuer of both tiles' scores: S = Q K_j^T (M=128, N=128, K=64)
 //             into the tile's TMEM score buffer as soon as its last scores are
-//             in registers, O += P V_j (M=128, N=64, K=128) with P from TMEM
+//             in registers
+//   warps 2-3 MMA issuers of tile A's and tile B's O += P V_j (M=128, N=64,
+//             K=128), P from TMEM
 //   warps 4-7 softmax of tile A, warps 8-11 of tile B: one query row per thread
 //             (TMEM lane), its 128 scores in registers; P goes back to TMEM
 // What bounds it: the chain of one softmax warp through a tile (about 430
@@ -33,7 +35,8 @@
 // the next item's first step: 5.03.
 // A sinks' tile before the window that holds WT_FEW sinks at most is worked off
 // as a tile of so many keys: 65536 tokens of 16 heads, window 1024, 4 sinks 448
-// us without, 422 with it (411 now).
+// us without, 422 with it; 399 now, 411 with each tile's scores and O issued by
+// one warp.
 // A row's probabilities are taken against a reference m, the maximum of the
 // first tile in which the row sees a key, raised only when a later tile's
 // maximum exceeds it by more than WA_RESCALE (log2 units); then O and the sum
@@ -59,7 +62,7 @@ namespace {
 
 constexpr int WA_D = 64;  // head width
 constexpr int WA_STAGES = 4;
-constexpr int WA_THREADS = 384;  // producer, two MMA issuers, an idle warp, two groups of four
+constexpr int WA_THREADS = 384;  // producer, three MMA issuers, two groups of four
 // A softmax thread holds a row's 128 scores: the control warps give registers up, of the
 // 168 that each thread has at launch.
 constexpr int WA_REGS_CTRL = 88, WA_REGS_ROWS = 208;
@@ -163,7 +166,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full + 8 * i, 1);
-      mbar_init(q_empty + 8 * i, 2);  // one arrival per MMA issuer
+      mbar_init(q_empty + 8 * i, 1);
       mbar_init(s_full(i), 1);
       mbar_init(s_free(i), 4);  // one arrival per softmax warp of the tile
       mbar_init(p_full(i), 4);
@@ -173,9 +176,9 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
     }
     for (int i = 0; i < WA_STAGES; ++i) {
       mbar_init(kv_full + 8 * i, 1);
-      mbar_init(kv_empty + 8 * i, 2);  // one arrival per MMA issuer
+      mbar_init(kv_empty + 8 * i, 2);  // one arrival per tile
     }
-    mbar_init(done, 2);
+    mbar_init(done, 3);
     fence_barrier_init();
   }
   if (warp == 1) {
@@ -224,46 +227,65 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
           kv_issued = g + 1;
         }
       }
-    } else if (warp == 1 || warp == 2) {
-      // ------------------------------------------------------------ MMA issuers
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ MMA issuer: scores
       // The whole warp runs the loop; one elected lane issues and commits.
-      const int w = warp - 1;
       constexpr uint32_t idesc_s = idesc_bf16_f32(WT, WT, 0, 0), idesc_few = idesc_bf16_f32(WT, WT_FEW, 0, 0);
-      constexpr uint32_t idesc_o = idesc_bf16_f32(WT, WA_D, 0, 1);
-      const uint32_t tS = tmem + 128 * w, tO = tmem + WA_TM_O + 64 * w, tP = tmem + WA_TM_P + 64 * w;
-      const uint64_t dq0 = smem_desc_sw128(sbase + w * WA_T_BYTES, 16, 1024);
+      const uint64_t dq0 = smem_desc_sw128(sbase, 16, 1024);
       const uint64_t dk0 = smem_desc_sw128(sbase + WA_OFF_KV, 16, 1024);
-      const uint64_t dv0 = smem_desc_sw128(sbase + WA_OFF_KV + WA_T_BYTES, 8192, 1024);
       constexpr uint64_t STEP = 2 * WA_T_BYTES >> 4;  // a stage, in a descriptor's units
-      uint32_t G = 0;   // stages so far
-      uint32_t gs = 0;  // score products so far; those of P V are one behind
-      uint32_t io = 0;  // items so far
-      // O (+)= P V of the tile in stage st, the group's product gp
-      auto issue_pv = [&](uint32_t st, uint32_t gp, bool few, bool first, bool last) -> bool {
-        if (!wait_warp(p_full(w), gp & 1)) return false;
-        if (first && io > 0 && !wait_warp(o_free(w), (io - 1) & 1)) return false;
+      uint32_t G = 0;         // stages so far
+      uint32_t gs0 = 0, gs1 = 0;  // score products of the tiles so far
+      // tile w's scores of step j, if it takes part in it
+      auto scores = [&](int w, const WaSteps& sp, int j, uint64_t dq, uint64_t dk, uint32_t& gs) -> bool {
+        if (j >= sp.a2 || (j >= sp.a0 && j < sp.a1)) return true;
+        if (gs > 0 && !wait_warp(s_free(w), (gs - 1) & 1)) return false;
         tc_fence_after();
-        const uint64_t dv = dv0 + st * STEP;
+        const uint32_t idesc = j == sp.few ? idesc_few : idesc_s, tS = tmem + 128 * w;
         if (elect_one()) {
 #pragma unroll
-          for (int kk = 0; kk < WT / 16; ++kk)
-            if (kk < WT_FEW / 16 || !few) tc_mma_f16_ts(tO, tP + kk * 8, dv + kk * (2048 >> 4), idesc_o, (!first || kk > 0) ? 1u : 0u);
-          tc_commit(p_free(w));
-          tc_commit(kv_empty + 8 * st);
-          if (last) tc_commit(o_full(w));
+          for (int kk = 0; kk < WA_D / 16; ++kk)
+            tc_mma_f16(tS, dq + kk * 2, dk + kk * 2, idesc, kk ? 1u : 0u);
+          tc_commit(s_full(w));
         }
         __syncwarp();
+        ++gs;
         return true;
       };
       uint32_t it = 0;
       for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items; k = wa_rank(blockIdx.x, ++rd), ++it) {
         const WaItem m(a, k);
-        const WaSteps sp(a, m, 2 * m.u + w);
+        const WaSteps sa(a, m, 2 * m.u), sb(a, m, 2 * m.u + 1);
         const uint32_t qb = it & 1;
         if (!wait_warp(q_full + 8 * qb, (it >> 1) & 1)) break;
-        const uint64_t dq = dq0 + qb * (2 * WA_T_BYTES >> 4);
-        uint32_t before = 0, seen = 0;  // stage of the tile before, tiles so far
-        bool few_before = false;
+        const uint64_t dqa = dq0 + qb * (2 * WA_T_BYTES >> 4), dqb = dqa + (WA_T_BYTES >> 4);
+        int j = 0;
+        for (; j < m.n; ++j) {
+          const uint32_t st = (G + j) % WA_STAGES;
+          if (!wait_warp(kv_full + 8 * st, ((G + j) / WA_STAGES) & 1)) break;
+          const uint64_t dk = dk0 + st * STEP;
+          if (!scores(0, sa, j, dqa, dk, gs0) || !scores(1, sb, j, dqb, dk, gs1)) break;
+        }
+        if (j < m.n) break;  // a wait ran out
+        if (elect_one()) tc_commit(q_empty + 8 * qb);
+        __syncwarp();
+        G += m.n;
+      }
+      if (elect_one()) tc_commit(done);
+      __syncwarp();
+    } else if (warp >= 2) {
+      // ------------------------------------------------------------ MMA issuers: O of tiles A, B
+      const int w = warp - 2;
+      constexpr uint32_t idesc_o = idesc_bf16_f32(WT, WA_D, 0, 1);
+      const uint32_t tO = tmem + WA_TM_O + 64 * w, tP = tmem + WA_TM_P + 64 * w;
+      const uint64_t dv0 = smem_desc_sw128(sbase + WA_OFF_KV + WA_T_BYTES, 8192, 1024);
+      constexpr uint64_t STEP = 2 * WA_T_BYTES >> 4;
+      uint32_t G = 0, gp = 0;  // stages, products so far
+      uint32_t io = 0;         // items so far
+      for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items; k = wa_rank(blockIdx.x, ++rd)) {
+        const WaItem m(a, k);
+        const WaSteps sp(a, m, 2 * m.u + w);
+        bool first = true;
         int j = 0;
         for (; j < m.n; ++j) {
           const uint32_t st = (G + j) % WA_STAGES;
@@ -274,31 +296,26 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
             __syncwarp();
             continue;
           }
-          if (gs > 0 && !wait_warp(s_free(w), (gs - 1) & 1)) break;
+          if (!wait_warp(p_full(w), gp & 1)) break;
+          if (first && io > 0 && !wait_warp(o_free(w), (io - 1) & 1)) break;
           tc_fence_after();
-          const uint64_t dk = dk0 + st * STEP;
+          const uint64_t dv = dv0 + st * STEP;
           const bool few = j == sp.few;
-          const uint32_t idesc = few ? idesc_few : idesc_s;
           if (elect_one()) {
 #pragma unroll
-            for (int kk = 0; kk < WA_D / 16; ++kk)
-              tc_mma_f16(tS, dq + kk * 2, dk + kk * 2, idesc, kk ? 1u : 0u);
-            tc_commit(s_full(w));
+            for (int kk = 0; kk < WT / 16; ++kk)
+              if (kk < WT_FEW / 16 || !few)
+                tc_mma_f16_ts(tO, tP + kk * 8, dv + kk * (2048 >> 4), idesc_o, (!first || kk > 0) ? 1u : 0u);
+            tc_commit(p_free(w));
+            tc_commit(kv_empty + 8 * st);
+            if (j == sp.a2 - 1) tc_commit(o_full(w));
           }
           __syncwarp();
-          if (seen > 0 && !issue_pv(before, gs - 1, few_before, seen == 1, false)) break;
-          before = st;
-          few_before = few;
-          ++seen;
-          ++gs;
+          first = false;
+          ++gp;
         }
         if (j < m.n) break;  // a wait ran out
-        if (elect_one()) tc_commit(q_empty + 8 * qb);
-        __syncwarp();
-        if (seen > 0) {
-          if (!issue_pv(before, gs - 1, few_before, seen == 1, true)) break;
-          ++io;
-        }
+        if (!first) ++io;
         G += m.n;
       }
       if (elect_one()) tc_commit(done);
