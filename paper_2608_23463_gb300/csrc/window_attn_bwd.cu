@@ -19,12 +19,12 @@
 // in three bf16 each (24 bits).  From shared memory every thread read both for each of
 // its columns, 128 KB a step at 128 bytes a cycle, and a producer warp staged them: 520
 // us for 16384 causal tokens of 8 heads, of which 106 for the reads alone.
-// Roles: warp 0 TMA producer, warp 1 MMA issuer of T, warp 2 MMA issuer of the sums, warps
-// 4-19 the row warps: four per TMEM lane quarter, each thread one row (TMEM lane) and
-// one quarter of the 128 streamed columns.  (One issuer for both took 700 cycles for T and
-// 900 to 1200 for the sums of a step, more than their MMAs: it shares its scheduler with
-// four row warps.  65536 tokens of 16 heads, window 1024: dK and dV 601 us with it, 493
-// so; dQ 453 and 444.)
+// Roles: warp 0 TMA producer, warp 1 MMA issuer of T, warp 2 MMA issuer of the sums, warp 3
+// their TMA stores, warps 4-19 the row warps: four per TMEM lane quarter, each thread one
+// row (TMEM lane) and one quarter of the 128 streamed columns.  (One issuer for both took
+// 700 cycles for T and 900 to 1200 for the sums of a step, more than their MMAs: it shares
+// its scheduler with four row warps.  65536 tokens of 16 heads, window 1024: dK and dV 601
+// us with it, 493 so; dQ 453 and 444.)
 // The sinks are seen by every later query: their key tiles' steps are cut into
 // pieces (wb_cut), as are all tiles' where there are few.  The pieces of a cut
 // tile leave fp32 sums, those past its window of the sinks' rows alone;
@@ -33,10 +33,18 @@
 // dealt to the CTAs in equal ranges instead: 65536 tokens of 16 heads on 4 key
 // heads, window 1024: 800 us, 664 so; a range's tiles are too far apart.)
 // An item's sums are read out in the next item's first step, when that step's E waits
-// for them anyway: no warp waits for the end of an item's products.
+// for them anyway: no warp waits for the end of an item's products.  They go out by TMA
+// from where the item's X was (a row's 32 bytes a thread, stored directly, held the first
+// step up by 1000 to 2000 cycles: dK and dV 493 us and dQ 444 so, 446 and 424 by TMA).
 // The producer alone works out the items; the others read them from shared memory and
 // count their steps up: what each step costs a warp beside its products and its 32
 // columns is on the chain of every step.
+// What bounds it: the chain of T's products (operands from shared memory at its 128 bytes a
+// cycle, beside 34 KB of TMA writes a step), their commit and the row warps' reads of T, 1500
+// to 1600 cycles a step, of which the MMAs take 1152 (DKDV) and 768 (DQ).  65536 tokens of 16
+// heads, window 1024, 4 sinks: dK and dV 446 us, dQ 424.  Not faster: T in halves of 64
+// columns or T1 and T2 handed over apart, so that the row warps' phases overlap; X in TMEM
+// for DQ; Di into DQ's T by an MMA; Di worked out by a warp of DQ; waits that probe.
 // Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the
 // end of a sequence read as zero.
 #include <algorithm>
@@ -56,7 +64,7 @@ constexpr int WB_EXT = 16;  // bf16 of a query's LSE and Di: three each, the res
 constexpr int WB_STAGES = 4;
 constexpr int WB_ROW_THREADS = 512;  // warps 4-19
 constexpr int WB_THREADS = 128 + WB_ROW_THREADS;
-// A row thread holds 64 values of a step: the control warps (two of them idle) give
+// A row thread holds 64 values of a step: the control warps give
 // registers up, of the 96 that each thread has at launch.
 constexpr int WB_REGS_CTRL = 64, WB_REGS_ROWS = 104;
 static_assert(WB_REGS_CTRL * 128 + WB_REGS_ROWS * 512 <= 96 * WB_THREADS, "register split");
@@ -75,7 +83,7 @@ constexpr uint32_t WB_TM_E = 384;
 constexpr int WB_ACC = 2 * WB_D;  // dV | dK of a key
 
 struct WbArgs {
-  bf16 *out_u, *out_w;  // DKDV: dV, dK; DQ: dQ.  Head h at column 64 h
+  bf16 *out_u, *out_w;  // window_join_kernel: dV, dK.  Head h at column 64 h
   long ld_u, ld_w;
   const float* lse;  // [B, H, L], log2 units
   const float* Di;   // [B, H, L]
@@ -186,19 +194,29 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
   return mbar_wait_warp(bar, parity);
 }
 
+// A tile of 64 columns and 128 rows (those past the end of the sequence are left out).
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t saddr, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+                   map),
+               "r"(x), "r"(y), "r"(z), "r"(saddr)
+               : "memory");
+}
+
 template <bool DKDV>
 __global__ void __launch_bounds__(WB_THREADS, 1)
     window_bwd_kernel(const __grid_constant__ CUtensorMap tmX1, const __grid_constant__ CUtensorMap tmX2,
                       const __grid_constant__ CUtensorMap tmY1, const __grid_constant__ CUtensorMap tmY2,
-                      const __grid_constant__ CUtensorMap tmE, WbArgs a) {
+                      const __grid_constant__ CUtensorMap tmE, const __grid_constant__ CUtensorMap tmU,
+                      const __grid_constant__ CUtensorMap tmW, WbArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   const uint32_t b0 = smem_u32(smem + WB_OFF_BAR);
-  // x_full[2] x_empty[2] y_full[S] y_empty[S] t_full t_free e_full e_free done
+  // x_full[2] x_empty[2] y_full[S] y_empty[S] t_full t_free e_full e_free done o_full
   const uint32_t x_full = b0, x_empty = b0 + 16, y_full = b0 + 32,
                  y_empty = y_full + 8 * WB_STAGES, t_full = y_empty + 8 * WB_STAGES,
-                 t_free = t_full + 8, e_full = t_free + 8, e_free = e_full + 8, done = e_free + 8;
+                 t_free = t_full + 8, e_full = t_free + 8, e_free = e_full + 8, done = e_free + 8,
+                 o_full = done + 8;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + WB_OFF_BAR + 240);
   const uint32_t sbase = smem_u32(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -206,7 +224,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(x_full + 8 * i, 1);
-      mbar_init(x_empty + 8 * i, 2 + WB_ROW_THREADS / 32);
+      mbar_init(x_empty + 8 * i, 3);  // both issuers, the sums' store
     }
     mbar_init(t_full, 1);
     mbar_init(t_free, WB_ROW_THREADS / 32);  // one arrival per row warp
@@ -217,6 +235,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       mbar_init(y_empty + 8 * i, 1);
     }
     mbar_init(done, 2);
+    mbar_init(o_full, WB_ROW_THREADS / 32);
     fence_barrier_init();
   }
   if (DKDV) {
@@ -269,8 +288,8 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     bool ok = true;
     for (uint32_t it = 0; ok; ++it) {
       const uint32_t xb = it & 1;
-      // (the row warps and the sums' issuer have begun item it - 2 too: its phase of x_full is not
-      // passed over, and the slot is not that of the item before it, whose sums they may still store)
+      // (item it - 2's sums have left this buffer: all have begun the item after it, no phase of
+      // x_full is passed over, and its slot is read no more)
       if (!wait_warp(x_empty + 8 * xb, ((it >> 1) & 1) ^ 1)) break;
       if (lane == 0) {
         ring[it & 3] = m;
@@ -395,6 +414,30 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
     }
     if (elect_one()) tc_commit(done);
     __syncwarp();
+  } else {
+    // ------------------------------------------------------------ store of the sums
+    // The row warps leave an item's dK and dV, or dQ, in the shared memory of its X, whose
+    // products are done.
+    const WbItem* const ring = reinterpret_cast<const WbItem*>(smem + WB_OFF_ITEM);
+    for (uint32_t it = 0;; ++it) {
+      const uint32_t xb = it & 1;
+      if (!wait_warp(x_full + 8 * xb, (it >> 1) & 1)) break;
+      if (ring[it & 3].n < 0 || !wait_warp(o_full, it & 1)) break;
+      if (lane == 0) {
+        const WbItem m = ring[it & 3];
+        if (m.piece < 0) {
+          const uint32_t src = sbase + xb * 2 * WB_T_BYTES;
+          tma_store_3d(&tmU, src, m.h * WB_D, m.t * WT, m.b);
+          if (DKDV) tma_store_3d(&tmW, src + WB_T_BYTES, m.h * WB_D, m.t * WT, m.b);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        }
+        mbar_arrive(x_empty + 8 * xb);
+      }
+      __syncwarp();
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    __syncwarp();
   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(WB_REGS_ROWS));
@@ -411,46 +454,48 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       tmem_ld16(tl + 256 + 16 * ch, v.u);
       if (DKDV) tmem_ld16(tl + 320 + 16 * ch, v.w);
     };
-    auto store_sums = [&](const WbItem& m, const Sums& sum) {  // dK, dV (DKDV) or dQ (DQ) rows
+    // item n's dV and dK (DKDV) or dQ to where warp 3 stores them from, or a piece's sums
+    auto store_sums = [&](uint32_t n, const Sums& sum) {
+      const WbItem& m = ring[n & 3];
       const uint32_t *u0 = sum.u, *w0 = sum.w;
-      const int row = m.t * WT + r;
-      if (row >= a.w.L) return;
-      const long srow = (long)m.b * a.w.L + row;
-      auto store = [&](bf16* o, const uint32_t* v, float sc) {
-#pragma unroll
-        for (int i = 0; i < 16; i += 8)
-          *reinterpret_cast<uint4*>(o + i) = make_uint4(
-              pack_bf16(__uint_as_float(v[i]) * sc, __uint_as_float(v[i + 1]) * sc),
-              pack_bf16(__uint_as_float(v[i + 2]) * sc, __uint_as_float(v[i + 3]) * sc),
-              pack_bf16(__uint_as_float(v[i + 4]) * sc, __uint_as_float(v[i + 5]) * sc),
-              pack_bf16(__uint_as_float(v[i + 6]) * sc, __uint_as_float(v[i + 7]) * sc));
-      };
       if (DKDV && m.piece >= 0) {  // sums of a cut tile
-        if (r >= m.rows) return;
-        float* o = a.part + ((long)m.piece * WT + r) * WB_ACC + 16 * ch;
+        if (r < m.rows && m.t * WT + r < a.w.L) {
+          float* o = a.part + ((long)m.piece * WT + r) * WB_ACC + 16 * ch;
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          *reinterpret_cast<uint4*>(o + i) = make_uint4(u0[i], u0[i + 1], u0[i + 2], u0[i + 3]);
-          *reinterpret_cast<uint4*>(o + WB_D + i) = make_uint4(w0[i], w0[i + 1], w0[i + 2], w0[i + 3]);
+          for (int i = 0; i < 16; i += 4) {
+            *reinterpret_cast<uint4*>(o + i) = make_uint4(u0[i], u0[i + 1], u0[i + 2], u0[i + 3]);
+            *reinterpret_cast<uint4*>(o + WB_D + i) = make_uint4(w0[i], w0[i + 1], w0[i + 2], w0[i + 3]);
+          }
         }
       } else {
-        store(a.out_u + srow * a.ld_u + m.h * WB_D + 16 * ch, u0, DKDV ? 1.f : a.scale);
-        if (DKDV) store(a.out_w + srow * a.ld_w + m.h * WB_D + 16 * ch, w0, a.scale);
+        uint8_t* const dst = smem + (n & 1) * 2 * WB_T_BYTES + r * 128;
+        auto put = [&](uint8_t* o, const uint32_t* v, float sc) {  // 128-byte swizzle
+#pragma unroll
+          for (int i = 0; i < 16; i += 8)
+            *reinterpret_cast<uint4*>(o + (((2 * ch + i / 8) ^ (r & 7)) << 4)) = make_uint4(
+                pack_bf16(__uint_as_float(v[i]) * sc, __uint_as_float(v[i + 1]) * sc),
+                pack_bf16(__uint_as_float(v[i + 2]) * sc, __uint_as_float(v[i + 3]) * sc),
+                pack_bf16(__uint_as_float(v[i + 4]) * sc, __uint_as_float(v[i + 5]) * sc),
+                pack_bf16(__uint_as_float(v[i + 6]) * sc, __uint_as_float(v[i + 7]) * sc));
+        };
+        put(dst, u0, DKDV ? 1.f : a.scale);
+        if (DKDV) put(dst + WB_T_BYTES, w0, a.scale);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // a TMA store reads them
       }
+      mbar_arrive_warp(o_full);
     };
     bool ok = true;
     uint32_t G = 0;
     for (uint32_t it = 0; ok; ++it) {
       if (!wait_warp(x_full + 8 * (it & 1), (it >> 1) & 1)) break;
       const WbItem m = ring[it & 3];
-      mbar_arrive_warp(x_empty + 8 * (it & 1));
       if (m.n < 0) {  // the last item's sums
         if (it > 0 && wait_warp(e_free, (G & 1) ^ 1)) {
           tc_fence_after();
           Sums v;
           load_sums(v);
           tc_fence_before();
-          store_sums(ring[(it - 1) & 3], v);
+          store_sums(it - 1, v);
         }
         break;
       }
@@ -547,7 +592,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
           Sums v;
           load_sums(v);
           put_e();
-          store_sums(ring[(it - 1) & 3], v);
+          store_sums(it - 1, v);
         } else {
           put_e();
         }
@@ -719,8 +764,9 @@ WbWs wb_carve(void* ws, const Window& c) {
 
 template <bool DKDV>
 cudaError_t wb_launch(const CUtensorMap& x1, const CUtensorMap& x2, const CUtensorMap& y1,
-                      const CUtensorMap& y2, const CUtensorMap& te, const WbArgs& a, const char* label, double flops,
-                      double bytes, cudaStream_t st) {
+                      const CUtensorMap& y2, const CUtensorMap& te, const CUtensorMap& u,
+                      const CUtensorMap& w, const WbArgs& a, const char* label, double flops, double bytes,
+                      cudaStream_t st) {
   auto kern = window_bwd_kernel<DKDV>;
   static KernelOnce once;
   const cudaError_t e = once(reinterpret_cast<const void*>(kern), WB_SMEM, WB_THREADS,
@@ -728,7 +774,7 @@ cudaError_t wb_launch(const CUtensorMap& x1, const CUtensorMap& x2, const CUtens
   if (e != cudaSuccess) return e;
   LaunchTimer lt(label, st, flops, bytes);
   const int grid = std::min(a.n_items, num_sms());
-  return launch_kernel(kern, grid, WB_THREADS, WB_SMEM, st, x1, x2, y1, y2, te, a);
+  return launch_kernel(kern, grid, WB_THREADS, WB_SMEM, st, x1, x2, y1, y2, te, u, w, a);
 }
 
 }  // namespace
@@ -738,11 +784,14 @@ size_t window_bwd_ws_bytes(const Window& c) { return wb_carve(nullptr, c).bytes;
 cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long ldo,
                        const WindowSaved& v, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
                        cudaStream_t st) {
-  CUtensorMap tq, tk, tv, td, te;
+  CUtensorMap tq, tk, tv, td, te, gq, gk, gv;
   if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WB_D, c.L, c.B, x.ldq, WB_D, WT) ||
       !tmap_bf16_seq(&tk, x.k, (uint64_t)c.KV * WB_D, c.L, c.B, x.ldk, WB_D, WT) ||
       !tmap_bf16_seq(&tv, x.v, (uint64_t)c.KV * WB_D, c.L, c.B, x.ldv, WB_D, WT) ||
-      !tmap_bf16_seq(&td, dout, (uint64_t)c.H * WB_D, c.L, c.B, lddo, WB_D, WT))
+      !tmap_bf16_seq(&td, dout, (uint64_t)c.H * WB_D, c.L, c.B, lddo, WB_D, WT) ||
+      !tmap_bf16_seq(&gq, dx.q, (uint64_t)c.H * WB_D, c.L, c.B, dx.ldq, WB_D, WT) ||
+      !tmap_bf16_seq(&gk, dx.k, (uint64_t)c.KV * WB_D, c.L, c.B, dx.ldk, WB_D, WT) ||
+      !tmap_bf16_seq(&gv, dx.v, (uint64_t)c.KV * WB_D, c.L, c.B, dx.ldv, WB_D, WT))
     return cudaErrorInvalidValue;
   const WbWs wk = wb_carve(ws, c);
   if (!tmap_bf16_rows32(&te, wk.ext, c.L, (uint64_t)c.B * c.H, WT)) return cudaErrorInvalidValue;
@@ -772,7 +821,7 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
   a.out_w = static_cast<bf16*>(dx.k);
   a.ld_w = dx.ldk;
   a.n_items = (int)k.items;
-  e = wb_launch<true>(tk, tv, tq, td, te, a, "window_bwd_dkdv", 8.0 * WB_D * pairs,
+  e = wb_launch<true>(tk, tv, tq, td, te, gv, gk, a, "window_bwd_dkdv", 8.0 * WB_D * pairs,
                       2.0 * rows * WB_D * (2.0 * c.H + 4.0 * c.KV), st);
   if (e != cudaSuccess) return e;
   const int cut = (k.np_s > 1 ? a.w.sT : 0) + (k.np_w > 1 ? a.w.n_t - a.w.sT : 0);
@@ -781,10 +830,8 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
     e = launch_kernel(window_join_kernel, dim3(WT / 16, c.KV * c.B, cut), 128, 0, st, a);
     if (e != cudaSuccess) return e;
   }
-  a.out_u = static_cast<bf16*>(dx.q);
-  a.ld_u = dx.ldq;
   a.n_items = (int)q_items;
-  return wb_launch<false>(tq, td, tk, tv, te, a, "window_bwd_dq", 6.0 * WB_D * pairs,
+  return wb_launch<false>(tq, td, tk, tv, te, gq, gq, a, "window_bwd_dq", 6.0 * WB_D * pairs,
                           2.0 * rows * WB_D * (3.0 * c.H + 2.0 * c.KV), st);
 }
 
