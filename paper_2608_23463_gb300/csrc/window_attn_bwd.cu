@@ -18,7 +18,9 @@
 // row: they come in as one more MMA (K=16) of ones with each query's LSE and Di, split
 // in three bf16 each (24 bits).  From shared memory every thread read both for each of
 // its columns, 128 KB a step at 128 bytes a cycle, and a producer warp staged them: 520
-// us for 16384 causal tokens of 8 heads, of which 106 for the reads alone.
+// us for 16384 causal tokens of 8 heads, of which 106 for the reads alone.  DQ's rows
+// take theirs from the same array, loaded with X (from global memory at an item's start,
+// each row waited 1000 cycles for them: dQ 424 us for 65536 tokens of 16 heads, 406 so).
 // Roles: warp 0 TMA producer, warp 1 MMA issuer of T, warp 2 MMA issuer of the sums, warp 3
 // their TMA stores, warps 4-19 the row warps: four per TMEM lane quarter, each thread one
 // row (TMEM lane) and one quarter of the 128 streamed columns.  (One issuer for both took
@@ -42,7 +44,7 @@
 // What bounds it: the chain of T's products (operands from shared memory at its 128 bytes a
 // cycle, beside 34 KB of TMA writes a step), their commit and the row warps' reads of T, 1500
 // to 1600 cycles a step, of which the MMAs take 1152 (DKDV) and 768 (DQ).  65536 tokens of 16
-// heads, window 1024, 4 sinks: dK and dV 446 us, dQ 424.  Not faster: T in halves of 64
+// heads, window 1024, 4 sinks: dK and dV 448 us, dQ 406.  Not faster: T in halves of 64
 // columns or T1 and T2 handed over apart, so that the row warps' phases overlap; X in TMEM
 // for DQ; Di into DQ's T by an MMA; Di worked out by a warp of DQ; waits that probe.
 // Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the
@@ -85,8 +87,6 @@ constexpr int WB_ACC = 2 * WB_D;  // dV | dK of a key
 struct WbArgs {
   bf16 *out_u, *out_w;  // window_join_kernel: dV, dK.  Head h at column 64 h
   long ld_u, ld_w;
-  const float* lse;  // [B, H, L], log2 units
-  const float* Di;   // [B, H, L]
   int B, H, KV, g;
   WinTiles w;
   // DKDV: steps of a piece, pieces of a sink tile and of another tile, and the
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
       prefetch_tmap(&tmX2);
       prefetch_tmap(&tmY1);
       prefetch_tmap(&tmY2);
-      if (DKDV) prefetch_tmap(&tmE);
+      prefetch_tmap(&tmE);
     }
     WbItem* const ring = reinterpret_cast<WbItem*>(smem + WB_OFF_ITEM);
     int rd = 0;
@@ -295,7 +295,10 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         ring[it & 3] = m;
         if (m.n > 0) {
           const uint32_t xdst = sbase + xb * 2 * WB_T_BYTES;
-          mbar_arrive_expect_tx(x_full + 8 * xb, 2 * WB_T_BYTES);
+          mbar_arrive_expect_tx(x_full + 8 * xb, 2 * WB_T_BYTES + (DKDV ? 0u : WB_E_BYTES));
+          if (!DKDV)
+            tma_load_3d(sbase + WB_OFF_E + xb * WB_E_BYTES, &tmE, x_full + 8 * xb, 0, m.t * WT,
+                        m.b * a.H + m.h);
           tma_load_3d(xdst, &tmX1, x_full + 8 * xb, m.h * WB_D, m.t * WT, m.b);
           tma_load_3d(xdst + WB_T_BYTES, &tmX2, x_full + 8 * xb, m.h * WB_D, m.t * WT, m.b);
         } else {
@@ -500,11 +503,15 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
         break;
       }
       const int row = m.t * WT + r;  // key (DKDV) or query (DQ) index in the sequence
-      float lse_r = 0.f, di_r = 0.f;
-      if (!DKDV && row < a.w.L) {
-        const long o = ((long)m.b * a.H + m.h) * a.w.L + row;
-        lse_r = a.lse[o];
-        di_r = a.Di[o];
+      float lse_r = 0.f, di_r = 0.f;  // DQ: the row's, negative
+      if (!DKDV) {
+        // (in one half of the 32 bytes, as the swizzle has it; the other is zeros)
+        const uint4* e = reinterpret_cast<const uint4*>(smem + WB_OFF_E + (it & 1) * WB_E_BYTES + r * 32);
+        float x[8], y[8];
+        load8_bf16(reinterpret_cast<const bf16*>(e), x);
+        load8_bf16(reinterpret_cast<const bf16*>(e + 1), y);
+        lse_r = (((x[2] + y[2]) + (x[1] + y[1])) + (x[0] + y[0])) * a.sl2;
+        di_r = ((x[5] + y[5]) + (x[4] + y[4])) + (x[3] + y[3]);
       }
       // streamed tiles in which some pair of a row is hidden: the diagonal's, DKDV those from
       // `edge` on, past some key's window or the sequence's end, DQ those before it that are
@@ -558,10 +565,10 @@ __global__ void __launch_bounds__(WB_THREADS, 1)
               const float2 dv2 =
                   make_float2(__uint_as_float(dv[2 * e]), __uint_as_float(dv[2 * e + 1]));
               const float2 z = DKDV ? __fmul2_rn(sv2, sl)
-                                    : __ffma2_rn(sv2, sl, make_float2(-lse_r, -lse_r));
+                                    : __ffma2_rn(sv2, sl, make_float2(lse_r, lse_r));
               const float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
               const float2 ds =
-                  __fmul2_rn(p, DKDV ? dv2 : __fadd2_rn(dv2, make_float2(-di_r, -di_r)));
+                  __fmul2_rn(p, DKDV ? dv2 : __fadd2_rn(dv2, make_float2(di_r, di_r)));
               pk[4 * g + e] = pack_bf16(p.x, p.y);
               dk[4 * g + e] = pack_bf16(ds.x, ds.y);
             }
@@ -652,8 +659,8 @@ __global__ void __launch_bounds__(128) window_join_kernel(WbArgs a) {
   store8_bf16(o + 8, v + 8);
 }
 
-// Di = rowsum(dO * O) per (sequence, head, query), alone and beside LSE: eight lanes per (row, head),
-// each eight of the head's 64 columns, of WB_DOT_U (row, head)s 32 apart, whose loads go out at once.
+// Di = rowsum(dO * O) per (sequence, head, query) beside LSE, in three bf16 each (24 bits) as an MMA
+// of DKDV takes them: eight lanes per (row, head), each eight of the head's 64 columns, of WB_DOT_U (row, head)s 32 apart, whose loads go out at once.
 // (One to a lane, and 64-bit divisions to find it: 86 us for 65536 tokens of 16 heads, 72 so; four to a lane 76.)
 constexpr int WB_DOT_U = 2;
 __global__ void __launch_bounds__(256) window_dot_kernel(const bf16* dO, long lddo,
@@ -661,8 +668,7 @@ __global__ void __launch_bounds__(256) window_dot_kernel(const bf16* dO, long ld
                                                          const bf16* rest,
                                                          const float* lse,
                                                          bf16* ext,
-                                                         float* Di, long items, int L,
-                                                         int H) {
+                                                         long items, int L, int H) {
   pdl_enter();
   const long it0 = (long)blockIdx.x * (32 * WB_DOT_U);
   const int row0 = (int)(it0 / H), h0 = (int)(it0 - (long)row0 * H);  // the CTA's first
@@ -691,10 +697,9 @@ __global__ void __launch_bounds__(256) window_dot_kernel(const bf16* dO, long ld
     for (int k = 0; k < 8; ++k) v = fmaf(a[k], b[k] + c[k], v);
 #pragma unroll
     for (int s = 4; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
-    if (it0 + i0 + 32 * u < items && sub < 2) {  // Di, and (LSE, Di) as the MMA of DKDV takes them
+    if (it0 + i0 + 32 * u < items && sub < 2) {
       uint4 w = make_uint4(0, 0, 0, 0);
       if (sub == 0) {
-        Di[at[u]] = v;
         // three bf16 that add up to x
         auto split = [](float x, bf16* p) {
 #pragma unroll
@@ -742,7 +747,7 @@ Cut wb_cut(const Window& c) {
 }
 
 struct WbWs {
-  float *Di, *part;
+  float* part;
   bf16* ext;  // [B, H, L][16]
   size_t bytes;
 };
@@ -751,14 +756,12 @@ WbWs wb_carve(void* ws, const Window& c) {
   const WinTiles w(c);
   const Cut k = wb_cut(c);
   WbWs r;
-  const size_t di = up((size_t)c.B * c.H * c.L * sizeof(float));
-  r.Di = static_cast<float*>(ws);
   const size_t ext = up((size_t)c.B * c.H * c.L * WB_EXT * sizeof(bf16));
-  r.ext = reinterpret_cast<bf16*>(static_cast<char*>(ws) + di);
-  r.part = reinterpret_cast<float*>(static_cast<char*>(ws) + di + ext);
+  r.ext = static_cast<bf16*>(ws);
+  r.part = reinterpret_cast<float*>(static_cast<char*>(ws) + ext);
   // pieces are numbered as the items, the sinks' first
   const long pieces = k.np_w > 1 ? k.items : k.np_s > 1 ? (long)c.KV * c.B * w.sT * k.np_s : 0;
-  r.bytes = di + ext + (size_t)pieces * WT * WB_ACC * sizeof(float) + 256;
+  r.bytes = ext + (size_t)pieces * WT * WB_ACC * sizeof(float) + 256;
   return r;
 }
 
@@ -796,8 +799,6 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
   const WbWs wk = wb_carve(ws, c);
   if (!tmap_bf16_rows32(&te, wk.ext, c.L, (uint64_t)c.B * c.H, WT)) return cudaErrorInvalidValue;
   WbArgs a{};
-  a.lse = v.lse;
-  a.Di = wk.Di;
   a.part = wk.part;
   a.B = c.B; a.H = c.H; a.KV = c.KV; a.g = c.H / c.KV;
   a.w = WinTiles(c);
@@ -810,10 +811,10 @@ cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long l
   const double rows = (double)c.B * c.L, pairs = (double)c.B * c.H * window_pairs(c);
   cudaError_t e;
   {
-    LaunchTimer lt("window_bwd_dot", st, 2.0 * rows * c.H * WB_D, rows * c.H * (6.0 * WB_D + 8.0 + 2.0 * WB_EXT));
+    LaunchTimer lt("window_bwd_dot", st, 2.0 * rows * c.H * WB_D, rows * c.H * (6.0 * WB_D + 4.0 + 2.0 * WB_EXT));
     const long n = (long)c.B * c.L * c.H;
     e = launch_kernel(window_dot_kernel, (unsigned)((n + 32 * WB_DOT_U - 1) / (32 * WB_DOT_U)), 256, 0, st,
-                      dout, lddo, out, ldo, v.rest, v.lse, wk.ext, wk.Di, n, c.L, c.H);
+                      dout, lddo, out, ldo, v.rest, v.lse, wk.ext, n, c.L, c.H);
     if (e != cudaSuccess) return e;
   }
   a.out_u = static_cast<bf16*>(dx.v);
