@@ -23,7 +23,7 @@
 // What bounds it: the chain of one softmax warp through a tile (about 430
 // instructions, two such warps on each scheduler), beside 1024 cycles of MMAs
 // and as many of exponentials for a pair of tiles.  262144 tokens of 16 heads on
-// 4, window 4096: 4.25 ms (1.04 PFLOP/s).  What shortened the chain: maxima of
+// 4, window 4096: 4.17 ms (1.06 PFLOP/s).  What shortened the chain: maxima of
 // the first half of the scores while the second comes from TMEM, P stored from
 // its half on, and a loop of its own for tiles without masked keys (4.50
 // without the three; 4.39 with the loop alone, 4.34 with it and either).
@@ -35,8 +35,8 @@
 // the next item's first step: 5.03.
 // A sinks' tile before the window that holds WT_FEW sinks at most is worked off
 // as a tile of so many keys: 65536 tokens of 16 heads, window 1024, 4 sinks 448
-// us without, 422 with it; 399 now, 411 with each tile's scores and O issued by
-// one warp.
+// us without, 422 with it; 411 with each tile's scores and O issued by one warp,
+// 399 so; 366 with the rows out by TMA, for which an item's end took a fifth of it.
 // A row's probabilities are taken against a reference m, the maximum of the
 // first tile in which the row sees a key, raised only when a later tile's
 // maximum exceeds it by more than WA_RESCALE (log2 units); then O and the sum
@@ -80,10 +80,7 @@ constexpr uint32_t WA_TMEM_COLS = 512;
 constexpr uint32_t WA_TM_O = 256, WA_TM_P = 384;
 
 struct WaArgs {
-  bf16* out;   // [B*L, ldo], head h at column h*64
   float* lse;  // [B, H, L] in log2 units, or null
-  bf16* rest;  // [B*L, H*64] out - bf16(out), with lse
-  long ldo;
   int B, H, g;  // g: query heads to a key head
   WinTiles w;
   int n_st, n_items;  // tile pairs
@@ -141,9 +138,18 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
   return mbar_wait_warp(bar, parity);
 }
 
+// A tile of 64 columns and the map's rows.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t saddr, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+                   map),
+               "r"(x), "r"(y), "r"(z), "r"(saddr)
+               : "memory");
+}
+
 __global__ void __launch_bounds__(WA_THREADS, 1)
     window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                      const __grid_constant__ CUtensorMap tmV, WaArgs a) {
+                      const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
+                      const __grid_constant__ CUtensorMap tmR, WaArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -332,10 +338,16 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
     const float2 sl = make_float2(a.sl2, a.sl2);
     bool ok = true;
     uint32_t g = 0, io = 0;
-    for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items && ok; k = wa_rank(blockIdx.x, ++rd)) {
-      const WaItem m(a, k);
+    int k = wa_rank(blockIdx.x, 0);
+    WaItem next(a, k);  // worked out while the item before it waits for its O
+    for (int rd = 1; k < a.n_items; ++rd) {
+      const WaItem m = next;
       const int t = 2 * m.u + w;
-      if (t >= a.w.n_t) continue;
+      if (t >= a.w.n_t) {
+        k = wa_rank(blockIdx.x, rd);
+        next = WaItem(a, k);
+        continue;
+      }
       const int q = t * WT + r;  // query index in the sequence
       // its key tiles: the sinks' [0, ns) and the window's [lo, t]; those of [whole, clear)
       // lie partly before some row's window and are not all sinks
@@ -473,6 +485,8 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
         for (; ok && kt < t; ++kt) ok = step(all, std::false_type{}, kt);
       }
       if (!ok) break;
+      k = wa_rank(blockIdx.x, rd);
+      next = WaItem(a, k);
       // the item's O: after its last P.V
       if (!wait_warp(o_full(w), io & 1)) break;
       ++io;
@@ -484,44 +498,48 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
       tmem_wait_ld(ov + 32);
       tc_fence_before();
       mbar_arrive_warp(o_free(w));
+      // the warp's 32 rows go out by TMA from its own stage (128-byte swizzle; rows past the end
+      // of the sequence are left out)
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      // the warp's 32 rows through its own stage (16-byte piece p of row i at piece
-      // p ^ (i & 7)), so that 8 lanes store a row's 128 bytes
       uint8_t* const stg = smem + WA_OFF_STG + (warp - 4) * 4096;
-      const int q0 = t * WT + q4 * 32;
-      auto put = [&](bf16* dst, long ld) {
-#pragma unroll
-        for (int i = 0; i < WA_D; i += 8) {
-          const float* o = reinterpret_cast<const float*>(ov + i);
-          *reinterpret_cast<uint4*>(stg + lane * 128 + (((i >> 3) ^ (lane & 7)) << 4)) =
-              make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]),
-                         pack_bf16(o[6], o[7]));
-        }
+      auto put = [&](const CUtensorMap* map, const uint32_t* v) {  // v: the row, bf16 pairs
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the store before
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          const int rr = i + (lane >> 3), p = lane & 7;
-          const uint4 v = *reinterpret_cast<const uint4*>(stg + rr * 128 + ((p ^ (rr & 7)) << 4));
-          if (q0 + rr < a.w.L)
-            *reinterpret_cast<uint4*>(dst + ((long)m.b * a.w.L + q0 + rr) * ld + m.h * WA_D + p * 8) =
-                v;
-        }
+        for (int i = 0; i < 8; ++i)
+          *reinterpret_cast<uint4*>(stg + lane * 128 + ((i ^ (lane & 7)) << 4)) =
+              make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
+        if (lane == 0) {
+          if (t * WT + q4 * 32 < a.w.L)
+            tma_store_3d(map, smem_u32(stg), m.h * WA_D, t * WT + q4 * 32, m.b);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
       };
+      uint32_t pk[WA_D / 2];
 #pragma unroll
-      for (int i = 0; i < WA_D; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * inv);
-      put(a.out, a.ldo);
+      for (int i = 0; i < WA_D / 2; ++i) {
+        const float2 o = __fmul2_rn(make_float2(__uint_as_float(ov[2 * i]), __uint_as_float(ov[2 * i + 1])),
+                                    make_float2(inv, inv));
+        pk[i] = pack_bf16(o.x, o.y);
+        ov[2 * i] = __float_as_uint(o.x);
+        ov[2 * i + 1] = __float_as_uint(o.y);
+      }
+      put(&tmO, pk);
       if (a.lse) {  // the backward's Di = dO . O cancels against dP: it wants more than bf16's O
 #pragma unroll
-        for (int i = 0; i < WA_D; ++i) {
-          const float o = __uint_as_float(ov[i]);
-          ov[i] = __float_as_uint(o - __bfloat162float(__float2bfloat16(o)));
+        for (int i = 0; i < WA_D / 2; ++i) {
+          const float2 b = unpack_bf16(pk[i]);
+          pk[i] = pack_bf16(__uint_as_float(ov[2 * i]) - b.x, __uint_as_float(ov[2 * i + 1]) - b.y);
         }
-        put(a.rest, (long)a.H * WA_D);
+        put(&tmR, pk);
         if (q < a.w.L)
           a.lse[((long)m.b * a.H + m.h) * a.w.L + q] = mref + log2f(l);  // log2 units
       }
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    __syncwarp();
   }
   tc_fence_before();
   if (__syncthreads_or(*(volatile int*)&g_dev_error != 0)) {
@@ -560,16 +578,16 @@ WindowSaved window_saved(const Window& c, void* p) {
 
 cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, const WindowSaved& v,
                        cudaStream_t st) {
-  CUtensorMap tq, tk, tv;
+  CUtensorMap tq, tk, tv, to, tr;
   if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WA_D, c.L, c.B, x.ldq, WA_D, WT) ||
       !tmap_bf16_seq(&tk, x.k, (uint64_t)c.KV * WA_D, c.L, c.B, x.ldk, WA_D, WT) ||
-      !tmap_bf16_seq(&tv, x.v, (uint64_t)c.KV * WA_D, c.L, c.B, x.ldv, WA_D, WT))
+      !tmap_bf16_seq(&tv, x.v, (uint64_t)c.KV * WA_D, c.L, c.B, x.ldv, WA_D, WT) ||
+      !tmap_bf16_seq(&to, out, (uint64_t)c.H * WA_D, c.L, c.B, ldo, WA_D, 32) ||
+      !tmap_bf16_seq(&tr, v.rest ? v.rest : out, (uint64_t)c.H * WA_D, c.L, c.B,
+                     v.rest ? (uint64_t)c.H * WA_D : ldo, WA_D, 32))
     return cudaErrorInvalidValue;
   WaArgs a{};
-  a.out = out;
   a.lse = v.lse;
-  a.rest = v.rest;
-  a.ldo = ldo;
   a.B = c.B;
   a.H = c.H;
   a.g = c.H / c.KV;
@@ -588,7 +606,7 @@ cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, co
                  2.0 * c.B * c.L * WA_D * ((v.lse ? 3.0 : 2.0) * c.H + 2.0 * c.KV) +
                      (v.lse ? 4.0 * c.B * c.H * c.L : 0.0));
   const int grid = std::min(a.n_items, num_sms());
-  return launch_kernel(window_fwd_kernel, grid, WA_THREADS, WA_SMEM, st, tq, tk, tv, a);
+  return launch_kernel(window_fwd_kernel, grid, WA_THREADS, WA_SMEM, st, tq, tk, tv, to, tr, a);
 }
 
 }  // namespace pf
