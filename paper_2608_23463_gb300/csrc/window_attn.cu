@@ -23,7 +23,7 @@
 // What bounds it: the chain of one softmax warp through a tile (about 430
 // instructions, two such warps on each scheduler), beside 1024 cycles of MMAs
 // and as many of exponentials for a pair of tiles.  262144 tokens of 16 heads on
-// 4, window 4096: 4.17 ms (1.06 PFLOP/s).  What shortened the chain: maxima of
+// 4, window 4096: 3.95 ms (1.13 PFLOP/s).  What shortened the chain: maxima of
 // the first half of the scores while the second comes from TMEM, P stored from
 // its half on, and a loop of its own for tiles without masked keys (4.50
 // without the three; 4.39 with the loop alone, 4.34 with it and either).
@@ -37,6 +37,9 @@
 // as a tile of so many keys: 65536 tokens of 16 heads, window 1024, 4 sinks 448
 // us without, 422 with it; 411 with each tile's scores and O issued by one warp,
 // 399 so; 366 with the rows out by TMA, for which an item's end took a fifth of it.
+// Code counts, its fetches more than its instructions: masks by the bits of a word in
+// place of two compares of a column (4.17 to 3.95 ms where a tile in seventeen has one).
+// One body for tiles with masks and without spills: 4.59.
 // A row's probabilities are taken against a reference m, the maximum of the
 // first tile in which the row sees a key, raised only when a later tile's
 // maximum exceeds it by more than WA_RESCALE (log2 units); then O and the sum
@@ -349,9 +352,9 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
         continue;
       }
       const int q = t * WT + r;  // query index in the sequence
-      // its key tiles: the sinks' [0, ns) and the window's [lo, t]; those of [whole, clear)
-      // lie partly before some row's window and are not all sinks
-      const int lo = a.w.lo(t), ns = min(a.w.sT, lo), whole = a.w.S / WT;
+      // its key tiles: the sinks' [0, ns) and the window's [lo, t]; those before `clear`
+      // and the diagonal's, t, hide keys from some row
+      const int lo = a.w.lo(t), ns = min(a.w.sT, lo);
       const int past = t * WT + WT - 1 - a.w.W, clear = past >= 0 ? past / WT + 1 : 0;
       const int few = a.w.few < lo ? a.w.few : -1;  // the few sinks' tile
       float mref = -INFINITY, l = 0.f;
@@ -398,16 +401,15 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
           for (int c = 0; c < NC; ++c)
             if (c >= a.w.S - kt * WT) sc[c] = 0xff800000u;  // -inf
         } else if (decltype(masked)::value) {
-          if (kt == t) {  // the diagonal
+          // seen keys: (q - W, q], and the sinks; bit c of a word: its column c
+          auto low = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-              if (c > r) sc[c] = 0xff800000u;  // -inf
-          }
-          if (kt < clear && kt >= whole) {  // keys that the window has passed
-            const int low = q - a.w.W + 1 - kt * WT, sk = a.w.S - kt * WT;
+          for (int c0 = 0; c0 < NC; c0 += 32) {
+            const int b0 = kt * WT + c0;
+            const uint32_t vis = low(q + 1 - b0) & (~low(q - a.w.W + 1 - b0) | low(a.w.S - b0));
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-              if (c < low && c >= sk) sc[c] = 0xff800000u;
+            for (int c = 0; c < 32; ++c)
+              if (!(vis >> c & 1)) sc[c0 + c] = 0xff800000u;  // -inf
           }
         }
         // the maximum (log2 units), three-input maxima
