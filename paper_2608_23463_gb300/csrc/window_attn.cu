@@ -39,7 +39,7 @@
 // 399 so; 366 with the rows out by TMA, for which an item's end took a fifth of it.
 // Code counts, its fetches more than its instructions: masks by the bits of a word in
 // place of two compares of a column (4.17 to 3.95 ms where a tile in seventeen has one).
-// One body for tiles with masks and without spills: 4.59.
+// One body for tiles with masks and tiles without them spills: 4.59.
 // A row's probabilities are taken against a reference m, the maximum of the
 // first tile in which the row sees a key, raised only when a later tile's
 // maximum exceeds it by more than WA_RESCALE (log2 units); then O and the sum
