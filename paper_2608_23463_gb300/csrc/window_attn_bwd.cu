@@ -43,8 +43,8 @@
 // columns is on the chain of every step.
 // What bounds it: the chain of T's products (operands from shared memory at its 128 bytes a
 // cycle, beside 34 KB of TMA writes a step), their commit and the row warps' reads of T, 1500
-// to 1600 cycles a step, of which the MMAs take 1152 (DKDV) and 768 (DQ).  65536 tokens of 16
-// heads, window 1024, 4 sinks: dK and dV 448 us, dQ 406.  Not faster: T in halves of 64
+// to 1600 cycles a step, of which the MMAs take 1152 (DKDV, 73 % of the tensor pipe's time)
+// and 768 (DQ).  65536 tokens of 16 heads, window 1024, 4 sinks: dK and dV 452 us, dQ 406.  Not faster: T in halves of 64
 // columns or T1 and T2 handed over apart, so that the row warps' phases overlap; X in TMEM
 // for DQ; Di into DQ's T by an MMA; Di worked out by a warp of DQ; waits that probe.
 // Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the

@@ -199,3 +199,16 @@ def test_training_rows_are_the_decoded_tokens(window, n_sink):
         mag = v.float().abs().max()
         assert ((o.float() - out[:, i].float()).abs() <= 4 * 2.0 ** -8 * mag).all()
     check()
+
+
+@pytest.mark.parametrize("B,L,H,KV,window,n_sink", [(4, 640, 32, 32, 1, 0), (4, 640, 32, 4, 2, 1), (8, 130, 40, 40, 1, 0),
+                                                    (3, 385, 48, 48, 129, 33)])
+def test_many_short_items(B, L, H, KV, window, n_sink):
+    """Several work items of a step or two on every SM: nothing runs ahead of an item that still uses its buffers."""
+    step(B, L, H, KV, window, n_sink, 17)
+
+
+@pytest.mark.parametrize("n_sink", [31, 32, 33, 128, 160, 161])
+def test_few_sinks(n_sink):
+    """The last tile of the sinks holds 32 of them at most, or more."""
+    step(2, 700, 4, 2, 150, n_sink, 19)
