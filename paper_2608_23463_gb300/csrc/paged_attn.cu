@@ -17,7 +17,8 @@
 // cp.async with the swizzle that its reads want; no barrier between the warps
 // while they stream.  Rows that the token does not see are filled with zeros,
 // not read: 0 times an infinity there would reach the sums.
-// The split over the cache: a unit is a tile for each of the CTA's warps, and
+// Short caches, or enough of them: a CTA to each (sequence, key head) (pa_whole).
+// Else the split over the cache: a unit is a tile for each of the CTA's warps, and
 // the units of all (sequence, key head) pairs, ragged as they are, are dealt
 // to the CTAs in equal contiguous ranges.  The lengths are read on the device;
 // every CTA sums them up itself.  A CTA that holds all of a pair writes its
@@ -61,6 +62,7 @@ struct PaArgs {
   long ldo;
   float* part;  // [2 G][g][DH] sums, then [2 G][g][2] (max, sum)
   int B, KV, g, page, max_pages, window, sinks, G;
+  bool whole;  // a CTA for each (sequence, key head), not equal ranges of units
   long n_pages;
   float sl2;  // log2(e) / sqrt(dh)
 };
@@ -154,37 +156,52 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
   // the join's CTAs may take their places now: they wait for this grid to end,
   // and all of its CTAs are running
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  pa_units(a, pre, PA_THREADS);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gid = lane >> 2, t = lane & 3;
-  // rows of sequences without keys
-  for (int b = blockIdx.x; b < a.B; b += a.G)
-    if (pre[b + 1] == pre[b])
-      for (int i = tid * 8; i < a.KV * a.g * DH; i += PA_THREADS * 8)
-        *reinterpret_cast<uint4*>(a.out + b * a.ldo + i) = make_uint4(0, 0, 0, 0);
-  const long T = (long)pre[a.B] * a.KV;
-  const int G = (int)min((long)a.G, T);
-  if ((int)blockIdx.x >= G) return;
-  const long r0 = pa_first(T, G, blockIdx.x), r1 = pa_first(T, G, blockIdx.x + 1);
+  auto zeros = [&](int b, int col, int n) {
+    for (int i = tid * 8; i < n; i += PA_THREADS * 8)
+      *reinterpret_cast<uint4*>(a.out + b * a.ldo + col + i) = make_uint4(0, 0, 0, 0);
+  };
+  int b = 0, h = 0, nu = 0;
+  long r0 = 0, r1;
+  if (a.whole) {
+    b = blockIdx.x / a.KV;
+    h = blockIdx.x - b * a.KV;
+    const int len = a.len[b];
+    if (tid == 0 && (len < 0 || len > (long)a.max_pages * a.page)) set_dev_error(DEVERR_CAPACITY);
+    r1 = nu = (pa_span(a, b).tiles + PA_WARPS - 1) / PA_WARPS;
+    if (nu == 0) zeros(b, h * a.g * DH, a.g * DH);
+  } else {
+    pa_units(a, pre, PA_THREADS);
+    // rows of sequences without keys
+    for (int e = blockIdx.x; e < a.B; e += a.G)
+      if (pre[e + 1] == pre[e]) zeros(e, 0, a.KV * a.g * DH);
+    const long T = (long)pre[a.B] * a.KV;
+    const int G = (int)min((long)a.G, T);
+    if ((int)blockIdx.x >= G) return;
+    r0 = pa_first(T, G, blockIdx.x);
+    r1 = pa_first(T, G, blockIdx.x + 1);
+    // the sequence of unit r0
+    int hi = a.B;
+    while (hi - b > 1) {
+      const int m = (b + hi) >> 1;
+      if ((long)pre[m] * a.KV <= r0) b = m; else hi = m;
+    }
+  }
   unsigned char* const wring = ring + warp * C::WARP_BYTES;
   const uint32_t wr = smem_u32(wring);
   float* const ml = a.part + 2L * a.G * a.g * DH;
 
   long pos = r0;
-  int b = 0;
-  {  // the sequence of unit r0
-    int lo = 0, hi = a.B;
-    while (hi - lo > 1) {
-      const int m = (lo + hi) >> 1;
-      if ((long)pre[m] * a.KV <= r0) lo = m; else hi = m;
-    }
-    b = lo;
-  }
   while (pos < r1) {
-    while (pre[b + 1] == pre[b] || (long)pre[b + 1] * a.KV <= pos) ++b;
-    const int nu = pre[b + 1] - pre[b];
-    const long off = pos - (long)pre[b] * a.KV;
-    const int h = (int)(off / nu), u0 = (int)(off % nu);
+    int u0 = 0;
+    if (!a.whole) {
+      while (pre[b + 1] == pre[b] || (long)pre[b + 1] * a.KV <= pos) ++b;
+      nu = pre[b + 1] - pre[b];
+      const long off = pos - (long)pre[b] * a.KV;
+      h = (int)(off / nu);
+      u0 = (int)(off % nu);
+    }
     const int u1 = (int)min((long)nu, u0 + (r1 - pos));
     const PaSpan sp = pa_span(a, b);
     const int t1 = min(sp.tiles, u1 * PA_WARPS);
@@ -367,7 +384,9 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
 }
 
 // Rows whose pair lies on several CTAs: the pieces joined in the order of the
-// CTAs.  CTA (query head, sequence, 32 columns): 16 threads to a column.
+// CTAs.  CTA x takes pair x, or, with more pairs than CTAs, the pair that
+// begins on CTA x and ends on a later one; CTAs y share its columns, 32 at a
+// time, 16 threads to a column.
 constexpr int PJ_THREADS = 512;
 template <int DH>
 __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a) {
@@ -377,43 +396,77 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a) {
   __shared__ float sL;
   pdl_enter();
   pa_units(a, pre, PJ_THREADS);
-  const int hq = blockIdx.x, b = blockIdx.y, h = hq / a.g, r = hq % a.g, tid = threadIdx.x;
+  const int tid = threadIdx.x, x = blockIdx.x;
+  const long T = (long)pre[a.B] * a.KV;
+  const int G = (int)min((long)a.G, T);
+  int b, h;
+  if (a.B * a.KV <= a.G) {
+    b = x / a.KV;
+    h = x - b * a.KV;
+  } else {
+    if (x + 1 >= G) return;
+    const long u = pa_first(T, G, x + 1);
+    int hi = a.B;
+    b = 0;
+    while (hi - b > 1) {
+      const int m = (b + hi) >> 1;
+      if ((long)pre[m] * a.KV <= u) b = m; else hi = m;
+    }
+    while (pre[b + 1] == pre[b]) ++b;  // (u < T: such a one follows)
+    h = (int)((u - (long)pre[b] * a.KV) / (pre[b + 1] - pre[b]));
+  }
   const int nu = pre[b + 1] - pre[b];
   if (nu == 0) return;
-  const long T = (long)pre[a.B] * a.KV, u0 = (long)pre[b] * a.KV + (long)h * nu;
-  const int G = (int)min((long)a.G, T);
+  const long u0 = (long)pre[b] * a.KV + (long)h * nu;
   const int c0 = pa_cta(T, G, u0), c1 = pa_cta(T, G, u0 + nu - 1);
-  if (c0 == c1) return;
+  if (c0 == c1 || (a.B * a.KV > a.G && c0 != x)) return;
   const int n = c1 - c0 + 1;
   const float* ml = a.part + 2L * a.G * a.g * DH;
   auto slot = [&](int i) { return 2L * (c0 + i) + (i == 0 && pa_first(T, G, c0) != u0 ? 1 : 0); };
-  const int d = blockIdx.z * 32 + (tid & 31), g = tid >> 5;
-  if (tid < 32) {
-    float M = -INFINITY, L = 0.f;
-    for (int i = tid; i < n; i += 32) M = fmaxf(M, ml[(slot(i) * a.g + r) * 2]);
+  for (int k = blockIdx.y; k < a.g * (DH / 32); k += gridDim.y) {
+    const int r = k / (DH / 32), d = k % (DH / 32) * 32 + (tid & 31), g = tid >> 5;
+    if (tid < 32) {
+      float M = -INFINITY, L = 0.f;
+      for (int i = tid; i < n; i += 32) M = fmaxf(M, ml[(slot(i) * a.g + r) * 2]);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    for (int i = tid; i < n; i += 32) {
-      const float* x = ml + (slot(i) * a.g + r) * 2;
-      const float f = M == -INFINITY ? 0.f : ex2_approx(x[0] - M);
-      sw[i] = f;
-      L = fmaf(x[1], f, L);
+      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      for (int i = tid; i < n; i += 32) {
+        const float* y = ml + (slot(i) * a.g + r) * 2;
+        const float f = M == -INFINITY ? 0.f : ex2_approx(y[0] - M);
+        sw[i] = f;
+        L = fmaf(y[1], f, L);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+      if (tid == 0) sL = L;
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-    if (tid == 0) sL = L;
-  }
-  __syncthreads();
-  float v = 0.f;
+    __syncthreads();
+    float v = 0.f;
 #pragma unroll 8
-  for (int i = g; i < n; i += 16) v = fmaf(a.part[(slot(i) * a.g + r) * DH + d], sw[i], v);
-  red[g][tid & 31] = v;
-  __syncthreads();
-  if (g) return;
-  v = 0.f;
+    for (int i = g; i < n; i += 16) v = fmaf(a.part[(slot(i) * a.g + r) * DH + d], sw[i], v);
+    red[g][tid & 31] = v;
+    __syncthreads();
+    if (g == 0) {
+      v = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v += red[i][tid & 31];
-  a.out[b * a.ldo + (long)hq * DH + d] = __float2bfloat16(sL > 0.f ? v / sL : 0.f);
+      for (int i = 0; i < 16; ++i) v += red[i][tid & 31];
+      a.out[b * a.ldo + ((long)h * a.g + r) * DH + d] = __float2bfloat16(sL > 0.f ? v / sL : 0.f);
+    }
+    __syncthreads();
+  }
+}
+
+// A CTA for each (sequence, key head), and no join, where none sees many rows: a CTA
+// streams 43 GB/s, and with a pair or more to each SM that is HBM's rate, while ranges that
+// span several short pairs cost their ends.  In us, whole and in ranges, ragged but for the
+// first two: 1 x 250 rows, 4 heads of 64: 4.9 and 7.3; 1 x 500: 8.0 and 7.3; 8 x 1000 rows, 8
+// heads of 128: 15.8 and 15.4; 32 x 1000: 20.3 and 41; 256 x 1000: 87 and 136; 300 x 200 rows of
+// one head: 7.4 and 48.
+bool pa_whole(const Paged& c) {
+  constexpr long FEW = 384, MANY = 2048, SMS = 152;
+  long rows = (long)c.max_pages * c.page;
+  if (c.window > 0) rows = std::min(rows, (long)c.window + c.sinks + 2 * PA_TILE);
+  return rows <= ((long)c.B * c.KV < SMS ? FEW : MANY);
 }
 
 // CTAs: two an SM, or a unit each.
@@ -436,7 +489,10 @@ cudaError_t pa_launch(const PaArgs& a, bool split, cudaStream_t st) {
     if (e != cudaSuccess || !split) return e;
   }
   LaunchTimer lt("paged_join", st, 0.0, 8.0 * a.G * a.g * (DH + 2));
-  return launch_kernel(paged_join_kernel<DH>, dim3(a.KV * a.g, a.B, DH / 32), PJ_THREADS, 0, st, a);
+  // about 1200 CTAs, or as many as there are columns for
+  const long pairs = (long)a.B * a.KV;
+  const int x = (int)std::min<long>(pairs, a.G), y = std::min(a.g * (DH / 32), (8 * 152 + x - 1) / x);
+  return launch_kernel(paged_join_kernel<DH>, dim3(x, y), PJ_THREADS, 0, st, a);
 }
 
 }  // namespace
@@ -460,9 +516,10 @@ cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long 
   a.B = c.B; a.KV = c.KV; a.g = c.H / c.KV; a.page = c.page; a.max_pages = c.max_pages;
   a.window = c.window; a.sinks = c.sinks;
   a.n_pages = c.n_pages;
-  a.G = pa_grid(c);
+  a.whole = pa_whole(c);
+  a.G = a.whole ? c.B * c.KV : pa_grid(c);
   a.sl2 = 1.4426950408889634f / sqrtf((float)c.dh);
-  const bool split = (long)c.max_pages * c.page > PA_UNIT;  // else no pair has two units
+  const bool split = !a.whole && (long)c.max_pages * c.page > PA_UNIT;  // else no pair has two units
   return c.dh == 128 ? pa_launch<128>(a, split, st) : pa_launch<64>(a, split, st);
 }
 

@@ -153,3 +153,15 @@ def test_decode_step_in_a_graph():
         assert torch.equal(out, ref), i
     check()
     assert c.len.tolist() == [41, 41]
+
+
+@pytest.mark.parametrize("B,H,KV,dh,longest", [(160, 4, 2, 64, 2100), (40, 24, 8, 128, 2500), (400, 1, 1, 64, 5000),
+                                               (40, 8, 4, 64, 2000), (38, 4, 4, 128, 400), (3, 8, 2, 64, 384), (3, 8, 2, 64, 385)])
+def test_pairs_and_splits(B, H, KV, dh, longest):
+    """More (sequence, key head) pairs than CTAs with long and empty ones among them, and either side of where a CTA
+    takes a whole pair."""
+    length = [0, 0] + [(53 * i) % 190 for i in range(B - 3)] + [longest]
+    c = paged(B, H, KV, dh, 16, length, 11)
+    attend(c, rand((B, H * dh), 12))
+    c = paged(B, H, KV, dh, 16, length[::-1], 13)
+    attend(c, rand((B, H * dh), 14))
