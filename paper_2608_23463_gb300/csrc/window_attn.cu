@@ -141,14 +141,6 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
   return mbar_wait_warp(bar, parity);
 }
 
-// A tile of 64 columns and the map's rows.
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t saddr, int x, int y, int z) {
-  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
-                   map),
-               "r"(x), "r"(y), "r"(z), "r"(saddr)
-               : "memory");
-}
-
 __global__ void __launch_bounds__(WA_THREADS, 1)
     window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                       const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,

@@ -50,6 +50,7 @@
 // Every mbarrier wait is bounded.  Masked columns have P = 0, and rows past the
 // end of a sequence read as zero.
 #include <algorithm>
+#include <type_traits>
 
 #include "local.h"
 #include "window_tiles.cuh"
@@ -66,8 +67,8 @@ constexpr int WB_EXT = 16;  // bf16 of a query's LSE and Di: three each, the res
 constexpr int WB_STAGES = 4;
 constexpr int WB_ROW_THREADS = 512;  // warps 4-19
 constexpr int WB_THREADS = 128 + WB_ROW_THREADS;
-// A row thread holds 64 values of a step: the control warps give
-// registers up, of the 96 that each thread has at launch.
+// A row thread holds 64 values of a step: the control warps give registers up, of the 96
+// that each thread has at launch.
 constexpr int WB_REGS_CTRL = 64, WB_REGS_ROWS = 104;
 static_assert(WB_REGS_CTRL * 128 + WB_REGS_ROWS * 512 <= 96 * WB_THREADS, "register split");
 constexpr uint32_t WB_T_BYTES = WT * WB_D * 2;  // 16 KB per tile
@@ -192,14 +193,6 @@ __device__ __forceinline__ uint64_t smem_desc_sw32(uint32_t saddr) {
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
   if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
   return mbar_wait_warp(bar, parity);
-}
-
-// A tile of 64 columns and 128 rows (those past the end of the sequence are left out).
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t saddr, int x, int y, int z) {
-  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
-                   map),
-               "r"(x), "r"(y), "r"(z), "r"(saddr)
-               : "memory");
 }
 
 template <bool DKDV>

@@ -34,4 +34,13 @@ struct WinTiles {
   }
 };
 
+// A tile of the map's rows from shared memory, 128-byte swizzle (rows past the end of the
+// sequence are left out).
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t saddr, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+                   map),
+               "r"(x), "r"(y), "r"(z), "r"(saddr)
+               : "memory");
+}
+
 }  // namespace pf
