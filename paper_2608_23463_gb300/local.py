@@ -147,16 +147,21 @@ class PagedKVCache:
                               device=self.K.device)
         self.free = list(range(n_pages - 1, -1, -1))  # pages that reserve() hands out
         self.held = [[] for _ in range(batch)]        # and has handed out, by sequence
+        self.left = set()                             # sequences released and not begun again
 
     def reserve(self, rows: Sequence[int]) -> None:
         """Pages for rows[b] rows in all of every sequence b (host bookkeeping; a
-        cache that was given its table keeps its own)."""
+        cache that was given its table keeps its own).  A released sequence that gets
+        pages again begins empty."""
         need = [max(0, -(-int(r) // self.page) - len(p)) for r, p in zip(rows, self.held)]
         if sum(need) > len(self.free) or any(
                 n + len(p) > self.max_pages for n, p in zip(need, self.held)):
             raise ProxyFormerError(PF_ERR_CAPACITY, "no pages left for these rows")
         for b, n in enumerate(need):
             if n:
+                if b in self.left:  # steps of one token have counted its rows on
+                    self.left.remove(b)
+                    self.len[b] = 0
                 new = [self.free.pop() for _ in range(n)]
                 at = len(self.held[b])
                 self.held[b] += new
@@ -164,9 +169,13 @@ class PagedKVCache:
                                                         device=self.table.device)
 
     def release(self, b: int) -> None:
-        """Sequence b gives its pages back and is empty."""
+        """Sequence b gives its pages back and is empty.  Its place in the table is cleared:
+        another sequence may own the pages when a step of one token for every sequence
+        reaches b too, which is flagged (PF_ERR_CAPACITY) and writes nothing."""
+        self.table[b, :len(self.held[b])] = -1
         self.free += self.held[b][::-1]
         self.held[b] = []
+        self.left.add(b % self.batch)
         self.len[b] = 0
 
     def advance(self, start: Optional[torch.Tensor] = None) -> None:

@@ -240,3 +240,30 @@ def test_pages_are_reserved_and_released():
     c.release(0)
     c.reserve([0, 48])
     assert len(c.free) == 1 and len(c.held[1]) == 3
+
+
+def test_released_sequences_write_nowhere():
+    """A released sequence's token in a step of one for all is flagged, and the pages' next owner keeps its rows."""
+    c = PagedKVCache(2, 2, 1, 64, 16, n_pages=4, max_pages=3)
+    starts = lambda *s: torch.tensor(s, dtype=torch.int32, device="cuda")
+    cut = lambda x: (x[:, :128], x[:, 128:192], x[:, 192:])
+    c.reserve([20, 0])
+    c.advance(starts(0, 20, 20))
+    c.append(*cut(rand((20, 256), 1)), start=starts(0, 20, 20))
+    c.release(0)
+    c.reserve([0, 40])
+    c.advance(starts(0, 0, 30))
+    c.append(*cut(rand((30, 256), 2)), start=starts(0, 0, 30))
+    check()
+    rows = lambda: [t[c.table[1, :3].long()].transpose(1, 2).reshape(48, 64).clone() for t in (c.K, c.V)]
+    before, x = rows(), rand((2, 256), 3)
+    c.advance()
+    c.append(*cut(x))  # a token for the released sequence too
+    with pytest.raises(pf.ProxyFormerError) as e:
+        check()
+    assert e.value.status == pf.PF_ERR_CAPACITY
+    for a, b, new in zip(rows(), before, cut(x)[1:]):
+        b[30] = new[1]
+        assert torch.equal(a, b)
+    c.reserve([16, 40])
+    assert c.len.tolist() == [0, 31]
