@@ -4,6 +4,8 @@
 //   o_h = sum_j softmax_j(q_h . K_j / sqrt(dh)) V_j over the sequence's rows
 //   j < len, with a window W also j >= len - W or j < S (the sinks);
 //   a sequence without rows gives zeros.
+// A token sees itself, so that a sum is never empty: a row whose scores are NaN, or all
+// -inf, comes out as NaN (0 / 0 the latter).
 //
 // Streaming the visible K and V rows from HBM once bounds it: the query heads
 // that share a key head (up to 16) are the 16 rows of the same m16n8k16 MMAs,
@@ -369,7 +371,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
         v = fmaf(x[d], f, v);
       }
       if (whole) {
-        a.out[b * a.ldo + (long)h * a.g * DH + i] = __float2bfloat16(L > 0.f ? v / L : 0.f);
+        a.out[b * a.ldo + (long)h * a.g * DH + i] = __float2bfloat16(v / L);
       } else {
         a.part[((long)slot * a.g + r) * DH + d] = v;
         if (d == 0) {
@@ -450,7 +452,7 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a) {
       v = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) v += red[i][tid & 31];
-      a.out[b * a.ldo + ((long)h * a.g + r) * DH + d] = __float2bfloat16(sL > 0.f ? v / sL : 0.f);
+      a.out[b * a.ldo + ((long)h * a.g + r) * DH + d] = __float2bfloat16(v / sL);
     }
     __syncthreads();
   }

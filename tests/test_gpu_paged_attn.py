@@ -2,6 +2,8 @@
 probabilities are rounded to bf16 for their products (2^-8 of sum p |v|), the
 result once more (2^-8 of itself), and the fp32 scores, exponentials and sums keep
 2e-5 of sum p |v|."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -165,3 +167,35 @@ def test_pairs_and_splits(B, H, KV, dh, longest):
     attend(c, rand((B, H * dh), 12))
     c = paged(B, H, KV, dh, 16, length[::-1], 13)
     attend(c, rand((B, H * dh), 14))
+
+
+@pytest.mark.parametrize("longest", [300, 3000])
+def test_visible_nan(longest):
+    """What is not finite and seen reaches the heads that see it, and no others: whole pairs and split ones."""
+    c = paged(2, 4, 2, 64, 16, [40, longest], 21)
+    q = rand((2, 256), 22)
+    ref = c.attend(q)
+    heads = lambda t: t.view(2, 4, 64)
+    K, V = c.K.clone(), c.V.clone()
+    for value in (float("nan"), float("inf")):
+        p = q.clone()
+        heads(p)[1, 3, 5] = value
+        out = c.attend(p)
+        assert heads(out)[1, 3].isnan().all()
+        assert torch.equal(heads(out)[1, :3], heads(ref)[1, :3]) and torch.equal(out[0], ref[0])
+        for row in (0, 17, longest - 1):
+            pg = int(c.table[1, row // 16])
+            c.K[pg, 1, row % 16] = value
+            out = c.attend(q)
+            c.K.copy_(K)
+            if math.isnan(value):
+                assert heads(out)[1, 2:].isnan().all(), row
+            assert torch.equal(heads(out)[1, :2], heads(ref)[1, :2]) and torch.equal(out[0], ref[0])
+            c.V[pg, 1, row % 16, 7] = value
+            out = c.attend(q)
+            c.V.copy_(V)
+            assert not heads(out)[1, 2:, 7].isfinite().any()
+    c.K[c.table[1, :-(-longest // 16)].long(), 1] = float("-inf")
+    out = c.attend(q.abs())
+    check()
+    assert heads(out)[1, 2:].isnan().all()
