@@ -74,6 +74,7 @@ struct PaArgs {
 struct PaSpan {
   int n, lo, ns, tiles, first;  // first: first row inside the window
 };
+__device__ __forceinline__ int pa_tiles(int rows) { return rows / PA_TILE + (rows % PA_TILE != 0); }
 __device__ __forceinline__ PaSpan pa_span(const PaArgs& a, int b) {
   PaSpan s;
   const long cap = (long)a.max_pages * a.page;
@@ -81,9 +82,9 @@ __device__ __forceinline__ PaSpan pa_span(const PaArgs& a, int b) {
   s.n = len < 0 || len > cap ? 0 : len;  // flagged by pa_units
   s.first = a.window > 0 && s.n > a.window ? s.n - a.window : 0;
   s.lo = s.first / PA_TILE;
-  s.ns = min((a.sinks + PA_TILE - 1) / PA_TILE, s.lo);
+  s.ns = min(pa_tiles(a.sinks), s.lo);
   if (a.window <= 0) s.ns = 0;
-  s.tiles = s.ns + (s.n + PA_TILE - 1) / PA_TILE - s.lo;
+  s.tiles = s.ns + pa_tiles(s.n) - s.lo;
   return s;
 }
 
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
           mma16816(s[n], a1, k.z, k.w);
         }
       const int row = tile_row(i);
-      if (row + PA_TILE > sp.n || row < sp.first) {  // the last tile, the sinks', the window's first
+      if (row > sp.n - PA_TILE || row < sp.first) {  // the last tile, the sinks', the window's first
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll

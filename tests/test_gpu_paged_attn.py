@@ -199,3 +199,16 @@ def test_visible_nan(longest):
     out = c.attend(q.abs())
     check()
     assert heads(out)[1, 2:].isnan().all()
+
+
+@pytest.mark.parametrize("n_sink", [(1 << 31) - 16, (1 << 31) - 15, (1 << 31) - 1])
+@pytest.mark.parametrize("longest", [300, 3000])
+def test_more_sinks_than_rows(n_sink, longest):
+    """Any number of sinks, up to the argument's last: every row is seen."""
+    length = [0, 1, 17, 200, longest]
+    c = paged(5, 8, 2, 64, 16, length, 23, window=20, n_sink=n_sink)
+    q = rand((5, 512), 24)
+    out = attend(c, q)
+    c.desc.window = c.desc.n_sink = 0
+    every = attend(c, q)
+    assert not out[0].any() and torch.equal(out[1:3], every[1:3])
