@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
       mbar_arrive_warp(o_free(w));
       // the warp's 32 rows go out by TMA from its own stage (128-byte swizzle; rows past the end
       // of the sequence are left out)
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const float inv = 1.f / l;  // (a row sees itself: 0 where its scores are all -inf, and 0 / 0 is NaN)
       uint8_t* const stg = smem + WA_OFF_STG + (warp - 4) * 4096;
       auto put = [&](const CUtensorMap* map, const uint32_t* v) {  // v: the row, bf16 pairs
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the store before

@@ -212,3 +212,16 @@ def test_many_short_items(B, L, H, KV, window, n_sink):
 def test_few_sinks(n_sink):
     """The last tile of the sinks holds 32 of them at most, or more."""
     step(2, 700, 4, 2, 150, n_sink, 19)
+
+
+def test_scores_of_minus_infinity():
+    """A row without a finite score has no softmax: NaN, as in any row that sees one; the others stay."""
+    q, k, v = rand((300, 64), 1), rand((300, 64), 2).abs() + 0.125, rand((300, 64), 3)
+    op = WindowAttention(1, 300, 1, 1, window=100, n_sink=3)
+    ref = op.forward(q, k, v, train=False)
+    q[140] = float("-inf")
+    out = op.forward(q, k, v, train=False)
+    check()
+    assert out[140].isnan().all()
+    out[140] = ref[140]
+    assert torch.equal(out, ref)
