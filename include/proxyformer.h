@@ -359,8 +359,8 @@ typedef struct {
  *   n_axes, pairs : position axes (0 to 3; 0: no rotation) and the pairs
  *                   (2j, 2j+1) of a head that each turns, one axis after the
  *                   other; at most dh/2 in total, the rest is not turned
- *   theta, eps    : base of the rotation's frequencies, and the norm's epsilon
- *                   (both > 0)                                               */
+ *   theta, eps    : base of the rotation's frequencies (1e-300 to 1e300), and
+ *                   the norm's epsilon (> 0)                                 */
 typedef struct {
   int32_t n_heads, n_kv, dh, dtype;
   int32_t n_axes, pairs[3];
@@ -374,7 +374,8 @@ typedef struct {
  * its sequence, row mod seq_len.  out->q, out->k are written (v is not used)
  * and may be x->q, x->k themselves (same leading dimension) but not overlap
  * them otherwise.  The angle is exact for every int32 position: frequencies
- * are kept as 64-bit fractions of a turn.                                    */
+ * are kept as 64-bit fractions of a turn.  (With theta < 1 some are more than a
+ * turn, and their fractions are as good as double precision has them.)       */
 pf_status pf_qk_rope_fwd(const pf_qk_desc *desc, int64_t rows, int64_t seq_len, const pf_qkv *x,
                          const float *w_q, const float *w_k, const int32_t *pos,
                          const pf_qkv *out, void *stream);

@@ -64,8 +64,8 @@ pf_status check_qk(const pf_qk_desc* s) {
     p += s->pairs[i];
   }
   if (p > s->dh / 2) return fail(PF_ERR_INVALID_ARG, "more pairs than the head holds");
-  if (!(s->theta > 0) || !(s->eps > 0) || s->theta > 1e300)
-    return fail(PF_ERR_INVALID_ARG, "theta and eps must be positive");
+  if (!(s->theta >= 1e-300) || !(s->eps > 0) || s->theta > 1e300)
+    return fail(PF_ERR_INVALID_ARG, "theta must be in [1e-300, 1e300] and eps positive");
   return PF_OK;
 }
 

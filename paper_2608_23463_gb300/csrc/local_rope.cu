@@ -515,7 +515,7 @@ RopeFreq freq_of(const QkRope& s) {
     const double step = std::pow(s.theta, -1.0 / std::max(1, s.pairs[ax]));
     double w = 0.15915494309189535;  // 1 / (2 pi): turns per position of the first pair
     for (int i = 0; i < s.pairs[ax]; ++i, ++p, w *= step) {
-      fr.f[p] = (unsigned long long)std::ldexp(w, 64);
+      fr.f[p] = (unsigned long long)std::ldexp(w - std::floor(w), 64);  // (theta < 1: whole turns count for nothing)
       fr.axis[p] = (unsigned char)ax;
     }
   }

@@ -267,3 +267,15 @@ def test_released_sequences_write_nowhere():
         assert torch.equal(a, b)
     c.reserve([16, 40])
     assert c.len.tolist() == [0, 31]
+
+
+@pytest.mark.parametrize("theta,pairs", [(0.1, (32,)), (1e-3, (32,)), (0.01, (12, 20)), (1e-5, (1, 2, 3))])
+def test_small_theta(theta, pairs):
+    """Frequencies of more than a turn a position."""
+    op = QKRope(2, 1, 64, pairs=pairs, theta=theta, dtype=F32)
+    pos = np.random.default_rng(1).integers(0, 1000, (200, len(pairs)))
+    q, k = rand((200, 128), 2, F32), rand((200, 64), 3, F32)
+    z = op.forward(q, k, pos=torch.from_numpy(pos.astype(np.int32)).cuda())
+    check()
+    for a, b in zip(z, (q, k)):
+        close("turned", a, OL.rope_fwd(f64(b).reshape(200, -1, 64), None, pos, pairs, theta, 1e-6), F32)

@@ -172,3 +172,8 @@ def test_python_refusals():
     refused(bad, lambda: local.PagedKVCache(1, 4, 2, 64, 16, 4, 2, device="cpu"))
     with pytest.raises(TypeError):
         local._local.rope_fwd(1, 2)
+
+
+def test_theta_out_of_range():
+    for theta in (1e-301, 1e301, -1.0, float("inf"), float("nan")):
+        refused(pf.PF_ERR_INVALID_ARG, pf.pf_qk_rope_fwd, qk(theta=theta), 8, 8, rows(), A, A, None, rows(q=2 * A, k=2 * A))
