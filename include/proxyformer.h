@@ -360,7 +360,8 @@ typedef struct {
  *                   (2j, 2j+1) of a head that each turns, one axis after the
  *                   other; at most dh/2 in total, the rest is not turned
  *   theta, eps    : base of the rotation's frequencies (1e-300 to 1e300), and
- *                   the norm's epsilon (> 0)                                 */
+ *                   the norm's epsilon (> 0; less than fp32's least normal
+ *                   number counts as that)                                   */
 typedef struct {
   int32_t n_heads, n_kv, dh, dtype;
   int32_t n_axes, pairs[3];

@@ -546,7 +546,7 @@ RopeArgs args_of(const QkRope& s, const QkvPtr& x, const QkvPtr& o, const float*
   a.seq_len = (int)seq_len;
   a.H = s.H;
   a.KV = s.KV;
-  a.eps = (float)s.eps;
+  a.eps = std::max((float)s.eps, 1.17549435e-38f);  // (fp32's least normal: an eps of 0 made a zero row NaN)
   return a;
 }
 

@@ -279,3 +279,15 @@ def test_small_theta(theta, pairs):
     check()
     for a, b in zip(z, (q, k)):
         close("turned", a, OL.rope_fwd(f64(b).reshape(200, -1, 64), None, pos, pairs, theta, 1e-6), F32)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_eps_below_fp32(dtype):
+    """An epsilon that fp32 does not hold: rows of zeros stay zeros."""
+    op = QKRope(2, 1, 64, *weights(64, 5), eps=1e-60, dtype=dtype)
+    q, k = rand((4, 128), 1, dtype), rand((4, 64), 2, dtype)
+    q[2], k[1] = 0, 0
+    z = op.forward(q, k)
+    check()
+    for a, b, w in zip(z, (q, k), (op.w_q, op.w_k)):
+        close("normed", a, OL.rope_fwd(f64(b).reshape(4, -1, 64), f64(w), np.arange(4)[:, None], (32,), 1e4, 1e-60), dtype)
