@@ -405,7 +405,8 @@ typedef struct {
 
 /* out_h = softmax(q_h K^T / sqrt(dh)) V over the keys that a row sees, key head
  * h / (n_heads/n_kv); rows b*L + i of x and out [batch*L, n_heads*dh] (leading
- * dimension ld_out).  saved: pf_window_attn_saved_size bytes for the backward
+ * dimension ld_out), which may be x->q itself (same leading dimension) but not
+ * overlap x otherwise.  saved: pf_window_attn_saved_size bytes for the backward
  * (the rows' log-sums, and what the rounding of out left), or NULL.
  * Values must be finite: those that a row does not see may be multiplied by
  * zero.                                                                      */
@@ -417,7 +418,7 @@ size_t pf_window_attn_workspace_size(const pf_window_desc *desc);
 
 /* Its backward: dx->q, dx->k, dx->v (overwritten; those of a key head sum over
  * its query heads) from the forward's x, out and saved and the gradient dout of
- * out.  dx may not overlap x, out or dout.                                   */
+ * out.  dx's matrices may not overlap x, out, dout or one another.           */
 pf_status pf_window_attn_bwd(const pf_window_desc *desc, const pf_qkv *x, const void *out,
                              int64_t ld_out, const void *saved, const void *dout,
                              int64_t ld_dout, const pf_qkv *dx, void *ws, size_t ws_bytes,

@@ -38,6 +38,41 @@ pf_status check_rows(const char* name, const void* p, int64_t ld, int64_t width,
   return PF_OK;
 }
 
+// A matrix in memory, in bytes.
+struct Area {
+  const char* name;
+  const void* p;
+  int64_t rows, width, ld;
+};
+
+// Whether two matrices share a byte.  Columns of one wide matrix do not meet.
+bool meet(const Area& a, const Area& b) {
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+  if (pa >= pb + (b.rows - 1) * b.ld + b.width || pb >= pa + (a.rows - 1) * a.ld + a.width) return false;
+  if (a.ld == b.ld) {
+    // b's rows begin at column r of a's rows j, j + 1, ..., and may reach into the rows after those
+    const int64_t d = static_cast<int64_t>(pb - pa);
+    const int64_t j = d >= 0 ? d / a.ld : -((a.ld - 1 - d) / a.ld), r = d - j * a.ld;
+    auto rows = [&](int64_t first) { return first < a.rows && -first < b.rows; };
+    return (r < a.width && rows(j)) || (r + b.width > a.ld && rows(j + 1));
+  }
+  const bool swap = b.rows < a.rows;  // the rows of the one with fewer, among the other's
+  const Area &x = swap ? b : a, &y = swap ? a : b;
+  const uintptr_t px = swap ? pb : pa, py = swap ? pa : pb;
+  for (int64_t i = 0; i < x.rows; ++i) {
+    const int64_t at = static_cast<int64_t>(px - py) + i * x.ld;  // from y's first byte
+    const int64_t k = at < y.width ? 0 : (at - y.width) / y.ld + 1;  // y's first row that ends after it
+    if (k < y.rows && k * y.ld < at + x.width) return true;
+  }
+  return false;
+}
+
+// A result must lie apart from what is read or written beside it.
+pf_status check_apart(const Area& out, const Area& other) {
+  if (!meet(out, other)) return PF_OK;
+  return fail(PF_ERR_INVALID_ARG, "%s overlaps %s", out.name, other.name);
+}
+
 #define PF_TRY(call)                     \
   do {                                   \
     pf_status s_ = (call);               \
@@ -118,6 +153,11 @@ pf_status check_window_rows(const char* what, const pf_qkv* x, const pf_window_d
   PF_TRY(check_rows("q", x->q, x->ld_q, nq, 2));
   PF_TRY(check_rows("k", x->k, x->ld_k, nk, 2));
   return check_rows("v", x->v, x->ld_v, nk, 2);
+}
+
+// The matrices of bf16 heads of a windowed call.
+Area window_area(const pf_window_desc& s, const char* name, const void* p, int64_t ld, int32_t heads) {
+  return {name, p, (int64_t)s.batch * s.L, (int64_t)heads * s.dh * 2, ld * 2};
 }
 
 pf_status check_paged(const pf_paged_desc* s) {
@@ -208,6 +248,11 @@ pf_status pf_window_attn_fwd(const pf_window_desc* desc, const pf_qkv* x, void* 
   PF_TRY(check_window_rows("x", x, *desc));
   PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
   if (!aligned16(saved)) return fail(PF_ERR_INVALID_ARG, "saved must be 16-byte aligned");
+  const Area o = window_area(*desc, "out", out, ld_out, desc->n_heads);
+  if (out != x->q || ld_out != x->ld_q)  // (a tile's queries are read before its rows are written)
+    PF_TRY(check_apart(o, window_area(*desc, "q", x->q, x->ld_q, desc->n_heads)));
+  PF_TRY(check_apart(o, window_area(*desc, "k", x->k, x->ld_k, desc->n_kv)));
+  PF_TRY(check_apart(o, window_area(*desc, "v", x->v, x->ld_v, desc->n_kv)));
   const Window c = window_of(*desc);
   PF_CUDA(window_fwd(c, ptr_of(*x), static_cast<bf16*>(out), (long)ld_out,
                      saved ? window_saved(c, saved) : WindowSaved{}, static_cast<cudaStream_t>(stream)));
@@ -233,15 +278,21 @@ pf_status pf_window_attn_bwd(const pf_window_desc* desc, const pf_qkv* x, const 
   PF_TRY(check_rows("dout", dout, ld_dout, (int64_t)desc->n_heads * desc->dh, 2));
   if (!saved || !aligned16(saved))
     return fail(PF_ERR_INVALID_ARG, "saved is required, 16-byte aligned");
-  for (const void* d : {dx->q, dx->k, dx->v})
-    for (const void* i : {static_cast<const void*>(x->q), static_cast<const void*>(x->k),
-                          static_cast<const void*>(x->v), out, dout})
-      if (d == i) return fail(PF_ERR_INVALID_ARG, "dx may not overlap an input");
   const Window c = window_of(*desc);
   const size_t need = window_bwd_ws_bytes(c);
   if (!ws || !aligned16(ws) || ws_bytes < need)
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need,
                 ws ? ws_bytes : 0);
+  const int32_t H = desc->n_heads, KV = desc->n_kv;
+  const Area grads[] = {window_area(*desc, "dq", dx->q, dx->ld_q, H), window_area(*desc, "dk", dx->k, dx->ld_k, KV),
+                        window_area(*desc, "dv", dx->v, dx->ld_v, KV)};
+  const Area read[] = {window_area(*desc, "q", x->q, x->ld_q, H), window_area(*desc, "k", x->k, x->ld_k, KV),
+                       window_area(*desc, "v", x->v, x->ld_v, KV), window_area(*desc, "out", out, ld_out, H),
+                       window_area(*desc, "dout", dout, ld_dout, H)};
+  for (int i = 0; i < 3; ++i) {
+    for (const Area& r : read) PF_TRY(check_apart(grads[i], r));
+    for (int j = 0; j < i; ++j) PF_TRY(check_apart(grads[i], grads[j]));
+  }
   PF_CUDA(window_bwd(c, ptr_of(*x), static_cast<const bf16*>(out), (long)ld_out,
                      window_saved(c, const_cast<void*>(saved)), static_cast<const bf16*>(dout), (long)ld_dout, ptr_of(*dx), ws,
                      static_cast<cudaStream_t>(stream)));

@@ -225,3 +225,20 @@ def test_scores_of_minus_infinity():
     assert out[140].isnan().all()
     out[140] = ref[140]
     assert torch.equal(out, ref)
+
+
+def test_results_beside_and_over_the_inputs():
+    """Results in the free columns of the inputs' own rows, or over the queries."""
+    B, L = 2, 333
+    x = rand((B * L, 12 * 64), 25)
+    q, k, v, free = x[:, :256], x[:, 256:384], x[:, 384:512], x[:, 512:]
+    op = WindowAttention(B, L, 4, 2, window=100, n_sink=3)
+    ref = op.forward(q, k, v, train=False)
+    assert op.forward(q, k, v, train=False, out=free).data_ptr() == free.data_ptr()
+    op.forward(q, k, v, train=False, out=q)
+    check()
+    assert torch.equal(free, ref) and torch.equal(q, ref)
+    for out in (x[:, 128:384], x[:, 320:576], x[:, 64:320]):
+        with pytest.raises(pf.ProxyFormerError) as e:
+            op.forward(q, k, v, train=False, out=out)
+        assert e.value.status == pf.PF_ERR_INVALID_ARG

@@ -177,3 +177,33 @@ def test_python_refusals():
 def test_theta_out_of_range():
     for theta in (1e-301, 1e301, -1.0, float("inf"), float("nan")):
         refused(pf.PF_ERR_INVALID_ARG, pf.pf_qk_rope_fwd, qk(theta=theta), 8, 8, rows(), A, A, None, rows(q=2 * A, k=2 * A))
+
+
+BASES = dict(q=1 << 28, k=2 << 28, v=3 << 28, out=4 << 28, dout=5 << 28, dq=6 << 28, dk=7 << 28, dv=8 << 28)
+
+
+def row_bytes(ld, **moved):
+    """A matrix's address after another one's: so many rows and bytes on."""
+    return {name: BASES[at] + rows * ld * 2 + b for name, (at, rows, b) in moved.items()}
+
+
+@pytest.mark.parametrize("moved", [
+    dict(out=("k", 0, 0)), dict(out=("v", 0, 0)), dict(out=("k", 599, 0)), dict(out=("v", -599, 0)),
+    dict(out=("q", 0, 16)), dict(out=("q", 1, 0)), dict(out=("k", 0, 240)), dict(out=("k", -1, 528)),
+    dict(q=("out", 0, 256))])
+def test_window_forward_overlaps(moved):
+    """Results over keys and values that other tiles still read, whole or in part; queries only as they are."""
+    at = {**BASES, **row_bytes(512, **moved)}
+    refused(pf.PF_ERR_INVALID_ARG, pf.pf_window_attn_fwd, win(),
+            rows(at["q"], at["k"], at["v"], 512, 512, 512), at["out"], 512, A)
+    refused(pf.PF_ERR_INVALID_ARG, pf.pf_window_attn_fwd, win(),  # leading dimensions that differ
+            rows(at["q"], at["k"], at["v"], 512, 512, 512), at["q"], 520, A)
+
+
+@pytest.mark.parametrize("moved", [
+    dict(dk=("dv", 0, 0)), dict(dq=("dk", 3, 64)), dict(dv=("dq", 0, 496)), dict(dk=("k", 0, 64)), dict(dq=("q", 5, 0)),
+    dict(dv=("out", 0, 256)), dict(dq=("dout", -2, -16)), dict(dk=("dv", 599, 0))])
+def test_window_backward_overlaps(moved):
+    at = {**BASES, **row_bytes(512, **moved)}
+    refused(pf.PF_ERR_INVALID_ARG, pf.pf_window_attn_bwd, win(), rows(at["q"], at["k"], at["v"], 512, 512, 512),
+            at["out"], 512, A, at["dout"], 512, rows(at["dq"], at["dk"], at["dv"], 512, 512, 512), A, 1 << 40)
