@@ -386,7 +386,8 @@ size_t pf_qk_rope_workspace_size(const pf_qk_desc *desc);
 /* Its backward: dx from the gradients dout of out, and the norms' gradients
  * dw_q, dw_k [dh] fp32 (overwritten; NULL where w_q, w_k is NULL, or where not
  * wanted).  x: the forward's input (of a head without norm it is not read).
- * dx->q, dx->k may be dout->q, dout->k.  ws: pf_qk_rope_workspace_size bytes,
+ * dx->q, dx->k may be dout->q, dout->k or x->q, x->k (same leading dimension)
+ * but not overlap them otherwise.  ws: pf_qk_rope_workspace_size bytes,
  * may be NULL without dw_q and dw_k.                                         */
 pf_status pf_qk_rope_bwd(const pf_qk_desc *desc, int64_t rows, int64_t seq_len, const pf_qkv *x,
                          const float *w_q, const float *w_k, const int32_t *pos,
@@ -464,7 +465,8 @@ pf_status pf_paged_advance(const pf_paged_desc *desc, const int32_t *start, pf_p
  * one token for each sequence, rows = batch.  Keys are normed and rotated on
  * the way as in pf_qk_rope_fwd, at the token's row in the sequence or, given,
  * at pos [rows, n_axes]; values are copied.  q_out [rows, n_heads*dh]: the
- * queries, normed and rotated (x->q and q_out may be NULL; q_out may be x->q).
+ * queries, normed and rotated (x->q and q_out may be NULL; q_out may be x->q but
+ * not overlap x otherwise).
  * qk: norm and rotation; its heads must be desc's.  A token whose row or page
  * is out of range is left out and flagged (PF_ERR_CAPACITY via pf_sync_check).
  */
@@ -476,7 +478,8 @@ pf_status pf_paged_append(const pf_paged_desc *desc, const pf_qk_desc *qk, int64
 size_t pf_paged_attn_workspace_size(const pf_paged_desc *desc);
 
 /* Attention of every sequence's newest token, with queries q [batch,
- * n_heads*dh] (leading dimension ld_q), over the rows that it sees:
+ * n_heads*dh] (leading dimension ld_q; out may be q but not overlap it
+ * otherwise), over the rows that it sees:
  *   out_h = softmax(q_h K^T / sqrt(dh)) V,   key head h / (n_heads/n_kv).
  * A sequence without rows gives zeros.  A length or page out of range is
  * flagged (PF_ERR_CAPACITY via pf_sync_check); such rows are not read.  The

@@ -121,6 +121,36 @@ pf_status check_qk_rows(const char* what, const pf_qkv* x, const pf_qk_desc& s) 
   return check_rows("k", x->k, x->ld_k, (int64_t)s.n_kv * s.dh, size);
 }
 
+Area head_area(const char* name, const void* p, int64_t rows, int64_t ld, int32_t heads, int32_t dh, int size) {
+  return {name, p, rows, (int64_t)heads * dh * size, ld * size};
+}
+
+// A result that may lie over the input that it comes from, value for value.
+pf_status check_over(const Area& out, const Area& from) {
+  if (out.p == from.p && (out.ld == from.ld || out.rows == 1)) return PF_OK;
+  return check_apart(out, from);
+}
+
+// Results of queries and keys: each may lie over its own input, and apart from all else
+// that is read (read_q, read_k: of `in`, what is).
+pf_status check_qk_results(const pf_qk_desc& s, int64_t rows, const pf_qkv& out, const pf_qkv& in, bool read_q,
+                           bool read_k) {
+  const int size = s.dtype == PF_F32 ? 4 : 2;
+  const Area oq = head_area("the result q", out.q, rows, out.ld_q, s.n_heads, s.dh, size),
+             ok = head_area("the result k", out.k, rows, out.ld_k, s.n_kv, s.dh, size),
+             q = head_area("q", in.q, rows, in.ld_q, s.n_heads, s.dh, size),
+             k = head_area("k", in.k, rows, in.ld_k, s.n_kv, s.dh, size);
+  if (read_q) {
+    PF_TRY(check_over(oq, q));
+    PF_TRY(check_apart(ok, q));
+  }
+  if (read_k) {
+    PF_TRY(check_over(ok, k));
+    PF_TRY(check_apart(oq, k));
+  }
+  return check_apart(oq, ok);
+}
+
 pf_status check_count(int64_t rows, int64_t seq_len, const int32_t* pos, int n_axes) {
   if (rows < 0 || rows > 0x7fffffff) return fail(PF_ERR_INVALID_ARG, "rows must be in [0, 2^31)");
   if (!pos && n_axes > 1) return fail(PF_ERR_INVALID_ARG, "several axes need positions");
@@ -157,7 +187,7 @@ pf_status check_window_rows(const char* what, const pf_qkv* x, const pf_window_d
 
 // The matrices of bf16 heads of a windowed call.
 Area window_area(const pf_window_desc& s, const char* name, const void* p, int64_t ld, int32_t heads) {
-  return {name, p, (int64_t)s.batch * s.L, (int64_t)heads * s.dh * 2, ld * 2};
+  return head_area(name, p, (int64_t)s.batch * s.L, ld, heads, s.dh, 2);
 }
 
 pf_status check_paged(const pf_paged_desc* s) {
@@ -207,6 +237,7 @@ pf_status pf_qk_rope_fwd(const pf_qk_desc* desc, int64_t rows, int64_t seq_len, 
   if (rows == 0) return PF_OK;
   PF_TRY(check_qk_rows("x", x, *desc));
   PF_TRY(check_qk_rows("out", out, *desc));
+  PF_TRY(check_qk_results(*desc, rows, *out, *x, true, true));
   PF_CUDA(qk_rope_fwd(rope_of(*desc), ptr_of(*x), ptr_of(*out), w_q, w_k, pos, rows, seq_len,
                       static_cast<cudaStream_t>(stream)));
   return PF_OK;
@@ -237,6 +268,8 @@ pf_status pf_qk_rope_bwd(const pf_qk_desc* desc, int64_t rows, int64_t seq_len, 
   if (dw && (!ws || !aligned16(ws) || ws_bytes < qk_rope_part_bytes(desc->dh)))
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu",
                 qk_rope_part_bytes(desc->dh), ws ? ws_bytes : 0);
+  PF_TRY(check_qk_results(*desc, rows, *dx, *dout, true, true));
+  PF_TRY(check_qk_results(*desc, rows, *dx, *x, w_q != nullptr, w_k != nullptr));
   PF_CUDA(qk_rope_bwd(rope_of(*desc), ptr_of(*x), ptr_of(*dout), ptr_of(*dx), w_q, w_k, pos, dw_q,
                       dw_k, static_cast<float*>(ws), rows, seq_len, cs));
   return PF_OK;
@@ -249,8 +282,8 @@ pf_status pf_window_attn_fwd(const pf_window_desc* desc, const pf_qkv* x, void* 
   PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
   if (!aligned16(saved)) return fail(PF_ERR_INVALID_ARG, "saved must be 16-byte aligned");
   const Area o = window_area(*desc, "out", out, ld_out, desc->n_heads);
-  if (out != x->q || ld_out != x->ld_q)  // (a tile's queries are read before its rows are written)
-    PF_TRY(check_apart(o, window_area(*desc, "q", x->q, x->ld_q, desc->n_heads)));
+  // (a tile's queries are read before its rows are written)
+  PF_TRY(check_over(o, window_area(*desc, "q", x->q, x->ld_q, desc->n_heads)));
   PF_TRY(check_apart(o, window_area(*desc, "k", x->k, x->ld_k, desc->n_kv)));
   PF_TRY(check_apart(o, window_area(*desc, "v", x->v, x->ld_v, desc->n_kv)));
   const Window c = window_of(*desc);
@@ -331,6 +364,12 @@ pf_status pf_paged_append(const pf_paged_desc* desc, const pf_qk_desc* qk, int64
   }
   PF_TRY(check_rows("k", x->k, x->ld_k, (int64_t)desc->n_kv * desc->dh, 2));
   PF_TRY(check_rows("v", x->v, x->ld_v, (int64_t)desc->n_kv * desc->dh, 2));
+  if (q_out) {
+    const Area o = head_area("q_out", q_out, rows, ld_q_out, desc->n_heads, desc->dh, 2);
+    PF_TRY(check_over(o, head_area("q", x->q, rows, x->ld_q, desc->n_heads, desc->dh, 2)));
+    PF_TRY(check_apart(o, head_area("k", x->k, rows, x->ld_k, desc->n_kv, desc->dh, 2)));
+    PF_TRY(check_apart(o, head_area("v", x->v, rows, x->ld_v, desc->n_kv, desc->dh, 2)));
+  }
   QkRope r = rope_of(*qk);
   if (!q_out) r.H = 0;
   PF_CUDA(paged_append(r, paged_of(*desc, cache), ptr_of(*x), static_cast<bf16*>(q_out), (long)ld_q_out,
@@ -354,6 +393,9 @@ pf_status pf_paged_attn(const pf_paged_desc* desc, const void* q, int64_t ld_q,
   if (!ws || !aligned16(ws) || ws_bytes < need)
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need,
                 ws ? ws_bytes : 0);
+  // (a head's query is read before its row is written)
+  PF_TRY(check_over(head_area("out", out, desc->batch, ld_out, desc->n_heads, desc->dh, 2),
+                    head_area("q", q, desc->batch, ld_q, desc->n_heads, desc->dh, 2)));
   PF_CUDA(paged_attn(p, static_cast<const bf16*>(q), (long)ld_q, static_cast<bf16*>(out), (long)ld_out,
                      static_cast<float*>(ws), static_cast<cudaStream_t>(stream)));
   return PF_OK;

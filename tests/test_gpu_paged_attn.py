@@ -212,3 +212,18 @@ def test_more_sinks_than_rows(n_sink, longest):
     c.desc.window = c.desc.n_sink = 0
     every = attend(c, q)
     assert not out[0].any() and torch.equal(out[1:3], every[1:3])
+
+
+def test_results_over_the_queries():
+    for longest in (300, 3000):
+        c = paged(3, 4, 2, 64, 16, [40, 0, longest], 25)
+        x = rand((3, 512), 26)
+        ref = c.attend(x[:, :256])
+        assert c.attend(x[:, :256], out=x[:, :256]).data_ptr() == x.data_ptr()
+        y = rand((3, 512), 27)
+        z = c.append(y[:, :256], y[:, 256:384], y[:, 384:])
+        c.append(y[:, :256], y[:, 256:384], y[:, 384:], out=y[:, :256])
+        with pytest.raises(pf.ProxyFormerError) as e:  # (the second sequence has no row)
+            check()
+        assert e.value.status == pf.PF_ERR_CAPACITY
+        assert torch.equal(x[:, :256], ref) and torch.equal(y[:, :256], z)

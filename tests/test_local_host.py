@@ -207,3 +207,28 @@ def test_window_backward_overlaps(moved):
     at = {**BASES, **row_bytes(512, **moved)}
     refused(pf.PF_ERR_INVALID_ARG, pf.pf_window_attn_bwd, win(), rows(at["q"], at["k"], at["v"], 512, 512, 512),
             at["out"], 512, A, at["dout"], 512, rows(at["dq"], at["dk"], at["dv"], 512, 512, 512), A, 1 << 40)
+
+
+@pytest.mark.parametrize("moved", [
+    dict(dq=("q", 0, 16)), dict(dq=("k", 0, 0)), dict(dk=("q", 1, 0)), dict(dk=("k", -1, 0)), dict(dq=("dk", 7, 240)),
+    dict(dk=("dq", 0, 256))])
+def test_rope_overlaps(moved):
+    """Each result over its own input or apart from all."""
+    at = {**BASES, **row_bytes(512, **moved)}
+    z, dz = (rows(at[a], at[b], 0, 512, 512) for a, b in (("q", "k"), ("dq", "dk")))
+    far = rows(9 << 28, 10 << 28, 0, 512, 512)
+    bad = pf.PF_ERR_INVALID_ARG
+    refused(bad, pf.pf_qk_rope_fwd, qk(), 8, 8, z, A, A, None, dz)
+    refused(bad, pf.pf_qk_rope_bwd, qk(), 8, 8, z, A, A, None, far, dz, None, None, None, 0)
+    refused(bad, pf.pf_qk_rope_bwd, qk(), 8, 8, far, A, A, None, z, dz, None, None, None, 0)
+    refused(bad, pf.pf_qk_rope_fwd, qk(), 8, 8, z, A, A, None, rows(at["q"], 11 << 28, 0, 520, 512))
+
+
+@pytest.mark.parametrize("moved", [dict(out=("q", 0, 16)), dict(out=("k", 0, 0)), dict(out=("v", 2, 240)), dict(out=("q", -1, 0))])
+def test_paged_overlaps(moved):
+    at = {**BASES, **row_bytes(512, **moved)}
+    x, bad = rows(at["q"], at["k"], at["v"], 512, 512, 512), pf.PF_ERR_INVALID_ARG
+    refused(bad, pf.pf_paged_append, paged(), qk(), 3, x, A, A, None, None, cache(), at["out"], 512)
+    if "q" in {m[0] for m in moved.values()}:
+        refused(bad, pf.pf_paged_attn, paged(), at["q"], 512, cache(), at["out"], 512, A, 1 << 30)
+    refused(bad, pf.pf_paged_attn, paged(), at["q"], 512, cache(), at["q"], 520, A, 1 << 30)
