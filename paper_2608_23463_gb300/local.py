@@ -30,6 +30,14 @@ except ImportError as e:
 _local.init(ProxyFormerError)
 
 
+def _workspace(ws: Optional[torch.Tensor], size, desc, q) -> Optional[torch.Tensor]:
+    """ws, or a new one of size(desc) bytes where it is not on q's GPU.  (What is no tensor on
+    a GPU has none: the call refuses it.)"""
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or (ws is not None and ws.device == q.device):
+        return ws
+    return torch.empty(size(desc), dtype=torch.uint8, device=q.device)
+
+
 class QKRope:
     """RMSNorm of every query and key head (with weights w_q, w_k [dh]; None: no
     norm) and its position rotation: ``pairs`` pairs of a head for every position
@@ -66,9 +74,8 @@ class QKRope:
         """From the forward's inputs and the gradients of its results: the gradients
         of q and k (into ``out``, which may be (dq, dk) itself) and of w_q and w_k
         (None without them)."""
-        if self.ws is None and (self.w_q is not None or self.w_k is not None):
-            self.ws = torch.empty(pf_qk_rope_workspace_size(self.desc), dtype=torch.uint8,
-                                  device=q.device)
+        if self.w_q is not None or self.w_k is not None:
+            self.ws = _workspace(self.ws, pf_qk_rope_workspace_size, self.desc, q)
         oq, ok = (None, None) if out is None else out
         return _local.rope_bwd(self.at, q, k, dq, dk, L, self.w_q, self.w_k, pos, oq, ok, self.ws)
 
@@ -100,9 +107,7 @@ class WindowAttention:
         """From the forward's inputs and result and the gradient of the result: the
         gradients of q, k and v (into ``into``, three matrices, if given).  saved: that
         forward's ``self.saved``, if another forward has run since."""
-        if self.ws is None:
-            self.ws = torch.empty(pf_window_attn_workspace_size(self.desc), dtype=torch.uint8,
-                                  device=q.device)
+        self.ws = _workspace(self.ws, pf_window_attn_workspace_size, self.desc, q)
         dq, dk, dv = (None, None, None) if into is None else into
         return _local.window_bwd(self.at, q, k, v, out, dout, self.saved if saved is None else saved,
                                  dq, dk, dv, self.ws)

@@ -242,3 +242,18 @@ def test_results_beside_and_over_the_inputs():
         with pytest.raises(pf.ProxyFormerError) as e:
             op.forward(q, k, v, train=False, out=out)
         assert e.value.status == pf.PF_ERR_INVALID_ARG
+
+
+def test_backward_after_refusals():
+    """A refused call leaves nothing behind that a later one stumbles over."""
+    q, k = rand((8, 256), 1), rand((8, 128), 2)
+    rope, att = QKRope(4, 2, 64, *(rand((64,), s, torch.float32) for s in (3, 4))), WindowAttention(1, 8, 4, 2)
+    out = att.forward(q, k, k)
+    for bad in (q.cpu(), None, 7):
+        for f in (lambda: rope.backward(bad, k, q, k), lambda: att.backward(bad, k, k, out, q)):
+            with pytest.raises(pf.ProxyFormerError) as e:
+                f()
+            assert e.value.status == pf.PF_ERR_INVALID_ARG
+    rope.backward(q, k, q, k)
+    att.backward(q, k, k, out, q)
+    check()

@@ -232,3 +232,16 @@ def test_paged_overlaps(moved):
     if "q" in {m[0] for m in moved.values()}:
         refused(bad, pf.pf_paged_attn, paged(), at["q"], 512, cache(), at["out"], 512, A, 1 << 30)
     refused(bad, pf.pf_paged_attn, paged(), at["q"], 512, cache(), at["q"], 520, A, 1 << 30)
+
+
+@pytest.mark.parametrize("x", ["cpu", "shape", None, 7])
+def test_refused_backward_keeps_no_workspace(x):
+    torch = pytest.importorskip("torch")
+    from paper_2608_23463_gb300 import local
+    q, k = torch.zeros(8, 256, dtype=torch.bfloat16), torch.zeros(8, 128, dtype=torch.bfloat16)
+    x = q if x == "cpu" else q[:, :128] if x == "shape" else x
+    att, rope = local.WindowAttention(1, 8, 4, 2), local.QKRope(4, 2, 64)
+    rope.w_q = torch.ones(64)  # (a norm's weights on the CPU are refused where the object is made)
+    refused(pf.PF_ERR_INVALID_ARG, att.backward, x, k, k, q, q)
+    refused(pf.PF_ERR_INVALID_ARG, rope.backward, x, k, q, k)
+    assert att.ws is None and rope.ws is None
