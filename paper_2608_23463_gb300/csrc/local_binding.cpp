@@ -6,6 +6,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -78,6 +79,8 @@ T* values(const char* name, PyObject* o, at::IntArrayRef shape, at::ScalarType t
   return static_cast<T*>(t.data_ptr());
 }
 
+// Scratch of an object, read and written on the current stream.  The object may drop it while
+// that stream still uses it: its memory then waits for the stream, whichever it was made on.
 void* bytes(const char* name, PyObject* o, c10::Device dev, size_t* n) {
   if (none(o)) {
     *n = 0;
@@ -86,6 +89,8 @@ void* bytes(const char* name, PyObject* o, c10::Device dev, size_t* n) {
   const at::Tensor& t = tensor(name, o);
   if (t.scalar_type() != at::kByte || t.device() != dev || !t.is_contiguous())
     raise(PF_ERR_INVALID_ARG, std::string(name) + " must be contiguous bytes on the tensors' GPU");
+  c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(),
+                                                c10::cuda::getCurrentCUDAStream(dev.index()));
   *n = (size_t)t.numel();
   return t.data_ptr();
 }

@@ -96,7 +96,8 @@ class WindowAttention:
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """q [batch*L, n_heads*dh], k, v [batch*L, n_kv*dh] -> [batch*L, n_heads*dh];
         ``train`` keeps what the backward needs beside them."""
-        # (saved is a new buffer: the last forward's may still be read on another stream)
+        # (saved is a new buffer: the last forward's may still be read on another stream, for
+        # which its memory waits)
         out, saved = _local.window_fwd(self.at, q, k, v, out, self.saved_size if train else 0)
         if train:
             self.saved = saved

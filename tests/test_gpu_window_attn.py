@@ -257,3 +257,25 @@ def test_backward_after_refusals():
     rope.backward(q, k, q, k)
     att.backward(q, k, k, out, q)
     check()
+
+
+def test_what_another_stream_reads():
+    """What the forward saved and the workspace are dropped while a backward on another stream still has to read them."""
+    q, do = rand((3000, 256), 1), rand((3000, 256), 2)
+    k, v = rand((3000, 128), 3), rand((3000, 128), 4)
+    op = WindowAttention(1, 3000, 4, 2, window=200, n_sink=4)
+    out = op.forward(q, k, v)
+    ref = op.backward(q, k, v, out, do)
+    torch.cuda.synchronize()
+    side, sizes = torch.cuda.Stream(), (op.saved_size, op.ws.numel())
+    fill = lambda n: torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    fill(16)  # (a first launch would wait for the other stream)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1_000_000_000)  # about half a second
+        d = op.backward(q, k, v, out, do)
+    op.saved = op.ws = None
+    junk = [fill(n) for n in sizes for _ in range(40)]
+    assert not side.query()
+    torch.cuda.synchronize()
+    check()
+    assert all(torch.equal(a, b) for a, b in zip(d, ref)) and junk
