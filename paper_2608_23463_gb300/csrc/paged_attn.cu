@@ -156,8 +156,10 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
   extern __shared__ __align__(128) unsigned char ring[];
   __shared__ int pre[PA_MAX_B + 1];
   pdl_enter();
-  // the join's CTAs may take their places now: they wait for this grid to end,
-  // and all of its CTAs are running
+  // the next kernel's CTAs may take their places now: they wait for this grid to end, and
+  // all of its CTAs are running.  That is the join, or (whole pairs) mostly the next layer's
+  // append, as small: a layer's append and attention, captured, 8 sequences of 60 rows 5.75 us
+  // so and 6.28 without, 300 of 200 8.3 and 8.7, 256 of 1000 (2048 CTAs) 164.4 and 163.0
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gid = lane >> 2, t = lane & 3;
