@@ -35,6 +35,17 @@ def _sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 
 
+def binding_tag() -> str:
+    """Interpreter and torch that local_binding.cpp is compiled for: its object's name and its
+    module's ``built_for`` hold them, so that an upgrade of either takes effect."""
+    import torch
+    return f"{sys.implementation.cache_tag}-torch-{torch.__version__}"
+
+
+def binding_object() -> str:
+    return os.path.join(OUT_DIR, f"local_binding.{binding_tag()}.o")
+
+
 def _compile_binding(obj: str) -> None:
     """local_binding.cpp against the headers of the installed torch."""
     import sysconfig
@@ -46,6 +57,7 @@ def _compile_binding(obj: str) -> None:
             sysconfig.get_paths()["include"], cuda]
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DPF_BUILT_FOR="{binding_tag()}"',
            *(f"-I{d}" for d in dirs), "-c", os.path.join(CSRC, "local_binding.cpp"), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
@@ -87,7 +99,7 @@ def build(verbose: bool = False, extra_flags=()) -> str:
             print(r.stderr, file=sys.stderr)
         return obj
 
-    bind_src, bind_obj = (os.path.join(d, "local_binding" + e) for d, e in ((CSRC, ".cpp"), (OUT_DIR, ".o")))
+    bind_src, bind_obj = os.path.join(CSRC, "local_binding.cpp"), binding_object()
     bind_deps = max(os.path.getmtime(bind_src), os.path.getmtime(deps[-1]))
 
     with ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:

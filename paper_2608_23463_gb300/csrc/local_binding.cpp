@@ -342,4 +342,11 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_local", nullptr, -1, kMethods};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__local() { return PyModule_Create(&kModule); }
+PyMODINIT_FUNC PyInit__local() {
+  PyObject* m = PyModule_Create(&kModule);
+  if (m && PyModule_AddStringConstant(m, "built_for", PF_BUILT_FOR) < 0) {
+    Py_DECREF(m);
+    m = nullptr;
+  }
+  return m;
+}

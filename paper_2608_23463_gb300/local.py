@@ -20,10 +20,13 @@ from . import (PF_BF16, PF_ERR_CAPACITY, PF_ERR_CUDA, PF_ERR_INVALID_ARG, PF_F32
                PagedDesc, ProxyFormerError, QKDesc, WindowDesc, load, pf_paged_advance,
                pf_paged_attn_workspace_size, pf_qk_rope_workspace_size, pf_window_attn_saved_size,
                pf_window_attn_workspace_size)
+from .buildlib import binding_tag
 
 load()
 try:
     from . import _local
+    if getattr(_local, "built_for", None) != binding_tag():
+        raise ImportError(f"_local.so was built for {getattr(_local, 'built_for', 'another')}")
 except ImportError as e:
     raise ProxyFormerError(PF_ERR_CUDA, "_local.so is not built for this interpreter and torch; run "
                            "`python -m paper_2608_23463_gb300.buildlib`") from e

@@ -245,3 +245,20 @@ def test_refused_backward_keeps_no_workspace(x):
     refused(pf.PF_ERR_INVALID_ARG, att.backward, x, k, k, q, q)
     refused(pf.PF_ERR_INVALID_ARG, rope.backward, x, k, q, k)
     assert att.ws is None and rope.ws is None
+
+
+def test_binding_of_another_torch(monkeypatch):
+    """The extension module is compiled again for another torch, and one that is not is refused."""
+    torch = pytest.importorskip("torch")
+    import importlib
+
+    from paper_2608_23463_gb300 import buildlib, local
+    here = buildlib.binding_object()
+    assert local._local.built_for == buildlib.binding_tag() and torch.__version__ in here
+    monkeypatch.setattr(torch, "__version__", "0.1+other")
+    assert buildlib.binding_object() != here
+    with pytest.raises(pf.ProxyFormerError) as e:
+        importlib.reload(local)
+    assert "_local.so" in str(e.value)
+    monkeypatch.undo()
+    importlib.reload(local)
