@@ -190,9 +190,10 @@ class PagedKVCache:
     def advance(self, start: Optional[torch.Tensor] = None) -> None:
         """The lengths at the start of a step: start[b+1] - start[b] more rows of
         every sequence b, or one."""
-        if start is not None and (tuple(start.shape) != (self.batch + 1,) or not start.is_cuda
+        if start is not None and (not isinstance(start, torch.Tensor) or start.device != self.len.device
+                                  or tuple(start.shape) != (self.batch + 1,)
                                   or start.dtype != torch.int32 or not start.is_contiguous()):
-            raise ProxyFormerError(PF_ERR_INVALID_ARG, "start must be batch + 1 int32 values on the GPU")
+            raise ProxyFormerError(PF_ERR_INVALID_ARG, "start must be batch + 1 int32 values on the cache's GPU")
         with torch.cuda.device(self.len.device):
             pf_paged_advance(self.desc, start, self.cache, torch.cuda.current_stream().cuda_stream)
 

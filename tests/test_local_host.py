@@ -262,3 +262,16 @@ def test_binding_of_another_torch(monkeypatch):
     assert "_local.so" in str(e.value)
     monkeypatch.undo()
     importlib.reload(local)
+
+
+def test_advance_refuses_other_devices():
+    """start on another device than the lengths, or no tensor, before anything is launched."""
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+
+    from paper_2608_23463_gb300 import local
+    c = local.PagedKVCache.__new__(local.PagedKVCache)
+    c.batch, c.len = 2, SimpleNamespace(device=torch.device("cuda", 1))
+    other = torch.zeros(3, dtype=torch.int32, device="meta")
+    for start in (other, torch.zeros(3, dtype=torch.int32), [0, 1, 2], 7):
+        refused(pf.PF_ERR_INVALID_ARG, c.advance, start)
