@@ -35,7 +35,8 @@
 
 namespace pf {
 
-int take_dev_error_local_rope() { return take_dev_error_tu(); }
+static Launched launched;
+int take_dev_error_local_rope() { return launched.take(take_dev_error_tu); }
 int set_wait_limit_local_rope(unsigned long long ns) { return set_wait_limit_tu(ns); }
 
 namespace {
@@ -559,6 +560,7 @@ int rope_grid(const RopeArgs& a, int per_sm) {
 cudaError_t qk_rope_fwd(const QkRope& s, const QkvPtr& x, const QkvPtr& o, const float* w_q,
                         const float* w_k, const int* pos, long rows, long seq_len,
                         cudaStream_t st) {
+  launched.mark();
   RopeArgs a = args_of(s, x, o, w_q, w_k, pos, rows, seq_len);
   set_parts(a, s, false);
   const double n = (double)rows * (s.H + s.KV) * s.dh;
@@ -574,6 +576,7 @@ size_t qk_rope_part_bytes(int dh) { return (size_t)RW_BWD_CTAS * RW_SMS * 2 * dh
 cudaError_t qk_rope_bwd(const QkRope& s, const QkvPtr& x, const QkvPtr& dout, const QkvPtr& dx,
                         const float* w_q, const float* w_k, const int* pos, float* dw_q,
                         float* dw_k, float* part, long rows, long seq_len, cudaStream_t st) {
+  launched.mark();
   RopeArgs a = args_of(s, x, dx, w_q, w_k, pos, rows, seq_len);
   a.dqo = dout.q;
   a.dko = dout.k;
@@ -598,6 +601,7 @@ cudaError_t qk_rope_bwd(const QkRope& s, const QkvPtr& x, const QkvPtr& dout, co
 cudaError_t paged_append(const QkRope& s, const Paged& c, const QkvPtr& x, bf16* q_out, long ldqo,
                          const float* w_q, const float* w_k, const int* start, const int* pos,
                          long rows, cudaStream_t st) {
+  launched.mark();
   QkvPtr o{};
   o.q = q_out;
   o.ldq = ldqo;
@@ -615,6 +619,7 @@ cudaError_t paged_append(const QkRope& s, const Paged& c, const QkvPtr& x, bf16*
 }
 
 cudaError_t paged_advance(const Paged& c, const int* start, int* len, cudaStream_t st) {
+  launched.mark();
   LaunchTimer lt("paged_advance", st, 0.0, 12.0 * c.B);
   const long cap = std::min<long>((long)c.max_pages * c.page, 0x7fffffffL);
   return launch_kernel(paged_advance_kernel, (c.B + 127) / 128, 128, 0, st, start, len, c.B, (int)cap);

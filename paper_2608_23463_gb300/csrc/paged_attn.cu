@@ -33,7 +33,8 @@
 
 namespace pf {
 
-int take_dev_error_paged_attn() { return take_dev_error_tu(); }
+static Launched launched;
+int take_dev_error_paged_attn() { return launched.take(take_dev_error_tu); }
 int set_wait_limit_paged_attn(unsigned long long ns) { return set_wait_limit_tu(ns); }
 
 namespace {
@@ -510,6 +511,7 @@ size_t paged_attn_ws_bytes(const Paged& c) {
 
 cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long ldo, float* ws,
                        cudaStream_t st) {
+  launched.mark();
   PaArgs a{};
   a.q = q;
   a.ldq = ldq;

@@ -58,7 +58,8 @@
 
 namespace pf {
 
-int take_dev_error_window_attn() { return take_dev_error_tu(); }
+static Launched launched;
+int take_dev_error_window_attn() { return launched.take(take_dev_error_tu); }
 int set_wait_limit_window_attn(unsigned long long ns) { return set_wait_limit_tu(ns); }
 
 namespace {
@@ -572,6 +573,7 @@ WindowSaved window_saved(const Window& c, void* p) {
 
 cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, const WindowSaved& v,
                        cudaStream_t st) {
+  launched.mark();
   CUtensorMap tq, tk, tv, to, tr;
   if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WA_D, c.L, c.B, x.ldq, WA_D, WT) ||
       !tmap_bf16_seq(&tk, x.k, (uint64_t)c.KV * WA_D, c.L, c.B, x.ldk, WA_D, WT) ||

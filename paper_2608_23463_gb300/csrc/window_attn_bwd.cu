@@ -57,7 +57,8 @@
 
 namespace pf {
 
-int take_dev_error_window_attn_bwd() { return take_dev_error_tu(); }
+static Launched launched;
+int take_dev_error_window_attn_bwd() { return launched.take(take_dev_error_tu); }
 int set_wait_limit_window_attn_bwd(unsigned long long ns) { return set_wait_limit_tu(ns); }
 
 namespace {
@@ -780,6 +781,7 @@ size_t window_bwd_ws_bytes(const Window& c) { return wb_carve(nullptr, c).bytes;
 cudaError_t window_bwd(const Window& c, const QkvPtr& x, const bf16* out, long ldo,
                        const WindowSaved& v, const bf16* dout, long lddo, const QkvPtr& dx, void* ws,
                        cudaStream_t st) {
+  launched.mark();
   CUtensorMap tq, tk, tv, td, te, gq, gk, gv;
   if (!tmap_bf16_seq(&tq, x.q, (uint64_t)c.H * WB_D, c.L, c.B, x.ldq, WB_D, WT) ||
       !tmap_bf16_seq(&tk, x.k, (uint64_t)c.KV * WB_D, c.L, c.B, x.ldk, WB_D, WT) ||
