@@ -372,12 +372,6 @@ def proxy_segments_bwd(desc, segs, shared, seg_params, X, saved, dX_out, dX, gra
                                      stream))
 
 
-def qkv(q=None, k=None, v=None) -> QKV:
-    """pf_qkv of 2D tensors (their row strides are the leading dimensions)."""
-    ld = lambda t: 0 if t is None else int(t.stride(0))
-    return QKV(_ptr(q), _ptr(k), _ptr(v), ld(q), ld(k), ld(v))
-
-
 def pf_qk_rope_fwd(desc, rows, seq_len, x, w_q, w_k, pos, out, stream=None):
     _check(load().pf_qk_rope_fwd(ctypes.byref(desc), int(rows), int(seq_len), ctypes.byref(x),
                                  _ptr(w_q), _ptr(w_k), _ptr(pos), ctypes.byref(out), stream))
