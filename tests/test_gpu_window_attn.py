@@ -11,6 +11,7 @@ import paper_2608_23463_gb300 as pf
 from oracle import local as OL
 from paper_2608_23463_gb300.local import PagedKVCache, QKRope, WindowAttention
 from tests.test_gpu_local_rope import BF, check, f64, rand
+from tests.test_local_gradients import CASES, difference, inputs
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -8 * 1.01
@@ -279,3 +280,20 @@ def test_what_another_stream_reads():
     torch.cuda.synchronize()
     check()
     assert all(torch.equal(a, b) for a, b in zip(d, ref)) and junk
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_gradients_along_themselves(case):
+    """dq, dk and dv against differences of the forward along each of them: the bar of test_local_gradients, which
+    tells a wrong sign, a wrong factor and a missing Di from the right gradient."""
+    B, L, H, KV, window, n_sink = case
+    op = WindowAttention(B, L, H, KV, window=window, n_sink=n_sink)
+    dev = lambda t: torch.from_numpy(t).to("cuda", BF).view(B * L, -1)
+    *x, do = inputs(case)
+    out = op.forward(*map(dev, x))
+    grads = op.backward(*map(dev, x), out, dev(do))
+    check()
+    forward = lambda *y: f64(op.forward(*map(dev, y), train=False)).reshape(do.shape)
+    for i, d in enumerate(grads):
+        got, want, bar = difference(forward, x, i, f64(d).reshape(x[i].shape), do)
+        assert abs(got - want) <= bar, (i, got, want, bar)
