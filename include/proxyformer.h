@@ -406,11 +406,10 @@ typedef struct {
 
 /* out_h = softmax(q_h K^T / sqrt(dh)) V over the keys that a row sees, key head
  * h / (n_heads/n_kv); rows b*L + i of x and out [batch*L, n_heads*dh] (leading
- * dimension ld_out), which may be x->q itself (same leading dimension) but not
- * overlap x otherwise.  saved: pf_window_attn_saved_size bytes for the backward
- * (the rows' log-sums, and what the rounding of out left), or NULL.
- * Values must be finite: those that a row does not see may be multiplied by
- * zero.                                                                      */
+ * dimension ld_out), which may not overlap x.  saved: pf_window_attn_saved_size
+ * bytes for the backward (the rows' log-sums, and what the rounding of out left),
+ * or NULL.
+ * What a row does not see does not matter, infinities and NaN among it.      */
 pf_status pf_window_attn_fwd(const pf_window_desc *desc, const pf_qkv *x, void *out,
                              int64_t ld_out, void *saved, void *stream);
 
@@ -419,7 +418,8 @@ size_t pf_window_attn_workspace_size(const pf_window_desc *desc);
 
 /* Its backward: dx->q, dx->k, dx->v (overwritten; those of a key head sum over
  * its query heads) from the forward's x, out and saved and the gradient dout of
- * out.  dx's matrices may not overlap x, out, dout or one another.           */
+ * out.  dx's matrices may not overlap x, out, dout or one another.  x and dout
+ * must be finite: what a row does not see may be multiplied by zero here.    */
 pf_status pf_window_attn_bwd(const pf_window_desc *desc, const pf_qkv *x, const void *out,
                              int64_t ld_out, const void *saved, const void *dout,
                              int64_t ld_dout, const pf_qkv *dx, void *ws, size_t ws_bytes,

@@ -282,8 +282,7 @@ pf_status pf_window_attn_fwd(const pf_window_desc* desc, const pf_qkv* x, void* 
   PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
   if (!aligned16(saved)) return fail(PF_ERR_INVALID_ARG, "saved must be 16-byte aligned");
   const Area o = window_area(*desc, "out", out, ld_out, desc->n_heads);
-  // (a tile's queries are read before its rows are written)
-  PF_TRY(check_over(o, window_area(*desc, "q", x->q, x->ld_q, desc->n_heads)));
+  PF_TRY(check_apart(o, window_area(*desc, "q", x->q, x->ld_q, desc->n_heads)));
   PF_TRY(check_apart(o, window_area(*desc, "k", x->k, x->ld_k, desc->n_kv)));
   PF_TRY(check_apart(o, window_area(*desc, "v", x->v, x->ld_v, desc->n_kv)));
   const Window c = window_of(*desc);

@@ -48,8 +48,9 @@
 // keys from a row (the window's first tile, seen by the tile's first rows
 // only): such a row keeps no reference and adds zeros.
 // Masked scores are set to -inf after the product, so a masked K may hold
-// anything; P = 0 meets its V in the MMA, so values must be finite up to the
-// end of the tile that a row sees.
+// anything.  P = 0 meets its V in the MMA: an infinity or a NaN there reaches rows
+// of its 128-row tile that do not see it.  A warp remembers that a row of its own
+// was not finite, and goes through its items again at the end (wa_repair).
 #include <algorithm>
 #include <type_traits>
 
@@ -89,6 +90,10 @@ struct WaArgs {
   WinTiles w;
   int n_st, n_items;  // tile pairs
   float sl2;          // log2(e) / sqrt(64)
+  // as wa_repair reads and writes them
+  const bf16 *q, *k, *v;
+  bf16 *out, *rest;
+  long ldq, ldk, ldv, ldo;
 };
 
 // Items are ranked from the last tile pair on (the first ones see the fewest
@@ -140,6 +145,123 @@ __device__ __forceinline__ float ex2_approx(float x) {
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
   if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
   return mbar_wait_warp(bar, parity);
+}
+
+// Whether one of the rows [r0, r1) of v (a head of a sequence) holds a value that is not
+// finite.  For a converged warp.
+__device__ __forceinline__ bool wa_not_finite(const bf16* v, long ldv, int r0, int r1) {
+  const int lane = threadIdx.x & 31;
+  bool bad = false;
+  for (int r = r0 + (lane >> 3); r < r1; r += 4) {
+    const uint4 u = *reinterpret_cast<const uint4*>(v + r * ldv + (lane & 7) * 8);
+    for (uint32_t w : {u.x, u.y, u.z, u.w}) bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+  }
+  return __any_sync(0xffffffffu, bad);
+}
+
+// Columns 2 lane, 2 lane + 1 of row i's output, from the keys that it sees and no others.
+// q: the row; k, v: its head and sequence.  For a converged warp: a key to a lane for the
+// scores, two columns to a lane for the sums.
+__device__ __forceinline__ float2 wa_row(const WaArgs& a, const bf16* q, const bf16* k, const bf16* v, int i) {
+  const int lane = threadIdx.x & 31, lo = max(0, i - a.w.W + 1);
+  float2 acc = make_float2(0.f, 0.f);
+  float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+  for (int part = 0; part < 2; ++part) {  // the sinks before the window, the window
+    const int end = part ? i + 1 : min(a.w.S, lo);
+#pragma unroll 1
+    for (int j = part ? lo : 0; j < end; j += 32) {
+      const bool in = j + lane < end;
+      float s = -INFINITY;
+      if (in) {
+        s = 0.f;
+#pragma unroll 2
+        for (int c = 0; c < WA_D; c += 8) {
+          float x[8], y[8];
+          load8_bf16(q + c, x);
+          load8_bf16(k + (j + lane) * a.ldk + c, y);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
+        }
+      }
+      float mx = s;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float next = fmaxf(m, mx * a.sl2), ref = next == -INFINITY ? 0.f : next;
+      const float corr = m == -INFINITY ? 1.f : ex2_approx(m - ref);
+      m = next;
+      const float p = in ? ex2_approx(fmaf(s, a.sl2, -ref)) : 0.f;
+      float sum = p;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      l = fmaf(l, corr, sum);
+      acc.x *= corr;
+      acc.y *= corr;
+#pragma unroll 8
+      for (int t = 0; t < min(32, end - j); ++t) {
+        const float pt = __shfl_sync(0xffffffffu, p, t);
+        const float2 y = unpack_bf16(*reinterpret_cast<const uint32_t*>(v + (j + t) * a.ldv + 2 * lane));
+        acc.x = fmaf(pt, y.x, acc.x);
+        acc.y = fmaf(pt, y.y, acc.y);
+      }
+      // NaN for good, whatever follows
+      if (__all_sync(0xffffffffu, acc.x != acc.x && acc.y != acc.y)) return acc;
+    }
+  }
+  return make_float2(acc.x / l, acc.y / l);
+}
+
+// Rows that came out other than finite beside hidden rows of v that are not: in the MMA P = 0
+// met them.  The softmax warp goes through its items' rows in memory again and works such
+// rows out from the keys that they see.  Out of line and after the loop over the items: calls
+// without such rows pay 0.1 of 9.7 us (3 x 1021 tokens, window 256) and 50 of 3930 (262144
+// tokens, window 4096); from inside the loop 0.4 and 140.  With them (65536 tokens of 16 heads, the
+// last 100 rows NaN): 3.6 ms in place of 0.36 at window 1024, 226 in place of 7 without a window.
+// The loads of more keys at once halve that, but their registers cost every call as much again.
+__device__ __noinline__ void wa_repair(WaArgs a, int warp) {
+  const int lane = threadIdx.x & 31, w = (warp - 4) >> 2, q4 = warp & 3;
+  asm volatile("fence.proxy.async;" ::: "memory");  // the rows went out by TMA
+  __syncwarp();
+#pragma unroll 1
+  for (int rd = 0, k = wa_rank(blockIdx.x, 0); k < a.n_items; k = wa_rank(blockIdx.x, ++rd)) {
+    const WaItem m(a, k);
+    const int t = 2 * m.u + w, q0 = t * WT + q4 * 32;
+    const long row0 = (long)m.b * a.w.L, kc = (long)(m.h / a.g) * WA_D;
+    bf16* const out = a.out + row0 * a.ldo + m.h * WA_D;
+    bool bad = false;
+    if (q0 + lane < a.w.L) {
+      float sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < WA_D; c += 8) {
+        const uint4 u = __ldcg(reinterpret_cast<const uint4*>(out + (q0 + lane) * a.ldo + c));
+        for (uint32_t x : {u.x, u.y, u.z, u.w}) sum = fmaf(unpack_bf16(x).x, 0.f, fmaf(unpack_bf16(x).y, 0.f, sum));
+      }
+      bad = sum != 0.f;
+    }
+    uint32_t again = __ballot_sync(0xffffffffu, bad);
+    if (!again) continue;
+    // rows of v that its tiles hold and some of the warp's rows do not see: past the diagonal,
+    // before the window, beside the sinks
+    const bf16 *kp = a.k + row0 * a.ldk + kc, *vp = a.v + row0 * a.ldv + kc;
+    const int lo = a.w.lo(t), ns = min(a.w.sT, lo);
+    const int held = ns < a.w.sT ? 0 : a.w.few >= 0 ? a.w.few * WT + WT_FEW : ns * WT;
+    if (!wa_not_finite(vp, a.ldv, q0 + 1, min(t * WT + WT, a.w.L)) &&
+        !wa_not_finite(vp, a.ldv, max(lo * WT, a.w.S), min(q0 + 32 - a.w.W, a.w.L)) &&
+        !wa_not_finite(vp, a.ldv, a.w.S, min(held, a.w.L)))
+      continue;
+#pragma unroll 1
+    for (; again; again &= again - 1) {
+      const int i = q0 + __ffs(again) - 1;
+      const float2 o = wa_row(a, a.q + (row0 + i) * a.ldq + m.h * WA_D, kp, vp, i);
+      const uint32_t x = pack_bf16(o.x, o.y);
+      *reinterpret_cast<uint32_t*>(out + i * a.ldo + 2 * lane) = x;
+      if (a.rest) {
+        const float2 y = unpack_bf16(x);
+        *reinterpret_cast<uint32_t*>(a.rest + ((row0 + i) * a.H + m.h) * WA_D + 2 * lane) =
+            pack_bf16(o.x - y.x, o.y - y.y);
+      }
+    }
+  }
 }
 
 __global__ void __launch_bounds__(WA_THREADS, 1)
@@ -332,7 +454,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
     const uint32_t ts = tl + 128 * w, to = tl + WA_TM_O + 64 * w, tp = tl + WA_TM_P + 64 * w;
     const float2 sl = make_float2(a.sl2, a.sl2);
-    bool ok = true;
+    bool ok = true, late = false;  // late: a row was not finite
     uint32_t g = 0, io = 0;
     int k = wa_rank(blockIdx.x, 0);
     WaItem next(a, k);  // worked out while the item before it waits for its O
@@ -493,6 +615,13 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
       tmem_wait_ld(ov + 32);
       tc_fence_before();
       mbar_arrive_warp(o_free(w));
+      float2 fin[4] = {};  // zero, but for sums that are not finite
+#pragma unroll
+      for (int i = 0; i < WA_D / 2; ++i)
+        fin[i % 4] = __ffma2_rn(make_float2(__uint_as_float(ov[2 * i]), __uint_as_float(ov[2 * i + 1])),
+                                make_float2(0.f, 0.f), fin[i % 4]);
+      fin[0] = __fadd2_rn(__fadd2_rn(fin[0], fin[1]), __fadd2_rn(fin[2], fin[3]));
+      late |= fin[0].x + fin[0].y != 0.f;
       // the warp's 32 rows go out by TMA from its own stage (128-byte swizzle; rows past the end
       // of the sequence are left out)
       const float inv = 1.f / l;  // (a row sees itself: 0 where its scores are all -inf, and 0 / 0 is NaN)
@@ -535,6 +664,7 @@ __global__ void __launch_bounds__(WA_THREADS, 1)
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     __syncwarp();
+    if (__any_sync(0xffffffffu, late)) wa_repair(a, warp);
   }
   tc_fence_before();
   if (__syncthreads_or(*(volatile int*)&g_dev_error != 0)) {
@@ -593,6 +723,15 @@ cudaError_t window_fwd(const Window& c, const QkvPtr& x, bf16* out, long ldo, co
   if (items > 0x3fffffff) return cudaErrorInvalidValue;
   a.n_items = (int)items;
   a.sl2 = 1.4426950408889634f / sqrtf((float)WA_D);
+  a.q = static_cast<const bf16*>(x.q);
+  a.k = static_cast<const bf16*>(x.k);
+  a.v = static_cast<const bf16*>(x.v);
+  a.out = out;
+  a.rest = v.rest;
+  a.ldq = x.ldq;
+  a.ldk = x.ldk;
+  a.ldv = x.ldv;
+  a.ldo = ldo;
   static KernelOnce once;
   const cudaError_t e = once(reinterpret_cast<const void*>(window_fwd_kernel), WA_SMEM, WA_THREADS,
                              WA_REGS_CTRL * 128 + WA_REGS_ROWS * 256);

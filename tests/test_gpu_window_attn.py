@@ -228,18 +228,17 @@ def test_scores_of_minus_infinity():
     assert torch.equal(out, ref)
 
 
-def test_results_beside_and_over_the_inputs():
-    """Results in the free columns of the inputs' own rows, or over the queries."""
+def test_results_beside_the_inputs():
+    """Results in the free columns of the inputs' own rows, and none over them."""
     B, L = 2, 333
     x = rand((B * L, 12 * 64), 25)
     q, k, v, free = x[:, :256], x[:, 256:384], x[:, 384:512], x[:, 512:]
     op = WindowAttention(B, L, 4, 2, window=100, n_sink=3)
     ref = op.forward(q, k, v, train=False)
     assert op.forward(q, k, v, train=False, out=free).data_ptr() == free.data_ptr()
-    op.forward(q, k, v, train=False, out=q)
     check()
-    assert torch.equal(free, ref) and torch.equal(q, ref)
-    for out in (x[:, 128:384], x[:, 320:576], x[:, 64:320]):
+    assert torch.equal(free, ref)
+    for out in (q, x[:, 128:384], x[:, 320:576], x[:, 64:320]):
         with pytest.raises(pf.ProxyFormerError) as e:
             op.forward(q, k, v, train=False, out=out)
         assert e.value.status == pf.PF_ERR_INVALID_ARG
@@ -297,3 +296,50 @@ def test_gradients_along_themselves(case):
     for i, d in enumerate(grads):
         got, want, bar = difference(forward, x, i, f64(d).reshape(x[i].shape), do)
         assert abs(got - want) <= bar, (i, got, want, bar)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("L,H,KV,window,n_sink,at", [
+    (300, 2, 1, 0, 0, 130), (300, 2, 1, 0, 0, 299), (300, 4, 2, 100, 3, 140), (300, 2, 2, 100, 3, 3), (300, 2, 2, 100, 3, 40),
+    (700, 2, 1, 129, 40, 41), (700, 2, 1, 129, 40, 100), (700, 2, 1, 1, 0, 200), (640, 1, 1, 300, 128, 128), (77, 2, 1, 0, 0, 40)])
+def test_hidden_values_do_not_matter(L, H, KV, window, n_sink, at, value):
+    """A value (one column of a row of v, or all of a row of k) that is not finite reaches the rows that see it and
+    no others, those of its 128-row tile among them."""
+    B = 2
+    q, k, v = (rand((B * L, n * 64), s) for n, s in ((H, 1), (KV, 2), (KV, 3)))
+    op = WindowAttention(B, L, H, KV, window=window, n_sink=n_sink)
+    s = lambda t, n: f64(t).reshape(B, L, n, 64)
+    ref, mag = OL.window_fwd(s(q, H), s(k, KV), s(v, KV), window, n_sink)
+    bar = U * (mag + np.abs(ref)) + 2e-5 * mag
+    seen = np.array([OL.visible(i, L, window, n_sink)[at] for i in range(L)])
+    assert seen[at] and not seen.all()
+    for train in (False, True):
+        bad = v.clone()
+        bad[L + at, 7] = value  # of the first key head
+        out = f64(op.forward(q, k, bad, train=train)).reshape(ref.shape)
+        check()
+        touched = np.zeros(ref.shape, bool)
+        touched[1, seen, :H // KV, 7] = True
+        assert not np.isfinite(out[touched]).any()
+        assert (np.abs(out - ref)[~touched] <= bar[~touched]).all()
+        bad = k.clone()
+        bad[L + at, :64] = value
+        out = f64(op.forward(q, bad, v, train=train)).reshape(ref.shape)
+        check()
+        touched = np.zeros(ref.shape, bool)
+        touched[1, seen, :H // KV] = True
+        assert (np.abs(out - ref)[~touched] <= bar[~touched]).all()
+
+
+def test_hidden_values_in_training():
+    """What a forward saved for rows before one that is not finite is theirs alone."""
+    L = 300
+    q, k, v, do = (rand((L, 64), s) for s in (1, 2, 3, 4))
+    op = WindowAttention(1, L, 1, 1, window=100, n_sink=2)
+    d = op.backward(q, k, v, op.forward(q, k, v), do)
+    lse, rest = op.saved[:L * 4].clone(), op.saved[-L * 128:].view(BF).view(L, 64).clone()
+    v[200] = float("nan")
+    op.forward(q, k, v)
+    check()
+    assert torch.equal(op.saved[:200 * 4], lse[:200 * 4]) and torch.isfinite(op.saved[-L * 128:].view(BF).view(L, 64)[:200]).all()
+    assert torch.isfinite(rest).all() and all(torch.isfinite(t).all() for t in d)

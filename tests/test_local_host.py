@@ -189,10 +189,10 @@ def row_bytes(ld, **moved):
 
 @pytest.mark.parametrize("moved", [
     dict(out=("k", 0, 0)), dict(out=("v", 0, 0)), dict(out=("k", 599, 0)), dict(out=("v", -599, 0)),
-    dict(out=("q", 0, 16)), dict(out=("q", 1, 0)), dict(out=("k", 0, 240)), dict(out=("k", -1, 528)),
+    dict(out=("q", 0, 0)), dict(out=("q", 0, 16)), dict(out=("q", 1, 0)), dict(out=("k", 0, 240)), dict(out=("k", -1, 528)),
     dict(q=("out", 0, 256))])
 def test_window_forward_overlaps(moved):
-    """Results over keys and values that other tiles still read, whole or in part; queries only as they are."""
+    """Results over inputs that are still read, whole or in part."""
     at = {**BASES, **row_bytes(512, **moved)}
     refused(pf.PF_ERR_INVALID_ARG, pf.pf_window_attn_fwd, win(),
             rows(at["q"], at["k"], at["v"], 512, 512, 512), at["out"], 512, A)
