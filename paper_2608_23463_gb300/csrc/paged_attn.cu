@@ -464,10 +464,11 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a) {
 
 // A CTA for each (sequence, key head), and no join, where none sees many rows: a CTA
 // streams 43 GB/s, and with a pair or more to each SM that is HBM's rate, while ranges that
-// span several short pairs cost their ends.  In us, whole and in ranges, ragged but for the
-// first two: 1 x 250 rows, 4 heads of 64: 4.9 and 7.3; 1 x 500: 8.0 and 7.3; 8 x 1000 rows, 8
-// heads of 128: 15.8 and 15.4; 32 x 1000: 20.3 and 41; 256 x 1000: 87 and 136; 300 x 200 rows of
-// one head: 7.4 and 48.
+// span several short pairs cost their ends.  In us, whole and in ranges, pages of 16 rows, ragged
+// but for the first two, captured: 1 x 250 rows, 16 heads on 4 of 64: 4.9 and 7.4; 1 x 500: 7.4 and
+// 7.4; 8 x 1000 rows, 8 heads of 128: 15.3 and 11.8; 32 x 1000: 20.0 and 35.5; 256 x 1000: 86 and
+// 114; 300 x 200 rows of one head of 64: 5.4 and 16.  The host knows the table's width, not the
+// lengths: short caches in a table of many pages are read in ranges.
 bool pa_whole(const Paged& c) {
   constexpr long FEW = 384, MANY = 2048, SMS = 152;
   long rows = (long)c.max_pages * c.page;
