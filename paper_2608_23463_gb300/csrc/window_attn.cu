@@ -23,7 +23,7 @@
 // What bounds it: the chain of one softmax warp through a tile (about 430
 // instructions, two such warps on each scheduler), beside 1024 cycles of MMAs
 // and as many of exponentials for a pair of tiles.  262144 tokens of 16 heads on
-// 4, window 4096: 3.95 ms (1.13 PFLOP/s).  What shortened the chain: maxima of
+// 4, window 4096: 3.98 ms (1.11 PFLOP/s).  What shortened the chain: maxima of
 // the first half of the scores while the second comes from TMEM, P stored from
 // its half on, and a loop of its own for tiles without masked keys (4.50
 // without the three; 4.39 with the loop alone, 4.34 with it and either).
@@ -38,7 +38,8 @@
 // us without, 422 with it; 411 with each tile's scores and O issued by one warp,
 // 399 so; 366 with the rows out by TMA, for which an item's end took a fifth of it.
 // Code counts, its fetches more than its instructions: masks by the bits of a word in
-// place of two compares of a column (4.17 to 3.95 ms where a tile in seventeen has one).
+// place of two compares of a column (4.17 to 3.95 ms where a tile in seventeen has one; 3.98 with
+// the test for rows that are not finite).
 // One body for tiles with masks and tiles without them spills: 4.59.
 // A row's probabilities are taken against a reference m, the maximum of the
 // first tile in which the row sees a key, raised only when a later tile's

@@ -85,7 +85,8 @@ class QKRope:
 
 class WindowAttention:
     """Causal attention of ``batch`` sequences of L rows: row i sees the last ``window``
-    rows up to itself (0: all) and the first ``n_sink``.  bf16, head width 64."""
+    rows up to itself (0: all) and the first ``n_sink``.  bf16, head width 64.  What a row
+    does not see does not matter to its result; the backward's inputs must be finite."""
 
     def __init__(self, batch: int, L: int, n_heads: int, n_kv: int, dh: int = 64, window: int = 0,
                  n_sink: int = 0):
