@@ -488,6 +488,68 @@ pf_status pf_paged_attn(const pf_paged_desc *desc, const void *q, int64_t ld_q,
                         const pf_paged_cache *cache, void *out, int64_t ld_out, void *ws,
                         size_t ws_bytes, void *stream);
 
+/* Exponents of a quantised cache, in the caller's device memory (16-byte aligned):
+ *   K, V  [n_pages, n_kv, page] int8
+ * beside a pf_paged_cache whose K and V are then int8, [n_pages, n_kv, page, dh].
+ * A row (one token and key head) y of dh values is held as whole numbers x and
+ * an exponent e, and stands for x 2^e:
+ *   e = min { e >= -126 : max |y| <= 127 2^e },   x = y 2^-e to the nearest
+ *   (ties to even)
+ * x 2^e is a bf16 number; it is off y by 2^e / 2 at most, max |y| / 127.  A row
+ * that is not finite, or reaches past 127 2^104, has e = -128: all of its values
+ * are NaN then.  A cache is quantised or not for good: all calls that reach it
+ * get the same exponents.                                                    */
+typedef struct {
+  int8_t *K, *V;
+} pf_paged_exp;
+
+/* pf_paged_append and pf_paged_attn for a quantised cache: keys are quantised as
+ * normed and rotated (without a rounding before that), values as they are.   */
+pf_status pf_paged_append_q8(const pf_paged_desc *desc, const pf_qk_desc *qk, int64_t rows,
+                             const pf_qkv *x, const float *w_q, const float *w_k,
+                             const int32_t *start, const int32_t *pos, pf_paged_cache *cache,
+                             const pf_paged_exp *exp, void *q_out, int64_t ld_q_out,
+                             void *stream);
+
+pf_status pf_paged_attn_q8(const pf_paged_desc *desc, const void *q, int64_t ld_q,
+                           const pf_paged_cache *cache, const pf_paged_exp *exp, void *out,
+                           int64_t ld_out, void *ws, size_t ws_bytes, void *stream);
+
+size_t pf_paged_chunk_workspace_size(const pf_paged_desc *desc, int64_t rows);
+
+/* Attention of the newest tokens of every sequence, any number of each, with
+ * queries q [rows, n_heads*dh] (leading dimension ld_q), over the cache, which
+ * holds them already (pf_paged_append) and whose len counts them.  Tokens
+ * start[b] .. start[b+1] of q (start [batch+1] int32, device, not NULL) are the
+ * last of sequence b, as in pf_paged_append, none or many; a token in row i of
+ * its sequence sees the rows j <= i, with a window those of i - j < window or
+ * j < n_sink.
+ *   out_h = softmax(q_h K^T / sqrt(dh)) V,   key head h / (n_heads/n_kv)
+ * out [rows, n_heads*dh] (leading dimension ld_out) may not overlap q.  Rows of
+ * q that are no sequence's (from start[batch] on) are left alone in out.  exp:
+ * of a quantised cache, else NULL.  ws: pf_paged_chunk_workspace_size bytes (0:
+ * may be NULL); calls that may run at the same time need one each.
+ * What a token does not see does not matter to its result, infinities and NaN
+ * among it.  A sequence whose tokens are not among the call's rows, or more than
+ * its length, or whose length its table or 2^31 - 256 does not hold, is flagged
+ * (PF_ERR_CAPACITY via pf_sync_check) and its rows, if they are the call's, become
+ * zeros; pages out of range are flagged and read as zeros.  Start and lengths stay
+ * on the device, so that a captured graph serves every step of as many rows.  */
+pf_status pf_paged_chunk_attn(const pf_paged_desc *desc, int64_t rows, const void *q, int64_t ld_q,
+                              const int32_t *start, const pf_paged_cache *cache,
+                              const pf_paged_exp *exp, void *out, int64_t ld_out, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/* Rows read back: k, v [rows, n_kv*dh] bf16 (leading dimensions ld_k, ld_v; they
+ * may not overlap), of which start[b] .. start[b+1] become the last rows of
+ * sequence b's cache (start NULL: the last row of each, rows = batch).  exp: of a
+ * quantised cache, else NULL.  Rows that are no sequence's are left alone; where
+ * the cache does not hold such a row they become zeros and are flagged
+ * (PF_ERR_CAPACITY via pf_sync_check).  start must not decrease.             */
+pf_status pf_paged_read(const pf_paged_desc *desc, int64_t rows, const int32_t *start,
+                        const pf_paged_cache *cache, const pf_paged_exp *exp, void *k,
+                        int64_t ld_k, void *v, int64_t ld_v, void *stream);
+
 /* Thread-local message describing the last non-OK status of this thread. */
 const char *pf_last_error(void);
 

@@ -126,3 +126,39 @@ def paged_attn(q, K, V, table, length, window, n_sink):
             p = _probabilities(q[b, h:h + 1], k[:, h // g], np.ones((1, len(j)), bool))
             out[b, h], mag[b, h] = (p @ v[:, h // g])[0], (p @ np.abs(v[:, h // g]))[0]
     return out, mag
+
+
+def quantise(y):
+    """Rows y [..., dh] as whole numbers and exponents: the least e >= -126 with max |y| <= 127 * 2^e, x the nearest
+    whole numbers to y / 2^e, ties to even ones; e = -128 (x = 0) where the row is not finite or e would pass 104."""
+    top = np.abs(y).max(-1)
+    fine = np.isfinite(top) & (top <= 127.0 * 2.0 ** 104)
+    m = np.where(fine, top, 0.0)
+    e = np.full(m.shape, -126, np.int64)
+    for k in range(7, -1, -1):  # 230 steps at most, by halves
+        e = np.where(m > 127.0 * np.ldexp(1.0, e + 2 ** k - 1), e + 2 ** k, e)
+    x = np.rint(np.ldexp(np.where(fine[..., None], y, 0.0), -e[..., None]))
+    return x.astype(np.int8), np.where(fine, e, -128).astype(np.int8)
+
+
+def values(x, e):
+    """What quantised rows stand for."""
+    return np.where(e[..., None] == -128, np.nan, np.ldexp(x.astype(np.float64), e.astype(int)[..., None]))
+
+
+def paged_chunk(q, K, V, table, length, start, window, n_sink):
+    """q [rows, H, dh], of which [start[b], start[b+1]) are the last tokens of sequence b -> (out, sum_j p_j |v_j|);
+    NaN where a row is no sequence's.  K, V hold zeros where what they held is not seen."""
+    out, mag = np.full_like(q, np.nan), np.full_like(q, np.nan)
+    page, g = K.shape[2], q.shape[1] // K.shape[1]
+    for b, n in enumerate(length):
+        t = np.arange(start[b], start[b + 1])
+        if len(t) == 0:
+            continue
+        j = np.arange(n)
+        k, v = (x[table[b, j // page], :, j % page] for x in (K, V))
+        seen = np.stack([visible(i, n, window, n_sink) for i in n - len(t) + np.arange(len(t))])
+        for h in range(q.shape[1]):
+            p = _probabilities(q[t, h], k[:, h // g], seen)
+            out[t, h], mag[t, h] = p @ v[:, h // g], p @ np.abs(v[:, h // g])
+    return out, mag

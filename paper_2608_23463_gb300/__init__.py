@@ -103,6 +103,10 @@ class PagedCache(ctypes.Structure):
     _fields_ = [(n, _vp) for n in ("K", "V", "table", "len")]
 
 
+class PagedExp(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("K", "V")]
+
+
 EXPORTED = ("proxy_layer_check", "proxy_layer_saved_size", "proxy_layer_workspace_size",
             "proxy_layer_fwd", "proxy_layer_bwd", "proxy_decode_workspace_size",
             "proxy_decode_step", "proxy_append_workspace_size", "proxy_kv_append",
@@ -112,6 +116,8 @@ EXPORTED = ("proxy_layer_check", "proxy_layer_saved_size", "proxy_layer_workspac
             "pf_window_attn_fwd", "pf_window_attn_saved_size", "pf_window_attn_workspace_size",
             "pf_window_attn_bwd",
             "pf_paged_advance", "pf_paged_append", "pf_paged_attn_workspace_size", "pf_paged_attn",
+            "pf_paged_append_q8", "pf_paged_attn_q8", "pf_paged_chunk_workspace_size",
+            "pf_paged_chunk_attn", "pf_paged_read",
             "pf_last_error", "pf_sync_check", "pf_gemm_bf16", "pf_timing_enable",
             "pf_timing_collect", "pf_timing_label", "pf_timing_ms", "pf_timing_launches",
             "pf_timing_flops", "pf_timing_bytes", "proxy_layer_bwd_noalloc",
@@ -199,6 +205,20 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pf_paged_attn_workspace_size.restype = sz
     lib.pf_paged_attn.argtypes = [P(PagedDesc), _vp, i64, P(PagedCache), _vp, i64, _vp, sz, _vp]
     lib.pf_paged_attn.restype = ctypes.c_int
+    lib.pf_paged_append_q8.argtypes = [P(PagedDesc), P(QKDesc), i64, P(QKV), _vp, _vp, _vp, _vp,
+                                       P(PagedCache), P(PagedExp), _vp, i64, _vp]
+    lib.pf_paged_append_q8.restype = ctypes.c_int
+    lib.pf_paged_attn_q8.argtypes = [P(PagedDesc), _vp, i64, P(PagedCache), P(PagedExp), _vp, i64,
+                                     _vp, sz, _vp]
+    lib.pf_paged_attn_q8.restype = ctypes.c_int
+    lib.pf_paged_chunk_workspace_size.argtypes = [P(PagedDesc), i64]
+    lib.pf_paged_chunk_workspace_size.restype = sz
+    lib.pf_paged_chunk_attn.argtypes = [P(PagedDesc), i64, _vp, i64, _vp, P(PagedCache),
+                                        P(PagedExp), _vp, i64, _vp, sz, _vp]
+    lib.pf_paged_chunk_attn.restype = ctypes.c_int
+    lib.pf_paged_read.argtypes = [P(PagedDesc), i64, _vp, P(PagedCache), P(PagedExp), _vp, i64,
+                                  _vp, i64, _vp]
+    lib.pf_paged_read.restype = ctypes.c_int
     lib.pf_last_error.argtypes = []
     lib.pf_last_error.restype = ctypes.c_char_p
     lib.pf_sync_check.argtypes = [_vp]
@@ -425,6 +445,40 @@ def pf_paged_attn_workspace_size(desc) -> int:
 def pf_paged_attn(desc, q, ld_q, cache, out, ld_out, ws, ws_bytes, stream=None):
     _check(load().pf_paged_attn(ctypes.byref(desc), _ptr(q), int(ld_q), ctypes.byref(cache),
                                 _ptr(out), int(ld_out), _ptr(ws), int(ws_bytes), stream))
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def pf_paged_append_q8(desc, qk, rows, x, w_q, w_k, start, pos, cache, exp, q_out, ld_q_out,
+                       stream=None):
+    _check(load().pf_paged_append_q8(ctypes.byref(desc), ctypes.byref(qk), int(rows),
+                                     ctypes.byref(x), _ptr(w_q), _ptr(w_k), _ptr(start), _ptr(pos),
+                                     ctypes.byref(cache), _ref(exp), _ptr(q_out), int(ld_q_out),
+                                     stream))
+
+
+def pf_paged_attn_q8(desc, q, ld_q, cache, exp, out, ld_out, ws, ws_bytes, stream=None):
+    _check(load().pf_paged_attn_q8(ctypes.byref(desc), _ptr(q), int(ld_q), ctypes.byref(cache),
+                                   _ref(exp), _ptr(out), int(ld_out), _ptr(ws), int(ws_bytes),
+                                   stream))
+
+
+def pf_paged_chunk_workspace_size(desc, rows) -> int:
+    return load().pf_paged_chunk_workspace_size(ctypes.byref(desc), int(rows))
+
+
+def pf_paged_chunk_attn(desc, rows, q, ld_q, start, cache, exp, out, ld_out, ws, ws_bytes,
+                        stream=None):
+    _check(load().pf_paged_chunk_attn(ctypes.byref(desc), int(rows), _ptr(q), int(ld_q),
+                                      _ptr(start), ctypes.byref(cache), _ref(exp), _ptr(out),
+                                      int(ld_out), _ptr(ws), int(ws_bytes), stream))
+
+
+def pf_paged_read(desc, rows, start, cache, exp, k, ld_k, v, ld_v, stream=None):
+    _check(load().pf_paged_read(ctypes.byref(desc), int(rows), _ptr(start), ctypes.byref(cache),
+                                _ref(exp), _ptr(k), int(ld_k), _ptr(v), int(ld_v), stream))
 
 
 def pf_sync_check(stream=None) -> None:

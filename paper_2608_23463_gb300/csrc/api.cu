@@ -1922,7 +1922,8 @@ pf_status pf_sync_check(void* stream) {
                 take_dev_error_attention_bwd_tc(),
                 take_dev_error_elementwise(), take_dev_error_decode(), take_dev_error_fp32(),
                 take_dev_error_layer2d(), take_dev_error_local_rope(), take_dev_error_paged_attn(),
-                take_dev_error_window_attn(), take_dev_error_window_attn_bwd()})
+                take_dev_error_window_attn(), take_dev_error_window_attn_bwd(), take_dev_error_paged_chunk(),
+                take_dev_error_paged_read()})
     if (v != 0 && e == 0) e = v;
   if (e < 0) return fail(PF_ERR_CUDA, "reading the device error flag failed");
   if (e == DEVERR_TIMEOUT) return fail(PF_ERR_TIMEOUT, "a kernel's bounded wait ran out");
@@ -1938,7 +1939,8 @@ pf_status pf_debug_set_wait_limit_ns(unsigned long long ns) {
                 set_wait_limit_elementwise(ns), set_wait_limit_decode(ns), set_wait_limit_fp32(ns),
                 set_wait_limit_layer2d(ns), set_wait_limit_local_rope(ns),
                 set_wait_limit_paged_attn(ns), set_wait_limit_window_attn(ns),
-                set_wait_limit_window_attn_bwd(ns)})
+                set_wait_limit_window_attn_bwd(ns), set_wait_limit_paged_chunk(ns),
+                set_wait_limit_paged_read(ns)})
     bad |= r;
   if (bad) return fail(PF_ERR_CUDA, "pf_debug_set_wait_limit_ns: writing the limit failed");
   return PF_OK;

@@ -335,6 +335,34 @@ bool tmap_bf16_seq(CUtensorMap* m, const void* base, uint64_t inner, uint64_t ou
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool tmap_bf16_heads(CUtensorMap* m, const void* base, uint64_t width, uint64_t n_heads, uint64_t rows, uint64_t ld,
+                     uint32_t box_heads, uint32_t box_rows) {
+  auto fn = encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[3] = {width, n_heads, rows};
+  cuuint64_t strides[2] = {width * 2, ld * 2};
+  cuuint32_t box[3] = {64, box_heads, box_rows};
+  cuuint32_t es[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool tmap_pages(CUtensorMap* m, const void* base, bool bytes, uint64_t width, uint64_t page, uint64_t n_kv,
+                uint64_t n_pages, uint32_t box_rows) {
+  auto fn = encode_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t row = bytes ? width : 2 * width;
+  cuuint64_t dims[4] = {width, page, n_kv, n_pages};
+  cuuint64_t strides[3] = {row, row * page, row * page * n_kv};
+  cuuint32_t box[4] = {bytes ? (cuuint32_t)width : 64, box_rows, 1, 1};
+  cuuint32_t es[4] = {1, 1, 1, 1};
+  return fn(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base),
+            dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool tmap_bf16_rows32(CUtensorMap* m, const void* base, uint64_t outer, uint64_t n_seq,
                       uint32_t box_outer) {
   auto fn = encode_fn();

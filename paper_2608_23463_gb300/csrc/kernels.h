@@ -244,6 +244,13 @@ bool tmap_bf16_2d(CUtensorMap* m, const void* base, uint64_t inner, uint64_t out
 bool tmap_bf16_seq(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint64_t n_seq,
                    uint64_t ld, uint32_t box_inner, uint32_t box_outer);
 
+// Heads of `width` bf16 side by side in rows of `ld` elements: box 64 x heads x rows, 128-byte swizzle.
+bool tmap_bf16_heads(CUtensorMap* m, const void* base, uint64_t width, uint64_t n_heads, uint64_t rows, uint64_t ld,
+                     uint32_t box_heads, uint32_t box_rows);
+// Pages [n_pages, n_kv, page] of rows of `width` bf16 (128-byte swizzle, box 64 x box_rows) or bytes (none, box
+// width x box_rows); a page past the last one reads as zero.
+bool tmap_pages(CUtensorMap* m, const void* base, bool bytes, uint64_t width, uint64_t page, uint64_t n_kv,
+                uint64_t n_pages, uint32_t box_rows);
 // n_seq matrices of `outer` rows of 16 bf16 that follow one another, as above but with a
 // 32-byte swizzle; box 16 x box_outer.
 bool tmap_bf16_rows32(CUtensorMap* m, const void* base, uint64_t outer, uint64_t n_seq,

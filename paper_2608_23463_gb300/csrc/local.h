@@ -59,6 +59,7 @@ struct Paged {
   int window, sinks;
   bf16 *K, *V;  // [n_pages, KV, page, dh]
   const int *table, *len;
+  signed char *Ke, *Ve;  // exponents [n_pages, KV, page]: K and V are int8 then; else null
 };
 
 // Windowed attention of B sequences of L rows: H query and KV key heads of 64.
@@ -101,6 +102,19 @@ size_t paged_attn_ws_bytes(const Paged& c);
 cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long ldo, float* ws,
                        cudaStream_t st);
 
+// Attention of the sequences' newest tokens, rows of q [rows, H * dh], over the cache: those of
+// sequence b are [start[b], start[b + 1]).
+size_t paged_chunk_ws_bytes(const Paged& c, long rows);
+cudaError_t paged_chunk(const Paged& c, long rows, const bf16* q, long ldq, const int* start, bf16* out, long ldo,
+                        void* ws, cudaStream_t st);
+// Their keys and values read back, k, v [rows, KV * dh].
+cudaError_t paged_read(const Paged& c, long rows, const int* start, bf16* k, long ldk, bf16* v, long ldv,
+                       cudaStream_t st);
+
+int take_dev_error_paged_chunk();
+int take_dev_error_paged_read();
+int set_wait_limit_paged_chunk(unsigned long long ns);
+int set_wait_limit_paged_read(unsigned long long ns);
 int take_dev_error_local_rope();
 int take_dev_error_paged_attn();
 int take_dev_error_window_attn();

@@ -213,9 +213,20 @@ pf_status check_cache(const pf_paged_cache* c) {
   return PF_OK;
 }
 
-Paged paged_of(const pf_paged_desc& s, const pf_paged_cache* c) {
+// Of a quantised cache; e NULL: none is.
+pf_status check_exp(const pf_paged_exp* e) {
+  if (e && (!e->K || !e->V || !aligned16(e->K) || !aligned16(e->V)))
+    return fail(PF_ERR_INVALID_ARG, "the exponents of K and V are required, 16-byte aligned");
+  return PF_OK;
+}
+
+Paged paged_of(const pf_paged_desc& s, const pf_paged_cache* c, const pf_paged_exp* e = nullptr) {
   Paged p{s.batch, s.n_heads, s.n_kv, s.dh, s.page, s.max_pages, (long)s.n_pages, s.window, s.n_sink,
-          nullptr, nullptr, nullptr, nullptr};
+          nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+  if (e) {
+    p.Ke = reinterpret_cast<signed char*>(e->K);
+    p.Ve = reinterpret_cast<signed char*>(e->V);
+  }
   if (c) {
     p.K = static_cast<bf16*>(c->K);
     p.V = static_cast<bf16*>(c->V);
@@ -223,6 +234,62 @@ Paged paged_of(const pf_paged_desc& s, const pf_paged_cache* c) {
     p.len = c->len;
   }
   return p;
+}
+
+pf_status append(const pf_paged_desc* desc, const pf_qk_desc* qk, int64_t rows, const pf_qkv* x, const float* w_q,
+                 const float* w_k, const int32_t* start, const int32_t* pos, const pf_paged_cache* cache,
+                 const pf_paged_exp* exp, void* q_out, int64_t ld_q_out, void* stream) {
+  PF_TRY(check_paged(desc));
+  PF_TRY(check_qk(qk));
+  if (qk->n_heads != desc->n_heads || qk->n_kv != desc->n_kv || qk->dh != desc->dh)
+    return fail(PF_ERR_INVALID_ARG, "the two descriptors' heads differ");
+  if (qk->dtype != PF_BF16) return fail(PF_ERR_UNSUPPORTED, "the paged cache takes bf16");
+  PF_TRY(check_count(rows, 1, pos, qk->n_axes));
+  if (!start && rows != desc->batch)
+    return fail(PF_ERR_INVALID_ARG, "without start every sequence has one token: rows must be batch");
+  PF_TRY(check_cache(cache));
+  PF_TRY(check_exp(exp));
+  if (rows == 0) return PF_OK;
+  if (!x) return fail(PF_ERR_INVALID_ARG, "x is NULL");
+  if ((x->q == nullptr) != (q_out == nullptr))
+    return fail(PF_ERR_INVALID_ARG, "x->q and q_out go together");
+  if (q_out) {
+    PF_TRY(check_rows("q", x->q, x->ld_q, (int64_t)desc->n_heads * desc->dh, 2));
+    PF_TRY(check_rows("q_out", q_out, ld_q_out, (int64_t)desc->n_heads * desc->dh, 2));
+  }
+  PF_TRY(check_rows("k", x->k, x->ld_k, (int64_t)desc->n_kv * desc->dh, 2));
+  PF_TRY(check_rows("v", x->v, x->ld_v, (int64_t)desc->n_kv * desc->dh, 2));
+  if (q_out) {
+    const Area o = head_area("q_out", q_out, rows, ld_q_out, desc->n_heads, desc->dh, 2);
+    PF_TRY(check_over(o, head_area("q", x->q, rows, x->ld_q, desc->n_heads, desc->dh, 2)));
+    PF_TRY(check_apart(o, head_area("k", x->k, rows, x->ld_k, desc->n_kv, desc->dh, 2)));
+    PF_TRY(check_apart(o, head_area("v", x->v, rows, x->ld_v, desc->n_kv, desc->dh, 2)));
+  }
+  QkRope r = rope_of(*qk);
+  if (!q_out) r.H = 0;
+  PF_CUDA(paged_append(r, paged_of(*desc, cache, exp), ptr_of(*x), static_cast<bf16*>(q_out), (long)ld_q_out,
+                       w_q, w_k, start, pos, rows, static_cast<cudaStream_t>(stream)));
+  return PF_OK;
+}
+
+pf_status attn(const pf_paged_desc* desc, const void* q, int64_t ld_q, const pf_paged_cache* cache,
+               const pf_paged_exp* exp, void* out, int64_t ld_out, void* ws, size_t ws_bytes, void* stream) {
+  PF_TRY(check_paged(desc));
+  PF_TRY(check_rows("q", q, ld_q, (int64_t)desc->n_heads * desc->dh, 2));
+  PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
+  PF_TRY(check_cache(cache));
+  PF_TRY(check_exp(exp));
+  const Paged p = paged_of(*desc, cache, exp);
+  const size_t need = paged_attn_ws_bytes(p);
+  if (!ws || !aligned16(ws) || ws_bytes < need)
+    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need,
+                ws ? ws_bytes : 0);
+  // (a head's query is read before its row is written)
+  PF_TRY(check_over(head_area("out", out, desc->batch, ld_out, desc->n_heads, desc->dh, 2),
+                    head_area("q", q, desc->batch, ld_q, desc->n_heads, desc->dh, 2)));
+  PF_CUDA(paged_attn(p, static_cast<const bf16*>(q), (long)ld_q, static_cast<bf16*>(out), (long)ld_out,
+                     static_cast<float*>(ws), static_cast<cudaStream_t>(stream)));
+  return PF_OK;
 }
 
 }  // namespace
@@ -344,36 +411,15 @@ pf_status pf_paged_append(const pf_paged_desc* desc, const pf_qk_desc* qk, int64
                           const pf_qkv* x, const float* w_q, const float* w_k,
                           const int32_t* start, const int32_t* pos, pf_paged_cache* cache,
                           void* q_out, int64_t ld_q_out, void* stream) {
-  PF_TRY(check_paged(desc));
-  PF_TRY(check_qk(qk));
-  if (qk->n_heads != desc->n_heads || qk->n_kv != desc->n_kv || qk->dh != desc->dh)
-    return fail(PF_ERR_INVALID_ARG, "the two descriptors' heads differ");
-  if (qk->dtype != PF_BF16) return fail(PF_ERR_UNSUPPORTED, "the paged cache is bf16");
-  PF_TRY(check_count(rows, 1, pos, qk->n_axes));
-  if (!start && rows != desc->batch)
-    return fail(PF_ERR_INVALID_ARG, "without start every sequence has one token: rows must be batch");
-  PF_TRY(check_cache(cache));
-  if (rows == 0) return PF_OK;
-  if (!x) return fail(PF_ERR_INVALID_ARG, "x is NULL");
-  if ((x->q == nullptr) != (q_out == nullptr))
-    return fail(PF_ERR_INVALID_ARG, "x->q and q_out go together");
-  if (q_out) {
-    PF_TRY(check_rows("q", x->q, x->ld_q, (int64_t)desc->n_heads * desc->dh, 2));
-    PF_TRY(check_rows("q_out", q_out, ld_q_out, (int64_t)desc->n_heads * desc->dh, 2));
-  }
-  PF_TRY(check_rows("k", x->k, x->ld_k, (int64_t)desc->n_kv * desc->dh, 2));
-  PF_TRY(check_rows("v", x->v, x->ld_v, (int64_t)desc->n_kv * desc->dh, 2));
-  if (q_out) {
-    const Area o = head_area("q_out", q_out, rows, ld_q_out, desc->n_heads, desc->dh, 2);
-    PF_TRY(check_over(o, head_area("q", x->q, rows, x->ld_q, desc->n_heads, desc->dh, 2)));
-    PF_TRY(check_apart(o, head_area("k", x->k, rows, x->ld_k, desc->n_kv, desc->dh, 2)));
-    PF_TRY(check_apart(o, head_area("v", x->v, rows, x->ld_v, desc->n_kv, desc->dh, 2)));
-  }
-  QkRope r = rope_of(*qk);
-  if (!q_out) r.H = 0;
-  PF_CUDA(paged_append(r, paged_of(*desc, cache), ptr_of(*x), static_cast<bf16*>(q_out), (long)ld_q_out,
-                       w_q, w_k, start, pos, rows, static_cast<cudaStream_t>(stream)));
-  return PF_OK;
+  return append(desc, qk, rows, x, w_q, w_k, start, pos, cache, nullptr, q_out, ld_q_out, stream);
+}
+
+pf_status pf_paged_append_q8(const pf_paged_desc* desc, const pf_qk_desc* qk, int64_t rows, const pf_qkv* x,
+                             const float* w_q, const float* w_k, const int32_t* start, const int32_t* pos,
+                             pf_paged_cache* cache, const pf_paged_exp* exp, void* q_out, int64_t ld_q_out,
+                             void* stream) {
+  if (!exp) return fail(PF_ERR_INVALID_ARG, "exp is NULL");
+  return append(desc, qk, rows, x, w_q, w_k, start, pos, cache, exp, q_out, ld_q_out, stream);
 }
 
 size_t pf_paged_attn_workspace_size(const pf_paged_desc* desc) {
@@ -383,20 +429,58 @@ size_t pf_paged_attn_workspace_size(const pf_paged_desc* desc) {
 pf_status pf_paged_attn(const pf_paged_desc* desc, const void* q, int64_t ld_q,
                         const pf_paged_cache* cache, void* out, int64_t ld_out, void* ws,
                         size_t ws_bytes, void* stream) {
+  return attn(desc, q, ld_q, cache, nullptr, out, ld_out, ws, ws_bytes, stream);
+}
+
+pf_status pf_paged_attn_q8(const pf_paged_desc* desc, const void* q, int64_t ld_q, const pf_paged_cache* cache,
+                           const pf_paged_exp* exp, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
+                           void* stream) {
+  if (!exp) return fail(PF_ERR_INVALID_ARG, "exp is NULL");
+  return attn(desc, q, ld_q, cache, exp, out, ld_out, ws, ws_bytes, stream);
+}
+
+size_t pf_paged_chunk_workspace_size(const pf_paged_desc* desc, int64_t rows) {
+  if (check_paged(desc) != PF_OK || check_count(rows, 1, nullptr, 0) != PF_OK) return 0;
+  return paged_chunk_ws_bytes(paged_of(*desc, nullptr), rows);
+}
+
+pf_status pf_paged_chunk_attn(const pf_paged_desc* desc, int64_t rows, const void* q, int64_t ld_q,
+                              const int32_t* start, const pf_paged_cache* cache, const pf_paged_exp* exp, void* out,
+                              int64_t ld_out, void* ws, size_t ws_bytes, void* stream) {
   PF_TRY(check_paged(desc));
+  PF_TRY(check_count(rows, 1, nullptr, 0));
+  if (!start) return fail(PF_ERR_INVALID_ARG, "start is required");
+  PF_TRY(check_cache(cache));
+  PF_TRY(check_exp(exp));
+  if (rows == 0) return PF_OK;
   PF_TRY(check_rows("q", q, ld_q, (int64_t)desc->n_heads * desc->dh, 2));
   PF_TRY(check_rows("out", out, ld_out, (int64_t)desc->n_heads * desc->dh, 2));
+  const Paged p = paged_of(*desc, cache, exp);
+  const size_t need = paged_chunk_ws_bytes(p, rows);
+  if (need > 0 && (!ws || !aligned16(ws) || ws_bytes < need))
+    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : 0);
+  PF_TRY(check_apart(head_area("out", out, rows, ld_out, desc->n_heads, desc->dh, 2),
+                     head_area("q", q, rows, ld_q, desc->n_heads, desc->dh, 2)));
+  PF_CUDA(paged_chunk(p, rows, static_cast<const bf16*>(q), (long)ld_q, start, static_cast<bf16*>(out), (long)ld_out,
+                      ws, static_cast<cudaStream_t>(stream)));
+  return PF_OK;
+}
+
+pf_status pf_paged_read(const pf_paged_desc* desc, int64_t rows, const int32_t* start, const pf_paged_cache* cache,
+                        const pf_paged_exp* exp, void* k, int64_t ld_k, void* v, int64_t ld_v, void* stream) {
+  PF_TRY(check_paged(desc));
+  PF_TRY(check_count(rows, 1, nullptr, 0));
+  if (!start && rows != desc->batch)
+    return fail(PF_ERR_INVALID_ARG, "without start every sequence has one row: rows must be batch");
   PF_TRY(check_cache(cache));
-  const Paged p = paged_of(*desc, cache);
-  const size_t need = paged_attn_ws_bytes(p);
-  if (!ws || !aligned16(ws) || ws_bytes < need)
-    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need,
-                ws ? ws_bytes : 0);
-  // (a head's query is read before its row is written)
-  PF_TRY(check_over(head_area("out", out, desc->batch, ld_out, desc->n_heads, desc->dh, 2),
-                    head_area("q", q, desc->batch, ld_q, desc->n_heads, desc->dh, 2)));
-  PF_CUDA(paged_attn(p, static_cast<const bf16*>(q), (long)ld_q, static_cast<bf16*>(out), (long)ld_out,
-                     static_cast<float*>(ws), static_cast<cudaStream_t>(stream)));
+  PF_TRY(check_exp(exp));
+  if (rows == 0) return PF_OK;
+  PF_TRY(check_rows("k", k, ld_k, (int64_t)desc->n_kv * desc->dh, 2));
+  PF_TRY(check_rows("v", v, ld_v, (int64_t)desc->n_kv * desc->dh, 2));
+  PF_TRY(check_apart(head_area("k", k, rows, ld_k, desc->n_kv, desc->dh, 2),
+                     head_area("v", v, rows, ld_v, desc->n_kv, desc->dh, 2)));
+  PF_CUDA(paged_read(paged_of(*desc, cache, exp), rows, start, static_cast<bf16*>(k), (long)ld_k,
+                     static_cast<bf16*>(v), (long)ld_v, static_cast<cudaStream_t>(stream)));
   return PF_OK;
 }
 

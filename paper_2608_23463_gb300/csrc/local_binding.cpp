@@ -62,7 +62,7 @@ struct Rows {
 Rows rows_of(const char* name, const at::Tensor& t, int64_t rows, int64_t width, at::ScalarType type,
              c10::Device dev) {
   if (t.dim() != 2 || t.size(0) != rows || t.size(1) != width || t.scalar_type() != type ||
-      !t.is_cuda() || t.device() != dev || (width > 1 && t.stride(1) != 1))
+      !t.is_cuda() || t.device() != dev || (rows > 0 && width > 1 && t.stride(1) != 1))
     raise(PF_ERR_INVALID_ARG, std::string(name) + " must be a [" + std::to_string(rows) + ", " +
                                   std::to_string(width) + "] " + c10::toString(type) +
                                   " matrix with contiguous rows on one GPU");
@@ -251,51 +251,100 @@ PyObject* window_bwd(PyObject* const* a) {
   return tuple(dq, dk, dv);
 }
 
-// paged_append(desc, qk_desc, cache, len, q or None, k, v, w_q, w_k, start, pos, out) -> q or None
+// (exp: a quantised cache's exponents, or 0)
+// paged_append(desc, qk_desc, cache, exp, len, q or None, k, v, w_q, w_k, start, pos, out) -> q or None
 PyObject* paged_append(PyObject* const* a) {
   const pf_paged_desc& d = *address<pf_paged_desc>(a[0]);
   const pf_qk_desc& r = *address<pf_qk_desc>(a[1]);
   pf_paged_cache* cache = address<pf_paged_cache>(a[2]);
-  const at::Tensor &k = tensor("k", a[5]), &v = tensor("v", a[6]);
+  const pf_paged_exp* exp = address<pf_paged_exp>(a[3]);
+  const at::Tensor &k = tensor("k", a[6]), &v = tensor("v", a[7]);
   const c10::Device dev = cuda_device("k", k);
-  values<int32_t>("len", a[3], {d.batch}, at::kInt, dev);  // the cache is on that GPU
+  values<int32_t>("len", a[4], {d.batch}, at::kInt, dev);  // the cache is on that GPU
   const int64_t n = row_count("k", k), nq = (int64_t)d.n_heads * d.dh, nk = (int64_t)d.n_kv * d.dh;
   const Rows kr = rows_of("k", k, n, nk, at::kBFloat16, dev), vr = rows_of("v", v, n, nk, at::kBFloat16, dev);
   Rows qr{nullptr, 0}, o{nullptr, 0};
   at::Tensor out;
-  if (!none(a[4])) {
-    qr = rows_of("q", tensor("q", a[4]), n, nq, at::kBFloat16, dev);
-    out = result(a[11], n, nq, at::kBFloat16, dev);
+  if (!none(a[5])) {
+    qr = rows_of("q", tensor("q", a[5]), n, nq, at::kBFloat16, dev);
+    out = result(a[12], n, nq, at::kBFloat16, dev);
     o = rows_of("out", out, n, nq, at::kBFloat16, dev);
   }
-  const float* w_q = values<float>("w_q", a[7], {r.dh}, at::kFloat, dev);
-  const float* w_k = values<float>("w_k", a[8], {r.dh}, at::kFloat, dev);
-  const int32_t* start = values<int32_t>("start", a[9], {d.batch + 1}, at::kInt, dev);
-  const int32_t* pos = values<int32_t>("pos", a[10], {n, r.n_axes}, at::kInt, dev);
+  const float* w_q = values<float>("w_q", a[8], {r.dh}, at::kFloat, dev);
+  const float* w_k = values<float>("w_k", a[9], {r.dh}, at::kFloat, dev);
+  const int32_t* start = values<int32_t>("start", a[10], {d.batch + 1}, at::kInt, dev);
+  const int32_t* pos = values<int32_t>("pos", a[11], {n, r.n_axes}, at::kInt, dev);
   const pf_qkv x = {qr.p, kr.p, vr.p, qr.ld, kr.ld, vr.ld};
   call(dev, [&](void* s) {
-    return pf_paged_append(&d, &r, n, &x, w_q, w_k, start, pos, cache, o.p, o.ld, s);
+    return exp ? pf_paged_append_q8(&d, &r, n, &x, w_q, w_k, start, pos, cache, exp, o.p, o.ld, s)
+               : pf_paged_append(&d, &r, n, &x, w_q, w_k, start, pos, cache, o.p, o.ld, s);
   });
   if (!out.defined()) Py_RETURN_NONE;
   return wrap(out);
 }
 
-// paged_attn(desc, cache, q, out, ws) -> out
+// paged_attn(desc, cache, exp, len, q, out, ws) -> out
 PyObject* paged_attn(PyObject* const* a) {
   const pf_paged_desc& d = *address<pf_paged_desc>(a[0]);
   const pf_paged_cache* cache = address<pf_paged_cache>(a[1]);
-  const at::Tensor& q = tensor("q", a[2]);
+  const pf_paged_exp* exp = address<pf_paged_exp>(a[2]);
+  const at::Tensor& q = tensor("q", a[4]);
   const c10::Device dev = cuda_device("q", q);
+  values<int32_t>("len", a[3], {d.batch}, at::kInt, dev);  // the cache is on that GPU
   const int64_t nq = (int64_t)d.n_heads * d.dh;
   const Rows qr = rows_of("q", q, d.batch, nq, at::kBFloat16, dev);
-  const at::Tensor out = result(a[3], d.batch, nq, at::kBFloat16, dev);
+  const at::Tensor out = result(a[5], d.batch, nq, at::kBFloat16, dev);
   const Rows o = rows_of("out", out, d.batch, nq, at::kBFloat16, dev);
   size_t size;
-  void* ws = bytes("ws", a[4], dev, &size);
+  void* ws = bytes("ws", a[6], dev, &size);
   call(dev, [&](void* s) {
-    return pf_paged_attn(&d, qr.p, qr.ld, cache, o.p, o.ld, ws, size, s);
+    return exp ? pf_paged_attn_q8(&d, qr.p, qr.ld, cache, exp, o.p, o.ld, ws, size, s)
+               : pf_paged_attn(&d, qr.p, qr.ld, cache, o.p, o.ld, ws, size, s);
   });
   return wrap(out);
+}
+
+// paged_chunk(desc, cache, exp, len, q, start, out) -> out
+PyObject* paged_chunk(PyObject* const* a) {
+  const pf_paged_desc& d = *address<pf_paged_desc>(a[0]);
+  const pf_paged_cache* cache = address<pf_paged_cache>(a[1]);
+  const pf_paged_exp* exp = address<pf_paged_exp>(a[2]);
+  const at::Tensor& q = tensor("q", a[4]);
+  const c10::Device dev = cuda_device("q", q);
+  values<int32_t>("len", a[3], {d.batch}, at::kInt, dev);
+  const int64_t n = row_count("q", q), nq = (int64_t)d.n_heads * d.dh;
+  const Rows qr = rows_of("q", q, n, nq, at::kBFloat16, dev);
+  const int32_t* start = values<int32_t>("start", a[5], {d.batch + 1}, at::kInt, dev);
+  const at::Tensor out = result(a[6], n, nq, at::kBFloat16, dev);
+  const Rows o = rows_of("out", out, n, nq, at::kBFloat16, dev);
+  // scratch of this call alone: the stream that it runs on gets its memory back
+  const size_t size = pf_paged_chunk_workspace_size(&d, n);
+  at::Tensor ws;
+  if (size > 0) {
+    const c10::cuda::CUDAGuard guard(dev);
+    ws = at::empty({(int64_t)size}, at::TensorOptions().dtype(at::kByte).device(dev));
+  }
+  call(dev, [&](void* s) {
+    return pf_paged_chunk_attn(&d, n, qr.p, qr.ld, start, cache, exp, o.p, o.ld, size > 0 ? ws.data_ptr() : nullptr,
+                               size, s);
+  });
+  return wrap(out);
+}
+
+// paged_read(desc, cache, exp, len, rows, start, k, v) -> (k, v)
+PyObject* paged_read(PyObject* const* a) {
+  const pf_paged_desc& d = *address<pf_paged_desc>(a[0]);
+  const pf_paged_cache* cache = address<pf_paged_cache>(a[1]);
+  const pf_paged_exp* exp = address<pf_paged_exp>(a[2]);
+  const at::Tensor& len = tensor("len", a[3]);
+  const c10::Device dev = cuda_device("len", len);
+  const int64_t n = integer(a[4]), nk = (int64_t)d.n_kv * d.dh;
+  if (n < 0) raise(PF_ERR_INVALID_ARG, "rows must not be negative");
+  const int32_t* start = values<int32_t>("start", a[5], {d.batch + 1}, at::kInt, dev);
+  const at::Tensor k = result(a[6], n, nk, at::kBFloat16, dev), v = result(a[7], n, nk, at::kBFloat16, dev);
+  const Rows kr = rows_of("out k", k, n, nk, at::kBFloat16, dev), vr = rows_of("out v", v, n, nk, at::kBFloat16, dev);
+  call(dev, [&](void* s) { return pf_paged_read(&d, n, start, cache, exp, kr.p, kr.ld, vr.p, vr.ld, s); });
+  return tuple(k, v);
 }
 
 // One of the functions above as Python calls it: N arguments, C++ exceptions turned into
@@ -334,8 +383,10 @@ PyMethodDef kMethods[] = {
     method<rope_bwd, 12>("rope_bwd"),
     method<window_fwd, 6>("window_fwd"),
     method<window_bwd, 11>("window_bwd"),
-    method<paged_append, 12>("paged_append"),
-    method<paged_attn, 5>("paged_attn"),
+    method<paged_append, 13>("paged_append"),
+    method<paged_attn, 7>("paged_attn"),
+    method<paged_chunk, 7>("paged_chunk"),
+    method<paged_read, 8>("paged_read"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_local", nullptr, -1, kMethods};

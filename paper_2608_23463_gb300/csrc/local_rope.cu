@@ -33,6 +33,7 @@
 #include <type_traits>
 
 #include "local.h"
+#include "paged_q8.cuh"
 
 namespace pf {
 
@@ -75,6 +76,7 @@ struct RopeArgs {
   const void* v;
   long ldv;
   bf16 *K, *V;                       // [n_pages, KV, page, dh]
+  signed char *Ke, *Ve;              // quantised: their exponents [n_pages, KV, page] (K and V are bytes then)
   const int *table, *len, *start;
   int B, page, max_pages;
   long n_pages;
@@ -153,9 +155,10 @@ __device__ __forceinline__ void stage_weights(RopeSmem& s, const RopeArgs& a) {
 
 // cos and sin of the lane's pairs at the token's position(s), packed as the
 // values.  bf16 rows take the hardware sine (absolute error below 2^-20 for
-// |angle| <= pi, a 2000th of the rounding of the result); fp32 rows the
-// library's.
-template <class T, int DH>
+// |angle| <= pi, a 2000th of the rounding of the result); fp32 rows, and those that
+// are quantised (whole numbers come out as they would of exact values but for one in
+// some ten thousand), the library's.
+template <class T, int DH, bool EXACT = sizeof(T) == 4>
 __device__ __forceinline__ void turn_of(const RopeSmem& s, const int* pos3, int lane, float2* cs,
                                         float2* sn) {
   using Ly = Lay<T, DH>;
@@ -166,7 +169,7 @@ __device__ __forceinline__ void turn_of(const RopeSmem& s, const int* pos3, int 
     const int ps = ax == 0 ? pos3[0] : ax == 1 ? pos3[1] : pos3[2];
     const unsigned long long ph = (unsigned long long)(long long)ps * s.f[p];
     const float h = (float)(int)(ph >> 32) * 4.656612873077393e-10f;  // half turns, [-1, 1]
-    if (sizeof(T) == 2)
+    if (!EXACT)
       __sincosf(h * 3.14159265358979f, &os[i], &oc[i]);
     else
       sincospif(h, &os[i], &oc[i]);
@@ -190,6 +193,32 @@ __device__ __forceinline__ float head_sum(float v) {
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
+// A head's 8 values of a lane (e, o as above) quantised: row and exponent.  All lanes of the head
+// take part; `in`: it is one to be written.
+template <int LANES>
+__device__ __forceinline__ void put_q8(const float2* e, const float2* o, signed char* row, signed char* ex, int sub,
+                                       bool in) {
+  const float y[8] = {e[0].x, o[0].x, e[0].y, o[0].y, e[1].x, o[1].x, e[1].y, o[1].y};
+  int m = 0;  // of the bits: NaN counts as larger than all else
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_int(y[i]) & 0x7fffffff);
+#pragma unroll
+  for (int s = LANES / 2; s > 0; s >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
+  const int x = pq_exp(__int_as_float(m));
+  const float f = pq_down(x);
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t n[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) n[k] = (uint32_t)__float2int_rn(y[4 * i + k] * f);
+    w[i] = __byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410);
+  }
+  if (!in) return;
+  *reinterpret_cast<uint2*>(row) = make_uint2(w[0], w[1]);
+  if (sub == 0) *ex = (signed char)x;
+}
+
 // n passes, U at a time without a branch between them, so that their shuffles overlap, and
 // what is left of them singly.
 template <int U, class F>
@@ -200,11 +229,12 @@ __device__ __forceinline__ void in_passes(int n, F pass) {
 }
 
 // Passes [p0, p1) of one token's heads (head p * HEADS + the lane's slot, below
-// nh), normed and turned: src + head * DH -> dst + head * dst_stride.
-template <class T, int DH>
-__device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride, int p0, int p1,
+// nh), normed and turned: src + head * DH -> dst + head * dst_stride; Q8: quantised, dst of bytes,
+// the exponents to ex + head * dst_stride / DH.
+template <class T, int DH, bool Q8 = false, class D = T>
+__device__ __forceinline__ void rope_heads(const T* src, D* dst, long dst_stride, int p0, int p1,
                                            int nh, const float2* w, bool norm, float eps,
-                                           const float2* cs, const float2* sn, int lane) {
+                                           const float2* cs, const float2* sn, int lane, signed char* ex = nullptr) {
   using Ly = Lay<T, DH>;
   constexpr int G = Ly::G;
   const int sub = lane % Ly::LANES, slot = lane / Ly::LANES;
@@ -220,7 +250,7 @@ __device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride
   }
   int h = p0 * Ly::HEADS + slot;
   const T* sp = src + (long)h * DH + sub * Ly::N;
-  T* dp = dst + h * dst_stride + sub * Ly::N;
+  D* dp = dst + h * dst_stride + sub * Ly::N;
   const long dstep = Ly::HEADS * dst_stride;
   auto pass = [&](auto count) {
     constexpr int U = decltype(count)::value;
@@ -252,7 +282,10 @@ __device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride
           zo[k] = __fmul2_rn(zo[k], both(r));
         }
       }
-      if (h + i * Ly::HEADS < nh) *reinterpret_cast<uint4*>(dp + i * dstep) = Vec<T>::put(ze, zo);
+      if constexpr (Q8)
+        put_q8<Ly::LANES>(ze, zo, dp + i * dstep, ex + (h + i * Ly::HEADS) * (dst_stride / DH), sub, h + i * Ly::HEADS < nh);
+      else if (h + i * Ly::HEADS < nh)
+        *reinterpret_cast<uint4*>(dp + i * dstep) = Vec<T>::put(ze, zo);
     }
     h += U * Ly::HEADS;
     sp += U * Ly::HEADS * DH;
@@ -261,9 +294,9 @@ __device__ __forceinline__ void rope_heads(const T* src, T* dst, long dst_stride
   in_passes<RW_FWD_U>(p1 - p0, pass);
 }
 
-// Forward (APPEND: keys and values go to their cache pages).  A unit is part
+// Forward (APPEND: keys and values go to their cache pages; Q8: quantised).  A unit is part
 // `pt` of a token's passes: q heads, then k heads, then (APPEND) v heads.
-template <class T, int DH, bool APPEND>
+template <class T, int DH, bool APPEND, bool Q8 = false>
 __global__ void __launch_bounds__(RW_THREADS, RW_FWD_CTAS)
     rope_fwd_kernel(RopeArgs a, const __grid_constant__ RopeFreq fr) {
   using Ly = Lay<T, DH>;
@@ -280,6 +313,7 @@ __global__ void __launch_bounds__(RW_THREADS, RW_FWD_CTAS)
     const int p0 = pt * passes / a.parts, p1 = (pt + 1) * passes / a.parts;
     int pos3[3] = {0, 0, 0};
     bf16 *kd = nullptr, *vd = nullptr;
+    long at = 0;  // the token's row of the pool, of its first head
     if (APPEND) {
       // the token's sequence: how many of them end at or before it
       int b = row;
@@ -299,9 +333,9 @@ __global__ void __launch_bounds__(RW_THREADS, RW_FWD_CTAS)
       if (pg < 0 || pg >= a.n_pages) {
         if (lane == 0) set_dev_error(DEVERR_CAPACITY);
       } else {
-        const long o = (pg * a.KV * a.page + crow % a.page) * DH;
-        kd = a.K + o;
-        vd = a.V + o;
+        at = pg * a.KV * a.page + crow % a.page;
+        kd = a.K + at * DH;
+        vd = a.V + at * DH;
       }
     } else if (!a.pos) {
       pos3[0] = row % a.seq_len;
@@ -312,7 +346,7 @@ __global__ void __launch_bounds__(RW_THREADS, RW_FWD_CTAS)
         if (i < fr.n_axes) pos3[i] = a.pos[(long)row * fr.n_axes + i];
     }
     float2 cs[Ly::G], sn[Ly::G];
-    turn_of<T, DH>(s, pos3, lane, cs, sn);
+    turn_of<T, DH, Q8 || sizeof(T) == 4>(s, pos3, lane, cs, sn);
     if (p0 < nq)
       rope_heads<T, DH>(static_cast<const T*>(a.q) + row * a.ldq, static_cast<T*>(a.qo) + row * a.ldqo,
                         DH, p0, min(p1, nq), a.H, s.w[0], a.w_q != nullptr, a.eps, cs, sn, lane);
@@ -324,6 +358,24 @@ __global__ void __launch_bounds__(RW_THREADS, RW_FWD_CTAS)
                           a.w_k != nullptr, a.eps, cs, sn, lane);
     } else if (kd) {
       const long hs = (long)a.page * DH;
+      if constexpr (Q8) {
+        if (k0 < k1)
+          rope_heads<T, DH, true>(ks, reinterpret_cast<signed char*>(a.K) + at * DH, hs, k0, k1, a.KV, s.w[1],
+                                  a.w_k != nullptr, a.eps, cs, sn, lane, a.Ke + at);
+        const int slot = lane / Ly::LANES, sub = lane % Ly::LANES;
+        const T* vs = static_cast<const T*>(a.v) + row * a.ldv;
+#pragma unroll 2
+        for (int p = max(p0, nq + nk) - nq - nk; p < p1 - nq - nk; ++p) {
+          const int h = p * Ly::HEADS + slot;
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if (h < a.KV) u = *reinterpret_cast<const uint4*>(vs + h * DH + sub * Ly::N);
+          float2 e[Ly::G], o[Ly::G];
+          Vec<T>::get(u, e, o);
+          put_q8<Ly::LANES>(e, o, reinterpret_cast<signed char*>(a.V) + at * DH + h * hs + sub * Ly::N,
+                            a.Ve + at + (long)h * a.page, sub, h < a.KV);
+        }
+        continue;
+      }
       if (k0 < k1)
         rope_heads<T, DH>(ks, reinterpret_cast<T*>(kd), hs, k0, k1, a.KV, s.w[1], a.w_k != nullptr,
                           a.eps, cs, sn, lane);
@@ -607,14 +659,17 @@ cudaError_t paged_append(const QkRope& s, const Paged& c, const QkvPtr& x, bf16*
   o.q = q_out;
   o.ldq = ldqo;
   RopeArgs a = args_of(s, x, o, w_q, w_k, pos, rows, 1);
-  a.K = c.K; a.V = c.V;
+  a.K = c.K; a.V = c.V; a.Ke = c.Ke; a.Ve = c.Ve;
   a.table = c.table; a.len = c.len; a.start = start;
   a.B = c.B; a.page = c.page; a.max_pages = c.max_pages;
   a.n_pages = c.n_pages;
   set_parts(a, s, true);
   const double n = (double)rows * s.dh;
-  LaunchTimer lt("paged_append", st, 8.0 * n * (s.H + s.KV), 4.0 * n * (s.H + 2 * s.KV));
+  LaunchTimer lt("paged_append", st, 8.0 * n * (s.H + s.KV), (4.0 * s.H + (c.Ke ? 6.0 : 8.0) * s.KV) * n);
   const int grid = rope_grid(a, RW_FWD_CTAS);
+  if (c.Ke)
+    return launch_kernel(s.dh == 64 ? rope_fwd_kernel<bf16, 64, true, true> : rope_fwd_kernel<bf16, 128, true, true>,
+                         grid, RW_THREADS, 0, st, a, freq_of(s));
   return launch_kernel(s.dh == 64 ? rope_fwd_kernel<bf16, 64, true> : rope_fwd_kernel<bf16, 128, true>,
                        grid, RW_THREADS, 0, st, a, freq_of(s));
 }

@@ -1,5 +1,5 @@
 // Attention of one new token per sequence over a paged cache of keys and
-// values, bf16 with fp32 arithmetic, grouped heads.
+// values, bf16 or quantised (paged_q8.cuh), with fp32 arithmetic, grouped heads.
 //
 //   o_h = sum_j softmax_j(q_h . K_j / sqrt(dh)) V_j over the sequence's rows
 //   j < len, with a window W also j >= len - W or j < S (the sinks);
@@ -27,9 +27,15 @@
 // rows; else it leaves (max, sum, acc) of its piece, at most two of them (its
 // first and its last), and paged_join_kernel joins them in the order of the
 // CTAs, so that results repeat bit for bit.
+//
+// Quantised rows are read as they lie, 16 bytes a chunk: their whole numbers become bf16 in
+// registers, and the powers of two go into the scores and into P, where they are exact.  A
+// transposing load hands a thread two columns of V for two keys: the even ones of 16 columns are
+// one MMA's, the odd ones another's.
 #include <algorithm>
 
 #include "local.h"
+#include "paged_q8.cuh"
 
 namespace pf {
 
@@ -47,11 +53,12 @@ constexpr int PA_MAX_B = 2048;
 constexpr int PA_CTAS = 2 * 152;  // two rings an SM, whatever the device has (splits keep their places)
 constexpr float PA_RESCALE = 8.f;
 
-template <int DH>
+template <int DH, bool Q8>
 struct PaCfg {
-  static constexpr int TILE_BYTES = PA_TILE * DH * 2;  // of K, and of V
-  static constexpr int STAGES = DH == 128 ? 3 : 6;     // 24 KB a warp
-  static constexpr int WARP_BYTES = STAGES * 2 * TILE_BYTES;
+  static constexpr int TILE_BYTES = PA_TILE * DH * (Q8 ? 1 : 2);  // of K, and of V
+  static constexpr int STAGES = (DH == 128 ? 3 : 6) * (Q8 ? 2 : 1);  // 24 KB a warp
+  static constexpr int EXP = STAGES * 2 * TILE_BYTES;  // the tiles' exponents, 16 bytes of K, 16 of V
+  static constexpr int WARP_BYTES = EXP + (Q8 ? STAGES * 2 * PA_TILE : 0);
   static constexpr int SMEM = PA_WARPS * WARP_BYTES;
   static_assert(WARP_BYTES >= 16 * (DH + 4) * 4, "a warp's sums fit its ring");
 };
@@ -60,6 +67,7 @@ struct PaArgs {
   const bf16* q;
   long ldq;
   const bf16 *K, *V;
+  const signed char *Ke, *Ve;  // quantised rows' exponents (K and V are bytes then)
   const int *table, *len;
   bf16* out;
   long ldo;
@@ -145,13 +153,26 @@ __device__ __forceinline__ float ex2_approx(float x) {
   return y;
 }
 
+// Chunk c of row r in a quantised tile of K, and of V: the reads of eight lanes (two rows' chunks
+// of K, eight rows' same chunk of V) meet all banks.
+template <int DH>
+__device__ __forceinline__ uint32_t pa_k8(int r, int c) {
+  return DH == 128 ? (r * 8 + (c ^ ((r & 1) << 2))) * 16 : (r * 4 + c) * 16;
+}
+template <int DH>
+__device__ __forceinline__ uint32_t pa_v8(int r, int c) {
+  return DH == 128 ? (r * 8 + (c ^ (r & 7))) * 16 : (r * 4 + (c ^ (r >> 1 & 3))) * 16;
+}
+// The factor of a row's exponent (PQ_NAN: NaN).
+__device__ __forceinline__ float pa_factor(int e) { return e == PQ_NAN ? __int_as_float(0x7fffffff) : pq_scale(e); }
+
 // First unit of CTA c of G <= T, and the CTA that holds unit u, of T units.
 __device__ __forceinline__ long pa_first(long T, int G, int c) { return T * c / G; }
 __device__ __forceinline__ int pa_cta(long T, int G, long u) { return (int)(((u + 1) * G - 1) / T); }
 
-template <int DH>
+template <int DH, bool Q8>
 __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
-  using C = PaCfg<DH>;
+  using C = PaCfg<DH, Q8>;
   constexpr int KC = DH / 32;  // 32-wide chunks of a row, two MMAs each
   constexpr int NT = DH / 8;   // 8-wide output tiles
   extern __shared__ __align__(128) unsigned char ring[];
@@ -225,9 +246,23 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
         const int row = tile_row(i);
         const bool ok = pg >= 0 && pg < a.n_pages;
         if (!ok && lane == 0) set_dev_error(DEVERR_CAPACITY);
-        const long o = (((ok ? (long)pg : 0L) * a.KV + h) * a.page + row % a.page) * DH;
+        const long at = ((ok ? (long)pg : 0L) * a.KV + h) * a.page + row % a.page, o = at * DH;
         const uint32_t ks = wr + (i % C::STAGES) * 2 * C::TILE_BYTES, vs = ks + C::TILE_BYTES;
-        constexpr int CPR = DH / 8;  // 16-byte chunks of a row
+        constexpr int CPR = DH / (Q8 ? 16 : 8);  // 16-byte chunks of a row
+        if (Q8) {
+          const signed char *kb = reinterpret_cast<const signed char*>(a.K), *vb = reinterpret_cast<const signed char*>(a.V);
+#pragma unroll
+          for (int j = 0; j < PA_TILE * CPR / 32; ++j) {
+            const int e = j * 32 + lane, r = e / CPR, c = e % CPR;
+            const int j2 = row + r;
+            const bool in = ok && j2 < sp.n && (j2 >= sp.first || j2 < a.sinks);
+            const long src = in ? o + r * DH + c * 16 : 0;
+            cp_async16(ks + pa_k8<DH>(r, c), kb + src, in);
+            cp_async16(vs + pa_v8<DH>(r, c), vb + src, in);
+          }
+          // (those of rows that it does not see too: they are passed over where they are read)
+          if (lane < 2) cp_async16(wr + C::EXP + (i % C::STAGES) * 32 + 16 * lane, (lane ? a.Ve : a.Ke) + at, ok);
+        } else
 #pragma unroll
         for (int j = 0; j < PA_TILE * CPR / 32; ++j) {
           const int e = j * 32 + lane, r = e / CPR, c = e % CPR;
@@ -250,12 +285,14 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
     // the group's queries: rows gid and gid + 8 of the MMAs' A
     uint4 qa[KC], qb[KC];
     {
-      const bf16* qr = a.q + b * a.ldq + (long)h * a.g * DH + 8 * t;
+      // (a chunk of 16 quantised values meets two of 8 of Q's)
+      const bf16* qr = a.q + b * a.ldq + (long)h * a.g * DH + (Q8 ? 16 : 8) * t;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
+        const int at = Q8 ? 64 * (c / 2) + 8 * (c % 2) : 32 * c;
         qa[c] = qb[c] = make_uint4(0, 0, 0, 0);
-        if (gid < a.g) qa[c] = *reinterpret_cast<const uint4*>(qr + gid * DH + 32 * c);
-        if (gid + 8 < a.g) qb[c] = *reinterpret_cast<const uint4*>(qr + (gid + 8) * DH + 32 * c);
+        if (gid < a.g) qa[c] = *reinterpret_cast<const uint4*>(qr + gid * DH + at);
+        if (gid + 8 < a.g) qb[c] = *reinterpret_cast<const uint4*>(qr + (gid + 8) * DH + at);
       }
     }
     float acc[NT][4] = {};
@@ -274,6 +311,22 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
       // takes 8 values of a row at once; the sum over them is free of order, and
       // Q's are taken alike.
       float s[2][4] = {};
+      if (Q8) {
+        const float2 one = make_float2(1.f, 1.f), off = make_float2(pq_shift(1.f), pq_shift(1.f));
+#pragma unroll
+        for (int c = 0; c < DH / 64; ++c)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const uint4 k = *reinterpret_cast<const uint4*>(kp + pa_k8<DH>(n * 8 + gid, 4 * c + t));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint2 kv = pq_values(w == 0 ? k.x : w == 1 ? k.y : w == 2 ? k.z : k.w, one, off);
+              const uint4 ua = qa[2 * c + w / 2], ub = qb[2 * c + w / 2];
+              const uint32_t qv[4] = {w % 2 ? ua.z : ua.x, w % 2 ? ub.z : ub.x, w % 2 ? ua.w : ua.y, w % 2 ? ub.w : ub.y};
+              mma16816(s[n], qv, kv.x, kv.y);
+            }
+          }
+      } else
 #pragma unroll
       for (int c = 0; c < KC; ++c)
 #pragma unroll
@@ -287,13 +340,30 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
           mma16816(s[n], a1, k.z, k.w);
         }
       const int row = tile_row(i);
+      float vf[4];  // the values' factors of keys 8 n + 2 t + e at 2 n + e
+      if (Q8) {
+        const unsigned char* ex = wring + C::EXP + (i % C::STAGES) * 32;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int j = n * 8 + 2 * t + e;
+            const float kf = pa_factor((signed char)ex[j]);
+            vf[2 * n + e] = pa_factor((signed char)ex[PA_TILE + j]);
+            s[n][e] *= kf;
+            s[n][e + 2] *= kf;
+          }
+      }
       if (row > sp.n - PA_TILE || row < sp.first) {  // the last tile, the sinks', the window's first
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int j = row + n * 8 + 2 * t + e;
-            if (j >= sp.n || (j < sp.first && j >= a.sinks)) s[n][e] = s[n][e + 2] = -INFINITY;
+            if (j >= sp.n || (j < sp.first && j >= a.sinks)) {
+              s[n][e] = s[n][e + 2] = -INFINITY;
+              if (Q8) vf[2 * n + e] = 0.f;
+            }
           }
       }
       float mx[2];
@@ -329,9 +399,28 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
 #pragma unroll
           for (int k = 0; k < 2; ++k) e[2 * n + k] = ex2_approx(fmaf(s[n][2 * r + k], a.sl2, -ref));
         l[r] += (e[0] + e[1]) + (e[2] + e[3]);
+        if (Q8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) e[k] *= vf[k];
         p[r] = pack_bf16(e[0], e[1]);
         p[r + 2] = pack_bf16(e[2], e[3]);
       }
+      if (Q8) {
+        const float2 one = make_float2(1.f, 1.f), off = make_float2(pq_shift(1.f), pq_shift(1.f));
+#pragma unroll
+        for (int c = 0; c < NT; c += 4) {  // 32 columns
+          uint32_t v[4];
+          ldmatrix_x4_trans(vs + pa_v8<DH>(lane & 15, c / 2 + (lane >> 4)), v);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            // bytes 0, 2: keys 2 t and 2 t + 1 of an even column; 1, 3: of the odd one
+            const uint2 lo = pq_values(__byte_perm(v[2 * u], 0, 0x3120), one, off),
+                        hi = pq_values(__byte_perm(v[2 * u + 1], 0, 0x3120), one, off);
+            mma16816(acc[c + 2 * u], p, lo.x, hi.x);
+            mma16816(acc[c + 2 * u + 1], p, lo.y, hi.y);
+          }
+        }
+      } else
 #pragma unroll
       for (int c = 0; c < NT; c += 2) {
         const int r = lane & 15, ch = c + (lane >> 4);
@@ -351,9 +440,15 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
       float* w = reinterpret_cast<float*>(wring) + (gid + 8 * r) * (DH + 4);
+      if (Q8) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        *reinterpret_cast<float2*>(w + 8 * n + 2 * t) = make_float2(acc[n][2 * r], acc[n][2 * r + 1]);
+        for (int n = 0; n < NT; n += 2)
+          *reinterpret_cast<float4*>(w + 8 * n + 4 * t) =
+              make_float4(acc[n][2 * r], acc[n + 1][2 * r], acc[n][2 * r + 1], acc[n + 1][2 * r + 1]);
+      } else
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          *reinterpret_cast<float2*>(w + 8 * n + 2 * t) = make_float2(acc[n][2 * r], acc[n][2 * r + 1]);
       if (t == 0) *reinterpret_cast<float2*>(w + DH) = make_float2(m[r], l[r]);
     }
     __syncthreads();
@@ -483,16 +578,16 @@ int pa_grid(const Paged& c) {
   return (int)std::min<long>(PA_CTAS, units);
 }
 
-template <int DH>
+template <int DH, bool Q8>
 cudaError_t pa_launch(const PaArgs& a, bool split, cudaStream_t st) {
   static KernelOnce once;
-  cudaError_t e = once(reinterpret_cast<const void*>(paged_attn_kernel<DH>), PaCfg<DH>::SMEM);
+  cudaError_t e = once(reinterpret_cast<const void*>(paged_attn_kernel<DH, Q8>), PaCfg<DH, Q8>::SMEM);
   if (e != cudaSuccess) return e;
   const double rows = (double)a.B * a.KV * std::min<long>((long)a.max_pages * a.page, 0x7fffffffL);
   {
     // work: upper bound (every cache full)
-    LaunchTimer lt("paged_attn", st, 4.0 * rows * a.g * DH, 4.0 * rows * DH);
-    e = launch_kernel(paged_attn_kernel<DH>, a.G, PA_THREADS, PaCfg<DH>::SMEM, st, a);
+    LaunchTimer lt("paged_attn", st, 4.0 * rows * a.g * DH, (Q8 ? 2.0 : 4.0) * rows * DH);
+    e = launch_kernel(paged_attn_kernel<DH, Q8>, a.G, PA_THREADS, PaCfg<DH, Q8>::SMEM, st, a);
     if (e != cudaSuccess || !split) return e;
   }
   LaunchTimer lt("paged_join", st, 0.0, 8.0 * a.G * a.g * (DH + 2));
@@ -516,7 +611,7 @@ cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long 
   PaArgs a{};
   a.q = q;
   a.ldq = ldq;
-  a.K = c.K; a.V = c.V;
+  a.K = c.K; a.V = c.V; a.Ke = c.Ke; a.Ve = c.Ve;
   a.table = c.table; a.len = c.len;
   a.out = out;
   a.ldo = ldo;
@@ -528,7 +623,8 @@ cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long 
   a.G = a.whole ? c.B * c.KV : pa_grid(c);
   a.sl2 = 1.4426950408889634f / sqrtf((float)c.dh);
   const bool split = !a.whole && (long)c.max_pages * c.page > PA_UNIT;  // else no pair has two units
-  return c.dh == 128 ? pa_launch<128>(a, split, st) : pa_launch<64>(a, split, st);
+  if (c.Ke) return c.dh == 128 ? pa_launch<128, true>(a, split, st) : pa_launch<64, true>(a, split, st);
+  return c.dh == 128 ? pa_launch<128, false>(a, split, st) : pa_launch<64, false>(a, split, st);
 }
 
 }  // namespace pf

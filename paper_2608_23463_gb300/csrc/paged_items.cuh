@@ -1,0 +1,94 @@
+// How the attention of many new tokens over a paged cache is cut into work (paged_chunk.cu).
+//
+// An item is (sequence, key head, two query tiles): a tile holds tpt = 128 / g tokens with
+// the g query heads of the key head, g rows to a token, so that a row of K and V serves all
+// of them.  Its steps are the 128-row tiles of the cache that its tokens see: the sinks' [0,
+// ns) and the window's [lo, ...], without those in between.
+// The items of all sequences stand in one line, (sequence, head, pair), each as long as its
+// weight, and the CTAs share the line out evenly: one may begin and end inside an item.
+// Weights within a sequence have a closed sum, so that a CTA finds its part from the
+// sequences' totals alone.
+#pragma once
+
+#include <stdint.h>
+
+namespace pf {
+
+constexpr int PC_T = 128;  // rows of a query tile, keys of a step
+
+struct PcGeo {
+  int B, KV, g, tpt;
+  int W, S;  // window (0: none), sinks
+};
+
+// A sequence: its new tokens are [t0, t0 + n) of the call's, the last n of its len rows.
+struct PcSeq {
+  int t0, n, len;
+};
+
+// A place in the line: step s of an item; b = B: its end.
+struct PcAt {
+  int b, h, u, s;
+};
+
+struct PcSpan {
+  int pf, pl;  // positions of the first and the last token
+  int ns, lo, steps;
+  __host__ __device__ __forceinline__ int tile(int s) const { return s < ns ? s : lo + s - ns; }
+};
+
+__host__ __device__ __forceinline__ int pc_tiles(int rows) { return rows / PC_T + (rows % PC_T != 0); }
+__host__ __device__ __forceinline__ int pc_pairs(const PcGeo& g, const PcSeq& q) {
+  const int R = 2 * g.tpt;
+  return q.n / R + (q.n % R != 0);
+}
+
+__host__ __device__ __forceinline__ PcSpan pc_span(const PcGeo& g, const PcSeq& q, int u) {
+  const int R = 2 * g.tpt, a = u * R, p0 = q.len - q.n;
+  PcSpan s;
+  s.pf = p0 + a;
+  s.pl = p0 + (q.n - a < R ? q.n : a + R) - 1;
+  s.lo = g.W > 0 && s.pf >= g.W ? (s.pf - g.W + 1) / PC_T : 0;
+  const int sT = g.W > 0 ? pc_tiles(g.S) : 0;
+  s.ns = sT < s.lo ? sT : s.lo;
+  s.steps = s.ns + s.pl / PC_T - s.lo + 1;
+  return s;
+}
+
+// An item weighs three times the keys that its last token sees, rounded up to those that a full
+// pair there would, and what an item costs beside them; with one tile twice.  The sum over the
+// pairs before u.
+__host__ __device__ __forceinline__ long long pc_cum(const PcGeo& g, const PcSeq& q, int u) {
+  constexpr long long ITEM = 256;
+  const int P = pc_pairs(g, q);
+  const long long R = 2 * g.tpt, p0 = q.len - q.n, cap = g.W > 0 ? (long long)g.W + g.S + R : (1ll << 40);
+  auto sum = [&](long long n) {
+    long long k = cap > p0 ? (cap - p0) / R : 0;
+    if (k > n) k = n;
+    return 3 * (k * p0 + R * (k * (k + 1) / 2) + (n - k) * cap + n * ITEM);
+  };
+  const bool single = u == P && q.n - (P - 1) * (int)R <= g.tpt;
+  return single ? sum(u) - (sum(u) - sum(u - 1)) / 3 : sum(u);
+}
+
+// The item at weight y < pc_cum(P) of one head's pairs, and the step (whole: items are not cut, a
+// place inside one is its end).
+__host__ __device__ __forceinline__ void pc_find(const PcGeo& g, const PcSeq& q, long long y, bool whole, int* u,
+                                                 int* s) {
+  int lo = 0, hi = pc_pairs(g, q);
+  while (hi - lo > 1) {
+    const int m = lo + (hi - lo) / 2;
+    if (pc_cum(g, q, m) <= y) lo = m; else hi = m;
+  }
+  const long long at = pc_cum(g, q, lo), w = pc_cum(g, q, lo + 1) - at;
+  const int steps = pc_span(g, q, lo).steps;
+  *u = lo;
+  *s = whole ? (y > at ? steps : 0) : (int)((y - at) * steps / w);
+}
+
+// Where CTA c of n begins on a line of length T.
+__host__ __device__ __forceinline__ long long pc_share(long long T, int n, int c) {
+  return T / n * c + T % n * c / n;
+}
+
+}  // namespace pf

@@ -3,8 +3,9 @@
 ``QKRope`` norms and rotates queries and keys (``pf_qk_rope_*``), ``WindowAttention``
 is causal attention in a sliding window with sinks (``pf_window_attn_*``) and
 ``PagedKVCache`` keeps the keys and values of many sequences in pages
-(``pf_paged_*``): ``append`` writes new tokens' rows, ``attend`` is the attention
-of every sequence's newest token.  All calls run on the current CUDA stream;
+(``pf_paged_*``), in bf16 or quantised to 8 bits: ``append`` writes new tokens' rows,
+``attend`` is the attention of every sequence's newest token, or tokens, and ``read``
+gives rows back.  All calls run on the current CUDA stream;
 none does arithmetic of its own.  An object's calls share its workspace: use it on
 one stream at a time.  Matrices are 2D tensors whose rows may lie
 apart (a slice of a projection's output serves as it is).
@@ -17,7 +18,7 @@ from typing import Optional, Sequence, Tuple
 import torch
 
 from . import (PF_BF16, PF_ERR_CAPACITY, PF_ERR_CUDA, PF_ERR_INVALID_ARG, PF_F32, PagedCache,
-               PagedDesc, ProxyFormerError, QKDesc, WindowDesc, load, pf_paged_advance,
+               PagedDesc, PagedExp, ProxyFormerError, QKDesc, WindowDesc, load, pf_paged_advance,
                pf_paged_attn_workspace_size, pf_qk_rope_workspace_size, pf_window_attn_saved_size,
                pf_window_attn_workspace_size)
 from .buildlib import binding_tag
@@ -125,34 +126,55 @@ class PagedKVCache:
     layers: pass those of the first.  A step: ``reserve`` pages for the new rows
     (host), ``advance`` the lengths once, then ``append`` and ``attend`` layer by
     layer.  ``rope`` (a QKRope) is applied to keys, and queries, on the way in;
-    without it they are taken as they are."""
+    without it they are taken as they are.
+
+    ``dtype`` torch.int8 holds each row (one token and key head) as whole numbers
+    K, V and an exponent K_exp, V_exp [n_pages, n_kv, page] of its own, x * 2^e with
+    the least e that the row allows: half the memory, each value off by at most
+    1/127 of its row's largest.  All operators take such a cache."""
 
     def __init__(self, batch: int, n_heads: int, n_kv: int, dh: int, page: int, n_pages: int,
                  max_pages: int, rope: Optional[QKRope] = None, window: int = 0, n_sink: int = 0,
                  K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None,
                  table: Optional[torch.Tensor] = None, len: Optional[torch.Tensor] = None,
-                 device="cuda"):
+                 device="cuda", dtype: torch.dtype = torch.bfloat16,
+                 K_exp: Optional[torch.Tensor] = None, V_exp: Optional[torch.Tensor] = None):
         self.batch, self.n_heads, self.n_kv, self.dh, self.page = batch, n_heads, n_kv, dh, page
         self.n_pages, self.max_pages = n_pages, max_pages
         self.rope = rope or QKRope(n_heads, n_kv, dh, pairs=())
+        if dtype not in (torch.bfloat16, torch.int8):
+            raise ProxyFormerError(PF_ERR_INVALID_ARG, "dtype must be torch.bfloat16 or torch.int8")
+        self.dtype = dtype
         shape = (n_pages, n_kv, page, dh)
-        self.K, self.V = (torch.zeros(shape, dtype=torch.bfloat16, device=device) if t is None else t
+        self.K, self.V = (torch.zeros(shape, dtype=dtype, device=device) if t is None else t
                           for t in (K, V))
         for t in (self.K, self.V):
-            if tuple(t.shape) != shape or t.dtype != torch.bfloat16 or not t.is_contiguous():
-                raise ProxyFormerError(PF_ERR_INVALID_ARG, f"K and V must be contiguous bf16 {shape}")
+            if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+                raise ProxyFormerError(PF_ERR_INVALID_ARG, f"K and V must be contiguous {dtype} {shape}")
+        self.K_exp, self.V_exp = K_exp, V_exp
+        if dtype == torch.int8:
+            self.K_exp, self.V_exp = (torch.zeros(shape[:3], dtype=torch.int8, device=device) if t is None else t
+                                      for t in (K_exp, V_exp))
+        for t in (self.K_exp, self.V_exp):
+            if (t is None) != (dtype == torch.bfloat16) or t is not None and (
+                    tuple(t.shape) != shape[:3] or t.dtype != torch.int8 or not t.is_contiguous()):
+                raise ProxyFormerError(PF_ERR_INVALID_ARG, f"K_exp and V_exp are an int8 cache's, contiguous int8 {shape[:3]}")
         self.table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device) \
             if table is None else table
         self.len = torch.zeros(batch, dtype=torch.int32, device=device) if len is None else len
         for name, t, shape in (("table", self.table, (batch, max_pages)), ("len", self.len, (batch,))):
             if tuple(t.shape) != shape or t.dtype != torch.int32 or not t.is_contiguous():
                 raise ProxyFormerError(PF_ERR_INVALID_ARG, f"{name} must be contiguous int32 {shape}")
-        if not all(t.is_cuda and t.device == self.K.device for t in (self.V, self.table, self.len)):
+        if not all(t.is_cuda and t.device == self.K.device for t in (self.V, self.table, self.len, self.K_exp, self.V_exp)
+                   if t is not None):
             raise ProxyFormerError(PF_ERR_INVALID_ARG, "K, V, table and len must be on one GPU")
         self.desc = PagedDesc(batch, n_heads, n_kv, dh, page, max_pages, n_pages, window, n_sink)
         self.cache = PagedCache(self.K.data_ptr(), self.V.data_ptr(),
                                 self.table.data_ptr(), self.len.data_ptr())
-        self.at, self.at_cache = addressof(self.desc), addressof(self.cache)
+        self.at, self.at_cache, self.at_exp = addressof(self.desc), addressof(self.cache), 0
+        if dtype == torch.int8:
+            self.exp = PagedExp(self.K_exp.data_ptr(), self.V_exp.data_ptr())
+            self.at_exp = addressof(self.exp)
         self.ws = torch.empty(max(16, pf_paged_attn_workspace_size(self.desc)), dtype=torch.uint8,
                               device=self.K.device)
         self.free = list(range(n_pages - 1, -1, -1))  # pages that reserve() hands out
@@ -205,9 +227,27 @@ class PagedKVCache:
         queries q [rows, n_heads*dh] normed and turned (None without them).  start
         [batch+1] int32: first token of every sequence; None: one each."""
         r = self.rope
-        return _local.paged_append(self.at, r.at, self.at_cache, self.len, q, k, v, r.w_q, r.w_k, start,
-                                   pos, out)
+        return _local.paged_append(self.at, r.at, self.at_cache, self.at_exp, self.len, q, k, v, r.w_q, r.w_k,
+                                   start, pos, out)
 
-    def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Attention of every sequence's newest token, q [batch, n_heads*dh]."""
-        return _local.paged_attn(self.at, self.at_cache, q, out, self.ws)
+    def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+               start: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of every sequence's newest token, q [batch, n_heads*dh], or with start
+        (as in append) of the step's tokens, q [rows, n_heads*dh]: each sees the rows up to
+        its own.  Rows of q from start[batch] on are left alone in out."""
+        if start is not None:
+            return _local.paged_chunk(self.at, self.at_cache, self.at_exp, self.len, q, start, out)
+        return _local.paged_attn(self.at, self.at_cache, self.at_exp, self.len, q, out, self.ws)
+
+    def read(self, start: Optional[torch.Tensor] = None, rows: Optional[int] = None,
+             out=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The last rows of every sequence, start[b+1] - start[b] of them (None: one), as they
+        lie in the cache: keys (normed and turned) and values, [rows, n_kv*dh] bf16 (into ``out``,
+        a pair).  rows: start[batch], or more: what is past it is left alone."""
+        if rows is None and out is not None:
+            rows = out[0].shape[0]
+        if rows is None and start is not None:
+            raise ProxyFormerError(PF_ERR_INVALID_ARG, "read needs the number of rows beside start")
+        k, v = (None, None) if out is None else out
+        return _local.paged_read(self.at, self.at_cache, self.at_exp, self.len,
+                                 self.batch if rows is None else rows, start, k, v)
