@@ -511,6 +511,8 @@ pf_status pf_paged_append_q8(const pf_paged_desc *desc, const pf_qk_desc *qk, in
                              const pf_paged_exp *exp, void *q_out, int64_t ld_q_out,
                              void *stream);
 
+size_t pf_paged_attn_q8_workspace_size(const pf_paged_desc *desc);
+
 pf_status pf_paged_attn_q8(const pf_paged_desc *desc, const void *q, int64_t ld_q,
                            const pf_paged_cache *cache, const pf_paged_exp *exp, void *out,
                            int64_t ld_out, void *ws, size_t ws_bytes, void *stream);

@@ -116,7 +116,7 @@ EXPORTED = ("proxy_layer_check", "proxy_layer_saved_size", "proxy_layer_workspac
             "pf_window_attn_fwd", "pf_window_attn_saved_size", "pf_window_attn_workspace_size",
             "pf_window_attn_bwd",
             "pf_paged_advance", "pf_paged_append", "pf_paged_attn_workspace_size", "pf_paged_attn",
-            "pf_paged_append_q8", "pf_paged_attn_q8", "pf_paged_chunk_workspace_size",
+            "pf_paged_append_q8", "pf_paged_attn_q8_workspace_size", "pf_paged_attn_q8", "pf_paged_chunk_workspace_size",
             "pf_paged_chunk_attn", "pf_paged_read",
             "pf_last_error", "pf_sync_check", "pf_gemm_bf16", "pf_timing_enable",
             "pf_timing_collect", "pf_timing_label", "pf_timing_ms", "pf_timing_launches",
@@ -208,6 +208,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pf_paged_append_q8.argtypes = [P(PagedDesc), P(QKDesc), i64, P(QKV), _vp, _vp, _vp, _vp,
                                        P(PagedCache), P(PagedExp), _vp, i64, _vp]
     lib.pf_paged_append_q8.restype = ctypes.c_int
+    lib.pf_paged_attn_q8_workspace_size.argtypes = [P(PagedDesc)]
+    lib.pf_paged_attn_q8_workspace_size.restype = sz
     lib.pf_paged_attn_q8.argtypes = [P(PagedDesc), _vp, i64, P(PagedCache), P(PagedExp), _vp, i64,
                                      _vp, sz, _vp]
     lib.pf_paged_attn_q8.restype = ctypes.c_int
@@ -457,6 +459,10 @@ def pf_paged_append_q8(desc, qk, rows, x, w_q, w_k, start, pos, cache, exp, q_ou
                                      ctypes.byref(x), _ptr(w_q), _ptr(w_k), _ptr(start), _ptr(pos),
                                      ctypes.byref(cache), _ref(exp), _ptr(q_out), int(ld_q_out),
                                      stream))
+
+
+def pf_paged_attn_q8_workspace_size(desc) -> int:
+    return load().pf_paged_attn_q8_workspace_size(ctypes.byref(desc))
 
 
 def pf_paged_attn_q8(desc, q, ld_q, cache, exp, out, ld_out, ws, ws_bytes, stream=None):

@@ -98,7 +98,7 @@ cudaError_t paged_advance(const Paged& c, const int* start, int* len, cudaStream
 
 #define PF_PAGED_MAX_BATCH 2048  // sequences of a call
 #define PF_PAGED_ROWS 16         // a page holds a multiple of so many rows
-size_t paged_attn_ws_bytes(const Paged& c);
+size_t paged_attn_ws_bytes(const Paged& c, bool q8);
 cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long ldo, float* ws,
                        cudaStream_t st);
 

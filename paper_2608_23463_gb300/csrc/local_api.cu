@@ -280,7 +280,7 @@ pf_status attn(const pf_paged_desc* desc, const void* q, int64_t ld_q, const pf_
   PF_TRY(check_cache(cache));
   PF_TRY(check_exp(exp));
   const Paged p = paged_of(*desc, cache, exp);
-  const size_t need = paged_attn_ws_bytes(p);
+  const size_t need = paged_attn_ws_bytes(p, exp != nullptr);
   if (!ws || !aligned16(ws) || ws_bytes < need)
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need,
                 ws ? ws_bytes : 0);
@@ -423,7 +423,11 @@ pf_status pf_paged_append_q8(const pf_paged_desc* desc, const pf_qk_desc* qk, in
 }
 
 size_t pf_paged_attn_workspace_size(const pf_paged_desc* desc) {
-  return check_paged(desc) == PF_OK ? paged_attn_ws_bytes(paged_of(*desc, nullptr)) : 0;
+  return check_paged(desc) == PF_OK ? paged_attn_ws_bytes(paged_of(*desc, nullptr), false) : 0;
+}
+
+size_t pf_paged_attn_q8_workspace_size(const pf_paged_desc* desc) {
+  return check_paged(desc) == PF_OK ? paged_attn_ws_bytes(paged_of(*desc, nullptr), true) : 0;
 }
 
 pf_status pf_paged_attn(const pf_paged_desc* desc, const void* q, int64_t ld_q,

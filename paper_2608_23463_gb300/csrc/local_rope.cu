@@ -205,7 +205,7 @@ __device__ __forceinline__ void put_q8(const float2* e, const float2* o, signed 
 #pragma unroll
   for (int s = LANES / 2; s > 0; s >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
   const int x = pq_exp(__int_as_float(m));
-  const float f = pq_down(x);
+  const float f = pq_inverse(x);
   uint32_t w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {

@@ -50,13 +50,14 @@ constexpr int PA_THREADS = 32 * PA_WARPS;
 constexpr int PA_TILE = 16;                    // rows of a warp's tile
 constexpr int PA_UNIT = PA_TILE * PA_WARPS;    // rows of a unit
 constexpr int PA_MAX_B = 2048;
-constexpr int PA_CTAS = 2 * 152;  // two rings an SM, whatever the device has (splits keep their places)
+// two rings an SM (quantised: three of them), whatever the device has (splits keep their places)
+constexpr int PA_CTAS = 2 * 152, PA_CTAS_Q8 = 3 * 152;
 constexpr float PA_RESCALE = 8.f;
 
 template <int DH, bool Q8>
 struct PaCfg {
   static constexpr int TILE_BYTES = PA_TILE * DH * (Q8 ? 1 : 2);  // of K, and of V
-  static constexpr int STAGES = (DH == 128 ? 3 : 6) * (Q8 ? 2 : 1);  // 24 KB a warp
+  static constexpr int STAGES = (DH == 128 ? 1 : 2) * (Q8 ? 4 : 3);  // 24 KB a warp, 16 KB
   static constexpr int EXP = STAGES * 2 * TILE_BYTES;  // the tiles' exponents, 16 bytes of K, 16 of V
   static constexpr int WARP_BYTES = EXP + (Q8 ? STAGES * 2 * PA_TILE : 0);
   static constexpr int SMEM = PA_WARPS * WARP_BYTES;
@@ -163,18 +164,21 @@ template <int DH>
 __device__ __forceinline__ uint32_t pa_v8(int r, int c) {
   return DH == 128 ? (r * 8 + (c ^ (r & 7))) * 16 : (r * 4 + (c ^ (r >> 1 & 3))) * 16;
 }
-// The factor of a row's exponent (PQ_NAN: NaN).
-__device__ __forceinline__ float pa_factor(int e) { return e == PQ_NAN ? __int_as_float(0x7fffffff) : pq_scale(e); }
+// The factor of a row's exponent (PQ_NAN: NaN), for values made 2^-PQ_DOWN of what they are.
+__device__ __forceinline__ float pa_factor(int e) {
+  return e == PQ_NAN ? __int_as_float(0x7fffffff) : pq_scale(e + PQ_DOWN);
+}
 
 // First unit of CTA c of G <= T, and the CTA that holds unit u, of T units.
 __device__ __forceinline__ long pa_first(long T, int G, int c) { return T * c / G; }
 __device__ __forceinline__ int pa_cta(long T, int G, long u) { return (int)(((u + 1) * G - 1) / T); }
 
 template <int DH, bool Q8>
-__global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
+__global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaArgs a) {
   using C = PaCfg<DH, Q8>;
   constexpr int KC = DH / 32;  // 32-wide chunks of a row, two MMAs each
   constexpr int NT = DH / 8;   // 8-wide output tiles
+  const uint32_t F0 = pq_factor(0), C0 = pq_offset(0);
   extern __shared__ __align__(128) unsigned char ring[];
   __shared__ int pre[PA_MAX_B + 1];
   pdl_enter();
@@ -312,7 +316,6 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
       // Q's are taken alike.
       float s[2][4] = {};
       if (Q8) {
-        const float2 one = make_float2(1.f, 1.f), off = make_float2(pq_shift(1.f), pq_shift(1.f));
 #pragma unroll
         for (int c = 0; c < DH / 64; ++c)
 #pragma unroll
@@ -320,7 +323,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
             const uint4 k = *reinterpret_cast<const uint4*>(kp + pa_k8<DH>(n * 8 + gid, 4 * c + t));
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-              const uint2 kv = pq_values(w == 0 ? k.x : w == 1 ? k.y : w == 2 ? k.z : k.w, one, off);
+              const uint2 kv = pq_down(w == 0 ? k.x : w == 1 ? k.y : w == 2 ? k.z : k.w, F0, C0);
               const uint4 ua = qa[2 * c + w / 2], ub = qb[2 * c + w / 2];
               const uint32_t qv[4] = {w % 2 ? ua.z : ua.x, w % 2 ? ub.z : ub.x, w % 2 ? ua.w : ua.y, w % 2 ? ub.w : ub.y};
               mma16816(s[n], qv, kv.x, kv.y);
@@ -406,7 +409,6 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
         p[r + 2] = pack_bf16(e[2], e[3]);
       }
       if (Q8) {
-        const float2 one = make_float2(1.f, 1.f), off = make_float2(pq_shift(1.f), pq_shift(1.f));
 #pragma unroll
         for (int c = 0; c < NT; c += 4) {  // 32 columns
           uint32_t v[4];
@@ -414,8 +416,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_kernel(PaArgs a) {
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             // bytes 0, 2: keys 2 t and 2 t + 1 of an even column; 1, 3: of the odd one
-            const uint2 lo = pq_values(__byte_perm(v[2 * u], 0, 0x3120), one, off),
-                        hi = pq_values(__byte_perm(v[2 * u + 1], 0, 0x3120), one, off);
+            const uint2 lo = pq_down_cols(v[2 * u], F0, C0), hi = pq_down_cols(v[2 * u + 1], F0, C0);
             mma16816(acc[c + 2 * u], p, lo.x, hi.x);
             mma16816(acc[c + 2 * u + 1], p, lo.y, hi.y);
           }
@@ -492,7 +493,7 @@ constexpr int PJ_THREADS = 512;
 template <int DH>
 __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a) {
   __shared__ int pre[PA_MAX_B + 1];
-  __shared__ float sw[PA_CTAS];
+  __shared__ float sw[PA_CTAS_Q8];
   __shared__ float red[16][33];
   __shared__ float sL;
   pdl_enter();
@@ -572,10 +573,10 @@ bool pa_whole(const Paged& c) {
 }
 
 // CTAs: two an SM, or a unit each.
-int pa_grid(const Paged& c) {
+int pa_grid(const Paged& c, bool q8) {
   const long rows = std::min<long>((long)c.max_pages * c.page, 0x7fffffffL);
   const long units = (rows + PA_UNIT - 1) / PA_UNIT * c.B * c.KV;
-  return (int)std::min<long>(PA_CTAS, units);
+  return (int)std::min<long>(q8 ? PA_CTAS_Q8 : PA_CTAS, units);
 }
 
 template <int DH, bool Q8>
@@ -601,8 +602,8 @@ cudaError_t pa_launch(const PaArgs& a, bool split, cudaStream_t st) {
 
 static_assert(PA_MAX_B == PF_PAGED_MAX_BATCH && PA_TILE == PF_PAGED_ROWS, "limits of the entry points");
 
-size_t paged_attn_ws_bytes(const Paged& c) {
-  return 2 * (size_t)pa_grid(c) * (c.H / c.KV) * (c.dh + 2) * sizeof(float);
+size_t paged_attn_ws_bytes(const Paged& c, bool q8) {
+  return 2 * (size_t)pa_grid(c, q8) * (c.H / c.KV) * (c.dh + 2) * sizeof(float);
 }
 
 cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long ldo, float* ws,
@@ -620,7 +621,7 @@ cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long 
   a.window = c.window; a.sinks = c.sinks;
   a.n_pages = c.n_pages;
   a.whole = pa_whole(c);
-  a.G = a.whole ? c.B * c.KV : pa_grid(c);
+  a.G = a.whole ? c.B * c.KV : pa_grid(c, c.Ke);
   a.sl2 = 1.4426950408889634f / sqrtf((float)c.dh);
   const bool split = !a.whole && (long)c.max_pages * c.page > PA_UNIT;  // else no pair has two units
   if (c.Ke) return c.dh == 128 ? pa_launch<128, true>(a, split, st) : pa_launch<64, true>(a, split, st);

@@ -16,8 +16,10 @@
 //   warps 2-3  MMA issuers of tile A's and tile B's O += P V (M=128, N=dh, K=128), P from TMEM
 //   warps 4-7  softmax of tile A, warps 8-11 of tile B: one row per thread (TMEM lane); the
 //              running maximum moves by more than 2^8 only, which then scales O
-//   warps 12-15 (quantised caches) fetch nothing: they turn the producer's raw tiles of bytes
-//              into the bf16 tiles that the MMAs read
+//   warps 12-19 (quantised caches) turn the producer's raw tiles of bytes into the bf16 tiles
+//              that the MMAs read, 2^-7 of the values
+// An item of one query tile shares its steps out between the two tiles' places, the even to A's
+// and the odd to B's, so that two steps are in flight as with two tiles.
 // TMEM holds both tiles' S and O; with dh = 128 P takes the place of S, from which it came.
 // An item that one CTA holds whole is written; pieces leave (O, maximum, sum) and
 // paged_chunk_join_kernel joins them in the order of the CTAs: results repeat bit for bit.
@@ -44,9 +46,10 @@ constexpr float PC_RESCALE = 8.f;
 
 template <int DH, bool Q8>
 struct PcCfg {
-  static constexpr int THREADS = Q8 ? 512 : 384;
+  static constexpr int CONV = Q8 ? 8 : 0;  // converting warps
+  static constexpr int THREADS = 384 + 32 * CONV;
   // registers of a control (and converting) and of a softmax thread, of the pool at launch
-  static constexpr int REGS_CTRL = Q8 ? 56 : 88, REGS_ROWS = Q8 ? 200 : 208;
+  static constexpr int REGS_CTRL = Q8 ? 72 : 88, REGS_ROWS = Q8 ? 128 : 208;
   static constexpr int POOL = REGS_CTRL * (THREADS - 256) + REGS_ROWS * 256;
   static_assert(POOL <= (65536 / THREADS / 8 * 8) * THREADS, "register split");
   static constexpr int HALVES = DH / 64;
@@ -54,14 +57,17 @@ struct PcCfg {
   static constexpr uint32_t TILE = HALVES * HALF;
   static constexpr int NK = DH == 64 ? 4 : 2, NV = DH == 64 ? 4 : (Q8 ? 2 : 3);  // stages
   static constexpr uint32_t RAW = PC_T * DH;  // a tile of bytes
-  static constexpr int NR = Q8 ? (DH == 64 ? 4 : 2) : 0;  // stages of them
-  static constexpr uint32_t OFF_K = 2 * TILE, OFF_V = OFF_K + NK * TILE, OFF_RAW = OFF_V + NV * TILE;
+  static constexpr int NR = Q8 ? (DH == 64 ? 4 : 2) : 0;  // stages of them, half for K, half for V
+  static constexpr int NQ = DH == 64 ? 2 : 1;  // items whose query tiles are held
+  static constexpr int AHEAD = NK < NV ? NK : NV;  // steps of an item that can be loaded before its queries
+  static constexpr uint32_t OFF_K = NQ * 2 * TILE, OFF_V = OFF_K + NK * TILE, OFF_RAW = OFF_V + NV * TILE;
   static constexpr uint32_t OFF_EXP = OFF_RAW + NR * RAW, OFF_BAR = OFF_EXP + NR * PC_T;
   static constexpr uint32_t SMEM = OFF_BAR + 512 + 1024;
   static_assert(SMEM <= 227 * 1024, "shared memory");
-  static_assert((PC_MAX_B + 1) * 8 <= (NK + NV) * TILE, "the sequences' totals lie in the rings at first");
+  static_assert((PC_MAX_B + 1) * 8 + PC_MAX_B * 12 <= (NK + NV) * TILE, "the totals lie in the rings at first");
   // TMEM columns of tile w: S at 128 w, O and P
   static constexpr bool ALIAS = DH == 128;
+  static constexpr float SCALE = Q8 ? 1 << PQ_DOWN : 1;  // the tiles hold so much less than the values
   __host__ __device__ static constexpr uint32_t tm_o(int w) { return 256 + DH * w; }
   __host__ __device__ static constexpr uint32_t tm_p(int w) { return ALIAS ? 128 * w : 384 + 64 * w; }
 };
@@ -70,20 +76,21 @@ struct PcArgs {
   PcGeo geo;
   const int *start, *len, *table;
   long rows;
-  int page, max_pages, box;  // box: rows of a TMA box
+  int page, max_pages, box, box_log;  // box: rows of a TMA box, 2^box_log
   long n_pages;
   int G;           // CTAs
   int whole, few;  // items to a CTA from which none is cut (whole: none ever); steps' weight to a CTA at least
-  float sl2;       // log2(e) / sqrt(dh)
+  int long_item;   // steps from which an item's unmasked ones take the long form
+  float sl2;       // log2(e) / sqrt(dh), of the tiles' keys
   const bf16* q;
   bf16* out;
   long ldq, ldo;
   const void *K, *V;
   const signed char *Ke, *Ve;
-  // pieces: where each CTA begins [G + 1], (maximum, sum) and O of the rows [2 G][rows of an item]
+  // pieces: where each CTA begins [G + 1], (maximum, sum) [2 G][rows of an item], O [2 G][dh / 4][rows]
   PcAt* at;
   float2* ml;
-  float* part;
+  float4* part;
   int piece_rows;
 };
 
@@ -113,53 +120,57 @@ __device__ __forceinline__ PcSeq pc_seq(const PcArgs& a, int b, bool* bad = null
   return s;
 }
 
+// A CTA's part of the line, and the sequence that it begins in.
+struct PcEnds {
+  PcAt at[2];
+  PcSeq q;
+};
+
+// A piece of an item: its steps [s0, s1).  s1 = 0: there are no more.
+struct PcItem {
+  PcSpan sp;
+  int b, h, t0, toks, s0, s1, place;  // place: of the piece among those of all CTAs
+  int two, duo, whole;  // with a tile B; tile A's steps shared with tile B's place; all of its steps
+};
+
 // The items from one place in the line to another.
 struct PcWalk {
   PcAt at, end;
   PcSeq q;
-  int pairs;
-  __device__ __forceinline__ PcWalk(const PcArgs& a, const PcAt* ends) : at(ends[0]), end(ends[1]) {
-    if (at.b < a.geo.B) load(a);
-  }
-  __device__ __forceinline__ void load(const PcArgs& a) {
-    q = pc_seq(a, at.b);
+  int pairs, n;  // n: items so far
+  __device__ __forceinline__ PcWalk(const PcArgs& a, const PcEnds& e) : at(e.at[0]), end(e.at[1]), q(e.q), n(0) {
     pairs = pc_pairs(a.geo, q);
   }
-  __device__ __forceinline__ bool same() const { return at.b == end.b && at.h == end.h && at.u == end.u; }
-  __device__ __forceinline__ bool more(const PcArgs& a) const {
-    return at.b < a.geo.B && (!same() || at.s < end.s);
-  }
-  __device__ __forceinline__ void next(const PcArgs& a) {
+  __device__ __forceinline__ void next(const PcArgs& a, PcItem& m) {
+    const bool last = at.b == end.b && at.h == end.h && at.u == end.u;
+    m.s1 = 0;
+    if (at.b >= a.geo.B || (last && at.s >= end.s)) return;
+    m.sp = pc_span(a.geo, q, at.u);
+    m.b = at.b;
+    m.h = at.h;
+    const int R = 2 * a.geo.tpt;
+    m.t0 = q.t0 + at.u * R;
+    m.toks = min(q.n - at.u * R, R);
+    m.s0 = at.s;
+    m.s1 = last ? end.s : m.sp.steps;
+    m.two = m.toks > a.geo.tpt;
+    m.duo = !m.two && m.s1 - m.s0 > 1;
+    m.whole = m.s0 == 0 && m.s1 == m.sp.steps;
+    m.place = 2 * blockIdx.x + (n++ ? 1 : 0);
     at.s = 0;
-    if (same()) at.s = end.s;  // (a piece that ends there)
-    else if (++at.u == pairs) {
+    if (last) {
+      at.s = end.s;
+    } else if (++at.u == pairs) {
       at.u = 0;
       if (++at.h == a.geo.KV) {
         at.h = 0;
         do {
           if (++at.b >= a.geo.B) return;
-          load(a);
+          q = pc_seq(a, at.b);
         } while (q.n == 0);
+        pairs = pc_pairs(a.geo, q);
       }
     }
-  }
-};
-
-// A piece of an item: its steps [s0, s1).
-struct PcItem {
-  PcSpan sp;
-  int h, t0, toks, s0, s1;
-  bool two, whole;  // with a tile B; all of its steps
-  __device__ __forceinline__ PcItem(const PcArgs& a, const PcWalk& w) {
-    sp = pc_span(a.geo, w.q, w.at.u);
-    h = w.at.h;
-    const int R = 2 * a.geo.tpt;
-    t0 = w.q.t0 + w.at.u * R;
-    toks = min(w.q.n - w.at.u * R, R);
-    two = toks > a.geo.tpt;
-    s0 = w.at.s;
-    s1 = w.same() ? w.end.s : sp.steps;
-    whole = s0 == 0 && s1 == sp.steps;
   }
 };
 
@@ -231,6 +242,7 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
     return;
   constexpr int C = DH / 32;  // columns of a lane
   const bf16* q = a.q + t * a.ldq + (long)hq * DH;
+  const float sl2 = a.sl2 / PcCfg<DH, Q8>::SCALE;
   float acc[C] = {}, m = -INFINITY, l = 0.f;
 #pragma unroll 1
   for (int part = 0; part < 2; ++part) {  // the sinks before the window, the window
@@ -255,10 +267,10 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
       float mx = s;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-      const float next = fmaxf(m, mx * a.sl2), ref = next == -INFINITY ? 0.f : next;
+      const float next = fmaxf(m, mx * sl2), ref = next == -INFINITY ? 0.f : next;
       const float corr = m == -INFINITY ? 1.f : ex2_approx(m - ref);
       m = next;
-      const float p = in ? ex2_approx(fmaf(s, a.sl2, -ref)) : 0.f;
+      const float p = in ? ex2_approx(fmaf(s, sl2, -ref)) : 0.f;
       float sum = p;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -288,91 +300,162 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
     *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(acc[c] / l, acc[c + 1] / l);
 }
 
-// The CTA's part of the line, ends[0] to ends[1], and its share in the pieces' index.  pre: room
-// for B + 1 totals.  Whole CTAs call it.
+// Weight and items of a sequence; any_bad becomes 1 if it cannot be.
+struct PcLoad {
+  PcSeq q;
+  long long weight;
+  int items;
+  __device__ __forceinline__ PcLoad(const PcArgs& a, int b, int* any_bad) {
+    bool bad;
+    q = pc_seq(a, b, &bad);
+    if (bad) {
+      set_dev_error(DEVERR_CAPACITY);
+      *any_bad = 1;
+      q.n = 0;
+    }
+    const int P = pc_pairs(a.geo, q);
+    weight = q.n > 0 ? a.geo.KV * pc_cum(a.geo, q, P) : 0;
+    items = P * a.geo.KV;
+  }
+};
+
+__device__ __forceinline__ long long warp_scan(long long v) {  // sums up to and with the lane
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long t = __shfl_up_sync(0xffffffffu, v, o);
+    if ((int)(threadIdx.x & 31) >= o) v += t;
+  }
+  return v;
+}
+
+// The CTA's part of the line, and its entry in the pieces' index.  room: for B + 1 totals and B
+// sequences.  (Each CTA works it out for itself: a kernel before this one would cost a launch.)
+// pc_totals: more than PC_FEW sequences, by all of a CTA's threads.  pc_share_out: warp 0 the CTA's
+// beginning, warp 1 the next one's.  Both are on the way to a call's first load, where every
+// instruction comes from L2, to all SMs at once: 12000 cycles in their first form, by one thread.
+struct PcRoom {
+  long long* pre;  // pre[b]: weight of the sequences before b
+  PcSeq* seq;
+  __device__ __forceinline__ PcRoom(void* room, int B)
+      : pre(static_cast<long long*>(room)), seq(reinterpret_cast<PcSeq*>(pre + B + 1)) {}
+};
+constexpr int PC_FEW = 128;
+static_assert((PC_FEW + 1) * 8 + PC_FEW * 12 <= 4096, "a room for each");
 template <int THREADS>
-__device__ __forceinline__ void pc_share_out(const PcArgs& a, long long* pre, PcAt* ends) {
-  __shared__ long long wsum[THREADS / 32], total;
-  __shared__ unsigned long long items;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) items = 0;
-  __syncthreads();
-  long long base = 0;
-  for (int b0 = 0; b0 < a.geo.B; b0 += THREADS) {
+__device__ __noinline__ void pc_totals(const PcArgs& a, void* room, long long* items, int* any_bad) {
+  __shared__ long long wsum[THREADS / 32];
+  __shared__ int wit[THREADS / 32];
+  const PcRoom m(room, a.geo.B);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = a.geo.B;
+  long long T = 0, n = 0;
+  for (int b0 = 0; b0 < B; b0 += THREADS) {
     const int b = b0 + tid;
     long long u = 0;
-    if (b < a.geo.B) {
-      bool bad;
-      PcSeq q = pc_seq(a, b, &bad);
-      if (bad) {
-        set_dev_error(DEVERR_CAPACITY);
-      } else if (q.n > 0) {
-        const int P = pc_pairs(a.geo, q);
-        u = a.geo.KV * pc_cum(a.geo, q, P);
-        atomicAdd(&items, (unsigned long long)P * a.geo.KV);
-      }
+    int it = 0;
+    if (b < B) {
+      const PcLoad x(a, b, any_bad);
+      m.seq[b] = x.q;
+      u = x.weight;
+      it = x.items;
     }
-    long long v = u;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long t = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += t;
+    const long long v = warp_scan(u);
+    it = __reduce_add_sync(0xffffffffu, it);
+    if (lane == 31) {
+      wsum[warp] = v;
+      wit[warp] = it;
     }
-    if (lane == 31) wsum[warp] = v;
     __syncthreads();
     long long before = 0, all = 0;
+#pragma unroll 1
     for (int w = 0; w < THREADS / 32; ++w) {
       if (w < warp) before += wsum[w];
       all += wsum[w];
+      n += wit[w];
     }
-    if (b < a.geo.B) pre[b] = base + before + v - u;
-    base += all;
+    if (b < B) m.pre[b] = T + before + v - u;
+    T += all;
     __syncthreads();
   }
   if (tid == 0) {
-    pre[a.geo.B] = base;
-    total = base;
+    m.pre[B] = T;
+    *items = n;
   }
   __syncthreads();
-  if (warp < 2 && lane == 0) {
-    const long long T = total;
-    const bool whole = a.whole == 0 || items >= (unsigned long long)a.whole * a.G;
-    const int n = whole ? a.G : (int)max(1ll, min((long long)a.G, T / a.few));
-    const int c = min((int)blockIdx.x + warp, n);
-    PcAt r{a.geo.B, 0, 0, 0};
-    const long long x = pc_share(T, n, c);
-    if (x < T) {
-      int b = 0, hi = a.geo.B;
-      while (hi - b > 1) {
-        const int m = (b + hi) >> 1;
-        if (pre[m] <= x) b = m; else hi = m;
-      }
-      // (the last of those that begin at x: it has tokens)
-      const PcSeq q = pc_seq(a, b);
-      const int P = pc_pairs(a.geo, q);
-      const long long per = pc_cum(a.geo, q, P), y = x - pre[b];
-      r.b = b;
-      r.h = (int)(y / per);
-      pc_find(a.geo, q, y % per, whole, &r.u, &r.s);
-      if (r.s >= pc_span(a.geo, q, r.u).steps) {  // the next item's beginning
-        r.s = 0;
-        if (++r.u == P) {
-          r.u = 0;
-          if (++r.h == a.geo.KV) {
-            r.h = 0;
-            do ++r.b;
-            while (r.b < a.geo.B && pre[r.b + 1] == pre[r.b]);
-          }
+}
+
+__device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, long long items, int warp, PcEnds& ends,
+                                             int* any_bad) {
+  // (few sequences: each of the two warps in a room of its own)
+  const PcRoom m(static_cast<char*>(room) + (a.geo.B <= PC_FEW ? warp * 4096 : 0), a.geo.B);
+  const int lane = threadIdx.x & 31, B = a.geo.B;
+  // the last of [0, hi) that does not begin behind the place, with all lanes
+  auto find = [&](int hi, auto before) {
+    int lo = 0;
+#pragma unroll 1
+    while (hi - lo > 1) {
+      const int d = (unsigned)(hi - lo + 31) / 32, i = lo + (lane + 1) * d;
+      const int k = __popc(__ballot_sync(0xffffffffu, i < hi && before(i)));
+      hi = min(hi, lo + (k + 1) * d);
+      lo += k * d;
+    }
+    return lo;
+  };
+  if (B <= PC_FEW) {
+    const int per = (B + 31) / 32;
+    long long u = 0;
+    int it = 0;
+#pragma unroll 1
+    for (int i = 0; i < per; ++i) {
+      const int b = lane * per + i;
+      if (b >= B) break;
+      const PcLoad x(a, b, any_bad);
+      m.seq[b] = x.q;
+      m.pre[b] = u;
+      u += x.weight;
+      it += x.items;
+    }
+    const long long v = warp_scan(u) - u;
+#pragma unroll 1
+    for (int b = lane * per; b < min(B, (lane + 1) * per); ++b) m.pre[b] += v;
+    if (lane == 31) m.pre[B] = v + u;
+    items = __reduce_add_sync(0xffffffffu, it);
+    __syncwarp();
+  }
+  PcSeq q{0, 0, 0};
+  const long long T = m.pre[B];
+  const bool whole = a.whole == 0 || items >= (long long)a.whole * a.G;
+  int n = a.G;
+  if (!whole && T < (long long)a.few * n) n = max(1, (int)T / a.few);
+  const int c = min((int)blockIdx.x + warp, n);
+  PcAt r{B, 0, 0, 0};
+  long long y = pc_share(T, n, c);
+  if (y < T) {
+    r.b = find(B, [&](int i) { return m.pre[i] <= y; });  // (the last of those that begin there: it has tokens)
+    y -= m.pre[r.b];
+    q = m.seq[r.b];
+    const int P = pc_pairs(a.geo, q);
+    r.h = pc_head(pc_cum(a.geo, q, P), y);
+    r.u = find(P, [&](int i) { return pc_cum(a.geo, q, i) <= y; });
+    r.s = pc_step(a.geo, q, r.u, y, whole);
+    if (r.s >= pc_span(a.geo, q, r.u).steps) {  // the next item's beginning
+      r.s = 0;
+      if (++r.u == P) {
+        r.u = 0;
+        if (++r.h == a.geo.KV) {
+          r.h = 0;
+          do q = ++r.b < B ? pc_seq(a, r.b) : PcSeq{0, 0, 0};
+          while (r.b < B && q.n == 0);
         }
       }
     }
-    ends[warp] = r;
-    if (a.at && (warp == 0 || c == a.G)) a.at[c] = r;
-    // (n < G: the CTAs from n on write the line's end, each its own)
-    if (a.at && warp == 0 && (int)blockIdx.x > n) a.at[blockIdx.x] = r;
+  }
+  if (lane == 0) {
+    ends.at[warp] = r;
+    if (warp == 0) ends.q = q;
+    // (CTAs without a part write the line's end, each its own place)
+    if (a.at && warp == 0) a.at[blockIdx.x] = r;
     if (a.at && warp == 1 && (int)blockIdx.x + 1 == a.G) a.at[a.G] = r;
   }
-  __syncthreads();
 }
 
 template <int DH, bool Q8>
@@ -381,17 +464,25 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
                        const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PcArgs a) {
   using C = PcCfg<DH, Q8>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ PcAt ends[2];
+  __shared__ PcEnds ends;
+  __shared__ PcItem slot[2];
+  __shared__ long long items;
+  __shared__ int any_bad;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   const uint32_t sbase = smem_u32(smem), b0 = sbase + C::OFF_BAR;
-  const uint32_t q_full = b0, q_empty = b0 + 8, done = b0 + 16, grp0 = b0 + 24, ring0 = grp0 + 2 * 48;
-  auto s_full = [&](int w) { return grp0 + 48 * w; };
-  auto s_free = [&](int w) { return grp0 + 48 * w + 8; };
-  auto p_full = [&](int w) { return grp0 + 48 * w + 16; };
-  auto p_free = [&](int w) { return grp0 + 48 * w + 24; };
-  auto o_full = [&](int w) { return grp0 + 48 * w + 32; };
-  auto o_free = [&](int w) { return grp0 + 48 * w + 40; };
+  const uint32_t done = b0, x_full = b0 + 8, x_free = b0 + 16, shared = b0 + 24, grp0 = b0 + 96, ring0 = grp0 + 2 * 56;
+  auto q_full = [&](int i) { return b0 + 32 + 8 * i; };
+  auto q_empty = [&](int i) { return b0 + 48 + 8 * i; };
+  auto i_full = [&](int i) { return b0 + 64 + 8 * i; };
+  auto i_empty = [&](int i) { return b0 + 80 + 8 * i; };
+  auto s_full = [&](int w) { return grp0 + 56 * w; };
+  auto s_free = [&](int w) { return grp0 + 56 * w + 8; };
+  auto p_full = [&](int w) { return grp0 + 56 * w + 16; };
+  auto p_free = [&](int w) { return grp0 + 56 * w + 24; };
+  auto o_full = [&](int w) { return grp0 + 56 * w + 32; };
+  auto o_free = [&](int w) { return grp0 + 56 * w + 40; };
+  auto p_half = [&](int w) { return grp0 + 56 * w + 48; };
   auto k_full = [&](int i) { return ring0 + 8 * i; };
   auto k_empty = [&](int i) { return ring0 + 8 * (C::NK + i); };
   auto v_full = [&](int i) { return ring0 + 8 * (2 * C::NK + i); };
@@ -402,28 +493,35 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    mbar_init(q_full, 1);
-    mbar_init(q_empty, 8);  // one arrival per softmax warp
+    any_bad = 0;
     mbar_init(done, 3);
+    mbar_init(x_full, 4);
+    mbar_init(x_free, 4);
+    mbar_init(shared, 2);
     for (int i = 0; i < 2; ++i) {
+      mbar_init(q_full(i), 1);
+      mbar_init(q_empty(i), 8);  // one arrival per softmax warp
+      mbar_init(i_full(i), 1);
+      mbar_init(i_empty(i), C::THREADS / 32 - 1);  // every warp but the producer's
       mbar_init(s_full(i), 1);
       mbar_init(s_free(i), 4);
       mbar_init(p_full(i), 4);
+      mbar_init(p_half(i), 4);
       mbar_init(p_free(i), 1);
       mbar_init(o_full(i), 1);
       mbar_init(o_free(i), 4);
     }
     for (int i = 0; i < C::NK; ++i) {
-      mbar_init(k_full(i), Q8 ? 4 : 1);  // (converting warps)
+      mbar_init(k_full(i), Q8 ? C::CONV : 1);  // (converting warps)
       mbar_init(k_empty(i), 1);
     }
     for (int i = 0; i < C::NV; ++i) {
-      mbar_init(v_full(i), Q8 ? 4 : 1);
+      mbar_init(v_full(i), Q8 ? C::CONV : 1);
       mbar_init(v_empty(i), 2);  // one arrival per tile
     }
     for (int i = 0; i < C::NR; ++i) {
       mbar_init(r_full(i), 1);
-      mbar_init(r_empty(i), 4);
+      mbar_init(r_empty(i), C::CONV);
     }
     fence_barrier_init();
   }
@@ -436,65 +534,85 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_enter();  // the setup above overlaps the kernel before this one
-  pc_share_out<C::THREADS>(a, reinterpret_cast<long long*>(smem + C::OFF_K), ends);
-  // rows of sequences whose length cannot be
-  for (int b = blockIdx.x; b < a.geo.B; b += gridDim.x) {
-    bool bad;
-    const PcSeq q = pc_seq(a, b, &bad);
-    const int per = a.geo.KV * a.geo.g * (DH / 8);
-    if (bad)
-      for (long i = threadIdx.x; i < (long)q.n * per; i += C::THREADS)
-        *reinterpret_cast<uint4*>(a.out + (q.t0 + i / per) * a.ldo + i % per * 8) = make_uint4(0, 0, 0, 0);
-  }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the totals lay where the rings are
-  __syncthreads();
+  // the join's launch may begin: it waits for this grid to end, and all of its CTAs are running
+  if (a.at) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  void* const room = smem + C::OFF_K;
+  if (a.geo.B > PC_FEW) pc_totals<C::THREADS>(a, room, &items, &any_bad);
   uint32_t k_issued = 0, v_issued = 0, r_issued = 0, q_issued = 0;
+  // Warp 0 walks the items and writes them down, two ahead at most, for the other warps.
+  // item n: bounded, false where it does not come; a copy of it is kept, its place is free again
+  auto take = [&](uint32_t n, PcItem& m) {
+    const uint32_t i = n & 1;
+    if (!wait_warp(i_full(i), (n >> 1) & 1)) return false;
+    m = slot[i];
+    mbar_arrive_warp(i_empty(i));
+    return m.s1 > 0;
+  };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_CTRL));
+    if (warp < 2) {
+      pc_share_out(a, room, items, warp, ends, &any_bad);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the totals lie where the rings will be
+      mbar_arrive_warp(shared);
+    }
     if (warp == 0) {
       // ------------------------------------------------------------ producer (all lanes)
-      if (lane == 0) {
-        prefetch_tmap(&tmQ);
-        prefetch_tmap(&tmK);
-        prefetch_tmap(&tmV);
-      }
-      const int nb = PC_T / a.box, H = Q8 ? 1 : C::HALVES;
+      const int nb = PC_T >> a.box_log, H = Q8 ? 1 : C::HALVES;
       // lane: block of rows and half of their columns, or (Q8) the blocks' exponents
-      const int blk = lane / H % nb, half = lane % H;
+      const int blk = lane / H & (nb - 1), half = lane % H;
       const bool data = lane < nb * H, exps = Q8 && lane >= nb && lane < 2 * nb;
       const uint32_t qbytes = (uint32_t)(a.geo.tpt * a.geo.g * 128 * C::HALVES);
-      bool ok = true;
-      for (PcWalk w(a, ends); w.more(a) && ok; w.next(a)) {
-        const PcItem m(a, w);
+      bool ok = wait_warp(shared, 0);
+      PcWalk walk(a, ends);
+      while (ok) {
+        PcItem m;
+        walk.next(a, m);
+        {
+          const uint32_t i = q_issued & 1;  // (items so far)
+          if (!wait_warp(i_empty(i), ((q_issued >> 1) & 1) ^ 1)) break;
+          if (lane == 0) slot[i] = m;
+          mbar_arrive_warp(i_full(i));
+        }
+        if (m.s1 == 0) break;
         auto page_of = [&](int s) -> int {  // the pool's page of the lane's block in step s
           if (s >= m.s1 || !(data || exps)) return 0;
           const int r = m.sp.tile(s) * PC_T + blk * a.box;
           const bool seen = r <= m.sp.pl && (a.geo.W == 0 || r + a.box - 1 > m.sp.pf - a.geo.W || r < a.geo.S);
-          const long pg = seen ? pc_page(a, w.at.b, r) : -1;
+          const long pg = seen ? pc_page(a, m.b, r) : -1;
           return (int)(pg < 0 ? a.n_pages : pg);  // (past the end: zeros)
         };
-        if (!wait_warp(q_empty, (q_issued & 1) ^ 1)) break;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(q_full, m.two ? 2 * qbytes : qbytes);
-          for (int t = 0; t < (m.two ? 2 : 1); ++t)
-            for (int c = 0; c < C::HALVES; ++c)
-              tma_load_3d(sbase + t * C::TILE + c * C::HALF, &tmQ, q_full, 64 * c, m.h * a.geo.g,
-                          m.t0 + t * a.geo.tpt);
-        }
-        __syncwarp();
-        ++q_issued;
         int pg_next = page_of(m.s0);
+        // the item's queries, as soon as those before them are done with and before a step's place is waited
+        // for that only this item's steps free
+        bool queries = false;
+#pragma unroll 1
         for (int s = m.s0; s < m.s1; ++s) {
+          const uint32_t qb = q_issued % C::NQ, par = ((q_issued / C::NQ) & 1) ^ 1;
+          const bool must = s - m.s0 == C::AHEAD - 1 || s == m.s1 - 1;
+          if (!queries && (must || __all_sync(0xffffffffu, mbar_test_wait(q_empty(qb), par)))) {
+            ok = wait_warp(q_empty(qb), par);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_expect_tx(q_full(qb), m.two ? 2 * qbytes : qbytes);
+            __syncwarp();
+            if (lane < C::HALVES * (m.two ? 2 : 1)) {
+              const int t = lane / C::HALVES, c = lane % C::HALVES;
+              tma_load_3d(sbase + (2 * qb + t) * C::TILE + c * C::HALF, &tmQ, q_full(qb), 64 * c, m.h * a.geo.g,
+                          m.t0 + t * a.geo.tpt);
+            }
+            __syncwarp();
+            queries = true;
+          }
           const int pg = pg_next, row = (m.sp.tile(s) * PC_T + blk * a.box) % a.page;
           pg_next = page_of(s + 1);
-          if (Q8) {
-            for (int kv = 0; kv < 2; ++kv) {
-              const uint32_t st = r_issued % (C::NR ? C::NR : 1);
-              if (!wait_warp(r_empty(st), ((r_issued / (C::NR ? C::NR : 1)) & 1) ^ 1)) {
-                ok = false;
-                break;
-              }
+#pragma unroll 1
+          for (int kv = 0; kv < 2 && ok; ++kv) {
+            const CUtensorMap* const map = kv ? &tmV : &tmK;
+            if (Q8) {
+              constexpr int N = C::NR ? C::NR / 2 : 1;
+              const uint32_t n = r_issued / 2, st = kv * N + n % N;
+              ok = wait_warp(r_empty(st), ((n / N) & 1) ^ 1);
+              if (!ok) break;
               // (exponents of blocks that no token sees, and of pages out of range: zeros)
               const bool in = exps && pg < a.n_pages;
               const uint32_t edst = sbase + C::OFF_EXP + st * PC_T + blk * a.box;
@@ -505,72 +623,64 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
               if (lane == 0) mbar_arrive_expect_tx(r_full(st), C::RAW + ebytes);
               __syncwarp();
               if (data)
-                tma_load_4d(sbase + C::OFF_RAW + st * C::RAW + blk * a.box * DH, kv ? &tmV : &tmK, r_full(st), 0, row,
-                            m.h, pg);
+                tma_load_4d(sbase + C::OFF_RAW + st * C::RAW + blk * a.box * DH, map, r_full(st), 0, row, m.h, pg);
               else if (in)
                 bulk_load(edst, (kv ? a.Ve : a.Ke) + ((long)pg * a.geo.KV + m.h) * a.page + row, a.box, r_full(st));
               __syncwarp();
               ++r_issued;
+            } else {
+              uint32_t& n = kv ? v_issued : k_issued;
+              const uint32_t ring = kv ? C::NV : C::NK, st = n % ring, full = kv ? v_full(st) : k_full(st);
+              ok = wait_warp(kv ? v_empty(st) : k_empty(st), ((n / ring) & 1) ^ 1);
+              if (!ok) break;
+              if (lane == 0) mbar_arrive_expect_tx(full, C::TILE);
+              __syncwarp();
+              if (data)
+                tma_load_4d(sbase + (kv ? C::OFF_V : C::OFF_K) + st * C::TILE + half * C::HALF + blk * a.box * 128, map,
+                            full, 64 * half, row, m.h, pg);
+              __syncwarp();
+              ++n;
             }
-            if (!ok) break;
-          } else {
-            const uint32_t sk = k_issued % C::NK, sv = v_issued % C::NV;
-            const uint32_t off = half * C::HALF + blk * a.box * 128;
-            if (!wait_warp(k_empty(sk), ((k_issued / C::NK) & 1) ^ 1)) {
-              ok = false;
-              break;
-            }
-            if (lane == 0) mbar_arrive_expect_tx(k_full(sk), C::TILE);
-            __syncwarp();
-            if (data) tma_load_4d(sbase + C::OFF_K + sk * C::TILE + off, &tmK, k_full(sk), 64 * half, row, m.h, pg);
-            __syncwarp();
-            ++k_issued;
-            if (!wait_warp(v_empty(sv), ((v_issued / C::NV) & 1) ^ 1)) {
-              ok = false;
-              break;
-            }
-            if (lane == 0) mbar_arrive_expect_tx(v_full(sv), C::TILE);
-            __syncwarp();
-            if (data) tma_load_4d(sbase + C::OFF_V + sv * C::TILE + off, &tmV, v_full(sv), 64 * half, row, m.h, pg);
-            __syncwarp();
-            ++v_issued;
           }
+          if (!ok) break;
         }
+        if (queries) ++q_issued;
       }
     } else if (warp == 1) {
       // ------------------------------------------------------------ MMA issuer: scores
       // The whole warp runs the loop; one elected lane issues and commits.
       constexpr uint32_t idesc = idesc_bf16_f32(PC_T, PC_T, 0, 0);
       const uint64_t dq0 = smem_desc_sw128(sbase, 16, 1024), dk0 = smem_desc_sw128(sbase + C::OFF_K, 16, 1024);
-      uint32_t G = 0, gs[2] = {0, 0}, it = 0;  // steps, products of the tiles, items so far
-      for (PcWalk wk(a, ends); wk.more(a); wk.next(a), ++it) {
-        const PcItem m(a, wk);
-        if (!wait_warp(q_full, it & 1)) break;
+      uint32_t G = 0, g0 = 0, g1 = 0;  // steps, products of the tiles so far
+      PcItem m;
+      for (uint32_t it = 0; take(it, m); ++it) {
+        const uint32_t qb = it % C::NQ;
+        if (!wait_warp(q_full(qb), (it / C::NQ) & 1)) break;
         int s = m.s0;
+#pragma unroll 1
         for (; s < m.s1; ++s, ++G) {
           const uint32_t st = G % C::NK;
           if (!wait_warp(k_full(st), (G / C::NK) & 1)) break;
           bool ok = true;
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
-            if (!ok || (w == 1 && !m.two)) continue;
+            if (!ok || (m.duo ? ((s - m.s0) & 1) != w : w > m.two)) continue;
             // S's place: read into registers, or (ALIAS) P in it taken up by its product
-            if (gs[w] > 0 && !wait_warp(C::ALIAS ? p_free(w) : s_free(w), (gs[w] - 1) & 1)) {
-              ok = false;
-              continue;
-            }
+            uint32_t& gs = w ? g1 : g0;
+            ok = gs == 0 || wait_warp(C::ALIAS ? p_free(w) : s_free(w), (gs - 1) & 1);
+            if (!ok) continue;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
               for (int kk = 0; kk < DH / 16; ++kk) {
                 const uint64_t o = (uint64_t)(kk / 4) * (C::HALF >> 4) + kk % 4 * 2;
-                tc_mma_f16(tmem + 128 * w, dq0 + w * (C::TILE >> 4) + o, dk0 + st * (C::TILE >> 4) + o, idesc,
-                           kk ? 1u : 0u);
+                tc_mma_f16(tmem + 128 * w, dq0 + (2 * qb + (m.two ? w : 0)) * (C::TILE >> 4) + o, dk0 + st * (C::TILE >> 4) + o,
+                           idesc, kk ? 1u : 0u);
               }
               tc_commit(s_full(w));
             }
             __syncwarp();
-            ++gs[w];
+            ++gs;
           }
           if (!ok) break;
           if (elect_one()) tc_commit(k_empty(st));
@@ -587,31 +697,46 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
       const uint32_t tO = tmem + C::tm_o(w), tP = tmem + C::tm_p(w);
       const uint64_t dv0 = smem_desc_sw128(sbase + C::OFF_V, C::HALF, 1024);
       uint32_t G = 0, gp = 0, io = 0;  // steps, products, items so far
-      for (PcWalk wk(a, ends); wk.more(a); wk.next(a)) {
-        const PcItem m(a, wk);
-        const bool mine = w == 0 || m.two;
+      PcItem m;
+      for (uint32_t it = 0; take(it, m); ++it) {
+        const bool mine = w == 0 || m.two || m.duo;
+        // (its first and last step)
+        const int first = m.duo ? m.s0 + w : m.s0, last = m.duo && ((m.s1 - 1 - first) & 1) ? m.s1 - 2 : m.s1 - 1;
         int s = m.s0;
+#pragma unroll 1
         for (; s < m.s1; ++s, ++G) {
           const uint32_t st = G % C::NV;
           if (!wait_warp(v_full(st), (G / C::NV) & 1)) break;
-          if (!mine) {  // (after the wait: else it could pass the ring's round)
+          if (!mine || (m.duo && ((s - first) & 1))) {  // (after the wait: else it could pass the ring's round)
             if (elect_one()) mbar_arrive(v_empty(st));
             __syncwarp();
             continue;
           }
-          if (!wait_warp(p_full(w), gp & 1)) break;
-          if (s == m.s0 && io > 0 && !wait_warp(o_free(w), (io - 1) & 1)) break;
-          tc_fence_after();
-          if (elect_one()) {
+          if (s == first && io > 0 && !wait_warp(o_free(w), (io - 1) & 1)) break;
+          constexpr int PARTS = C::ALIAS ? 2 : 1;  // (the first half of the keys while the second half's P is made)
+          bool ok = true;
 #pragma unroll
-            for (int kk = 0; kk < PC_T / 16; ++kk)
-              tc_mma_f16_ts(tO, tP + kk * 8, dv0 + st * (C::TILE >> 4) + kk * (2048 >> 4), idesc,
-                            (s > m.s0 || kk > 0) ? 1u : 0u);
-            tc_commit(p_free(w));
-            tc_commit(v_empty(st));
-            if (s == m.s1 - 1) tc_commit(o_full(w));
+          for (int part = 0; part < PARTS; ++part) {
+            const bool end = part == PARTS - 1;
+            ok = ok && wait_warp(end ? p_full(w) : p_half(w), gp & 1);
+            if (!ok) continue;
+            tc_fence_after();
+            if (elect_one()) {
+              constexpr int N = PC_T / 16 / PARTS;
+              const uint32_t p = tP + part * (N * 8);
+              const uint64_t v = dv0 + st * (C::TILE >> 4) + part * (N * (2048 >> 4));
+#pragma unroll
+              for (int kk = 0; kk < N; ++kk)
+                tc_mma_f16_ts(tO, p + kk * 8, v + kk * (2048 >> 4), idesc, (s > first || part > 0 || kk > 0) ? 1u : 0u);
+              if (end) {
+                tc_commit(p_free(w));
+                tc_commit(v_empty(st));
+                if (s == last) tc_commit(o_full(w));
+              }
+            }
+            __syncwarp();
           }
-          __syncwarp();
+          if (!ok) break;
           ++gp;
         }
         if (s < m.s1) break;  // a wait ran out
@@ -631,25 +756,66 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
     const uint32_t ts = tl + 128 * w, to = tl + C::tm_o(w), tp = tl + C::tm_p(w);
     const float2 sl = make_float2(a.sl2, a.sl2);
     bool ok = true, late = false;  // late: a row was not finite
-    uint32_t g = 0, io = 0, it = 0;
-    for (PcWalk wk(a, ends); wk.more(a); wk.next(a), ++it) {
-      const PcItem m(a, wk);
-      if (w == 1 && !m.two) {
-        if (!wait_warp(q_full, it & 1)) break;  // (else it could pass the other warps by a round)
-        mbar_arrive_warp(q_empty);
+    uint32_t g = 0, io = 0, ix = 0;
+    PcItem m;
+    for (uint32_t it = 0; take(it, m); ++it) {
+      if (w == 1 && !m.two && !m.duo) {
+        // (else it could pass the other warps by a round)
+        if (!wait_warp(q_full(it % C::NQ), (it / C::NQ) & 1)) break;
+        mbar_arrive_warp(q_empty(it % C::NQ));
         continue;
       }
-      const int pos = m.sp.pf + w * a.geo.tpt + tok;  // row of the token in its sequence
+      const int mate = m.two ? w * a.geo.tpt : 0;  // the tile's first token in the item
+      const int pos = m.sp.pf + mate + tok;        // row of the token in its sequence
       // tiles with keys hidden from some row of this tile: past the first one's diagonal, or
       // before the last one's window
-      const int diag = m.sp.pf + w * a.geo.tpt;
+      const int diag = m.sp.pf + mate;
       const int edge = a.geo.W > 0 ? diag + a.geo.tpt - a.geo.W : -0x7fffffff;
       float mref = -INFINITY, l = 0.f;
-      auto step = [&](auto masked, int kt) -> bool {
-        constexpr bool MASKED = decltype(masked)::value;
+      // a warp without a row of the item's hands its steps on as they are: its rows of P and O go nowhere
+      const int toks = m.two && w ? m.toks - a.geo.tpt : min(m.toks, a.geo.tpt);
+      const bool idle = q4 * 32 >= toks * a.geo.g;
+      // The maximum mt of a step's scores (log2 units) against the reference: the first keys set it,
+      // later ones raise it only by more than PC_RESCALE, scaling O and the running sum.
+      auto raise = [&](float mt) -> bool {
+        if (!__any_sync(0xffffffffu, mt > mref + PC_RESCALE)) return true;
+        float corr = 1.f;
+        if (mt > mref + PC_RESCALE) {
+          if (mref != -INFINITY) corr = ex2_approx(mref - mt);
+          mref = mt;
+        }
+        if (__any_sync(0xffffffffu, corr != 1.f)) {  // this warp's rows of O
+          if (!wait_warp(p_free(w), (g - 1) & 1)) return false;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < DH; c += 16) {
+            uint32_t ov[16];
+            tmem_ld16(to + c, ov);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+            tmem_st16(to + c, ov);
+          }
+          l *= corr;
+        }
+        return true;
+      };
+      // P = 2^(s * sl2 - m) of 32 keys as bf16 pairs (key 2c, 2c + 1 in column c), and their sums, with
+      // packed fp32x2 arithmetic
+      auto probabilities = [&](const uint32_t* sc, float2 nm, float2* ps, uint32_t* pk) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          const float2 z =
+              __ffma2_rn(make_float2(__uint_as_float(sc[2 * c]), __uint_as_float(sc[2 * c + 1])), sl, nm);
+          const float2 pp = make_float2(ex2_approx(z.x), ex2_approx(z.y));
+          ps[c & 1] = __fadd2_rn(ps[c & 1], pp);
+          pk[c] = pack_bf16(pp.x, pp.y);
+        }
+      };
+      // a step whose keys every row sees: the scores in registers
+      auto step = [&]() -> bool {
         if (!wait_warp(s_full(w), g & 1)) return false;
         tc_fence_after();
-        // the scores into registers, the first half's maxima while the second comes
+        // the first half's maxima while the second half comes
         uint32_t sc[PC_T];
         float mx[8];
         auto maxima = [&](int c0) {
@@ -660,91 +826,46 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
               mx[e] = c == 0 ? fmaxf(__uint_as_float(sc[2 * e]), __uint_as_float(sc[2 * e + 1]))
                              : max3f(mx[e], __uint_as_float(sc[c + 2 * e]), __uint_as_float(sc[c + 2 * e + 1]));
         };
-        if (!MASKED) {
-          tmem_ld32_async(ts, sc);
-          tmem_ld32_async(ts + 32, sc + 32);
-          tmem_wait_ld(sc);
-          tmem_wait_ld(sc + 32);
-          tmem_ld32_async(ts + 64, sc + 64);
-          tmem_ld32_async(ts + 96, sc + 96);
-          maxima(0);
+        tmem_ld32_async(ts, sc);
+        tmem_ld32_async(ts + 32, sc + 32);
+        tmem_wait_ld(sc);
+        tmem_wait_ld(sc + 32);
+        tmem_ld32_async(ts + 64, sc + 64);
+        tmem_ld32_async(ts + 96, sc + 96);
+        maxima(0);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) asm volatile("" : "+f"(mx[e]));
-          tmem_wait_ld(sc + 64);
-          tmem_wait_ld(sc + 96);
-        } else {
-#pragma unroll
-          for (int c = 0; c < PC_T; c += 32) tmem_ld32_async(ts + c, sc + c);
-#pragma unroll
-          for (int c = 0; c < PC_T; c += 32) tmem_wait_ld(sc + c);
-        }
+        for (int e = 0; e < 8; ++e) asm volatile("" : "+f"(mx[e]));
+        tmem_wait_ld(sc + 64);
+        tmem_wait_ld(sc + 96);
         if (!C::ALIAS) {  // the next scores may replace them
           tc_fence_before();
           mbar_arrive_warp(s_free(w));
         }
-        if (MASKED) {
-          // seen keys: (pos - W, pos], and the sinks; bit c of a word: its column c
-          auto low = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
-#pragma unroll
-          for (int c0 = 0; c0 < PC_T; c0 += 32) {
-            const int b0 = kt * PC_T + c0;
-            uint32_t vis = low(pos + 1 - b0);
-            if (a.geo.W > 0) vis &= ~low(pos - a.geo.W + 1 - b0) | low(a.geo.S - b0);
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-              if (!(vis >> c & 1)) sc[c0 + c] = 0xff800000u;  // -inf
-          }
-          maxima(0);
-        }
         maxima(PC_T / 2);
-        const float mt =
-            max3f(max3f(mx[0], mx[1], mx[2]), max3f(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * a.sl2;
-        // the first keys set the reference; later ones raise it only by more than
-        // PC_RESCALE, scaling O and the running sum
-        if (__any_sync(0xffffffffu, mt > mref + PC_RESCALE)) {
-          float corr = 1.f;
-          if (mt > mref + PC_RESCALE) {
-            if (mref != -INFINITY) corr = ex2_approx(mref - mt);
-            mref = mt;
-          }
-          if (__any_sync(0xffffffffu, corr != 1.f)) {  // this warp's rows of O
-            if (!wait_warp(p_free(w), (g - 1) & 1)) return false;
-            tc_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < DH; c += 16) {
-              uint32_t ov[16];
-              tmem_ld16(to + c, ov);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
-              tmem_st16(to + c, ov);
-            }
-            l *= corr;
-          }
-        }
-        // P = 2^(s * sl2 - m) as bf16 pairs (key 2c, 2c + 1 in column c) and the row
-        // sum, with packed fp32x2 arithmetic
+        if (!raise(max3f(max3f(mx[0], mx[1], mx[2]), max3f(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * a.sl2))
+          return false;
         const float ref = mref == -INFINITY ? 0.f : mref;
         const float2 nm = make_float2(-ref, -ref);
         float2 ps[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         uint32_t pk[PC_T / 2];
 #pragma unroll
         for (int hh = 0; hh < PC_T / 32; ++hh) {
-#pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const float2 z = __ffma2_rn(make_float2(__uint_as_float(sc[32 * hh + 2 * c]),
-                                                    __uint_as_float(sc[32 * hh + 2 * c + 1])),
-                                        sl, nm);
-            const float2 pp = make_float2(ex2_approx(z.x), ex2_approx(z.y));
-            ps[c & 1] = __fadd2_rn(ps[c & 1], pp);
-            pk[16 * hh + c] = pack_bf16(pp.x, pp.y);
-          }
-          if (hh == 2 && !C::ALIAS) {  // the last tile's P has been consumed (ALIAS: before its S came)
-            if (g > 0 && !wait_warp(p_free(w), (g - 1) & 1)) return false;
-            tc_fence_after();
-          }
-          if (hh >= 2)
+          probabilities(sc + 32 * hh, nm, ps, pk + 16 * hh);
+          if (C::ALIAS) {
+            tmem_st16(tp + 16 * hh, pk + 16 * hh);
+            if (hh == 1) {
+              tmem_wait_st();
+              tc_fence_before();
+              mbar_arrive_warp(p_half(w));
+            }
+          } else if (hh >= 2) {
+            if (hh == 2) {  // the last tile's P has been consumed (ALIAS: before its S came)
+              if (g > 0 && !wait_warp(p_free(w), (g - 1) & 1)) return false;
+              tc_fence_after();
+            }
 #pragma unroll
             for (int c = hh == 2 ? 0 : 16 * hh; c <= 16 * hh; c += 16) tmem_st16(tp + c, pk + c);
+          }
         }
         tmem_wait_st();
         tc_fence_before();
@@ -753,27 +874,176 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
         ++g;
         return true;
       };
+      // any step, 32 keys at a time, from TMEM twice: a quarter of the instructions, all of which a
+      // kernel's first steps wait for (they come from L2 at some 15 cycles each)
+      auto step_short = [&](int kt) -> bool {
+        if (!wait_warp(s_full(w), g & 1)) return false;
+        tc_fence_after();
+        const bool masked = kt * PC_T + PC_T - 1 > diag || kt * PC_T < edge;
+        uint32_t sc[32];
+        auto scores = [&](int c0) {
+          tmem_ld32_async(ts + c0, sc);
+          tmem_wait_ld(sc);
+          if (masked) {
+            // seen keys: (pos - W, pos], and the sinks; bit c of a word: its column c
+            auto low = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+            const int b0 = kt * PC_T + c0;
+            uint32_t vis = low(pos + 1 - b0);
+            if (a.geo.W > 0) vis &= ~low(pos - a.geo.W + 1 - b0) | low(a.geo.S - b0);
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              if (!(vis >> c & 1)) sc[c] = 0xff800000u;  // -inf
+          }
+        };
+        float mt = -INFINITY;
 #pragma unroll 1
-      for (int s = m.s0; ok && s < m.s1; ++s) {
+        for (int c0 = 0; c0 < PC_T; c0 += 32) {
+          scores(c0);
+          float mx[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            mx[e] = max3f(__uint_as_float(sc[8 * e]), __uint_as_float(sc[8 * e + 1]), __uint_as_float(sc[8 * e + 2]));
+#pragma unroll
+            for (int c = 3; c < 7; c += 2)
+              mx[e] = max3f(mx[e], __uint_as_float(sc[8 * e + c]), __uint_as_float(sc[8 * e + c + 1]));
+            mx[e] = fmaxf(mx[e], __uint_as_float(sc[8 * e + 7]));
+          }
+          mt = max3f(mt, max3f(mx[0], mx[1], mx[2]), mx[3]);
+        }
+        if (!raise(mt * a.sl2)) return false;
+        if (!C::ALIAS && g > 0 && !wait_warp(p_free(w), (g - 1) & 1)) return false;
+        tc_fence_after();
+        const float ref = mref == -INFINITY ? 0.f : mref;
+        const float2 nm = make_float2(-ref, -ref);
+        float2 ps[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+        for (int c0 = 0; c0 < PC_T; c0 += 32) {
+          scores(c0);
+          uint32_t pk[16];
+          probabilities(sc, nm, ps, pk);
+          tmem_st16(tp + c0 / 2, pk);
+          if (C::ALIAS && c0 == 32) {
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive_warp(p_half(w));
+          }
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        if (!C::ALIAS) mbar_arrive_warp(s_free(w));
+        mbar_arrive_warp(p_full(w));
+        l += (ps[0].x + ps[0].y) + (ps[1].x + ps[1].y);
+        ++g;
+        return true;
+      };
+      const int by = m.duo ? 2 : 1;
+#pragma unroll 1
+      for (int s = m.duo ? m.s0 + w : m.s0; ok && s < m.s1; s += by) {
+        if (idle) {
+          // (not ALIAS: the next scores may come before the last P has, which must be all four warps' first)
+          ok = wait_warp(s_full(w), g & 1) && (C::ALIAS || g == 0 || wait_warp(p_free(w), (g - 1) & 1));
+          if (!ok) break;
+          ++g;
+          mbar_arrive_warp(C::ALIAS ? p_half(w) : s_free(w));
+          mbar_arrive_warp(p_full(w));
+          continue;
+        }
         const int kt = m.sp.tile(s);
-        ok = kt * PC_T + PC_T - 1 > diag || kt * PC_T < edge ? step(std::true_type{}, kt) : step(std::false_type{}, kt);
+        if constexpr (Q8)
+          ok = step_short(kt);
+        else
+          ok = !m.two || m.s1 - m.s0 < a.long_item || kt * PC_T + PC_T - 1 > diag || kt * PC_T < edge ? step_short(kt) : step();
       }
       if (!ok) break;
       // the item's O: after its last P V
       if (!wait_warp(o_full(w), io & 1)) break;
       ++io;
       tc_fence_after();
-      const int toks = w ? m.toks - a.geo.tpt : min(m.toks, a.geo.tpt);
-      if (m.whole) {
-        // the warp's rows through the query tile's own, which no MMA reads any more, and out row by row
-        const float inv = 1.f / l;  // (a row sees itself: 0 where its scores are all -inf, and 0 / 0 is NaN)
-        float2 fin = make_float2(0.f, 0.f);  // zero, but for sums that are not finite
+      // shared steps: tile B's place hands its (maximum, sum) and its O, in two halves, to A's
+      // through the second query tile's memory, which such an item does not use
+      constexpr int XC = DH / 2;  // columns of a half: so many rows of 128 float4s
+      const uint32_t qb = it % C::NQ;
+      float4* const xch = reinterpret_cast<float4*>(smem + (2 * qb + 1) * C::TILE);
+      if (m.duo && w == 1) {
+        ok = wait_warp(x_free, (ix & 1) ^ 1);
+        if (!ok) break;
+        if (!idle) xch[r] = make_float4(mref, l, 0.f, 0.f);
+        mbar_arrive_warp(x_full);
+        ++ix;
+#pragma unroll 1
+        for (int c0 = 0; ok && c0 < DH; c0 += XC, ++ix) {
+          ok = wait_warp(x_free, (ix & 1) ^ 1);
+          if (!ok) break;
+#pragma unroll 1
+          for (int c = 0; c < XC && !idle; c += 32) {
+            uint32_t ov[32];
+            tmem_ld32_async(to + c0 + c, ov);
+            tmem_wait_ld(ov);
 #pragma unroll
-        for (int c = 0; c < DH; c += 32) {
-          uint32_t ov[32];
-          tmem_ld32_async(to + c, ov);
-          tmem_wait_ld(ov);
-          uint8_t* stg = smem + w * C::TILE + c / 64 * C::HALF + r * 128;
+            for (int i = 0; i < 32; i += 4)
+              xch[(c + i) / 4 * PC_T + r] = make_float4(__uint_as_float(ov[i]), __uint_as_float(ov[i + 1]),
+                                                        __uint_as_float(ov[i + 2]), __uint_as_float(ov[i + 3]));
+          }
+          mbar_arrive_warp(x_full);
+        }
+        if (!ok) break;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tc_fence_before();
+        mbar_arrive_warp(o_free(w));
+        mbar_arrive_warp(q_empty(qb));
+        continue;
+      }
+      float fa = 1.f, fb = 0.f;  // factors of A's own and of B's
+      if (m.duo) {
+        ok = wait_warp(x_full, ix & 1);
+        if (!ok) break;
+        const float4 y = xch[r];
+        mbar_arrive_warp(x_free);
+        ++ix;
+        const float M = fmaxf(mref, y.x);
+        fa = mref == M ? 1.f : ex2_approx(mref - M);
+        fb = y.x == M ? 1.f : ex2_approx(y.x - M);
+        l = fmaf(l, fa, y.y * fb);
+        mref = M;
+      }
+      const bool row_in = tok < toks;
+      const float inv = m.whole ? C::SCALE / l : 1.f;  // (a row sees itself: 0 where its scores are all -inf, and 0 / 0 is NaN)
+      const long place = m.place;
+      float4* const part = a.part + (place * (DH / 4)) * a.piece_rows + w * PC_T + r;
+      float2 fin = make_float2(0.f, 0.f);  // zero, but for sums that are not finite
+#pragma unroll 1
+      for (int c = 0; c < DH; c += 32) {
+        if (idle) {
+          if (m.duo && c % XC == 0) {
+            ok = wait_warp(x_full, ix & 1);
+            if (!ok) break;
+            mbar_arrive_warp(x_free);
+            ++ix;
+          }
+          continue;
+        }
+        uint32_t ov[32];
+        tmem_ld32_async(to + c, ov);
+        tmem_wait_ld(ov);
+        if (m.duo) {
+          if (c % XC == 0) ok = wait_warp(x_full, ix & 1);
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 y = xch[(c % XC + i) / 4 * PC_T + r];
+            ov[i] = __float_as_uint(fmaf(__uint_as_float(ov[i]), fa, y.x * fb));
+            ov[i + 1] = __float_as_uint(fmaf(__uint_as_float(ov[i + 1]), fa, y.y * fb));
+            ov[i + 2] = __float_as_uint(fmaf(__uint_as_float(ov[i + 2]), fa, y.z * fb));
+            ov[i + 3] = __float_as_uint(fmaf(__uint_as_float(ov[i + 3]), fa, y.w * fb));
+          }
+          if (c % XC == XC - 32) {
+            mbar_arrive_warp(x_free);
+            ++ix;
+          }
+        }
+        if (m.whole) {
+          // the warp's rows through the query tile's own, which no MMA reads any more
+          uint8_t* stg = smem + (2 * qb + w) * C::TILE + c / 64 * C::HALF + r * 128;
 #pragma unroll
           for (int i = 0; i < 32; i += 8) {
             uint32_t pk[4];
@@ -786,46 +1056,43 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
             }
             *reinterpret_cast<uint4*>(stg + ((((c % 64 + i) / 8) ^ (r & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
           }
+        } else if (row_in) {
+          // (four columns of a row, row by row: a lane to a row writes lines, not a piece of 32 of them)
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            part[(c + i) / 4 * a.piece_rows] = make_float4(__uint_as_float(ov[i]), __uint_as_float(ov[i + 1]),
+                                                           __uint_as_float(ov[i + 2]), __uint_as_float(ov[i + 3]));
         }
-        late |= fin.x + fin.y != 0.f && tok < toks;
-        tc_fence_before();
-        mbar_arrive_warp(o_free(w));
-        bf16* const row = tok < toks ? a.out + (long)(m.t0 + w * a.geo.tpt + tok) * a.ldo +
-                                           ((long)m.h * a.geo.g + r % a.geo.g) * DH
-                                     : nullptr;
+      }
+      if (!ok) break;
+      tc_fence_before();
+      mbar_arrive_warp(o_free(w));
+      if (m.whole && !idle) {
+        late |= fin.x + fin.y != 0.f && row_in;
+        bf16* const row = row_in ? a.out + (long)(m.t0 + w * a.geo.tpt + tok) * a.ldo +
+                                       ((long)m.h * a.geo.g + r % a.geo.g) * DH
+                                 : nullptr;
         constexpr int CH = DH / 8;  // 16-byte pieces of a row
 #pragma unroll 4
         for (int i = 0; i < CH; ++i) {
           const int e = i * 32 + lane, rr = e / CH, c = e % CH;
           bf16* const dst = reinterpret_cast<bf16*>(__shfl_sync(0xffffffffu, (unsigned long long)row, rr));
-          const uint4 u = *reinterpret_cast<const uint4*>(smem + w * C::TILE + c / 8 * C::HALF + (q4 * 32 + rr) * 128 +
+          const uint4 u = *reinterpret_cast<const uint4*>(smem + (2 * qb + w) * C::TILE + c / 8 * C::HALF + (q4 * 32 + rr) * 128 +
                                                           (((c % 8) ^ (rr & 7)) << 4));
           if (dst) *reinterpret_cast<uint4*>(dst + c * 8) = u;
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      } else {
-        const long slot = (2l * blockIdx.x + (wk.at.b == ends[0].b && wk.at.h == ends[0].h && wk.at.u == ends[0].u ? 0 : 1)) *
-                              a.piece_rows + w * PC_T + r;
-        if (tok < toks) a.ml[slot] = make_float2(mref, l);
-#pragma unroll 1
-        for (int c = 0; c < DH; c += 32) {
-          uint32_t ov[32];
-          tmem_ld32_async(to + c, ov);
-          tmem_wait_ld(ov);
-          if (tok < toks)
-#pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              *reinterpret_cast<uint4*>(a.part + slot * DH + c + i) = make_uint4(ov[i], ov[i + 1], ov[i + 2], ov[i + 3]);
-        }
-        tc_fence_before();
-        mbar_arrive_warp(o_free(w));
+      } else if (row_in) {
+        a.ml[place * a.piece_rows + w * PC_T + r] = make_float2(mref, l);
       }
-      mbar_arrive_warp(q_empty);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive_warp(q_empty(qb));
     }
     if (__any_sync(0xffffffffu, late)) {
       __syncwarp();
-      for (PcWalk wk(a, ends); wk.more(a); wk.next(a)) {
-        const PcItem m(a, wk);
+      PcWalk walk(a, ends);
+      for (;;) {
+        walk.next(a, m);
+        if (m.s1 == 0) break;
         const int toks = w ? m.toks - a.geo.tpt : min(m.toks, a.geo.tpt);
         if (!m.whole) continue;
         bool bad = false;
@@ -840,44 +1107,72 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
         }
         for (uint32_t again = __ballot_sync(0xffffffffu, bad); again; again &= again - 1) {
           const int src = __ffs(again) - 1;
-          pc_repair<DH, Q8>(a, wk.at.b, m.h, __shfl_sync(0xffffffffu, hq, src), __shfl_sync(0xffffffffu, t, src),
+          pc_repair<DH, Q8>(a, m.b, m.h, __shfl_sync(0xffffffffu, hq, src), __shfl_sync(0xffffffffu, t, src),
                             __shfl_sync(0xffffffffu, m.sp.pf + w * a.geo.tpt + tok, src), m.sp.pf, m.sp.pl);
         }
       }
     }
-  } else if (Q8) {
+  } else if constexpr (Q8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_CTRL));
     // ------------------------------------------------------------ bytes to bf16
     constexpr int LPR = DH / 16, RPW = 32 / LPR;  // lanes of a row, rows of a warp's load
-    constexpr int NR = C::NR ? C::NR : 1;
+    constexpr int NR = C::NR ? C::NR / 2 : 1;
     const int c = lane % LPR, sub = lane / LPR;
     bool ok = true;
-    uint32_t R = 0, G = 0;  // raw tiles, steps so far
-    for (PcWalk wk(a, ends); wk.more(a) && ok; wk.next(a)) {
-      const PcItem m(a, wk);
+    uint32_t G = 0;  // steps so far
+    PcItem m;
+    for (uint32_t it = 0; ok && take(it, m); ++it) {
+#pragma unroll 1
       for (int s = m.s0; s < m.s1 && ok; ++s, ++G) {
 #pragma unroll 1
-        for (int kv = 0; kv < 2 && ok; ++kv, ++R) {
-          const uint32_t st = R % NR, n = kv ? C::NV : C::NK, dst = G % n;
+        for (int kv = 0; kv < 2; ++kv) {
+          const uint32_t n = kv ? C::NV : C::NK, st = kv * NR + G % NR, dst = G % n;
           const uint32_t full = kv ? v_full(dst) : k_full(dst), empty = kv ? v_empty(dst) : k_empty(dst);
-          ok = wait_warp(empty, ((G / n) & 1) ^ 1) && wait_warp(r_full(st), (R / NR) & 1);
+          ok = ok && wait_warp(empty, ((G / n) & 1) ^ 1) && wait_warp(r_full(st), (G / NR) & 1);
           if (!ok) break;
           const uint8_t* raw = smem + C::OFF_RAW + st * C::RAW;
           const signed char* ex = reinterpret_cast<const signed char*>(smem + C::OFF_EXP + st * PC_T);
           uint8_t* tile = smem + (kv ? C::OFF_V : C::OFF_K) + dst * C::TILE;
-#pragma unroll 2
-          for (int i = 0; i < PC_T / (4 * RPW); ++i) {
-            const int row = (i * 4 + warp - 12) * RPW + sub;
-            const uint4 u = *reinterpret_cast<const uint4*>(raw + row * DH + c * 16);
-            const float f = pq_scale(ex[row]), sh = pq_shift(f);
-            const float2 ff = make_float2(f, f), bb = make_float2(sh, sh);
-            const uint2 v0 = pq_values(u.x, ff, bb), v1 = pq_values(u.y, ff, bb), v2 = pq_values(u.z, ff, bb),
-                        v3 = pq_values(u.w, ff, bb);
-            const uint4 lo = make_uint4(v0.x, v0.y, v1.x, v1.y), hi = make_uint4(v2.x, v2.y, v3.x, v3.y);
-            uint8_t* o = tile + (c / 4) * C::HALF + row * 128;
-            const int p = c % 4 * 2, flip = c / 4;  // (lanes of the second half write their pieces the other way round)
-            *reinterpret_cast<uint4*>(o + (((p + flip) ^ (row & 7)) << 4)) = flip ? hi : lo;
-            *reinterpret_cast<uint4*>(o + (((p + 1 - flip) ^ (row & 7)) << 4)) = flip ? lo : hi;
+          constexpr int TURNS = PC_T / (C::CONV * RPW), U = 2;  // rows of a lane; at a time (all four: 71 us where two take 68)
+          static_assert(TURNS * C::CONV * RPW == PC_T && TURNS % U == 0, "each row once");
+          uint8_t* const o0 = tile + (c / 4) * C::HALF;
+          const int p = c % 4 * 2, flip = c / 4;  // (lanes of the second half write their pieces the other way round)
+#pragma unroll 1
+          for (int i = 0; i < TURNS; i += U) {
+            uint4 u[U];
+            int e[U];
+            bool small = true;
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+              const int row = ((i + k) * C::CONV + warp - 12) * RPW + sub;
+              u[k] = *reinterpret_cast<const uint4*>(raw + row * DH + c * 16);
+              e[k] = ex[row];
+              small &= pq_small(e[k]);
+            }
+            auto put = [&](int k, uint2 v0, uint2 v1, uint2 v2, uint2 v3) {
+              const int row = ((i + k) * C::CONV + warp - 12) * RPW + sub;
+              const uint4 lo = make_uint4(v0.x, v0.y, v1.x, v1.y), hi = make_uint4(v2.x, v2.y, v3.x, v3.y);
+              uint8_t* const o = o0 + row * 128;
+              *reinterpret_cast<uint4*>(o + (((p + flip) ^ (row & 7)) << 4)) = flip ? hi : lo;
+              *reinterpret_cast<uint4*>(o + (((p + 1 - flip) ^ (row & 7)) << 4)) = flip ? lo : hi;
+            };
+            if (__all_sync(0xffffffffu, small)) {
+#pragma unroll
+              for (int k = 0; k < U; ++k) {
+                const uint32_t f = pq_factor(e[k]), b = pq_offset(e[k]);
+                put(k, pq_down(u[k].x, f, b), pq_down(u[k].y, f, b), pq_down(u[k].z, f, b), pq_down(u[k].w, f, b));
+              }
+            } else {
+#pragma unroll
+              for (int k = 0; k < U; ++k) {
+                // (of the least exponents 2^(e - PQ_DOWN) is no fp32 number: in two factors)
+                const float f = pq_scale(e[k] == PQ_NAN ? e[k] : max(e[k] - PQ_DOWN, PQ_LOW)), b = pq_shift(f);
+                const uint32_t g = pq_twice(min(e[k] - PQ_DOWN - PQ_LOW, 0));
+                const float2 ff = make_float2(f, f), bb = make_float2(b, b);
+                put(k, pq_times(pq_values(u[k].x, ff, bb), g), pq_times(pq_values(u[k].y, ff, bb), g),
+                    pq_times(pq_values(u[k].z, ff, bb), g), pq_times(pq_values(u[k].w, ff, bb), g));
+              }
+            }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           mbar_arrive_warp(r_empty(st));
@@ -895,9 +1190,12 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
       for (uint32_t i = v_issued > C::NV ? v_issued - C::NV : 0; i < v_issued; ++i)
         mbar_wait_drain(v_full(i % C::NV), (i / C::NV) & 1);
       if (Q8)
-        for (uint32_t i = r_issued > C::NR ? r_issued - C::NR : 0; i < r_issued; ++i)
-          mbar_wait_drain(r_full(i % (C::NR ? C::NR : 1)), (i / (C::NR ? C::NR : 1)) & 1);
-      if (q_issued > 0) mbar_wait_drain(q_full, (q_issued - 1) & 1);
+        for (uint32_t i = r_issued > C::NR ? r_issued - C::NR : 0; i < r_issued; ++i) {
+          constexpr int N = C::NR ? C::NR / 2 : 1;
+          mbar_wait_drain(r_full((i & 1) * N + i / 2 % N), (i / 2 / N) & 1);
+        }
+      for (uint32_t i = q_issued > C::NQ ? q_issued - C::NQ : 0; i < q_issued; ++i)
+        mbar_wait_drain(q_full(i % C::NQ), (i / C::NQ) & 1);
     }
     if (warp == 1 && lane == 0) mbar_wait_drain(done, 0);
   } else if (warp == 1 && lane == 0) {
@@ -908,68 +1206,97 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+  // rows of sequences whose length cannot be
+  for (int b = any_bad ? blockIdx.x : a.geo.B; b < a.geo.B; b += gridDim.x) {
+    bool bad;
+    const PcSeq q = pc_seq(a, b, &bad);
+    const int per = a.geo.KV * a.geo.g * (DH / 8);
+    if (bad)
+      for (long i = threadIdx.x; i < (long)q.n * per; i += C::THREADS)
+        *reinterpret_cast<uint4*>(a.out + (q.t0 + i / per) * a.ldo + i % per * 8) = make_uint4(0, 0, 0, 0);
+  }
 }
 
 // Items that lie on several CTAs: the pieces joined in the order of the CTAs.  CTA x takes the item
-// that begins on CTA x and ends on a later one; CTAs y share its rows, a warp to a row.
+// that begins on CTA x and ends on a later one; CTAs y take 32 of its rows each, a lane to a row and
+// the columns four by four to the warps.
 constexpr int PJ_WARPS = 8;
 template <int DH, bool Q8>
 __global__ void __launch_bounds__(32 * PJ_WARPS) paged_chunk_join_kernel(const __grid_constant__ PcArgs a) {
-  __shared__ PcAt at[PC_CTAS + 1];
+  __shared__ uint32_t again;
   pdl_enter();
-  for (int i = threadIdx.x; i <= a.G; i += 32 * PJ_WARPS) at[i] = a.at[i];
-  __syncthreads();
   const int x = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const PcAt m = at[x + 1];
+  const PcAt m = a.at[x + 1], begin = a.at[x];
   auto same = [&](const PcAt& p) { return p.b == m.b && p.h == m.h && p.u == m.u; };
-  if (m.s == 0 || (same(at[x]) && at[x].s > 0)) return;
-  int n = 2;  // CTAs that begin inside the item, and this one (at[G] is the line's end)
-  while (same(at[x + n]) && at[x + n].s > 0) ++n;
-  // whether CTA x + k holds a piece of it: it may begin where the next one does
-  auto holds = [&](int k) { return k < n && !(k > 0 && same(at[x + k + 1]) && at[x + k + 1].s == at[x + k].s); };
+  if (m.s == 0 || (same(begin) && begin.s > 0)) return;
   const PcSeq q = pc_seq(a, m.b);
   const PcSpan sp = pc_span(a.geo, q, m.u);
   const int R = 2 * a.geo.tpt, toks = min(q.n - m.u * R, R), g = a.geo.g;
-  const int first = same(at[x]) ? 0 : 1;  // piece 0 is the last of its CTA's, the others the first
-  constexpr int C = DH / 32;
-  for (int i = blockIdx.y * PJ_WARPS + warp; i < toks * g; i += gridDim.y * PJ_WARPS) {
-    const int tok = i / g, hg = i % g, w = tok / a.geo.tpt, rr = w * PC_T + (tok - w * a.geo.tpt) * g + hg;
-    auto slot = [&](int k) { return (2l * (x + k) + (k == 0 ? first : 0)) * a.piece_rows + rr; };
-    float M = -INFINITY, L = 0.f, acc[C] = {};
-    for (int k = lane; k < n; k += 32)
-      if (holds(k)) M = fmaxf(M, a.ml[slot(k)].x);
+  const int rr = blockIdx.y * 32 + lane, w = rr / PC_T, tok = w * a.geo.tpt + rr % PC_T / g;
+  const bool row_in = rr % PC_T < a.geo.tpt * g && tok < toks;
+  if (!__any_sync(0xffffffffu, row_in)) return;  // (the same for all warps)
+  if (threadIdx.x == 0) again = 0;
+  __syncthreads();
+  int n = 1;  // this CTA and those that begin inside the item (a.at[a.G] is the line's end)
+  for (uint32_t in = ~0u; in == ~0u; n += __popc(in)) {
+    const int k = x + n + lane;
+    bool is = k <= a.G;
+    if (is) {
+      const PcAt p = a.at[k];
+      is = same(p) && p.s > 0;
+    }
+    in = __ballot_sync(0xffffffffu, is);
+  }
+  // whether CTA x + k < n holds a piece of it: it may begin where the next one does
+  auto holds = [&](int k) { return k == 0 || k == n - 1 || a.at[x + k + 1].s != a.at[x + k].s; };
+  const int first = same(begin) ? 0 : 1;  // piece 0 is the last of its CTA's, the others the first
+  auto place = [&](int k) { return 2l * (x + k) + (k == 0 ? first : 0); };
+  float M = -INFINITY, L = 0.f;
+  if (row_in) {
+#pragma unroll 4
+    for (int k = 0; k < n; ++k)
+      if (holds(k)) M = fmaxf(M, a.ml[place(k) * a.piece_rows + rr].x);
+  }
+  constexpr int C4 = DH / 4, U = C4 / PJ_WARPS;  // groups of four columns; of a warp
+  float4 acc[U] = {};
+  if (row_in) {
+#pragma unroll 2
+    for (int k = 0; k < n; ++k) {
+      if (!holds(k)) continue;
+      const float2 y = a.ml[place(k) * a.piece_rows + rr];
+      const float4* p = a.part + (place(k) * C4 + warp * U) * a.piece_rows + rr;
+      const float f = y.x == M ? 1.f : ex2_approx(y.x - M);  // (-inf, no keys at all: 1 of nothing)
+      L = fmaf(y.y, f, L);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    for (int k0 = 0; k0 < n; k0 += 32) {
-      float f = 0.f;
-      const bool in = holds(k0 + lane);
-      if (in) {
-        const float2 y = a.ml[slot(k0 + lane)];
-        f = M == -INFINITY ? 0.f : ex2_approx(y.x - M);
-        L = fmaf(y.y, f, L);
-      }
-      const uint32_t held = __ballot_sync(0xffffffffu, in);
-#pragma unroll 8
-      for (int k = 0; k < min(32, n - k0); ++k) {
-        const float fk = __shfl_sync(0xffffffffu, f, k);
-        if (!(held >> k & 1)) continue;
-        const float* p = a.part + slot(k0 + k) * DH + C * lane;
-#pragma unroll
-        for (int c = 0; c < C; ++c) acc[c] = fmaf(p[c], fk, acc[c]);
+      for (int u = 0; u < U; ++u) {
+        const float4 v = p[u * a.piece_rows];
+        acc[u].x = fmaf(v.x, f, acc[u].x);
+        acc[u].y = fmaf(v.y, f, acc[u].y);
+        acc[u].z = fmaf(v.z, f, acc[u].z);
+        acc[u].w = fmaf(v.w, f, acc[u].w);
       }
     }
+  }
+  const int t = q.t0 + m.u * R + tok, hq = m.h * g + rr % PC_T % g;
+  if (row_in) {
+    const float inv = PcCfg<DH, Q8>::SCALE / L;
+    bf16* o = a.out + t * a.ldo + (long)hq * DH + warp * U * 4;
+    float fin = 0.f;  // zero, but for sums that are not finite
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-    const int t = q.t0 + m.u * R + tok, hq = m.h * g + hg;
-    bf16* o = a.out + t * a.ldo + (long)hq * DH + C * lane;
-    bool bad = false;
-#pragma unroll
-    for (int c = 0; c < C; c += 2) {
-      const float2 v = make_float2(acc[c] / L, acc[c + 1] / L);
-      bad |= fmaf(v.x, 0.f, v.y * 0.f) != 0.f;
-      *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(v.x, v.y);
+    for (int u = 0; u < U; ++u) {
+      const float4 v = make_float4(acc[u].x * inv, acc[u].y * inv, acc[u].z * inv, acc[u].w * inv);
+      fin = fmaf(v.x, 0.f, fmaf(v.y, 0.f, fmaf(v.z, 0.f, fmaf(v.w, 0.f, fin))));
+      *reinterpret_cast<uint2*>(o + 4 * u) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
     }
-    if (__any_sync(0xffffffffu, bad)) pc_repair<DH, Q8>(a, m.b, m.h, hq, t, sp.pf + tok, sp.pf, sp.pl);
+    if (fin != 0.f) atomicOr(&again, 1u << lane);
+  }
+  __syncthreads();
+  uint32_t mask = again;
+  for (int i = 0; mask; ++i, mask &= mask - 1) {
+    if (i % PJ_WARPS != warp) continue;
+    const int src = __ffs(mask) - 1;
+    pc_repair<DH, Q8>(a, m.b, m.h, __shfl_sync(0xffffffffu, hq, src), __shfl_sync(0xffffffffu, t, src),
+                      __shfl_sync(0xffffffffu, sp.pf + tok, src), sp.pf, sp.pl);
   }
 }
 
@@ -1020,7 +1347,7 @@ cudaError_t pc_launch(const Paged& c, const PcArgs& a, const PcPlan& p, cudaStre
     if (e != cudaSuccess || !p.split) return e;
   }
   LaunchTimer lt("paged_chunk_join", st, 0.0, 8.0 * a.G * p.piece_rows * DH);
-  return launch_kernel(paged_chunk_join_kernel<DH, Q8>, dim3(a.G, 8), 32 * PJ_WARPS, 0, st, a);
+  return launch_kernel(paged_chunk_join_kernel<DH, Q8>, dim3(a.G, p.piece_rows / 32), 32 * PJ_WARPS, 0, st, a);
 }
 
 }  // namespace
@@ -1040,10 +1367,12 @@ cudaError_t paged_chunk(const Paged& c, long rows, const bf16* q, long ldq, cons
   a.page = c.page; a.max_pages = c.max_pages;
   a.n_pages = c.n_pages;
   a.box = std::min(PC_T, c.page & -c.page);
+  while (1 << a.box_log < a.box) ++a.box_log;
   a.G = p.G;
   a.whole = p.split ? 8 : 0;
   a.few = 3 * PC_T;
-  a.sl2 = 1.4426950408889634f / sqrtf((float)c.dh);
+  a.long_item = 8;
+  a.sl2 = (c.Ke ? 1 << PQ_DOWN : 1) * 1.4426950408889634f / sqrtf((float)c.dh);
   a.q = q; a.ldq = ldq;
   a.out = out; a.ldo = ldo;
   a.K = c.K; a.V = c.V; a.Ke = c.Ke; a.Ve = c.Ve;
@@ -1051,7 +1380,7 @@ cudaError_t paged_chunk(const Paged& c, long rows, const bf16* q, long ldq, cons
     char* w = static_cast<char*>(ws);
     a.at = reinterpret_cast<PcAt*>(w + p.at);
     a.ml = reinterpret_cast<float2*>(w + p.ml);
-    a.part = reinterpret_cast<float*>(w + p.bytes) - 2 * (size_t)p.G * p.piece_rows * c.dh;
+    a.part = reinterpret_cast<float4*>(w + p.bytes) - 2 * (size_t)p.G * p.piece_rows * (c.dh / 4);
   }
   a.piece_rows = p.piece_rows;
   if (c.Ke) return c.dh == 128 ? pc_launch<128, true>(c, a, p, st) : pc_launch<64, true>(c, a, p, st);

@@ -61,18 +61,47 @@ __host__ __device__ __forceinline__ PcSpan pc_span(const PcGeo& g, const PcSeq& 
 __host__ __device__ __forceinline__ long long pc_cum(const PcGeo& g, const PcSeq& q, int u) {
   constexpr long long ITEM = 256;
   const int P = pc_pairs(g, q);
-  const long long R = 2 * g.tpt, p0 = q.len - q.n, cap = g.W > 0 ? (long long)g.W + g.S + R : (1ll << 40);
-  auto sum = [&](long long n) {
-    long long k = cap > p0 ? (cap - p0) / R : 0;
-    if (k > n) k = n;
-    return 3 * (k * p0 + R * (k * (k + 1) / 2) + (n - k) * cap + n * ITEM);
+  const int R = 2 * g.tpt, p0 = q.len - q.n;
+  const long long cap = (long long)g.W + g.S + R;
+  auto sum = [&](int n) {
+    int k = n;  // pairs that see no more than cap
+    if (g.W > 0 && p0 + (long long)R * n > cap) k = cap > p0 ? (int)((unsigned)(cap - p0) / (unsigned)R) : 0;
+    return 3 * ((long long)k * p0 + R * ((long long)k * (k + 1) / 2) + (n - k) * cap + n * ITEM);
   };
   const bool single = u == P && q.n - (P - 1) * (int)R <= g.tpt;
   return single ? sum(u) - (sum(u) - sum(u - 1)) / 3 : sum(u);
 }
 
-// The item at weight y < pc_cum(P) of one head's pairs, and the step (whole: items are not cut, a
-// place inside one is its end).
+__host__ __device__ __forceinline__ float pc_quotient(float a, float b) {
+#ifdef __CUDA_ARCH__
+  return __fdividef(a, b);
+#else
+  return a / b;
+#endif
+}
+
+// The step at weight y of pair u (whole: items are not cut, a place inside one is its end).  Neither
+// this nor pc_share has to be exact, only the same for whoever asks, and to grow with y or c: a
+// division of 64-bit numbers, cold, took 1000 cycles of a call's first 20000.
+__host__ __device__ __forceinline__ int pc_step(const PcGeo& g, const PcSeq& q, int u, long long y, bool whole) {
+  const long long at = pc_cum(g, q, u);
+  const int steps = pc_span(g, q, u).steps;
+  if (y <= at || whole) return y > at ? steps : 0;
+  const int s = (int)(pc_quotient((float)(y - at), (float)(pc_cum(g, q, u + 1) - at)) * (float)steps);
+  return s < steps ? s : steps - 1;
+}
+
+// The head of weight y, of `per` each; y becomes what is left.
+__host__ __device__ __forceinline__ int pc_head(long long per, long long& y) {
+  int h = (int)pc_quotient((float)y, (float)per);
+  while (h > 0 && h * per > y) --h;  // (off by one at most)
+  while ((h + 1) * per <= y) ++h;
+  y -= h * per;
+  return h;
+}
+
+// The pair at weight y < pc_cum(P) of one head's pairs, and the step.  (The kernel's warps look for
+// the pair with all lanes.)
 __host__ __device__ __forceinline__ void pc_find(const PcGeo& g, const PcSeq& q, long long y, bool whole, int* u,
                                                  int* s) {
   int lo = 0, hi = pc_pairs(g, q);
@@ -80,15 +109,15 @@ __host__ __device__ __forceinline__ void pc_find(const PcGeo& g, const PcSeq& q,
     const int m = lo + (hi - lo) / 2;
     if (pc_cum(g, q, m) <= y) lo = m; else hi = m;
   }
-  const long long at = pc_cum(g, q, lo), w = pc_cum(g, q, lo + 1) - at;
-  const int steps = pc_span(g, q, lo).steps;
   *u = lo;
-  *s = whole ? (y > at ? steps : 0) : (int)((y - at) * steps / w);
+  *s = pc_step(g, q, lo, y, whole);
 }
 
 // Where CTA c of n begins on a line of length T.
 __host__ __device__ __forceinline__ long long pc_share(long long T, int n, int c) {
-  return T / n * c + T % n * c / n;
+  if (c >= n) return T;
+  const unsigned f = (unsigned)(pc_quotient((float)c, (float)n) * 4294967296.f);  // c <= 151, n <= 152: below 2^32
+  return (long long)(((unsigned long long)T >> 32) * f + ((((unsigned long long)T & 0xffffffffu) * f) >> 32));
 }
 
 }  // namespace pf

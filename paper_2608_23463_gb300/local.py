@@ -19,7 +19,7 @@ import torch
 
 from . import (PF_BF16, PF_ERR_CAPACITY, PF_ERR_CUDA, PF_ERR_INVALID_ARG, PF_F32, PagedCache,
                PagedDesc, PagedExp, ProxyFormerError, QKDesc, WindowDesc, load, pf_paged_advance,
-               pf_paged_attn_workspace_size, pf_qk_rope_workspace_size, pf_window_attn_saved_size,
+               pf_paged_attn_q8_workspace_size, pf_paged_attn_workspace_size, pf_qk_rope_workspace_size, pf_window_attn_saved_size,
                pf_window_attn_workspace_size)
 from .buildlib import binding_tag
 
@@ -175,8 +175,8 @@ class PagedKVCache:
         if dtype == torch.int8:
             self.exp = PagedExp(self.K_exp.data_ptr(), self.V_exp.data_ptr())
             self.at_exp = addressof(self.exp)
-        self.ws = torch.empty(max(16, pf_paged_attn_workspace_size(self.desc)), dtype=torch.uint8,
-                              device=self.K.device)
+        size = pf_paged_attn_workspace_size if dtype == torch.bfloat16 else pf_paged_attn_q8_workspace_size
+        self.ws = torch.empty(max(16, size(self.desc)), dtype=torch.uint8, device=self.K.device)
         self.free = list(range(n_pages - 1, -1, -1))  # pages that reserve() hands out
         self.held = [[] for _ in range(batch)]        # and has handed out, by sequence
         self.left = set()                             # sequences released and not begun again
