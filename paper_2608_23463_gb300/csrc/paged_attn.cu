@@ -74,6 +74,7 @@ struct PaArgs {
   long ldo;
   float* part;  // [2 G][g][DH] sums, then [2 G][g][2] (max, sum)
   int B, KV, g, page, max_pages, window, sinks, G;
+  int page_log;  // a page of 2^n rows: n; else -1
   bool whole;  // a CTA for each (sequence, key head), not equal ranges of units
   long n_pages;
   float sl2;  // log2(e) / sqrt(dh)
@@ -136,6 +137,9 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool f
   const int n = full ? 16 : 0;  // 0: zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
                : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -244,17 +248,30 @@ __global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaAr
       const int k = t0 + i * PA_WARPS;
       return (k < sp.ns ? k : sp.lo + k - sp.ns) * PA_TILE;
     };
-    auto page_of = [&](int i) { return i < nt ? tab[tile_row(i) / a.page] : 0; };
+    // (quantised tiles are half as long: the divisions of their rows show, so that pages of 2^n rows do without)
+    auto page_at = [&](int row) { return Q8 && a.page_log >= 0 ? row >> a.page_log : row / a.page; };
+    auto row_in = [&](int row) { return Q8 && a.page_log >= 0 ? row & (a.page - 1) : row % a.page; };
+    auto page_of = [&](int i) { return i < nt ? tab[page_at(tile_row(i))] : 0; };
     auto fill = [&](int i, int pg) {  // tile i into its stage
       if (i < nt) {
         const int row = tile_row(i);
         const bool ok = pg >= 0 && pg < a.n_pages;
         if (!ok && lane == 0) set_dev_error(DEVERR_CAPACITY);
-        const long at = ((ok ? (long)pg : 0L) * a.KV + h) * a.page + row % a.page, o = at * DH;
+        const long at = ((ok ? (long)pg : 0L) * a.KV + h) * a.page + row_in(row), o = at * DH;
         const uint32_t ks = wr + (i % C::STAGES) * 2 * C::TILE_BYTES, vs = ks + C::TILE_BYTES;
         constexpr int CPR = DH / (Q8 ? 16 : 8);  // 16-byte chunks of a row
         if (Q8) {
           const signed char *kb = reinterpret_cast<const signed char*>(a.K), *vb = reinterpret_cast<const signed char*>(a.V);
+          if (ok && row <= sp.n - PA_TILE && (row >= sp.first || row <= a.sinks - PA_TILE)) {  // every row is seen
+            kb += o + lane * 16;
+            vb += o + lane * 16;
+#pragma unroll
+            for (int j = 0; j < PA_TILE * CPR / 32; ++j) {
+              const int r = j * (32 / CPR) + lane / CPR, c = lane % CPR;
+              cp_async16(ks + pa_k8<DH>(r, c), kb + j * 512);
+              cp_async16(vs + pa_v8<DH>(r, c), vb + j * 512);
+            }
+          } else
 #pragma unroll
           for (int j = 0; j < PA_TILE * CPR / 32; ++j) {
             const int e = j * 32 + lane, r = e / CPR, c = e % CPR;
@@ -287,16 +304,19 @@ __global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaAr
       fill(i, pg);
     }
     // the group's queries: rows gid and gid + 8 of the MMAs' A
-    uint4 qa[KC], qb[KC];
+    uint32_t qf[2 * KC][4];
     {
       // (a chunk of 16 quantised values meets two of 8 of Q's)
       const bf16* qr = a.q + b * a.ldq + (long)h * a.g * DH + (Q8 ? 16 : 8) * t;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         const int at = Q8 ? 64 * (c / 2) + 8 * (c % 2) : 32 * c;
-        qa[c] = qb[c] = make_uint4(0, 0, 0, 0);
-        if (gid < a.g) qa[c] = *reinterpret_cast<const uint4*>(qr + gid * DH + at);
-        if (gid + 8 < a.g) qb[c] = *reinterpret_cast<const uint4*>(qr + (gid + 8) * DH + at);
+        uint4 u = make_uint4(0, 0, 0, 0), v = u;
+        if (gid < a.g) u = *reinterpret_cast<const uint4*>(qr + gid * DH + at);
+        if (gid + 8 < a.g) v = *reinterpret_cast<const uint4*>(qr + (gid + 8) * DH + at);
+        const uint32_t w[8] = {u.x, v.x, u.y, v.y, u.z, v.z, u.w, v.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qf[2 * c + e / 4][e % 4] = w[e];
       }
     }
     float acc[NT][4] = {};
@@ -324,9 +344,7 @@ __global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaAr
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
               const uint2 kv = pq_down(w == 0 ? k.x : w == 1 ? k.y : w == 2 ? k.z : k.w, F0, C0);
-              const uint4 ua = qa[2 * c + w / 2], ub = qb[2 * c + w / 2];
-              const uint32_t qv[4] = {w % 2 ? ua.z : ua.x, w % 2 ? ub.z : ub.x, w % 2 ? ua.w : ua.y, w % 2 ? ub.w : ub.y};
-              mma16816(s[n], qv, kv.x, kv.y);
+              mma16816(s[n], qf[4 * c + w], kv.x, kv.y);
             }
           }
       } else
@@ -337,22 +355,20 @@ __global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaAr
           const int r = n * 8 + gid;
           const uint4 k = *reinterpret_cast<const uint4*>(
               kp + (r * (DH / 8) + ((4 * c + t) ^ ((r & 1) << 2))) * 16);
-          const uint32_t a0[4] = {qa[c].x, qb[c].x, qa[c].y, qb[c].y};
-          mma16816(s[n], a0, k.x, k.y);
-          const uint32_t a1[4] = {qa[c].z, qb[c].z, qa[c].w, qb[c].w};
-          mma16816(s[n], a1, k.z, k.w);
+          mma16816(s[n], qf[2 * c], k.x, k.y);
+          mma16816(s[n], qf[2 * c + 1], k.z, k.w);
         }
       const int row = tile_row(i);
       float vf[4];  // the values' factors of keys 8 n + 2 t + e at 2 n + e
       if (Q8) {
-        const unsigned char* ex = wring + C::EXP + (i % C::STAGES) * 32;
+        // each lane the factor of one exponent, of K's rows and then V's, handed round
+        const float f = pa_factor((signed char)wring[C::EXP + (i % C::STAGES) * 32 + lane]);
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int j = n * 8 + 2 * t + e;
-            const float kf = pa_factor((signed char)ex[j]);
-            vf[2 * n + e] = pa_factor((signed char)ex[PA_TILE + j]);
+            const float kf = __shfl_sync(0xffffffffu, f, n * 8 + 2 * t + e);
+            vf[2 * n + e] = __shfl_sync(0xffffffffu, f, PA_TILE + n * 8 + 2 * t + e);
             s[n][e] *= kf;
             s[n][e + 2] *= kf;
           }
@@ -619,6 +635,9 @@ cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long 
   a.part = ws;
   a.B = c.B; a.KV = c.KV; a.g = c.H / c.KV; a.page = c.page; a.max_pages = c.max_pages;
   a.window = c.window; a.sinks = c.sinks;
+  a.page_log = -1;
+  for (int n = 4; n < 31; ++n)
+    if (c.page == 1 << n) a.page_log = n;
   a.n_pages = c.n_pages;
   a.whole = pa_whole(c);
   a.G = a.whole ? c.B * c.KV : pa_grid(c, c.Ke);
