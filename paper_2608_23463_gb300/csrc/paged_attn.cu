@@ -29,9 +29,11 @@
 // CTAs, so that results repeat bit for bit.
 //
 // Quantised rows are read as they lie, 16 bytes a chunk: their whole numbers become bf16 in
-// registers, and the powers of two go into the scores and into P, where they are exact.  A
-// transposing load hands a thread two columns of V for two keys: the even ones of 16 columns are
-// one MMA's, the odd ones another's.
+// registers, and the powers of two go into the scores and into P, where they are exact.  What
+// takes the time there is their instructions, not HBM: so keys are the MMAs' rows and the query
+// heads their 8 columns (or twice 8), half the MMAs, sums and exponentials of the form above, and
+// the same for O^T = V^T P^T.  A transposing load hands a thread two columns of V for two keys: the
+// even ones of 16 columns are the first 8 rows of V^T, the odd ones the others.
 #include <algorithm>
 
 #include "local.h"
@@ -158,6 +160,13 @@ __device__ __forceinline__ float ex2_approx(float x) {
   return y;
 }
 
+// An 8 x 8 matrix of bf16, row lane / 4 and columns 2 (lane % 4), + 1 of each lane, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
 // Chunk c of row r in a quantised tile of K, and of V: the reads of eight lanes (two rows' chunks
 // of K, eight rows' same chunk of V) meet all banks.
 template <int DH>
@@ -177,12 +186,13 @@ __device__ __forceinline__ float pa_factor(int e) {
 __device__ __forceinline__ long pa_first(long T, int G, int c) { return T * c / G; }
 __device__ __forceinline__ int pa_cta(long T, int G, long u) { return (int)(((u + 1) * G - 1) / T); }
 
-template <int DH, bool Q8>
+// NH: groups of 8 query heads to a key head (quantised caches; else 1)
+template <int DH, bool Q8, int NH>
 __global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaArgs a) {
   using C = PaCfg<DH, Q8>;
   constexpr int KC = DH / 32;  // 32-wide chunks of a row, two MMAs each
   constexpr int NT = DH / 8;   // 8-wide output tiles
-  const uint32_t F0 = pq_factor(0), C0 = pq_offset(0);
+  const uint32_t F0 = pq_factor(0), C0 = pq_offset(0);  // of quantised values, whose own factors come in later
   extern __shared__ __align__(128) unsigned char ring[];
   __shared__ int pre[PA_MAX_B + 1];
   pdl_enter();
@@ -303,170 +313,263 @@ __global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaAr
       pg_next = page_of(i + 1);
       fill(i, pg);
     }
-    // the group's queries: rows gid and gid + 8 of the MMAs' A
-    uint32_t qf[2 * KC][4];
-    {
-      // (a chunk of 16 quantised values meets two of 8 of Q's)
-      const bf16* qr = a.q + b * a.ldq + (long)h * a.g * DH + (Q8 ? 16 : 8) * t;
-#pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        const int at = Q8 ? 64 * (c / 2) + 8 * (c % 2) : 32 * c;
-        uint4 u = make_uint4(0, 0, 0, 0), v = u;
-        if (gid < a.g) u = *reinterpret_cast<const uint4*>(qr + gid * DH + at);
-        if (gid + 8 < a.g) v = *reinterpret_cast<const uint4*>(qr + (gid + 8) * DH + at);
-        const uint32_t w[8] = {u.x, v.x, u.y, v.y, u.z, v.z, u.w, v.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qf[2 * c + e / 4][e % 4] = w[e];
-      }
-    }
-    float acc[NT][4] = {};
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    for (int i = 0; i < nt; ++i) {
-      cp_wait<C::STAGES - 2>();
-      __syncwarp();
+    if constexpr (Q8) {
+      // the group's queries, heads gid (and gid + 8) as columns of the MMAs' B; a chunk of 16 quantised
+      // values meets two of 8 of theirs
+      uint32_t qf[NH][2 * KC][2];
       {
-        const int pg = pg_next;
-        pg_next = page_of(i + C::STAGES);
-        fill(i + C::STAGES - 1, pg);  // the stage read in the last round
-      }
-      const uint32_t ks = wr + (i % C::STAGES) * 2 * C::TILE_BYTES, vs = ks + C::TILE_BYTES;
-      const unsigned char* kp = wring + (i % C::STAGES) * 2 * C::TILE_BYTES;
-      // scores: rows of S are query heads, columns keys 8 n + 2 t, + 1.  A thread
-      // takes 8 values of a row at once; the sum over them is free of order, and
-      // Q's are taken alike.
-      float s[2][4] = {};
-      if (Q8) {
+        const bf16* qr = a.q + b * a.ldq + (long)h * a.g * DH + 16 * t;
 #pragma unroll
-        for (int c = 0; c < DH / 64; ++c)
+        for (int n = 0; n < NH; ++n)
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const uint4 k = *reinterpret_cast<const uint4*>(kp + pa_k8<DH>(n * 8 + gid, 4 * c + t));
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint2 kv = pq_down(w == 0 ? k.x : w == 1 ? k.y : w == 2 ? k.z : k.w, F0, C0);
-              mma16816(s[n], qf[4 * c + w], kv.x, kv.y);
-            }
+          for (int c = 0; c < KC; ++c) {
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (8 * n + gid < a.g)
+              u = *reinterpret_cast<const uint4*>(qr + (8 * n + gid) * DH + 64 * (c / 2) + 8 * (c % 2));
+            qf[n][2 * c][0] = u.x;
+            qf[n][2 * c][1] = u.y;
+            qf[n][2 * c + 1][0] = u.z;
+            qf[n][2 * c + 1][1] = u.w;
           }
-      } else
+      }
+      float acc[NH][DH / 16][4] = {};  // O^T: columns 16 c + 2 gid (and + 1 at [2], [3]) of heads 2 t, 2 t + 1
+      float m[NH][2], l[NH][2];        // of heads 2 t, 2 t + 1
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const int r = n * 8 + gid;
-          const uint4 k = *reinterpret_cast<const uint4*>(
-              kp + (r * (DH / 8) + ((4 * c + t) ^ ((r & 1) << 2))) * 16);
-          mma16816(s[n], qf[2 * c], k.x, k.y);
-          mma16816(s[n], qf[2 * c + 1], k.z, k.w);
+      for (int n = 0; n < NH; ++n) {
+        m[n][0] = m[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = 0.f;
+      }
+      for (int i = 0; i < nt; ++i) {
+        cp_wait<C::STAGES - 2>();
+        __syncwarp();
+        {
+          const int pg = pg_next;
+          pg_next = page_of(i + C::STAGES);
+          fill(i + C::STAGES - 1, pg);  // the stage read in the last round
         }
-      const int row = tile_row(i);
-      float vf[4];  // the values' factors of keys 8 n + 2 t + e at 2 n + e
-      if (Q8) {
+        const uint32_t vs = wr + (i % C::STAGES) * 2 * C::TILE_BYTES + C::TILE_BYTES;
+        const unsigned char* kp = wring + (i % C::STAGES) * 2 * C::TILE_BYTES;
         // each lane the factor of one exponent, of K's rows and then V's, handed round
         const float f = pa_factor((signed char)wring[C::EXP + (i % C::STAGES) * 32 + lane]);
+        // scores: rows of S^T are keys gid and gid + 8, columns heads 2 t, 2 t + 1.  A thread takes 16
+        // values of a row at once; the sum over them is free of order, and Q's are taken alike.
+        float s[NH][4] = {};
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int c = 0; c < DH / 64; ++c) {
+          const uint4 k0 = *reinterpret_cast<const uint4*>(kp + pa_k8<DH>(gid, 4 * c + t));
+          const uint4 k1 = *reinterpret_cast<const uint4*>(kp + pa_k8<DH>(8 + gid, 4 * c + t));
+          const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float kf = __shfl_sync(0xffffffffu, f, n * 8 + 2 * t + e);
-            vf[2 * n + e] = __shfl_sync(0xffffffffu, f, PA_TILE + n * 8 + 2 * t + e);
-            s[n][e] *= kf;
-            s[n][e + 2] *= kf;
-          }
-      }
-      if (row > sp.n - PA_TILE || row < sp.first) {  // the last tile, the sinks', the window's first
+          for (int w = 0; w < 4; ++w) {
+            const uint2 x = pq_down(w0[w], F0, C0), y = pq_down(w1[w], F0, C0);
+            const uint32_t ka[4] = {x.x, y.x, x.y, y.y};
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int j = row + n * 8 + 2 * t + e;
-            if (j >= sp.n || (j < sp.first && j >= a.sinks)) {
-              s[n][e] = s[n][e + 2] = -INFINITY;
-              if (Q8) vf[2 * n + e] = 0.f;
-            }
-          }
-      }
-      float mx[2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        mx[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]));
-        mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
-        mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2)) * a.sl2;
-      }
-      // the reference is raised only by more than PA_RESCALE (log2 units): until then
-      // every probability is at most 2^PA_RESCALE, as exact in bf16 as any other
-      if (__any_sync(0xffffffffu, mx[0] > m[0] + PA_RESCALE || mx[1] > m[1] + PA_RESCALE)) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          if (!(mx[r] > m[r] + PA_RESCALE)) continue;
-          const float f = ex2_approx(m[r] - mx[r]);  // first keys: 2^-inf = 0 of nothing
-          m[r] = mx[r];
-          l[r] *= f;
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            acc[n][2 * r] *= f;
-            acc[n][2 * r + 1] *= f;
+            for (int n = 0; n < NH; ++n) mma16816(s[n], ka, qf[n][4 * c + w][0], qf[n][4 * c + w][1]);
           }
         }
-      }
-      uint32_t p[4];  // P as the A operand: bf16, the sums take it unrounded
+        const float kf[2] = {__shfl_sync(0xffffffffu, f, gid), __shfl_sync(0xffffffffu, f, 8 + gid)};
+        float vf[2] = {__shfl_sync(0xffffffffu, f, 16 + gid), __shfl_sync(0xffffffffu, f, 24 + gid)};
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float ref = m[r] == -INFINITY ? 0.f : m[r];
-        float e[4];
+        for (int n = 0; n < NH; ++n)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+          for (int e = 0; e < 4; ++e) s[n][e] *= kf[e / 2];
+        const int row = tile_row(i);
+        if (row > sp.n - PA_TILE || row < sp.first) {  // the last tile, the sinks', the window's first
 #pragma unroll
-          for (int k = 0; k < 2; ++k) e[2 * n + k] = ex2_approx(fmaf(s[n][2 * r + k], a.sl2, -ref));
-        l[r] += (e[0] + e[1]) + (e[2] + e[3]);
-        if (Q8)
+          for (int k = 0; k < 2; ++k) {
+            const int j = row + 8 * k + gid;
+            if (j >= sp.n || (j < sp.first && j >= a.sinks)) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) e[k] *= vf[k];
-        p[r] = pack_bf16(e[0], e[1]);
-        p[r + 2] = pack_bf16(e[2], e[3]);
-      }
-      if (Q8) {
+              for (int n = 0; n < NH; ++n) s[n][2 * k] = s[n][2 * k + 1] = -INFINITY;
+              vf[k] = 0.f;
+            }
+          }
+        }
+        // as above: the reference is raised only by more than PA_RESCALE
+        float mx[NH][2];
+        bool up = false;
 #pragma unroll
-        for (int c = 0; c < NT; c += 4) {  // 32 columns
+        for (int n = 0; n < NH; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            mx[n][e] = fmaxf(s[n][e], s[n][2 + e]);
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xffffffffu, mx[n][e], o));
+            mx[n][e] *= a.sl2;
+            up |= mx[n][e] > m[n][e] + PA_RESCALE;
+          }
+        if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+          for (int n = 0; n < NH; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              if (!(mx[n][e] > m[n][e] + PA_RESCALE)) continue;
+              const float d = ex2_approx(m[n][e] - mx[n][e]);  // first keys: 2^-inf = 0 of nothing
+              m[n][e] = mx[n][e];
+              l[n][e] *= d;
+#pragma unroll
+              for (int c = 0; c < DH / 16; ++c) {
+                acc[n][c][e] *= d;
+                acc[n][c][2 + e] *= d;
+              }
+            }
+        }
+        uint32_t p[NH][2];  // P as the B operand: keys 2 t, 2 t + 1 (and + 8) of head gid
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {
+          float e[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float ref = m[n][k % 2] == -INFINITY ? 0.f : m[n][k % 2];
+            e[k] = ex2_approx(fmaf(s[n][k], a.sl2, -ref));
+          }
+          l[n][0] += e[0] + e[2];
+          l[n][1] += e[1] + e[3];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) p[n][k] = transposed(pack_bf16(e[2 * k] * vf[k], e[2 * k + 1] * vf[k]));
+        }
+#pragma unroll
+        for (int c = 0; c < DH / 32; ++c) {  // 32 columns
           uint32_t v[4];
-          ldmatrix_x4_trans(vs + pa_v8<DH>(lane & 15, c / 2 + (lane >> 4)), v);
+          ldmatrix_x4_trans(vs + pa_v8<DH>(lane & 15, 2 * c + (lane >> 4)), v);
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             // bytes 0, 2: keys 2 t and 2 t + 1 of an even column; 1, 3: of the odd one
             const uint2 lo = pq_down_cols(v[2 * u], F0, C0), hi = pq_down_cols(v[2 * u + 1], F0, C0);
-            mma16816(acc[c + 2 * u], p, lo.x, hi.x);
-            mma16816(acc[c + 2 * u + 1], p, lo.y, hi.y);
+            const uint32_t va[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+            for (int n = 0; n < NH; ++n) mma16816(acc[n][2 * c + u], va, p[n][0], p[n][1]);
           }
         }
-      } else
-#pragma unroll
-      for (int c = 0; c < NT; c += 2) {
-        const int r = lane & 15, ch = c + (lane >> 4);
-        uint32_t v[4];
-        ldmatrix_x4_trans(vs + (r * (DH / 8) + (ch ^ (r & 7))) * 16, v);
-        mma16816(acc[c], p, v[0], v[1]);
-        mma16816(acc[c + 1], p, v[2], v[3]);
+        __syncwarp();
       }
+      cp_wait<0>();
       __syncwarp();
-    }
-    cp_wait<0>();
-    __syncwarp();
-    // the warps' sums through their rings: row r of a warp at r * (DH + 4), its (max, sum)
-    // after the values
+      // the warps' sums through their rings: head r of a warp at r * (DH + 4), its (max, sum)
+      // after the values
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-      float* w = reinterpret_cast<float*>(wring) + (gid + 8 * r) * (DH + 4);
-      if (Q8) {
+      for (int n = 0; n < NH; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; n += 2)
-          *reinterpret_cast<float4*>(w + 8 * n + 4 * t) =
-              make_float4(acc[n][2 * r], acc[n + 1][2 * r], acc[n][2 * r + 1], acc[n + 1][2 * r + 1]);
-      } else
+        for (int e = 0; e < 2; ++e) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-          *reinterpret_cast<float2*>(w + 8 * n + 2 * t) = make_float2(acc[n][2 * r], acc[n][2 * r + 1]);
-      if (t == 0) *reinterpret_cast<float2*>(w + DH) = make_float2(m[r], l[r]);
+          for (int o = 4; o < 32; o <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], o);
+          float* w = reinterpret_cast<float*>(wring) + (8 * n + 2 * t + e) * (DH + 4);
+#pragma unroll
+          for (int c = 0; c < DH / 16; ++c)
+            *reinterpret_cast<float2*>(w + 16 * c + 2 * gid) = make_float2(acc[n][c][e], acc[n][c][2 + e]);
+          if (gid == 0) *reinterpret_cast<float2*>(w + DH) = make_float2(m[n][e], l[n][e]);
+        }
+    } else {
+      // the group's queries: rows gid and gid + 8 of the MMAs' A
+      uint32_t qf[2 * KC][4];
+      {
+        const bf16* qr = a.q + b * a.ldq + (long)h * a.g * DH + 8 * t;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          uint4 u = make_uint4(0, 0, 0, 0), v = u;
+          if (gid < a.g) u = *reinterpret_cast<const uint4*>(qr + gid * DH + 32 * c);
+          if (gid + 8 < a.g) v = *reinterpret_cast<const uint4*>(qr + (gid + 8) * DH + 32 * c);
+          const uint32_t w[8] = {u.x, v.x, u.y, v.y, u.z, v.z, u.w, v.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) qf[2 * c + e / 4][e % 4] = w[e];
+        }
+      }
+      float acc[NT][4] = {};
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+      for (int i = 0; i < nt; ++i) {
+        cp_wait<C::STAGES - 2>();
+        __syncwarp();
+        {
+          const int pg = pg_next;
+          pg_next = page_of(i + C::STAGES);
+          fill(i + C::STAGES - 1, pg);  // the stage read in the last round
+        }
+        const uint32_t ks = wr + (i % C::STAGES) * 2 * C::TILE_BYTES, vs = ks + C::TILE_BYTES;
+        const unsigned char* kp = wring + (i % C::STAGES) * 2 * C::TILE_BYTES;
+        // scores: rows of S are query heads, columns keys 8 n + 2 t, + 1.  A thread
+        // takes 8 values of a row at once; the sum over them is free of order, and
+        // Q's are taken alike.
+        float s[2][4] = {};
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const int r = n * 8 + gid;
+            const uint4 k = *reinterpret_cast<const uint4*>(
+                kp + (r * (DH / 8) + ((4 * c + t) ^ ((r & 1) << 2))) * 16);
+            mma16816(s[n], qf[2 * c], k.x, k.y);
+            mma16816(s[n], qf[2 * c + 1], k.z, k.w);
+          }
+        const int row = tile_row(i);
+        if (row > sp.n - PA_TILE || row < sp.first) {  // the last tile, the sinks', the window's first
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int j = row + n * 8 + 2 * t + e;
+              if (j >= sp.n || (j < sp.first && j >= a.sinks)) s[n][e] = s[n][e + 2] = -INFINITY;
+            }
+        }
+        float mx[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          mx[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]));
+          mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
+          mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2)) * a.sl2;
+        }
+        // the reference is raised only by more than PA_RESCALE (log2 units): until then
+        // every probability is at most 2^PA_RESCALE, as exact in bf16 as any other
+        if (__any_sync(0xffffffffu, mx[0] > m[0] + PA_RESCALE || mx[1] > m[1] + PA_RESCALE)) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            if (!(mx[r] > m[r] + PA_RESCALE)) continue;
+            const float f = ex2_approx(m[r] - mx[r]);  // first keys: 2^-inf = 0 of nothing
+            m[r] = mx[r];
+            l[r] *= f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              acc[n][2 * r] *= f;
+              acc[n][2 * r + 1] *= f;
+            }
+          }
+        }
+        uint32_t p[4];  // P as the A operand: bf16, the sums take it unrounded
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float ref = m[r] == -INFINITY ? 0.f : m[r];
+          float e[4];
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) e[2 * n + k] = ex2_approx(fmaf(s[n][2 * r + k], a.sl2, -ref));
+          l[r] += (e[0] + e[1]) + (e[2] + e[3]);
+          p[r] = pack_bf16(e[0], e[1]);
+          p[r + 2] = pack_bf16(e[2], e[3]);
+        }
+#pragma unroll
+        for (int c = 0; c < NT; c += 2) {
+          const int r = lane & 15, ch = c + (lane >> 4);
+          uint32_t v[4];
+          ldmatrix_x4_trans(vs + (r * (DH / 8) + (ch ^ (r & 7))) * 16, v);
+          mma16816(acc[c], p, v[0], v[1]);
+          mma16816(acc[c + 1], p, v[2], v[3]);
+        }
+        __syncwarp();
+      }
+      cp_wait<0>();
+      __syncwarp();
+      // the warps' sums through their rings: row r of a warp at r * (DH + 4), its (max, sum)
+      // after the values
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+        float* w = reinterpret_cast<float*>(wring) + (gid + 8 * r) * (DH + 4);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            *reinterpret_cast<float2*>(w + 8 * n + 2 * t) = make_float2(acc[n][2 * r], acc[n][2 * r + 1]);
+        if (t == 0) *reinterpret_cast<float2*>(w + DH) = make_float2(m[r], l[r]);
+      }
     }
     __syncthreads();
     const bool whole = u0 == 0 && u1 == nu;
@@ -595,16 +698,16 @@ int pa_grid(const Paged& c, bool q8) {
   return (int)std::min<long>(q8 ? PA_CTAS_Q8 : PA_CTAS, units);
 }
 
-template <int DH, bool Q8>
+template <int DH, bool Q8, int NH = 1>
 cudaError_t pa_launch(const PaArgs& a, bool split, cudaStream_t st) {
   static KernelOnce once;
-  cudaError_t e = once(reinterpret_cast<const void*>(paged_attn_kernel<DH, Q8>), PaCfg<DH, Q8>::SMEM);
+  cudaError_t e = once(reinterpret_cast<const void*>(paged_attn_kernel<DH, Q8, NH>), PaCfg<DH, Q8>::SMEM);
   if (e != cudaSuccess) return e;
   const double rows = (double)a.B * a.KV * std::min<long>((long)a.max_pages * a.page, 0x7fffffffL);
   {
     // work: upper bound (every cache full)
     LaunchTimer lt("paged_attn", st, 4.0 * rows * a.g * DH, (Q8 ? 2.0 : 4.0) * rows * DH);
-    e = launch_kernel(paged_attn_kernel<DH, Q8>, a.G, PA_THREADS, PaCfg<DH, Q8>::SMEM, st, a);
+    e = launch_kernel(paged_attn_kernel<DH, Q8, NH>, a.G, PA_THREADS, PaCfg<DH, Q8>::SMEM, st, a);
     if (e != cudaSuccess || !split) return e;
   }
   LaunchTimer lt("paged_join", st, 0.0, 8.0 * a.G * a.g * (DH + 2));
@@ -643,6 +746,7 @@ cudaError_t paged_attn(const Paged& c, const bf16* q, long ldq, bf16* out, long 
   a.G = a.whole ? c.B * c.KV : pa_grid(c, c.Ke);
   a.sl2 = 1.4426950408889634f / sqrtf((float)c.dh);
   const bool split = !a.whole && (long)c.max_pages * c.page > PA_UNIT;  // else no pair has two units
+  if (c.Ke && a.g > 8) return c.dh == 128 ? pa_launch<128, true, 2>(a, split, st) : pa_launch<64, true, 2>(a, split, st);
   if (c.Ke) return c.dh == 128 ? pa_launch<128, true>(a, split, st) : pa_launch<64, true>(a, split, st);
   return c.dh == 128 ? pa_launch<128, false>(a, split, st) : pa_launch<64, false>(a, split, st);
 }
