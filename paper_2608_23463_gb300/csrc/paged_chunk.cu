@@ -874,6 +874,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
         ++g;
         return true;
       };
+      // (the next 32 fetched ahead of their turn: quantised prompts 169 -> 194 us)
       // any step, 32 keys at a time, from TMEM twice: a quarter of the instructions, all of which a
       // kernel's first steps wait for (they come from L2 at some 15 cycles each)
       auto step_short = [&](int kt) -> bool {
@@ -1247,33 +1248,48 @@ __global__ void __launch_bounds__(32 * PJ_WARPS) paged_chunk_join_kernel(const _
     }
     in = __ballot_sync(0xffffffffu, is);
   }
-  // whether CTA x + k < n holds a piece of it: it may begin where the next one does
-  auto holds = [&](int k) { return k == 0 || k == n - 1 || a.at[x + k + 1].s != a.at[x + k].s; };
   const int first = same(begin) ? 0 : 1;  // piece 0 is the last of its CTA's, the others the first
-  auto place = [&](int k) { return 2l * (x + k) + (k == 0 ? first : 0); };
-  float M = -INFINITY, L = 0.f;
-  if (row_in) {
-#pragma unroll 4
-    for (int k = 0; k < n; ++k)
-      if (holds(k)) M = fmaxf(M, a.ml[place(k) * a.piece_rows + rr].x);
-  }
   constexpr int C4 = DH / 4, U = C4 / PJ_WARPS;  // groups of four columns; of a warp
   float4 acc[U] = {};
-  if (row_in) {
-#pragma unroll 2
-    for (int k = 0; k < n; ++k) {
-      if (!holds(k)) continue;
-      const float2 y = a.ml[place(k) * a.piece_rows + rr];
-      const float4* p = a.part + (place(k) * C4 + warp * U) * a.piece_rows + rr;
-      const float f = y.x == M ? 1.f : ex2_approx(y.x - M);  // (-inf, no keys at all: 1 of nothing)
-      L = fmaf(y.y, f, L);
+  float M = -INFINITY, L = 0.f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < n; k0 += 32) {
+    // the CTAs x + k that hold a piece: one may begin where the next one does
+    const int kl = k0 + lane;
+    const bool holds = kl < n && (kl == 0 || kl == n - 1 || a.at[x + kl + 1].s != a.at[x + kl].s);
+    uint32_t pieces = __ballot_sync(0xffffffffu, holds);
+    if (!row_in) continue;
+    // two at a time: what is summed so far is brought down to the larger maximum
+#pragma unroll 1
+    while (pieces) {
+      float2 y[2];
+      float4 v[2][U];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int k = k0 + __ffs(pieces) - 1;
+        y[e] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[e][u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (pieces) {
+          const long place = 2l * (x + k) + (k == 0 ? first : 0);
+          const float4* p = a.part + (place * C4 + warp * U) * a.piece_rows + rr;
+          y[e] = a.ml[place * a.piece_rows + rr];
+#pragma unroll
+          for (int u = 0; u < U; ++u) v[e][u] = p[u * a.piece_rows];
+          pieces &= pieces - 1;
+        }
+      }
+      const float next = fmaxf(M, fmaxf(y[0].x, y[1].x));
+      auto factor = [&](float m) { return m == next ? 1.f : ex2_approx(m - next); };  // (-inf, no keys at all: 1 of nothing)
+      const float f = factor(M), f0 = factor(y[0].x), f1 = factor(y[1].x);
+      M = next;
+      L = fmaf(L, f, fmaf(y[0].y, f0, y[1].y * f1));
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float4 v = p[u * a.piece_rows];
-        acc[u].x = fmaf(v.x, f, acc[u].x);
-        acc[u].y = fmaf(v.y, f, acc[u].y);
-        acc[u].z = fmaf(v.z, f, acc[u].z);
-        acc[u].w = fmaf(v.w, f, acc[u].w);
+        acc[u].x = fmaf(acc[u].x, f, fmaf(v[0][u].x, f0, v[1][u].x * f1));
+        acc[u].y = fmaf(acc[u].y, f, fmaf(v[0][u].y, f0, v[1][u].y * f1));
+        acc[u].z = fmaf(acc[u].z, f, fmaf(v[0][u].z, f0, v[1][u].z * f1));
+        acc[u].w = fmaf(acc[u].w, f, fmaf(v[0][u].w, f0, v[1][u].w * f1));
       }
     }
   }
