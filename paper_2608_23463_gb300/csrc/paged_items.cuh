@@ -55,21 +55,23 @@ __host__ __device__ __forceinline__ PcSpan pc_span(const PcGeo& g, const PcSeq& 
   return s;
 }
 
-// An item weighs three times the keys that its last token sees, rounded up to those that a full
-// pair there would, and what an item costs beside them; with one tile twice.  The sum over the
-// pairs before u.
+// What an item weighs, about in 8 cycles: a key (that its last token sees, of those that a full pair
+// there would) 3, with one tile 2, half a step more for the last one's rest, and its beginning and end,
+// some 8000 cycles.  (At 700, 1300 and 2000: 64 mixed sequences 89.7, 87.7 and 88.9 us, four quantised
+// prompts 165, 170 and 175.)  The sum over the pairs before u.
 __host__ __device__ __forceinline__ long long pc_cum(const PcGeo& g, const PcSeq& q, int u) {
-  constexpr long long ITEM = 256;
+  constexpr int ITEM = 1000, REST = 64;
   const int P = pc_pairs(g, q);
   const int R = 2 * g.tpt, p0 = q.len - q.n;
   const long long cap = (long long)g.W + g.S + R;
-  auto sum = [&](int n) {
+  auto sum = [&](int n) {  // of keys
     int k = n;  // pairs that see no more than cap
     if (g.W > 0 && p0 + (long long)R * n > cap) k = cap > p0 ? (int)((unsigned)(cap - p0) / (unsigned)R) : 0;
-    return 3 * ((long long)k * p0 + R * ((long long)k * (k + 1) / 2) + (n - k) * cap + n * ITEM);
+    return (long long)k * p0 + R * ((long long)k * (k + 1) / 2) + (n - k) * cap + (long long)n * REST;
   };
-  const bool single = u == P && q.n - (P - 1) * (int)R <= g.tpt;
-  return single ? sum(u) - (sum(u) - sum(u - 1)) / 3 : sum(u);
+  const bool single = u == P && q.n - (P - 1) * R <= g.tpt;
+  const long long keys = sum(u);
+  return 3 * keys - (single ? keys - sum(u - 1) : 0) + (long long)u * ITEM;
 }
 
 __host__ __device__ __forceinline__ float pc_quotient(float a, float b) {
