@@ -3,7 +3,9 @@
 Training: queries and keys are normed and rotated, attention runs in a sliding window with sinks, and the backward
 comes back through both.  Serving: a ragged batch of prompts is appended to a paged cache, its rows come from the same
 windowed attention, and new tokens follow one by one from the pages, as a captured graph.  The tokens' rows agree with
-those of the training forward over the whole sequences.
+those of the training forward over the whole sequences.  The same in mixed steps: prompts come in pieces beside other
+sequences' single tokens, attention reads the pages for all of them in one call, and the cache is in bf16 or in 8 bits;
+at the end its rows are read back, and the windowed attention over them gives the rows that were served.
 
     python examples/local_attention.py
 """
@@ -93,6 +95,37 @@ def serve(block, x, prompts, L):
     return torch.stack(got, 1)
 
 
+def serve_in_pieces(block, x, prompts, piece, dtype):
+    """All rows of x [batch, L, D] in steps of up to ``piece`` tokens of a sequence that is in its prompt and one of
+    any other; and the rows that the windowed attention gives over what the cache holds in the end."""
+    B, L, _ = x.shape
+    pages = -(-L // PAGE)
+    cache = PagedKVCache(B, HEADS, KV, DH, PAGE, B * pages, pages, rope=block.rope, window=WINDOW, n_sink=SINKS,
+                         dtype=dtype)
+    cache.reserve([L] * B)
+    starts = lambda new: torch.tensor([0] + new, dtype=torch.int32).cumsum(0, dtype=torch.int32).cuda()
+    done, parts = [0] * B, [[] for _ in range(B)]
+    while min(done) < L:
+        new = [min(piece, n - d) if d < n else min(1, L - d) for n, d in zip(prompts, done)]
+        start = starts(new)
+        cache.advance(start)
+        q = cache.append(*block.project(torch.cat([x[b, d:d + n] for b, (d, n) in enumerate(zip(done, new))])),
+                         start=start)
+        a = cache.attend(q, start=start)
+        for p, rows in zip(parts, zip(q.split(new), a.split(new))):
+            p.append(rows)
+        done = [d + n for d, n in zip(done, new)]
+    q, a = (torch.cat([torch.cat([t[i] for t in p]) for p in parts]) for i in range(2))
+    k, v = cache.read(starts([L] * B), rows=B * L)
+    attn = WindowAttention(B, L, HEADS, KV, DH, window=WINDOW, n_sink=SINKS)
+    pf.pf_sync_check(torch.cuda.current_stream().cuda_stream)
+    return ((t @ block.w_o.T).view(B, L, D) for t in (a, attn.forward(q, k, v, train=False)))
+
+
+def far(got, want):
+    return float((got.float() - want.float()).abs().max() / want.float().abs().max())
+
+
 def main():
     torch.manual_seed(1)
     block, L, B = LocalBlock(), 384, 3
@@ -103,9 +136,13 @@ def main():
     got = serve(block, x.view(B, L, D), prompts, L)
     y = block.forward(x, L).view(B, L, D)
     want = torch.stack([y[b, n:n + got.shape[1]] for b, n in enumerate(prompts)])
-    diff = float((got.float() - want.float()).abs().max() / want.float().abs().max())
+    diff = far(got, want)
     print("loss %.3f -> %.3f; %d tokens a sequence served, largest difference from the forward %.1e"
           % (losses[0], losses[-1], got.shape[1], diff))
+    for dtype in (torch.bfloat16, torch.int8):
+        got, held = serve_in_pieces(block, x.view(B, L, D), prompts, 96, dtype)
+        print("in pieces, %s: largest difference from the rows of what the cache holds %.1e, from the forward %.1e"
+              % (dtype, far(got, held), far(got, y)))
     return losses, diff
 
 

@@ -102,19 +102,6 @@ __host__ __device__ __forceinline__ int pc_head(long long per, long long& y) {
   return h;
 }
 
-// The pair at weight y < pc_cum(P) of one head's pairs, and the step.  (The kernel's warps look for
-// the pair with all lanes.)
-__host__ __device__ __forceinline__ void pc_find(const PcGeo& g, const PcSeq& q, long long y, bool whole, int* u,
-                                                 int* s) {
-  int lo = 0, hi = pc_pairs(g, q);
-  while (hi - lo > 1) {
-    const int m = lo + (hi - lo) / 2;
-    if (pc_cum(g, q, m) <= y) lo = m; else hi = m;
-  }
-  *u = lo;
-  *s = pc_step(g, q, lo, y, whole);
-}
-
 // Where CTA c of n begins on a line of length T.
 __host__ __device__ __forceinline__ long long pc_share(long long T, int n, int c) {
   if (c >= n) return T;

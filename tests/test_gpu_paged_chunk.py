@@ -166,6 +166,15 @@ def test_pieces(quant, dh):
     chunk(c, [min(n, 1 + i % 3) for i, n in enumerate(length)], 15)
 
 
+@pytest.mark.parametrize("quant", [False, True])
+def test_many_sequences(quant):
+    """As many sequences as a call takes; and more than a warp's lanes share out at once."""
+    for B, i0 in ((2048, 40), (129, 50)):
+        length = [(29 * i) % 150 for i in range(B)]
+        c = make(length, 2, 1, 64, 16, i0, quant)
+        chunk(c, [min(n, (7 * i) % 4) for i, n in enumerate(length)], i0 + 1)
+
+
 def test_many_items():
     """Enough items that none is cut: 4 * 16 heads of 33 pairs."""
     c = make([2100] * 4, 16, 16, 64, 64, 16)

@@ -92,6 +92,19 @@ def test_chunk_workspace_stays_small():
     assert size(paged(max_pages=8), 100) == 0 and size(paged(), 0) == 0
 
 
+def test_newest_token_workspace():
+    """Of a quantised cache: what the call needs is what it takes, and a broken description has none."""
+    size = pf.pf_paged_attn_q8_workspace_size
+    d = paged(max_pages=1 << 20)
+    need = size(d)
+    assert need > 0
+    attn = lambda ws, n: pf.pf_paged_attn_q8(d, A, 256, cache(), exp(), A, 256, ws, n)
+    for ws, n in ((A, need - 1), (None, need), (A + 8, need)):
+        refused(pf.PF_ERR_WORKSPACE, lambda: attn(ws, n))
+    for kw in (dict(batch=0), dict(batch=2049), dict(dh=80), dict(page=24)):
+        assert size(paged(**kw)) == 0
+
+
 def test_python_refusals():
     torch = pytest.importorskip("torch")
     from types import SimpleNamespace
