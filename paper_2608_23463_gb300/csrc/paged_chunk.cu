@@ -559,9 +559,10 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
     if (warp == 0) {
       // ------------------------------------------------------------ producer (all lanes)
       const int nb = PC_T >> a.box_log, H = Q8 ? 1 : C::HALVES;
-      // lane: block of rows and half of their columns, or (Q8) the blocks' exponents
-      const int blk = lane / H & (nb - 1), half = lane % H;
-      const bool data = lane < nb * H, exps = Q8 && lane >= nb && lane < 2 * nb;
+      // lane, of 16 for K and 16 for V: block of rows and half of their columns, or (Q8) the blocks' exponents
+      const int sub = lane & 15, blk = sub / H & (nb - 1), half = sub % H;
+      const bool data = sub < nb * H, exps = Q8 && sub >= nb && sub < 2 * nb;
+      const int pages = PC_T / a.page, rest = PC_T - pages * a.page;  // that a step goes on by
       const uint32_t qbytes = (uint32_t)(a.geo.tpt * a.geo.g * 128 * C::HALVES);
       bool ok = wait_warp(shared, 0);
       PcWalk walk(a, ends);
@@ -575,14 +576,23 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
           mbar_arrive_warp(i_full(i));
         }
         if (m.s1 == 0) break;
-        auto page_of = [&](int s) -> int {  // the pool's page of the lane's block in step s
-          if (s >= m.s1 || !(data || exps)) return 0;
-          const int r = m.sp.tile(s) * PC_T + blk * a.box;
-          const bool seen = r <= m.sp.pl && (a.geo.W == 0 || r + a.box - 1 > m.sp.pf - a.geo.W || r < a.geo.S);
-          const long pg = seen ? pc_page(a, m.b, r) : -1;
-          return (int)(pg < 0 ? a.n_pages : pg);  // (past the end: zeros)
+        // The lane's block in a step: its row, the row's place in the table, and what stands there, which is
+        // looked up a step ahead and not looked at before its turn.  (With divisions, and looked at once, a
+        // step took the producer 2200 cycles and all else waited for it: 64 mixed sequences 89 us, 81 so.)
+        int r, at, row, entry = 0;
+        bool seen;
+        const int* const table = a.table + (long)m.b * a.max_pages;
+        auto place = [&](int s) {
+          r = m.sp.tile(s) * PC_T + blk * a.box;
+          at = r / a.page;
+          row = r - at * a.page;
         };
-        int pg_next = page_of(m.s0);
+        auto look = [&] {
+          seen = (data || exps) && r <= m.sp.pl && (a.geo.W == 0 || r + a.box - 1 > m.sp.pf - a.geo.W || r < a.geo.S);
+          if (seen) entry = table[at];
+        };
+        place(m.s0);
+        look();
         // the item's queries, as soon as those before them are done with and before a step's place is waited
         // for that only this item's steps free
         bool queries = false;
@@ -603,29 +613,48 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
             __syncwarp();
             queries = true;
           }
-          const int pg = pg_next, row = (m.sp.tile(s) * PC_T + blk * a.box) % a.page;
-          pg_next = page_of(s + 1);
+          int pg = entry;
+          const int from = row;
+          if (!seen || pg < 0 || pg >= a.n_pages) {
+            if (seen) set_dev_error(DEVERR_CAPACITY);
+            pg = (int)a.n_pages;  // (past the end: zeros)
+          }
+          if (s + 1 < m.s1) {
+            if (s + 1 == m.sp.ns) {
+              place(s + 1);
+            } else {
+              r += PC_T;
+              at += pages;
+              row += rest;
+              if (row >= a.page) {
+                row -= a.page;
+                ++at;
+              }
+            }
+            look();
+          }
 #pragma unroll 1
           for (int kv = 0; kv < 2 && ok; ++kv) {
             const CUtensorMap* const map = kv ? &tmV : &tmK;
+            const bool mine = lane >> 4 == kv;
             if (Q8) {
               constexpr int N = C::NR ? C::NR / 2 : 1;
               const uint32_t n = r_issued / 2, st = kv * N + n % N;
               ok = wait_warp(r_empty(st), ((n / N) & 1) ^ 1);
               if (!ok) break;
               // (exponents of blocks that no token sees, and of pages out of range: zeros)
-              const bool in = exps && pg < a.n_pages;
+              const bool in = mine && exps && pg < a.n_pages;
               const uint32_t edst = sbase + C::OFF_EXP + st * PC_T + blk * a.box;
-              if (exps && !in)
+              if (mine && exps && !in)
                 for (int i = 0; i < a.box; i += 16)
                   asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(edst + i), "r"(0) : "memory");
               const uint32_t ebytes = a.box * __popc(__ballot_sync(0xffffffffu, in));
               if (lane == 0) mbar_arrive_expect_tx(r_full(st), C::RAW + ebytes);
               __syncwarp();
-              if (data)
-                tma_load_4d(sbase + C::OFF_RAW + st * C::RAW + blk * a.box * DH, map, r_full(st), 0, row, m.h, pg);
+              if (mine && data)
+                tma_load_4d(sbase + C::OFF_RAW + st * C::RAW + blk * a.box * DH, map, r_full(st), 0, from, m.h, pg);
               else if (in)
-                bulk_load(edst, (kv ? a.Ve : a.Ke) + ((long)pg * a.geo.KV + m.h) * a.page + row, a.box, r_full(st));
+                bulk_load(edst, (kv ? a.Ve : a.Ke) + ((long)pg * a.geo.KV + m.h) * a.page + from, a.box, r_full(st));
               __syncwarp();
               ++r_issued;
             } else {
@@ -635,9 +664,9 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
               if (!ok) break;
               if (lane == 0) mbar_arrive_expect_tx(full, C::TILE);
               __syncwarp();
-              if (data)
+              if (mine && data)
                 tma_load_4d(sbase + (kv ? C::OFF_V : C::OFF_K) + st * C::TILE + half * C::HALF + blk * a.box * 128, map,
-                            full, 64 * half, row, m.h, pg);
+                            full, 64 * half, from, m.h, pg);
               __syncwarp();
               ++n;
             }
