@@ -281,27 +281,29 @@ __global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaAr
               cp_async16(ks + pa_k8<DH>(r, c), kb + j * 512);
               cp_async16(vs + pa_v8<DH>(r, c), vb + j * 512);
             }
-          } else
+          } else {
+#pragma unroll
+            for (int j = 0; j < PA_TILE * CPR / 32; ++j) {
+              const int e = j * 32 + lane, r = e / CPR, c = e % CPR;
+              const int j2 = row + r;
+              const bool in = ok && j2 < sp.n && (j2 >= sp.first || j2 < a.sinks);
+              const long src = in ? o + r * DH + c * 16 : 0;
+              cp_async16(ks + pa_k8<DH>(r, c), kb + src, in);
+              cp_async16(vs + pa_v8<DH>(r, c), vb + src, in);
+            }
+          }
+          // (those of rows that it does not see too: they are passed over where they are read)
+          if (lane < 2) cp_async16(wr + C::EXP + (i % C::STAGES) * 32 + 16 * lane, (lane ? a.Ve : a.Ke) + at, ok);
+        } else {
 #pragma unroll
           for (int j = 0; j < PA_TILE * CPR / 32; ++j) {
             const int e = j * 32 + lane, r = e / CPR, c = e % CPR;
             const int j2 = row + r;
             const bool in = ok && j2 < sp.n && (j2 >= sp.first || j2 < a.sinks);
-            const long src = in ? o + r * DH + c * 16 : 0;
-            cp_async16(ks + pa_k8<DH>(r, c), kb + src, in);
-            cp_async16(vs + pa_v8<DH>(r, c), vb + src, in);
+            const long src = in ? o + r * DH + c * 8 : 0;
+            cp_async16(ks + (r * CPR + (c ^ ((r & 1) << 2))) * 16, a.K + src, in);
+            cp_async16(vs + (r * CPR + (c ^ (r & 7))) * 16, a.V + src, in);
           }
-          // (those of rows that it does not see too: they are passed over where they are read)
-          if (lane < 2) cp_async16(wr + C::EXP + (i % C::STAGES) * 32 + 16 * lane, (lane ? a.Ve : a.Ke) + at, ok);
-        } else
-#pragma unroll
-        for (int j = 0; j < PA_TILE * CPR / 32; ++j) {
-          const int e = j * 32 + lane, r = e / CPR, c = e % CPR;
-          const int j2 = row + r;
-          const bool in = ok && j2 < sp.n && (j2 >= sp.first || j2 < a.sinks);
-          const long src = in ? o + r * DH + c * 8 : 0;
-          cp_async16(ks + (r * CPR + (c ^ ((r & 1) << 2))) * 16, a.K + src, in);
-          cp_async16(vs + (r * CPR + (c ^ (r & 7))) * 16, a.V + src, in);
         }
       }
       cp_commit();

@@ -79,7 +79,7 @@ struct PcArgs {
   int page, max_pages, box, box_log;  // box: rows of a TMA box, 2^box_log
   long n_pages;
   int G;           // CTAs
-  int whole, few;  // items to a CTA from which none is cut (whole: none ever); steps' weight to a CTA at least
+  int few;         // weight to a CTA at least
   int long_item;   // steps from which an item's unmasked ones take the long form
   float sl2;       // log2(e) / sqrt(dh), of the tiles' keys
   const bf16* q;
@@ -300,11 +300,10 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
     *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(acc[c] / l, acc[c + 1] / l);
 }
 
-// Weight and items of a sequence; any_bad becomes 1 if it cannot be.
+// Weight of a sequence; any_bad becomes 1 if it cannot be.
 struct PcLoad {
   PcSeq q;
   long long weight;
-  int items;
   __device__ __forceinline__ PcLoad(const PcArgs& a, int b, int* any_bad) {
     bool bad;
     q = pc_seq(a, b, &bad);
@@ -313,9 +312,7 @@ struct PcLoad {
       *any_bad = 1;
       q.n = 0;
     }
-    const int P = pc_pairs(a.geo, q);
-    weight = q.n > 0 ? a.geo.KV * pc_cum(a.geo, q, P) : 0;
-    items = P * a.geo.KV;
+    weight = q.n > 0 ? a.geo.KV * pc_cum(a.geo, q, pc_pairs(a.geo, q)) : 0;
   }
 };
 
@@ -342,49 +339,37 @@ struct PcRoom {
 constexpr int PC_FEW = 128;
 static_assert((PC_FEW + 1) * 8 + PC_FEW * 12 <= 4096, "a room for each");
 template <int THREADS>
-__device__ __noinline__ void pc_totals(const PcArgs& a, void* room, long long* items, int* any_bad) {
+__device__ __noinline__ void pc_totals(const PcArgs& a, void* room, int* any_bad) {
   __shared__ long long wsum[THREADS / 32];
-  __shared__ int wit[THREADS / 32];
   const PcRoom m(room, a.geo.B);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = a.geo.B;
-  long long T = 0, n = 0;
+  long long T = 0;
   for (int b0 = 0; b0 < B; b0 += THREADS) {
     const int b = b0 + tid;
     long long u = 0;
-    int it = 0;
     if (b < B) {
       const PcLoad x(a, b, any_bad);
       m.seq[b] = x.q;
       u = x.weight;
-      it = x.items;
     }
     const long long v = warp_scan(u);
-    it = __reduce_add_sync(0xffffffffu, it);
-    if (lane == 31) {
-      wsum[warp] = v;
-      wit[warp] = it;
-    }
+    if (lane == 31) wsum[warp] = v;
     __syncthreads();
     long long before = 0, all = 0;
 #pragma unroll 1
     for (int w = 0; w < THREADS / 32; ++w) {
       if (w < warp) before += wsum[w];
       all += wsum[w];
-      n += wit[w];
     }
     if (b < B) m.pre[b] = T + before + v - u;
     T += all;
     __syncthreads();
   }
-  if (tid == 0) {
-    m.pre[B] = T;
-    *items = n;
-  }
+  if (tid == 0) m.pre[B] = T;
   __syncthreads();
 }
 
-__device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, long long items, int warp, PcEnds& ends,
-                                             int* any_bad) {
+__device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, int warp, PcEnds& ends, int* any_bad) {
   // (few sequences: each of the two warps in a room of its own)
   const PcRoom m(static_cast<char*>(room) + (a.geo.B <= PC_FEW ? warp * 4096 : 0), a.geo.B);
   const int lane = threadIdx.x & 31, B = a.geo.B;
@@ -403,7 +388,6 @@ __device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, long l
   if (B <= PC_FEW) {
     const int per = (B + 31) / 32;
     long long u = 0;
-    int it = 0;
 #pragma unroll 1
     for (int i = 0; i < per; ++i) {
       const int b = lane * per + i;
@@ -412,20 +396,17 @@ __device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, long l
       m.seq[b] = x.q;
       m.pre[b] = u;
       u += x.weight;
-      it += x.items;
     }
     const long long v = warp_scan(u) - u;
 #pragma unroll 1
     for (int b = lane * per; b < min(B, (lane + 1) * per); ++b) m.pre[b] += v;
     if (lane == 31) m.pre[B] = v + u;
-    items = __reduce_add_sync(0xffffffffu, it);
     __syncwarp();
   }
   PcSeq q{0, 0, 0};
   const long long T = m.pre[B];
-  const bool whole = a.whole == 0 || items >= (long long)a.whole * a.G;
   int n = a.G;
-  if (!whole && T < (long long)a.few * n) n = max(1, (int)T / a.few);
+  if (T < (long long)a.few * n) n = max(1, (int)T / a.few);
   const int c = min((int)blockIdx.x + warp, n);
   PcAt r{B, 0, 0, 0};
   long long y = pc_share(T, n, c);
@@ -436,18 +417,7 @@ __device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, long l
     const int P = pc_pairs(a.geo, q);
     r.h = pc_head(pc_cum(a.geo, q, P), y);
     r.u = find(P, [&](int i) { return pc_cum(a.geo, q, i) <= y; });
-    r.s = pc_step(a.geo, q, r.u, y, whole);
-    if (r.s >= pc_span(a.geo, q, r.u).steps) {  // the next item's beginning
-      r.s = 0;
-      if (++r.u == P) {
-        r.u = 0;
-        if (++r.h == a.geo.KV) {
-          r.h = 0;
-          do q = ++r.b < B ? pc_seq(a, r.b) : PcSeq{0, 0, 0};
-          while (r.b < B && q.n == 0);
-        }
-      }
-    }
+    r.s = pc_step(a.geo, q, r.u, y);
   }
   if (lane == 0) {
     ends.at[warp] = r;
@@ -466,7 +436,6 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   __shared__ PcEnds ends;
   __shared__ PcItem slot[2];
-  __shared__ long long items;
   __shared__ int any_bad;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -537,7 +506,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
   // the join's launch may begin: it waits for this grid to end, and all of its CTAs are running
   if (a.at) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   void* const room = smem + C::OFF_K;
-  if (a.geo.B > PC_FEW) pc_totals<C::THREADS>(a, room, &items, &any_bad);
+  if (a.geo.B > PC_FEW) pc_totals<C::THREADS>(a, room, &any_bad);
   uint32_t k_issued = 0, v_issued = 0, r_issued = 0, q_issued = 0;
   // Warp 0 walks the items and writes them down, two ahead at most, for the other warps.
   // item n: bounded, false where it does not come; a copy of it is kept, its place is free again
@@ -552,7 +521,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_CTRL));
     if (warp < 2) {
-      pc_share_out(a, room, items, warp, ends, &any_bad);
+      pc_share_out(a, room, warp, ends, &any_bad);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the totals lie where the rings will be
       mbar_arrive_warp(shared);
     }
@@ -1414,7 +1383,6 @@ cudaError_t paged_chunk(const Paged& c, long rows, const bf16* q, long ldq, cons
   a.box = std::min(PC_T, c.page & -c.page);
   while (1 << a.box_log < a.box) ++a.box_log;
   a.G = p.G;
-  a.whole = p.split ? 8 : 0;
   a.few = 400;  // (about a step and a half; three short sequences, up to 7 tokens on 1000 rows: 13.2 us so, 15.1 at 1000)
   a.long_item = 8;
   a.sl2 = (c.Ke ? 1 << PQ_DOWN : 1) * 1.4426950408889634f / sqrtf((float)c.dh);

@@ -82,13 +82,13 @@ __host__ __device__ __forceinline__ float pc_quotient(float a, float b) {
 #endif
 }
 
-// The step at weight y of pair u (whole: items are not cut, a place inside one is its end).  Neither
-// this nor pc_share has to be exact, only the same for whoever asks, and to grow with y or c: a
-// division of 64-bit numbers, cold, took 1000 cycles of a call's first 20000.
-__host__ __device__ __forceinline__ int pc_step(const PcGeo& g, const PcSeq& q, int u, long long y, bool whole) {
+// The step at weight y of pair u.  Neither this nor pc_share has to be exact, only the same for
+// whoever asks, and to grow with y or c: a division of 64-bit numbers, cold, took 1000 cycles of a
+// call's first 20000.
+__host__ __device__ __forceinline__ int pc_step(const PcGeo& g, const PcSeq& q, int u, long long y) {
   const long long at = pc_cum(g, q, u);
   const int steps = pc_span(g, q, u).steps;
-  if (y <= at || whole) return y > at ? steps : 0;
+  if (y <= at) return 0;
   const int s = (int)(pc_quotient((float)(y - at), (float)(pc_cum(g, q, u + 1) - at)) * (float)steps);
   return s < steps ? s : steps - 1;
 }
