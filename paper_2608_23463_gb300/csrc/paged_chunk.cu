@@ -64,7 +64,7 @@ struct PcCfg {
   static constexpr uint32_t OFF_EXP = OFF_RAW + NR * RAW, OFF_BAR = OFF_EXP + NR * PC_T;
   static constexpr uint32_t SMEM = OFF_BAR + 512 + 1024;
   static_assert(SMEM <= 227 * 1024, "shared memory");
-  static_assert((PC_MAX_B + 1) * 8 + PC_MAX_B * 12 <= (NK + NV) * TILE, "the totals lie in the rings at first");
+  static_assert((PC_MAX_B + 1) * 8 + PC_MAX_B * 20 <= (NK + NV) * TILE, "the totals lie in the rings at first");
   // TMEM columns of tile w: S at 128 w, O and P
   static constexpr bool ALIAS = DH == 128;
   static constexpr float SCALE = Q8 ? 1 << PQ_DOWN : 1;  // the tiles hold so much less than the values
@@ -300,7 +300,7 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
     *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(acc[c] / l, acc[c + 1] / l);
 }
 
-// Weight of a sequence; any_bad becomes 1 if it cannot be.
+// Weight of a head of a sequence's; any_bad becomes 1 if it cannot be.
 struct PcLoad {
   PcSeq q;
   long long weight;
@@ -312,7 +312,7 @@ struct PcLoad {
       *any_bad = 1;
       q.n = 0;
     }
-    weight = q.n > 0 ? a.geo.KV * pc_cum(a.geo, q, pc_pairs(a.geo, q)) : 0;
+    weight = q.n > 0 ? pc_cum(a.geo, q, pc_pairs(a.geo, q)) : 0;
   }
 };
 
@@ -325,19 +325,20 @@ __device__ __forceinline__ long long warp_scan(long long v) {  // sums up to and
   return v;
 }
 
-// The CTA's part of the line, and its entry in the pieces' index.  room: for B + 1 totals and B
-// sequences.  (Each CTA works it out for itself: a kernel before this one would cost a launch.)
+// The CTA's part of the line, and its entry in the pieces' index.  room: for B + 1 totals, B
+// heads' weights and sequences.  (Each CTA works it out for itself: a kernel before this one would cost a launch.)
 // pc_totals: more than PC_FEW sequences, by all of a CTA's threads.  pc_share_out: warp 0 the CTA's
 // beginning, warp 1 the next one's.  Both are on the way to a call's first load, where every
 // instruction comes from L2, to all SMs at once: 12000 cycles in their first form, by one thread.
 struct PcRoom {
   long long* pre;  // pre[b]: weight of the sequences before b
+  long long* head;  // of a head of each
   PcSeq* seq;
   __device__ __forceinline__ PcRoom(void* room, int B)
-      : pre(static_cast<long long*>(room)), seq(reinterpret_cast<PcSeq*>(pre + B + 1)) {}
+      : pre(static_cast<long long*>(room)), head(pre + B + 1), seq(reinterpret_cast<PcSeq*>(head + B)) {}
 };
 constexpr int PC_FEW = 128;
-static_assert((PC_FEW + 1) * 8 + PC_FEW * 12 <= 4096, "a room for each");
+static_assert((PC_FEW + 1) * 8 + PC_FEW * 20 <= 4096, "a room for each");
 template <int THREADS>
 __device__ __noinline__ void pc_totals(const PcArgs& a, void* room, int* any_bad) {
   __shared__ long long wsum[THREADS / 32];
@@ -350,7 +351,8 @@ __device__ __noinline__ void pc_totals(const PcArgs& a, void* room, int* any_bad
     if (b < B) {
       const PcLoad x(a, b, any_bad);
       m.seq[b] = x.q;
-      u = x.weight;
+      m.head[b] = x.weight;
+      u = a.geo.KV * x.weight;
     }
     const long long v = warp_scan(u);
     if (lane == 31) wsum[warp] = v;
@@ -394,8 +396,9 @@ __device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, int wa
       if (b >= B) break;
       const PcLoad x(a, b, any_bad);
       m.seq[b] = x.q;
+      m.head[b] = x.weight;
       m.pre[b] = u;
-      u += x.weight;
+      u += a.geo.KV * x.weight;
     }
     const long long v = warp_scan(u) - u;
 #pragma unroll 1
@@ -415,9 +418,11 @@ __device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, int wa
     y -= m.pre[r.b];
     q = m.seq[r.b];
     const int P = pc_pairs(a.geo, q);
-    r.h = pc_head(pc_cum(a.geo, q, P), y);
+    r.h = pc_head(m.head[r.b], y);
     r.u = find(P, [&](int i) { return pc_cum(a.geo, q, i) <= y; });
-    r.s = pc_step(a.geo, q, r.u, y);
+    // (pc_cum's copies are fetched one by one: lane 0 the weight before the pair, lane 1 with it)
+    const long long w = pc_cum(a.geo, q, r.u + (lane & 1)), w0 = __shfl_sync(0xffffffffu, w, 0);
+    r.s = pc_step(pc_span(a.geo, q, r.u).steps, y - w0, __shfl_sync(0xffffffffu, w, 1) - w0);
   }
   if (lane == 0) {
     ends.at[warp] = r;

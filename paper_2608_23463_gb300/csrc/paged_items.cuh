@@ -82,14 +82,12 @@ __host__ __device__ __forceinline__ float pc_quotient(float a, float b) {
 #endif
 }
 
-// The step at weight y of pair u.  Neither this nor pc_share has to be exact, only the same for
-// whoever asks, and to grow with y or c: a division of 64-bit numbers, cold, took 1000 cycles of a
-// call's first 20000.
-__host__ __device__ __forceinline__ int pc_step(const PcGeo& g, const PcSeq& q, int u, long long y) {
-  const long long at = pc_cum(g, q, u);
-  const int steps = pc_span(g, q, u).steps;
-  if (y <= at) return 0;
-  const int s = (int)(pc_quotient((float)(y - at), (float)(pc_cum(g, q, u + 1) - at)) * (float)steps);
+// The step at weight y of a pair that weighs so much.  Neither this nor pc_share has to be exact, only
+// the same for whoever asks, and to grow with y or c: a division of 64-bit numbers, cold, took 1000
+// cycles of a call's first 20000.
+__host__ __device__ __forceinline__ int pc_step(int steps, long long y, long long weight) {
+  if (y <= 0) return 0;
+  const int s = (int)(pc_quotient((float)y, (float)weight) * (float)steps);
   return s < steps ? s : steps - 1;
 }
 
