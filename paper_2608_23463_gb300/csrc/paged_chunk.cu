@@ -77,6 +77,7 @@ struct PcArgs {
   const int *start, *len, *table;
   long rows;
   int page, max_pages, box, box_log;  // box: rows of a TMA box, 2^box_log
+  int step_pages, step_rows;          // that a step of PC_T rows is
   long n_pages;
   int G;           // CTAs
   int few;         // weight to a CTA at least
@@ -312,7 +313,8 @@ struct PcLoad {
       *any_bad = 1;
       q.n = 0;
     }
-    weight = q.n > 0 ? pc_cum(a.geo, q, pc_pairs(a.geo, q)) : 0;
+    const int P = pc_pairs(a.geo, q);
+    weight = P > 0 ? pc_cum(a.geo, q, P, P) : 0;
   }
 };
 
@@ -419,9 +421,9 @@ __device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, int wa
     q = m.seq[r.b];
     const int P = pc_pairs(a.geo, q);
     r.h = pc_head(m.head[r.b], y);
-    r.u = find(P, [&](int i) { return pc_cum(a.geo, q, i) <= y; });
+    r.u = find(P, [&](int i) { return pc_cum(a.geo, q, i, P) <= y; });
     // (pc_cum's copies are fetched one by one: lane 0 the weight before the pair, lane 1 with it)
-    const long long w = pc_cum(a.geo, q, r.u + (lane & 1)), w0 = __shfl_sync(0xffffffffu, w, 0);
+    const long long w = pc_cum(a.geo, q, r.u + (lane & 1), P), w0 = __shfl_sync(0xffffffffu, w, 0);
     r.s = pc_step(pc_span(a.geo, q, r.u).steps, y - w0, __shfl_sync(0xffffffffu, w, 1) - w0);
   }
   if (lane == 0) {
@@ -536,7 +538,6 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
       // lane, of 16 for K and 16 for V: block of rows and half of their columns, or (Q8) the blocks' exponents
       const int sub = lane & 15, blk = sub / H & (nb - 1), half = sub % H;
       const bool data = sub < nb * H, exps = Q8 && sub >= nb && sub < 2 * nb;
-      const int pages = PC_T / a.page, rest = PC_T - pages * a.page;  // that a step goes on by
       const uint32_t qbytes = (uint32_t)(a.geo.tpt * a.geo.g * 128 * C::HALVES);
       bool ok = wait_warp(shared, 0);
       PcWalk walk(a, ends);
@@ -558,7 +559,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
         const int* const table = a.table + (long)m.b * a.max_pages;
         auto place = [&](int s) {
           r = m.sp.tile(s) * PC_T + blk * a.box;
-          at = r / a.page;
+          at = (int)((unsigned)r / (unsigned)a.page);
           row = r - at * a.page;
         };
         auto look = [&] {
@@ -598,8 +599,8 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
               place(s + 1);
             } else {
               r += PC_T;
-              at += pages;
-              row += rest;
+              at += a.step_pages;
+              row += a.step_rows;
               if (row >= a.page) {
                 row -= a.page;
                 ++at;
@@ -1387,6 +1388,8 @@ cudaError_t paged_chunk(const Paged& c, long rows, const bf16* q, long ldq, cons
   a.n_pages = c.n_pages;
   a.box = std::min(PC_T, c.page & -c.page);
   while (1 << a.box_log < a.box) ++a.box_log;
+  a.step_pages = PC_T / c.page;
+  a.step_rows = PC_T % c.page;
   a.G = p.G;
   a.few = 400;  // (about a step and a half; three short sequences, up to 7 tokens on 1000 rows: 13.2 us so, 15.1 at 1000)
   a.long_item = 8;

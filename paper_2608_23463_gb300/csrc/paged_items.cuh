@@ -39,8 +39,8 @@ struct PcSpan {
 
 __host__ __device__ __forceinline__ int pc_tiles(int rows) { return rows / PC_T + (rows % PC_T != 0); }
 __host__ __device__ __forceinline__ int pc_pairs(const PcGeo& g, const PcSeq& q) {
-  const int R = 2 * g.tpt;
-  return q.n / R + (q.n % R != 0);
+  const unsigned R = 2 * g.tpt;
+  return (int)((q.n + (R - 1)) / R);  // (0 <= n: unsigned, which takes fewer instructions)
 }
 
 __host__ __device__ __forceinline__ PcSpan pc_span(const PcGeo& g, const PcSeq& q, int u) {
@@ -59,9 +59,8 @@ __host__ __device__ __forceinline__ PcSpan pc_span(const PcGeo& g, const PcSeq& 
 // there would) 3, with one tile 2, half a step more for the last one's rest, and its beginning and end,
 // some 8000 cycles.  (At 700, 1300 and 2000: 64 mixed sequences 89.7, 87.7 and 88.9 us, four quantised
 // prompts 165, 170 and 175.)  The sum over the pairs before u.
-__host__ __device__ __forceinline__ long long pc_cum(const PcGeo& g, const PcSeq& q, int u) {
+__host__ __device__ __forceinline__ long long pc_cum(const PcGeo& g, const PcSeq& q, int u, int P) {
   constexpr int ITEM = 1000, REST = 64;
-  const int P = pc_pairs(g, q);
   const int R = 2 * g.tpt, p0 = q.len - q.n;
   const long long cap = (long long)g.W + g.S + R;
   auto sum = [&](int n) {  // of keys
