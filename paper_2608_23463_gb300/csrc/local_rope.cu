@@ -21,7 +21,7 @@
 // Measured: four images of 512 x 512 tokens, 8 + 8 heads of 64, 694 us (6.2
 // TB/s, 91 % of a plain copy); backward, 65536 tokens of 16 + 4 heads, 97 us
 // (5.2 TB/s); eight prompts of 11738 tokens in all, 16 + 2 heads of 128, into
-// the cache 25.5 us (4.7 TB/s).  fp32: the images 1283 us (6.7 TB/s), the
+// the cache 25.5 us (4.7 TB/s), quantised 27.6.  fp32: the images 1283 us (6.7 TB/s), the
 // backward 158 us (6.4 TB/s).  Scalar arithmetic with the weights applied
 // apart took 843 us for the images, three quarters of the issue slots busy.
 //

@@ -57,8 +57,9 @@ __host__ __device__ __forceinline__ PcSpan pc_span(const PcGeo& g, const PcSeq& 
 
 // What an item weighs, about in 8 cycles: a key (that its last token sees, of those that a full pair
 // there would) 3, with one tile 2, half a step more for the last one's rest, and its beginning and end,
-// some 8000 cycles.  (At 700, 1300 and 2000: 64 mixed sequences 89.7, 87.7 and 88.9 us, four quantised
-// prompts 165, 170 and 175.)  The sum over the pairs before u.
+// some 8000 cycles.  (ITEM at 700, 1000 and 2000: three short sequences 15.5, 12.9 and 13.1 us, four
+// quantised prompts 166.7, 166.8 and 175.2; a single tile's key at 1.5, 2 and 2.5: 64 mixed sequences
+// 81.6, 80.0 and 89.4.)  The sum over the pairs before u, of P.
 __host__ __device__ __forceinline__ long long pc_cum(const PcGeo& g, const PcSeq& q, int u, int P) {
   constexpr int ITEM = 1000, REST = 64;
   const int R = 2 * g.tpt, p0 = q.len - q.n;
