@@ -1387,7 +1387,8 @@ cudaError_t paged_chunk(const Paged& c, long rows, const bf16* q, long ldq, cons
   launched.mark();
   const PcPlan p = pc_plan(c, rows);
   PcArgs a{};
-  a.geo = {c.B, c.KV, c.H / c.KV, p.tpt, c.window, c.sinks};
+  // (no sequence is as long as the widest windows: none, and sums with it stay within an int)
+  a.geo = {c.B, c.KV, c.H / c.KV, p.tpt, c.window < PC_LONGEST ? c.window : 0, c.sinks};
   a.start = start; a.len = c.len; a.table = c.table;
   a.rows = rows;
   a.page = c.page; a.max_pages = c.max_pages;

@@ -83,6 +83,27 @@ def test_lengths(quant, H, KV, dh, page, new, before):
 
 
 @pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("page,window,n_sink", [(144, 0, 0), (144, 300, 20), (256, 0, 0), (400, 150, 200), (80, 0, 0), (112, 500, 3),
+                                                (1024, 0, 0)])
+@pytest.mark.parametrize("KV,dh", [(2, 128), (4, 64)])
+def test_pages_of_other_lengths(quant, page, window, n_sink, KV, dh):
+    """Pages longer than a step, and such that neither fits the other."""
+    new, before = [3, 1, 140, 1, 30], [1500, 2 * page, page - 70, page - 1, 897]
+    c = make([a + b for a, b in zip(new, before)], 8, KV, dh, page, 60, quant, window=window, n_sink=n_sink)
+    chunk(c, new, 61)
+
+
+@pytest.mark.parametrize("quant", [False, True])
+def test_sequences_that_share_pages(quant):
+    """A prompt's pages in the tables of several sequences."""
+    c = make([500, 480, 300], 8, 2, 64, 16, 62, quant, spare=0)
+    c.table[1, :20] = c.table[0, :20]
+    c.table[2, :18] = c.table[0, :18]
+    c.len.copy_(torch.tensor([500, 480, 290], dtype=I32))
+    chunk(c, [4, 120, 2], 63)
+
+
+@pytest.mark.parametrize("quant", [False, True])
 @pytest.mark.parametrize("window,n_sink", [(1, 0), (1, 1), (5, 3), (16, 16), (64, 100), (1000, 2), (333, 17), (200, 3000),
                                            (129, (1 << 31) - 1), ((1 << 31) - 1, 5)])
 @pytest.mark.parametrize("KV,dh,page", [(2, 128, 32), (8, 64, 16)])
