@@ -107,6 +107,14 @@ __device__ __forceinline__ float ex2_approx(float x) {
   return y;
 }
 
+// 16 bytes, or as many zeros, and the arrival of a thread's copies at a barrier that counts it.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool full) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(full ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
 // mbar_wait_warp with the common case, a phase that has completed, up front.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
   if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
@@ -502,7 +510,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
       mbar_init(v_empty(i), 2);  // one arrival per tile
     }
     for (int i = 0; i < C::NR; ++i) {
-      mbar_init(r_full(i), 1);
+      mbar_init(r_full(i), 1 + 32);  // (the copies of the exponents)
       mbar_init(r_empty(i), C::CONV);
     }
     fence_barrier_init();
@@ -541,9 +549,10 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
     if (warp == 0) {
       // ------------------------------------------------------------ producer (all lanes)
       const int nb = PC_T >> a.box_log, H = Q8 ? 1 : C::HALVES;
-      // lane, of 16 for K and 16 for V: block of rows and half of their columns, or (Q8) the blocks' exponents
-      const int sub = lane & 15, blk = sub / H & (nb - 1), half = sub % H;
-      const bool data = sub < nb * H, exps = Q8 && sub >= nb && sub < 2 * nb;
+      // lane, of 16 for K and 16 for V: a block of rows and half of its columns; Q8: 16 rows, of whose block
+      // the first of its lanes has the data copied, and each 16 exponents
+      const int sub = lane & 15, blk = Q8 ? (sub & 7) * 16 >> a.box_log : sub / H & (nb - 1), half = sub % H;
+      const bool exps = Q8 && sub < 8, data = Q8 ? exps && (sub * 16 & (a.box - 1)) == 0 : sub < nb * H;
       const uint32_t qbytes = (uint32_t)(a.geo.tpt * a.geo.g * 128 * C::HALVES);
       bool ok = wait_warp(shared, 0);
       PcWalk walk(a, ends);
@@ -623,19 +632,19 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
               const uint32_t n = r_issued / 2, st = kv * N + n % N;
               ok = wait_warp(r_empty(st), ((n / N) & 1) ^ 1);
               if (!ok) break;
-              // (exponents of blocks that no token sees, and of pages out of range: zeros)
-              const bool in = mine && exps && pg < a.n_pages;
-              const uint32_t edst = sbase + C::OFF_EXP + st * PC_T + blk * a.box;
-              if (mine && exps && !in)
-                for (int i = 0; i < a.box; i += 16)
-                  asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(edst + i), "r"(0) : "memory");
-              const uint32_t ebytes = a.box * __popc(__ballot_sync(0xffffffffu, in));
-              if (lane == 0) mbar_arrive_expect_tx(r_full(st), C::RAW + ebytes);
+              if (lane == 0) mbar_arrive_expect_tx(r_full(st), C::RAW);
               __syncwarp();
               if (mine && data)
                 tma_load_4d(sbase + C::OFF_RAW + st * C::RAW + blk * a.box * DH, map, r_full(st), 0, from, m.h, pg);
-              else if (in)
-                bulk_load(edst, (kv ? a.Ve : a.Ke) + ((long)pg * a.geo.KV + m.h) * a.page + from, a.box, r_full(st));
+              // one instruction for all of a tile's exponents (a bulk copy to a block took 130 cycles, as its data's
+              // does); those of blocks that no token sees, and of pages out of range: zeros
+              if (mine && exps) {
+                const bool in = pg < a.n_pages;
+                const signed char* e = kv ? a.Ve : a.Ke;
+                cp_async16(sbase + C::OFF_EXP + st * PC_T + sub * 16,
+                           in ? e + ((long)pg * a.geo.KV + m.h) * a.page + from + (sub * 16 & (a.box - 1)) : e, in);
+              }
+              cp_async_arrive(r_full(st));
               __syncwarp();
               ++r_issued;
             } else {
