@@ -623,40 +623,48 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
             }
             look();
           }
+          if constexpr (Q8) {
+            // K's and V's bytes and exponents; at dh = 64 both at once, which at dh = 128, with a stage each,
+            // would keep K's waiting for V's to be converted
+            constexpr int N = C::NR / 2;
+            constexpr bool BOTH = N > 1;
 #pragma unroll 1
-          for (int kv = 0; kv < 2 && ok; ++kv) {
-            const CUtensorMap* const map = kv ? &tmV : &tmK;
-            const bool mine = lane >> 4 == kv;
-            if (Q8) {
-              constexpr int N = C::NR ? C::NR / 2 : 1;
-              const uint32_t n = r_issued / 2, st = kv * N + n % N;
-              ok = wait_warp(r_empty(st), ((n / N) & 1) ^ 1);
+            for (int kv = 0; kv < (BOTH ? 1 : 2); ++kv) {
+              const uint32_t ring = r_issued / 2 % N, par = ((r_issued / 2 / N) & 1) ^ 1;
+              ok = wait_warp(r_empty(kv * N + ring), par) && (!BOTH || wait_warp(r_empty(N + ring), par));
               if (!ok) break;
-              if (lane == 0) mbar_arrive_expect_tx(r_full(st), C::RAW);
+              const int own = BOTH ? lane >> 4 : kv;
+              const uint32_t st = own * N + ring;
+              if (lane == 0 || (BOTH && lane == 16)) mbar_arrive_expect_tx(r_full(st), C::RAW);
               __syncwarp();
-              if (mine && data)
-                tma_load_4d(sbase + C::OFF_RAW + st * C::RAW + blk * a.box * DH, map, r_full(st), 0, from, m.h, pg);
+              if (data && own == lane >> 4)
+                tma_load_4d(sbase + C::OFF_RAW + st * C::RAW + blk * a.box * DH, own ? &tmV : &tmK, r_full(st), 0, from, m.h,
+                            pg);
               // one instruction for all of a tile's exponents (a bulk copy to a block took 130 cycles, as its data's
               // does); those of blocks that no token sees, and of pages out of range: zeros
-              if (mine && exps) {
+              if (exps && own == lane >> 4) {
                 const bool in = pg < a.n_pages;
-                const signed char* e = kv ? a.Ve : a.Ke;
+                const signed char* e = own ? a.Ve : a.Ke;
                 cp_async16(sbase + C::OFF_EXP + st * PC_T + sub * 16,
                            in ? e + ((long)pg * a.geo.KV + m.h) * a.page + from + (sub * 16 & (a.box - 1)) : e, in);
               }
-              cp_async_arrive(r_full(st));
+              cp_async_arrive(r_full(kv * N + ring));
+              if (BOTH) cp_async_arrive(r_full(N + ring));
               __syncwarp();
-              ++r_issued;
-            } else {
+              r_issued += BOTH ? 2 : 1;
+            }
+          } else {
+#pragma unroll 1
+            for (int kv = 0; kv < 2; ++kv) {
               uint32_t& n = kv ? v_issued : k_issued;
               const uint32_t ring = kv ? C::NV : C::NK, st = n % ring, full = kv ? v_full(st) : k_full(st);
               ok = wait_warp(kv ? v_empty(st) : k_empty(st), ((n / ring) & 1) ^ 1);
               if (!ok) break;
               if (lane == 0) mbar_arrive_expect_tx(full, C::TILE);
               __syncwarp();
-              if (mine && data)
-                tma_load_4d(sbase + (kv ? C::OFF_V : C::OFF_K) + st * C::TILE + half * C::HALF + blk * a.box * 128, map,
-                            full, 64 * half, from, m.h, pg);
+              if (data && lane >> 4 == kv)
+                tma_load_4d(sbase + (kv ? C::OFF_V : C::OFF_K) + st * C::TILE + half * C::HALF + blk * a.box * 128,
+                            kv ? &tmV : &tmK, full, 64 * half, from, m.h, pg);
               __syncwarp();
               ++n;
             }
@@ -1148,7 +1156,9 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
         for (int kv = 0; kv < 2; ++kv) {
           const uint32_t n = kv ? C::NV : C::NK, st = kv * NR + G % NR, dst = G % n;
           const uint32_t full = kv ? v_full(dst) : k_full(dst), empty = kv ? v_empty(dst) : k_empty(dst);
-          ok = ok && wait_warp(empty, ((G / n) & 1) ^ 1) && wait_warp(r_full(st), (G / NR) & 1);
+          const bool e = mbar_test_wait(empty, ((G / n) & 1) ^ 1), f = mbar_test_wait(r_full(st), (G / NR) & 1);
+          if (!__all_sync(0xffffffffu, e && f))  // (mostly both have)
+            ok = mbar_wait_warp(empty, ((G / n) & 1) ^ 1) && mbar_wait_warp(r_full(st), (G / NR) & 1);
           if (!ok) break;
           const uint8_t* raw = smem + C::OFF_RAW + st * C::RAW;
           const signed char* ex = reinterpret_cast<const signed char*>(smem + C::OFF_EXP + st * PC_T);
