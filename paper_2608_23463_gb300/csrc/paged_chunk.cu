@@ -28,7 +28,7 @@
 // Few tokens on long caches are bound by HBM (up to 8 tokens of each of 8 sequences over 77K rows of
 // 16 heads of 128, 107 us: 5.9 TB/s), a long prompt's chunk by a tile's chain of scores, softmax and sum
 // (2048 tokens on 30000 rows, 16 heads on 2: 340 us, 1.5 PFLOP/s, tensor pipe 67 %), quantised caches by
-// the conversion beside the softmax (up to 5 tokens of each of 32 sequences of 16 heads on 2, 60 us; from
+// the conversion beside the softmax (up to 5 tokens of each of 32 sequences of 16 heads on 2, 58 us; from
 // bf16 pages 54), short calls by instructions that come from L2 (12000 cycles before the first sum).
 #include <algorithm>
 #include <type_traits>
@@ -1163,7 +1163,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
           const uint8_t* raw = smem + C::OFF_RAW + st * C::RAW;
           const signed char* ex = reinterpret_cast<const signed char*>(smem + C::OFF_EXP + st * PC_T);
           uint8_t* tile = smem + (kv ? C::OFF_V : C::OFF_K) + dst * C::TILE;
-          constexpr int TURNS = PC_T / (C::CONV * RPW), U = 2;  // rows of a lane; at a time (all four: 71 us where two take 68)
+          constexpr int TURNS = PC_T / (C::CONV * RPW), U = 2;  // rows of a lane; at a time (all four: 60.4 us where two take 58)
           static_assert(TURNS * C::CONV * RPW == PC_T && TURNS % U == 0, "each row once");
           uint8_t* const o0 = tile + (c / 4) * C::HALF;
           const int p = c % 4 * 2, flip = c / 4;  // (lanes of the second half write their pieces the other way round)
