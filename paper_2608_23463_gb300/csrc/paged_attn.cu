@@ -708,12 +708,12 @@ __global__ void __launch_bounds__(PJ_THREADS, 2) paged_join_kernel(PaArgs a) {
 // A CTA for each (sequence, key head), and no join, where none sees many rows: a CTA
 // streams 43 GB/s, and with a pair or more to each SM that is HBM's rate, while ranges that
 // span several short pairs cost their ends.  In us, whole and in ranges, pages of 16 rows, ragged
-// but for the first two, captured: 1 x 250 rows, 16 heads on 4 of 64: 4.9 and 7.4; 1 x 500: 7.4 and
-// 7.4; 8 x 1000 rows, 8 heads of 128: 15.3 and 11.8; 32 x 1000: 20.0 and 35.5; 256 x 1000: 86 and
-// 114; 300 x 200 rows of one head of 64: 5.4 and 16.  The host knows the table's width, not the
+// but for the first two, captured: 1 x 250 rows, 16 heads on 4 of 64: 4.9 and 7.4; 1 x 500: 7.0 and
+// 7.4; 8 x 1000 rows, 8 heads of 128: 14.5 and 11.4; 32 x 1000: 17.7 and 24.1; 256 x 1000: 84 and
+// 111; 300 x 200 rows of one head of 64: 5.2 and 16.6.  The host knows the table's width, not the
 // lengths: short caches in a table of many pages are read in ranges.  Quantised rows come faster to
-// a CTA (64 x 900 rows, 2 heads of 128: 13.7 and 18.2 us; 16 x 900, 4 of 64: 11.0 and 14.2; 16 x 2000,
-// 8 of 128: 22.9 and 20.1).
+// a CTA (64 x 900 rows, 2 heads of 128: 13.8 and 18.1; 16 x 900, 4 of 64: 11.2 and 14.0; 16 x 2000,
+// 8 of 128: 23.0 and 20.1).
 bool pa_whole(const Paged& c) {
   constexpr long FEW = 384, SOME = 1024, MANY = 2048, SMS = 152;
   const long pairs = (long)c.B * c.KV;
