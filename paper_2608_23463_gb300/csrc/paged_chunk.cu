@@ -244,10 +244,11 @@ __device__ __forceinline__ bool pc_not_finite(const PcArgs& a, int b, int h, int
 // the MMA P = 0 met them.  Token t of the call (row i of sequence b), query head hq of key head h:
 // where the blocks fetched for it (of the item with positions [pf, pl]) hold hidden rows of V that
 // are not finite, it is worked out again from the rows that it sees.  For a converged warp: a
-// key to a lane for the scores, columns for the sums.  Out of line: calls without such rows have
-// none of its registers.
+// key to a lane for the scores, columns for the sums, of which those from c0 to c1 are written.  Out of
+// line: calls without such rows have none of its registers.
 template <int DH, bool Q8>
-__device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, int t, int i, int pf, int pl) {
+__device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, int t, int i, int pf, int pl, int c0 = 0,
+                                       int c1 = DH) {
   const int lane = threadIdx.x & 31, W = a.geo.W, bx = a.box;
   const int lo = W > 0 && i >= W ? i - W + 1 : 0, S = min(a.geo.S, lo);
   const int first = W > 0 && pf >= W ? (pf - W + 1) / bx * bx : 0;
@@ -310,6 +311,7 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
     }
   }
   bf16* o = a.out + t * a.ldo + (long)hq * DH + C * lane;
+  if (C * lane < c0 || C * lane >= c1) return;
 #pragma unroll
   for (int c = 0; c < C; c += 2)
     *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(acc[c] / l, acc[c + 1] / l);
@@ -1249,16 +1251,38 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
 
 // Items that lie on several CTAs: the pieces joined in the order of the CTAs.  CTA x takes the item
 // that begins on CTA x and ends on a later one; CTAs y take 32 of its rows each, a lane to a row and
-// the columns four by four to the warps.
+// the columns four by four to the warps, U such groups each, N pieces at a time.
+// FEW: a call of few items, each of eight pieces or more: CTA x takes the x-th such item, and CTAs z share
+// its columns out.  (8 tokens on 30000 rows, 16 heads on 2 of 128: 32 us so, 37 otherwise; three short
+// sequences 12.0 and 12.8; 8 x 4 tokens on 2000 rows, 4 heads of 64, more items: 19.2 and 17.1.)
 constexpr int PJ_WARPS = 8;
-template <int DH, bool Q8>
+template <int DH, bool Q8, bool FEW>
 __global__ void __launch_bounds__(32 * PJ_WARPS) paged_chunk_join_kernel(const __grid_constant__ PcArgs a) {
+  constexpr int C4 = DH / 4;  // groups of four columns
+  constexpr int U = FEW ? 1 : C4 / PJ_WARPS, N = FEW ? 8 : 2;
   __shared__ uint32_t again;
   pdl_enter();
-  const int x = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = FEW ? blockIdx.z : 0,
+            c4 = (part * PJ_WARPS + warp) * U;
+  auto same = [](const PcAt& p, const PcAt& m) { return p.b == m.b && p.h == m.h && p.u == m.u; };
+  // whether an item begins on CTA k and ends on a later one
+  auto cut = [&](const PcAt& begin, const PcAt& next) { return next.s > 0 && !(same(begin, next) && begin.s > 0); };
+  int x = blockIdx.x;
+  if (FEW) {
+    int left = x;
+    uint32_t in = 0;
+    int k = -32;
+    do {
+      left -= __popc(in);
+      k += 32;
+      if (k >= a.G) return;
+      in = __ballot_sync(0xffffffffu, k + lane < a.G && cut(a.at[min(k + lane, a.G)], a.at[min(k + lane + 1, a.G)]));
+    } while (left >= __popc(in));
+    for (; left > 0; --left) in &= in - 1;
+    x = k + __ffs(in) - 1;
+  }
   const PcAt m = a.at[x + 1], begin = a.at[x];
-  auto same = [&](const PcAt& p) { return p.b == m.b && p.h == m.h && p.u == m.u; };
-  if (m.s == 0 || (same(begin) && begin.s > 0)) return;
+  if (!cut(begin, m)) return;
   const PcSeq q = pc_seq(a, m.b);
   const PcSpan sp = pc_span(a.geo, q, m.u);
   const int R = 2 * a.geo.tpt, toks = min(q.n - m.u * R, R), g = a.geo.g;
@@ -1273,12 +1297,11 @@ __global__ void __launch_bounds__(32 * PJ_WARPS) paged_chunk_join_kernel(const _
     bool is = k <= a.G;
     if (is) {
       const PcAt p = a.at[k];
-      is = same(p) && p.s > 0;
+      is = same(p, m) && p.s > 0;
     }
     in = __ballot_sync(0xffffffffu, is);
   }
-  const int first = same(begin) ? 0 : 1;  // piece 0 is the last of its CTA's, the others the first
-  constexpr int C4 = DH / 4, U = C4 / PJ_WARPS;  // groups of four columns; of a warp
+  const int first = same(begin, m) ? 0 : 1;  // piece 0 is the last of its CTA's, the others the first
   float4 acc[U] = {};
   float M = -INFINITY, L = 0.f;
 #pragma unroll 1
@@ -1288,44 +1311,55 @@ __global__ void __launch_bounds__(32 * PJ_WARPS) paged_chunk_join_kernel(const _
     const bool holds = kl < n && (kl == 0 || kl == n - 1 || a.at[x + kl + 1].s != a.at[x + kl].s);
     uint32_t pieces = __ballot_sync(0xffffffffu, holds);
     if (!row_in) continue;
-    // two at a time: what is summed so far is brought down to the larger maximum
+    // what is summed so far is brought down to the largest maximum
 #pragma unroll 1
     while (pieces) {
-      float2 y[2];
-      float4 v[2][U];
+      float2 y[N];
+      float4 v[N][U];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
+      for (int e = 0; e < N; ++e) {
         const int k = k0 + __ffs(pieces) - 1;
         y[e] = make_float2(-INFINITY, 0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) v[e][u] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (pieces) {
           const long place = 2l * (x + k) + (k == 0 ? first : 0);
-          const float4* p = a.part + (place * C4 + warp * U) * a.piece_rows + rr;
+          const float4* p = a.part + (place * C4 + c4) * a.piece_rows + rr;
           y[e] = a.ml[place * a.piece_rows + rr];
 #pragma unroll
           for (int u = 0; u < U; ++u) v[e][u] = p[u * a.piece_rows];
           pieces &= pieces - 1;
         }
       }
-      const float next = fmaxf(M, fmaxf(y[0].x, y[1].x));
+      float next = M;
+#pragma unroll
+      for (int e = 0; e < N; ++e) next = fmaxf(next, y[e].x);
       auto factor = [&](float m) { return m == next ? 1.f : ex2_approx(m - next); };  // (-inf, no keys at all: 1 of nothing)
-      const float f = factor(M), f0 = factor(y[0].x), f1 = factor(y[1].x);
+      const float f = factor(M);
       M = next;
-      L = fmaf(L, f, fmaf(y[0].y, f0, y[1].y * f1));
+      float fe[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) fe[e] = factor(y[e].x);
+      auto sum = [&](auto of, float before) {  // the last first
+        float t = of(N - 1) * fe[N - 1];
+#pragma unroll
+        for (int e = N - 2; e >= 0; --e) t = fmaf(of(e), fe[e], t);
+        return fmaf(before, f, t);
+      };
+      L = sum([&](int e) { return y[e].y; }, L);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        acc[u].x = fmaf(acc[u].x, f, fmaf(v[0][u].x, f0, v[1][u].x * f1));
-        acc[u].y = fmaf(acc[u].y, f, fmaf(v[0][u].y, f0, v[1][u].y * f1));
-        acc[u].z = fmaf(acc[u].z, f, fmaf(v[0][u].z, f0, v[1][u].z * f1));
-        acc[u].w = fmaf(acc[u].w, f, fmaf(v[0][u].w, f0, v[1][u].w * f1));
+        acc[u].x = sum([&](int e) { return v[e][u].x; }, acc[u].x);
+        acc[u].y = sum([&](int e) { return v[e][u].y; }, acc[u].y);
+        acc[u].z = sum([&](int e) { return v[e][u].z; }, acc[u].z);
+        acc[u].w = sum([&](int e) { return v[e][u].w; }, acc[u].w);
       }
     }
   }
   const int t = q.t0 + m.u * R + tok, hq = m.h * g + rr % PC_T % g;
   if (row_in) {
     const float inv = PcCfg<DH, Q8>::SCALE / L;
-    bf16* o = a.out + t * a.ldo + (long)hq * DH + warp * U * 4;
+    bf16* o = a.out + t * a.ldo + (long)hq * DH + c4 * 4;
     float fin = 0.f;  // zero, but for sums that are not finite
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -1337,17 +1371,19 @@ __global__ void __launch_bounds__(32 * PJ_WARPS) paged_chunk_join_kernel(const _
   }
   __syncthreads();
   uint32_t mask = again;
+  constexpr int COLS = 4 * PJ_WARPS * U;  // of the CTA
   for (int i = 0; mask; ++i, mask &= mask - 1) {
     if (i % PJ_WARPS != warp) continue;
     const int src = __ffs(mask) - 1;
     pc_repair<DH, Q8>(a, m.b, m.h, __shfl_sync(0xffffffffu, hq, src), __shfl_sync(0xffffffffu, t, src),
-                      __shfl_sync(0xffffffffu, sp.pf + tok, src), sp.pf, sp.pl);
+                      __shfl_sync(0xffffffffu, sp.pf + tok, src), sp.pf, sp.pl, part * COLS, (part + 1) * COLS);
   }
 }
 
 struct PcPlan {
   int tpt, G, piece_rows;
   bool split;
+  long items;  // at most
   size_t at, ml, bytes;
 };
 PcPlan pc_plan(const Paged& c, long rows) {
@@ -1359,6 +1395,7 @@ PcPlan pc_plan(const Paged& c, long rows) {
   const long steps = (keys + PC_T - 1) / PC_T, R = 2 * p.tpt;
   // items at most: a pair of each sequence that is not full, and the full ones
   const long items = (std::min<long>(c.B, rows) + rows / R) * c.KV;
+  p.items = items;
   p.split = steps > 1;
   p.G = (int)std::min<long>(PC_CTAS, p.split ? (items > PC_CTAS ? PC_CTAS : items * std::min<long>(steps, PC_CTAS)) : items);
   p.G = std::max(p.G, 1);
@@ -1392,7 +1429,10 @@ cudaError_t pc_launch(const Paged& c, const PcArgs& a, const PcPlan& p, cudaStre
     if (e != cudaSuccess || !p.split) return e;
   }
   LaunchTimer lt("paged_chunk_join", st, 0.0, 8.0 * a.G * p.piece_rows * DH);
-  return launch_kernel(paged_chunk_join_kernel<DH, Q8>, dim3(a.G, p.piece_rows / 32), 32 * PJ_WARPS, 0, st, a);
+  const int y = p.piece_rows / 32, z = DH / 4 / PJ_WARPS;
+  if (8 * p.items <= PC_CTAS && p.items * y * z <= 3 * PC_CTAS)
+    return launch_kernel(paged_chunk_join_kernel<DH, Q8, true>, dim3(p.items, y, z), 32 * PJ_WARPS, 0, st, a);
+  return launch_kernel(paged_chunk_join_kernel<DH, Q8, false>, dim3(a.G, y), 32 * PJ_WARPS, 0, st, a);
 }
 
 }  // namespace

@@ -158,6 +158,27 @@ def test_not_finite_beyond_a_token(quant, before, new, window, sinks):
             t.copy_(s)
 
 
+@pytest.mark.parametrize("dh,before,new", [(128, 0, 200), (64, 0, 100), (128, 3000, 5), (64, 3000, 5), (128, 1000, 300), (64, 6, 20)])
+def test_one_column_not_finite_beyond_a_token(dh, before, new):
+    """A hidden row with an infinity in one column alone: whole items, pieces of few items and of many."""
+    c = make([before + new, 70], 8, 2, dh, 16, 64)
+    r = before + new - 1
+    for col in (0, 37, dh - 1):
+        V = c.V.clone()
+        c.V[int(c.table[0, r // 16]), 1, r % 16, col] = float("inf")
+        start = starts([new, 3])
+        q = rand((new + 3, 8 * dh), 65)
+        out = c.attend(q, start=start)
+        again = c.attend(q, start=start)
+        check()
+        assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+        sees = out[new - 1].view(8, dh)[4:]  # its own token's heads of that key head
+        assert not sees[:, col].isfinite().any() and sees[:, [i for i in range(dh) if i != col]].isfinite().all()
+        compare(c, q, start, torch.where(out.isfinite(), out, torch.zeros_like(out)), [i for i in range(new + 3) if i != new - 1])
+        assert out[[i for i in range(new + 3) if i != new - 1]].isfinite().all()
+        c.V.copy_(V)
+
+
 def test_scores_far_apart():
     """Scores of hundreds (the reference is raised over and over), and all alike."""
     c = make([300, 77], 4, 2, 64, 16, 7)
