@@ -1197,9 +1197,12 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
             } else {
 #pragma unroll
               for (int k = 0; k < U; ++k) {
-                // (of the least exponents 2^(e - PQ_DOWN) is no fp32 number: in two factors)
-                const float f = pq_scale(e[k] == PQ_NAN ? e[k] : max(e[k] - PQ_DOWN, PQ_LOW)), b = pq_shift(f);
-                const uint32_t g = pq_twice(min(e[k] - PQ_DOWN - PQ_LOW, 0));
+                // (of the least exponents 2^(e - PQ_DOWN) is no fp32 number: in two factors.  Rows that hold
+                // nothing yet may have exponents past the largest, whose shift is an infinity: what no token
+                // sees must be finite, or P = 0 makes NaN of it)
+                const int x = min(e[k], PQ_TOP);
+                const float f = pq_scale(x == PQ_NAN ? x : max(x - PQ_DOWN, PQ_LOW)), b = pq_shift(f);
+                const uint32_t g = pq_twice(min(x - PQ_DOWN - PQ_LOW, 0));
                 const float2 ff = make_float2(f, f), bb = make_float2(b, b);
                 put(k, pq_times(pq_values(u[k].x, ff, bb), g), pq_times(pq_values(u[k].y, ff, bb), g),
                     pq_times(pq_values(u[k].z, ff, bb), g), pq_times(pq_values(u[k].w, ff, bb), g));
