@@ -66,3 +66,60 @@ def test_rows_that_hold_nothing(KV, dh, new, before, window, n_sink):
         compare(c, q, start, out)
         compare(c, q[-1:], starts([1]), newest)
         assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("KV,dh", [(2, 128), (4, 64), (1, 64)])
+@pytest.mark.parametrize("new,before", SHAPES)
+def test_exponents_of_values(KV, dh, new, before):
+    """V's rows from the least numbers to the largest, both sides of what the fast conversion takes in one tile, and
+    results that are all small."""
+    c = make([before + new, 200], 8, KV, dh, 64, 93, True)
+    start, q = starts([new, 2]), rand((new + 2, 8 * dh), 94)
+    for low, high in ((-126, 104), (-3, 5), (2, 104), (-126, -110), (-126, -126), (104, 104), (-119, -118)):
+        put_exponents(c.V_exp, 95, low, high)
+        out = c.attend(q, start=start)
+        again = c.attend(q, start=start)
+        check()
+        assert torch.equal(out, again)
+        compare(c, q, start, out)
+
+
+@pytest.mark.parametrize("KV,dh", [(2, 128), (4, 64)])
+@pytest.mark.parametrize("new,before", SHAPES)
+def test_exponents_of_keys(KV, dh, new, before):
+    """K's rows alike.  Queries are as small as the largest keys are large, so that scores lie within some tens."""
+    c = make([before + new, 200], 8, KV, dh, 64, 96, True)
+    start, q0 = starts([new, 2]), rand((new + 2, 8 * dh), 97)
+    for low, high in ((-10, 25), (2, 104), (-126, -120), (-126, 104), (104, 104)):
+        put_exponents(c.K_exp, 98, low, high)
+        # keys are normal numbers of 127 2^high at most: of 2^(high + 5) mostly
+        q = q0 * 2.0 ** (-(high + 5))
+        assert q.isfinite().all() and q.abs().max() > 0
+        out = c.attend(q, start=start)
+        again = c.attend(q, start=start)
+        check()
+        assert torch.equal(out, again)
+        compare(c, q, start, out)
+
+
+@pytest.mark.parametrize("KV,dh", [(2, 128), (4, 64)])
+@pytest.mark.parametrize("new,before", SHAPES)
+def test_not_finite_beside_large_exponents(KV, dh, new, before):
+    """A row that is not finite, of K or of V, among rows of large exponents: who sees it gets NaN, nobody else."""
+    c = make([before + new, 200], 8, KV, dh, 64, 99, True)
+    start, q = starts([new, 2]), rand((new + 2, 8 * dh), 100)
+    put_exponents(c.V_exp, 101, -3, 30)
+    own = torch.arange(new + 2, device="cuda") < new
+    for i in (0, new // 2, new - 1):
+        r = before + i
+        for e in (c.K_exp, c.V_exp):
+            was = e.clone()
+            e[int(c.table[0, r // 64]), KV - 1, r % 64] = -128
+            out = c.attend(q, start=start)
+            check()
+            sees = own & (torch.arange(new + 2, device="cuda") >= i)
+            o, g = out.view(new + 2, 8, dh), 8 // KV
+            assert o[sees][:, -g:].isnan().all()
+            assert o[~sees].isfinite().all() and o[:, :-g].isfinite().all()
+            compare(c, q, start, torch.where(o.isnan(), 0, o).view(new + 2, -1), np.flatnonzero(~sees.cpu().numpy()))
+            e.copy_(was)
