@@ -243,7 +243,8 @@ __device__ __forceinline__ bool pc_not_finite(const PcArgs& a, int b, int h, int
 // A row whose sums are not finite, though what spoilt them may be values that it does not see: in
 // the MMA P = 0 met them.  Token t of the call (row i of sequence b), query head hq of key head h:
 // where the blocks fetched for it (of the item with positions [pf, pl]) hold hidden rows of V that
-// are not finite, it is worked out again from the rows that it sees.  For a converged warp: a
+// are not finite and that another of the item's tokens sees, or that lie before those in a block of
+// the window's first or the sinks' last, it is worked out again from the rows that it sees.  For a converged warp: a
 // key to a lane for the scores, columns for the sums, of which those from c0 to c1 are written.  Out of
 // line: calls without such rows have none of its registers.
 template <int DH, bool Q8>
@@ -253,7 +254,7 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
   const int lo = W > 0 && i >= W ? i - W + 1 : 0, S = min(a.geo.S, lo);
   const int first = W > 0 && pf >= W ? (pf - W + 1) / bx * bx : 0;
   const int held = (int)min(min(((long)a.geo.S + bx - 1) / bx * bx, (long)lo), (long)(pf - pf % bx));
-  if (!pc_not_finite<DH, Q8>(a, b, h, i + 1, (pl / bx + 1) * bx) &&
+  if (!pc_not_finite<DH, Q8>(a, b, h, i + 1, pl + 1) &&
       !(W > 0 && (pc_not_finite<DH, Q8>(a, b, h, max(first, S), lo) || pc_not_finite<DH, Q8>(a, b, h, S, held))))
     return;
   constexpr int C = DH / 32;  // columns of a lane
@@ -742,6 +743,21 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
             continue;
           }
           if (s == first && io > 0 && !wait_warp(o_free(w), (io - 1) & 1)) break;
+          if constexpr (!Q8) {
+            // The item's last step: rows of V behind its last token, which may hold anything, become zeros (P = 0
+            // times what is not finite is NaN), beside the softmax.  Tile B's warp writes the same zeros again,
+            // maybe while tile A's product reads them: neither can see anything else.
+            if (s == m.sp.steps - 1) {
+              const int end = m.sp.pl % PC_T + 1, to = (end + a.box - 1) & -a.box;  // (blocks from there on: zeros)
+#pragma unroll 1
+              for (int i = end * 8 + lane; i < to * 8; i += 32)
+#pragma unroll
+                for (int hf = 0; hf < C::HALVES; ++hf)
+                  *reinterpret_cast<uint4*>(smem + C::OFF_V + st * C::TILE + hf * C::HALF + i * 16) = make_uint4(0, 0, 0, 0);
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+            }
+          }
           constexpr int PARTS = C::ALIAS ? 2 : 1;  // (the first half of the keys while the second half's P is made)
           bool ok = true;
 #pragma unroll
@@ -1154,6 +1170,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
     for (uint32_t it = 0; ok && take(it, m); ++it) {
 #pragma unroll 1
       for (int s = m.s0; s < m.s1 && ok; ++s, ++G) {
+        const int end = s == m.sp.steps - 1 ? m.sp.pl % PC_T + 1 : PC_T;  // rows behind the last token: any finite ones
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv) {
           const uint32_t n = kv ? C::NV : C::NK, st = kv * NR + G % NR, dst = G % n;
@@ -1178,7 +1195,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
             for (int k = 0; k < U; ++k) {
               const int row = ((i + k) * C::CONV + warp - 12) * RPW + sub;
               u[k] = *reinterpret_cast<const uint4*>(raw + row * DH + c * 16);
-              e[k] = ex[row];
+              e[k] = row < end ? ex[row] : 0;
               small &= pq_small(e[k]);
             }
             auto put = [&](int k, uint2 v0, uint2 v1, uint2 v2, uint2 v3) {
