@@ -244,7 +244,8 @@ __device__ __forceinline__ bool pc_not_finite(const PcArgs& a, int b, int h, int
 // the MMA P = 0 met them.  Token t of the call (row i of sequence b), query head hq of key head h:
 // where the blocks fetched for it (of the item with positions [pf, pl]) hold hidden rows of V that
 // are not finite and that another of the item's tokens sees, or that lie before those in a block of
-// the window's first or the sinks' last, it is worked out again from the rows that it sees.  For a converged warp: a
+// the window's first or the sinks' last, it is worked out again from the rows that it sees, the newest first: of a
+// sequence that has turned to NaN those are NaN themselves, and the end of it.  For a converged warp: a
 // key to a lane for the scores, columns for the sums, of which those from c0 to c1 are written.  Out of
 // line: calls without such rows have none of its registers.
 template <int DH, bool Q8>
@@ -262,13 +263,14 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
   const float sl2 = a.sl2 / PcCfg<DH, Q8>::SCALE;
   float acc[C] = {}, m = -INFINITY, l = 0.f;
 #pragma unroll 1
-  for (int part = 0; part < 2; ++part) {  // the sinks before the window, the window
-    const int end = part ? i + 1 : S;
+  for (int part = 0; part < 2; ++part) {  // the window, the sinks before it, newest keys first
+    const int begin = part ? 0 : lo;
 #pragma unroll 1
-    for (int j = part ? lo : 0; j < end; j += 32) {
-      const bool in = j + lane < end;
-      const long pg = in ? pc_page(a, b, j + lane) : -1;
-      const long at = pg < 0 ? -1 : (pg * a.geo.KV + h) * a.page + (j + lane) % a.page;
+    for (int j = part ? S : i + 1; j > begin; j -= 32) {
+      const int key = j - 1 - lane;
+      const bool in = key >= begin;
+      const long pg = in ? pc_page(a, b, key) : -1;
+      const long at = pg < 0 ? -1 : (pg * a.geo.KV + h) * a.page + key % a.page;
       float s = 0.f;  // (a page out of range reads as zero)
       if (at >= 0) {
 #pragma unroll 1
@@ -296,7 +298,7 @@ __device__ __noinline__ void pc_repair(const PcArgs& a, int b, int h, int hq, in
 #pragma unroll
       for (int c = 0; c < C; ++c) acc[c] *= corr;
 #pragma unroll 1
-      for (int k = 0; k < min(32, end - j); ++k) {
+      for (int k = 0; k < min(32, j - begin); ++k) {
         const float pk = __shfl_sync(0xffffffffu, p, k);
         const long ak = __shfl_sync(0xffffffffu, at, k);
         if (ak < 0) continue;
