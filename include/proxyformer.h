@@ -579,9 +579,14 @@ pf_status pf_gemm_bf16(int M, int N, int K, const void *A, int a_mn, const void 
  *     every contraction of the layer) issues none of its operand loads, so its
  *     MMA warp waits for data that never comes and the wait runs out.  Nothing
  *     is in flight when the kernel leaves; the outputs hold garbage.  For tests
- *     of the timeout path only; off by default.                              */
+ *     of the timeout path only; off by default.
+ *   pf_debug_paged_chunk_steps(steps): calls of pf_paged_chunk_attn from then
+ *     on load so many steps (128 rows of a cache) for each CTA and no more, so
+ *     that the waits for the next one run out; negative: as many as there are,
+ *     which is the default.                                                  */
 pf_status pf_debug_set_wait_limit_ns(unsigned long long ns);
 pf_status pf_debug_gemm_skip_loads(int on);
+pf_status pf_debug_paged_chunk_steps(int steps);
 
 /* ---------------------------------------------------------------------------
  * Allocation-free backward.  The paper has no counterpart; this is a calling

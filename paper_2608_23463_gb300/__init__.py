@@ -121,7 +121,8 @@ EXPORTED = ("proxy_layer_check", "proxy_layer_saved_size", "proxy_layer_workspac
             "pf_last_error", "pf_sync_check", "pf_gemm_bf16", "pf_timing_enable",
             "pf_timing_collect", "pf_timing_label", "pf_timing_ms", "pf_timing_launches",
             "pf_timing_flops", "pf_timing_bytes", "proxy_layer_bwd_noalloc",
-            "pf_debug_set_wait_limit_ns", "pf_debug_gemm_skip_loads", "pf_probe_ffma")
+            "pf_debug_set_wait_limit_ns", "pf_debug_gemm_skip_loads", "pf_debug_paged_chunk_steps",
+            "pf_probe_ffma")
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -246,6 +247,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pf_debug_set_wait_limit_ns.restype = ctypes.c_int
     lib.pf_debug_gemm_skip_loads.argtypes = [ctypes.c_int]
     lib.pf_debug_gemm_skip_loads.restype = ctypes.c_int
+    lib.pf_debug_paged_chunk_steps.argtypes = [ctypes.c_int]
+    lib.pf_debug_paged_chunk_steps.restype = ctypes.c_int
     lib.pf_probe_ffma.argtypes = [_vp, ctypes.c_int, ctypes.c_int, _vp]
     lib.pf_probe_ffma.restype = ctypes.c_int
     _lib = lib
@@ -509,6 +512,11 @@ def pf_debug_set_wait_limit_ns(ns: int) -> None:
 def pf_debug_gemm_skip_loads(on: bool) -> None:
     """Test hook: the GEMM kernel issues no operand loads while on."""
     _check(load().pf_debug_gemm_skip_loads(1 if on else 0))
+
+
+def pf_debug_paged_chunk_steps(steps: int) -> None:
+    """Test hook: the chunk attention's CTAs load so many steps and no more (negative: all)."""
+    _check(load().pf_debug_paged_chunk_steps(int(steps)))
 
 
 def pf_probe_ffma(out, blocks: int, iters: int, stream=None) -> None:

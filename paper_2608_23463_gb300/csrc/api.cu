@@ -1952,6 +1952,11 @@ pf_status pf_debug_gemm_skip_loads(int on) {
   return PF_OK;
 }
 
+pf_status pf_debug_paged_chunk_steps(int steps) {
+  set_debug_chunk_steps(steps);
+  return PF_OK;
+}
+
 pf_status pf_gemm_bf16(int M, int N, int K, const void* A, int a_mn, const void* B, int b_mn,
                        float* D, int ldd, void* stream) {
   if (M < 1 || N < 1 || K < 1 || N % 32 != 0 || !A || !B || !D || ldd < N || ldd % 4 != 0)

@@ -114,6 +114,7 @@ cudaError_t paged_read(const Paged& c, long rows, const int* start, bf16* k, lon
 int take_dev_error_paged_chunk();
 int take_dev_error_paged_read();
 int set_wait_limit_paged_chunk(unsigned long long ns);
+void set_debug_chunk_steps(int steps);
 int set_wait_limit_paged_read(unsigned long long ns);
 int take_dev_error_local_rope();
 int take_dev_error_paged_attn();

@@ -13,7 +13,9 @@
 //              by the lane that looked its page up; blocks that no token of the item sees are
 //              asked past the pool's end, which reads as zero
 //   warp 1     MMA issuer of both tiles' scores: S = Q K^T (M=128, N=128)
-//   warps 2-3  MMA issuers of tile A's and tile B's O += P V (M=128, N=dh, K=128), P from TMEM
+//   warps 2-3  MMA issuers of tile A's and tile B's O += P V (M=128, N=dh, K=128), P from TMEM; rows of V
+//              behind an item's last token become zeros before its last product (quantised: finite, by the
+//              warps that convert them)
 //   warps 4-7  softmax of tile A, warps 8-11 of tile B: one row per thread (TMEM lane); the
 //              running maximum moves by more than 2^8 only, which then scales O
 //   warps 12-19 (quantised caches) turn the producer's raw tiles of bytes into the bf16 tiles
@@ -27,10 +29,11 @@
 //
 // Few tokens on long caches are bound by HBM (up to 8 tokens of each of 8 sequences over 77K rows of
 // 16 heads of 128, 107 us: 5.9 TB/s), a long prompt's chunk by a tile's chain of scores, softmax and sum
-// (2048 tokens on 30000 rows, 16 heads on 2: 340 us, 1.5 PFLOP/s, tensor pipe 67 %), quantised caches by
-// the conversion beside the softmax (up to 5 tokens of each of 32 sequences of 16 heads on 2, 58 us; from
-// bf16 pages 54), short calls by instructions that come from L2 (12000 cycles before the first sum).
+// (2048 tokens on 30000 rows, 16 heads on 2: 338 to 364 us by what ran before it, 1.43 to 1.54 PFLOP/s,
+// tensor pipe 67 %), quantised caches by the conversion beside the softmax (up to 5 tokens of each of 32
+// sequences of 16 heads on 2, 58 us; from bf16 pages 54), short calls by instructions that come from L2 (12000 cycles before the first sum).
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "local.h"
@@ -42,6 +45,8 @@ namespace pf {
 static Launched launched;
 int take_dev_error_paged_chunk() { return launched.take(take_dev_error_tu); }
 int set_wait_limit_paged_chunk(unsigned long long ns) { return set_wait_limit_tu(ns); }
+static std::atomic<int> stop_after{-1};
+void set_debug_chunk_steps(int steps) { stop_after.store(steps); }
 
 namespace {
 
@@ -88,6 +93,7 @@ struct PcArgs {
   int G;           // CTAs
   int few;         // weight to a CTA at least
   int long_item;   // steps from which an item's unmasked ones take the long form
+  int stop;        // steps that a CTA's producer loads, for a test
   float sl2;       // log2(e) / sqrt(dh), of the tiles' keys
   const bf16* q;
   bf16* out;
@@ -454,7 +460,9 @@ __device__ __forceinline__ void pc_share_out(const PcArgs& a, void* room, int wa
   }
 }
 
-template <int DH, bool Q8>
+// CUT: for a test of the waits, the producer loads a.stop steps and no more (a kernel of its own: as a branch of the
+// one that serves it cost 0.3 to 1 us of 78)
+template <int DH, bool Q8, bool CUT>
 __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
     paged_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                        const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PcArgs a) {
@@ -560,6 +568,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
       const bool exps = Q8 && sub < 8, data = Q8 ? exps && (sub * 16 & (a.box - 1)) == 0 : sub < nb * H;
       const uint32_t qbytes = (uint32_t)(a.geo.tpt * a.geo.g * 128 * C::HALVES);
       bool ok = wait_warp(shared, 0);
+      int left = a.stop;
       PcWalk walk(a, ends);
       while (ok) {
         PcItem m;
@@ -571,6 +580,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
           mbar_arrive_warp(i_full(i));
         }
         if (m.s1 == 0) break;
+        if (CUT) m.s1 = min(m.s1, m.s0 + left);
         // The lane's block in a step: its row, the row's place in the table, and what stands there, which is
         // looked up a step ahead and not looked at before its turn.  (With divisions, and looked at once, a
         // step took the producer 2200 cycles and all else waited for it: 64 mixed sequences 89 us, 81 so.)
@@ -677,6 +687,7 @@ __global__ void __launch_bounds__(PcCfg<DH, Q8>::THREADS, 1)
           if (!ok) break;
         }
         if (queries) ++q_issued;
+        if (CUT && (left -= m.s1 - m.s0) == 0) break;
       }
     } else if (warp == 1) {
       // ------------------------------------------------------------ MMA issuer: scores
@@ -1439,15 +1450,16 @@ cudaError_t pc_launch(const Paged& c, const PcArgs& a, const PcPlan& p, cudaStre
       !tmap_pages(&tk, c.K, Q8, DH, c.page, c.KV, c.n_pages, a.box) ||
       !tmap_pages(&tv, c.V, Q8, DH, c.page, c.KV, c.n_pages, a.box))
     return cudaErrorInvalidValue;
-  static KernelOnce once;
-  cudaError_t e = once(reinterpret_cast<const void*>(paged_chunk_kernel<DH, Q8>), C::SMEM, C::THREADS, C::POOL);
+  static KernelOnce once[2];
+  const auto kern = a.stop < 0 ? paged_chunk_kernel<DH, Q8, false> : paged_chunk_kernel<DH, Q8, true>;
+  cudaError_t e = once[a.stop >= 0](reinterpret_cast<const void*>(kern), C::SMEM, C::THREADS, C::POOL);
   if (e != cudaSuccess) return e;
   // work: upper bound (every cache full, all rows of the longest)
   const double keys = (double)std::min<long>((long)c.max_pages * c.page, 0x7fffffffL);
   {
     LaunchTimer lt("paged_chunk", st, 4.0 * a.rows * c.H * DH * keys,
                    (double)c.B * c.KV * keys * DH * (Q8 ? 2.0 : 4.0) + 4.0 * a.rows * c.H * DH);
-    e = launch_kernel(paged_chunk_kernel<DH, Q8>, a.G, C::THREADS, C::SMEM, st, tq, tk, tv, a);
+    e = launch_kernel(kern, a.G, C::THREADS, C::SMEM, st, tq, tk, tv, a);
     if (e != cudaSuccess || !p.split) return e;
   }
   LaunchTimer lt("paged_chunk_join", st, 0.0, 8.0 * a.G * p.piece_rows * DH);
@@ -1484,6 +1496,7 @@ cudaError_t paged_chunk(const Paged& c, long rows, const bf16* q, long ldq, cons
   // of up to 1000 tokens, 16 heads on 8 of 64, 55.5 us so, 57.2 with all items' in the long one.
   a.few = 400;
   a.long_item = 8;
+  a.stop = stop_after.load(std::memory_order_relaxed);
   a.sl2 = (c.Ke ? 1 << PQ_DOWN : 1) * 1.4426950408889634f / sqrtf((float)c.dh);
   a.q = q; a.ldq = ldq;
   a.out = out; a.ldo = ldo;
