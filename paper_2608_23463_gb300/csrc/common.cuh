@@ -67,7 +67,8 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) {
 // access to global memory, until they are visible.  This takes a dependent
 // launch from about 6.5 us of a stream to 4.5 (a step of 36 small kernels 247
 // -> 175 us; the 262144-token layer, whose 33 launches lie under the power
-// cap, 3430 -> 3347 us).  No kernel but paged_attn_kernel, which small ones follow,
+// cap, 3430 -> 3347 us).  No kernel but paged_attn_kernel, which small ones follow, and
+// paged_chunk_kernel where a join follows, which waits for that grid's end before it reads a piece,
 // lets its successor start any earlier (griddepcontrol.launch_dependents): CTAs that arrive while others still run
 // pack onto the SMs that are free first, and a grid of one CTA per SM then
 // shares some SMs and leaves others idle (fp32 layer 61.7 us so, 69.3 with

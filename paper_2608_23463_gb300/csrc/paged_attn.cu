@@ -29,7 +29,9 @@
 // CTAs, so that results repeat bit for bit.
 //
 // Quantised rows are read as they lie, 16 bytes a chunk: their whole numbers become bf16 in
-// registers, and the powers of two go into the scores and into P, where they are exact.  What
+// registers, and the powers of two go into the scores and into P, where they are exact while
+// p 2^(e + 7) is a normal number; below that P is off by 2^-134 at most, 2^-15 of what the least
+// row of V (e = -126) counts for with p = 1.  What
 // takes the time there is their instructions, not HBM: so keys are the MMAs' rows and the query
 // heads their 8 columns (or twice 8), half the MMAs, sums and exponentials of the form above, and
 // the same for O^T = V^T P^T.  A transposing load hands a thread two columns of V for two keys: the
@@ -722,7 +724,7 @@ bool pa_whole(const Paged& c) {
   return rows <= (pairs >= SMS ? MANY : c.Ke && pairs >= 64 ? SOME : FEW);
 }
 
-// CTAs: two an SM, or a unit each.
+// CTAs: two an SM (quantised rows: three), or a unit each.
 int pa_grid(const Paged& c, bool q8) {
   const long rows = std::min<long>((long)c.max_pages * c.page, 0x7fffffffL);
   const long units = (rows + PA_UNIT - 1) / PA_UNIT * c.B * c.KV;
