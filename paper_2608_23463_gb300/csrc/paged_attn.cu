@@ -613,12 +613,13 @@ __global__ void __launch_bounds__(PA_THREADS, Q8 ? 3 : 1) paged_attn_kernel(PaAr
 // Rows whose pair lies on several CTAs: the pieces joined in the order of the
 // CTAs.  CTA x takes pair x, or, with more pairs than CTAs, the pair that
 // begins on CTA x and ends on a later one; CTAs y share its columns, 32 at a
-// time, 16 threads to a column.  Where that leaves a CTA several turns and the pieces are few,
-// a thread takes a column and a warp a turn: the same sums in the same order.  With two CTAs an SM
+// time, 16 threads to a column.  Where that leaves a CTA several turns (TURNS; a kernel of its own, as the rest
+// of a call's instructions comes from L2: one token over 600 rows, 16 heads of 64, two sequences, 8.5 us, 8.7 in one
+// for both) and the pieces are few, a thread takes a column and a warp a turn: the same sums in the same order.  With two CTAs an SM
 // (eight before: most of their time is their beginning) attention and join of 64 x 900 quantised
 // rows, 16 heads on 2 of 128, take 18 us, 44 before; of 64 x 4000, 16 on 8, 96 and 120.
 constexpr int PJ_THREADS = 512, PJ_FEW = 16;
-template <int DH>
+template <int DH, bool TURNS>
 __global__ void __launch_bounds__(PJ_THREADS, 2) paged_join_kernel(PaArgs a) {
   __shared__ int pre[PA_MAX_B + 1];
   __shared__ float sw[PA_CTAS_Q8];
@@ -653,7 +654,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 2) paged_join_kernel(PaArgs a) {
   const int n = c1 - c0 + 1;
   const float* ml = a.part + 2L * a.G * a.g * DH;
   auto slot = [&](int i) { return 2L * (c0 + i) + (i == 0 && pa_first(T, G, c0) != u0 ? 1 : 0); };
-  if (n <= PJ_FEW && a.g * (DH / 32) > (int)gridDim.y) {
+  if (TURNS && n <= PJ_FEW) {
     const int lane = tid & 31;
     for (int k = blockIdx.y + gridDim.y * (tid >> 5); k < a.g * (DH / 32); k += gridDim.y * (PJ_THREADS / 32)) {
       const int r = k / (DH / 32), d = k % (DH / 32) * 32 + lane;
@@ -747,7 +748,8 @@ cudaError_t pa_launch(const PaArgs& a, bool split, cudaStream_t st) {
   // two CTAs an SM, or as many as there are columns for
   const long pairs = (long)a.B * a.KV;
   const int x = (int)std::min<long>(pairs, a.G), y = std::min(a.g * (DH / 32), (2 * 152 + x - 1) / x);
-  return launch_kernel(paged_join_kernel<DH>, dim3(x, y), PJ_THREADS, 0, st, a);
+  return launch_kernel(a.g * (DH / 32) > y ? paged_join_kernel<DH, true> : paged_join_kernel<DH, false>, dim3(x, y),
+                       PJ_THREADS, 0, st, a);
 }
 
 }  // namespace
