@@ -532,7 +532,11 @@ size_t pf_paged_chunk_workspace_size(const pf_paged_desc *desc, int64_t rows);
  * of a quantised cache, else NULL.  ws: pf_paged_chunk_workspace_size bytes (0:
  * may be NULL); calls that may run at the same time need one each.
  * What a token does not see does not matter to its result, infinities and NaN
- * among it.  A sequence whose tokens are not among the call's rows, or more than
+ * among it: nor to its time, behind the sequence's last row.  Where a row of V that
+ * is not finite is hidden from a token but seen by a later one of the call, or
+ * lies just before its window or behind the sinks, the token's heads are worked
+ * out again one by one, about 1 us to a row that they see (8 bits: 1.6).
+ * A sequence whose tokens are not among the call's rows, or more than
  * its length, or whose length its table or 2^31 - 256 does not hold, is flagged
  * (PF_ERR_CAPACITY via pf_sync_check) and its rows, if they are the call's, become
  * zeros; pages out of range are flagged and read as zeros.  Start and lengths stay
